@@ -483,6 +483,112 @@ int twa_layered_step_adam(twa_ctx* ctx, const twa_layered_basis* lb, const void*
                           const twa_adam* opt, float* beta, float* m, float* v, const float* wbar, float* w,
                           float* c_out, void* sws, size_t sws_bytes);
 
+/* ---- between w and g: the model's operators -------------------------------------------- */
+
+/* A model that trains in the subspace reads its parameters as slices of the flat w that the lift
+ * writes, and its gradients have to become the flat g that the step takes.  The calls below are what
+ * lies between besides matrix products: layer norm, embedding, the log probabilities of the target
+ * tokens, each with its gradient, and the norm of all gradients with clipping into g.
+ *  - Matrices here are row-major: row i starts at data + i * ld elements, ld >= the row's length.
+ *  - Pointers need the alignment of their elements only (a slice of w starts anywhere); workspaces
+ *    16 bytes.  Where pointers and row lengths lie on 16 bytes the kernels use wider accesses.
+ *  - Activations and gradients are float32 or bfloat16 as each call's dtype says.  Sums, means,
+ *    exponentials and norms are float32 or float64; an output is rounded to its type once.
+ *  - Zero rows, tokens or tensors are accepted and give what empty sums give; the pointers of empty
+ *    arrays are not looked at.
+ *  - Outputs must not overlap inputs unless a call says so.
+ *  - All calls only enqueue kernels (and clear workspace) on the context's stream, may be
+ *    captured, and repeat bit for bit on one device model. */
+typedef enum { TWA_I32 = 0, TWA_I64 = 1 } twa_itype; /* type of token numbers */
+
+#define TWA_LAYER_NORM_MAX_COLS (1 << 24)
+#define TWA_EMBEDDING_MAX_TOKENS (1 << 24)
+#define TWA_EMBEDDING_MAX_DIM (1 << 15)
+#define TWA_LOGPROBS_MAX_ROWS (1 << 24)
+#define TWA_LOGPROBS_MAX_VOCAB (1 << 24)
+#define TWA_LOGPROBS_MAX_TOP 32
+#define TWA_MAX_TENSORS 65536
+
+/* y = (x - mean) rstd w + b for every row, mean = sum x / cols, rstd = 1 / sqrt(sum (x - mean)^2 / cols + eps).
+ *  x, y   rows x cols of dtype, row strides ldx, ldy; y may be x (with ldy == ldx).
+ *  w, b   cols elements of w_dtype, or NULL (1 and 0).
+ *  mean, rstd  out: rows floats for the backward call, or NULL. */
+int twa_layer_norm(twa_ctx* ctx, const void* x, int64_t ldx, twa_dtype dtype, const void* w, const void* b,
+                   twa_dtype w_dtype, int64_t rows, int cols, float eps, void* y, int64_t ldy, float* mean,
+                   float* rstd);
+/* With h = (x - mean) rstd and v = dy w:  dx = rstd (v - sum v / cols - h sum(v h) / cols),
+ * dw = sum over rows of dy h,  db = sum over rows of dy.
+ *  dx       rows x cols of dtype; may be dy or x (with the same row stride).
+ *  dw, db   cols elements of g_dtype, or NULL; accumulate = 1 adds to what they hold.
+ *  ws       twa_layer_norm_workspace_bytes(rows, cols); not looked at when dw and db are NULL. */
+int twa_layer_norm_backward(twa_ctx* ctx, const void* dy, int64_t lddy, const void* x, int64_t ldx, twa_dtype dtype,
+                            const void* w, twa_dtype w_dtype, const float* mean, const float* rstd, int64_t rows,
+                            int cols, void* dx, int64_t lddx, void* dw, void* db, twa_dtype g_dtype, int accumulate,
+                            void* ws, size_t ws_bytes);
+size_t twa_layer_norm_workspace_bytes(int64_t rows, int cols);
+
+/* out[t] = scale * table[ids[t]].
+ *  table  vocab x dim of t_dtype;  out  tokens x dim of out_dtype;  ids  tokens numbers of id_type.
+ * Device-side error: TWA_ERR_INVALID_ARG, detail = a position whose id is outside 0 .. vocab-1; its
+ * row of out is zero. */
+int twa_embedding(twa_ctx* ctx, const void* table, int64_t ldt, twa_dtype t_dtype, int vocab, int dim,
+                  const void* ids, twa_itype id_type, int64_t tokens, float scale, void* out, int64_t ldo,
+                  twa_dtype out_dtype);
+/* dtable[v] = scale * sum of dout[t] over the positions t with ids[t] == v, added in the order of t.
+ *  padding_id  an id whose row gets no gradient, or -1.
+ *  dtable      vocab x dim of g_dtype, every row written; accumulate = 1: the sums are added to
+ *              what it holds (a table that the output layer shares), other rows are not touched.
+ *  ws          twa_embedding_workspace_bytes(tokens, vocab, dim).
+ * Device-side error as above; such a position adds nothing. */
+int twa_embedding_backward(twa_ctx* ctx, const void* dout, int64_t ldd, twa_dtype d_dtype, const void* ids,
+                           twa_itype id_type, int64_t tokens, int vocab, int dim, float scale, int64_t padding_id,
+                           void* dtable, int64_t ldg, twa_dtype g_dtype, int accumulate, void* ws, size_t ws_bytes);
+size_t twa_embedding_workspace_bytes(int64_t tokens, int vocab, int dim);
+
+/* For every row z of logits: lse = log sum exp z, logp = z[target] - lse, entropy = lse - sum p z with
+ * p = exp(z - lse), and the `top` most likely tokens with their log probabilities, best first, equal
+ * logits by the lower index.
+ *  targets   rows numbers of t_type; a target equal to ignore_id stands for no token, its logp is 0.
+ *  logp, lse out: rows floats.  entropy  out: rows floats, or NULL.
+ *  top       0 .. TWA_LOGPROBS_MAX_TOP, at most vocab; top_ids, top_logp  out: rows x top.
+ * A logit of -inf has probability 0 and adds nothing to the entropy.  A row of -inf only: lse, logp and
+ * top_logp are -inf, the entropy 0.
+ * Device-side errors: TWA_ERR_NONFINITE, detail = a row with a NaN or +inf; TWA_ERR_INVALID_ARG,
+ * detail = a row whose target is neither ignore_id nor in 0 .. vocab-1 (logp = NaN). */
+int twa_token_logprobs(twa_ctx* ctx, const void* logits, int64_t ld, twa_dtype dtype, int64_t rows, int vocab,
+                       const void* targets, twa_itype t_type, int64_t ignore_id, float* logp, float* lse,
+                       float* entropy, int top, int32_t* top_ids, float* top_logp);
+/* dlogits[j] = d_logp ([j == target] - p[j]) - d_entropy p[j] (log p[j] + entropy), with lse and entropy as the
+ * forward call gave them; rows whose target is ignored have the second part only, rows of -inf only are 0.
+ *  entropy, d_entropy  rows floats, or both NULL.   dlogits  rows x vocab of dtype; may be logits
+ *  (with ldd == ld).  A mean cross entropy over m rows: d_logp = -1/m. */
+int twa_token_logprobs_backward(twa_ctx* ctx, const void* logits, int64_t ld, twa_dtype dtype, int64_t rows,
+                                int vocab, const void* targets, twa_itype t_type, int64_t ignore_id, const float* lse,
+                                const float* entropy, const float* d_logp, const float* d_entropy, void* dlogits,
+                                int64_t ldd);
+
+/* Gradients that lie in `count` contiguous tensors: HOST arrays of their device addresses, element counts
+ * and types (twa_dtype).  At most TWA_MAX_ROWS elements together. */
+typedef struct {
+  void* const* data;
+  const int64_t* sizes;
+  const int32_t* dtypes;
+  int32_t count;
+} twa_tensors;
+/* norm = square root of the sum of all squares.  norm: one float on the device.
+ *  ws  twa_grad_norm_workspace_bytes(count).
+ * The squares are float32 and are added in float64 beyond 16 bytes of elements: elements above 1.8e19 give an infinite norm.
+ * Device-side error: TWA_ERR_NONFINITE where the norm is not finite. */
+int twa_grad_norm(twa_ctx* ctx, const twa_tensors* tensors, float* norm, void* ws, size_t ws_bytes);
+/* The norm, and g = min(1, max_norm / (norm + eps)) times the tensors one after another, the flat gradient
+ * that twa_step takes.  g: sum of the sizes elements of g_dtype. */
+int twa_clip_gather(twa_ctx* ctx, const twa_tensors* tensors, float max_norm, float eps, void* g, twa_dtype g_dtype,
+                    float* norm, void* ws, size_t ws_bytes);
+/* The same factor applied to the tensors in place. */
+int twa_clip_grads(twa_ctx* ctx, const twa_tensors* tensors, float max_norm, float eps, float* norm, void* ws,
+                   size_t ws_bytes);
+size_t twa_grad_norm_workspace_bytes(int count);
+
 /* ---- projection without any allocation ----------------------------------------------- */
 
 /* (No counterpart in the paper: this entry point exists for the way some programs manage

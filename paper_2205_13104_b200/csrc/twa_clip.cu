@@ -1,0 +1,295 @@
+// The norm of all gradients together, and clipping by it.
+//
+//   norm = sqrt(sum over all tensors of g^2),   factor = min(1, max_norm / (norm + eps)),   out = factor g
+//
+// The gradients lie in many tensors of different sizes, addresses and types; the result is the flat vector that a
+// subspace step takes, or the tensors themselves.  One kernel adds the squares, one scales; both are bound by memory, and
+// the gradients are read twice because the factor depends on all of them.  The second kernel walks backwards, so that
+// what the first read last is found in L2.
+//
+// The tensors' addresses travel as kernel arguments (CLIP_TENSORS of them a launch), so a call uploads nothing.  They are
+// cut into chunks of at most CLIP_CHUNK elements; a block takes a run of chunks of equal length in either kernel.
+// Squares are added in float32 over a few elements and in float64 beyond, in a fixed order.
+#include <math.h>
+
+#include "twa_ops.cuh"
+
+namespace {
+
+constexpr int CLIP_TENSORS = 512;       // tensors of one launch
+constexpr int CLIP_CHUNK = 16384;       // elements
+constexpr int CLIP_THREADS = 256;
+constexpr int CLIP_MAX_BLOCKS = 148 * 8;
+constexpr int CLIP_HEAD = 256;          // bytes of the workspace before the partial sums: the factor
+
+struct ClipTable {
+  const void* data[CLIP_TENSORS];
+  long long flat[CLIP_TENSORS];         // where the tensor begins in the flat vector
+  int chunk[CLIP_TENSORS + 1];          // first chunk of each tensor, and the number of chunks
+  unsigned char dtype[CLIP_TENSORS];
+  int count;
+};
+struct ClipSizes {                       // elements of each tensor
+  long long size[CLIP_TENSORS];
+};
+
+// Tensor that chunk q belongs to.
+__device__ __forceinline__ int clip_find(const ClipTable& t, int q) {
+  int lo = 0, hi = t.count - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) / 2;
+    if (t.chunk[mid] <= q) lo = mid;
+    else hi = mid - 1;
+  }
+  return lo;
+}
+
+template <typename T>
+__device__ __forceinline__ double clip_square_sum(const T* p, int n) {
+  constexpr int E = twa_vec<T>;
+  double sum = 0.0;
+  const int skew = static_cast<int>((reinterpret_cast<uintptr_t>(p) & 15) / sizeof(T));
+  const int head = min(n, skew ? E - skew : 0), units = (n - head) / E, tail = head + units * E;
+  if (static_cast<int>(threadIdx.x) < head) {
+    const float v = twa_to_float(p[threadIdx.x]);
+    sum += static_cast<double>(v * v);
+  }
+  if (tail + static_cast<int>(threadIdx.x) < n) {
+    const float v = twa_to_float(p[tail + threadIdx.x]);
+    sum += static_cast<double>(v * v);
+  }
+  constexpr int AHEAD = 4;
+  for (int u0 = threadIdx.x; u0 < units; u0 += AHEAD * CLIP_THREADS) {
+    twa_pack<T, E> q[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k)
+      if (u0 + k * CLIP_THREADS < units) q[k].load(p + head + (u0 + k * CLIP_THREADS) * E);
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      if (u0 + k * CLIP_THREADS >= units) break;
+      float v[E], s = 0.0f;
+      q[k].widen(v);
+#pragma unroll
+      for (int e = 0; e < E; ++e) s += v[e] * v[e];
+      sum += static_cast<double>(s);
+    }
+  }
+  return sum;
+}
+
+__device__ __forceinline__ double clip_block_sum(double v, double* red) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
+  __syncthreads();
+  v = 0.0;
+  for (int k = 0; k < CLIP_THREADS / 32; ++k) v += red[k];
+  __syncthreads();
+  return v;
+}
+
+// Partial sums of this launch's tensors to part[base + block]; the last block of the last launch adds all `total` of them.
+__global__ void __launch_bounds__(CLIP_THREADS) clip_norm_kernel(const __grid_constant__ ClipTable t,
+                                                                 const __grid_constant__ ClipSizes z, double* part, int base,
+                                                                 int total, unsigned* ticket, float max_norm, float eps,
+                                                                 float* norm_out, float* factor, int* status) {
+  __shared__ double red[CLIP_THREADS / 32];
+  __shared__ unsigned last;
+  const int chunks = t.chunk[t.count];
+  const int from = static_cast<int>(static_cast<long long>(chunks) * blockIdx.x / gridDim.x);
+  const int to = static_cast<int>(static_cast<long long>(chunks) * (blockIdx.x + 1) / gridDim.x);
+  double sum = 0.0;
+  int i = from < to ? clip_find(t, from) : 0;
+  for (int q = from; q < to; ++q) {
+    while (t.chunk[i + 1] <= q) ++i;
+    const long long off = static_cast<long long>(q - t.chunk[i]) * CLIP_CHUNK;
+    const int n = static_cast<int>(min(static_cast<long long>(CLIP_CHUNK), z.size[i] - off));
+    sum += t.dtype[i] == TWA_BF16 ? clip_square_sum(static_cast<const bf16*>(t.data[i]) + off, n)
+                                  : clip_square_sum(static_cast<const float*>(t.data[i]) + off, n);
+  }
+  sum = clip_block_sum(sum, red);
+  if (threadIdx.x == 0) part[base + blockIdx.x] = sum;
+  if (total == 0) return;
+  __threadfence();
+  if (threadIdx.x == 0) last = atomicAdd(ticket, 1u);
+  __syncthreads();
+  if (last != gridDim.x - 1) return;
+  __threadfence();
+  double all = 0.0;
+  for (int k = threadIdx.x; k < total; k += CLIP_THREADS) all += __ldcg(part + k);
+  all = clip_block_sum(all, red);
+  if (threadIdx.x == 0) {
+    *ticket = 0;
+    const double norm = sqrt(all);
+    *norm_out = static_cast<float>(norm);
+    const double f = static_cast<double>(max_norm) / (norm + static_cast<double>(eps));
+    if (factor) *factor = static_cast<float>(f >= 1.0 ? 1.0 : f);      // a norm that is no number gives none
+    if (!isfinite(norm)) twa_set_status(status, TWA_ERR_NONFINITE, -1);
+  }
+}
+
+template <typename T, typename TO>
+__device__ __forceinline__ void clip_scale(const T* p, TO* o, int n, float f) {
+  constexpr int E = 8;
+  if (((reinterpret_cast<uintptr_t>(p) | reinterpret_cast<uintptr_t>(o)) & 15) == 0) {
+    const int units = n / E;
+    for (int u = threadIdx.x; u < units; u += CLIP_THREADS) {
+      float v[E];
+#pragma unroll
+      for (int k = 0; k < E; k += twa_vec<T>) {
+        twa_pack<T, twa_vec<T>> q;
+        q.load(p + u * E + k);
+        q.widen(v + k);
+      }
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[e] *= f;
+#pragma unroll
+      for (int k = 0; k < E; k += twa_vec<TO>) twa_pack<TO, twa_vec<TO>>::store(o + u * E + k, v + k);
+    }
+    const int j = units * E + threadIdx.x;
+    if (j < n) o[j] = twa_from_float<TO>(twa_to_float(p[j]) * f);
+  } else {
+    for (int j = threadIdx.x; j < n; j += CLIP_THREADS) o[j] = twa_from_float<TO>(twa_to_float(p[j]) * f);
+  }
+}
+
+// out == null: in place.
+__global__ void __launch_bounds__(CLIP_THREADS) clip_scale_kernel(const __grid_constant__ ClipTable t,
+                                                                  const __grid_constant__ ClipSizes z,
+                                                                  const float* __restrict__ factor, void* out, int out_dtype) {
+  const float f = __ldg(factor);
+  if (!out && f == 1.0f) return;
+  const int chunks = t.chunk[t.count], block = gridDim.x - 1 - blockIdx.x;
+  const int from = static_cast<int>(static_cast<long long>(chunks) * block / gridDim.x);
+  const int to = static_cast<int>(static_cast<long long>(chunks) * (block + 1) / gridDim.x);
+  int i = from < to ? clip_find(t, to - 1) : 0;
+  for (int q = to - 1; q >= from; --q) {
+    while (t.chunk[i] > q) --i;
+    const long long off = static_cast<long long>(q - t.chunk[i]) * CLIP_CHUNK;
+    const int n = static_cast<int>(min(static_cast<long long>(CLIP_CHUNK), z.size[i] - off));
+    const long long at = t.flat[i] + off;
+    if (t.dtype[i] == TWA_BF16) {
+      bf16* p = static_cast<bf16*>(const_cast<void*>(t.data[i])) + off;
+      if (!out) clip_scale(p, p, n, f);
+      else if (out_dtype == TWA_BF16) clip_scale(p, static_cast<bf16*>(out) + at, n, f);
+      else clip_scale(p, static_cast<float*>(out) + at, n, f);
+    } else {
+      float* p = static_cast<float*>(const_cast<void*>(t.data[i])) + off;
+      if (!out) clip_scale(p, p, n, f);
+      else if (out_dtype == TWA_BF16) clip_scale(p, static_cast<bf16*>(out) + at, n, f);
+      else clip_scale(p, static_cast<float*>(out) + at, n, f);
+    }
+  }
+}
+
+int clip_check(const twa_ctx* ctx, const twa_tensors* t) {
+  if (!ctx || !t || t->count < 0 || (t->count && (!t->data || !t->sizes || !t->dtypes))) return TWA_ERR_INVALID_ARG;
+  if (t->count > TWA_MAX_TENSORS) return TWA_ERR_UNSUPPORTED;
+  long long total = 0;
+  for (int i = 0; i < t->count; ++i) {
+    if (t->sizes[i] < 0 || !twa_dtype_ok(t->dtypes[i]) || (t->sizes[i] && !t->data[i])) return TWA_ERR_INVALID_ARG;
+    if (t->sizes[i] > TWA_MAX_ROWS || (total += t->sizes[i]) > TWA_MAX_ROWS) return TWA_ERR_UNSUPPORTED;
+    if (twa_misaligned_to(t->data[i], twa_dtype_size(t->dtypes[i]))) return TWA_ERR_MISALIGNED;
+  }
+  return TWA_OK;
+}
+
+// Fills the table of one launch from tensor `first` on; returns the first tensor that is not in it.
+int clip_fill(const twa_tensors* s, int first, long long* flat, ClipTable* t, ClipSizes* z) {
+  int i = first;
+  t->count = 0;
+  t->chunk[0] = 0;
+  for (; i < s->count && t->count < CLIP_TENSORS; ++i) {
+    const long long n = s->sizes[i];
+    if (n) {
+      const int k = t->count++;
+      t->data[k] = s->data[i];
+      t->flat[k] = *flat;
+      t->dtype[k] = static_cast<unsigned char>(s->dtypes[i]);
+      z->size[k] = n;
+      t->chunk[k + 1] = t->chunk[k] + static_cast<int>(twa_ceil_div(n, CLIP_CHUNK));
+    }
+    *flat += n;
+  }
+  return i;
+}
+
+int clip_blocks(const twa_ctx* ctx, int chunks) {
+  int most = 8 * ctx->sm_count;
+  if (most > CLIP_MAX_BLOCKS) most = CLIP_MAX_BLOCKS;
+  return chunks < 1 ? 1 : (chunks < most ? chunks : most);
+}
+
+int clip_run(twa_ctx* ctx, const twa_tensors* s, float max_norm, float eps, bool scale, void* out, int out_dtype, float* norm,
+             void* ws, size_t ws_bytes) {
+  if (!ws || ws_bytes < twa_grad_norm_workspace_bytes(s->count)) return TWA_ERR_WORKSPACE;
+  if (twa_misaligned_to(ws, 16)) return TWA_ERR_MISALIGNED;
+  TWA_CUDA_OK(ctx, cudaSetDevice(ctx->device));
+  float* factor = static_cast<float*>(ws);
+  double* part = reinterpret_cast<double*>(static_cast<char*>(ws) + CLIP_HEAD);
+  ClipTable t;
+  ClipSizes z;
+  int base = 0, next = 0;
+  long long flat = 0;
+  do {
+    next = clip_fill(s, next, &flat, &t, &z);
+    const int blocks = clip_blocks(ctx, t.chunk[t.count]);
+    const bool end = next >= s->count;
+    clip_norm_kernel<<<blocks, CLIP_THREADS, 0, ctx->stream>>>(t, z, part, base, end ? base + blocks : 0, ctx->d_ticket, max_norm,
+                                                               eps, norm, scale ? factor : nullptr, ctx->d_status);
+    base += blocks;
+  } while (next < s->count);
+  TWA_CUDA_OK(ctx, cudaGetLastError());
+  if (!scale) return TWA_OK;
+  // last launch first; its table is still filled when there was one launch only
+  const int launches = s->count > CLIP_TENSORS ? 2 : 1;
+  if (launches == 1) {
+    clip_scale_kernel<<<clip_blocks(ctx, t.chunk[t.count]), CLIP_THREADS, 0, ctx->stream>>>(t, z, factor, out, out_dtype);
+  } else {
+    next = 0;
+    flat = 0;
+    while (next < s->count) {
+      next = clip_fill(s, next, &flat, &t, &z);
+      clip_scale_kernel<<<clip_blocks(ctx, t.chunk[t.count]), CLIP_THREADS, 0, ctx->stream>>>(t, z, factor, out, out_dtype);
+    }
+  }
+  TWA_CUDA_OK(ctx, cudaGetLastError());
+  return TWA_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t twa_grad_norm_workspace_bytes(int count) {
+  if (count < 0 || count > TWA_MAX_TENSORS) return 0;
+  const long long launches = count ? twa_ceil_div(count, CLIP_TENSORS) : 1;
+  return CLIP_HEAD + sizeof(double) * CLIP_MAX_BLOCKS * launches;
+}
+
+int twa_grad_norm(twa_ctx* ctx, const twa_tensors* tensors, float* norm, void* ws, size_t ws_bytes) {
+  int rc = clip_check(ctx, tensors);
+  if (rc) return rc;
+  if (!norm) return TWA_ERR_INVALID_ARG;
+  if (twa_misaligned_to(norm, 4)) return TWA_ERR_MISALIGNED;
+  return clip_run(ctx, tensors, 1.0f, 0.0f, false, nullptr, TWA_F32, norm, ws, ws_bytes);
+}
+
+int twa_clip_gather(twa_ctx* ctx, const twa_tensors* tensors, float max_norm, float eps, void* g, twa_dtype g_dtype, float* norm,
+                    void* ws, size_t ws_bytes) {
+  int rc = clip_check(ctx, tensors);
+  if (rc) return rc;
+  if (!norm || !g || !twa_dtype_ok(g_dtype) || !(max_norm > 0.0f) || !(eps >= 0.0f)) return TWA_ERR_INVALID_ARG;
+  if (twa_misaligned_to(norm, 4) || twa_misaligned_to(g, twa_dtype_size(g_dtype))) return TWA_ERR_MISALIGNED;
+  return clip_run(ctx, tensors, max_norm, eps, true, g, g_dtype, norm, ws, ws_bytes);
+}
+
+int twa_clip_grads(twa_ctx* ctx, const twa_tensors* tensors, float max_norm, float eps, float* norm, void* ws, size_t ws_bytes) {
+  int rc = clip_check(ctx, tensors);
+  if (rc) return rc;
+  if (!norm || !(max_norm > 0.0f) || !(eps >= 0.0f)) return TWA_ERR_INVALID_ARG;
+  if (twa_misaligned_to(norm, 4)) return TWA_ERR_MISALIGNED;
+  return clip_run(ctx, tensors, max_norm, eps, true, nullptr, TWA_F32, norm, ws, ws_bytes);
+}
+
+}  // extern "C"

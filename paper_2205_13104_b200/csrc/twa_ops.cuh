@@ -1,0 +1,97 @@
+// Shared by the model-side operators (layer norm, embedding, token log probabilities, clipping): element
+// loads and stores of the two types, sums over a warp and a block, argument checks.  sm_100a only.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <stdio.h>
+
+#include "twa_common.cuh"
+
+inline bool twa_dtype_ok(int t) { return t == TWA_F32 || t == TWA_BF16; }
+inline bool twa_itype_ok(int t) { return t == TWA_I32 || t == TWA_I64; }
+inline size_t twa_dtype_size(int t) { return t == TWA_BF16 ? 2 : 4; }
+inline size_t twa_itype_size(int t) { return t == TWA_I64 ? 8 : 4; }
+// A pointer to elements of `size` bytes that is not on an element boundary.
+inline bool twa_misaligned_to(const void* p, size_t size) { return (reinterpret_cast<uintptr_t>(p) & (size - 1)) != 0; }
+inline long long twa_ceil_div(long long a, long long b) { return (a + b - 1) / b; }
+inline size_t twa_round256(size_t b) { return (b + 255) & ~static_cast<size_t>(255); }
+
+typedef __nv_bfloat16 bf16;
+
+__device__ __forceinline__ float twa_to_float(float v) { return v; }
+__device__ __forceinline__ float twa_to_float(bf16 v) { return __bfloat162float(v); }
+// One rounding, to nearest even.
+template <typename T>
+__device__ __forceinline__ T twa_from_float(float v);
+template <>
+__device__ __forceinline__ float twa_from_float<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ bf16 twa_from_float<bf16>(float v) { return __float2bfloat16_rn(v); }
+
+// Element i of an array whose type is known at run time.
+__device__ __forceinline__ float twa_load_any(const void* p, int dtype, long long i) {
+  return dtype == TWA_BF16 ? twa_to_float(static_cast<const bf16*>(p)[i]) : static_cast<const float*>(p)[i];
+}
+__device__ __forceinline__ void twa_store_any(void* p, int dtype, long long i, float v) {
+  if (dtype == TWA_BF16) static_cast<bf16*>(p)[i] = twa_from_float<bf16>(v);
+  else static_cast<float*>(p)[i] = v;
+}
+__device__ __forceinline__ long long twa_load_id(const void* p, int itype, long long i) {
+  return itype == TWA_I64 ? static_cast<const long long*>(p)[i] : static_cast<long long>(static_cast<const int*>(p)[i]);
+}
+
+// E consecutive elements as they lie in memory: E = 1, or 16 bytes (E = 4 float, 8 bfloat16; the address on 16
+// bytes).  Loading and widening are apart so that the loads of the next row can be under way while this one is worked on.
+template <typename T, int E>
+struct twa_pack;
+template <>
+struct twa_pack<float, 1> {
+  float r;
+  __device__ __forceinline__ void load(const float* p) { r = __ldg(p); }
+  __device__ __forceinline__ void widen(float* v) const { v[0] = r; }
+  static __device__ __forceinline__ void store(float* p, const float* v) { *p = v[0]; }
+};
+template <>
+struct twa_pack<bf16, 1> {
+  unsigned short r;
+  __device__ __forceinline__ void load(const bf16* p) { r = __ldg(reinterpret_cast<const unsigned short*>(p)); }
+  __device__ __forceinline__ void widen(float* v) const { v[0] = __uint_as_float(static_cast<uint32_t>(r) << 16); }
+  static __device__ __forceinline__ void store(bf16* p, const float* v) { *p = twa_from_float<bf16>(v[0]); }
+};
+template <>
+struct twa_pack<float, 4> {
+  float4 r;
+  __device__ __forceinline__ void load(const float* p) { r = __ldg(reinterpret_cast<const float4*>(p)); }
+  __device__ __forceinline__ void widen(float* v) const { v[0] = r.x; v[1] = r.y; v[2] = r.z; v[3] = r.w; }
+  static __device__ __forceinline__ void store(float* p, const float* v) {
+    *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+  }
+};
+__device__ __forceinline__ uint32_t twa_bf16_pair(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+template <>
+struct twa_pack<bf16, 8> {
+  uint4 r;
+  __device__ __forceinline__ void load(const bf16* p) { r = __ldg(reinterpret_cast<const uint4*>(p)); }
+  __device__ __forceinline__ void widen(float* v) const {
+    v[0] = twa_bf16_lo(r.x); v[1] = twa_bf16_hi(r.x); v[2] = twa_bf16_lo(r.y); v[3] = twa_bf16_hi(r.y);
+    v[4] = twa_bf16_lo(r.z); v[5] = twa_bf16_hi(r.z); v[6] = twa_bf16_lo(r.w); v[7] = twa_bf16_hi(r.w);
+  }
+  static __device__ __forceinline__ void store(bf16* p, const float* v) {
+    uint4 o;
+    o.x = twa_bf16_pair(v[0], v[1]); o.y = twa_bf16_pair(v[2], v[3]);
+    o.z = twa_bf16_pair(v[4], v[5]); o.w = twa_bf16_pair(v[6], v[7]);
+    *reinterpret_cast<uint4*>(p) = o;
+  }
+};
+template <typename T>
+constexpr int twa_vec = 16 / sizeof(T);   // elements of one 16-byte access
+
+__device__ __forceinline__ float twa_warp_sum(float v) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}

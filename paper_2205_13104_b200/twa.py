@@ -17,7 +17,7 @@ _ROOT = os.path.dirname(_HERE)
 LIB_PATH = os.path.join(_HERE, "libtwa.so")
 CSRC = os.path.join(_HERE, "csrc")
 SOURCES = ["twa_api.cu", "twa_basis.cu", "twa_chunked.cu", "twa_layered_build.cu", "twa_layered_step.cu", "twa_project_batch.cu", "twa_panel.cu", "twa_stream.cu",
-           "twa_stream_mma.cu", "twa_noalloc.cu"]
+           "twa_stream_mma.cu", "twa_noalloc.cu", "twa_layer_norm.cu", "twa_embedding.cu", "twa_logprobs.cu", "twa_clip.cu"]
 
 TWA_MAX_N = 128
 TWA_OK = 0
@@ -31,6 +31,10 @@ TWA_ERR_CUDA = -7
 TWA_ERR_WORKSPACE = -8
 TWA_F32 = 0
 TWA_BF16 = 1
+TWA_I32 = 0
+TWA_I64 = 1
+TWA_LOGPROBS_MAX_TOP = 32
+TWA_MAX_TENSORS = 65536
 TWA_TUNE_PROJECT_WARPS = 1
 TWA_TUNE_LIFT_WARPS = 2
 TWA_TUNE_STAGES = 3
@@ -53,6 +57,9 @@ EXPORTS = [
     "twa_layered_build_begin", "twa_layered_build_feed", "twa_layered_build_end_pass",
     "twa_layered_step_workspace_bytes", "twa_layered_project", "twa_layered_lift", "twa_layered_step",
     "twa_project_noalloc", "twa_noalloc_last_error", "twa_noalloc_scratch_bytes",
+    "twa_layer_norm", "twa_layer_norm_backward", "twa_layer_norm_workspace_bytes", "twa_embedding", "twa_embedding_backward",
+    "twa_embedding_workspace_bytes", "twa_token_logprobs", "twa_token_logprobs_backward", "twa_grad_norm", "twa_clip_gather",
+    "twa_clip_grads", "twa_grad_norm_workspace_bytes",
 ]
 
 
@@ -78,6 +85,12 @@ class twa_layered_basis(ctypes.Structure):
                 ("tiles_per_cta", ctypes.c_int32), ("total_runs", ctypes.c_int32),
                 ("cta_first_layer", ctypes.c_void_p), ("cta_run_base", ctypes.c_void_p),
                 ("code_bits", ctypes.c_int32), ("planes", ctypes.c_int32)]
+
+
+class twa_tensors(ctypes.Structure):
+    """Mirror of the C struct twa_tensors."""
+    _fields_ = [("data", ctypes.c_void_p), ("sizes", ctypes.c_void_p), ("dtypes", ctypes.c_void_p),
+                ("count", ctypes.c_int32)]
 
 
 class TwaError(RuntimeError):
@@ -211,6 +224,19 @@ def load():
         "twa_project_noalloc": (i32, [i32, vp, bp, vp, i32, vp, vp]),
         "twa_noalloc_last_error": (ctypes.c_char_p, []),
         "twa_noalloc_scratch_bytes": (szt, []),
+        "twa_layer_norm": (i32, [vp, vp, i64, i32, vp, vp, i32, i64, i32, f32, vp, i64, vp, vp]),
+        "twa_layer_norm_backward": (i32, [vp, vp, i64, vp, i64, i32, vp, i32, vp, vp, i64, i32, vp, i64, vp, vp, i32, i32,
+                                          vp, szt]),
+        "twa_layer_norm_workspace_bytes": (szt, [i64, i32]),
+        "twa_embedding": (i32, [vp, vp, i64, i32, i32, i32, vp, i32, i64, f32, vp, i64, i32]),
+        "twa_embedding_backward": (i32, [vp, vp, i64, i32, vp, i32, i64, i32, i32, f32, i64, vp, i64, i32, i32, vp, szt]),
+        "twa_embedding_workspace_bytes": (szt, [i64, i32, i32]),
+        "twa_token_logprobs": (i32, [vp, vp, i64, i32, i64, i32, vp, i32, i64, vp, vp, vp, i32, vp, vp]),
+        "twa_token_logprobs_backward": (i32, [vp, vp, i64, i32, i64, i32, vp, i32, i64, vp, vp, vp, vp, vp, i64]),
+        "twa_grad_norm": (i32, [vp, ctypes.POINTER(twa_tensors), vp, vp, szt]),
+        "twa_clip_gather": (i32, [vp, ctypes.POINTER(twa_tensors), f32, f32, vp, i32, vp, vp, szt]),
+        "twa_clip_grads": (i32, [vp, ctypes.POINTER(twa_tensors), f32, f32, vp, vp, szt]),
+        "twa_grad_norm_workspace_bytes": (szt, [i32]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -716,3 +742,193 @@ def twa_weighted_average(ctx, W, D, weights, w_out, ws):
                                      _ptr(w_out), _ptr(ws), ws.numel())
     _check(rc, "twa_weighted_average", ctx)
     return w_out
+
+
+# --------------------------------------------------------------------------------------
+# between w and g: the model's operators.  Matrices are two-dimensional tensors whose rows are
+# contiguous (any row stride); parameters may be slices of the flat w.
+# --------------------------------------------------------------------------------------
+_DTYPES = {torch.float32: TWA_F32, torch.bfloat16: TWA_BF16}
+_ITYPES = {torch.int32: TWA_I32, torch.int64: TWA_I64}
+
+
+def _floats(t, what):
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{what}: dtype {t.dtype} not supported (float32 or bfloat16)")
+    return code
+
+
+def _numbers(t, count, what):
+    code = _ITYPES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{what}: dtype {t.dtype} not supported (int32 or int64)")
+    if t.dim() != 1 or t.shape[0] != count or not t.is_contiguous():
+        raise ValueError(f"{what}: a contiguous vector of {count} token numbers is needed, got shape {tuple(t.shape)}")
+    return code
+
+
+def _rows(t, shape, what, dtype=None):
+    """Row stride of a matrix of that shape whose rows are contiguous."""
+    if t.shape != shape or dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{what}: shape {tuple(shape)}{'' if dtype is None else f' of {dtype}'} is needed, "
+                         f"got {tuple(t.shape)} of {t.dtype}")
+    ld, one = t.stride()
+    if one != 1 and shape[1] > 1:
+        raise ValueError(f"{what}: the elements of a row have to be contiguous")
+    return ld if shape[0] > 1 else max(ld, shape[1])
+
+
+def _vector(t, count, dtype, what):
+    if t.dtype != dtype or t.dim() != 1 or t.shape[0] != count or not t.is_contiguous():
+        raise ValueError(f"{what}: a contiguous vector of {count} {dtype} is needed, got {tuple(t.shape)} of {t.dtype}")
+    return t.data_ptr()
+
+
+def _optional(t, count, dtype, what):
+    return None if t is None else _vector(t, count, dtype, what)
+
+
+def twa_layer_norm_workspace_bytes(rows, cols):
+    return int(load().twa_layer_norm_workspace_bytes(int(rows), int(cols)))
+
+
+def twa_layer_norm(ctx, x, weight, bias, eps, y, mean=None, rstd=None):
+    """x, y: (rows, cols); weight, bias: (cols,) of one type, or None; mean, rstd: (rows,) float32, or None."""
+    dt, shape = _floats(x, "x"), x.shape
+    rows, cols = shape
+    p = weight if weight is not None else bias
+    wt = _floats(p, "weight") if p is not None else TWA_F32
+    rc = load().twa_layer_norm(ctx, x.data_ptr(), _rows(x, shape, "x"), dt,
+                               _optional(weight, cols, p.dtype if p is not None else None, "weight"),
+                               _optional(bias, cols, p.dtype if p is not None else None, "bias"), wt, rows, cols, eps,
+                               y.data_ptr(), _rows(y, shape, "y", x.dtype), _optional(mean, rows, torch.float32, "mean"),
+                               _optional(rstd, rows, torch.float32, "rstd"))
+    _check(rc, "twa_layer_norm", ctx)
+    return y
+
+
+def twa_layer_norm_backward(ctx, dy, x, weight, mean, rstd, dx, dw, db, ws, accumulate=False):
+    """dw, db: (cols,) of one type, or None (then ws may be None too when both are)."""
+    dt, shape = _floats(x, "x"), x.shape
+    rows, cols = shape
+    p = dw if dw is not None else db
+    gt = _floats(p, "dw") if p is not None else TWA_F32
+    rc = load().twa_layer_norm_backward(
+        ctx, dy.data_ptr(), _rows(dy, shape, "dy", x.dtype), x.data_ptr(), _rows(x, shape, "x"), dt,
+        _optional(weight, cols, weight.dtype if weight is not None else None, "weight"),
+        _floats(weight, "weight") if weight is not None else TWA_F32, _vector(mean, rows, torch.float32, "mean"),
+        _vector(rstd, rows, torch.float32, "rstd"), rows, cols, dx.data_ptr(), _rows(dx, shape, "dx", x.dtype),
+        _optional(dw, cols, p.dtype if p is not None else None, "dw"),
+        _optional(db, cols, p.dtype if p is not None else None, "db"), gt, 1 if accumulate else 0, _ptr(ws),
+        ws.numel() * ws.element_size() if ws is not None else 0)
+    _check(rc, "twa_layer_norm_backward", ctx)
+    return dx
+
+
+def twa_embedding_workspace_bytes(tokens, vocab, dim):
+    return int(load().twa_embedding_workspace_bytes(int(tokens), int(vocab), int(dim)))
+
+
+def twa_embedding(ctx, table, ids, scale, out):
+    """table: (vocab, dim); ids: (tokens,) int32 or int64; out: (tokens, dim)."""
+    vocab, dim = table.shape
+    tokens = ids.shape[0]
+    rc = load().twa_embedding(ctx, table.data_ptr(), _rows(table, table.shape, "table"), _floats(table, "table"), vocab, dim,
+                              ids.data_ptr(), _numbers(ids, tokens, "ids"), tokens, scale, out.data_ptr(),
+                              _rows(out, (tokens, dim), "out"), _floats(out, "out"))
+    _check(rc, "twa_embedding", ctx)
+    return out
+
+
+def twa_embedding_backward(ctx, dout, ids, scale, dtable, ws, padding_id=-1, accumulate=False):
+    """dout: (tokens, dim); dtable: (vocab, dim)."""
+    vocab, dim = dtable.shape
+    tokens = ids.shape[0]
+    rc = load().twa_embedding_backward(ctx, dout.data_ptr(), _rows(dout, (tokens, dim), "dout"), _floats(dout, "dout"),
+                                       ids.data_ptr(), _numbers(ids, tokens, "ids"), tokens, vocab, dim, scale, padding_id,
+                                       dtable.data_ptr(), _rows(dtable, dtable.shape, "dtable"), _floats(dtable, "dtable"),
+                                       1 if accumulate else 0, ws.data_ptr(), ws.numel() * ws.element_size())
+    _check(rc, "twa_embedding_backward", ctx)
+    return dtable
+
+
+def twa_token_logprobs(ctx, logits, targets, logp, lse, entropy=None, top_ids=None, top_logp=None, ignore_id=-100):
+    """logits: (rows, vocab); targets: (rows,); logp, lse, entropy: (rows,) float32; top_ids: (rows, k) int32 and
+    top_logp: (rows, k) float32, contiguous, or both None."""
+    rows, vocab = logits.shape
+    top = 0
+    if top_ids is not None or top_logp is not None:
+        if top_ids is None or top_logp is None or top_ids.dtype != torch.int32 or top_logp.dtype != torch.float32 or \
+                top_ids.shape != top_logp.shape or top_ids.dim() != 2 or top_ids.shape[0] != rows or \
+                not top_ids.is_contiguous() or not top_logp.is_contiguous():
+            raise ValueError(f"top_ids and top_logp: contiguous ({rows}, k) matrices of int32 and float32 are needed, both or neither")
+        top = top_ids.shape[1]
+    rc = load().twa_token_logprobs(ctx, logits.data_ptr(), _rows(logits, logits.shape, "logits"), _floats(logits, "logits"), rows,
+                                   vocab, targets.data_ptr(), _numbers(targets, rows, "targets"), ignore_id,
+                                   _vector(logp, rows, torch.float32, "logp"), _vector(lse, rows, torch.float32, "lse"),
+                                   _optional(entropy, rows, torch.float32, "entropy"), top, _ptr(top_ids), _ptr(top_logp))
+    _check(rc, "twa_token_logprobs", ctx)
+    return logp
+
+
+def twa_token_logprobs_backward(ctx, logits, targets, lse, d_logp, dlogits, entropy=None, d_entropy=None, ignore_id=-100):
+    """lse, entropy: from the forward call; d_logp, d_entropy: (rows,) float32; dlogits: (rows, vocab) of logits' type, or
+    logits itself."""
+    rows, vocab = shape = logits.shape
+    rc = load().twa_token_logprobs_backward(
+        ctx, logits.data_ptr(), _rows(logits, shape, "logits"), _floats(logits, "logits"), rows, vocab, targets.data_ptr(),
+        _numbers(targets, rows, "targets"), ignore_id, _vector(lse, rows, torch.float32, "lse"),
+        _optional(entropy, rows, torch.float32, "entropy"), _vector(d_logp, rows, torch.float32, "d_logp"),
+        _optional(d_entropy, rows, torch.float32, "d_entropy"), dlogits.data_ptr(),
+        _rows(dlogits, shape, "dlogits", logits.dtype))
+    _check(rc, "twa_token_logprobs_backward", ctx)
+    return dlogits
+
+
+class Tensors:
+    """A twa_tensors descriptor of contiguous float32 or bfloat16 CUDA tensors; keeps them alive.  It holds their
+    addresses: make a new one when a gradient is replaced by another tensor."""
+
+    def __init__(self, tensors):
+        self.tensors = list(tensors)
+        for t in self.tensors:
+            if not t.is_contiguous():
+                raise ValueError("gradients have to be contiguous")
+        n = len(self.tensors)
+        self._data = (ctypes.c_void_p * n)(*[t.data_ptr() for t in self.tensors])
+        self._sizes = (ctypes.c_int64 * n)(*[t.numel() for t in self.tensors])
+        self._dtypes = (ctypes.c_int32 * n)(*[_floats(t, "gradient") for t in self.tensors])
+        self.total = sum(self._sizes)
+        self.desc = twa_tensors(ctypes.addressof(self._data), ctypes.addressof(self._sizes), ctypes.addressof(self._dtypes), n)
+
+
+def twa_grad_norm_workspace_bytes(tensors):
+    """tensors: a Tensors, or the number of tensors."""
+    count = tensors.desc.count if isinstance(tensors, Tensors) else tensors
+    return int(load().twa_grad_norm_workspace_bytes(int(count)))
+
+
+def twa_grad_norm(ctx, tensors, norm, ws):
+    """tensors: a Tensors; norm: (1,) float32."""
+    rc = load().twa_grad_norm(ctx, ctypes.byref(tensors.desc), _vector(norm, 1, torch.float32, "norm"), ws.data_ptr(),
+                              ws.numel() * ws.element_size())
+    _check(rc, "twa_grad_norm", ctx)
+    return norm
+
+
+def twa_clip_gather(ctx, tensors, max_norm, g, norm, ws, eps=1e-6):
+    """g: contiguous, of at least as many elements as the tensors together (a padded flat gradient keeps its tail)."""
+    if g.dim() != 1 or g.numel() < tensors.total or not g.is_contiguous():
+        raise ValueError(f"g: a contiguous vector of at least {tensors.total} elements is needed, got {tuple(g.shape)}")
+    rc = load().twa_clip_gather(ctx, ctypes.byref(tensors.desc), max_norm, eps, g.data_ptr(), _floats(g, "g"),
+                                _vector(norm, 1, torch.float32, "norm"), ws.data_ptr(), ws.numel() * ws.element_size())
+    _check(rc, "twa_clip_gather", ctx)
+    return g
+
+
+def twa_clip_grads(ctx, tensors, max_norm, norm, ws, eps=1e-6):
+    rc = load().twa_clip_grads(ctx, ctypes.byref(tensors.desc), max_norm, eps, _vector(norm, 1, torch.float32, "norm"),
+                               ws.data_ptr(), ws.numel() * ws.element_size())
+    _check(rc, "twa_clip_grads", ctx)
+    return norm

@@ -1,0 +1,35 @@
+"""What of the model's operators runs without a GPU: workspace sizes, refusals before anything is enqueued."""
+
+import ctypes
+
+from paper_2205_13104_b200 import twa
+
+
+def test_workspace_sizes():
+    twa.build_library()
+    assert twa.twa_layer_norm_workspace_bytes(0, 4) >= 2 * 4 * 4
+    assert twa.twa_layer_norm_workspace_bytes(10, 1000) >= 10 * 2 * 1000 * 4
+    assert twa.twa_layer_norm_workspace_bytes(1 << 30, 1000) == twa.twa_layer_norm_workspace_bytes(1 << 20, 1000)
+    assert twa.twa_layer_norm_workspace_bytes(-1, 4) == 0
+    assert twa.twa_embedding_workspace_bytes(1000, 50272, 64) >= 4 * 4 * 1000 + 50272 // 8
+    assert twa.twa_embedding_workspace_bytes(1 << 40, 5, 4) == 0
+    assert twa.twa_grad_norm_workspace_bytes(0) > 0
+    assert twa.twa_grad_norm_workspace_bytes(513) > twa.twa_grad_norm_workspace_bytes(512)
+    assert twa.twa_grad_norm_workspace_bytes(twa.TWA_MAX_TENSORS + 1) == 0
+
+
+def test_calls_without_a_context_are_refused():
+    twa.build_library()
+    lib = twa.load()
+    d = 4096                                   # never looked at
+    bad = twa.TWA_ERR_INVALID_ARG
+    assert lib.twa_layer_norm(None, d, 8, 0, d, d, 0, 4, 8, 1e-5, d, 8, d, d) == bad
+    assert lib.twa_layer_norm_backward(None, d, 8, d, 8, 0, d, 0, d, d, 4, 8, d, 8, d, d, 0, 0, d, 1 << 20) == bad
+    assert lib.twa_embedding(None, d, 8, 0, 5, 8, d, 0, 4, 1.0, d, 8, 0) == bad
+    assert lib.twa_embedding_backward(None, d, 8, 0, d, 0, 4, 5, 8, 1.0, -1, d, 8, 0, 0, d, 1 << 20) == bad
+    assert lib.twa_token_logprobs(None, d, 8, 0, 4, 8, d, 0, -100, d, d, d, 0, None, None) == bad
+    assert lib.twa_token_logprobs_backward(None, d, 8, 0, 4, 8, d, 0, -100, d, None, d, None, d, 8) == bad
+    t = twa.twa_tensors(None, None, None, 0)
+    assert lib.twa_grad_norm(None, ctypes.byref(t), d, d, 1 << 20) == bad
+    assert lib.twa_clip_gather(None, ctypes.byref(t), 1.0, 1e-6, d, 0, d, d, 1 << 20) == bad
+    assert lib.twa_clip_grads(None, ctypes.byref(t), 1.0, 1e-6, d, d, 1 << 20) == bad
