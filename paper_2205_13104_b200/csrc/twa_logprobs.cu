@@ -5,24 +5,45 @@
 //              with m = max z, S = sum exp(z - m), A = sum exp(z - m) (z - m)
 //   backward   dz[j] = d_logp ([j == target] - p[j]) - d_H p[j] (log p[j] + H)
 //
-// Forward is one pass: every thread keeps the running m, S and A of the elements it meets (S and A are rescaled when m
-// grows); the threads' triples are merged at the end.  Exponents are differences to the maximum times log2 e: a mask of
-// the type's lowest value would overflow if the product came first, and far from zero the difference is the more exact.
-// Backward is one read and one write.  Both are bound by memory.
+// Both are bound by memory: forward reads the logits once, backward reads and writes them once.
 //
-// The most likely tokens cost no second pass.  Each thread also remembers in which 16-byte unit of its elements its
-// maximum lay.  Order all elements by (value, smaller unit first): the k-th best of the threads' maxima, T, bounds the
-// k-th best element from below, because the k maxima are k elements; so every one of the k best elements ranks at or
-// above T, and lies in one of the k threads whose maximum does.  Only those threads look at their elements again (in
-// L2), and the few elements that rank at or above T are sorted by (value, smaller index first).
+// Forward: a block streams its rows through a ring of bulk copies.  One warp issues the copies, eight add up, and two
+// finish, even and odd rows in turn: they take the eight warps' results of a row while those are at the next ones, so
+// that neither memory nor the sums wait for the merges, the search and the stores at the end of a row.  Every summing thread keeps the running m, S and A of the elements it meets (S and A are
+// rescaled when m grows); the threads' triples are merged at the end of the row.  The arithmetic has to stay below five
+// instructions an element to keep up with memory in bfloat16: exponents are one packed multiply-add,
+// d = z log2 e - c with c = m log2 e as rounded (the rounding error is known and taken out of S and A at the end), one
+// ex2 each, and packed sums.  -inf would make p d = 0 * -inf: values are raised to -2^126 first (p is 0 there either way).
+// c loses its digits when m is far from zero, so it is held within +-8192 log2 e; a row (or a block's part of one) whose
+// maximum lies beyond is summed once more with differences to that maximum taken first.
+//
+// The most likely tokens cost no second pass.  Each thread also remembers the chunk of the row in which its maximum
+// lay.  Order all elements by (value, earlier chunk first): with T the k-th best of the maxima of 32 groups of threads, k
+// elements rank at T or above, so each of the k best elements does, and lies with a thread whose own maximum does.
+// Only those threads' elements (some 1.5 k threads) are looked at again, in L2, and the few that rank at T or above are
+// sorted by (value, smaller index first).
 #include "twa_ops.cuh"
 
 namespace {
 
-constexpr int LP_THREADS = 512, LP_WARPS = LP_THREADS / 32;
+constexpr int LP_WARPS = 8, LP_THREADS = LP_WARPS * 32;     // threads that add up
+constexpr int LP_COPY = LP_WARPS, LP_FINISH = LP_WARPS + 1; // the warp that issues copies, the first that finishes rows
+constexpr int LP_FINISHERS = 2;
+constexpr int LP_BLOCK = LP_THREADS + 32 * (1 + LP_FINISHERS);
+constexpr int LP_PER_THREAD = 4;                            // 16-byte units of a thread in a chunk
+constexpr int LP_CHUNK = LP_THREADS * LP_PER_THREAD;        // units
+// Without the search three blocks fit an SM's registers, with it two: 146 and 154 us, 180 and 163 us for 8192 x 50272
+// bfloat16 with entropy, without tokens and with 5.
+template <bool TOP>
+constexpr int LP_BLOCKS_PER_SM = TOP ? 2 : 3;
+template <bool TOP>
+constexpr int LP_STAGES = TOP ? 4 : 3;
+constexpr int LP_BUFFER = 128;                              // candidates that are sorted without a further look
 constexpr int LP_MAX_CLUSTER = 8;
-constexpr int LP_BUFFER = LP_THREADS;           // candidates that are sorted at once
+constexpr long long LP_SPLIT_ROWS = 2;                      // blocks an SM up to which rows are split over clusters
+constexpr uint32_t LP_SUSPEND_NS = 20000;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr float LP_FAR = 8192.0f;                           // bound of what exponents are taken against
 typedef unsigned long long u64;
 
 __device__ __forceinline__ float lp_exp2(float x) {
@@ -30,6 +51,68 @@ __device__ __forceinline__ float lp_exp2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
+
+// Pairs of floats, two sums or products an instruction.
+__device__ __forceinline__ u64 lp_pair(float lo, float hi) {
+  u64 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void lp_unpair(u64 v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ u64 lp_fma2(u64 a, u64 b, u64 c) {
+  u64 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ u64 lp_add2(u64 a, u64 b) {
+  u64 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ u64 lp_mul2(u64 a, u64 b) {
+  u64 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
+// The four words of a 16-byte unit: the maximum of the elements of two words, elements raised to -2^126 (NaN stays), a
+// word's elements widened to pairs of floats.
+template <typename T>
+struct LpWord;
+template <>
+struct LpWord<bf16> {
+  static constexpr uint32_t NONE = 0xff80ff80u;              // -inf twice
+  static __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+  }
+  static __device__ __forceinline__ float max1(uint32_t a) { return fmaxf(twa_bf16_lo(a), twa_bf16_hi(a)); }
+  static __device__ __forceinline__ uint32_t raise(uint32_t a) {
+    uint32_t r;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(0xfe80fe80u));
+    return r;
+  }
+  static constexpr int PAIRS = 4;                            // of a unit
+  static __device__ __forceinline__ u64 pair(const uint32_t* w, int i) { return lp_pair(twa_bf16_lo(w[i]), twa_bf16_hi(w[i])); }
+};
+template <>
+struct LpWord<float> {
+  static constexpr uint32_t NONE = 0xff800000u;
+  static __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
+    return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+  }
+  static __device__ __forceinline__ float max1(uint32_t a) { return __uint_as_float(a); }
+  static __device__ __forceinline__ uint32_t raise(uint32_t a) {
+    uint32_t r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(0xfe800000u));
+    return r;
+  }
+  static constexpr int PAIRS = 2;
+  static __device__ __forceinline__ u64 pair(const uint32_t* w, int i) {
+    return lp_pair(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+  }
+};
 
 // Order-preserving bits of a value; zeros of both signs are equal.  0 is below every value, -inf included.
 __device__ __forceinline__ uint32_t lp_rank(float v) {
@@ -41,33 +124,29 @@ __device__ __forceinline__ float lp_unrank(uint32_t r) {
 }
 __device__ __forceinline__ u64 lp_key(float v, uint32_t place) { return static_cast<u64>(lp_rank(v)) << 32 | (0xffffffffu - place); }
 
-// A row as 16-byte units counted from the aligned address at or below its first element; the first and the last
-// unit may be partly outside and are read element by element.
+// A row as 16-byte units counted from the aligned address at or below its first element.  The units that lie wholly in
+// it are first .. first + whole - 1; the elements before and after them (at most E - 1 each) are read one by one.
 template <typename T>
 struct LpRow {
   static constexpr int E = twa_vec<T>;
   const T* base;       // unit 0, element 0 (may lie before the row)
   int skew, cols;      // the row's element j is base[skew + j]
+  int first, whole;
   __device__ __forceinline__ LpRow(const T* row, int n) {
     const uintptr_t a = reinterpret_cast<uintptr_t>(row);
     skew = static_cast<int>((a & 15) / sizeof(T));
     base = reinterpret_cast<const T*>(a & ~static_cast<uintptr_t>(15));
     cols = n;
+    first = skew ? 1 : 0;
+    whole = max(0, (skew + cols) / E - first);
   }
-  __device__ __forceinline__ int units() const { return (skew + cols + E - 1) / E; }
-  __device__ __forceinline__ bool whole(int u) const { return u * E >= skew && (u + 1) * E <= skew + cols; }
-  // Elements outside the row are -inf, and `valid` has their bits clear.
-  __device__ __forceinline__ unsigned load_partial(int u, float* v) const {
-    unsigned valid = 0;
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int j = u * E + e - skew;
-      const bool in = j >= 0 && j < cols;
-      v[e] = in ? twa_to_float(base[u * E + e]) : -INFINITY;
-      valid |= in ? 1u << e : 0u;
-    }
-    return valid;
+  // first of the whole units of part p of 2^log_parts
+  __device__ __forceinline__ int part_from(int p, int log_parts) const {
+    return static_cast<int>(static_cast<unsigned long long>(whole) * p >> log_parts);
   }
+  // elements before the whole units, and after them
+  __device__ __forceinline__ int head() const { return min(cols, first * E - skew); }
+  __device__ __forceinline__ int tail_from() const { return min(cols, (first + whole) * E - skew); }
 };
 
 // Sums of some elements of a row: m = their maximum (-inf: none above -inf), with d = (z - m) log2 e
@@ -75,6 +154,24 @@ struct LpRow {
 struct LpStat {
   float m, s, a;
 };
+// The base of a thread's sums.
+__device__ __forceinline__ float lp_base(float m) { return fminf(fmaxf(m, -LP_FAR), LP_FAR); }
+// Sums relative to lp_base(m) of groups of LANES neighbouring lanes, of the maximum of all 32 in every lane.
+template <bool ENT, int LANES>
+__device__ __forceinline__ LpStat lp_merge_near(const LpStat& x) {
+  LpStat r;
+  r.m = lp_unrank(__reduce_max_sync(0xffffffffu, lp_rank(x.m)));
+  const float d = fmaxf((lp_base(x.m) - lp_base(r.m)) * LOG2E, -150.0f), f = lp_exp2(d);
+  r.s = x.s * f;
+  r.a = ENT ? f * (x.a + d * x.s) : 0.0f;
+#pragma unroll
+  for (int o = LANES / 2; o; o >>= 1) {
+    r.s += __shfl_xor_sync(0xffffffffu, r.s, o);
+    if (ENT) r.a += __shfl_xor_sync(0xffffffffu, r.a, o);
+  }
+  return r;
+}
+// Sums relative to m.
 template <bool ENT>
 __device__ __forceinline__ LpStat lp_merge(const LpStat& x, const LpStat& y) {
   LpStat r;
@@ -88,7 +185,7 @@ __device__ __forceinline__ LpStat lp_merge(const LpStat& x, const LpStat& y) {
   return r;
 }
 
-// ---- the best 32 of a block's keys -------------------------------------------------------------------
+// ---- sorting keys ------------------------------------------------------------------------------------
 __device__ __forceinline__ u64 lp_shfl_xor(u64 v, int o) { return __shfl_xor_sync(0xffffffffu, v, o); }
 
 // Sorts 32 keys of a warp, largest in lane 0 (bitonic network).
@@ -115,17 +212,24 @@ __device__ __forceinline__ u64 lp_merge32(u64 v, u64 other_reversed) {
   }
   return v;
 }
-// The block's 32 best of one key per thread, sorted, in the lanes of warp 0 (other warps: undefined).
-__device__ __forceinline__ u64 lp_block_best(u64 v, u64 (*list)[32]) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  v = lp_sort32(v);
-  for (int half = LP_WARPS / 2; half; half >>= 1) {
-    if (warp >= half && warp < 2 * half) list[warp][lane] = v;
-    __syncthreads();
-    if (warp < half) v = lp_merge32(v, list[warp + half][31 - lane]);
-    __syncthreads();
+// The number of the warp's keys above `v`: its place in descending order, where keys differ.  32 independent comparisons
+// against keys read from shared memory (`row`, the warp's own) take a third of the time of the network's 15 dependent steps.
+__device__ __forceinline__ int lp_place32(u64 v, u64* row) {
+  row[threadIdx.x & 31] = v;
+  __syncwarp();
+  int above = 0;
+#pragma unroll
+  for (int i = 0; i < 32; i += 2) {
+    const ulonglong2 o = *reinterpret_cast<const ulonglong2*>(row + i);
+    above += (o.x > v) + (o.y > v);
   }
-  return v;
+  __syncwarp();
+  return above;
+}
+// Adds one key per lane to a sorted list of the 32 best.
+__device__ __forceinline__ u64 lp_take32(u64 list, u64 key) {
+  if (!__any_sync(0xffffffffu, key > __shfl_sync(0xffffffffu, list, 31))) return list;
+  return lp_merge32(list, __shfl_xor_sync(0xffffffffu, lp_sort32(key), 31));
 }
 
 struct LpArgs {
@@ -138,18 +242,24 @@ struct LpArgs {
   void* dlogits;
   long long ld, ldd, rows, ignore_id;
   int vocab, itype, top;
+  unsigned long long wait_limit_ns;
   int* status;
 };
 
+template <bool TOP>
 struct LpShared {
-  u64 list[LP_WARPS][32];
-  u64 buffer[LP_BUFFER];
-  u64 best[32];                // this block's best, read by the first block of the cluster
-  LpStat stat[LP_WARPS];
-  LpStat mine;                 // this block's sums, read by the first block of the cluster
-  u64 bound;
-  int count;
-  u64 round;
+  uint4 ring[LP_STAGES<TOP>][LP_CHUNK];
+  u64 full[LP_STAGES<TOP>], empty[LP_STAGES<TOP>];        // the ring's stages
+  u64 row_full[LP_FINISHERS], row_empty[LP_FINISHERS];    // a row's results, by the warp that finishes it
+  LpStat stat[LP_FINISHERS][LP_WARPS];
+  u64 key[LP_FINISHERS][LP_THREADS];
+  uint4 hit[LP_FINISHERS][LP_BUFFER];           // units with candidates, candidates
+  alignas(16) u64 buffer[LP_FINISHERS][LP_BUFFER];
+  int hit_unit[LP_FINISHERS][LP_BUFFER];
+  int chosen[LP_FINISHERS][LP_THREADS];
+  u64 best[32];                                 // this block's best, read by the first block of the cluster
+  LpStat mine;                                  // this block's sums, likewise
+  int gave_up;
 };
 
 __device__ __forceinline__ uint32_t lp_cluster_rank() {
@@ -177,178 +287,425 @@ __device__ __forceinline__ V lp_remote(const V* p, uint32_t rank) {
   return v;
 }
 
-// A row per cluster of `parts` blocks; units are dealt to the cluster's threads in turn.
+// By one warp, for rows that are out of the ordinary.  Sums over row[from .. to - 1] with differences to m taken first;
+template <typename T, bool ENT>
+__device__ __noinline__ LpStat lp_sum_far(const T* row, int from, int to, float m) {
+  float s = 0.0f, w = 0.0f;
+  for (int j = from + static_cast<int>(threadIdx.x & 31); j < to; j += 32) {
+    const float d = (twa_to_float(row[j]) - m) * LOG2E, p = lp_exp2(d);
+    s += p;
+    if (ENT) w = fmaf(p, fmaxf(d, -150.0f), w);
+  }
+  return {m, twa_warp_sum(s), ENT ? twa_warp_sum(w) : 0.0f};
+}
+// the best 32 of row[from .. to - 1], sorted.
+template <typename T>
+__device__ __noinline__ u64 lp_best_of_all(const T* row, int from, int to) {
+  u64 list = 0;
+  for (int j0 = from; j0 < to; j0 += 128) {
+    float z[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int j = j0 + i * 32 + static_cast<int>(threadIdx.x & 31);
+      z[i] = j < to ? twa_to_float(row[j]) : 0.0f;
+    }
+#pragma unroll 1
+    for (int i = 0; i < 4; ++i) {
+      const int j = j0 + i * 32 + static_cast<int>(threadIdx.x & 31);
+      list = lp_take32(list, j < to ? lp_key(z[i], j) : 0);
+    }
+  }
+  return list;
+}
+
+// twa_mbar_wait with a hint to suspend the thread: several warps of a block wait most of the time, and ones that poll
+// take issue slots from those that add up.
+__device__ __forceinline__ bool lp_wait(u64* bar, uint32_t parity, volatile int* abort_flag, unsigned long long limit_ns) {
+  const uint32_t at = twa_smem_u32(bar);
+  unsigned long long begun = 0;
+  for (;;) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(at), "r"(parity), "r"(LP_SUSPEND_NS)
+        : "memory");
+    if (ok) return true;
+    if (*abort_flag) return false;
+    const unsigned long long now = twa_globaltimer();
+    if (!begun) begun = now;
+    if (now - begun > limit_ns) {
+      *abort_flag = 1;
+      return false;
+    }
+  }
+}
+
+// Untiled bulk copy into this block's shared memory: addresses and size in multiples of 16 bytes.
+__device__ __forceinline__ void lp_bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
+               "r"(bytes), "r"(bar)
+               : "memory");
+}
+
+// A row per cluster of 2^log_parts blocks, each a run of its units; with one part a block goes on to further rows.
 template <typename T, bool ENT, bool TOP>
-__global__ void __launch_bounds__(LP_THREADS) logprobs_kernel(const LpArgs a, const int parts) {
+__global__ void __launch_bounds__(LP_BLOCK, LP_BLOCKS_PER_SM<TOP>) logprobs_kernel(const LpArgs a, const int log_parts) {
   constexpr int E = twa_vec<T>;
-  __shared__ LpShared sh;
-  const uint32_t part = parts > 1 ? lp_cluster_rank() : 0;
-  const long long row = blockIdx.x / parts;
-  const LpRow<T> x(static_cast<const T*>(a.logits) + row * a.ld, a.vocab);
-  const int units = x.units(), stride = LP_THREADS * parts, first = static_cast<int>(part) * LP_THREADS + threadIdx.x;
+  const int parts = 1 << log_parts;
+  typedef LpWord<T> W;
+  extern __shared__ __align__(128) unsigned char lp_smem[];
+  constexpr int STAGES = LP_STAGES<TOP>;
+  LpShared<TOP>& sh = *reinterpret_cast<LpShared<TOP>*>(lp_smem);
+  const int part = parts > 1 ? static_cast<int>(lp_cluster_rank()) : 0;
+  const long long row0 = blockIdx.x >> log_parts, rows_step = gridDim.x >> log_parts;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-
-  float m = -INFINITY, s = 0.0f, w = 0.0f;
-  int best = first;
-  auto take = [&](const float* v, int u) {
-    float um = v[0];
-#pragma unroll
-    for (int e = 1; e < E; ++e) um = fmaxf(um, v[e]);
-    if (um == -INFINITY) return;
-    if (um > m) {
-      if (m > -INFINITY) {
-        const float d = fmaxf((m - um) * LOG2E, -150.0f), f = lp_exp2(d);
-        if (ENT) w = f * (w + d * s);
-        s *= f;
-      }
-      m = um;
-      best = u;
+  if (threadIdx.x == 0) {
+    for (int q = 0; q < STAGES; ++q) {
+      twa_mbar_init(twa_smem_u32(&sh.full[q]), 1);
+      twa_mbar_init(twa_smem_u32(&sh.empty[q]), LP_WARPS);
     }
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const float d = (v[e] - m) * LOG2E, p = lp_exp2(d);
-      s += p;
-      if (ENT) w = fmaf(p, fmaxf(d, -150.0f), w);
+    for (int q = 0; q < LP_FINISHERS; ++q) {
+      twa_mbar_init(twa_smem_u32(&sh.row_full[q]), LP_WARPS);
+      twa_mbar_init(twa_smem_u32(&sh.row_empty[q]), 1);
     }
-  };
-  constexpr int AHEAD = 4;
-  for (int u0 = first; u0 < units; u0 += AHEAD * stride) {
-    twa_pack<T, E> q[AHEAD];
-#pragma unroll
-    for (int k = 0; k < AHEAD; ++k) {
-      const int u = u0 + k * stride;
-      if (u < units && x.whole(u)) q[k].load(x.base + static_cast<long long>(u) * E);
-    }
-#pragma unroll
-    for (int k = 0; k < AHEAD; ++k) {
-      const int u = u0 + k * stride;
-      if (u >= units) break;
-      float v[E];
-      if (x.whole(u)) q[k].widen(v);
-      else x.load_partial(u, v);
-      take(v, u);
-    }
+    sh.gave_up = 0;
+    twa_fence_barrier_init();
   }
-
-  // the block's sums
-  LpStat st = {m, s, w};
-#pragma unroll
-  for (int o = 16; o; o >>= 1) {
-    LpStat other;
-    other.m = __shfl_xor_sync(0xffffffffu, st.m, o);
-    other.s = __shfl_xor_sync(0xffffffffu, st.s, o);
-    other.a = ENT ? __shfl_xor_sync(0xffffffffu, st.a, o) : 0.0f;
-    st = lp_merge<ENT>(st, other);
-  }
-  if (lane == 0) sh.stat[warp] = st;
-  if (threadIdx.x == 0) sh.count = 0;
   __syncthreads();
-  if (warp == 0) {
-    st = lane < LP_WARPS ? sh.stat[lane] : LpStat{-INFINITY, 0.0f, 0.0f};
-#pragma unroll
-    for (int o = LP_WARPS / 2; o; o >>= 1) {
-      LpStat other;
-      other.m = __shfl_xor_sync(0xffffffffu, st.m, o);
-      other.s = __shfl_xor_sync(0xffffffffu, st.s, o);
-      other.a = ENT ? __shfl_xor_sync(0xffffffffu, st.a, o) : 0.0f;
-      st = lp_merge<ENT>(st, other);
+  const T* logits = static_cast<const T*>(a.logits);
+
+  if (warp == LP_COPY) {
+    // ---- copies: every chunk of every row of this block, as the ring has room
+    if (lane == 0) {
+      int it = 0;
+      bool good = true;
+      for (long long row = row0; row < a.rows && good; row += rows_step) {
+        const LpRow<T> x(logits + row * a.ld, a.vocab);
+        const int u0 = x.part_from(part, log_parts);
+        const int u1 = x.part_from(part + 1, log_parts);
+        for (int u = u0; u < u1; u += LP_CHUNK, ++it) {
+          const int q = it % STAGES;
+          if (it >= STAGES &&
+              !lp_wait(&sh.empty[q], (it / STAGES & 1) ^ 1, &sh.gave_up, a.wait_limit_ns)) {
+            good = false;
+            break;
+          }
+          const uint32_t bytes = static_cast<uint32_t>(min(LP_CHUNK, u1 - u)) * 16;
+          twa_mbar_expect_tx(twa_smem_u32(&sh.full[q]), bytes);
+          lp_bulk_load(twa_smem_u32(sh.ring[q]), x.base + static_cast<long long>(x.first + u) * E, bytes, twa_smem_u32(&sh.full[q]));
+        }
+      }
+      // no copy may still be on its way into this block's shared memory when it ends
+      for (int back = 1; back <= STAGES && back <= it; ++back) {
+        const int last = it - back, q = last % STAGES;
+        const u64 begun = twa_globaltimer();
+        while (!twa_mbar_try_wait(twa_smem_u32(&sh.full[q]), last / STAGES & 1))
+          if (twa_globaltimer() - begun > a.wait_limit_ns) break;
+      }
     }
-    if (lane == 0) sh.mine = st;
+    __syncwarp();
+    if (parts > 1) {
+      lp_cluster_sync();
+      lp_cluster_sync();
+    }
+    return;
   }
 
-  u64 found = 0;                 // warp 0: the block's best, sorted
-  if (TOP) {
-    const u64 mine = first < units ? lp_key(m, best) : 0;
-    const u64 heads = lp_block_best(mine, sh.list);
-    if (warp == 0 && lane == a.top - 1) sh.bound = heads;
-    __syncthreads();
-    const u64 bound = sh.bound;
-    auto scan = [&](auto&& use) {
-      if (mine == 0 || mine < bound) return;
-      for (int u = first; u < units; u += stride) {
-        float v[E];
-        unsigned valid = (1u << E) - 1;
-        if (x.whole(u)) {
-          twa_pack<T, E> q;
-          q.load(x.base + static_cast<long long>(u) * E);
-          q.widen(v);
-        } else {
-          valid = x.load_partial(u, v);
-        }
+  if (warp >= LP_FINISH) {
+    // ---- finish
+    const int turn = warp - LP_FINISH;
+    if (parts > 1 && turn) {       // a cluster has one row
+      lp_cluster_sync();
+      lp_cluster_sync();
+      return;
+    }
+    int r = 0;                     // of this warp's rows
+    for (long long row = row0 + turn * rows_step; row < a.rows; row += LP_FINISHERS * rows_step, ++r) {
+      const LpRow<T> x(logits + row * a.ld, a.vocab);
+      const int u0 = x.part_from(part, log_parts);
+      const int u1 = x.part_from(part + 1, log_parts);
+      const int chunks = (u1 - u0 + LP_CHUNK - 1) / LP_CHUNK;
+      const int last_place = u1 > u0 ? u0 + (chunks - 1) * LP_CHUNK : u0;
+      // the elements of this block's part: from .. to - 1
+      const int from = part == 0 ? 0 : (x.first + u0) * E - x.skew, to = part == parts - 1 ? a.vocab : (x.first + u1) * E - x.skew;
+      long long target = 0;
+      float zt = 0.0f;
+      if (part == 0 && lane == 0) {
+        target = twa_load_id(a.targets, a.itype, row);
+        if (target >= 0 && target < a.vocab) zt = twa_to_float(x.base[x.skew + target]);
+      }
+      const bool waited = lp_wait(&sh.row_full[turn], r & 1, &sh.gave_up, a.wait_limit_ns);
+      LpStat st = lp_merge_near<ENT, LP_WARPS>(sh.stat[turn][lane & (LP_WARPS - 1)]);
+      u64 key[LP_WARPS];
+      if (TOP)
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-          if ((valid >> e & 1) && lp_key(v[e], u) >= bound) use(lp_key(v[e], u * E + e - x.skew));
+        for (int i = 0; i < LP_WARPS; ++i) key[i] = sh.key[turn][i * 32 + lane];
+      __syncwarp();
+      if (lane == 0) twa_mbar_arrive(twa_smem_u32(&sh.row_empty[turn]));
+      if (fabsf(st.m) >= LP_FAR && st.m != -INFINITY) st = lp_sum_far<T, ENT>(x.base + x.skew, from, to, st.m);
+
+      u64 found = 0;                 // sorted
+      if (TOP) {
+        if (st.m == -INFINITY) {     // nothing above -inf: the first indices
+          if (lane < to - from) found = lp_key(-INFINITY, from + lane);
+        } else {
+          // a group: the eight threads of one lane number
+          u64 g = key[0];
+#pragma unroll
+          for (int i = 1; i < LP_WARPS; ++i) g = g > key[i] ? g : key[i];
+          // the top-th largest of the groups': the last one with fewer than `top` above it
+          const int above = lp_place32(g, sh.buffer[turn]);
+          const int most = __reduce_max_sync(0xffffffffu, above < a.top ? above : -1);
+          const u64 bound = __shfl_sync(0xffffffffu, g, __ffs(__ballot_sync(0xffffffffu, above == most)) - 1);
+          const float bound_value = bound ? lp_unrank(static_cast<uint32_t>(bound >> 32)) : -INFINITY;
+          int chosen = 0;
+#pragma unroll
+          for (int i = 0; i < LP_WARPS; ++i) {
+            const bool yes = key[i] && key[i] >= bound;
+            const unsigned all = __ballot_sync(0xffffffffu, yes);
+            if (yes) sh.chosen[turn][chosen + __popc(all & ((1u << lane) - 1))] = i * 32 + lane;
+            chosen += __popc(all);
+          }
+          __syncwarp();
+          // their units that hold a value as large as the bound's
+          constexpr int AHEAD = 8;
+          const int tasks = chosen * chunks * LP_PER_THREAD;
+          int hits = 0, what = lane / chosen, who = lane % chosen;     // of the lane's next task
+          const int what_step = 32 / chosen, who_step = 32 % chosen;
+          for (int i0 = 0; i0 < tasks; i0 += 32 * AHEAD) {
+            uint4 q[AHEAD];
+            int u[AHEAD];
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j) {
+              u[j] = i0 + 32 * j + lane < tasks ? u0 + what * LP_THREADS + sh.chosen[turn][who] : u1;
+              what += what_step;
+              who += who_step;
+              if (who >= chosen) {
+                who -= chosen;
+                ++what;
+              }
+              if (u[j] < u1) q[j] = __ldg(reinterpret_cast<const uint4*>(x.base + static_cast<long long>(x.first + u[j]) * E));
+            }
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j) {
+              const bool hit = u[j] < u1 && W::max1(W::max2(W::max2(q[j].x, q[j].y), W::max2(q[j].z, q[j].w))) >= bound_value;
+              const unsigned all = __ballot_sync(0xffffffffu, hit);
+              const int to = hits + __popc(all & ((1u << lane) - 1));
+              hits += __popc(all);
+              if (hit && to < LP_BUFFER) {
+                sh.hit[turn][to] = q[j];
+                sh.hit_unit[turn][to] = u[j];
+              }
+            }
+          }
+          __syncwarp();
+          // their elements, and the row's ragged ends, that rank at the bound or above
+          int count = 0;
+          const int heads = part == 0 ? x.head() : 0, tails = part == parts - 1 ? a.vocab - x.tail_from() : 0;
+          const int elements = hits <= LP_BUFFER ? hits * E : 0;
+          for (int i0 = 0; i0 < elements + heads + tails; i0 += 32) {
+            const int i = i0 + lane;
+            u64 key = 0;
+            if (i < elements) {
+              const int u = sh.hit_unit[turn][i / E];
+              const float z = twa_to_float(reinterpret_cast<const T*>(sh.hit[turn])[i]);
+              if (lp_key(z, u - (u - u0) % LP_CHUNK) >= bound) key = lp_key(z, (x.first + u) * E + i % E - x.skew);
+            } else if (i < elements + heads + tails) {
+              const bool head = i < elements + heads;
+              const int j = head ? i - elements : x.tail_from() + i - elements - heads;
+              const float z = twa_to_float(x.base[x.skew + j]);
+              if (lp_key(z, head ? u0 : last_place) >= bound) key = lp_key(z, j);
+            }
+            const unsigned all = __ballot_sync(0xffffffffu, key != 0);
+            const int to = count + __popc(all & ((1u << lane) - 1));
+            count += __popc(all);
+            if (key && to < LP_BUFFER) sh.buffer[turn][to] = key;
+          }
+          __syncwarp();
+          if (hits <= LP_BUFFER && count <= LP_BUFFER) {
+            if (count <= 32) {
+              const u64 v = lane < count ? sh.buffer[turn][lane] : 0;
+              __syncwarp();
+              const int place = lp_place32(v, sh.buffer[turn]);
+              __syncwarp();
+              sh.buffer[turn][lane] = 0;
+              __syncwarp();
+              if (v) sh.buffer[turn][place] = v;
+              __syncwarp();
+              found = sh.buffer[turn][lane];
+            } else {
+              found = lp_sort32(sh.buffer[turn][lane]);
+            }
+            for (int i = 32; i < count; i += 32) found = lp_take32(found, i + lane < count ? sh.buffer[turn][i + lane] : 0);
+          } else {
+            found = lp_best_of_all(x.base + x.skew, from, to);     // a row with many equal values
+          }
+        }
+      }
+
+      // ---- the cluster's
+      if (parts > 1) {
+        if (lane == 0) sh.mine = st;
+        if (TOP) sh.best[lane] = found;
+        lp_cluster_sync();
+        if (part == 0) {
+          for (int p = 1; p < parts; ++p) {
+            LpStat other;
+            other.m = lp_remote(&sh.mine.m, p);
+            other.s = lp_remote(&sh.mine.s, p);
+            other.a = ENT ? lp_remote(&sh.mine.a, p) : 0.0f;
+            st = lp_merge<ENT>(st, other);
+            if (TOP) found = lp_merge32(found, lp_remote(&sh.best[31 - lane], p));
+          }
+        }
+        lp_cluster_sync();           // no block leaves while its shared memory is read
+        if (part != 0) return;
+      }
+      const float logs = LN2 * log2f(st.s);
+      const float lse = st.m == -INFINITY ? (st.s == 0.0f ? -INFINITY : NAN) : st.m + logs;
+      if (lane == 0) {
+        a.lse[row] = lse;
+        if (!waited) twa_set_status(a.status, TWA_ERR_TIMEOUT, -1);
+        else if (!(lse < INFINITY)) twa_set_status(a.status, TWA_ERR_NONFINITE, static_cast<int>(row));
+        const bool none = lse == -INFINITY;
+        if (ENT) a.entropy[row] = none ? 0.0f : logs - LN2 * (st.a / st.s);
+        float lp = 0.0f;
+        if (target != a.ignore_id) {
+          if (target < 0 || target >= a.vocab) {
+            twa_set_status(a.status, TWA_ERR_INVALID_ARG, static_cast<int>(row));
+            lp = NAN;
+          } else {
+            lp = none ? -INFINITY : zt - st.m - logs;
+          }
+        }
+        a.logp[row] = lp;
+      }
+      if (TOP && lane < a.top) {
+        a.top_ids[row * a.top + lane] = static_cast<int>(0xffffffffu - static_cast<uint32_t>(found));
+        a.top_logp[row * a.top + lane] = lse == -INFINITY ? -INFINITY : lp_unrank(static_cast<uint32_t>(found >> 32)) - st.m - logs;
+      }
+    }
+    return;
+  }
+
+  // ---- sums
+  int it = 0, r = 0;
+  for (long long row = row0; row < a.rows; row += rows_step, ++r) {
+    const int turn = r % LP_FINISHERS, round = r / LP_FINISHERS;
+    const LpRow<T> x(logits + row * a.ld, a.vocab);
+    const int u0 = x.part_from(part, log_parts);
+    const int u1 = x.part_from(part + 1, log_parts);
+    const int chunks = (u1 - u0 + LP_CHUNK - 1) / LP_CHUNK;
+    const int last_place = u1 > u0 ? u0 + (chunks - 1) * LP_CHUNK : u0;
+    float m = -INFINITY, c = -LP_FAR * LOG2E;
+    u64 s2 = 0, w2 = 0;            // pairs of sums
+    int place = u0;                // first unit of the chunk of the maximum
+    bool some = u1 - u0 >= LP_CHUNK;   // whether this thread has any element
+    // the sums become relative to the new maximum um
+    auto raise_max = [&](float um, int at) {
+      const float nc = lp_base(um) * LOG2E, d = fmaxf(c - nc, -150.0f), f = lp_exp2(d);
+      const u64 f2 = lp_pair(f, f);
+      if (ENT) w2 = lp_mul2(f2, lp_fma2(lp_pair(d, d), s2, w2));
+      s2 = lp_mul2(f2, s2);
+      m = um;
+      c = nc;
+      place = at;
+    };
+    // a thread's units of the chunk that begins at unit `at`
+    auto take_units = [&](auto& units, int at) {
+      constexpr int N = sizeof(units) / sizeof(uint4);
+      uint32_t high[N];
+#pragma unroll
+      for (int j = 0; j < N; ++j) high[j] = W::max2(W::max2(units[j].x, units[j].y), W::max2(units[j].z, units[j].w));
+#pragma unroll
+      for (int half = N / 2; half; half >>= 1)
+#pragma unroll
+        for (int j = 0; j < half; ++j) high[j] = W::max2(high[j], high[j + half]);
+      const float um = W::max1(high[0]);
+      if (um > m) raise_max(um, at);
+      const u64 c2 = lp_pair(-c, -c), l2 = lp_pair(LOG2E, LOG2E);
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        uint32_t w[4] = {units[j].x, units[j].y, units[j].z, units[j].w};
+        if (ENT)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) w[i] = W::raise(w[i]);
+#pragma unroll
+        for (int i = 0; i < W::PAIRS; ++i) {
+          const u64 d2 = lp_fma2(W::pair(w, i), l2, c2);
+          float d0, d1;
+          lp_unpair(d2, d0, d1);
+          const u64 p2 = lp_pair(lp_exp2(d0), lp_exp2(d1));
+          s2 = lp_add2(s2, p2);
+          if (ENT) w2 = lp_fma2(p2, d2, w2);
+        }
       }
     };
-    scan([&](u64 key) {
-      const int at = atomicAdd(&sh.count, 1);
-      if (at < LP_BUFFER) sh.buffer[at] = key;
-    });
-    __syncthreads();
-    if (sh.count <= LP_BUFFER) {
-      found = lp_block_best(static_cast<int>(threadIdx.x) < sh.count ? sh.buffer[threadIdx.x] : 0, sh.list);
-    } else {
-      // too many elements rank with the bound (a row with many equal values): one round per token
-      u64 below = ~0ull;
-      for (int i = 0; i < a.top; ++i) {
-        u64 top = 0;
-        scan([&](u64 key) { if (key < below && key > top) top = key; });
-        if (threadIdx.x == 0) sh.round = 0;
-        __syncthreads();
-        if (top) atomicMax(&sh.round, top);
-        __syncthreads();
-        below = sh.round;
-        if (lane == i) found = below;
-        __syncthreads();
+    // the row's ragged ends: thread 0 of the first part, thread 1 of the last
+    const int ends = part == 0 && threadIdx.x == 0 ? 0 : (part == parts - 1 && threadIdx.x == 1 ? 1 : -1);
+    const int end_from = ends == 0 ? 0 : x.tail_from(), end_to = ends == 0 ? x.head() : (ends == 1 ? a.vocab : 0);
+    auto take_ends = [&](int at) {
+      for (int j = end_from; j < end_to; ++j) {
+        const float z = twa_to_float(x.base[x.skew + j]);
+        some = true;
+        if (z > m) raise_max(z, at);
+        const float d = fmaf(z, LOG2E, -c), p = lp_exp2(d);
+        s2 = lp_add2(s2, lp_pair(p, 0.0f));
+        if (ENT) w2 = lp_fma2(lp_pair(p, 0.0f), lp_pair(fmaxf(d, -150.0f), 0.0f), w2);
+      }
+    };
+    if (ends == 0) take_ends(u0);
+    for (int k = 0; k < chunks; ++k, ++it) {
+      const int q = it % STAGES, n = min(LP_CHUNK, u1 - u0 - k * LP_CHUNK);
+      // after a wait that ran out the row's results are not defined, and every later wait ends at once
+      lp_wait(&sh.full[q], it / STAGES & 1, &sh.gave_up, a.wait_limit_ns);
+      if (n == LP_CHUNK) {
+        uint4 w[LP_PER_THREAD];
+#pragma unroll
+        for (int j = 0; j < LP_PER_THREAD; ++j) w[j] = sh.ring[q][j * LP_THREADS + threadIdx.x];
+        __syncwarp();
+        if (lane == 0) twa_mbar_arrive(twa_smem_u32(&sh.empty[q]));
+        take_units(w, u0 + k * LP_CHUNK);
+      } else {
+        // the last chunk, a unit a thread at a time; a warp without a unit has nothing to do
+        for (int j = warp * 32; j < n; j += LP_THREADS) {
+          uint4 w[1] = {make_uint4(W::NONE, W::NONE, W::NONE, W::NONE)};
+          if (j + lane < n) w[0] = sh.ring[q][j + lane];
+          some |= j + lane < n;
+          take_units(w, u0 + k * LP_CHUNK);
+        }
+        __syncwarp();
+        if (lane == 0) twa_mbar_arrive(twa_smem_u32(&sh.empty[q]));
       }
     }
-    if (warp == 0) sh.best[lane] = found;
-  }
+    if (ends == 1) take_ends(last_place);
 
-  // the cluster's
+    // ---- the warp's sums
+    LpStat st = {m, 0.0f, 0.0f};
+    {
+      float s0, s1, w0, w1;
+      lp_unpair(s2, s0, s1);
+      lp_unpair(w2, w0, w1);
+      st.s = s0 + s1;
+      st.a = w0 + w1;
+      const float e = fmaf(lp_base(m), LOG2E, -c), g = e * LN2;      // c is off by e, at most 2^-11: 2^-e = 1 - g + g^2 / 2
+      const float f = fmaf(g, fmaf(g, 0.5f, -1.0f), 1.0f);
+      st.a = f * (st.a - e * st.s);
+      st.s *= f;
+    }
+    st = lp_merge_near<ENT, 32>(st);
+    if (round) lp_wait(&sh.row_empty[turn], (round & 1) ^ 1, &sh.gave_up, a.wait_limit_ns);
+    if (lane == 0) sh.stat[turn][warp] = st;
+    if (TOP) sh.key[turn][threadIdx.x] = some ? lp_key(m, place) : 0;
+    __syncwarp();
+    if (lane == 0) twa_mbar_arrive(twa_smem_u32(&sh.row_full[turn]));
+  }
   if (parts > 1) {
     lp_cluster_sync();
-    if (part == 0 && warp == 0) {
-      for (int p = 1; p < parts; ++p) {
-        LpStat other;
-        other.m = lp_remote(&sh.mine.m, p);
-        other.s = lp_remote(&sh.mine.s, p);
-        other.a = ENT ? lp_remote(&sh.mine.a, p) : 0.0f;
-        if (lane == 0) st = lp_merge<ENT>(st, other);
-        if (TOP) found = lp_merge32(found, lp_remote(&sh.best[31 - lane], p));
-      }
-    }
-    lp_cluster_sync();           // no block leaves while its shared memory is read
-  }
-  if (part != 0 || warp != 0) return;
-  float lse = 0.0f, logs = 0.0f;
-  if (lane == 0) {
-    logs = LN2 * log2f(st.s);
-    lse = st.m == -INFINITY ? (st.s == 0.0f ? -INFINITY : NAN) : st.m + logs;
-    a.lse[row] = lse;
-    if (!(lse < INFINITY)) twa_set_status(a.status, TWA_ERR_NONFINITE, static_cast<int>(row));
-    const bool none = lse == -INFINITY;
-    if (ENT) a.entropy[row] = none ? 0.0f : logs - LN2 * (st.a / st.s);
-    const long long t = twa_load_id(a.targets, a.itype, row);
-    float lp = 0.0f;
-    if (t != a.ignore_id) {
-      if (t < 0 || t >= a.vocab) {
-        twa_set_status(a.status, TWA_ERR_INVALID_ARG, static_cast<int>(row));
-        lp = NAN;
-      } else {
-        lp = none ? -INFINITY : twa_to_float(x.base[x.skew + t]) - st.m - logs;
-      }
-    }
-    a.logp[row] = lp;
-  }
-  if (TOP) {
-    lse = __shfl_sync(0xffffffffu, lse, 0);
-    logs = __shfl_sync(0xffffffffu, logs, 0);
-    const float top = __shfl_sync(0xffffffffu, st.m, 0);
-    if (lane < a.top) {
-      a.top_ids[row * a.top + lane] = static_cast<int>(0xffffffffu - static_cast<uint32_t>(found));
-      a.top_logp[row * a.top + lane] = lse == -INFINITY ? -INFINITY : lp_unrank(static_cast<uint32_t>(found >> 32)) - top - logs;
-    }
+    lp_cluster_sync();
   }
 }
 
@@ -380,23 +737,23 @@ __global__ void __launch_bounds__(LPB_THREADS) logprobs_backward_kernel(const Lp
   };
   if (SAME) {
     const LpRow<T> x(src, a.vocab);
-    const int units = x.units();
     T* out = dst - x.skew;
-    for (int u = part * LPB_THREADS + threadIdx.x; u < units; u += parts * LPB_THREADS) {
-      float v[E];
-      if (x.whole(u)) {
-        twa_pack<T, E> q;
-        q.load(x.base + static_cast<long long>(u) * E);
-        q.widen(v);
-#pragma unroll
-        for (int e = 0; e < E; ++e) v[e] = grad(v[e], u * E + e - x.skew);
-        twa_pack<T, E>::store(out + static_cast<long long>(u) * E, v);
-      } else {
-        const unsigned valid = x.load_partial(u, v);
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (valid >> e & 1) out[u * E + e] = twa_from_float<T>(grad(v[e], u * E + e - x.skew));
+    if (part == 0) {
+      const int ends = x.head() + a.vocab - x.tail_from();
+      if (static_cast<int>(threadIdx.x) < ends) {
+        const int j = static_cast<int>(threadIdx.x) < x.head() ? threadIdx.x : threadIdx.x - x.head() + x.tail_from();
+        dst[j] = twa_from_float<T>(grad(twa_to_float(src[j]), j));
       }
+    }
+    for (int u = part * LPB_THREADS + threadIdx.x; u < x.whole; u += parts * LPB_THREADS) {
+      const long long at = static_cast<long long>(x.first + u) * E;
+      float v[E];
+      twa_pack<T, E> q;
+      q.load(x.base + at);
+      q.widen(v);
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[e] = grad(v[e], (x.first + u) * E + e - x.skew);
+      twa_pack<T, E>::store(out + at, v);
     }
   } else {
     for (int j = part * LPB_THREADS + threadIdx.x; j < a.vocab; j += parts * LPB_THREADS)
@@ -405,10 +762,17 @@ __global__ void __launch_bounds__(LPB_THREADS) logprobs_backward_kernel(const Lp
 }
 
 template <typename T, bool ENT, bool TOP>
-int lp_launch(twa_ctx* ctx, const LpArgs& a, int parts) {
+int lp_launch(twa_ctx* ctx, const LpArgs& a, int log_parts) {
+  const int parts = 1 << log_parts;
+  static int smem_set[64] = {};
+  const void* kernel = reinterpret_cast<const void*>(logprobs_kernel<T, ENT, TOP>);
+  int rc = twa_ensure_smem(ctx, kernel, &smem_set[ctx->device & 63], sizeof(LpShared<TOP>));
+  if (rc) return rc;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(a.rows * parts));
-  cfg.blockDim = dim3(LP_THREADS);
+  const long long most = static_cast<long long>(ctx->sm_count) * LP_BLOCKS_PER_SM<TOP>;
+  cfg.gridDim = dim3(static_cast<unsigned>(parts > 1 ? a.rows * parts : (a.rows < most ? a.rows : most)));
+  cfg.blockDim = dim3(LP_BLOCK);
+  cfg.dynamicSmemBytes = sizeof(LpShared<TOP>);
   cfg.stream = ctx->stream;
   cudaLaunchAttribute attr = {};
   attr.id = cudaLaunchAttributeClusterDimension;
@@ -416,14 +780,14 @@ int lp_launch(twa_ctx* ctx, const LpArgs& a, int parts) {
   attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = parts > 1 ? 1 : 0;
-  TWA_CUDA_OK(ctx, cudaLaunchKernelEx(&cfg, logprobs_kernel<T, ENT, TOP>, a, parts));
+  TWA_CUDA_OK(ctx, cudaLaunchKernelEx(&cfg, logprobs_kernel<T, ENT, TOP>, a, log_parts));
   return TWA_OK;
 }
 
 template <typename T>
-int lp_launch_any(twa_ctx* ctx, const LpArgs& a, int parts) {
-  if (a.entropy) return a.top ? lp_launch<T, true, true>(ctx, a, parts) : lp_launch<T, true, false>(ctx, a, parts);
-  return a.top ? lp_launch<T, false, true>(ctx, a, parts) : lp_launch<T, false, false>(ctx, a, parts);
+int lp_launch_any(twa_ctx* ctx, const LpArgs& a, int log_parts) {
+  if (a.entropy) return a.top ? lp_launch<T, true, true>(ctx, a, log_parts) : lp_launch<T, true, false>(ctx, a, log_parts);
+  return a.top ? lp_launch<T, false, true>(ctx, a, log_parts) : lp_launch<T, false, false>(ctx, a, log_parts);
 }
 
 template <typename T, bool ENT>
@@ -471,11 +835,14 @@ int twa_token_logprobs(twa_ctx* ctx, const void* logits, int64_t ld, twa_dtype d
   a.vocab = vocab;
   a.itype = t_type;
   a.top = top;
+  a.wait_limit_ns = ctx->wait_limit_ns;
   a.status = ctx->d_status;
-  int parts = 1;
+  int log_parts = 0;
   const long long units = twa_ceil_div(static_cast<long long>(vocab) * twa_dtype_size(dtype), 16);
-  while (parts < LP_MAX_CLUSTER && rows * parts < ctx->sm_count && units > 2LL * LP_THREADS * parts) parts *= 2;
-  return dtype == TWA_BF16 ? lp_launch_any<bf16>(ctx, a, parts) : lp_launch_any<float>(ctx, a, parts);
+  while ((1 << log_parts) < LP_MAX_CLUSTER && rows << (log_parts + 1) <= LP_SPLIT_ROWS * ctx->sm_count &&
+         units > LP_CHUNK / 2 << log_parts)
+    ++log_parts;
+  return dtype == TWA_BF16 ? lp_launch_any<bf16>(ctx, a, log_parts) : lp_launch_any<float>(ctx, a, log_parts);
 }
 
 int twa_token_logprobs_backward(twa_ctx* ctx, const void* logits, int64_t ld, twa_dtype dtype, int64_t rows, int vocab,
