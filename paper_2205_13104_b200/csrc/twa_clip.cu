@@ -93,6 +93,7 @@ __global__ void __launch_bounds__(CLIP_THREADS) clip_norm_kernel(const __grid_co
                                                                  const __grid_constant__ ClipSizes z, double* part, int base,
                                                                  int total, unsigned* ticket, float max_norm, float eps,
                                                                  float* norm_out, float* factor, int* status) {
+  twa_begin(part, ticket, norm_out, factor);
   __shared__ double red[CLIP_THREADS / 32];
   __shared__ unsigned last;
   const int chunks = t.chunk[t.count];
@@ -104,8 +105,10 @@ __global__ void __launch_bounds__(CLIP_THREADS) clip_norm_kernel(const __grid_co
     while (t.chunk[i + 1] <= q) ++i;
     const long long off = static_cast<long long>(q - t.chunk[i]) * CLIP_CHUNK;
     const int n = static_cast<int>(min(static_cast<long long>(CLIP_CHUNK), z.size[i] - off));
-    sum += t.dtype[i] == TWA_BF16 ? clip_square_sum(static_cast<const bf16*>(t.data[i]) + off, n)
-                                  : clip_square_sum(static_cast<const float*>(t.data[i]) + off, n);
+    const void* data = t.data[i];
+    twa_renew(data);
+    sum += t.dtype[i] == TWA_BF16 ? clip_square_sum(static_cast<const bf16*>(data) + off, n)
+                                  : clip_square_sum(static_cast<const float*>(data) + off, n);
   }
   sum = clip_block_sum(sum, red);
   if (threadIdx.x == 0) part[base + blockIdx.x] = sum;
@@ -157,6 +160,7 @@ __device__ __forceinline__ void clip_scale(const T* p, TO* o, int n, float f) {
 __global__ void __launch_bounds__(CLIP_THREADS) clip_scale_kernel(const __grid_constant__ ClipTable t,
                                                                   const __grid_constant__ ClipSizes z,
                                                                   const float* __restrict__ factor, void* out, int out_dtype) {
+  twa_begin(factor, out);
   const float f = __ldg(factor);
   if (!out && f == 1.0f) return;
   const int chunks = t.chunk[t.count], block = gridDim.x - 1 - blockIdx.x;
@@ -168,13 +172,15 @@ __global__ void __launch_bounds__(CLIP_THREADS) clip_scale_kernel(const __grid_c
     const long long off = static_cast<long long>(q - t.chunk[i]) * CLIP_CHUNK;
     const int n = static_cast<int>(min(static_cast<long long>(CLIP_CHUNK), z.size[i] - off));
     const long long at = t.flat[i] + off;
+    void* data = const_cast<void*>(t.data[i]);
+    twa_renew(data);
     if (t.dtype[i] == TWA_BF16) {
-      bf16* p = static_cast<bf16*>(const_cast<void*>(t.data[i])) + off;
+      bf16* p = static_cast<bf16*>(data) + off;
       if (!out) clip_scale(p, p, n, f);
       else if (out_dtype == TWA_BF16) clip_scale(p, static_cast<bf16*>(out) + at, n, f);
       else clip_scale(p, static_cast<float*>(out) + at, n, f);
     } else {
-      float* p = static_cast<float*>(const_cast<void*>(t.data[i])) + off;
+      float* p = static_cast<float*>(data) + off;
       if (!out) clip_scale(p, p, n, f);
       else if (out_dtype == TWA_BF16) clip_scale(p, static_cast<bf16*>(out) + at, n, f);
       else clip_scale(p, static_cast<float*>(out) + at, n, f);
@@ -235,7 +241,7 @@ int clip_run(twa_ctx* ctx, const twa_tensors* s, float max_norm, float eps, bool
     next = clip_fill(s, next, &flat, &t, &z);
     const int blocks = clip_blocks(ctx, t.chunk[t.count]);
     const bool end = next >= s->count;
-    clip_norm_kernel<<<blocks, CLIP_THREADS, 0, ctx->stream>>>(t, z, part, base, end ? base + blocks : 0, ctx->d_ticket, max_norm,
+    twa_launch(ctx->stream, clip_norm_kernel, blocks, CLIP_THREADS, 0, t, z, part, base, end ? base + blocks : 0, ctx->d_ticket, max_norm,
                                                                eps, norm, scale ? factor : nullptr, ctx->d_status);
     base += blocks;
   } while (next < s->count);
@@ -244,13 +250,13 @@ int clip_run(twa_ctx* ctx, const twa_tensors* s, float max_norm, float eps, bool
   // last launch first; its table is still filled when there was one launch only
   const int launches = s->count > CLIP_TENSORS ? 2 : 1;
   if (launches == 1) {
-    clip_scale_kernel<<<clip_blocks(ctx, t.chunk[t.count]), CLIP_THREADS, 0, ctx->stream>>>(t, z, factor, out, out_dtype);
+    twa_launch(ctx->stream, clip_scale_kernel, clip_blocks(ctx, t.chunk[t.count]), CLIP_THREADS, 0, t, z, factor, out, out_dtype);
   } else {
     next = 0;
     flat = 0;
     while (next < s->count) {
       next = clip_fill(s, next, &flat, &t, &z);
-      clip_scale_kernel<<<clip_blocks(ctx, t.chunk[t.count]), CLIP_THREADS, 0, ctx->stream>>>(t, z, factor, out, out_dtype);
+      twa_launch(ctx->stream, clip_scale_kernel, clip_blocks(ctx, t.chunk[t.count]), CLIP_THREADS, 0, t, z, factor, out, out_dtype);
     }
   }
   TWA_CUDA_OK(ctx, cudaGetLastError());

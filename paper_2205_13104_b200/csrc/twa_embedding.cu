@@ -7,30 +7,39 @@
 // Backward sorts (id, position) by id with a stable radix sort, so that equal ids lie side by side in the order of
 // their positions, and adds the rows of each id in that order: the sum does not depend on which block came first, and
 // a frequent token costs no conflicting atomics.  The sorted list is cut into runs of EMB_RUN entries whatever the
-// ids are (a run is one block's work, so a frequent token is shared by many blocks); an id that crosses the end of a
-// run leaves a float32 partial sum per run, and a last kernel adds those in run order.  Rows of the table that no token
-// names are set to zero by a kernel that needs only the ids' bitmap.
+// ids are; a run is one block's work.  An id that goes on into the next run and ends there is added up by the block of
+// the run it begins in.  One that covers a run whole (a frequent token) leaves a float32 partial sum in each of its runs,
+// and a last kernel adds those in run order.
+//
+// Most of what a whole table's gradient has to write are the zeros of rows that no token names.  They need the ids'
+// bitmap only, which the first, short kernel leaves: the kernels that sort, latency-bound on a few SMs, carry blocks that
+// write zeros on the others, and the rest of them go beside the sums.  Up to SMALL_TOKENS ids one block sorts them in
+// shared memory, in one launch.
 #include "twa_ops.cuh"
 
 namespace {
 
 constexpr int SORT_THREADS = 256, SORT_WARPS = SORT_THREADS / 32;
-constexpr int SORT_KEYS = 8;                               // keys of a thread
+constexpr int SORT_KEYS = 4;                               // keys of a thread
 constexpr int SORT_TILE = SORT_THREADS * SORT_KEYS;        // keys of a block
 constexpr int SORT_MAX_BITS = 9, SORT_BINS = 1 << SORT_MAX_BITS;
 constexpr int EMB_RUN = 32;                                // sorted entries a block adds up
+constexpr int SMALL_THREADS = 512, SMALL_WARPS = SMALL_THREADS / 32, SMALL_TOKENS = SMALL_THREADS * SORT_KEYS;
+constexpr int SMALL_BITS = 8, SMALL_BINS = 1 << SMALL_BITS;
+constexpr int SMALL_VOCAB = 1 << 20;                       // ids whose bitmap one block clears
+constexpr int FILL_BYTES = 1 << 16;                        // zeros of a block
+constexpr long long FILL_BESIDE_SORT = 32LL << 20;         // zeros written beside a sorting kernel: what its few us have room for
 
 // E elements of any pairing of the two types; E = 8 wants both addresses on 16 bytes, E = 1 nothing.
 template <typename T, int E>
 __device__ __forceinline__ void load_row(const T* p, float* v) {
-  if constexpr (E == 1) v[0] = twa_to_float(p[0]);
-  else
+  constexpr int N = E == 1 ? 1 : twa_vec<T>;
 #pragma unroll
-    for (int i = 0; i < E; i += twa_vec<T>) {
-      twa_pack<T, twa_vec<T>> q;
-      q.load(p + i);
-      q.widen(v + i);
-    }
+  for (int i = 0; i < E; i += N) {
+    twa_pack<T, N> q;
+    q.load(p + i);
+    q.widen(v + i);
+  }
 }
 template <typename T, int E>
 __device__ __forceinline__ void store_row(T* p, const float* v) {
@@ -42,12 +51,15 @@ __device__ __forceinline__ void store_row(T* p, const float* v) {
 
 // ---- forward -------------------------------------------------------------------------------------
 // A warp takes FWD_UNITS x 32 units of E elements of one row.
-constexpr int FWD_UNITS = 4, FWD_WARPS = 4;
+template <int E>
+constexpr int FWD_UNITS = E == 1 ? 16 : 4;
+constexpr int FWD_WARPS = 4;
 
 template <typename TT, typename TO, int E>
 __global__ void embedding_kernel(const TT* __restrict__ table, long long ldt, int vocab, const void* __restrict__ ids, int itype,
                                  long long tokens, int dim, float scale, TO* __restrict__ out, long long ldo, int parts,
                                  int* status) {
+  twa_begin(table, ids);
   const long long task = static_cast<long long>(blockIdx.x) * FWD_WARPS + (threadIdx.x >> 5);
   const long long t = task / parts;
   if (t >= tokens) return;
@@ -55,17 +67,17 @@ __global__ void embedding_kernel(const TT* __restrict__ table, long long ldt, in
   const long long id = twa_load_id(ids, itype, t);
   const bool good = id >= 0 && id < vocab;
   if (!good && part == 0 && (threadIdx.x & 31) == 0) twa_set_status(status, TWA_ERR_INVALID_ARG, static_cast<int>(t));
-  const int c0 = (part * FWD_UNITS * 32 + (threadIdx.x & 31)) * E;
-  float v[FWD_UNITS][E];
+  const int c0 = (part * FWD_UNITS<E> * 32 + (threadIdx.x & 31)) * E;
+  float v[FWD_UNITS<E>][E];
 #pragma unroll
-  for (int k = 0; k < FWD_UNITS; ++k) {
+  for (int k = 0; k < FWD_UNITS<E>; ++k) {
     const int c = c0 + k * 32 * E;
 #pragma unroll
     for (int e = 0; e < E; ++e) v[k][e] = 0.0f;
     if (good && c < dim) load_row<TT, E>(table + id * ldt + c, v[k]);
   }
 #pragma unroll
-  for (int k = 0; k < FWD_UNITS; ++k) {
+  for (int k = 0; k < FWD_UNITS<E>; ++k) {
     const int c = c0 + k * 32 * E;
 #pragma unroll
     for (int e = 0; e < E; ++e) v[k][e] *= scale;
@@ -113,6 +125,7 @@ __device__ __forceinline__ uint32_t emb_key(const void* ids, int itype, long lon
 // Counts of the first digit per tile; marks the ids that occur.
 __global__ void emb_count_kernel(const void* __restrict__ ids, int itype, int tokens, int vocab, long long padding, int bits,
                                  uint32_t* used, int* __restrict__ hist, int* status) {
+  twa_begin(ids);
   __shared__ int count[SORT_BINS];
   const int bins = 1 << bits;
   for (int d = threadIdx.x; d < bins; d += SORT_THREADS) count[d] = 0;
@@ -128,16 +141,141 @@ __global__ void emb_count_kernel(const void* __restrict__ ids, int itype, int to
   for (int d = threadIdx.x; d < bins; d += SORT_THREADS) hist[blockIdx.x * SORT_BINS + d] = count[d];
 }
 
-// One pass of the radix sort over the digit at `shift`: stable, a tile per block.  key_in == null: the keys are the ids'.
+// The rows of a table as bytes, for writing zeros; `each` rows a block.
+struct EmbFill {
+  char* table;
+  long long stride;             // bytes between rows
+  long long bytes;              // of a row
+  const uint32_t* used;
+  int row0, row1, each;         // rows row0 .. row1 - 1
+  int size;                     // of an element
+};
+// Zeros into the unused ones of the block's rows: 16 bytes a store between the ragged ends.
+__device__ __forceinline__ void emb_fill(const EmbFill& f, int block) {
+  const int r0 = f.row0 + block * f.each, rows = min(f.each, f.row1 - r0);
+  const int slots = static_cast<int>(f.bytes / 16) + 1;           // 0: the ends
+  for (int i = threadIdx.x; i < rows * slots; i += blockDim.x) {
+    const int r = i / slots, slot = i - r * slots, v = r0 + r;
+    if (__ldg(f.used + (v >> 5)) >> (v & 31) & 1) continue;
+    char* row = f.table + v * f.stride;
+    const int head = static_cast<int>(min(f.bytes, static_cast<long long>(-reinterpret_cast<uintptr_t>(row) & 15)));
+    const int whole = static_cast<int>((f.bytes - head) / 16);
+    if (slot) {
+      if (slot <= whole) *reinterpret_cast<uint4*>(row + head + (slot - 1) * 16LL) = make_uint4(0, 0, 0, 0);
+    } else {
+      for (int b = 0; b < head; b += f.size) {
+        if (f.size == 2) *reinterpret_cast<unsigned short*>(row + b) = 0;
+        else *reinterpret_cast<unsigned*>(row + b) = 0;
+      }
+      for (long long b = head + whole * 16LL; b < f.bytes; b += f.size) {
+        if (f.size == 2) *reinterpret_cast<unsigned short*>(row + b) = 0;
+        else *reinterpret_cast<unsigned*>(row + b) = 0;
+      }
+    }
+  }
+}
+
+// Up to SMALL_TOKENS ids sorted by one block; the bitmap too.
+__global__ void __launch_bounds__(SMALL_THREADS) emb_sort_small_kernel(const void* __restrict__ ids, int itype, int tokens, int vocab,
+                                                                       long long padding, int total_bits, uint32_t* used,
+                                                                       uint32_t* __restrict__ key_out,
+                                                                       uint32_t* __restrict__ pos_out, int* status) {
+  twa_begin(ids);
+  __shared__ uint32_t keys[SMALL_TOKENS];
+  __shared__ unsigned short place[SMALL_TOKENS];
+  __shared__ unsigned short count[SMALL_WARPS][SMALL_BINS];
+  __shared__ int warp_total[SMALL_BINS / 32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (used) {
+    for (int i = threadIdx.x; i < (vocab + 31) / 32; i += SMALL_THREADS) used[i] = 0;
+    __syncthreads();
+  }
+  const int t0 = warp * 32 * SORT_KEYS + lane;
+  uint32_t key[SORT_KEYS];
+  int pos[SORT_KEYS];
+#pragma unroll
+  for (int k = 0; k < SORT_KEYS; ++k) {
+    pos[k] = t0 + k * 32;
+    key[k] = 0xffffffffu;                            // beyond the tokens: after all of them, by stability and by digit
+    if (pos[k] < tokens) {
+      key[k] = emb_key(ids, itype, pos[k], vocab, padding, status);
+      if (used && key[k] < static_cast<uint32_t>(vocab)) atomicOr(&used[key[k] >> 5], 1u << (key[k] & 31));
+    }
+  }
+  for (int shift = 0; shift < total_bits; shift += SMALL_BITS) {
+    for (int d = threadIdx.x; d < SMALL_WARPS * SMALL_BINS; d += SMALL_THREADS) (&count[0][0])[d] = 0;
+    __syncthreads();
+    int rank[SORT_KEYS];
+#pragma unroll
+    for (int k = 0; k < SORT_KEYS; ++k) {
+      const int d = (key[k] >> shift) & (SMALL_BINS - 1);
+      const unsigned same = __match_any_sync(0xffffffffu, d);
+      const int before = __popc(same & ((1u << lane) - 1));
+      rank[k] = count[warp][d] + before;
+      __syncwarp();
+      if (before == 0) count[warp][d] += static_cast<unsigned short>(__popc(same));
+      __syncwarp();
+    }
+    __syncthreads();
+    int all = 0, sum = 0;
+    if (threadIdx.x < SMALL_BINS) {
+      for (int w = 0; w < SMALL_WARPS; ++w) all += count[w][threadIdx.x];
+      sum = all;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int up = __shfl_up_sync(0xffffffffu, sum, o);
+        if (lane >= o) sum += up;
+      }
+      if (lane == 31) warp_total[warp] = sum;
+    }
+    __syncthreads();
+    if (threadIdx.x < SMALL_BINS) {
+      int at = sum - all;
+      for (int w = 0; w < warp; ++w) at += warp_total[w];
+      for (int w = 0; w < SMALL_WARPS; ++w) {
+        const int c = count[w][threadIdx.x];
+        count[w][threadIdx.x] = static_cast<unsigned short>(at);
+        at += c;
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < SORT_KEYS; ++k) {
+      const int to = count[warp][(key[k] >> shift) & (SMALL_BINS - 1)] + rank[k];
+      keys[to] = key[k];
+      place[to] = static_cast<unsigned short>(pos[k]);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < SORT_KEYS; ++k) {
+      key[k] = keys[t0 + k * 32];
+      pos[k] = place[t0 + k * 32];
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < SORT_KEYS; ++k)
+    if (t0 + k * 32 < tokens) {
+      key_out[t0 + k * 32] = key[k];
+      pos_out[t0 + k * 32] = pos[k];
+    }
+}
+
+// One pass of the radix sort over the digit at `shift`: stable, a tile per block, and blocks that write zeros.  key_in == null: the keys are the ids'.
 // Counts the next digit of every key in the tile that the key moves to (hist_next, cleared; integer sums).
 __global__ void emb_scatter_kernel(const void* __restrict__ ids, int itype, int vocab, long long padding,
                                    const uint32_t* __restrict__ key_in, const uint32_t* __restrict__ pos_in, int tokens,
                                    int shift, int bits, const int* __restrict__ hist, int* __restrict__ hist_next,
-                                   uint32_t* __restrict__ key_out, uint32_t* __restrict__ pos_out) {
+                                   uint32_t* __restrict__ key_out, uint32_t* __restrict__ pos_out, int tiles,
+                                   EmbFill fill) {
+  twa_begin(ids, key_in, pos_in, hist, fill.used);
+  if (static_cast<int>(blockIdx.x) >= tiles) {
+    emb_fill(fill, blockIdx.x - tiles);
+    return;
+  }
   __shared__ int count[SORT_WARPS][SORT_BINS];
   __shared__ int base[SORT_BINS];
   __shared__ int warp_total[SORT_WARPS];
-  const int bins = 1 << bits, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, tile = blockIdx.x, tiles = gridDim.x;
+  const int bins = 1 << bits, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, tile = blockIdx.x;
   for (int d = threadIdx.x; d < SORT_WARPS * SORT_BINS; d += SORT_THREADS) (&count[0][0])[d] = 0;
   __syncthreads();
   // rank of every key among the equal digits of its warp, in the order of the keys
@@ -212,121 +350,141 @@ __global__ void emb_scatter_kernel(const void* __restrict__ ids, int itype, int 
   }
 }
 
-// ---- zero rows, sums, joins ------------------------------------------------------------------------
-template <typename T, int E>
-__global__ void emb_zero_kernel(const uint32_t* __restrict__ used, int vocab, int dim, T* __restrict__ dtable, long long ldg) {
-  float zero[E];
-#pragma unroll
-  for (int e = 0; e < E; ++e) zero[e] = 0.0f;
-  for (long long v = blockIdx.x; v < vocab; v += gridDim.x) {
-    if (__ldg(used + (v >> 5)) >> (v & 31) & 1) continue;
-    for (int c = threadIdx.x * E; c < dim; c += blockDim.x * E) store_row<T, E>(dtable + v * ldg + c, zero);
-  }
-}
-
+// ---- sums, joins ------------------------------------------------------------------------------------
 template <typename TG, int E>
 __device__ __forceinline__ void emb_write(TG* to, float (&sum)[E], float scale, int accumulate) {
 #pragma unroll
   for (int e = 0; e < E; ++e) sum[e] *= scale;
   if (accumulate) {
+    float held[E];
+    load_row<TG, E>(to, held);
 #pragma unroll
-    for (int e = 0; e < E; ++e) sum[e] += twa_to_float(to[e]);
+    for (int e = 0; e < E; ++e) sum[e] += held[e];
   }
   store_row<TG, E>(to, sum);
 }
 
-// Run blockIdx.x of the sorted list, columns of blockIdx.y: the rows of every id in the run are added in order.  An id
-// that also lies in the run before, or in the run after, leaves its sum in partial[run][0], or [run][1].
+// Run `block / column_blocks` of the sorted list, columns of block % column_blocks: the rows of every id that begins in the
+// run are added in order.  An id that covers some run whole leaves its sum over this run in partial[run][1] if it begins
+// here, in partial[run][0] otherwise.  Blocks from sum_blocks on write zeros.
+constexpr int SUM_THREADS = 128;
 template <typename TD, typename TG, int E>
-__global__ void emb_sum_kernel(const uint32_t* __restrict__ key, const uint32_t* __restrict__ pos, int tokens, int vocab, int dim,
-                               const TD* __restrict__ dout, long long ldd, float scale, TG* __restrict__ dtable, long long ldg,
-                               int accumulate, float* __restrict__ partial) {
-  constexpr int AHEAD = 4;
-  __shared__ uint32_t k[EMB_RUN + 2], p[EMB_RUN];
-  const int first = blockIdx.x * EMB_RUN, n = min(EMB_RUN, tokens - first);
-  if (threadIdx.x < EMB_RUN + 2) {
-    const int i = first + static_cast<int>(threadIdx.x) - 1;      // one entry before and one after
-    k[threadIdx.x] = i >= 0 && i < tokens ? key[i] : 0xffffffffu;
-    if (threadIdx.x >= 1 && static_cast<int>(threadIdx.x) <= n) p[threadIdx.x - 1] = pos[i];
+__global__ void __launch_bounds__(SUM_THREADS) emb_sum_kernel(const uint32_t* __restrict__ key, const uint32_t* __restrict__ pos,
+                                                              int tokens, int vocab, int dim, const TD* __restrict__ dout,
+                                                              long long ldd, float scale, TG* __restrict__ dtable, long long ldg,
+                                                              int accumulate, float* __restrict__ partial, int column_blocks,
+                                                              int sum_blocks, EmbFill fill) {
+  twa_begin(key, pos, dout, dtable, fill.used);
+  if (static_cast<int>(blockIdx.x) >= sum_blocks) {
+    emb_fill(fill, blockIdx.x - sum_blocks);
+    return;
   }
+  constexpr int P = E == 1 ? 1 : E / twa_vec<TD>;                 // packs of E elements
+  constexpr int AHEAD = 8 / P;
+  typedef twa_pack<TD, E == 1 ? 1 : twa_vec<TD>> Pack;
+  static_assert(EMB_RUN == 32, "a lane per entry of a run");
+  __shared__ uint32_t keys[2 * EMB_RUN + 1], p[2 * EMB_RUN], far;
+  uint32_t* k = keys + 1;                                         // k[i]: entry first + i
+  const int run = blockIdx.x / column_blocks, first = run * EMB_RUN;
+  const int n = min(EMB_RUN, tokens - first), n2 = min(2 * EMB_RUN, tokens - first);
+  for (int i = static_cast<int>(threadIdx.x) - 1; i < 2 * EMB_RUN; i += SUM_THREADS) {
+    k[i] = first + i >= 0 && i < n2 ? key[first + i] : 0xffffffffu;
+    if (i >= 0 && i < n2) p[i] = pos[first + i];
+  }
+  if (threadIdx.x == 0) far = first > EMB_RUN ? key[first - EMB_RUN - 1] : 0xffffffffu;    // the last entry two runs before
   __syncthreads();
-  const int c = (blockIdx.y * blockDim.x + threadIdx.x) * E;
+  const int lane = threadIdx.x & 31;
+  // the id that the run begins with, if it began before, and the one it ends with, if that goes on
+  const bool before = k[-1] == k[0], after = n2 > n && k[n] == k[n - 1];
+  const uint32_t lead = k[0], trail = k[n - 1];
+  const bool lead_partial = before && (far == lead || (n == EMB_RUN && trail == lead));
+  const bool trail_partial = after && (k[-1] == trail || (n2 == 2 * EMB_RUN && k[n2 - 1] == trail));
+  const unsigned leading = __ballot_sync(0xffffffffu, lane < n && k[lane] == lead);
+  const unsigned trailing = __ballot_sync(0xffffffffu, EMB_RUN + lane < n2 && k[EMB_RUN + lane] == trail);
+  const int from = before && !lead_partial ? __popc(leading) : 0;
+  const int to = after && !trail_partial ? n + __popc(trailing) : n;
+  const int c = ((blockIdx.x - run * column_blocks) * SUM_THREADS + threadIdx.x) * E;
   if (c >= dim) return;
   float sum[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) sum[e] = 0.0f;
-  for (int i0 = 0; i0 < n; i0 += AHEAD) {
-    float v[AHEAD][E];
+  for (int i0 = from; i0 < to; i0 += AHEAD) {
+    Pack q[AHEAD][P];
 #pragma unroll
     for (int j = 0; j < AHEAD; ++j)
-      if (i0 + j < n && k[i0 + j + 1] < static_cast<uint32_t>(vocab))
-        load_row<TD, E>(dout + static_cast<long long>(p[i0 + j]) * ldd + c, v[j]);
+      if (i0 + j < to && k[i0 + j] < static_cast<uint32_t>(vocab))
+#pragma unroll
+        for (int h = 0; h < P; ++h) q[j][h].load(dout + static_cast<long long>(p[i0 + j]) * ldd + c + h * (E / P));
 #pragma unroll
     for (int j = 0; j < AHEAD; ++j) {
       const int i = i0 + j;
-      if (i >= n) break;
-      const uint32_t id = k[i + 1];
+      if (i >= to) break;
+      const uint32_t id = k[i];
       if (id >= static_cast<uint32_t>(vocab)) return;             // the rest contributes nothing
+      float v[E];
 #pragma unroll
-      for (int e = 0; e < E; ++e) sum[e] += v[j][e];
-      const bool last = i + 1 == n;
-      if (!last && k[i + 2] == id) continue;
-      const bool before = k[0] == id, after = last && k[i + 2] == id;
-      if (before || after) {
-        float* to = partial + (static_cast<long long>(blockIdx.x) * 2 + (before ? 0 : 1)) * dim + c;
+      for (int h = 0; h < P; ++h) q[j][h].widen(v + h * (E / P));
 #pragma unroll
-        for (int e = 0; e < E; ++e) to[e] = sum[e];
-      } else {
+      for (int e = 0; e < E; ++e) sum[e] += v[e];
+      const bool last = i + 1 == to;
+      if (!last && k[i + 1] == id) continue;
+      const bool first_part = lead_partial && id == lead;
+      if (first_part || (last && trail_partial))
+        store_row<float, E>(partial + (static_cast<long long>(run) * 2 + (first_part ? 0 : 1)) * dim + c, sum);
+      else
         emb_write<TG, E>(dtable + static_cast<long long>(id) * ldg + c, sum, scale, accumulate);
-      }
 #pragma unroll
       for (int e = 0; e < E; ++e) sum[e] = 0.0f;
     }
   }
 }
 
-// An id that begins in run blockIdx.x and goes on: its partial sums over the runs, JOIN_WAYS stretches of runs side by side.
+// An id that begins in run blockIdx.x and covers the next whole: its partial sums over the runs, JOIN_WAYS stretches of runs side by side;
+// the columns of blockIdx.y.
 constexpr int JOIN_WAYS = 8, JOIN_LANES = 32;
 template <typename TG, int E>
 __global__ void emb_join_kernel(const uint32_t* __restrict__ key, int tokens, int vocab, int dim, float scale,
                                 TG* __restrict__ dtable, long long ldg, int accumulate, const float* __restrict__ partial) {
+  twa_begin(key, dtable, partial);
   __shared__ float part[JOIN_WAYS][JOIN_LANES][E + 1];
-  const long long first = static_cast<long long>(blockIdx.x) * EMB_RUN, next = first + EMB_RUN;
-  if (next >= tokens) return;
+  const int from = blockIdx.x, runs = (tokens + EMB_RUN - 1) / EMB_RUN;
+  const long long first = static_cast<long long>(from) * EMB_RUN, next = first + EMB_RUN;
   const uint32_t id = key[next - 1];
-  if (id >= static_cast<uint32_t>(vocab) || key[next] != id) return;
-  if (first > 0 && key[first - 1] == id) return;                  // it began in an earlier run
-  long long low = next, high = tokens;                            // the first entry after the id's
-  while (low < high) {
-    const long long mid = (low + high) / 2;
-    if (key[mid] == id) low = mid + 1;
-    else high = mid;
+  if (next + EMB_RUN > tokens || key[next + EMB_RUN - 1] != id) return;
+  if (id >= static_cast<uint32_t>(vocab) || (first > 0 && key[first - 1] == id)) return;   // nothing, or begun in an earlier run
+  // its runs are from .. to - 1: those after `low` begin with it as far as all threads' probes reach, and so on ever closer
+  int low = from + 1, high = runs;
+  while (low + 1 < high) {
+    const int step = (high - low - 1 + JOIN_WAYS * JOIN_LANES - 1) / (JOIN_WAYS * JOIN_LANES);
+    const long long probe = low + (threadIdx.x + 1LL) * step;
+    const int inside = __syncthreads_count(probe < high && key[probe * EMB_RUN] == id);
+    const long long beyond = low + (inside + 1LL) * step;
+    low += inside * step;
+    if (beyond < high) high = static_cast<int>(beyond);
   }
-  const int from = blockIdx.x, to = static_cast<int>((low - 1) / EMB_RUN) + 1;    // runs
+  const int to = low + 1;
   const int lane = threadIdx.x % JOIN_LANES, way = threadIdx.x / JOIN_LANES;
   const int each = (to - from + JOIN_WAYS - 1) / JOIN_WAYS;
   const int a = from + way * each, b = min(to, a + each);
-  for (int c0 = 0; c0 < dim; c0 += JOIN_LANES * E) {
-    const int c = c0 + lane * E;
-    float sum[E];
+  const int c = (blockIdx.y * JOIN_LANES + lane) * E;
+  float sum[E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) sum[e] = 0.0f;
-    if (c < dim)
-      for (int r = a; r < b; ++r) {
-        const float* src = partial + (static_cast<long long>(r) * 2 + (r == from ? 1 : 0)) * dim + c;
+  for (int e = 0; e < E; ++e) sum[e] = 0.0f;
+  if (c < dim)
+    for (int r = a; r < b; ++r) {
+      float v[E];
+      load_row<float, E>(partial + (static_cast<long long>(r) * 2 + (r == from ? 1 : 0)) * dim + c, v);
 #pragma unroll
-        for (int e = 0; e < E; ++e) sum[e] += src[e];
-      }
-#pragma unroll
-    for (int e = 0; e < E; ++e) part[way][lane][e] = sum[e];
-    __syncthreads();
-    if (way == 0 && c < dim) {
-      for (int w = 1; w < JOIN_WAYS; ++w)
-#pragma unroll
-        for (int e = 0; e < E; ++e) sum[e] += part[w][lane][e];
-      emb_write<TG, E>(dtable + static_cast<long long>(id) * ldg + c, sum, scale, accumulate);
+      for (int e = 0; e < E; ++e) sum[e] += v[e];
     }
-    __syncthreads();
+#pragma unroll
+  for (int e = 0; e < E; ++e) part[way][lane][e] = sum[e];
+  __syncthreads();
+  if (way == 0 && c < dim) {
+    for (int w = 1; w < JOIN_WAYS; ++w)
+#pragma unroll
+      for (int e = 0; e < E; ++e) sum[e] += part[w][lane][e];
+    emb_write<TG, E>(dtable + static_cast<long long>(id) * ldg + c, sum, scale, accumulate);
   }
 }
 
@@ -335,46 +493,50 @@ bool emb_packs(const void* p, long long ld, size_t size) { return !twa_misaligne
 template <typename TT, typename TO>
 void launch_embedding(twa_ctx* ctx, bool packs, const void* table, int64_t ldt, int vocab, const void* ids, int itype,
                       int64_t tokens, int dim, float scale, void* out, int64_t ldo) {
-  const int parts = static_cast<int>(twa_ceil_div(dim, (packs ? 8 : 1) * 32 * FWD_UNITS));
+  const int parts = static_cast<int>(twa_ceil_div(dim, packs ? 8 * 32 * FWD_UNITS<8> : 32 * FWD_UNITS<1>));
   const unsigned blocks = static_cast<unsigned>(twa_ceil_div(tokens * parts, FWD_WARPS));
   if (packs)
-    embedding_kernel<TT, TO, 8><<<blocks, 32 * FWD_WARPS, 0, ctx->stream>>>(static_cast<const TT*>(table), ldt, vocab, ids, itype,
+    twa_launch(ctx->stream, embedding_kernel<TT, TO, 8>, blocks, 32 * FWD_WARPS, 0, static_cast<const TT*>(table), ldt, vocab, ids, itype,
                                                                           tokens, dim, scale, static_cast<TO*>(out), ldo, parts,
                                                                           ctx->d_status);
   else
-    embedding_kernel<TT, TO, 1><<<blocks, 32 * FWD_WARPS, 0, ctx->stream>>>(static_cast<const TT*>(table), ldt, vocab, ids, itype,
+    twa_launch(ctx->stream, embedding_kernel<TT, TO, 1>, blocks, 32 * FWD_WARPS, 0, static_cast<const TT*>(table), ldt, vocab, ids, itype,
                                                                           tokens, dim, scale, static_cast<TO*>(out), ldo, parts,
                                                                           ctx->d_status);
+}
+
+// The number of blocks that write the zeros of rows row0 .. of `fill` within `budget` bytes (0: all that are left); the
+// rows are taken off `left`.
+unsigned emb_fill_blocks(const EmbFill& left, long long budget, EmbFill* part) {
+  *part = left;
+  if (budget) {
+    const long long rows = budget / left.bytes / left.each * left.each;
+    if (left.row0 + rows < left.row1) part->row1 = static_cast<int>(left.row0 + rows);
+  }
+  return static_cast<unsigned>(twa_ceil_div(part->row1 - part->row0, left.each));
 }
 
 template <typename TD, typename TG, int E>
 void launch_sums(twa_ctx* ctx, const EmbSpace& s, const uint32_t* key, const uint32_t* pos, int tokens, int vocab, int dim,
-                 const void* dout, int64_t ldd, float scale, void* dtable, int64_t ldg, int accumulate) {
+                 const void* dout, int64_t ldd, float scale, void* dtable, int64_t ldg, int accumulate, const EmbFill& fill) {
   TG* g = static_cast<TG*>(dtable);
-  if (tokens) {
-    const unsigned runs = static_cast<unsigned>(twa_ceil_div(tokens, EMB_RUN));
-    const int units = (dim + E - 1) / E, threads = units >= 128 ? 128 : (units < 64 ? 64 : (units + 31) / 32 * 32);
-    const dim3 grid(runs, static_cast<unsigned>(twa_ceil_div(units, threads)));
-    emb_sum_kernel<TD, TG, E><<<grid, threads, 0, ctx->stream>>>(key, pos, tokens, vocab, dim, static_cast<const TD*>(dout), ldd,
-                                                                 scale, g, ldg, accumulate, s.partial);
-    if (runs > 1)
-      emb_join_kernel<TG, E><<<runs - 1, JOIN_WAYS * JOIN_LANES, 0, ctx->stream>>>(key, tokens, vocab, dim, scale, g, ldg,
-                                                                                 accumulate, s.partial);
-  }
+  const unsigned runs = static_cast<unsigned>(twa_ceil_div(tokens, EMB_RUN));
+  const unsigned column_blocks = static_cast<unsigned>(twa_ceil_div(dim, E * SUM_THREADS));
+  EmbFill rest;
+  const unsigned zeros = emb_fill_blocks(fill, 0, &rest);
+  if (runs * column_blocks + zeros)
+    twa_launch(ctx->stream, emb_sum_kernel<TD, TG, E>, runs * column_blocks + zeros, SUM_THREADS, 0, key, pos, tokens, vocab, dim, static_cast<const TD*>(dout), ldd, scale, g, ldg, accumulate, s.partial, column_blocks,
+        runs * column_blocks, rest);
+  if (tokens >= 2 * EMB_RUN)
+    twa_launch(ctx->stream, emb_join_kernel<TG, E>, dim3(runs - 1, static_cast<unsigned>(twa_ceil_div(dim, E * JOIN_LANES))), JOIN_WAYS * JOIN_LANES, 0, key, tokens, vocab, dim, scale, g, ldg, accumulate, s.partial);
 }
 
 template <typename TD, typename TG>
 void launch_sums_any(twa_ctx* ctx, bool packs, const EmbSpace& s, const uint32_t* key, const uint32_t* pos, int tokens, int vocab,
-                     int dim, const void* dout, int64_t ldd, float scale, void* dtable, int64_t ldg, int accumulate) {
-  if (packs) launch_sums<TD, TG, 8>(ctx, s, key, pos, tokens, vocab, dim, dout, ldd, scale, dtable, ldg, accumulate);
-  else launch_sums<TD, TG, 1>(ctx, s, key, pos, tokens, vocab, dim, dout, ldd, scale, dtable, ldg, accumulate);
-}
-
-template <typename TG>
-void launch_zero(twa_ctx* ctx, bool packs, const uint32_t* used, int vocab, int dim, void* dtable, int64_t ldg) {
-  const int blocks = vocab < 8 * ctx->sm_count ? vocab : 8 * ctx->sm_count;
-  if (packs) emb_zero_kernel<TG, 8><<<blocks, 256, 0, ctx->stream>>>(used, vocab, dim, static_cast<TG*>(dtable), ldg);
-  else emb_zero_kernel<TG, 1><<<blocks, 256, 0, ctx->stream>>>(used, vocab, dim, static_cast<TG*>(dtable), ldg);
+                     int dim, const void* dout, int64_t ldd, float scale, void* dtable, int64_t ldg, int accumulate,
+                     const EmbFill& fill) {
+  if (packs) launch_sums<TD, TG, 8>(ctx, s, key, pos, tokens, vocab, dim, dout, ldd, scale, dtable, ldg, accumulate, fill);
+  else launch_sums<TD, TG, 1>(ctx, s, key, pos, tokens, vocab, dim, dout, ldd, scale, dtable, ldg, accumulate, fill);
 }
 
 }  // namespace
@@ -423,35 +585,41 @@ int twa_embedding_backward(twa_ctx* ctx, const void* dout, int64_t ldd, twa_dtyp
   const EmbSpace s = emb_space(ws, tokens, vocab, dim);
   const int n = static_cast<int>(tokens), tiles = static_cast<int>(twa_ceil_div(tokens, SORT_TILE));
   const bool packs = dim % 8 == 0 && emb_packs(dout, ldd, ds) && emb_packs(dtable, ldg, gs);
-  TWA_CUDA_OK(ctx, cudaMemsetAsync(s.used, 0, reinterpret_cast<char*>(s.key[0]) - reinterpret_cast<char*>(s.used), ctx->stream));
   int total_bits = 1;
   while (total_bits < 32 && (static_cast<long long>(vocab) >> total_bits)) ++total_bits;      // keys 0 .. vocab
-  const int passes = (total_bits + SORT_MAX_BITS - 1) / SORT_MAX_BITS, bits = (total_bits + passes - 1) / passes;
+  EmbFill fill = {static_cast<char*>(dtable), static_cast<long long>(ldg * gs), static_cast<long long>(dim * gs), s.used, 0,
+                  accumulate ? 0 : vocab, 1, static_cast<int>(gs)};
+  if (fill.bytes < FILL_BYTES) fill.each = static_cast<int>(FILL_BYTES / fill.bytes);
   int at = 0;
-  if (n) {
-    emb_count_kernel<<<tiles, SORT_THREADS, 0, ctx->stream>>>(ids, id_type, n, vocab, padding_id, bits, s.used, s.hist[0],
-                                                              ctx->d_status);
-    for (int p = 0; p < passes; ++p) {
+  if (n <= SMALL_TOKENS && vocab <= SMALL_VOCAB) {
+    twa_launch(ctx->stream, emb_sort_small_kernel, 1, SMALL_THREADS, 0, ids, id_type, n, vocab, padding_id, total_bits,
+                                                                accumulate ? nullptr : s.used, s.key[at], s.pos[at], ctx->d_status);
+  } else {
+    TWA_CUDA_OK(ctx, cudaMemsetAsync(s.used, 0, reinterpret_cast<char*>(s.key[0]) - reinterpret_cast<char*>(s.used), ctx->stream));
+    const int passes = (total_bits + SORT_MAX_BITS - 1) / SORT_MAX_BITS, bits = (total_bits + passes - 1) / passes;
+    if (n)
+      twa_launch(ctx->stream, emb_count_kernel, tiles, SORT_THREADS, 0, ids, id_type, n, vocab, padding_id, bits, s.used, s.hist[0],
+                                                                ctx->d_status);
+    for (int p = 0; n && p < passes; ++p) {
       int* next = p + 1 < passes ? s.hist[(p + 1) & 1] : nullptr;
-      if (p >= 1 && next)
-        TWA_CUDA_OK(ctx, cudaMemsetAsync(next, 0, sizeof(int) * SORT_BINS * tiles, ctx->stream));
-      emb_scatter_kernel<<<tiles, SORT_THREADS, 0, ctx->stream>>>(ids, id_type, vocab, padding_id, p ? s.key[at] : nullptr,
-                                                                  p ? s.pos[at] : nullptr, n, p * bits, bits, s.hist[p & 1], next,
-                                                                  s.key[at ^ 1], s.pos[at ^ 1]);
+      if (p >= 1 && next) TWA_CUDA_OK(ctx, cudaMemsetAsync(next, 0, sizeof(int) * SORT_BINS * tiles, ctx->stream));
+      EmbFill part;
+      const unsigned zeros = emb_fill_blocks(fill, FILL_BESIDE_SORT, &part);
+      twa_launch(ctx->stream, emb_scatter_kernel, tiles + zeros, SORT_THREADS, 0, ids, id_type, vocab, padding_id, p ? s.key[at] : nullptr,
+                                                                          p ? s.pos[at] : nullptr, n, p * bits, bits,
+                                                                          s.hist[p & 1], next, s.key[at ^ 1], s.pos[at ^ 1], tiles,
+                                                                          part);
+      fill.row0 = part.row1;
       at ^= 1;
     }
-    TWA_CUDA_OK(ctx, cudaGetLastError());
   }
+  TWA_CUDA_OK(ctx, cudaGetLastError());
   const bool db = d_dtype == TWA_BF16, gb = g_dtype == TWA_BF16;
-  if (!accumulate) {
-    if (gb) launch_zero<bf16>(ctx, packs, s.used, vocab, dim, dtable, ldg);
-    else launch_zero<float>(ctx, packs, s.used, vocab, dim, dtable, ldg);
-  }
   const uint32_t *key = s.key[at], *pos = s.pos[at];
-  if (db && gb) launch_sums_any<bf16, bf16>(ctx, packs, s, key, pos, n, vocab, dim, dout, ldd, scale, dtable, ldg, accumulate);
-  else if (db) launch_sums_any<bf16, float>(ctx, packs, s, key, pos, n, vocab, dim, dout, ldd, scale, dtable, ldg, accumulate);
-  else if (gb) launch_sums_any<float, bf16>(ctx, packs, s, key, pos, n, vocab, dim, dout, ldd, scale, dtable, ldg, accumulate);
-  else launch_sums_any<float, float>(ctx, packs, s, key, pos, n, vocab, dim, dout, ldd, scale, dtable, ldg, accumulate);
+  if (db && gb) launch_sums_any<bf16, bf16>(ctx, packs, s, key, pos, n, vocab, dim, dout, ldd, scale, dtable, ldg, accumulate, fill);
+  else if (db) launch_sums_any<bf16, float>(ctx, packs, s, key, pos, n, vocab, dim, dout, ldd, scale, dtable, ldg, accumulate, fill);
+  else if (gb) launch_sums_any<float, bf16>(ctx, packs, s, key, pos, n, vocab, dim, dout, ldd, scale, dtable, ldg, accumulate, fill);
+  else launch_sums_any<float, float>(ctx, packs, s, key, pos, n, vocab, dim, dout, ldd, scale, dtable, ldg, accumulate, fill);
   TWA_CUDA_OK(ctx, cudaGetLastError());
   return TWA_OK;
 }

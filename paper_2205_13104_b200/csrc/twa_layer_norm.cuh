@@ -1,0 +1,225 @@
+// Shared by the two directions of layer norm: arguments, the place of rows and columns, weights in shared memory.  sm_100a only.
+#pragma once
+
+#include "twa_ops.cuh"
+
+namespace {
+
+constexpr int LN_MAX_BLOCKS = 592;     // (a multiple of 8) blocks of the backward pass at most: rows of partial sums in the workspace
+constexpr int LN_WARP_THREADS = 128;   // a warp or less per row: threads of a block at most
+constexpr int LN_BLOCK_THREADS = 512;  // a block per row: at most
+constexpr int LN_WIDE_THREADS = 1024, LN_WIDE_HELD = 16;
+constexpr int LN_LOOP_THREADS = 512;   // rows wider than the registers of a block
+constexpr int LN_MAX_SMEM = 220 * 1024;
+
+struct LnArgs {
+  const void* x;
+  const void* dy;      // backward
+  void* y;             // forward: y; backward: dx
+  const void* w;
+  const void* b;
+  float* mean;
+  float* rstd;
+  float* part;         // backward: [blocks][2][cols] partial sums of dw and db
+  long long ldx, lddy, ldy, rows;
+  int cols, w_dtype;
+  int log_lanes;       // a warp per row or less: log2 of the threads of a row
+  int log_classes;     // rows lie in 2^log_classes ways on 16-byte boundaries; a block takes rows of one
+  float eps;
+};
+
+// Sum over the threads of a row, PER <= 32.
+template <int PER>
+__device__ __forceinline__ float ln_sum_lanes(float v, int log_lanes) {
+  if constexpr (PER != 0) {
+    return twa_warp_sum(v);
+  } else {
+    for (int o = 0; o < log_lanes; ++o) v += __shfl_xor_sync(0xffffffffu, v, 1 << o);
+    return v;
+  }
+}
+
+// Sum of N values over the block (one barrier; `red` is used in turn by successive calls, two sets, so that a set is
+// written again only after the next barrier).
+template <int N>
+__device__ __forceinline__ void block_sum(float (&v)[N], float (*red)[32][N], int& turn) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = twa_warp_sum(v[i]);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  float(*set)[N] = red[turn];
+  turn ^= 1;
+  if (lane == 0)
+#pragma unroll
+    for (int i = 0; i < N; ++i) set[warp][i] = v[i];
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = 0.0f;
+  for (int w = 0; w < warps; ++w)
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] += set[w][i];
+}
+
+// PER: threads of a row.  32: a warp; more: a block of so many; 0: a part of a warp, 2^log_lanes threads.  With PER known all
+// of a thread's addresses are constants apart (16384 x 2048 bfloat16: 918 instructions a row against 570, 32 us against 26).
+template <int PER>
+constexpr int LN_THREADS = PER > 32 ? PER : LN_WARP_THREADS;      // of a block
+
+// Which rows and columns a thread works on.  Rows: r = first + i * step, all with the same place on 16-byte boundaries.
+// Columns: units of E elements counted from the 16-byte boundary at or below the row, unit k * per + t for k = 0, 1, ..;
+// `skew` elements of the first unit lie before the row.
+template <int E, int NV, int PER, bool FULL>
+struct LnPlace {
+  int lanes, t, group;        // PER == 0: threads of a row; this one's number; rows from the warp's first to this one's
+  long long first, step;
+  int skew, row_units, cols;
+  __device__ __forceinline__ LnPlace(const LnArgs& a, int size) {
+    const int classes = FULL ? 1 : 1 << a.log_classes, cls = FULL ? 0 : blockIdx.x & (classes - 1);
+    const int block = FULL ? blockIdx.x : blockIdx.x >> a.log_classes, blocks = FULL ? gridDim.x : gridDim.x >> a.log_classes;
+    long long q;
+    if (PER <= 32) {
+      const int lane = threadIdx.x & 31, log_lanes = PER ? 5 : a.log_lanes, groups = 32 >> log_lanes, warps = LN_WARP_THREADS / 32;
+      lanes = 1 << log_lanes;
+      t = lane & (lanes - 1);
+      group = lane >> log_lanes;
+      q = (static_cast<long long>(block) * warps + (threadIdx.x >> 5)) * groups;
+      step = static_cast<long long>(blocks) * warps * groups * classes;
+    } else {
+      lanes = PER;
+      t = threadIdx.x;
+      group = 0;
+      q = block;
+      step = static_cast<long long>(blocks) * classes;
+    }
+    first = q * classes + cls;
+    group *= classes;
+    cols = a.cols;
+    skew = FULL || E == 1 ? 0 : static_cast<int>(((reinterpret_cast<uintptr_t>(a.x) + cls * a.ldx * size) & 15) / size);
+    row_units = (skew + cols + E - 1) / E;
+  }
+  // units of the vectors in shared memory: all that the threads can have
+  __device__ __forceinline__ int units() const { return (PER ? PER : lanes) * NV; }
+  __device__ __forceinline__ int unit(int k) const { return k * (PER ? PER : lanes) + t; }
+  __device__ __forceinline__ bool in(int k) const { return FULL || unit(k) < row_units; }
+  __device__ __forceinline__ int column(int k, int e) const { return unit(k) * E + e - skew; }
+  __device__ __forceinline__ bool valid(int k, int e) const {
+    return FULL || (E == 1 ? in(k) : column(k, e) >= 0 && column(k, e) < cols);
+  }
+  // every element of the unit in the row
+  __device__ __forceinline__ bool whole(int k) const {
+    return FULL || (E == 1 ? in(k) : unit(k) * E >= skew && (unit(k) + 1) * E <= skew + cols);
+  }
+  // the unit of the row that begins at `row`; elements outside are 0
+  template <typename T>
+  __device__ __forceinline__ void load(twa_pack<T, E>& p, const T* row, int k) const {
+    if (whole(k)) {
+      p.load(row - skew + unit(k) * E);
+    } else if constexpr (E > 1) {
+      float v[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[e] = valid(k, e) ? twa_to_float(row[column(k, e)]) : 0.0f;
+      twa_pack<T, E>::store(reinterpret_cast<T*>(&p), v);
+    }
+  }
+  template <typename T>
+  __device__ __forceinline__ void store(T* row, int k, const float* v) const {
+    if (whole(k)) {
+      twa_pack<T, E>::store(row - skew + unit(k) * E, v);
+    } else if constexpr (E > 1) {
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (valid(k, e)) row[column(k, e)] = twa_from_float<T>(v[e]);
+    }
+  }
+};
+
+extern __shared__ __align__(16) float ln_planes[];
+// A vector of float32 per column in shared memory, by units of E elements; E == 8: in two planes of half a unit each so that
+// 16-byte accesses of neighbouring threads do not collide.
+template <int E>
+struct LnPlane {
+  static constexpr int HALF = E == 8 ? 4 : E;
+  int from, units;             // its place in ln_planes
+  __device__ __forceinline__ int at(int unit, int e) const { return from + (e / HALF * units + unit) * HALF + e % HALF; }
+  __device__ __forceinline__ void load(int unit, float* v) const {
+#pragma unroll
+    for (int e = 0; e < E; e += HALF) {
+      if constexpr (HALF == 4) {
+        const float4 q = *reinterpret_cast<const float4*>(&ln_planes[at(unit, e)]);
+        v[e] = q.x; v[e + 1] = q.y; v[e + 2] = q.z; v[e + 3] = q.w;
+      } else {
+        v[e] = ln_planes[at(unit, e)];
+      }
+    }
+  }
+  __device__ __forceinline__ void store(int unit, const float* v) const {
+#pragma unroll
+    for (int e = 0; e < E; e += HALF) {
+      if constexpr (HALF == 4) *reinterpret_cast<float4*>(&ln_planes[at(unit, e)]) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+      else ln_planes[at(unit, e)] = v[e];
+    }
+  }
+};
+// Fills it from a vector of any type and alignment whose element 0 is `skew` elements into the first unit, or with `missing`;
+// LN_STAGE loads of a thread are under way at once.
+constexpr int LN_STAGE = 16;
+template <int E>
+__device__ __forceinline__ void ln_stage(const LnPlane<E>& to, const void* from, int dtype, int skew, int cols, float missing) {
+  const int n = to.units * E;
+  for (int c0 = threadIdx.x; c0 < n; c0 += LN_STAGE * blockDim.x) {
+    float v[LN_STAGE];
+#pragma unroll
+    for (int i = 0; i < LN_STAGE; ++i) {
+      const int c = c0 + i * blockDim.x - skew;
+      v[i] = from && c >= 0 && c < cols ? twa_load_any(from, dtype, c) : missing;
+    }
+#pragma unroll
+    for (int i = 0; i < LN_STAGE; ++i) {
+      const int c = c0 + i * blockDim.x;
+      if (c < n) ln_planes[to.at(c / E, c % E)] = v[i];
+    }
+  }
+}
+
+// The NV * E elements of a thread as pairs.
+template <int E, int NV>
+struct LnPairs {
+  static constexpr int N = E * NV, P = (N + 1) / 2;
+  static __device__ __forceinline__ twa_f2 get(const float* v, int i) { return twa_pair(v[2 * i], 2 * i + 1 < N ? v[2 * i + 1] : 0.0f); }
+  static __device__ __forceinline__ void put(float* v, int i, twa_f2 p) {
+    float lo, hi;
+    twa_unpair(p, lo, hi);
+    v[2 * i] = lo;
+    if (2 * i + 1 < N) v[2 * i + 1] = hi;
+  }
+};
+
+typedef void (*LnKernel)(LnArgs);
+struct LnPlan {
+  LnKernel kernel;                 // null: the rows do not fit a block
+  int threads, blocks, log_lanes;  // threads of a block, blocks, log2 of the threads of a row where those are in one warp
+  int log_classes;
+  size_t smem;
+};
+
+// What a thread holds of a row at most.  The backward pass holds x, dy and two sums per column.
+template <int E, bool BACK, int PER>
+constexpr int LN_HELD = BACK ? 16 : (PER == 32 && E == 8 ? 64 : 32);
+
+// Ways in which the rows of all matrices lie on 16-byte boundaries, if they do alike.
+int ln_classes(const void* p, long long ld, const void* q, long long ldq, const void* s, long long lds, long long rows, int cols,
+               size_t size) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p) & 15;
+  const long long d = (ld * static_cast<long long>(size)) & 15;
+  if ((reinterpret_cast<uintptr_t>(q) & 15) != a || (reinterpret_cast<uintptr_t>(s) & 15) != a) return 0;
+  if (rows > 1 && (((ldq * static_cast<long long>(size)) & 15) != d || ((lds * static_cast<long long>(size)) & 15) != d)) return 0;
+  if (a == 0 && (d == 0 || rows <= 1) && cols * size % 16 == 0) return 1;
+  return static_cast<int>(16 / size);
+}
+
+int ln_check(const twa_ctx* ctx, twa_dtype dt, twa_dtype wt, int64_t rows, int cols) {
+  if (!ctx || !twa_dtype_ok(dt) || !twa_dtype_ok(wt) || rows < 0 || cols < 1) return TWA_ERR_INVALID_ARG;
+  if (rows > (1LL << 40) || cols > TWA_LAYER_NORM_MAX_COLS) return TWA_ERR_UNSUPPORTED;
+  return TWA_OK;
+}
+
+}  // namespace

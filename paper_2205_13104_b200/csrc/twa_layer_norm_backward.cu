@@ -1,0 +1,427 @@
+// Gradient of layer norm: dx, dw and db (formulas and design beside the forward pass, twa_layer_norm.cu).
+#include "twa_layer_norm.cuh"
+
+namespace {
+
+template <typename T, int E, int NV, int PER, bool FULL>
+__global__ void __launch_bounds__(LN_THREADS<PER>, 512 / LN_THREADS<PER>) ln_backward_kernel(LnArgs a) {
+  twa_begin(a.x, a.dy, a.w, a.mean, a.rstd);
+  __shared__ float red[2][32][2];
+  typedef LnPairs<E, NV> Q;
+  constexpr int P = Q::P;
+  int turn = 0;
+  constexpr bool WARP = PER <= 32, ALONE = PER != 0;   // ALONE: a warp's threads are all of one row
+  const LnPlace<E, NV, PER, FULL> at(a, sizeof(T));
+  const T* x = static_cast<const T*>(a.x);
+  const T* dy = static_cast<const T*>(a.dy);
+  T* dx = static_cast<T*>(a.y);
+  const LnPlane<E> w = {0, at.units()};
+  const float inv = 1.0f / static_cast<float>(a.cols);
+  twa_f2 dw[P], db[P];
+#pragma unroll
+  for (int i = 0; i < P; ++i) dw[i] = db[i] = 0;
+  twa_pack<T, E> rx[NV] = {}, rd[NV] = {};             // what is beyond the row stays 0 in rd, and with it all that is added up
+  float mean = 0.0f, rstd = 0.0f;
+  auto fetch = [&](long long r) {
+    if (r >= a.rows) return;
+    mean = __ldg(a.mean + r);
+    rstd = __ldg(a.rstd + r);
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+      if (at.in(k)) {
+        at.load(rx[k], x + r * a.ldx, k);
+        at.load(rd[k], dy + r * a.lddy, k);
+      }
+  };
+  fetch(at.first + at.group);
+  ln_stage<E>(w, a.w, a.w_dtype, at.skew, a.cols, 1.0f);
+  __syncthreads();
+  for (long long base = at.first; base < a.rows; base += at.step) {
+    const long long r = base + at.group;
+    twa_f2 h[P], v[P], s0 = 0, s1 = 0;
+    const float rs = rstd;
+    if (ALONE || r < a.rows) {
+      float f[Q::N], d[Q::N], wv[Q::N];
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        rx[k].widen(f + k * E);
+        rd[k].widen(d + k * E);
+        w.load(at.unit(k), wv + k * E);
+      }
+      const twa_f2 m2 = twa_pair(-mean), r2 = twa_pair(rs);
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        const twa_f2 di = Q::get(d, i);
+        h[i] = twa_mul2(twa_add2(Q::get(f, i), m2), r2);
+        dw[i] = twa_fma2(di, h[i], dw[i]);
+        db[i] = twa_add2(db[i], di);
+        v[i] = twa_mul2(di, Q::get(wv, i));
+        s0 = twa_add2(s0, v[i]);
+        s1 = twa_fma2(v[i], h[i], s1);
+      }
+    }
+    fetch(r + at.step);
+    float s[2] = {twa_pair_sum(s0), twa_pair_sum(s1)};
+    if (WARP) {
+      s[0] = ln_sum_lanes<PER>(s[0], a.log_lanes);
+      s[1] = ln_sum_lanes<PER>(s[1], a.log_lanes);
+    } else {
+      block_sum<2>(s, red, turn);
+    }
+    if (ALONE || r < a.rows) {
+      // rstd (v - c1 - h c2)
+      const twa_f2 c1 = twa_pair(-s[0] * inv), c2 = twa_pair(-s[1] * inv), r2 = twa_pair(rs);
+      float f[Q::N];
+#pragma unroll
+      for (int i = 0; i < P; ++i) Q::put(f, i, twa_mul2(r2, twa_fma2(h[i], c2, twa_add2(v[i], c1))));
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+        if (at.in(k)) at.store(dx + r * a.ldy, k, f + k * E);
+    }
+  }
+  if (!a.part) return;
+  float* out = a.part + static_cast<long long>(blockIdx.x) * 2 * a.cols;
+  if constexpr (WARP) {
+    // the rows of a warp side by side
+#pragma unroll
+    for (int i = 0; i < P; ++i)
+      for (int o = PER ? 5 : a.log_lanes; o < 5; ++o) {
+        dw[i] = twa_add2(dw[i], __shfl_xor_sync(0xffffffffu, dw[i], 1 << o));
+        db[i] = twa_add2(db[i], __shfl_xor_sync(0xffffffffu, db[i], 1 << o));
+      }
+  }
+  float fw[Q::N], fb[Q::N];
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    Q::put(fw, i, dw[i]);
+    Q::put(fb, i, db[i]);
+  }
+  if constexpr (WARP) {
+    for (int which = 0; which < LN_WARP_THREADS / 32; ++which) {      // the warps in order
+      __syncthreads();
+      if (which == static_cast<int>(threadIdx.x >> 5) && at.group == 0)
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+          for (int e = 0; e < E; ++e)
+            if (at.valid(k, e)) {
+              const int c = at.column(k, e);
+              ln_planes[c] = which ? ln_planes[c] + fw[k * E + e] : fw[k * E + e];
+              ln_planes[a.cols + c] = which ? ln_planes[a.cols + c] + fb[k * E + e] : fb[k * E + e];
+            }
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < 2 * a.cols; c += blockDim.x) out[c] = ln_planes[c];
+  } else {
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (at.valid(k, e)) {
+          out[at.column(k, e)] = fw[k * E + e];
+          out[a.cols + at.column(k, e)] = fb[k * E + e];
+        }
+  }
+}
+
+// Rows of 8193 .. 16384 columns: a block of 1024 threads, 16 elements a thread as they lie in memory, the weights and the partial
+// sums of dw and db in shared memory.
+template <typename T, int E>
+__global__ void __launch_bounds__(LN_WIDE_THREADS) ln_backward_wide_kernel(LnArgs a) {
+  twa_begin(a.x, a.dy, a.w, a.mean, a.rstd);
+  __shared__ float red[2][32][2];
+  int turn = 0;
+  constexpr int NV = LN_WIDE_HELD / E;
+  const int units = (a.cols + E - 1) / E, t = threadIdx.x;
+  const LnPlane<E> w = {0, units}, dw = {units * E, units}, db = {2 * units * E, units};
+  ln_stage<E>(w, a.w, a.w_dtype, 0, a.cols, 1.0f);
+  for (int c = t; c < 2 * units * E; c += LN_WIDE_THREADS) ln_planes[units * E + c] = 0.0f;
+  __syncthreads();
+  const T* x = static_cast<const T*>(a.x);
+  const T* dy = static_cast<const T*>(a.dy);
+  T* dx = static_cast<T*>(a.y);
+  const float inv = 1.0f / static_cast<float>(a.cols);
+  for (long long r = blockIdx.x; r < a.rows; r += gridDim.x) {
+    const float mean = __ldg(a.mean + r), rstd = __ldg(a.rstd + r);
+    twa_pack<T, E> rx[NV], rd[NV];
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+      if (k * LN_WIDE_THREADS + t < units) {
+        rx[k].load(x + r * a.ldx + (k * LN_WIDE_THREADS + t) * E);
+        rd[k].load(dy + r * a.lddy + (k * LN_WIDE_THREADS + t) * E);
+      }
+    float s[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int u = k * LN_WIDE_THREADS + t;
+      if (u >= units) continue;
+      float h[E], d[E], q[E];
+      rx[k].widen(h);
+      rd[k].widen(d);
+#pragma unroll
+      for (int e = 0; e < E; ++e) h[e] = (h[e] - mean) * rstd;
+      dw.load(u, q);
+#pragma unroll
+      for (int e = 0; e < E; ++e) q[e] += d[e] * h[e];
+      dw.store(u, q);
+      db.load(u, q);
+#pragma unroll
+      for (int e = 0; e < E; ++e) q[e] += d[e];
+      db.store(u, q);
+      w.load(u, q);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float v = d[e] * q[e];
+        s[0] += v;
+        s[1] += v * h[e];
+      }
+    }
+    block_sum<2>(s, red, turn);
+    const float c1 = s[0] * inv, c2 = s[1] * inv;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int u = k * LN_WIDE_THREADS + t;
+      if (u >= units) continue;
+      float h[E], d[E], q[E];
+      rx[k].widen(h);
+      rd[k].widen(d);
+      w.load(u, q);
+#pragma unroll
+      for (int e = 0; e < E; ++e) h[e] = rstd * (d[e] * q[e] - c1 - (h[e] - mean) * rstd * c2);
+      twa_pack<T, E>::store(dx + r * a.ldy + u * E, h);
+    }
+  }
+  if (!a.part) return;
+  float* out = a.part + static_cast<long long>(blockIdx.x) * 2 * a.cols;
+  __syncthreads();
+  for (int c = t; c < a.cols; c += LN_WIDE_THREADS) {
+    out[c] = ln_planes[dw.at(c / E, c % E)];
+    out[a.cols + c] = ln_planes[db.at(c / E, c % E)];
+  }
+}
+
+template <typename T>
+__global__ void ln_backward_loop_kernel(LnArgs a) {
+  twa_begin(a.x, a.dy, a.w, a.b, a.mean, a.rstd);
+  __shared__ float red[2][32][2];
+  int turn = 0;
+  const T* x = static_cast<const T*>(a.x);
+  const T* dy = static_cast<const T*>(a.dy);
+  T* dx = static_cast<T*>(a.y);
+  for (long long r = blockIdx.x; r < a.rows; r += gridDim.x) {
+    const T *xr = x + r * a.ldx, *dr = dy + r * a.lddy;
+    const float mean = a.mean[r], rstd = a.rstd[r];
+    float s[2] = {0.0f, 0.0f};
+    for (int c = threadIdx.x; c < a.cols; c += blockDim.x) {
+      const float v = twa_to_float(dr[c]) * (a.w ? twa_load_any(a.w, a.w_dtype, c) : 1.0f);
+      s[0] += v;
+      s[1] += v * ((twa_to_float(xr[c]) - mean) * rstd);
+    }
+    block_sum<2>(s, red, turn);
+    const float c1 = s[0] / static_cast<float>(a.cols), c2 = s[1] / static_cast<float>(a.cols);
+    for (int c = threadIdx.x; c < a.cols; c += blockDim.x) {
+      const float v = twa_to_float(dr[c]) * (a.w ? twa_load_any(a.w, a.w_dtype, c) : 1.0f);
+      const float h = (twa_to_float(xr[c]) - mean) * rstd;
+      dx[r * a.ldy + c] = twa_from_float<T>(rstd * (v - c1 - h * c2));
+    }
+  }
+}
+
+// The columns' partial sums for those rows: a thread per column, blockIdx.y takes every gridDim.y-th row.
+template <typename T>
+__global__ void ln_weights_loop_kernel(LnArgs a) {
+  twa_begin(a.x, a.dy, a.w, a.b, a.mean, a.rstd);
+  const int c = blockIdx.x * blockDim.x + threadIdx.x;
+  if (c >= a.cols) return;
+  const T* x = static_cast<const T*>(a.x);
+  const T* dy = static_cast<const T*>(a.dy);
+  float dw = 0.0f, db = 0.0f;
+  for (long long r = blockIdx.y; r < a.rows; r += gridDim.y) {
+    const float d = twa_to_float(dy[r * a.lddy + c]);
+    dw += d * ((twa_to_float(x[r * a.ldx + c]) - a.mean[r]) * a.rstd[r]);
+    db += d;
+  }
+  float* out = a.part + static_cast<long long>(blockIdx.y) * 2 * a.cols;
+  out[c] = dw;
+  out[a.cols + c] = db;
+}
+
+// Adds the blocks' partial sums in block order: 32 columns a block, its warps each a run of the blocks.
+constexpr int LN_SUM_WARPS = 16;
+__global__ void ln_sum_kernel(const float* __restrict__ part, int blocks, int cols, void* dw, void* db, int g_dtype,
+                              int accumulate) {
+  twa_begin(part);
+  __shared__ double run[LN_SUM_WARPS][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int c = blockIdx.x * 32 + lane;               // 0 .. 2 cols: dw, then db
+  const int each = (blocks + LN_SUM_WARPS - 1) / LN_SUM_WARPS;
+  const int from = warp * each, to = min(blocks, from + each);
+  double s = 0.0;
+  if (c < 2 * cols)
+#pragma unroll 8
+    for (int k = from; k < to; ++k) s += static_cast<double>(__ldg(part + static_cast<long long>(k) * 2 * cols + c));
+  run[warp][lane] = s;
+  __syncthreads();
+  if (warp || c >= 2 * cols) return;
+  for (int k = 1; k < LN_SUM_WARPS; ++k) s += run[k][lane];
+  void* out = c < cols ? dw : db;
+  const int i = c < cols ? c : c - cols;
+  if (!out) return;
+  if (accumulate) s += static_cast<double>(twa_load_any(out, g_dtype, i));
+  twa_store_any(out, g_dtype, i, static_cast<float>(s));
+}
+
+// The kernel that holds at least nv units a thread, and how many that is.
+template <typename T, int E, bool BACK, int PER>
+LnKernel ln_pick(int* nv, int units, bool aligned) {
+  const int wanted = *nv;
+  constexpr int held = LN_HELD<E, BACK, PER>;
+#define LN_TRY(n, if_more)                                                              \
+  if constexpr (E * n <= held && (PER <= 32 || 2 * E * n >= held) && (if_more)) {       \
+    if (wanted <= n) {                                                                  \
+      *nv = n;                                                                          \
+      if constexpr (E > 1 && PER > 0)                                                   \
+        if (aligned && units == PER * n) return ln_backward_kernel<T, E, n, PER, true>;          \
+      return ln_backward_kernel<T, E, n, PER, false>;                                            \
+    }                                                                                   \
+  }
+  LN_TRY(1, true)
+  LN_TRY(2, true)
+  LN_TRY(3, E > 1 && PER > 0)
+  LN_TRY(4, true)
+  LN_TRY(6, E > 1 && PER > 0)
+  LN_TRY(8, true)
+  LN_TRY(16, true)
+  LN_TRY(32, true)
+#undef LN_TRY
+  return nullptr;
+}
+
+template <typename T, int E, bool BACK>
+int ln_plan_units(twa_ctx* ctx, int classes, long long rows, int cols, LnPlan* plan) {
+  // with several classes a row can begin anywhere in its first unit
+  const int units = (cols + E - 1) / E + (classes > 1 ? 1 : 0);
+  constexpr int warp_held = LN_HELD<E, BACK, 32> / E, held = LN_HELD<E, BACK, 64> / E;
+  const bool aligned = classes == 1;
+  LnPlan p = {nullptr, 0, 0, 5, 0, 0};
+  while (1 << p.log_classes < classes) ++p.log_classes;
+  int nv = 0, per = 32;
+  long long blocks = rows;
+  p.threads = LN_WARP_THREADS;
+  if (units <= 32 * warp_held) {
+    // as few threads a row as hold it, while there are rows enough to keep the SMs busy
+    while (p.log_lanes > 0 && units <= held << (p.log_lanes - 1) && (rows << (p.log_lanes - 1)) >= 32LL * 16 * ctx->sm_count) --p.log_lanes;
+    while (p.log_lanes > 0 && units <= 1 << (p.log_lanes - 1)) --p.log_lanes;
+    per = 1 << p.log_lanes;
+    nv = (units + per - 1) / per;
+    p.kernel = per == 32 ? ln_pick<T, E, BACK, 32>(&nv, units, aligned) : ln_pick<T, E, BACK, 0>(&nv, units, aligned);
+    blocks = twa_ceil_div(rows, p.threads / per);
+  } else if (units <= LN_BLOCK_THREADS * held) {
+    for (per = 64; units > per * held;) per *= 2;
+    nv = (units + per - 1) / per;
+    p.threads = per;
+    p.kernel = per == 64 ? ln_pick<T, E, BACK, 64>(&nv, units, aligned)
+               : per == 128 ? ln_pick<T, E, BACK, 128>(&nv, units, aligned)
+               : per == 256 ? ln_pick<T, E, BACK, 256>(&nv, units, aligned) : ln_pick<T, E, BACK, 512>(&nv, units, aligned);
+  }
+  p.smem = sizeof(float) * 2 * per * nv * E;
+  if constexpr (BACK) {
+    if (!p.kernel && aligned && units <= LN_WIDE_THREADS * (LN_WIDE_HELD / E)) {
+      p.threads = LN_WIDE_THREADS;
+      p.smem = sizeof(float) * 3 * units * E;
+      p.kernel = ln_backward_wide_kernel<T, E>;
+    }
+  }
+  if (p.kernel && p.smem > 44 * 1024) {      // 48 KB with what the kernel declares
+    // which of the kernels that can need as much: by threads and what they hold
+    static int smem_set[5][40][2][64] = {};
+    int log = 0;
+    while (64 << log < p.threads) ++log;
+    int rc = twa_ensure_smem(ctx, reinterpret_cast<const void*>(p.kernel),
+                             &smem_set[log][nv][aligned && units == per * nv][ctx->device & 63], static_cast<int>(p.smem));
+    if (rc) return rc;
+  }
+  const long long per_sm = p.threads < 512 ? 512 / p.threads : 1;
+  long long most = ctx->sm_count * per_sm;
+  if (BACK && most > LN_MAX_BLOCKS) most = LN_MAX_BLOCKS;
+  if (blocks > most) blocks = most;
+  if (classes > 1) blocks = twa_ceil_div(blocks, classes) * classes;
+  p.blocks = static_cast<int>(blocks);
+  *plan = p;
+  return TWA_OK;
+}
+
+// classes: ways in which the rows lie on 16-byte boundaries (1: all begin on one), 0: the matrices differ in that.
+template <typename T, bool BACK>
+int ln_plan(twa_ctx* ctx, int classes, long long rows, int cols, LnPlan* plan) {
+  if (classes) {
+    int rc = ln_plan_units<T, twa_vec<T>, BACK>(ctx, classes, rows, cols, plan);
+    if (rc || plan->kernel) return rc;
+  }
+  return ln_plan_units<T, 1, BACK>(ctx, 1, rows, cols, plan);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t twa_layer_norm_workspace_bytes(int64_t rows, int cols) {
+  if (rows < 0 || cols < 1) return 0;
+  const long long blocks = rows < LN_MAX_BLOCKS ? (rows + 8) / 8 * 8 : LN_MAX_BLOCKS;      // a plan rounds up by classes
+  return twa_round256(sizeof(float) * 2 * static_cast<size_t>(cols) * blocks);
+}
+
+int twa_layer_norm_backward(twa_ctx* ctx, const void* dy, int64_t lddy, const void* x, int64_t ldx, twa_dtype dtype,
+                            const void* w, twa_dtype w_dtype, const float* mean, const float* rstd, int64_t rows, int cols,
+                            void* dx, int64_t lddx, void* dw, void* db, twa_dtype g_dtype, int accumulate, void* ws,
+                            size_t ws_bytes) {
+  int rc = ln_check(ctx, dtype, w_dtype, rows, cols);
+  if (rc) return rc;
+  if (!twa_dtype_ok(g_dtype) || accumulate < 0 || accumulate > 1) return TWA_ERR_INVALID_ARG;
+  const size_t size = twa_dtype_size(dtype);
+  if (rows && (!dy || !x || !mean || !rstd || !dx || lddy < cols || ldx < cols || lddx < cols)) return TWA_ERR_INVALID_ARG;
+  if (twa_misaligned_to(dy, size) || twa_misaligned_to(x, size) || twa_misaligned_to(dx, size) ||
+      twa_misaligned_to(w, twa_dtype_size(w_dtype)) || twa_misaligned_to(mean, 4) || twa_misaligned_to(rstd, 4) ||
+      twa_misaligned_to(dw, twa_dtype_size(g_dtype)) || twa_misaligned_to(db, twa_dtype_size(g_dtype)))
+    return TWA_ERR_MISALIGNED;
+  const bool weights = dw || db;
+  if (weights) {
+    if (!ws || ws_bytes < twa_layer_norm_workspace_bytes(rows, cols)) return TWA_ERR_WORKSPACE;
+    if (twa_misaligned_to(ws, 16)) return TWA_ERR_MISALIGNED;
+  }
+  TWA_CUDA_OK(ctx, cudaSetDevice(ctx->device));
+  LnArgs a = {x, dy, dx, w, nullptr, const_cast<float*>(mean), const_cast<float*>(rstd),
+              weights ? static_cast<float*>(ws) : nullptr, ldx, lddy, lddx, rows, cols, w_dtype, 5, 0, 0.0f};
+  int parts = 0;
+  if (rows) {
+    const int classes = ln_classes(x, ldx, dy, lddy, dx, lddx, rows, cols, size);
+    LnPlan p;
+    rc = dtype == TWA_BF16 ? ln_plan<bf16, true>(ctx, classes, rows, cols, &p) : ln_plan<float, true>(ctx, classes, rows, cols, &p);
+    if (rc) return rc;
+    a.log_lanes = p.log_lanes;
+  a.log_classes = p.log_classes;
+    if (p.kernel) {
+      parts = p.blocks;
+      twa_launch(ctx->stream, p.kernel, p.blocks, p.threads, p.smem, a);
+    } else {
+      const int blocks = static_cast<int>(rows < 8LL * ctx->sm_count ? rows : 8LL * ctx->sm_count);
+      if (weights) {
+        parts = static_cast<int>(rows < 64 ? rows : 64);
+        const dim3 grid(static_cast<unsigned>(twa_ceil_div(cols, 256)), parts);
+        if (dtype == TWA_BF16) twa_launch(ctx->stream, ln_weights_loop_kernel<bf16>, grid, 256, 0, a);
+        else twa_launch(ctx->stream, ln_weights_loop_kernel<float>, grid, 256, 0, a);
+        TWA_CUDA_OK(ctx, cudaGetLastError());
+      }
+      if (dtype == TWA_BF16) twa_launch(ctx->stream, ln_backward_loop_kernel<bf16>, blocks, LN_LOOP_THREADS, 0, a);
+      else twa_launch(ctx->stream, ln_backward_loop_kernel<float>, blocks, LN_LOOP_THREADS, 0, a);
+    }
+    TWA_CUDA_OK(ctx, cudaGetLastError());
+  }
+  if (weights) {
+    twa_launch(ctx->stream, ln_sum_kernel, static_cast<unsigned>(twa_ceil_div(2LL * cols, 32)), 32 * LN_SUM_WARPS, 0, static_cast<const float*>(ws), parts, cols, dw, db, g_dtype, accumulate);
+    TWA_CUDA_OK(ctx, cudaGetLastError());
+  }
+  return TWA_OK;
+}
+
+}  // extern "C"

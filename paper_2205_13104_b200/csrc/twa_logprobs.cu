@@ -52,29 +52,6 @@ __device__ __forceinline__ float lp_exp2(float x) {
   return r;
 }
 
-// Pairs of floats, two sums or products an instruction.
-__device__ __forceinline__ u64 lp_pair(float lo, float hi) {
-  u64 r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-  return r;
-}
-__device__ __forceinline__ void lp_unpair(u64 v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
-__device__ __forceinline__ u64 lp_fma2(u64 a, u64 b, u64 c) {
-  u64 r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-__device__ __forceinline__ u64 lp_add2(u64 a, u64 b) {
-  u64 r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ u64 lp_mul2(u64 a, u64 b) {
-  u64 r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-
 // The four words of a 16-byte unit: the maximum of the elements of two words, elements raised to -2^126 (NaN stays), a
 // word's elements widened to pairs of floats.
 template <typename T>
@@ -94,7 +71,7 @@ struct LpWord<bf16> {
     return r;
   }
   static constexpr int PAIRS = 4;                            // of a unit
-  static __device__ __forceinline__ u64 pair(const uint32_t* w, int i) { return lp_pair(twa_bf16_lo(w[i]), twa_bf16_hi(w[i])); }
+  static __device__ __forceinline__ u64 pair(const uint32_t* w, int i) { return twa_pair(twa_bf16_lo(w[i]), twa_bf16_hi(w[i])); }
 };
 template <>
 struct LpWord<float> {
@@ -110,7 +87,7 @@ struct LpWord<float> {
   }
   static constexpr int PAIRS = 2;
   static __device__ __forceinline__ u64 pair(const uint32_t* w, int i) {
-    return lp_pair(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+    return twa_pair(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
   }
 };
 
@@ -352,7 +329,7 @@ __device__ __forceinline__ void lp_bulk_load(uint32_t dst, const void* src, uint
 
 // A row per cluster of 2^log_parts blocks, each a run of its units; with one part a block goes on to further rows.
 template <typename T, bool ENT, bool TOP>
-__global__ void __launch_bounds__(LP_BLOCK, LP_BLOCKS_PER_SM<TOP>) logprobs_kernel(const LpArgs a, const int log_parts) {
+__global__ void __launch_bounds__(LP_BLOCK, LP_BLOCKS_PER_SM<TOP>) logprobs_kernel(LpArgs a, const int log_parts) {
   constexpr int E = twa_vec<T>;
   const int parts = 1 << log_parts;
   typedef LpWord<T> W;
@@ -375,6 +352,7 @@ __global__ void __launch_bounds__(LP_BLOCK, LP_BLOCKS_PER_SM<TOP>) logprobs_kern
     twa_fence_barrier_init();
   }
   __syncthreads();
+  twa_begin(a.logits, a.targets);
   const T* logits = static_cast<const T*>(a.logits);
 
   if (warp == LP_COPY) {
@@ -607,9 +585,9 @@ __global__ void __launch_bounds__(LP_BLOCK, LP_BLOCKS_PER_SM<TOP>) logprobs_kern
     // the sums become relative to the new maximum um
     auto raise_max = [&](float um, int at) {
       const float nc = lp_base(um) * LOG2E, d = fmaxf(c - nc, -150.0f), f = lp_exp2(d);
-      const u64 f2 = lp_pair(f, f);
-      if (ENT) w2 = lp_mul2(f2, lp_fma2(lp_pair(d, d), s2, w2));
-      s2 = lp_mul2(f2, s2);
+      const u64 f2 = twa_pair(f, f);
+      if (ENT) w2 = twa_mul2(f2, twa_fma2(twa_pair(d, d), s2, w2));
+      s2 = twa_mul2(f2, s2);
       m = um;
       c = nc;
       place = at;
@@ -626,7 +604,7 @@ __global__ void __launch_bounds__(LP_BLOCK, LP_BLOCKS_PER_SM<TOP>) logprobs_kern
         for (int j = 0; j < half; ++j) high[j] = W::max2(high[j], high[j + half]);
       const float um = W::max1(high[0]);
       if (um > m) raise_max(um, at);
-      const u64 c2 = lp_pair(-c, -c), l2 = lp_pair(LOG2E, LOG2E);
+      const u64 c2 = twa_pair(-c, -c), l2 = twa_pair(LOG2E, LOG2E);
 #pragma unroll
       for (int j = 0; j < N; ++j) {
         uint32_t w[4] = {units[j].x, units[j].y, units[j].z, units[j].w};
@@ -635,12 +613,12 @@ __global__ void __launch_bounds__(LP_BLOCK, LP_BLOCKS_PER_SM<TOP>) logprobs_kern
           for (int i = 0; i < 4; ++i) w[i] = W::raise(w[i]);
 #pragma unroll
         for (int i = 0; i < W::PAIRS; ++i) {
-          const u64 d2 = lp_fma2(W::pair(w, i), l2, c2);
+          const u64 d2 = twa_fma2(W::pair(w, i), l2, c2);
           float d0, d1;
-          lp_unpair(d2, d0, d1);
-          const u64 p2 = lp_pair(lp_exp2(d0), lp_exp2(d1));
-          s2 = lp_add2(s2, p2);
-          if (ENT) w2 = lp_fma2(p2, d2, w2);
+          twa_unpair(d2, d0, d1);
+          const u64 p2 = twa_pair(lp_exp2(d0), lp_exp2(d1));
+          s2 = twa_add2(s2, p2);
+          if (ENT) w2 = twa_fma2(p2, d2, w2);
         }
       }
     };
@@ -653,8 +631,8 @@ __global__ void __launch_bounds__(LP_BLOCK, LP_BLOCKS_PER_SM<TOP>) logprobs_kern
         some = true;
         if (z > m) raise_max(z, at);
         const float d = fmaf(z, LOG2E, -c), p = lp_exp2(d);
-        s2 = lp_add2(s2, lp_pair(p, 0.0f));
-        if (ENT) w2 = lp_fma2(lp_pair(p, 0.0f), lp_pair(fmaxf(d, -150.0f), 0.0f), w2);
+        s2 = twa_add2(s2, twa_pair(p, 0.0f));
+        if (ENT) w2 = twa_fma2(twa_pair(p, 0.0f), twa_pair(fmaxf(d, -150.0f), 0.0f), w2);
       }
     };
     if (ends == 0) take_ends(u0);
@@ -687,8 +665,8 @@ __global__ void __launch_bounds__(LP_BLOCK, LP_BLOCKS_PER_SM<TOP>) logprobs_kern
     LpStat st = {m, 0.0f, 0.0f};
     {
       float s0, s1, w0, w1;
-      lp_unpair(s2, s0, s1);
-      lp_unpair(w2, w0, w1);
+      twa_unpair(s2, s0, s1);
+      twa_unpair(w2, w0, w1);
       st.s = s0 + s1;
       st.a = w0 + w1;
       const float e = fmaf(lp_base(m), LOG2E, -c), g = e * LN2;      // c is off by e, at most 2^-11: 2^-e = 1 - g + g^2 / 2
@@ -713,7 +691,8 @@ constexpr int LPB_THREADS = 256;
 
 // Rows x parts blocks; SAME: logits and dlogits rows lie alike on 16-byte boundaries, else element by element.
 template <typename T, bool ENT, bool SAME>
-__global__ void __launch_bounds__(LPB_THREADS) logprobs_backward_kernel(const LpArgs a, const int parts) {
+__global__ void __launch_bounds__(LPB_THREADS) logprobs_backward_kernel(LpArgs a, const int parts) {
+  twa_begin(a.logits, a.targets, a.lse, a.entropy, a.d_logp, a.d_entropy);
   constexpr int E = twa_vec<T>;
   const long long row = blockIdx.x / parts;
   const int part = static_cast<int>(blockIdx.x - row * parts);
@@ -774,12 +753,14 @@ int lp_launch(twa_ctx* ctx, const LpArgs& a, int log_parts) {
   cfg.blockDim = dim3(LP_BLOCK);
   cfg.dynamicSmemBytes = sizeof(LpShared<TOP>);
   cfg.stream = ctx->stream;
-  cudaLaunchAttribute attr = {};
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = parts;
-  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = parts > 1 ? 1 : 0;
+  cudaLaunchAttribute attr[2] = {};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = parts;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = parts > 1 ? 2 : 1;
   TWA_CUDA_OK(ctx, cudaLaunchKernelEx(&cfg, logprobs_kernel<T, ENT, TOP>, a, log_parts));
   return TWA_OK;
 }
@@ -793,8 +774,8 @@ int lp_launch_any(twa_ctx* ctx, const LpArgs& a, int log_parts) {
 template <typename T, bool ENT>
 void lp_launch_backward(twa_ctx* ctx, const LpArgs& a, int parts, bool same) {
   const unsigned blocks = static_cast<unsigned>(a.rows * parts);
-  if (same) logprobs_backward_kernel<T, ENT, true><<<blocks, LPB_THREADS, 0, ctx->stream>>>(a, parts);
-  else logprobs_backward_kernel<T, ENT, false><<<blocks, LPB_THREADS, 0, ctx->stream>>>(a, parts);
+  if (same) twa_launch(ctx->stream, logprobs_backward_kernel<T, ENT, true>, blocks, LPB_THREADS, 0, a, parts);
+  else twa_launch(ctx->stream, logprobs_backward_kernel<T, ENT, false>, blocks, LPB_THREADS, 0, a, parts);
 }
 
 int lp_check(const twa_ctx* ctx, twa_dtype dt, twa_itype it, int64_t rows, int vocab) {

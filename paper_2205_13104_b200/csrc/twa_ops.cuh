@@ -30,14 +30,15 @@ __device__ __forceinline__ bf16 twa_from_float<bf16>(float v) { return __float2b
 
 // Element i of an array whose type is known at run time.
 __device__ __forceinline__ float twa_load_any(const void* p, int dtype, long long i) {
-  return dtype == TWA_BF16 ? twa_to_float(static_cast<const bf16*>(p)[i]) : static_cast<const float*>(p)[i];
+  return dtype == TWA_BF16 ? __uint_as_float(static_cast<uint32_t>(__ldg(static_cast<const unsigned short*>(p) + i)) << 16)
+                           : __ldg(static_cast<const float*>(p) + i);
 }
 __device__ __forceinline__ void twa_store_any(void* p, int dtype, long long i, float v) {
   if (dtype == TWA_BF16) static_cast<bf16*>(p)[i] = twa_from_float<bf16>(v);
   else static_cast<float*>(p)[i] = v;
 }
 __device__ __forceinline__ long long twa_load_id(const void* p, int itype, long long i) {
-  return itype == TWA_I64 ? static_cast<const long long*>(p)[i] : static_cast<long long>(static_cast<const int*>(p)[i]);
+  return itype == TWA_I64 ? __ldg(static_cast<const long long*>(p) + i) : static_cast<long long>(__ldg(static_cast<const int*>(p) + i));
 }
 
 // E consecutive elements as they lie in memory: E = 1, or 16 bytes (E = 4 float, 8 bfloat16; the address on 16
@@ -94,4 +95,62 @@ __device__ __forceinline__ float twa_warp_sum(float v) {
 #pragma unroll
   for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
+}
+
+// Pairs of floats: two sums or products an instruction.
+typedef unsigned long long twa_f2;
+__device__ __forceinline__ twa_f2 twa_pair(float lo, float hi) {
+  twa_f2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ twa_f2 twa_pair(float both) { return twa_pair(both, both); }
+__device__ __forceinline__ void twa_unpair(twa_f2 v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ float twa_pair_sum(twa_f2 v) {
+  float lo, hi;
+  twa_unpair(v, lo, hi);
+  return lo + hi;
+}
+__device__ __forceinline__ twa_f2 twa_fma2(twa_f2 a, twa_f2 b, twa_f2 c) {
+  twa_f2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ twa_f2 twa_add2(twa_f2 a, twa_f2 b) {
+  twa_f2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ twa_f2 twa_mul2(twa_f2 a, twa_f2 b) {
+  twa_f2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
+// Launches that may begin while the kernel before them in the stream ends (programmatic dependent launch).  A kernel launched
+// so first calls twa_begin(pointers it reads ...): the next kernel's blocks may take free places from here on, and this one goes on
+// when the kernels before it are complete and their writes visible.  The pointers come out of the call as new values, so that
+// no load through them, not even one of data the compiler takes for constant, can be moved before it.
+template <typename P>
+__device__ __forceinline__ void twa_renew(P& pointer) { asm volatile("" : "+l"(pointer) : : "memory"); }
+template <typename... P>
+__device__ __forceinline__ void twa_begin(P&... pointers) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  (..., twa_renew(pointers));
+}
+
+template <typename... Params, typename... Args>
+cudaError_t twa_launch(cudaStream_t stream, void (*kernel)(Params...), dim3 grid, int threads, size_t smem, Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr = {};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);
 }

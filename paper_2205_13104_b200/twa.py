@@ -17,7 +17,7 @@ _ROOT = os.path.dirname(_HERE)
 LIB_PATH = os.path.join(_HERE, "libtwa.so")
 CSRC = os.path.join(_HERE, "csrc")
 SOURCES = ["twa_api.cu", "twa_basis.cu", "twa_chunked.cu", "twa_layered_build.cu", "twa_layered_step.cu", "twa_project_batch.cu", "twa_panel.cu", "twa_stream.cu",
-           "twa_stream_mma.cu", "twa_noalloc.cu", "twa_layer_norm.cu", "twa_embedding.cu", "twa_logprobs.cu", "twa_clip.cu"]
+           "twa_stream_mma.cu", "twa_noalloc.cu", "twa_layer_norm.cu", "twa_layer_norm_backward.cu", "twa_embedding.cu", "twa_logprobs.cu", "twa_clip.cu"]
 
 TWA_MAX_N = 128
 TWA_OK = 0
