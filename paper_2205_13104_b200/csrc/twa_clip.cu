@@ -17,24 +17,25 @@
 namespace {
 
 constexpr int CLIP_TENSORS = 512;       // tensors of one launch
-constexpr int CLIP_CHUNK = 16384;       // elements
+constexpr int CLIP_FEW = 32;            // a smaller table, which costs less to hand over
+constexpr int CLIP_CHUNK = 8192;        // elements
 constexpr int CLIP_THREADS = 256;
+constexpr int CLIP_SM_BLOCKS = 5;       // blocks an SM
 constexpr int CLIP_MAX_BLOCKS = 148 * 8;
 constexpr int CLIP_HEAD = 256;          // bytes of the workspace before the partial sums: the factor
 
+template <int N>
 struct ClipTable {
-  const void* data[CLIP_TENSORS];
-  long long flat[CLIP_TENSORS];         // where the tensor begins in the flat vector
-  int chunk[CLIP_TENSORS + 1];          // first chunk of each tensor, and the number of chunks
-  unsigned char dtype[CLIP_TENSORS];
+  const void* data[N];
+  long long flat[N + 1];                // where the tensor begins in the flat vector, and where the last one ends
+  int chunk[N + 1];                     // first chunk of each tensor, and the number of chunks
+  unsigned char dtype[N];
   int count;
-};
-struct ClipSizes {                       // elements of each tensor
-  long long size[CLIP_TENSORS];
 };
 
 // Tensor that chunk q belongs to.
-__device__ __forceinline__ int clip_find(const ClipTable& t, int q) {
+template <int N>
+__device__ __forceinline__ int clip_find(const ClipTable<N>& t, int q) {
   int lo = 0, hi = t.count - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) / 2;
@@ -59,20 +60,29 @@ __device__ __forceinline__ double clip_square_sum(const T* p, int n) {
     sum += static_cast<double>(v * v);
   }
   constexpr int AHEAD = 4;
-  for (int u0 = threadIdx.x; u0 < units; u0 += AHEAD * CLIP_THREADS) {
+  const T* from = p + head + threadIdx.x * E;
+  int left = units - static_cast<int>(threadIdx.x);
+  auto squares = [&](const twa_pack<T, E>& q) {
+    float v[E], s = 0.0f;
+    q.widen(v);
+#pragma unroll
+    for (int e = 0; e < E; ++e) s += v[e] * v[e];
+    sum += static_cast<double>(s);
+  };
+  for (; left > (AHEAD - 1) * CLIP_THREADS; left -= AHEAD * CLIP_THREADS) {
     twa_pack<T, E> q[AHEAD];
 #pragma unroll
-    for (int k = 0; k < AHEAD; ++k)
-      if (u0 + k * CLIP_THREADS < units) q[k].load(p + head + (u0 + k * CLIP_THREADS) * E);
+    for (int k = 0; k < AHEAD; ++k) q[k].load(from + k * CLIP_THREADS * E);
 #pragma unroll
-    for (int k = 0; k < AHEAD; ++k) {
-      if (u0 + k * CLIP_THREADS >= units) break;
-      float v[E], s = 0.0f;
-      q[k].widen(v);
-#pragma unroll
-      for (int e = 0; e < E; ++e) s += v[e] * v[e];
-      sum += static_cast<double>(s);
-    }
+    for (int k = 0; k < AHEAD; ++k) squares(q[k]);
+    from += AHEAD * CLIP_THREADS * E;
+  }
+#pragma unroll 1
+  for (; left > 0; left -= CLIP_THREADS) {
+    twa_pack<T, E> q;
+    q.load(from);
+    squares(q);
+    from += CLIP_THREADS * E;
   }
   return sum;
 }
@@ -89,9 +99,8 @@ __device__ __forceinline__ double clip_block_sum(double v, double* red) {
 }
 
 // Partial sums of this launch's tensors to part[base + block]; the last block of the last launch adds all `total` of them.
-__global__ void __launch_bounds__(CLIP_THREADS) clip_norm_kernel(const __grid_constant__ ClipTable t,
-                                                                 const __grid_constant__ ClipSizes z, double* part, int base,
-                                                                 int total, unsigned* ticket, float max_norm, float eps,
+template <int N>
+__global__ void __launch_bounds__(CLIP_THREADS, CLIP_SM_BLOCKS) clip_norm_kernel(const __grid_constant__ ClipTable<N> t, double* part, int base, int total, unsigned* ticket, float max_norm, float eps,
                                                                  float* norm_out, float* factor, int* status) {
   twa_begin(part, ticket, norm_out, factor);
   __shared__ double red[CLIP_THREADS / 32];
@@ -104,7 +113,7 @@ __global__ void __launch_bounds__(CLIP_THREADS) clip_norm_kernel(const __grid_co
   for (int q = from; q < to; ++q) {
     while (t.chunk[i + 1] <= q) ++i;
     const long long off = static_cast<long long>(q - t.chunk[i]) * CLIP_CHUNK;
-    const int n = static_cast<int>(min(static_cast<long long>(CLIP_CHUNK), z.size[i] - off));
+    const int n = static_cast<int>(min(static_cast<long long>(CLIP_CHUNK), t.flat[i + 1] - t.flat[i] - off));
     const void* data = t.data[i];
     twa_renew(data);
     sum += t.dtype[i] == TWA_BF16 ? clip_square_sum(static_cast<const bf16*>(data) + off, n)
@@ -131,35 +140,77 @@ __global__ void __launch_bounds__(CLIP_THREADS) clip_norm_kernel(const __grid_co
   }
 }
 
+// 8 elements of a thread and AHEAD such loads under way at once where both lie on 16 bytes, else element by element, SINGLY loads
+// at once.
 template <typename T, typename TO>
 __device__ __forceinline__ void clip_scale(const T* p, TO* o, int n, float f) {
-  constexpr int E = 8;
+  constexpr int E = 8, PACK = twa_vec<T>, PACKS = E / PACK, AHEAD = 4 / PACKS, SINGLY = 8;
+  typedef twa_pack<T, PACK> Pack;
+  auto eight = [&](const Pack (&q)[PACKS], TO* to) {
+    float v[E];
+#pragma unroll
+    for (int k = 0; k < PACKS; ++k) q[k].widen(v + k * PACK);
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] *= f;
+#pragma unroll
+    for (int k = 0; k < E; k += twa_vec<TO>) twa_pack<TO, twa_vec<TO>>::store(to + k, v + k);
+  };
+  int j = threadIdx.x;
   if (((reinterpret_cast<uintptr_t>(p) | reinterpret_cast<uintptr_t>(o)) & 15) == 0) {
     const int units = n / E;
-    for (int u = threadIdx.x; u < units; u += CLIP_THREADS) {
-      float v[E];
+    const T* from = p + threadIdx.x * E;
+    TO* to = o + threadIdx.x * E;
+    int left = units - static_cast<int>(threadIdx.x);
+    for (; left > (AHEAD - 1) * CLIP_THREADS; left -= AHEAD * CLIP_THREADS) {
+      Pack q[AHEAD][PACKS];
 #pragma unroll
-      for (int k = 0; k < E; k += twa_vec<T>) {
-        twa_pack<T, twa_vec<T>> q;
-        q.load(p + u * E + k);
-        q.widen(v + k);
-      }
+      for (int i = 0; i < AHEAD; ++i)
 #pragma unroll
-      for (int e = 0; e < E; ++e) v[e] *= f;
+        for (int k = 0; k < PACKS; ++k) q[i][k].load(from + i * CLIP_THREADS * E + k * PACK);
 #pragma unroll
-      for (int k = 0; k < E; k += twa_vec<TO>) twa_pack<TO, twa_vec<TO>>::store(o + u * E + k, v + k);
+      for (int i = 0; i < AHEAD; ++i) eight(q[i], to + i * CLIP_THREADS * E);
+      from += AHEAD * CLIP_THREADS * E;
+      to += AHEAD * CLIP_THREADS * E;
     }
-    const int j = units * E + threadIdx.x;
-    if (j < n) o[j] = twa_from_float<TO>(twa_to_float(p[j]) * f);
-  } else {
-    for (int j = threadIdx.x; j < n; j += CLIP_THREADS) o[j] = twa_from_float<TO>(twa_to_float(p[j]) * f);
+#pragma unroll 1
+    for (; left > 0; left -= CLIP_THREADS) {
+      Pack q[PACKS];
+#pragma unroll
+      for (int k = 0; k < PACKS; ++k) q[k].load(from + k * PACK);
+      eight(q, to);
+      from += CLIP_THREADS * E;
+      to += CLIP_THREADS * E;
+    }
+    j += units * E;
+  }
+  const T* from = p + j;
+  TO* to = o + j;
+  int left = n - j;
+  for (; left > (SINGLY - 1) * CLIP_THREADS; left -= SINGLY * CLIP_THREADS) {
+    twa_pack<T, 1> q[SINGLY];
+#pragma unroll
+    for (int i = 0; i < SINGLY; ++i) q[i].load(from + i * CLIP_THREADS);
+#pragma unroll
+    for (int i = 0; i < SINGLY; ++i) {
+      float v[1];
+      q[i].widen(v);
+      to[i * CLIP_THREADS] = twa_from_float<TO>(v[0] * f);
+    }
+    from += SINGLY * CLIP_THREADS;
+    to += SINGLY * CLIP_THREADS;
+  }
+#pragma unroll 1
+  for (; left > 0; left -= CLIP_THREADS) {
+    *to = twa_from_float<TO>(twa_to_float(*from) * f);
+    from += CLIP_THREADS;
+    to += CLIP_THREADS;
   }
 }
 
 // out == null: in place.
-__global__ void __launch_bounds__(CLIP_THREADS) clip_scale_kernel(const __grid_constant__ ClipTable t,
-                                                                  const __grid_constant__ ClipSizes z,
-                                                                  const float* __restrict__ factor, void* out, int out_dtype) {
+template <int N>
+__global__ void __launch_bounds__(CLIP_THREADS, CLIP_SM_BLOCKS) clip_scale_kernel(const __grid_constant__ ClipTable<N> t, const float* __restrict__ factor,
+                                                                  void* out, int out_dtype) {
   twa_begin(factor, out);
   const float f = __ldg(factor);
   if (!out && f == 1.0f) return;
@@ -170,7 +221,7 @@ __global__ void __launch_bounds__(CLIP_THREADS) clip_scale_kernel(const __grid_c
   for (int q = to - 1; q >= from; --q) {
     while (t.chunk[i] > q) --i;
     const long long off = static_cast<long long>(q - t.chunk[i]) * CLIP_CHUNK;
-    const int n = static_cast<int>(min(static_cast<long long>(CLIP_CHUNK), z.size[i] - off));
+    const int n = static_cast<int>(min(static_cast<long long>(CLIP_CHUNK), t.flat[i + 1] - t.flat[i] - off));
     const long long at = t.flat[i] + off;
     void* data = const_cast<void*>(t.data[i]);
     twa_renew(data);
@@ -201,66 +252,66 @@ int clip_check(const twa_ctx* ctx, const twa_tensors* t) {
 }
 
 // Fills the table of one launch from tensor `first` on; returns the first tensor that is not in it.
-int clip_fill(const twa_tensors* s, int first, long long* flat, ClipTable* t, ClipSizes* z) {
+template <int N>
+int clip_fill(const twa_tensors* s, int first, long long* flat, ClipTable<N>* t) {
   int i = first;
   t->count = 0;
   t->chunk[0] = 0;
-  for (; i < s->count && t->count < CLIP_TENSORS; ++i) {
+  for (; i < s->count && t->count < N; ++i) {
     const long long n = s->sizes[i];
-    if (n) {
-      const int k = t->count++;
-      t->data[k] = s->data[i];
-      t->flat[k] = *flat;
-      t->dtype[k] = static_cast<unsigned char>(s->dtypes[i]);
-      z->size[k] = n;
-      t->chunk[k + 1] = t->chunk[k] + static_cast<int>(twa_ceil_div(n, CLIP_CHUNK));
-    }
+    if (!n) continue;
+    const int k = t->count++;
+    t->data[k] = s->data[i];
+    t->flat[k] = *flat;
+    t->dtype[k] = static_cast<unsigned char>(s->dtypes[i]);
+    t->chunk[k + 1] = t->chunk[k] + static_cast<int>(twa_ceil_div(n, CLIP_CHUNK));
     *flat += n;
+    t->flat[k + 1] = *flat;
   }
   return i;
 }
 
 int clip_blocks(const twa_ctx* ctx, int chunks) {
-  int most = 8 * ctx->sm_count;
+  int most = CLIP_SM_BLOCKS * ctx->sm_count;
   if (most > CLIP_MAX_BLOCKS) most = CLIP_MAX_BLOCKS;
   return chunks < 1 ? 1 : (chunks < most ? chunks : most);
 }
 
+template <int N>
 int clip_run(twa_ctx* ctx, const twa_tensors* s, float max_norm, float eps, bool scale, void* out, int out_dtype, float* norm,
+             void* ws) {
+  float* factor = static_cast<float*>(ws);
+  double* part = reinterpret_cast<double*>(static_cast<char*>(ws) + CLIP_HEAD);
+  ClipTable<N> t;
+  int base = 0, next = 0, launches = 0;
+  long long flat = 0;
+  do {
+    next = clip_fill(s, next, &flat, &t);
+    const int blocks = clip_blocks(ctx, t.chunk[t.count]);
+    TWA_CUDA_OK(ctx, twa_launch(ctx->stream, clip_norm_kernel<N>, blocks, CLIP_THREADS, 0, t, part, base,
+                                next < s->count ? 0 : base + blocks, ctx->d_ticket, max_norm, eps, norm, scale ? factor : nullptr,
+                                ctx->d_status));
+    base += blocks;
+    ++launches;
+  } while (next < s->count);
+  if (!scale) return TWA_OK;
+  next = launches == 1 ? next : 0;
+  flat = 0;
+  do {
+    if (launches > 1) next = clip_fill(s, next, &flat, &t);       // else the table is still there
+    TWA_CUDA_OK(ctx, twa_launch(ctx->stream, clip_scale_kernel<N>, clip_blocks(ctx, t.chunk[t.count]), CLIP_THREADS, 0, t, factor,
+                                out, out_dtype));
+  } while (next < s->count);
+  return TWA_OK;
+}
+
+int clip_any(twa_ctx* ctx, const twa_tensors* s, float max_norm, float eps, bool scale, void* out, int out_dtype, float* norm,
              void* ws, size_t ws_bytes) {
   if (!ws || ws_bytes < twa_grad_norm_workspace_bytes(s->count)) return TWA_ERR_WORKSPACE;
   if (twa_misaligned_to(ws, 16)) return TWA_ERR_MISALIGNED;
   TWA_CUDA_OK(ctx, cudaSetDevice(ctx->device));
-  float* factor = static_cast<float*>(ws);
-  double* part = reinterpret_cast<double*>(static_cast<char*>(ws) + CLIP_HEAD);
-  ClipTable t;
-  ClipSizes z;
-  int base = 0, next = 0;
-  long long flat = 0;
-  do {
-    next = clip_fill(s, next, &flat, &t, &z);
-    const int blocks = clip_blocks(ctx, t.chunk[t.count]);
-    const bool end = next >= s->count;
-    twa_launch(ctx->stream, clip_norm_kernel, blocks, CLIP_THREADS, 0, t, z, part, base, end ? base + blocks : 0, ctx->d_ticket, max_norm,
-                                                               eps, norm, scale ? factor : nullptr, ctx->d_status);
-    base += blocks;
-  } while (next < s->count);
-  TWA_CUDA_OK(ctx, cudaGetLastError());
-  if (!scale) return TWA_OK;
-  // last launch first; its table is still filled when there was one launch only
-  const int launches = s->count > CLIP_TENSORS ? 2 : 1;
-  if (launches == 1) {
-    twa_launch(ctx->stream, clip_scale_kernel, clip_blocks(ctx, t.chunk[t.count]), CLIP_THREADS, 0, t, z, factor, out, out_dtype);
-  } else {
-    next = 0;
-    flat = 0;
-    while (next < s->count) {
-      next = clip_fill(s, next, &flat, &t, &z);
-      twa_launch(ctx->stream, clip_scale_kernel, clip_blocks(ctx, t.chunk[t.count]), CLIP_THREADS, 0, t, z, factor, out, out_dtype);
-    }
-  }
-  TWA_CUDA_OK(ctx, cudaGetLastError());
-  return TWA_OK;
+  if (s->count <= CLIP_FEW) return clip_run<CLIP_FEW>(ctx, s, max_norm, eps, scale, out, out_dtype, norm, ws);
+  return clip_run<CLIP_TENSORS>(ctx, s, max_norm, eps, scale, out, out_dtype, norm, ws);
 }
 
 }  // namespace
@@ -278,7 +329,7 @@ int twa_grad_norm(twa_ctx* ctx, const twa_tensors* tensors, float* norm, void* w
   if (rc) return rc;
   if (!norm) return TWA_ERR_INVALID_ARG;
   if (twa_misaligned_to(norm, 4)) return TWA_ERR_MISALIGNED;
-  return clip_run(ctx, tensors, 1.0f, 0.0f, false, nullptr, TWA_F32, norm, ws, ws_bytes);
+  return clip_any(ctx, tensors, 1.0f, 0.0f, false, nullptr, TWA_F32, norm, ws, ws_bytes);
 }
 
 int twa_clip_gather(twa_ctx* ctx, const twa_tensors* tensors, float max_norm, float eps, void* g, twa_dtype g_dtype, float* norm,
@@ -287,7 +338,7 @@ int twa_clip_gather(twa_ctx* ctx, const twa_tensors* tensors, float max_norm, fl
   if (rc) return rc;
   if (!norm || !g || !twa_dtype_ok(g_dtype) || !(max_norm > 0.0f) || !(eps >= 0.0f)) return TWA_ERR_INVALID_ARG;
   if (twa_misaligned_to(norm, 4) || twa_misaligned_to(g, twa_dtype_size(g_dtype))) return TWA_ERR_MISALIGNED;
-  return clip_run(ctx, tensors, max_norm, eps, true, g, g_dtype, norm, ws, ws_bytes);
+  return clip_any(ctx, tensors, max_norm, eps, true, g, g_dtype, norm, ws, ws_bytes);
 }
 
 int twa_clip_grads(twa_ctx* ctx, const twa_tensors* tensors, float max_norm, float eps, float* norm, void* ws, size_t ws_bytes) {
@@ -295,7 +346,7 @@ int twa_clip_grads(twa_ctx* ctx, const twa_tensors* tensors, float max_norm, flo
   if (rc) return rc;
   if (!norm || !(max_norm > 0.0f) || !(eps >= 0.0f)) return TWA_ERR_INVALID_ARG;
   if (twa_misaligned_to(norm, 4)) return TWA_ERR_MISALIGNED;
-  return clip_run(ctx, tensors, max_norm, eps, true, nullptr, TWA_F32, norm, ws, ws_bytes);
+  return clip_any(ctx, tensors, max_norm, eps, true, nullptr, TWA_F32, norm, ws, ws_bytes);
 }
 
 }  // extern "C"

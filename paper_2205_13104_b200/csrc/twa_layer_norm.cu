@@ -41,7 +41,7 @@ __global__ void __launch_bounds__(LN_THREADS<PER>, 512 / LN_THREADS<PER>) ln_for
     if (r >= a.rows) return;
 #pragma unroll
     for (int k = 0; k < NV; ++k)
-      if (at.in(k)) at.load(raw[k], x + r * a.ldx, k);
+      if (at.in(k)) at.load(raw[k], x + r * a.ldx, k, r > 0 && r + 1 < a.rows);
   };
   fetch(at.first + at.group);
   ln_stage<E>(w, a.w, a.w_dtype, at.skew, a.cols, 1.0f);
@@ -66,6 +66,7 @@ __global__ void __launch_bounds__(LN_THREADS<PER>, 512 / LN_THREADS<PER>) ln_for
     for (int k = 0; k < NV; ++k) {
       if ((!ALONE && r >= a.rows) || !at.in(k)) raw[k] = twa_pack<T, E>{};
       raw[k].widen(f + k * E);
+      at.keep_valid(k, f + k * E);
     }
 #pragma unroll
     for (int i = 0; i < P; ++i) {
@@ -283,7 +284,7 @@ int twa_layer_norm(twa_ctx* ctx, const void* x, int64_t ldx, twa_dtype dtype, co
       twa_misaligned_to(mean, 4) || twa_misaligned_to(rstd, 4))
     return TWA_ERR_MISALIGNED;
   TWA_CUDA_OK(ctx, cudaSetDevice(ctx->device));
-  LnArgs a = {x, nullptr, y, w, b, mean, rstd, nullptr, ldx, 0, ldy, rows, cols, w_dtype, 5, 0, eps};
+  LnArgs a = {x, nullptr, y, w, b, mean, rstd, nullptr, ldx, 0, ldy, rows, cols, w_dtype, 5, 0, eps, ctx->wait_limit_ns, ctx->d_status};
   const int classes = ln_classes(x, ldx, y, ldy, y, ldy, rows, cols, size);
   LnPlan p;
   rc = dtype == TWA_BF16 ? ln_plan<bf16, false>(ctx, classes, rows, cols, &p) : ln_plan<float, false>(ctx, classes, rows, cols, &p);

@@ -26,6 +26,8 @@ struct LnArgs {
   int log_lanes;       // a warp per row or less: log2 of the threads of a row
   int log_classes;     // rows lie in 2^log_classes ways on 16-byte boundaries; a block takes rows of one
   float eps;
+  unsigned long long wait_limit_ns;
+  int* status;
 };
 
 // Sum over the threads of a row, PER <= 32.
@@ -108,16 +110,25 @@ struct LnPlace {
   __device__ __forceinline__ bool whole(int k) const {
     return FULL || (E == 1 ? in(k) : unit(k) * E >= skew && (unit(k) + 1) * E <= skew + cols);
   }
-  // the unit of the row that begins at `row`; elements outside are 0
+  // The unit of the row that begins at `row`.  Of a unit that the row has in part, elements outside are what is beside the row in
+  // memory (`inner`: there are rows before and after it), or 0.
   template <typename T>
-  __device__ __forceinline__ void load(twa_pack<T, E>& p, const T* row, int k) const {
-    if (whole(k)) {
+  __device__ __forceinline__ void load(twa_pack<T, E>& p, const T* row, int k, bool inner) const {
+    if (E == 1 || inner || whole(k)) {
       p.load(row - skew + unit(k) * E);
-    } else if constexpr (E > 1) {
+    } else {
       float v[E];
 #pragma unroll
       for (int e = 0; e < E; ++e) v[e] = valid(k, e) ? twa_to_float(row[column(k, e)]) : 0.0f;
-      twa_pack<T, E>::store(reinterpret_cast<T*>(&p), v);
+      p.from(v);
+    }
+  }
+  // 0 for what is not of the row
+  __device__ __forceinline__ void keep_valid(int k, float* v) const {
+    if constexpr (!FULL) {
+      if (whole(k)) return;
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[e] = valid(k, e) ? v[e] : 0.0f;
     }
   }
   template <typename T>

@@ -3,49 +3,100 @@
 
 namespace {
 
-template <typename T, int E, int NV, int PER, bool FULL>
+// NV units a thread.  RING (rows on 16-byte boundaries, a warp or a block each): LN_RING_ROWS rows of x and dy are under way as bulk
+// copies into shared memory, which costs no registers; else the next row is on its way into registers.  FULL: as forward.
+template <int NV>
+constexpr int LN_RING_ROWS = NV >= 3 ? 2 : 4;      // 16 KB of x and dy a block of 128 threads either way, four blocks an SM
+template <typename T, int E, int NV, int PER, bool FULL, bool RING>
 __global__ void __launch_bounds__(LN_THREADS<PER>, 512 / LN_THREADS<PER>) ln_backward_kernel(LnArgs a) {
-  twa_begin(a.x, a.dy, a.w, a.mean, a.rstd);
+  constexpr bool WARP = PER <= 32, ALONE = PER != 0;   // ALONE: a warp's threads are all of one row
+  constexpr int LN_RING = LN_RING_ROWS<NV>;
+  constexpr int TEAMS = PER == 32 ? LN_WARP_THREADS / 32 : 1, ROW = PER * NV;      // rings of a block, units of a row in one
   __shared__ float red[2][32][2];
+  __shared__ unsigned long long full[RING ? TEAMS * LN_RING : 1];
+  __shared__ int gave_up;
   typedef LnPairs<E, NV> Q;
   constexpr int P = Q::P;
   int turn = 0;
-  constexpr bool WARP = PER <= 32, ALONE = PER != 0;   // ALONE: a warp's threads are all of one row
   const LnPlace<E, NV, PER, FULL> at(a, sizeof(T));
+  const LnPlane<E> w = {0, at.units()};
+  const int team = PER == 32 ? threadIdx.x >> 5 : 0;
+  const bool issuer = RING && (PER == 32 ? (threadIdx.x & 31) == 0 : threadIdx.x == 0);
+  uint4* ring = reinterpret_cast<uint4*>(ln_planes + 2 * at.units() * E) + team * LN_RING * 2 * ROW;
+  if (RING) {
+    if (threadIdx.x == 0) {
+      for (int q = 0; q < TEAMS * LN_RING; ++q) twa_mbar_init(twa_smem_u32(&full[q]), 1);
+      gave_up = 0;
+      twa_fence_barrier_init();
+    }
+    __syncthreads();
+  }
+  twa_begin(a.x, a.dy, a.w, a.mean, a.rstd);
   const T* x = static_cast<const T*>(a.x);
   const T* dy = static_cast<const T*>(a.dy);
   T* dx = static_cast<T*>(a.y);
-  const LnPlane<E> w = {0, at.units()};
   const float inv = 1.0f / static_cast<float>(a.cols);
   twa_f2 dw[P], db[P];
 #pragma unroll
   for (int i = 0; i < P; ++i) dw[i] = db[i] = 0;
   twa_pack<T, E> rx[NV] = {}, rd[NV] = {};             // what is beyond the row stays 0 in rd, and with it all that is added up
   float mean = 0.0f, rstd = 0.0f;
+  // copies of the team's i-th row, where there is one
+  auto issue = [&](int i) {
+    const long long r = at.first + i * at.step;
+    if (r >= a.rows) return;
+    const int q = i % LN_RING;
+    const uint32_t bytes = (FULL ? ROW : at.row_units) * 16;
+    unsigned long long* bar = &full[team * LN_RING + q];
+    twa_mbar_expect_tx(twa_smem_u32(bar), 2 * bytes);
+    twa_bulk_load(twa_smem_u32(ring + q * 2 * ROW), x + r * a.ldx, bytes, twa_smem_u32(bar));
+    twa_bulk_load(twa_smem_u32(ring + q * 2 * ROW + ROW), dy + r * a.lddy, bytes, twa_smem_u32(bar));
+  };
   auto fetch = [&](long long r) {
     if (r >= a.rows) return;
     mean = __ldg(a.mean + r);
     rstd = __ldg(a.rstd + r);
+    if (!RING)
 #pragma unroll
-    for (int k = 0; k < NV; ++k)
-      if (at.in(k)) {
-        at.load(rx[k], x + r * a.ldx, k);
-        at.load(rd[k], dy + r * a.lddy, k);
-      }
+      for (int k = 0; k < NV; ++k)
+        if (at.in(k)) {
+          const bool inner = r > 0 && r + 1 < a.rows;
+          at.load(rx[k], x + r * a.ldx, k, inner);
+          at.load(rd[k], dy + r * a.lddy, k, inner);
+        }
   };
+  if (issuer)
+    for (int i = 0; i < LN_RING; ++i) issue(i);
   fetch(at.first + at.group);
   ln_stage<E>(w, a.w, a.w_dtype, at.skew, a.cols, 1.0f);
   __syncthreads();
-  for (long long base = at.first; base < a.rows; base += at.step) {
+  int it = 0;
+  bool landed = true;
+  for (long long base = at.first; base < a.rows; base += at.step, ++it) {
     const long long r = base + at.group;
     twa_f2 h[P], v[P], s0 = 0, s1 = 0;
     const float rs = rstd;
+    if constexpr (RING) {
+      const int q = it % LN_RING;
+      // after a wait that ran out the results are not defined, and every later wait ends at once
+      landed &= twa_wait(&full[team * LN_RING + q], it / LN_RING & 1, &gave_up, a.wait_limit_ns);
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+        if (at.in(k)) {
+          rx[k].load_shared(ring + q * 2 * ROW + at.unit(k));
+          rd[k].load_shared(ring + q * 2 * ROW + ROW + at.unit(k));
+        }
+    }
     if (ALONE || r < a.rows) {
       float f[Q::N], d[Q::N], wv[Q::N];
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
         rx[k].widen(f + k * E);
         rd[k].widen(d + k * E);
+        if (!RING) {
+          at.keep_valid(k, f + k * E);
+          at.keep_valid(k, d + k * E);
+        }
         w.load(at.unit(k), wv + k * E);
       }
       const twa_f2 m2 = twa_pair(-mean), r2 = twa_pair(rs);
@@ -66,8 +117,10 @@ __global__ void __launch_bounds__(LN_THREADS<PER>, 512 / LN_THREADS<PER>) ln_bac
       s[0] = ln_sum_lanes<PER>(s[0], a.log_lanes);
       s[1] = ln_sum_lanes<PER>(s[1], a.log_lanes);
     } else {
-      block_sum<2>(s, red, turn);
+      block_sum<2>(s, red, turn);                      // and with its barrier the row has been read
     }
+    if (WARP) __syncwarp();
+    if (issuer) issue(it + LN_RING);
     if (ALONE || r < a.rows) {
       // rstd (v - c1 - h c2)
       const twa_f2 c1 = twa_pair(-s[0] * inv), c2 = twa_pair(-s[1] * inv), r2 = twa_pair(rs);
@@ -78,6 +131,16 @@ __global__ void __launch_bounds__(LN_THREADS<PER>, 512 / LN_THREADS<PER>) ln_bac
       for (int k = 0; k < NV; ++k)
         if (at.in(k)) at.store(dx + r * a.ldy, k, f + k * E);
     }
+  }
+  if (RING && !landed) {
+    twa_set_status(a.status, TWA_ERR_TIMEOUT, -1);
+    // no copy may still be on its way into this block's shared memory when it ends
+    if (issuer)
+      for (int i = max(0, it - LN_RING); i < it; ++i) {
+        const unsigned long long begun = twa_globaltimer();
+        while (!twa_mbar_try_wait(twa_smem_u32(&full[team * LN_RING + i % LN_RING]), i / LN_RING & 1))
+          if (twa_globaltimer() - begun > a.wait_limit_ns) break;
+      }
   }
   if (!a.part) return;
   float* out = a.part + static_cast<long long>(blockIdx.x) * 2 * a.cols;
@@ -246,24 +309,31 @@ __global__ void ln_weights_loop_kernel(LnArgs a) {
   out[a.cols + c] = db;
 }
 
-// Adds the blocks' partial sums in block order: 32 columns a block, its warps each a run of the blocks.
-constexpr int LN_SUM_WARPS = 16;
-__global__ void ln_sum_kernel(const float* __restrict__ part, int blocks, int cols, void* dw, void* db, int g_dtype,
-                              int accumulate) {
+// Adds the blocks' partial sums: 32 columns a block, a warp for every LN_SUM_WARPS-th of the blocks' rows, all loads of a thread
+// under way at once; then a warp a column, in a fixed tree.
+constexpr int LN_SUM_WARPS = 32, LN_SUM_EACH = (LN_MAX_BLOCKS + LN_SUM_WARPS - 1) / LN_SUM_WARPS;
+__global__ void __launch_bounds__(32 * LN_SUM_WARPS) ln_sum_kernel(const float* part, int blocks, int cols, void* dw, void* db,
+                                                                  int g_dtype, int accumulate) {
   twa_begin(part);
-  __shared__ double run[LN_SUM_WARPS][32];
+  __shared__ double run[LN_SUM_WARPS][33];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int c = blockIdx.x * 32 + lane;               // 0 .. 2 cols: dw, then db
-  const int each = (blocks + LN_SUM_WARPS - 1) / LN_SUM_WARPS;
-  const int from = warp * each, to = min(blocks, from + each);
+  int c = blockIdx.x * 32 + lane;                     // 0 .. 2 cols - 1: dw, then db
+  float v[LN_SUM_EACH];
+#pragma unroll
+  for (int k = 0; k < LN_SUM_EACH; ++k) {
+    const int b = k * LN_SUM_WARPS + warp;
+    v[k] = b < blocks && c < 2 * cols ? __ldg(part + static_cast<long long>(b) * 2 * cols + c) : 0.0f;
+  }
   double s = 0.0;
-  if (c < 2 * cols)
-#pragma unroll 8
-    for (int k = from; k < to; ++k) s += static_cast<double>(__ldg(part + static_cast<long long>(k) * 2 * cols + c));
+#pragma unroll
+  for (int k = 0; k < LN_SUM_EACH; ++k) s += static_cast<double>(v[k]);
   run[warp][lane] = s;
   __syncthreads();
-  if (warp || c >= 2 * cols) return;
-  for (int k = 1; k < LN_SUM_WARPS; ++k) s += run[k][lane];
+  c = blockIdx.x * 32 + warp;
+  s = run[lane][warp];
+#pragma unroll
+  for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  if (lane || c >= 2 * cols) return;
   void* out = c < cols ? dw : db;
   const int i = c < cols ? c : c - cols;
   if (!out) return;
@@ -280,9 +350,11 @@ LnKernel ln_pick(int* nv, int units, bool aligned) {
   if constexpr (E * n <= held && (PER <= 32 || 2 * E * n >= held) && (if_more)) {       \
     if (wanted <= n) {                                                                  \
       *nv = n;                                                                          \
-      if constexpr (E > 1 && PER > 0)                                                   \
-        if (aligned && units == PER * n) return ln_backward_kernel<T, E, n, PER, true>;          \
-      return ln_backward_kernel<T, E, n, PER, false>;                                            \
+      if constexpr (E > 1 && PER > 0) {                                                 \
+        if (aligned && units == PER * n) return ln_backward_kernel<T, E, n, PER, true, true>; \
+        if (aligned) return ln_backward_kernel<T, E, n, PER, false, true>;              \
+      }                                                                                 \
+      return ln_backward_kernel<T, E, n, PER, false, false>;                            \
     }                                                                                   \
   }
   LN_TRY(1, true)
@@ -325,6 +397,7 @@ int ln_plan_units(twa_ctx* ctx, int classes, long long rows, int cols, LnPlan* p
                : per == 256 ? ln_pick<T, E, BACK, 256>(&nv, units, aligned) : ln_pick<T, E, BACK, 512>(&nv, units, aligned);
   }
   p.smem = sizeof(float) * 2 * per * nv * E;
+  if (E > 1 && per >= 32 && aligned) p.smem += 16LL * 2 * per * nv * (nv >= 3 ? LN_RING_ROWS<3> : LN_RING_ROWS<1>) * (per == 32 ? LN_WARP_THREADS / 32 : 1);
   if constexpr (BACK) {
     if (!p.kernel && aligned && units <= LN_WIDE_THREADS * (LN_WIDE_HELD / E)) {
       p.threads = LN_WIDE_THREADS;
@@ -334,11 +407,11 @@ int ln_plan_units(twa_ctx* ctx, int classes, long long rows, int cols, LnPlan* p
   }
   if (p.kernel && p.smem > 44 * 1024) {      // 48 KB with what the kernel declares
     // which of the kernels that can need as much: by threads and what they hold
-    static int smem_set[5][40][2][64] = {};
-    int log = 0;
-    while (64 << log < p.threads) ++log;
+    static int smem_set[6][40][3][64] = {};
+    int log = per == 32 ? 5 : 0;
+    while (per > 32 && 64 << log < p.threads) ++log;
     int rc = twa_ensure_smem(ctx, reinterpret_cast<const void*>(p.kernel),
-                             &smem_set[log][nv][aligned && units == per * nv][ctx->device & 63], static_cast<int>(p.smem));
+                             &smem_set[log][nv][aligned ? (units == per * nv ? 2 : 1) : 0][ctx->device & 63], static_cast<int>(p.smem));
     if (rc) return rc;
   }
   const long long per_sm = p.threads < 512 ? 512 / p.threads : 1;
@@ -391,7 +464,7 @@ int twa_layer_norm_backward(twa_ctx* ctx, const void* dy, int64_t lddy, const vo
   }
   TWA_CUDA_OK(ctx, cudaSetDevice(ctx->device));
   LnArgs a = {x, dy, dx, w, nullptr, const_cast<float*>(mean), const_cast<float*>(rstd),
-              weights ? static_cast<float*>(ws) : nullptr, ldx, lddy, lddx, rows, cols, w_dtype, 5, 0, 0.0f};
+              weights ? static_cast<float*>(ws) : nullptr, ldx, lddy, lddx, rows, cols, w_dtype, 5, 0, 0.0f, ctx->wait_limit_ns, ctx->d_status};
   int parts = 0;
   if (rows) {
     const int classes = ln_classes(x, ldx, dy, lddy, dx, lddx, rows, cols, size);

@@ -41,7 +41,6 @@ constexpr int LP_STAGES = TOP ? 4 : 3;
 constexpr int LP_BUFFER = 128;                              // candidates that are sorted without a further look
 constexpr int LP_MAX_CLUSTER = 8;
 constexpr long long LP_SPLIT_ROWS = 2;                      // blocks an SM up to which rows are split over clusters
-constexpr uint32_t LP_SUSPEND_NS = 20000;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float LP_FAR = 8192.0f;                           // bound of what exponents are taken against
 typedef unsigned long long u64;
@@ -295,38 +294,6 @@ __device__ __noinline__ u64 lp_best_of_all(const T* row, int from, int to) {
   return list;
 }
 
-// twa_mbar_wait with a hint to suspend the thread: several warps of a block wait most of the time, and ones that poll
-// take issue slots from those that add up.
-__device__ __forceinline__ bool lp_wait(u64* bar, uint32_t parity, volatile int* abort_flag, unsigned long long limit_ns) {
-  const uint32_t at = twa_smem_u32(bar);
-  unsigned long long begun = 0;
-  for (;;) {
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(at), "r"(parity), "r"(LP_SUSPEND_NS)
-        : "memory");
-    if (ok) return true;
-    if (*abort_flag) return false;
-    const unsigned long long now = twa_globaltimer();
-    if (!begun) begun = now;
-    if (now - begun > limit_ns) {
-      *abort_flag = 1;
-      return false;
-    }
-  }
-}
-
-// Untiled bulk copy into this block's shared memory: addresses and size in multiples of 16 bytes.
-__device__ __forceinline__ void lp_bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
-               "r"(bytes), "r"(bar)
-               : "memory");
-}
-
 // A row per cluster of 2^log_parts blocks, each a run of its units; with one part a block goes on to further rows.
 template <typename T, bool ENT, bool TOP>
 __global__ void __launch_bounds__(LP_BLOCK, LP_BLOCKS_PER_SM<TOP>) logprobs_kernel(LpArgs a, const int log_parts) {
@@ -367,13 +334,13 @@ __global__ void __launch_bounds__(LP_BLOCK, LP_BLOCKS_PER_SM<TOP>) logprobs_kern
         for (int u = u0; u < u1; u += LP_CHUNK, ++it) {
           const int q = it % STAGES;
           if (it >= STAGES &&
-              !lp_wait(&sh.empty[q], (it / STAGES & 1) ^ 1, &sh.gave_up, a.wait_limit_ns)) {
+              !twa_wait(&sh.empty[q], (it / STAGES & 1) ^ 1, &sh.gave_up, a.wait_limit_ns)) {
             good = false;
             break;
           }
           const uint32_t bytes = static_cast<uint32_t>(min(LP_CHUNK, u1 - u)) * 16;
           twa_mbar_expect_tx(twa_smem_u32(&sh.full[q]), bytes);
-          lp_bulk_load(twa_smem_u32(sh.ring[q]), x.base + static_cast<long long>(x.first + u) * E, bytes, twa_smem_u32(&sh.full[q]));
+          twa_bulk_load(twa_smem_u32(sh.ring[q]), x.base + static_cast<long long>(x.first + u) * E, bytes, twa_smem_u32(&sh.full[q]));
         }
       }
       // no copy may still be on its way into this block's shared memory when it ends
@@ -415,7 +382,7 @@ __global__ void __launch_bounds__(LP_BLOCK, LP_BLOCKS_PER_SM<TOP>) logprobs_kern
         target = twa_load_id(a.targets, a.itype, row);
         if (target >= 0 && target < a.vocab) zt = twa_to_float(x.base[x.skew + target]);
       }
-      const bool waited = lp_wait(&sh.row_full[turn], r & 1, &sh.gave_up, a.wait_limit_ns);
+      const bool waited = twa_wait(&sh.row_full[turn], r & 1, &sh.gave_up, a.wait_limit_ns);
       LpStat st = lp_merge_near<ENT, LP_WARPS>(sh.stat[turn][lane & (LP_WARPS - 1)]);
       u64 key[LP_WARPS];
       if (TOP)
@@ -639,7 +606,7 @@ __global__ void __launch_bounds__(LP_BLOCK, LP_BLOCKS_PER_SM<TOP>) logprobs_kern
     for (int k = 0; k < chunks; ++k, ++it) {
       const int q = it % STAGES, n = min(LP_CHUNK, u1 - u0 - k * LP_CHUNK);
       // after a wait that ran out the row's results are not defined, and every later wait ends at once
-      lp_wait(&sh.full[q], it / STAGES & 1, &sh.gave_up, a.wait_limit_ns);
+      twa_wait(&sh.full[q], it / STAGES & 1, &sh.gave_up, a.wait_limit_ns);
       if (n == LP_CHUNK) {
         uint4 w[LP_PER_THREAD];
 #pragma unroll
@@ -675,7 +642,7 @@ __global__ void __launch_bounds__(LP_BLOCK, LP_BLOCKS_PER_SM<TOP>) logprobs_kern
       st.s *= f;
     }
     st = lp_merge_near<ENT, 32>(st);
-    if (round) lp_wait(&sh.row_empty[turn], (round & 1) ^ 1, &sh.gave_up, a.wait_limit_ns);
+    if (round) twa_wait(&sh.row_empty[turn], (round & 1) ^ 1, &sh.gave_up, a.wait_limit_ns);
     if (lane == 0) sh.stat[turn][warp] = st;
     if (TOP) sh.key[turn][threadIdx.x] = some ? lp_key(m, place) : 0;
     __syncwarp();

@@ -42,7 +42,7 @@ __device__ __forceinline__ long long twa_load_id(const void* p, int itype, long 
 }
 
 // E consecutive elements as they lie in memory: E = 1, or 16 bytes (E = 4 float, 8 bfloat16; the address on 16
-// bytes).  Loading and widening are apart so that the loads of the next row can be under way while this one is worked on.
+// bytes).  from() packs values of the type, as widen() gave them.  Loading and widening are apart so that the loads of the next row can be under way while this one is worked on.
 template <typename T, int E>
 struct twa_pack;
 template <>
@@ -50,6 +50,7 @@ struct twa_pack<float, 1> {
   float r;
   __device__ __forceinline__ void load(const float* p) { r = __ldg(p); }
   __device__ __forceinline__ void widen(float* v) const { v[0] = r; }
+  __device__ __forceinline__ void from(const float* v) { r = v[0]; }
   static __device__ __forceinline__ void store(float* p, const float* v) { *p = v[0]; }
 };
 template <>
@@ -57,13 +58,16 @@ struct twa_pack<bf16, 1> {
   unsigned short r;
   __device__ __forceinline__ void load(const bf16* p) { r = __ldg(reinterpret_cast<const unsigned short*>(p)); }
   __device__ __forceinline__ void widen(float* v) const { v[0] = __uint_as_float(static_cast<uint32_t>(r) << 16); }
+  __device__ __forceinline__ void from(const float* v) { r = static_cast<unsigned short>(__float_as_uint(v[0]) >> 16); }
   static __device__ __forceinline__ void store(bf16* p, const float* v) { *p = twa_from_float<bf16>(v[0]); }
 };
 template <>
 struct twa_pack<float, 4> {
   float4 r;
   __device__ __forceinline__ void load(const float* p) { r = __ldg(reinterpret_cast<const float4*>(p)); }
+  __device__ __forceinline__ void load_shared(const uint4* p) { r = *reinterpret_cast<const float4*>(p); }
   __device__ __forceinline__ void widen(float* v) const { v[0] = r.x; v[1] = r.y; v[2] = r.z; v[3] = r.w; }
+  __device__ __forceinline__ void from(const float* v) { r = make_float4(v[0], v[1], v[2], v[3]); }
   static __device__ __forceinline__ void store(float* p, const float* v) {
     *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
   }
@@ -77,6 +81,11 @@ template <>
 struct twa_pack<bf16, 8> {
   uint4 r;
   __device__ __forceinline__ void load(const bf16* p) { r = __ldg(reinterpret_cast<const uint4*>(p)); }
+  __device__ __forceinline__ void load_shared(const uint4* p) { r = *p; }
+  __device__ __forceinline__ void from(const float* v) {
+    r.x = twa_bf16_pair(v[0], v[1]); r.y = twa_bf16_pair(v[2], v[3]);
+    r.z = twa_bf16_pair(v[4], v[5]); r.w = twa_bf16_pair(v[6], v[7]);
+  }
   __device__ __forceinline__ void widen(float* v) const {
     v[0] = twa_bf16_lo(r.x); v[1] = twa_bf16_hi(r.x); v[2] = twa_bf16_lo(r.y); v[3] = twa_bf16_hi(r.y);
     v[4] = twa_bf16_lo(r.z); v[5] = twa_bf16_hi(r.z); v[6] = twa_bf16_lo(r.w); v[7] = twa_bf16_hi(r.w);
@@ -127,15 +136,47 @@ __device__ __forceinline__ twa_f2 twa_mul2(twa_f2 a, twa_f2 b) {
   return r;
 }
 
+// twa_mbar_wait with a hint to suspend the thread: several warps of a block wait most of the time, and ones that poll
+// take issue slots from those that add up.
+__device__ __forceinline__ bool twa_wait(unsigned long long* bar, uint32_t parity, volatile int* abort_flag, unsigned long long limit_ns) {
+  const uint32_t at = twa_smem_u32(bar);
+  unsigned long long begun = 0;
+  for (;;) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(at), "r"(parity), "r"(20000u)
+        : "memory");
+    if (ok) return true;
+    if (*abort_flag) return false;
+    const unsigned long long now = twa_globaltimer();
+    if (!begun) begun = now;
+    if (now - begun > limit_ns) {
+      *abort_flag = 1;
+      return false;
+    }
+  }
+}
+
+// Untiled bulk copy into this block's shared memory: addresses and size in multiples of 16 bytes.
+__device__ __forceinline__ void twa_bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
+               "r"(bytes), "r"(bar)
+               : "memory");
+}
+
 // Launches that may begin while the kernel before them in the stream ends (programmatic dependent launch).  A kernel launched
-// so first calls twa_begin(pointers it reads ...): the next kernel's blocks may take free places from here on, and this one goes on
-// when the kernels before it are complete and their writes visible.  The pointers come out of the call as new values, so that
-// no load through them, not even one of data the compiler takes for constant, can be moved before it.
+// so first calls twa_begin(pointers it reads ...), which goes on when the kernels before it are complete and their writes
+// visible.  The pointers come out of the call as new values, so that no load through them, not even one of data the compiler
+// takes for constant, can be moved before it.  No kernel lets the next one begin before its own blocks end: waiting blocks take
+// places from the kernel after them (gradient of a layer norm of 16384 x 2048 bfloat16: 63 us if it does, 49 us if not).
 template <typename P>
 __device__ __forceinline__ void twa_renew(P& pointer) { asm volatile("" : "+l"(pointer) : : "memory"); }
 template <typename... P>
 __device__ __forceinline__ void twa_begin(P&... pointers) {
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   (..., twa_renew(pointers));
 }

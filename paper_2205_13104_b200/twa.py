@@ -763,30 +763,39 @@ def _numbers(t, count, what):
     code = _ITYPES.get(t.dtype)
     if code is None:
         raise TypeError(f"{what}: dtype {t.dtype} not supported (int32 or int64)")
-    if t.dim() != 1 or t.shape[0] != count or not t.is_contiguous():
-        raise ValueError(f"{what}: a contiguous vector of {count} token numbers is needed, got shape {tuple(t.shape)}")
+    if t.numel() != count or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError(f"{what}: {count} contiguous token numbers on the device are needed, got shape {tuple(t.shape)} on {t.device}")
     return code
 
 
 def _rows(t, shape, what, dtype=None):
     """Row stride of a matrix of that shape whose rows are contiguous."""
-    if t.shape != shape or dtype is not None and t.dtype != dtype:
-        raise ValueError(f"{what}: shape {tuple(shape)}{'' if dtype is None else f' of {dtype}'} is needed, "
-                         f"got {tuple(t.shape)} of {t.dtype}")
+    if t.shape != shape or dtype is not None and t.dtype is not dtype or not t.is_cuda:
+        raise ValueError(f"{what}: shape {tuple(shape)}{'' if dtype is None else f' of {dtype}'} on the device is needed, "
+                         f"got {tuple(t.shape)} of {t.dtype} on {t.device}")
     ld, one = t.stride()
     if one != 1 and shape[1] > 1:
         raise ValueError(f"{what}: the elements of a row have to be contiguous")
-    return ld if shape[0] > 1 else max(ld, shape[1])
+    return ld if ld >= shape[1] or shape[0] > 1 else shape[1]
 
 
 def _vector(t, count, dtype, what):
-    if t.dtype != dtype or t.dim() != 1 or t.shape[0] != count or not t.is_contiguous():
-        raise ValueError(f"{what}: a contiguous vector of {count} {dtype} is needed, got {tuple(t.shape)} of {t.dtype}")
+    """Address of a contiguous tensor of `count` elements (0 for None)."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.numel() != count or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError(f"{what}: {count} contiguous elements of {dtype} on the device are needed, got {tuple(t.shape)} of {t.dtype} "
+                         f"on {t.device}")
     return t.data_ptr()
 
 
-def _optional(t, count, dtype, what):
-    return None if t is None else _vector(t, count, dtype, what)
+def _space(ws):
+    """Address and size of a workspace."""
+    if ws is None:
+        return None, 0
+    if not ws.is_cuda or not ws.is_contiguous():
+        raise ValueError("ws: a contiguous tensor on the device is needed")
+    return ws.data_ptr(), ws.nbytes
 
 
 def twa_layer_norm_workspace_bytes(rows, cols):
@@ -798,13 +807,13 @@ def twa_layer_norm(ctx, x, weight, bias, eps, y, mean=None, rstd=None):
     dt, shape = _floats(x, "x"), x.shape
     rows, cols = shape
     p = weight if weight is not None else bias
-    wt = _floats(p, "weight") if p is not None else TWA_F32
+    pt, wt = (p.dtype, _floats(p, "weight")) if p is not None else (None, TWA_F32)
     rc = load().twa_layer_norm(ctx, x.data_ptr(), _rows(x, shape, "x"), dt,
-                               _optional(weight, cols, p.dtype if p is not None else None, "weight"),
-                               _optional(bias, cols, p.dtype if p is not None else None, "bias"), wt, rows, cols, eps,
-                               y.data_ptr(), _rows(y, shape, "y", x.dtype), _optional(mean, rows, torch.float32, "mean"),
-                               _optional(rstd, rows, torch.float32, "rstd"))
-    _check(rc, "twa_layer_norm", ctx)
+                               _vector(weight, cols, pt, "weight"), _vector(bias, cols, pt, "bias"), wt, rows, cols, eps,
+                               y.data_ptr(), _rows(y, shape, "y", x.dtype), _vector(mean, rows, torch.float32, "mean"),
+                               _vector(rstd, rows, torch.float32, "rstd"))
+    if rc:
+        _check(rc, "twa_layer_norm", ctx)
     return y
 
 
@@ -813,16 +822,15 @@ def twa_layer_norm_backward(ctx, dy, x, weight, mean, rstd, dx, dw, db, ws, accu
     dt, shape = _floats(x, "x"), x.shape
     rows, cols = shape
     p = dw if dw is not None else db
-    gt = _floats(p, "dw") if p is not None else TWA_F32
+    pt, gt = (p.dtype, _floats(p, "dw")) if p is not None else (None, TWA_F32)
     rc = load().twa_layer_norm_backward(
         ctx, dy.data_ptr(), _rows(dy, shape, "dy", x.dtype), x.data_ptr(), _rows(x, shape, "x"), dt,
-        _optional(weight, cols, weight.dtype if weight is not None else None, "weight"),
+        _vector(weight, cols, weight.dtype if weight is not None else None, "weight"),
         _floats(weight, "weight") if weight is not None else TWA_F32, _vector(mean, rows, torch.float32, "mean"),
         _vector(rstd, rows, torch.float32, "rstd"), rows, cols, dx.data_ptr(), _rows(dx, shape, "dx", x.dtype),
-        _optional(dw, cols, p.dtype if p is not None else None, "dw"),
-        _optional(db, cols, p.dtype if p is not None else None, "db"), gt, 1 if accumulate else 0, _ptr(ws),
-        ws.numel() * ws.element_size() if ws is not None else 0)
-    _check(rc, "twa_layer_norm_backward", ctx)
+        _vector(dw, cols, pt, "dw"), _vector(db, cols, pt, "db"), gt, 1 if accumulate else 0, *_space(ws))
+    if rc:
+        _check(rc, "twa_layer_norm_backward", ctx)
     return dx
 
 
@@ -837,7 +845,8 @@ def twa_embedding(ctx, table, ids, scale, out):
     rc = load().twa_embedding(ctx, table.data_ptr(), _rows(table, table.shape, "table"), _floats(table, "table"), vocab, dim,
                               ids.data_ptr(), _numbers(ids, tokens, "ids"), tokens, scale, out.data_ptr(),
                               _rows(out, (tokens, dim), "out"), _floats(out, "out"))
-    _check(rc, "twa_embedding", ctx)
+    if rc:
+        _check(rc, "twa_embedding", ctx)
     return out
 
 
@@ -848,8 +857,9 @@ def twa_embedding_backward(ctx, dout, ids, scale, dtable, ws, padding_id=-1, acc
     rc = load().twa_embedding_backward(ctx, dout.data_ptr(), _rows(dout, (tokens, dim), "dout"), _floats(dout, "dout"),
                                        ids.data_ptr(), _numbers(ids, tokens, "ids"), tokens, vocab, dim, scale, padding_id,
                                        dtable.data_ptr(), _rows(dtable, dtable.shape, "dtable"), _floats(dtable, "dtable"),
-                                       1 if accumulate else 0, ws.data_ptr(), ws.numel() * ws.element_size())
-    _check(rc, "twa_embedding_backward", ctx)
+                                       1 if accumulate else 0, *_space(ws))
+    if rc:
+        _check(rc, "twa_embedding_backward", ctx)
     return dtable
 
 
@@ -859,16 +869,17 @@ def twa_token_logprobs(ctx, logits, targets, logp, lse, entropy=None, top_ids=No
     rows, vocab = logits.shape
     top = 0
     if top_ids is not None or top_logp is not None:
-        if top_ids is None or top_logp is None or top_ids.dtype != torch.int32 or top_logp.dtype != torch.float32 or \
-                top_ids.shape != top_logp.shape or top_ids.dim() != 2 or top_ids.shape[0] != rows or \
+        if top_ids is None or top_logp is None or not top_ids.is_cuda or not top_logp.is_cuda or top_ids.dtype is not torch.int32 or top_logp.dtype is not torch.float32 or \
+                top_ids.shape != top_logp.shape or top_ids.dim() != 2 or len(top_ids) != rows or \
                 not top_ids.is_contiguous() or not top_logp.is_contiguous():
             raise ValueError(f"top_ids and top_logp: contiguous ({rows}, k) matrices of int32 and float32 are needed, both or neither")
         top = top_ids.shape[1]
     rc = load().twa_token_logprobs(ctx, logits.data_ptr(), _rows(logits, logits.shape, "logits"), _floats(logits, "logits"), rows,
                                    vocab, targets.data_ptr(), _numbers(targets, rows, "targets"), ignore_id,
                                    _vector(logp, rows, torch.float32, "logp"), _vector(lse, rows, torch.float32, "lse"),
-                                   _optional(entropy, rows, torch.float32, "entropy"), top, _ptr(top_ids), _ptr(top_logp))
-    _check(rc, "twa_token_logprobs", ctx)
+                                   _vector(entropy, rows, torch.float32, "entropy"), top, _ptr(top_ids), _ptr(top_logp))
+    if rc:
+        _check(rc, "twa_token_logprobs", ctx)
     return logp
 
 
@@ -879,10 +890,11 @@ def twa_token_logprobs_backward(ctx, logits, targets, lse, d_logp, dlogits, entr
     rc = load().twa_token_logprobs_backward(
         ctx, logits.data_ptr(), _rows(logits, shape, "logits"), _floats(logits, "logits"), rows, vocab, targets.data_ptr(),
         _numbers(targets, rows, "targets"), ignore_id, _vector(lse, rows, torch.float32, "lse"),
-        _optional(entropy, rows, torch.float32, "entropy"), _vector(d_logp, rows, torch.float32, "d_logp"),
-        _optional(d_entropy, rows, torch.float32, "d_entropy"), dlogits.data_ptr(),
+        _vector(entropy, rows, torch.float32, "entropy"), _vector(d_logp, rows, torch.float32, "d_logp"),
+        _vector(d_entropy, rows, torch.float32, "d_entropy"), dlogits.data_ptr(),
         _rows(dlogits, shape, "dlogits", logits.dtype))
-    _check(rc, "twa_token_logprobs_backward", ctx)
+    if rc:
+        _check(rc, "twa_token_logprobs_backward", ctx)
     return dlogits
 
 
@@ -893,8 +905,8 @@ class Tensors:
     def __init__(self, tensors):
         self.tensors = list(tensors)
         for t in self.tensors:
-            if not t.is_contiguous():
-                raise ValueError("gradients have to be contiguous")
+            if not t.is_contiguous() or not t.is_cuda:
+                raise ValueError("gradients have to be contiguous and on the device")
         n = len(self.tensors)
         self._data = (ctypes.c_void_p * n)(*[t.data_ptr() for t in self.tensors])
         self._sizes = (ctypes.c_int64 * n)(*[t.numel() for t in self.tensors])
@@ -911,24 +923,26 @@ def twa_grad_norm_workspace_bytes(tensors):
 
 def twa_grad_norm(ctx, tensors, norm, ws):
     """tensors: a Tensors; norm: (1,) float32."""
-    rc = load().twa_grad_norm(ctx, ctypes.byref(tensors.desc), _vector(norm, 1, torch.float32, "norm"), ws.data_ptr(),
-                              ws.numel() * ws.element_size())
-    _check(rc, "twa_grad_norm", ctx)
+    rc = load().twa_grad_norm(ctx, ctypes.byref(tensors.desc), _vector(norm, 1, torch.float32, "norm"), *_space(ws))
+    if rc:
+        _check(rc, "twa_grad_norm", ctx)
     return norm
 
 
 def twa_clip_gather(ctx, tensors, max_norm, g, norm, ws, eps=1e-6):
     """g: contiguous, of at least as many elements as the tensors together (a padded flat gradient keeps its tail)."""
-    if g.dim() != 1 or g.numel() < tensors.total or not g.is_contiguous():
-        raise ValueError(f"g: a contiguous vector of at least {tensors.total} elements is needed, got {tuple(g.shape)}")
+    if g.dim() != 1 or g.numel() < tensors.total or not g.is_contiguous() or not g.is_cuda:
+        raise ValueError(f"g: a contiguous vector of at least {tensors.total} elements on the device is needed, got {tuple(g.shape)} on {g.device}")
     rc = load().twa_clip_gather(ctx, ctypes.byref(tensors.desc), max_norm, eps, g.data_ptr(), _floats(g, "g"),
-                                _vector(norm, 1, torch.float32, "norm"), ws.data_ptr(), ws.numel() * ws.element_size())
-    _check(rc, "twa_clip_gather", ctx)
+                                _vector(norm, 1, torch.float32, "norm"), *_space(ws))
+    if rc:
+        _check(rc, "twa_clip_gather", ctx)
     return g
 
 
 def twa_clip_grads(ctx, tensors, max_norm, norm, ws, eps=1e-6):
     rc = load().twa_clip_grads(ctx, ctypes.byref(tensors.desc), max_norm, eps, _vector(norm, 1, torch.float32, "norm"),
-                               ws.data_ptr(), ws.numel() * ws.element_size())
-    _check(rc, "twa_clip_grads", ctx)
+                               *_space(ws))
+    if rc:
+        _check(rc, "twa_clip_grads", ctx)
     return norm

@@ -652,7 +652,9 @@ def test_refusals(ctx):
     for call in (lambda: twa.twa_layer_norm(ctx, x, w[:4], None, 1e-5, x), lambda: twa.twa_layer_norm(ctx, x, w, None, 1e-5, x[:2]),
                  lambda: twa.twa_layer_norm(ctx, x.t(), None, None, 1e-5, x.t()),
                  lambda: twa.twa_embedding(ctx, x, ids, 1.0, x[:, :4]), lambda: twa.twa_token_logprobs(ctx, x, ids[:2], v, v),
-                 lambda: twa.twa_token_logprobs(ctx, x, ids, v[:2], v), lambda: twa.Tensors([x.t()]),
+                 lambda: twa.twa_token_logprobs(ctx, x, ids, v[:2], v), lambda: twa.Tensors([x.t()]), lambda: twa.Tensors([x.cpu()]),
+                 lambda: twa.twa_layer_norm(ctx, x.cpu(), w, None, 1e-5, x), lambda: twa.twa_embedding(ctx, x, ids.cpu(), 1.0, x),
+                 lambda: twa.twa_layer_norm_backward(ctx, x, x, w, v, v.cpu(), x, w, w, ws),
                  lambda: twa.twa_clip_gather(ctx, ts, 1.0, torch.zeros(31, device=DEV), norm, ws)):
         with pytest.raises(ValueError):
             call()
