@@ -17,11 +17,10 @@
 // c loses its digits when m is far from zero, so it is held within +-8192 log2 e; a row (or a block's part of one) whose
 // maximum lies beyond is summed once more with differences to that maximum taken first.
 //
-// The most likely tokens cost no second pass.  Each thread also remembers the chunk of the row in which its maximum
-// lay.  Order all elements by (value, earlier chunk first): with T the k-th best of the maxima of 32 groups of threads, k
-// elements rank at T or above, so each of the k best elements does, and lies with a thread whose own maximum does.
-// Only those threads' elements (some 1.5 k threads) are looked at again, in L2, and the few that rank at T or above are
-// sorted by (value, smaller index first).
+// The most likely tokens cost no second pass.  With T the k-th largest of the maxima of 32 groups of threads, k elements
+// are T or more, so each of the k best elements is, and lies with a thread whose maximum is.  Each thread also leaves the
+// maxima of its parts of the row (SLOTS of them): only the parts of those threads that reach T (some 1.5 k) are
+// looked at again, in L2, and the few elements of T or more are sorted by (value, smaller index first).
 #include "twa_ops.cuh"
 
 namespace {
@@ -38,6 +37,7 @@ template <bool TOP>
 constexpr int LP_BLOCKS_PER_SM = TOP ? 2 : 3;
 template <bool TOP>
 constexpr int LP_STAGES = TOP ? 4 : 3;
+constexpr int LP_SLOTS = 16;                                // parts of a row whose maxima a thread leaves
 constexpr int LP_BUFFER = 128;                              // candidates that are sorted without a further look
 constexpr int LP_MAX_CLUSTER = 8;
 constexpr long long LP_SPLIT_ROWS = 2;                      // blocks an SM up to which rows are split over clusters
@@ -147,17 +147,14 @@ __device__ __forceinline__ LpStat lp_merge_near(const LpStat& x) {
   }
   return r;
 }
-// Sums relative to m.
+// Sums relative to m (0 or NaN where m is -inf) of all lanes.
 template <bool ENT>
-__device__ __forceinline__ LpStat lp_merge(const LpStat& x, const LpStat& y) {
+__device__ __forceinline__ LpStat lp_merge(const LpStat& x) {
   LpStat r;
-  r.m = fmaxf(x.m, y.m);
-  const float base = r.m == -INFINITY ? 0.0f : r.m;
-  // a side without any value (m = -inf) has the sums 0, or NaN where a NaN was met
-  const float dx = fmaxf((x.m - base) * LOG2E, -150.0f), dy = fmaxf((y.m - base) * LOG2E, -150.0f);
-  const float fx = lp_exp2(dx), fy = lp_exp2(dy);
-  r.s = x.s * fx + y.s * fy;
-  r.a = ENT ? fx * (x.a + dx * x.s) + fy * (y.a + dy * y.s) : 0.0f;
+  r.m = lp_unrank(__reduce_max_sync(0xffffffffu, lp_rank(x.m)));
+  const float base = r.m == -INFINITY ? 0.0f : r.m, d = fmaxf((x.m - base) * LOG2E, -150.0f), f = lp_exp2(d);
+  r.s = twa_warp_sum(x.s * f);
+  r.a = ENT ? twa_warp_sum(f * (x.a + d * x.s)) : 0.0f;
   return r;
 }
 
@@ -190,14 +187,23 @@ __device__ __forceinline__ u64 lp_merge32(u64 v, u64 other_reversed) {
 }
 // The number of the warp's keys above `v`: its place in descending order, where keys differ.  32 independent comparisons
 // against keys read from shared memory (`row`, the warp's own) take a third of the time of the network's 15 dependent steps.
-__device__ __forceinline__ int lp_place32(u64 v, u64* row) {
+template <typename K>
+__device__ __forceinline__ int lp_place32(K v, K* row) {
   row[threadIdx.x & 31] = v;
   __syncwarp();
   int above = 0;
+  if constexpr (sizeof(K) == 8) {
 #pragma unroll
-  for (int i = 0; i < 32; i += 2) {
-    const ulonglong2 o = *reinterpret_cast<const ulonglong2*>(row + i);
-    above += (o.x > v) + (o.y > v);
+    for (int i = 0; i < 32; i += 2) {
+      const ulonglong2 o = *reinterpret_cast<const ulonglong2*>(row + i);
+      above += (o.x > v) + (o.y > v);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 32; i += 4) {
+      const uint4 o = *reinterpret_cast<const uint4*>(row + i);
+      above += (o.x > v) + (o.y > v) + (o.z > v) + (o.w > v);
+    }
   }
   __syncwarp();
   return above;
@@ -206,6 +212,24 @@ __device__ __forceinline__ int lp_place32(u64 v, u64* row) {
 __device__ __forceinline__ u64 lp_take32(u64 list, u64 key) {
   if (!__any_sync(0xffffffffu, key > __shfl_sync(0xffffffffu, list, 31))) return list;
   return lp_merge32(list, __shfl_xor_sync(0xffffffffu, lp_sort32(key), 31));
+}
+
+// The best 32 of the first `count` keys of a buffer of at least 32, sorted; the buffer is used up.
+__device__ __forceinline__ u64 lp_sort_buffer(u64* buffer, int count) {
+  const int lane = threadIdx.x & 31;
+  u64 list = lane < count ? buffer[lane] : 0;
+  if (count <= 32) {
+    __syncwarp();
+    const int place = lp_place32(list, buffer);
+    buffer[lane] = 0;
+    __syncwarp();
+    if (list) buffer[place] = list;
+    __syncwarp();
+    return buffer[lane];
+  }
+  list = lp_sort32(list);
+  for (int i = 32; i < count; i += 32) list = lp_take32(list, i + lane < count ? buffer[i + lane] : 0);
+  return list;
 }
 
 struct LpArgs {
@@ -228,11 +252,14 @@ struct LpShared {
   u64 full[LP_STAGES<TOP>], empty[LP_STAGES<TOP>];        // the ring's stages
   u64 row_full[LP_FINISHERS], row_empty[LP_FINISHERS];    // a row's results, by the warp that finishes it
   LpStat stat[LP_FINISHERS][LP_WARPS];
-  u64 key[LP_FINISHERS][LP_THREADS];
-  uint4 hit[LP_FINISHERS][LP_BUFFER];           // units with candidates, candidates
-  alignas(16) u64 buffer[LP_FINISHERS][LP_BUFFER];
-  int hit_unit[LP_FINISHERS][LP_BUFFER];
-  int chosen[LP_FINISHERS][LP_THREADS];
+  uint32_t key[LP_FINISHERS][TOP ? LP_THREADS : 1];           // ranks of the threads' maxima, 0: no element
+  float slot[LP_FINISHERS][TOP ? LP_SLOTS : 1][LP_THREADS];
+  uint4 hit[LP_FINISHERS][TOP ? LP_BUFFER : 1]; // units with candidates, candidates
+  alignas(16) u64 buffer[LP_FINISHERS][TOP ? LP_BUFFER : 2];
+  alignas(16) uint32_t group[LP_FINISHERS][32];
+  int hit_unit[LP_FINISHERS][TOP ? LP_BUFFER : 1];
+  int pair[LP_FINISHERS][TOP ? LP_BUFFER : 1];  // slot and thread
+  int chosen[LP_FINISHERS][TOP ? LP_THREADS : 1];
   u64 best[32];                                 // this block's best, read by the first block of the cluster
   LpStat mine;                                  // this block's sums, likewise
   int gave_up;
@@ -292,6 +319,13 @@ __device__ __noinline__ u64 lp_best_of_all(const T* row, int from, int to) {
     }
   }
   return list;
+}
+
+// Chunks of a slot, as a power of two.
+__device__ __forceinline__ int lp_log_slot(int chunks) {
+  int log = 0;
+  while (LP_SLOTS << log < chunks) ++log;
+  return log;
 }
 
 // A row per cluster of 2^log_parts blocks, each a run of its units; with one part a block goes on to further rows.
@@ -373,7 +407,7 @@ __global__ void __launch_bounds__(LP_BLOCK, LP_BLOCKS_PER_SM<TOP>) logprobs_kern
       const int u0 = x.part_from(part, log_parts);
       const int u1 = x.part_from(part + 1, log_parts);
       const int chunks = (u1 - u0 + LP_CHUNK - 1) / LP_CHUNK;
-      const int last_place = u1 > u0 ? u0 + (chunks - 1) * LP_CHUNK : u0;
+      const int log_slot = lp_log_slot(chunks);
       // the elements of this block's part: from .. to - 1
       const int from = part == 0 ? 0 : (x.first + u0) * E - x.skew, to = part == parts - 1 ? a.vocab : (x.first + u1) * E - x.skew;
       long long target = 0;
@@ -384,7 +418,7 @@ __global__ void __launch_bounds__(LP_BLOCK, LP_BLOCKS_PER_SM<TOP>) logprobs_kern
       }
       const bool waited = twa_wait(&sh.row_full[turn], r & 1, &sh.gave_up, a.wait_limit_ns);
       LpStat st = lp_merge_near<ENT, LP_WARPS>(sh.stat[turn][lane & (LP_WARPS - 1)]);
-      u64 key[LP_WARPS];
+      uint32_t key[LP_WARPS];
       if (TOP)
 #pragma unroll
         for (int i = 0; i < LP_WARPS; ++i) key[i] = sh.key[turn][i * 32 + lane];
@@ -398,14 +432,14 @@ __global__ void __launch_bounds__(LP_BLOCK, LP_BLOCKS_PER_SM<TOP>) logprobs_kern
           if (lane < to - from) found = lp_key(-INFINITY, from + lane);
         } else {
           // a group: the eight threads of one lane number
-          u64 g = key[0];
+          uint32_t g = key[0];
 #pragma unroll
-          for (int i = 1; i < LP_WARPS; ++i) g = g > key[i] ? g : key[i];
+          for (int i = 1; i < LP_WARPS; ++i) g = max(g, key[i]);
           // the top-th largest of the groups': the last one with fewer than `top` above it
-          const int above = lp_place32(g, sh.buffer[turn]);
+          const int above = lp_place32(g, sh.group[turn]);
           const int most = __reduce_max_sync(0xffffffffu, above < a.top ? above : -1);
-          const u64 bound = __shfl_sync(0xffffffffu, g, __ffs(__ballot_sync(0xffffffffu, above == most)) - 1);
-          const float bound_value = bound ? lp_unrank(static_cast<uint32_t>(bound >> 32)) : -INFINITY;
+          const uint32_t bound = __shfl_sync(0xffffffffu, g, __ffs(__ballot_sync(0xffffffffu, above == most)) - 1);
+          const float bound_value = bound ? lp_unrank(bound) : -INFINITY;
           int chosen = 0;
 #pragma unroll
           for (int i = 0; i < LP_WARPS; ++i) {
@@ -415,22 +449,47 @@ __global__ void __launch_bounds__(LP_BLOCK, LP_BLOCKS_PER_SM<TOP>) logprobs_kern
             chosen += __popc(all);
           }
           __syncwarp();
+          // their parts that reach the bound
+          int pairs = 0;
+          {
+            int slot = lane / chosen, who = lane % chosen;
+            const int slot_step = 32 / chosen, who_step = 32 % chosen;
+            const int slots = (chunks + (1 << log_slot) - 1) >> log_slot;
+            for (int i0 = 0; i0 < chosen * slots; i0 += 32) {
+              int thread = 0;
+              bool yes = slot < slots;
+              if (yes) {
+                thread = sh.chosen[turn][who];
+                yes = sh.slot[turn][slot][thread] >= bound_value;
+              }
+              const unsigned all = __ballot_sync(0xffffffffu, yes);
+              const int to = pairs + __popc(all & ((1u << lane) - 1));
+              if (yes && to < LP_BUFFER) sh.pair[turn][to] = slot * LP_THREADS + thread;
+              pairs += __popc(all);
+              slot += slot_step;
+              who += who_step;
+              if (who >= chosen) {
+                who -= chosen;
+                ++slot;
+              }
+            }
+          }
+          __syncwarp();
           // their units that hold a value as large as the bound's
-          constexpr int AHEAD = 8;
-          const int tasks = chosen * chunks * LP_PER_THREAD;
-          int hits = 0, what = lane / chosen, who = lane % chosen;     // of the lane's next task
-          const int what_step = 32 / chosen, who_step = 32 % chosen;
+          constexpr int AHEAD = 4;
+          const int log_each = 2 + log_slot, tasks = pairs <= LP_BUFFER ? pairs << log_each : 0;
+          static_assert(LP_PER_THREAD == 4, "log_each");
+          int hits = 0;
           for (int i0 = 0; i0 < tasks; i0 += 32 * AHEAD) {
             uint4 q[AHEAD];
             int u[AHEAD];
 #pragma unroll
             for (int j = 0; j < AHEAD; ++j) {
-              u[j] = i0 + 32 * j + lane < tasks ? u0 + what * LP_THREADS + sh.chosen[turn][who] : u1;
-              what += what_step;
-              who += who_step;
-              if (who >= chosen) {
-                who -= chosen;
-                ++what;
+              const int i = i0 + 32 * j + lane;
+              u[j] = u1;
+              if (i < tasks) {
+                const int pair = sh.pair[turn][i >> log_each], of = i & ((1 << log_each) - 1);
+                u[j] = u0 + (((pair / LP_THREADS) << log_each) + of) * LP_THREADS + pair % LP_THREADS;
               }
               if (u[j] < u1) q[j] = __ldg(reinterpret_cast<const uint4*>(x.base + static_cast<long long>(x.first + u[j]) * E));
             }
@@ -447,7 +506,7 @@ __global__ void __launch_bounds__(LP_BLOCK, LP_BLOCKS_PER_SM<TOP>) logprobs_kern
             }
           }
           __syncwarp();
-          // their elements, and the row's ragged ends, that rank at the bound or above
+          // their elements, and the row's ragged ends, of the bound's rank or above
           int count = 0;
           const int heads = part == 0 ? x.head() : 0, tails = part == parts - 1 ? a.vocab - x.tail_from() : 0;
           const int elements = hits <= LP_BUFFER ? hits * E : 0;
@@ -457,12 +516,12 @@ __global__ void __launch_bounds__(LP_BLOCK, LP_BLOCKS_PER_SM<TOP>) logprobs_kern
             if (i < elements) {
               const int u = sh.hit_unit[turn][i / E];
               const float z = twa_to_float(reinterpret_cast<const T*>(sh.hit[turn])[i]);
-              if (lp_key(z, u - (u - u0) % LP_CHUNK) >= bound) key = lp_key(z, (x.first + u) * E + i % E - x.skew);
+              if (lp_rank(z) >= bound) key = lp_key(z, (x.first + u) * E + i % E - x.skew);
             } else if (i < elements + heads + tails) {
               const bool head = i < elements + heads;
               const int j = head ? i - elements : x.tail_from() + i - elements - heads;
               const float z = twa_to_float(x.base[x.skew + j]);
-              if (lp_key(z, head ? u0 : last_place) >= bound) key = lp_key(z, j);
+              if (lp_rank(z) >= bound) key = lp_key(z, j);
             }
             const unsigned all = __ballot_sync(0xffffffffu, key != 0);
             const int to = count + __popc(all & ((1u << lane) - 1));
@@ -470,21 +529,8 @@ __global__ void __launch_bounds__(LP_BLOCK, LP_BLOCKS_PER_SM<TOP>) logprobs_kern
             if (key && to < LP_BUFFER) sh.buffer[turn][to] = key;
           }
           __syncwarp();
-          if (hits <= LP_BUFFER && count <= LP_BUFFER) {
-            if (count <= 32) {
-              const u64 v = lane < count ? sh.buffer[turn][lane] : 0;
-              __syncwarp();
-              const int place = lp_place32(v, sh.buffer[turn]);
-              __syncwarp();
-              sh.buffer[turn][lane] = 0;
-              __syncwarp();
-              if (v) sh.buffer[turn][place] = v;
-              __syncwarp();
-              found = sh.buffer[turn][lane];
-            } else {
-              found = lp_sort32(sh.buffer[turn][lane]);
-            }
-            for (int i = 32; i < count; i += 32) found = lp_take32(found, i + lane < count ? sh.buffer[turn][i + lane] : 0);
+          if (pairs <= LP_BUFFER && hits <= LP_BUFFER && count <= LP_BUFFER) {
+            found = lp_sort_buffer(sh.buffer[turn], count);
           } else {
             found = lp_best_of_all(x.base + x.skew, from, to);     // a row with many equal values
           }
@@ -497,13 +543,40 @@ __global__ void __launch_bounds__(LP_BLOCK, LP_BLOCKS_PER_SM<TOP>) logprobs_kern
         if (TOP) sh.best[lane] = found;
         lp_cluster_sync();
         if (part == 0) {
-          for (int p = 1; p < parts; ++p) {
-            LpStat other;
-            other.m = lp_remote(&sh.mine.m, p);
-            other.s = lp_remote(&sh.mine.s, p);
-            other.a = ENT ? lp_remote(&sh.mine.a, p) : 0.0f;
-            st = lp_merge<ENT>(st, other);
-            if (TOP) found = lp_merge32(found, lp_remote(&sh.best[31 - lane], p));
+          // a lane a part's sums
+          LpStat one = {-INFINITY, 0.0f, 0.0f};
+          if (lane < parts) {
+            one.m = lp_remote(&sh.mine.m, lane);
+            one.s = lp_remote(&sh.mine.s, lane);
+            one.a = ENT ? lp_remote(&sh.mine.a, lane) : 0.0f;
+          }
+          st = lp_merge<ENT>(one);
+          if (TOP) {
+            // the parts' lists: the top-th largest of a sample, the first 32 / parts of each list, bounds what is left to sort
+            u64 list[LP_MAX_CLUSTER];
+#pragma unroll
+            for (int p = 0; p < LP_MAX_CLUSTER; ++p) list[p] = p < parts ? lp_remote(&sh.best[lane], p) : 0;
+            const u64 sample = lp_remote(&sh.best[lane & ((32 >> log_parts) - 1)], lane >> (5 - log_parts));
+            const int above = lp_place32(sample, sh.buffer[turn]);
+            const int most = __reduce_max_sync(0xffffffffu, above < a.top ? above : -1);
+            const u64 bound = __shfl_sync(0xffffffffu, sample, __ffs(__ballot_sync(0xffffffffu, above == most)) - 1);
+            int count = 0;
+#pragma unroll
+            for (int p = 0; p < LP_MAX_CLUSTER; ++p) {
+              const bool yes = list[p] && list[p] >= bound;
+              const unsigned all = __ballot_sync(0xffffffffu, yes);
+              const int to = count + __popc(all & ((1u << lane) - 1));
+              if (yes && to < LP_BUFFER) sh.buffer[turn][to] = list[p];
+              count += __popc(all);
+            }
+            __syncwarp();
+            if (count <= LP_BUFFER) {
+              found = lp_sort_buffer(sh.buffer[turn], count);
+            } else {
+              found = list[0];
+#pragma unroll 1
+              for (int p = 1; p < parts; ++p) found = lp_merge32(found, lp_remote(&sh.best[31 - lane], p));
+            }
           }
         }
         lp_cluster_sync();           // no block leaves while its shared memory is read
@@ -544,23 +617,21 @@ __global__ void __launch_bounds__(LP_BLOCK, LP_BLOCKS_PER_SM<TOP>) logprobs_kern
     const int u0 = x.part_from(part, log_parts);
     const int u1 = x.part_from(part + 1, log_parts);
     const int chunks = (u1 - u0 + LP_CHUNK - 1) / LP_CHUNK;
-    const int last_place = u1 > u0 ? u0 + (chunks - 1) * LP_CHUNK : u0;
+    const int log_slot = lp_log_slot(chunks);
     float m = -INFINITY, c = -LP_FAR * LOG2E;
     u64 s2 = 0, w2 = 0;            // pairs of sums
-    int place = u0;                // first unit of the chunk of the maximum
     bool some = u1 - u0 >= LP_CHUNK;   // whether this thread has any element
     // the sums become relative to the new maximum um
-    auto raise_max = [&](float um, int at) {
+    auto raise_max = [&](float um) {
       const float nc = lp_base(um) * LOG2E, d = fmaxf(c - nc, -150.0f), f = lp_exp2(d);
       const u64 f2 = twa_pair(f, f);
       if (ENT) w2 = twa_mul2(f2, twa_fma2(twa_pair(d, d), s2, w2));
       s2 = twa_mul2(f2, s2);
       m = um;
       c = nc;
-      place = at;
     };
-    // a thread's units of the chunk that begins at unit `at`
-    auto take_units = [&](auto& units, int at) {
+    // some units of a thread; returns their maximum
+    auto take_units = [&](auto& units) {
       constexpr int N = sizeof(units) / sizeof(uint4);
       uint32_t high[N];
 #pragma unroll
@@ -570,7 +641,7 @@ __global__ void __launch_bounds__(LP_BLOCK, LP_BLOCKS_PER_SM<TOP>) logprobs_kern
 #pragma unroll
         for (int j = 0; j < half; ++j) high[j] = W::max2(high[j], high[j + half]);
       const float um = W::max1(high[0]);
-      if (um > m) raise_max(um, at);
+      if (um > m) raise_max(um);
       const u64 c2 = twa_pair(-c, -c), l2 = twa_pair(LOG2E, LOG2E);
 #pragma unroll
       for (int j = 0; j < N; ++j) {
@@ -588,21 +659,25 @@ __global__ void __launch_bounds__(LP_BLOCK, LP_BLOCKS_PER_SM<TOP>) logprobs_kern
           if (ENT) w2 = twa_fma2(p2, d2, w2);
         }
       }
+      return um;
     };
     // the row's ragged ends: thread 0 of the first part, thread 1 of the last
     const int ends = part == 0 && threadIdx.x == 0 ? 0 : (part == parts - 1 && threadIdx.x == 1 ? 1 : -1);
     const int end_from = ends == 0 ? 0 : x.tail_from(), end_to = ends == 0 ? x.head() : (ends == 1 ? a.vocab : 0);
-    auto take_ends = [&](int at) {
+    auto take_ends = [&] {
       for (int j = end_from; j < end_to; ++j) {
         const float z = twa_to_float(x.base[x.skew + j]);
         some = true;
-        if (z > m) raise_max(z, at);
+        if (z > m) raise_max(z);
         const float d = fmaf(z, LOG2E, -c), p = lp_exp2(d);
         s2 = twa_add2(s2, twa_pair(p, 0.0f));
         if (ENT) w2 = twa_fma2(twa_pair(p, 0.0f), twa_pair(fmaxf(d, -150.0f), 0.0f), w2);
       }
     };
-    if (ends == 0) take_ends(u0);
+    if (ends == 0) take_ends();
+    float part_max = -INFINITY;    // of the slot's part of the row
+    // the warp that finishes has taken this buffer's last row
+    if (round) twa_wait(&sh.row_empty[turn], (round & 1) ^ 1, &sh.gave_up, a.wait_limit_ns);
     for (int k = 0; k < chunks; ++k, ++it) {
       const int q = it % STAGES, n = min(LP_CHUNK, u1 - u0 - k * LP_CHUNK);
       // after a wait that ran out the row's results are not defined, and every later wait ends at once
@@ -613,20 +688,24 @@ __global__ void __launch_bounds__(LP_BLOCK, LP_BLOCKS_PER_SM<TOP>) logprobs_kern
         for (int j = 0; j < LP_PER_THREAD; ++j) w[j] = sh.ring[q][j * LP_THREADS + threadIdx.x];
         __syncwarp();
         if (lane == 0) twa_mbar_arrive(twa_smem_u32(&sh.empty[q]));
-        take_units(w, u0 + k * LP_CHUNK);
+        part_max = fmaxf(part_max, take_units(w));
       } else {
         // the last chunk, a unit a thread at a time; a warp without a unit has nothing to do
         for (int j = warp * 32; j < n; j += LP_THREADS) {
           uint4 w[1] = {make_uint4(W::NONE, W::NONE, W::NONE, W::NONE)};
           if (j + lane < n) w[0] = sh.ring[q][j + lane];
           some |= j + lane < n;
-          take_units(w, u0 + k * LP_CHUNK);
+          part_max = fmaxf(part_max, take_units(w));
         }
         __syncwarp();
         if (lane == 0) twa_mbar_arrive(twa_smem_u32(&sh.empty[q]));
       }
+      if (TOP && (((k + 1) & ((1 << log_slot) - 1)) == 0 || k + 1 == chunks)) {
+        sh.slot[turn][k >> log_slot][threadIdx.x] = part_max;
+        part_max = -INFINITY;
+      }
     }
-    if (ends == 1) take_ends(last_place);
+    if (ends == 1) take_ends();
 
     // ---- the warp's sums
     LpStat st = {m, 0.0f, 0.0f};
@@ -642,9 +721,8 @@ __global__ void __launch_bounds__(LP_BLOCK, LP_BLOCKS_PER_SM<TOP>) logprobs_kern
       st.s *= f;
     }
     st = lp_merge_near<ENT, 32>(st);
-    if (round) twa_wait(&sh.row_empty[turn], (round & 1) ^ 1, &sh.gave_up, a.wait_limit_ns);
     if (lane == 0) sh.stat[turn][warp] = st;
-    if (TOP) sh.key[turn][threadIdx.x] = some ? lp_key(m, place) : 0;
+    if (TOP) sh.key[turn][threadIdx.x] = some ? lp_rank(m) : 0;
     __syncwarp();
     if (lane == 0) twa_mbar_arrive(twa_smem_u32(&sh.row_full[turn]));
   }
