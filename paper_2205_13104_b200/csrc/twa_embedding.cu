@@ -13,8 +13,8 @@
 //
 // Most of what a whole table's gradient has to write are the zeros of rows that no token names.  They need the ids'
 // bitmap only, which the first, short kernel leaves: the kernels that sort, latency-bound on a few SMs, carry blocks that
-// write zeros on the others, and the rest of them go beside the sums.  Up to SMALL_TOKENS ids one block sorts them in
-// shared memory, in one launch.
+// write zeros on the others, and the rest of them go beside the sums.  Up to 16384 ids a cluster of blocks sorts them in
+// its shared memory, in one launch: that is shorter than the three launches that would carry zeros.
 #include "twa_ops.cuh"
 
 namespace {
@@ -24,10 +24,11 @@ constexpr int SORT_KEYS = 4;                               // keys of a thread
 constexpr int SORT_TILE = SORT_THREADS * SORT_KEYS;        // keys of a block
 constexpr int SORT_MAX_BITS = 9, SORT_BINS = 1 << SORT_MAX_BITS;
 constexpr int EMB_RUN = 32;                                // sorted entries a block adds up
-constexpr int SMALL_THREADS = 512, SMALL_WARPS = SMALL_THREADS / 32, SMALL_TOKENS = SMALL_THREADS * SORT_KEYS;
+constexpr int SMALL_THREADS = 512, SMALL_WARPS = SMALL_THREADS / 32, SMALL_TILE = SMALL_THREADS * SORT_KEYS;
+constexpr int SMALL_BLOCKS = 8, SMALL_TOKENS = SMALL_BLOCKS * SMALL_TILE;      // of a cluster
 constexpr int SMALL_BITS = 8, SMALL_BINS = 1 << SMALL_BITS;
-constexpr int SMALL_VOCAB = 1 << 20;                       // ids whose bitmap one block clears
-constexpr int FILL_BYTES = 1 << 16;                        // zeros of a block
+constexpr int SMALL_VOCAB = 1 << 20;                       // ids whose bitmap a block clears
+constexpr int FILL_BYTES = 1 << 15;                        // zeros of a block
 constexpr long long FILL_BESIDE_SORT = 32LL << 20;         // zeros written beside a sorting kernel: what its few us have room for
 
 // E elements of any pairing of the two types; E = 8 wants both addresses on 16 bytes, E = 1 nothing.
@@ -175,51 +176,62 @@ __device__ __forceinline__ void emb_fill(const EmbFill& f, int block) {
   }
 }
 
-// Up to SMALL_TOKENS ids sorted by one block; the bitmap too.
-__global__ void __launch_bounds__(SMALL_THREADS) emb_sort_small_kernel(const void* __restrict__ ids, int itype, int tokens, int vocab,
+// Ids sorted by one cluster of gridDim.x blocks, SMALL_TILE ids each in shared memory; the bitmap too.  Each pass moves a key
+// straight into the block of its new place.
+__global__ void __launch_bounds__(SMALL_THREADS) emb_sort_small_kernel(const void* ids, int itype, int tokens, int vocab,
                                                                        long long padding, int total_bits, uint32_t* used,
-                                                                       uint32_t* __restrict__ key_out,
-                                                                       uint32_t* __restrict__ pos_out, int* status) {
+                                                                       uint32_t* key_out, uint32_t* pos_out, int* status) {
   twa_begin(ids);
-  __shared__ uint32_t keys[SMALL_TOKENS];
-  __shared__ unsigned short place[SMALL_TOKENS];
+  __shared__ unsigned long long tile[SMALL_TILE];              // key, position
   __shared__ unsigned short count[SMALL_WARPS][SMALL_BINS];
+  __shared__ unsigned all_of[SMALL_BINS];                      // keys of each digit in this block
   __shared__ int warp_total[SMALL_BINS / 32];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, blocks = gridDim.x, rank = blockIdx.x;
   if (used) {
-    for (int i = threadIdx.x; i < (vocab + 31) / 32; i += SMALL_THREADS) used[i] = 0;
-    __syncthreads();
+    for (int i = rank * SMALL_THREADS + threadIdx.x; i < (vocab + 31) / 32; i += blocks * SMALL_THREADS) used[i] = 0;
+    twa_cluster_sync();
   }
-  const int t0 = warp * 32 * SORT_KEYS + lane;
-  uint32_t key[SORT_KEYS];
-  int pos[SORT_KEYS];
+  const int i0 = warp * 32 * SORT_KEYS + lane;
+  unsigned long long entry[SORT_KEYS];
 #pragma unroll
   for (int k = 0; k < SORT_KEYS; ++k) {
-    pos[k] = t0 + k * 32;
-    key[k] = 0xffffffffu;                            // beyond the tokens: after all of them, by stability and by digit
-    if (pos[k] < tokens) {
-      key[k] = emb_key(ids, itype, pos[k], vocab, padding, status);
-      if (used && key[k] < static_cast<uint32_t>(vocab)) atomicOr(&used[key[k] >> 5], 1u << (key[k] & 31));
+    const int t = rank * SMALL_TILE + i0 + k * 32;
+    uint32_t key = 0xffffffffu;                                // beyond the tokens: after all of them
+    if (t < tokens) {
+      key = emb_key(ids, itype, t, vocab, padding, status);
+      if (used && key < static_cast<uint32_t>(vocab)) atomicOr(&used[key >> 5], 1u << (key & 31));
     }
+    entry[k] = static_cast<unsigned long long>(key) << 32 | static_cast<uint32_t>(t);
   }
-  for (int shift = 0; shift < total_bits; shift += SMALL_BITS) {
-    for (int d = threadIdx.x; d < SMALL_WARPS * SMALL_BINS; d += SMALL_THREADS) (&count[0][0])[d] = 0;
+  for (int shift = 32; shift < 32 + total_bits; shift += SMALL_BITS) {
+    for (int d = threadIdx.x; d < SMALL_WARPS * SMALL_BINS / 2; d += SMALL_THREADS) reinterpret_cast<unsigned*>(count)[d] = 0;
     __syncthreads();
-    int rank[SORT_KEYS];
+    int before_me[SORT_KEYS];                                  // equal digits of the warp's earlier keys
 #pragma unroll
     for (int k = 0; k < SORT_KEYS; ++k) {
-      const int d = (key[k] >> shift) & (SMALL_BINS - 1);
+      const int d = static_cast<int>(entry[k] >> shift) & (SMALL_BINS - 1);
       const unsigned same = __match_any_sync(0xffffffffu, d);
       const int before = __popc(same & ((1u << lane) - 1));
-      rank[k] = count[warp][d] + before;
+      before_me[k] = count[warp][d] + before;
       __syncwarp();
       if (before == 0) count[warp][d] += static_cast<unsigned short>(__popc(same));
       __syncwarp();
     }
     __syncthreads();
-    int all = 0, sum = 0;
+    int here = 0;
     if (threadIdx.x < SMALL_BINS) {
-      for (int w = 0; w < SMALL_WARPS; ++w) all += count[w][threadIdx.x];
+      for (int w = 0; w < SMALL_WARPS; ++w) here += count[w][threadIdx.x];
+      all_of[threadIdx.x] = here;
+    }
+    twa_cluster_sync();                                        // every block's counts are there, and its tile has been read
+    // where the block's keys of each digit begin: smaller digits, then the digit in earlier blocks, then in earlier warps
+    int all = 0, earlier = 0, sum = 0;
+    if (threadIdx.x < SMALL_BINS) {
+      for (int b = 0; b < blocks; ++b) {
+        const int c = b == rank ? here : static_cast<int>(twa_remote(&all_of[threadIdx.x], b));
+        if (b < rank) earlier += c;
+        all += c;
+      }
       sum = all;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -230,7 +242,7 @@ __global__ void __launch_bounds__(SMALL_THREADS) emb_sort_small_kernel(const voi
     }
     __syncthreads();
     if (threadIdx.x < SMALL_BINS) {
-      int at = sum - all;
+      int at = sum - all + earlier;
       for (int w = 0; w < warp; ++w) at += warp_total[w];
       for (int w = 0; w < SMALL_WARPS; ++w) {
         const int c = count[w][threadIdx.x];
@@ -241,23 +253,21 @@ __global__ void __launch_bounds__(SMALL_THREADS) emb_sort_small_kernel(const voi
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < SORT_KEYS; ++k) {
-      const int to = count[warp][(key[k] >> shift) & (SMALL_BINS - 1)] + rank[k];
-      keys[to] = key[k];
-      place[to] = static_cast<unsigned short>(pos[k]);
+      const int to = count[warp][static_cast<int>(entry[k] >> shift) & (SMALL_BINS - 1)] + before_me[k];
+      twa_store_remote(&tile[to % SMALL_TILE], to / SMALL_TILE, entry[k]);
     }
-    __syncthreads();
+    twa_cluster_sync();
 #pragma unroll
-    for (int k = 0; k < SORT_KEYS; ++k) {
-      key[k] = keys[t0 + k * 32];
-      pos[k] = place[t0 + k * 32];
-    }
+    for (int k = 0; k < SORT_KEYS; ++k) entry[k] = tile[i0 + k * 32];
   }
 #pragma unroll
-  for (int k = 0; k < SORT_KEYS; ++k)
-    if (t0 + k * 32 < tokens) {
-      key_out[t0 + k * 32] = key[k];
-      pos_out[t0 + k * 32] = pos[k];
+  for (int k = 0; k < SORT_KEYS; ++k) {
+    const int t = rank * SMALL_TILE + i0 + k * 32;
+    if (t < tokens) {
+      key_out[t] = static_cast<uint32_t>(entry[k] >> 32);
+      pos_out[t] = static_cast<uint32_t>(entry[k]);
     }
+  }
 }
 
 // One pass of the radix sort over the digit at `shift`: stable, a tile per block, and blocks that write zeros.  key_in == null: the keys are the ids'.
@@ -439,52 +449,66 @@ __global__ void __launch_bounds__(SUM_THREADS) emb_sum_kernel(const uint32_t* __
   }
 }
 
-// An id that begins in run blockIdx.x and covers the next whole: its partial sums over the runs, JOIN_WAYS stretches of runs side by side;
-// the columns of blockIdx.y.
-constexpr int JOIN_WAYS = 8, JOIN_LANES = 32;
+// The ids that begin in one of the runs JOIN_RUNS * blockIdx.x .. and cover the next run whole: their partial sums over their
+// runs, JOIN_WAYS stretches of runs side by side; the columns of blockIdx.y.
+constexpr int JOIN_WAYS = 8, JOIN_LANES = 32, JOIN_RUNS = 16;
 template <typename TG, int E>
-__global__ void emb_join_kernel(const uint32_t* __restrict__ key, int tokens, int vocab, int dim, float scale,
-                                TG* __restrict__ dtable, long long ldg, int accumulate, const float* __restrict__ partial) {
+__global__ void __launch_bounds__(JOIN_WAYS* JOIN_LANES)
+    emb_join_kernel(const uint32_t* __restrict__ key, int tokens, int vocab, int dim, float scale, TG* __restrict__ dtable,
+                    long long ldg, int accumulate, const float* __restrict__ partial) {
   twa_begin(key, dtable, partial);
   __shared__ float part[JOIN_WAYS][JOIN_LANES][E + 1];
-  const int from = blockIdx.x, runs = (tokens + EMB_RUN - 1) / EMB_RUN;
-  const long long first = static_cast<long long>(from) * EMB_RUN, next = first + EMB_RUN;
-  const uint32_t id = key[next - 1];
-  if (next + EMB_RUN > tokens || key[next + EMB_RUN - 1] != id) return;
-  if (id >= static_cast<uint32_t>(vocab) || (first > 0 && key[first - 1] == id)) return;   // nothing, or begun in an earlier run
-  // its runs are from .. to - 1: those after `low` begin with it as far as all threads' probes reach, and so on ever closer
-  int low = from + 1, high = runs;
-  while (low + 1 < high) {
-    const int step = (high - low - 1 + JOIN_WAYS * JOIN_LANES - 1) / (JOIN_WAYS * JOIN_LANES);
-    const long long probe = low + (threadIdx.x + 1LL) * step;
-    const int inside = __syncthreads_count(probe < high && key[probe * EMB_RUN] == id);
-    const long long beyond = low + (inside + 1LL) * step;
-    low += inside * step;
-    if (beyond < high) high = static_cast<int>(beyond);
-  }
-  const int to = low + 1;
-  const int lane = threadIdx.x % JOIN_LANES, way = threadIdx.x / JOIN_LANES;
-  const int each = (to - from + JOIN_WAYS - 1) / JOIN_WAYS;
-  const int a = from + way * each, b = min(to, a + each);
-  const int c = (blockIdx.y * JOIN_LANES + lane) * E;
-  float sum[E];
-#pragma unroll
-  for (int e = 0; e < E; ++e) sum[e] = 0.0f;
-  if (c < dim)
-    for (int r = a; r < b; ++r) {
-      float v[E];
-      load_row<float, E>(partial + (static_cast<long long>(r) * 2 + (r == from ? 1 : 0)) * dim + c, v);
-#pragma unroll
-      for (int e = 0; e < E; ++e) sum[e] += v[e];
+  __shared__ unsigned begins;
+  const int runs = (tokens + EMB_RUN - 1) / EMB_RUN;
+  if (threadIdx.x < 32) {
+    const long long first = (static_cast<long long>(blockIdx.x) * JOIN_RUNS + threadIdx.x) * EMB_RUN, next = first + EMB_RUN;
+    bool yes = threadIdx.x < JOIN_RUNS && next + EMB_RUN <= tokens;
+    if (yes) {
+      const uint32_t id = key[next - 1], end = key[next + EMB_RUN - 1], before = first > 0 ? key[first - 1] : 0xffffffffu;
+      yes = id < static_cast<uint32_t>(vocab) && end == id && before != id;
     }
-#pragma unroll
-  for (int e = 0; e < E; ++e) part[way][lane][e] = sum[e];
+    const unsigned all = __ballot_sync(0xffffffffu, yes);
+    if (threadIdx.x == 0) begins = all;
+  }
   __syncthreads();
-  if (way == 0 && c < dim) {
-    for (int w = 1; w < JOIN_WAYS; ++w)
+  const int lane = threadIdx.x % JOIN_LANES, way = threadIdx.x / JOIN_LANES;
+  for (unsigned left = begins; left; left &= left - 1) {
+    const int from = blockIdx.x * JOIN_RUNS + __ffs(left) - 1;
+    const uint32_t id = key[from * static_cast<long long>(EMB_RUN) + EMB_RUN - 1];
+    // its runs are from .. to - 1: all threads probe the runs after `low`, ever closer together
+    int low = from + 1, high = runs;
+    while (low + 1 < high) {
+      const int step = (high - low - 1 + JOIN_WAYS * JOIN_LANES - 1) / (JOIN_WAYS * JOIN_LANES);
+      const long long probe = low + (threadIdx.x + 1LL) * step;
+      const int inside = __syncthreads_count(probe < high && key[probe * EMB_RUN] == id);
+      const long long beyond = low + (inside + 1LL) * step;
+      low += inside * step;
+      if (beyond < high) high = static_cast<int>(beyond);
+    }
+    const int to = low + 1;
+    const int each = (to - from + JOIN_WAYS - 1) / JOIN_WAYS;
+    const int a = from + way * each, b = min(to, a + each);
+    const int c = (blockIdx.y * JOIN_LANES + lane) * E;
+    float sum[E];
 #pragma unroll
-      for (int e = 0; e < E; ++e) sum[e] += part[w][lane][e];
-    emb_write<TG, E>(dtable + static_cast<long long>(id) * ldg + c, sum, scale, accumulate);
+    for (int e = 0; e < E; ++e) sum[e] = 0.0f;
+    if (c < dim)
+      for (int r = a; r < b; ++r) {
+        float v[E];
+        load_row<float, E>(partial + (static_cast<long long>(r) * 2 + (r == from ? 1 : 0)) * dim + c, v);
+#pragma unroll
+        for (int e = 0; e < E; ++e) sum[e] += v[e];
+      }
+#pragma unroll
+    for (int e = 0; e < E; ++e) part[way][lane][e] = sum[e];
+    __syncthreads();
+    if (way == 0 && c < dim) {
+      for (int w = 1; w < JOIN_WAYS; ++w)
+#pragma unroll
+        for (int e = 0; e < E; ++e) sum[e] += part[w][lane][e];
+      emb_write<TG, E>(dtable + static_cast<long long>(id) * ldg + c, sum, scale, accumulate);
+    }
+    __syncthreads();
   }
 }
 
@@ -528,7 +552,7 @@ void launch_sums(twa_ctx* ctx, const EmbSpace& s, const uint32_t* key, const uin
     twa_launch(ctx->stream, emb_sum_kernel<TD, TG, E>, runs * column_blocks + zeros, SUM_THREADS, 0, key, pos, tokens, vocab, dim, static_cast<const TD*>(dout), ldd, scale, g, ldg, accumulate, s.partial, column_blocks,
         runs * column_blocks, rest);
   if (tokens >= 2 * EMB_RUN)
-    twa_launch(ctx->stream, emb_join_kernel<TG, E>, dim3(runs - 1, static_cast<unsigned>(twa_ceil_div(dim, E * JOIN_LANES))), JOIN_WAYS * JOIN_LANES, 0, key, tokens, vocab, dim, scale, g, ldg, accumulate, s.partial);
+    twa_launch(ctx->stream, emb_join_kernel<TG, E>, dim3(static_cast<unsigned>(twa_ceil_div(runs - 1, JOIN_RUNS)), static_cast<unsigned>(twa_ceil_div(dim, E * JOIN_LANES))), JOIN_WAYS * JOIN_LANES, 0, key, tokens, vocab, dim, scale, g, ldg, accumulate, s.partial);
 }
 
 template <typename TD, typename TG>
@@ -592,7 +616,8 @@ int twa_embedding_backward(twa_ctx* ctx, const void* dout, int64_t ldd, twa_dtyp
   if (fill.bytes < FILL_BYTES) fill.each = static_cast<int>(FILL_BYTES / fill.bytes);
   int at = 0;
   if (n <= SMALL_TOKENS && vocab <= SMALL_VOCAB) {
-    twa_launch(ctx->stream, emb_sort_small_kernel, 1, SMALL_THREADS, 0, ids, id_type, n, vocab, padding_id, total_bits,
+    const int blocks = n <= SMALL_TILE ? 1 : (n <= 2 * SMALL_TILE ? 2 : (n <= 4 * SMALL_TILE ? 4 : 8));
+    twa_launch_clusters(ctx->stream, emb_sort_small_kernel, blocks, blocks, SMALL_THREADS, 0, ids, id_type, n, vocab, padding_id, total_bits,
                                                                 accumulate ? nullptr : s.used, s.key[at], s.pos[at], ctx->d_status);
   } else {
     TWA_CUDA_OK(ctx, cudaMemsetAsync(s.used, 0, reinterpret_cast<char*>(s.key[0]) - reinterpret_cast<char*>(s.used), ctx->stream));

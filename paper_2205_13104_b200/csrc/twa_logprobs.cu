@@ -265,31 +265,6 @@ struct LpShared {
   int gave_up;
 };
 
-__device__ __forceinline__ uint32_t lp_cluster_rank() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ void lp_cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-template <typename V>
-__device__ __forceinline__ V lp_remote(const V* p, uint32_t rank) {
-  uint32_t at;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(twa_smem_u32(p)), "r"(rank));
-  V v;
-  if constexpr (sizeof(V) == 8) {
-    u64 w;
-    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(w) : "r"(at) : "memory");
-    v = w;
-  } else {
-    uint32_t w;
-    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(w) : "r"(at) : "memory");
-    memcpy(&v, &w, 4);
-  }
-  return v;
-}
-
 // By one warp, for rows that are out of the ordinary.  Sums over row[from .. to - 1] with differences to m taken first;
 template <typename T, bool ENT>
 __device__ __noinline__ LpStat lp_sum_far(const T* row, int from, int to, float m) {
@@ -337,7 +312,7 @@ __global__ void __launch_bounds__(LP_BLOCK, LP_BLOCKS_PER_SM<TOP>) logprobs_kern
   extern __shared__ __align__(128) unsigned char lp_smem[];
   constexpr int STAGES = LP_STAGES<TOP>;
   LpShared<TOP>& sh = *reinterpret_cast<LpShared<TOP>*>(lp_smem);
-  const int part = parts > 1 ? static_cast<int>(lp_cluster_rank()) : 0;
+  const int part = parts > 1 ? static_cast<int>(twa_cluster_rank()) : 0;
   const long long row0 = blockIdx.x >> log_parts, rows_step = gridDim.x >> log_parts;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   if (threadIdx.x == 0) {
@@ -387,8 +362,8 @@ __global__ void __launch_bounds__(LP_BLOCK, LP_BLOCKS_PER_SM<TOP>) logprobs_kern
     }
     __syncwarp();
     if (parts > 1) {
-      lp_cluster_sync();
-      lp_cluster_sync();
+      twa_cluster_sync();
+      twa_cluster_sync();
     }
     return;
   }
@@ -397,8 +372,8 @@ __global__ void __launch_bounds__(LP_BLOCK, LP_BLOCKS_PER_SM<TOP>) logprobs_kern
     // ---- finish
     const int turn = warp - LP_FINISH;
     if (parts > 1 && turn) {       // a cluster has one row
-      lp_cluster_sync();
-      lp_cluster_sync();
+      twa_cluster_sync();
+      twa_cluster_sync();
       return;
     }
     int r = 0;                     // of this warp's rows
@@ -541,22 +516,22 @@ __global__ void __launch_bounds__(LP_BLOCK, LP_BLOCKS_PER_SM<TOP>) logprobs_kern
       if (parts > 1) {
         if (lane == 0) sh.mine = st;
         if (TOP) sh.best[lane] = found;
-        lp_cluster_sync();
+        twa_cluster_sync();
         if (part == 0) {
           // a lane a part's sums
           LpStat one = {-INFINITY, 0.0f, 0.0f};
           if (lane < parts) {
-            one.m = lp_remote(&sh.mine.m, lane);
-            one.s = lp_remote(&sh.mine.s, lane);
-            one.a = ENT ? lp_remote(&sh.mine.a, lane) : 0.0f;
+            one.m = twa_remote(&sh.mine.m, lane);
+            one.s = twa_remote(&sh.mine.s, lane);
+            one.a = ENT ? twa_remote(&sh.mine.a, lane) : 0.0f;
           }
           st = lp_merge<ENT>(one);
           if (TOP) {
             // the parts' lists: the top-th largest of a sample, the first 32 / parts of each list, bounds what is left to sort
             u64 list[LP_MAX_CLUSTER];
 #pragma unroll
-            for (int p = 0; p < LP_MAX_CLUSTER; ++p) list[p] = p < parts ? lp_remote(&sh.best[lane], p) : 0;
-            const u64 sample = lp_remote(&sh.best[lane & ((32 >> log_parts) - 1)], lane >> (5 - log_parts));
+            for (int p = 0; p < LP_MAX_CLUSTER; ++p) list[p] = p < parts ? twa_remote(&sh.best[lane], p) : 0;
+            const u64 sample = twa_remote(&sh.best[lane & ((32 >> log_parts) - 1)], lane >> (5 - log_parts));
             const int above = lp_place32(sample, sh.buffer[turn]);
             const int most = __reduce_max_sync(0xffffffffu, above < a.top ? above : -1);
             const u64 bound = __shfl_sync(0xffffffffu, sample, __ffs(__ballot_sync(0xffffffffu, above == most)) - 1);
@@ -575,11 +550,11 @@ __global__ void __launch_bounds__(LP_BLOCK, LP_BLOCKS_PER_SM<TOP>) logprobs_kern
             } else {
               found = list[0];
 #pragma unroll 1
-              for (int p = 1; p < parts; ++p) found = lp_merge32(found, lp_remote(&sh.best[31 - lane], p));
+              for (int p = 1; p < parts; ++p) found = lp_merge32(found, twa_remote(&sh.best[31 - lane], p));
             }
           }
         }
-        lp_cluster_sync();           // no block leaves while its shared memory is read
+        twa_cluster_sync();           // no block leaves while its shared memory is read
         if (part != 0) return;
       }
       const float logs = LN2 * log2f(st.s);
@@ -727,8 +702,8 @@ __global__ void __launch_bounds__(LP_BLOCK, LP_BLOCKS_PER_SM<TOP>) logprobs_kern
     if (lane == 0) twa_mbar_arrive(twa_smem_u32(&sh.row_full[turn]));
   }
   if (parts > 1) {
-    lp_cluster_sync();
-    lp_cluster_sync();
+    twa_cluster_sync();
+    twa_cluster_sync();
   }
 }
 
@@ -792,21 +767,10 @@ int lp_launch(twa_ctx* ctx, const LpArgs& a, int log_parts) {
   const void* kernel = reinterpret_cast<const void*>(logprobs_kernel<T, ENT, TOP>);
   int rc = twa_ensure_smem(ctx, kernel, &smem_set[ctx->device & 63], sizeof(LpShared<TOP>));
   if (rc) return rc;
-  cudaLaunchConfig_t cfg = {};
   const long long most = static_cast<long long>(ctx->sm_count) * LP_BLOCKS_PER_SM<TOP>;
-  cfg.gridDim = dim3(static_cast<unsigned>(parts > 1 ? a.rows * parts : (a.rows < most ? a.rows : most)));
-  cfg.blockDim = dim3(LP_BLOCK);
-  cfg.dynamicSmemBytes = sizeof(LpShared<TOP>);
-  cfg.stream = ctx->stream;
-  cudaLaunchAttribute attr[2] = {};
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = parts;
-  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = parts > 1 ? 2 : 1;
-  TWA_CUDA_OK(ctx, cudaLaunchKernelEx(&cfg, logprobs_kernel<T, ENT, TOP>, a, log_parts));
+  const unsigned blocks = static_cast<unsigned>(parts > 1 ? a.rows * parts : (a.rows < most ? a.rows : most));
+  TWA_CUDA_OK(ctx, twa_launch_clusters(ctx->stream, logprobs_kernel<T, ENT, TOP>, blocks, parts, LP_BLOCK, sizeof(LpShared<TOP>), a,
+                                       log_parts));
   return TWA_OK;
 }
 

@@ -4,6 +4,7 @@
 
 #include <cuda_bf16.h>
 #include <stdio.h>
+#include <string.h>
 
 #include "twa_common.cuh"
 
@@ -168,6 +169,39 @@ __device__ __forceinline__ void twa_bulk_load(uint32_t dst, const void* src, uin
                : "memory");
 }
 
+// Thread-block clusters: this block's rank, a barrier of all the cluster's threads, and loads and stores of a variable of this
+// block's shared memory in the block `rank`.
+__device__ __forceinline__ uint32_t twa_cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void twa_cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+template <typename V>
+__device__ __forceinline__ V twa_remote(const V* p, uint32_t rank) {
+  uint32_t at;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(twa_smem_u32(p)), "r"(rank));
+  V v;
+  if constexpr (sizeof(V) == 8) {
+    unsigned long long w;
+    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(w) : "r"(at) : "memory");
+    v = w;
+  } else {
+    uint32_t w;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(w) : "r"(at) : "memory");
+    memcpy(&v, &w, 4);
+  }
+  return v;
+}
+
+__device__ __forceinline__ void twa_store_remote(unsigned long long* p, uint32_t rank, unsigned long long v) {
+  uint32_t at;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(twa_smem_u32(p)), "r"(rank));
+  asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(at), "l"(v) : "memory");
+}
+
 // Launches that may begin while the kernel before them in the stream ends (programmatic dependent launch).  A kernel launched
 // so first calls twa_begin(pointers it reads ...), which goes on when the kernels before it are complete and their writes
 // visible.  The pointers come out of the call as new values, so that no load through them, not even one of data the compiler
@@ -182,16 +216,24 @@ __device__ __forceinline__ void twa_begin(P&... pointers) {
 }
 
 template <typename... Params, typename... Args>
-cudaError_t twa_launch(cudaStream_t stream, void (*kernel)(Params...), dim3 grid, int threads, size_t smem, Args... args) {
+cudaError_t twa_launch_clusters(cudaStream_t stream, void (*kernel)(Params...), dim3 grid, int cluster, int threads, size_t smem,
+                                Args... args) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
-  cudaLaunchAttribute attr = {};
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
+  cudaLaunchAttribute attr[2] = {};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = cluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kernel, static_cast<Params>(args)...);
+}
+template <typename... Params, typename... Args>
+cudaError_t twa_launch(cudaStream_t stream, void (*kernel)(Params...), dim3 grid, int threads, size_t smem, Args... args) {
+  return twa_launch_clusters(stream, kernel, grid, 1, threads, smem, args...);
 }
