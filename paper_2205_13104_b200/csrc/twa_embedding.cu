@@ -14,7 +14,7 @@
 // Most of what a whole table's gradient has to write are the zeros of rows that no token names.  They need the ids'
 // bitmap only, which the first, short kernel leaves: the kernels that sort, latency-bound on a few SMs, carry blocks that
 // write zeros on the others, and the rest of them go beside the sums.  Up to 16384 ids a cluster of blocks sorts them in
-// its shared memory, in one launch: that is shorter than the three launches that would carry zeros.
+// its shared memory, in one launch; the zeros beside it go to rows whether used or not (the sums come later).
 #include "twa_ops.cuh"
 
 namespace {
@@ -29,7 +29,9 @@ constexpr int SMALL_BLOCKS = 8, SMALL_TOKENS = SMALL_BLOCKS * SMALL_TILE;      /
 constexpr int SMALL_BITS = 8, SMALL_BINS = 1 << SMALL_BITS;
 constexpr int SMALL_VOCAB = 1 << 20;                       // ids whose bitmap a block clears
 constexpr int FILL_BYTES = 1 << 15;                        // zeros of a block
-constexpr long long FILL_BESIDE_SORT = 32LL << 20;         // zeros written beside a sorting kernel: what its few us have room for
+// Zeros written beside a sorting kernel: what its few us have room for, and those of the cluster's sort (16384 x 2048 into 50272
+// rows: 107.5 us with 32 MB beside that, 103.7 with 64, 99.6 with 96).
+constexpr long long FILL_BESIDE_SORT = 32LL << 20, FILL_BESIDE_CLUSTER = 96LL << 20;
 
 // E elements of any pairing of the two types; E = 8 wants both addresses on 16 bytes, E = 1 nothing.
 template <typename T, int E>
@@ -147,17 +149,17 @@ struct EmbFill {
   char* table;
   long long stride;             // bytes between rows
   long long bytes;              // of a row
-  const uint32_t* used;
+  const uint32_t* used;         // null: all rows
   int row0, row1, each;         // rows row0 .. row1 - 1
   int size;                     // of an element
 };
-// Zeros into the unused ones of the block's rows: 16 bytes a store between the ragged ends.
+// Zeros into the unused ones of the block's rows (or all): 16 bytes a store between the ragged ends.
 __device__ __forceinline__ void emb_fill(const EmbFill& f, int block) {
-  const int r0 = f.row0 + block * f.each, rows = min(f.each, f.row1 - r0);
+  const int r0 = f.row0 + block * f.each, rows = min(f.each, f.row1 - r0);      // none for a cluster's spare blocks
   const int slots = static_cast<int>(f.bytes / 16) + 1;           // 0: the ends
   for (int i = threadIdx.x; i < rows * slots; i += blockDim.x) {
     const int r = i / slots, slot = i - r * slots, v = r0 + r;
-    if (__ldg(f.used + (v >> 5)) >> (v & 31) & 1) continue;
+    if (f.used && (__ldg(f.used + (v >> 5)) >> (v & 31) & 1)) continue;
     char* row = f.table + v * f.stride;
     const int head = static_cast<int>(min(f.bytes, static_cast<long long>(-reinterpret_cast<uintptr_t>(row) & 15)));
     const int whole = static_cast<int>((f.bytes - head) / 16);
@@ -176,17 +178,21 @@ __device__ __forceinline__ void emb_fill(const EmbFill& f, int block) {
   }
 }
 
-// Ids sorted by one cluster of gridDim.x blocks, SMALL_TILE ids each in shared memory; the bitmap too.  Each pass moves a key
-// straight into the block of its new place.
+// Ids sorted by the first cluster, SMALL_TILE ids a block in shared memory; the bitmap too.  Each pass moves a key straight into
+// the block of its new place.  The other clusters' blocks write zeros.
 __global__ void __launch_bounds__(SMALL_THREADS) emb_sort_small_kernel(const void* ids, int itype, int tokens, int vocab,
                                                                        long long padding, int total_bits, uint32_t* used,
-                                                                       uint32_t* key_out, uint32_t* pos_out, int* status) {
+                                                                       uint32_t* key_out, uint32_t* pos_out, int* status, int blocks, const EmbFill fill) {
   twa_begin(ids);
+  if (static_cast<int>(blockIdx.x) >= blocks) {
+    emb_fill(fill, blockIdx.x - blocks);
+    return;
+  }
   __shared__ unsigned long long tile[SMALL_TILE];              // key, position
   __shared__ unsigned short count[SMALL_WARPS][SMALL_BINS];
   __shared__ unsigned all_of[SMALL_BINS];                      // keys of each digit in this block
   __shared__ int warp_total[SMALL_BINS / 32];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, blocks = gridDim.x, rank = blockIdx.x;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rank = blockIdx.x;
   if (used) {
     for (int i = rank * SMALL_THREADS + threadIdx.x; i < (vocab + 31) / 32; i += blocks * SMALL_THREADS) used[i] = 0;
     twa_cluster_sync();
@@ -617,8 +623,15 @@ int twa_embedding_backward(twa_ctx* ctx, const void* dout, int64_t ldd, twa_dtyp
   int at = 0;
   if (n <= SMALL_TOKENS && vocab <= SMALL_VOCAB) {
     const int blocks = n <= SMALL_TILE ? 1 : (n <= 2 * SMALL_TILE ? 2 : (n <= 4 * SMALL_TILE ? 4 : 8));
-    twa_launch_clusters(ctx->stream, emb_sort_small_kernel, blocks, blocks, SMALL_THREADS, 0, ids, id_type, n, vocab, padding_id, total_bits,
-                                                                accumulate ? nullptr : s.used, s.key[at], s.pos[at], ctx->d_status);
+    EmbFill part;
+    const unsigned zeros = emb_fill_blocks(fill, FILL_BESIDE_CLUSTER, &part);
+    part.used = nullptr;
+    const unsigned grid = blocks + static_cast<unsigned>(twa_ceil_div(zeros, blocks)) * blocks;
+    const cudaError_t launched =
+        twa_launch_clusters(ctx->stream, emb_sort_small_kernel, grid, blocks, SMALL_THREADS, 0, ids, id_type, n, vocab, padding_id,
+                            total_bits, accumulate ? nullptr : s.used, s.key[at], s.pos[at], ctx->d_status, blocks, part);
+    TWA_CUDA_OK(ctx, launched);
+    fill.row0 = part.row1;
   } else {
     TWA_CUDA_OK(ctx, cudaMemsetAsync(s.used, 0, reinterpret_cast<char*>(s.key[0]) - reinterpret_cast<char*>(s.used), ctx->stream));
     const int passes = (total_bits + SORT_MAX_BITS - 1) / SORT_MAX_BITS, bits = (total_bits + passes - 1) / passes;
