@@ -504,6 +504,7 @@ typedef enum { TWA_I32 = 0, TWA_I64 = 1 } twa_itype; /* type of token numbers */
 #define TWA_LAYER_NORM_MAX_COLS (1 << 24)
 #define TWA_EMBEDDING_MAX_TOKENS (1 << 24)
 #define TWA_EMBEDDING_MAX_DIM (1 << 15)
+#define TWA_EMBEDDING_MAX_VOCAB (1 << 30)
 #define TWA_LOGPROBS_MAX_ROWS (1 << 24)
 #define TWA_LOGPROBS_MAX_VOCAB (1 << 24)
 #define TWA_LOGPROBS_MAX_TOP 32

@@ -577,7 +577,7 @@ int twa_embedding(twa_ctx* ctx, const void* table, int64_t ldt, twa_dtype t_dtyp
                   twa_itype id_type, int64_t tokens, float scale, void* out, int64_t ldo, twa_dtype out_dtype) {
   if (!ctx || !twa_dtype_ok(t_dtype) || !twa_dtype_ok(out_dtype) || !twa_itype_ok(id_type)) return TWA_ERR_INVALID_ARG;
   if (vocab < 1 || dim < 1 || tokens < 0) return TWA_ERR_INVALID_ARG;
-  if (tokens > TWA_EMBEDDING_MAX_TOKENS || dim > TWA_EMBEDDING_MAX_DIM) return TWA_ERR_UNSUPPORTED;
+  if (tokens > TWA_EMBEDDING_MAX_TOKENS || dim > TWA_EMBEDDING_MAX_DIM || vocab > TWA_EMBEDDING_MAX_VOCAB) return TWA_ERR_UNSUPPORTED;
   if (tokens == 0) return TWA_OK;
   if (!table || !ids || !out || ldt < dim || ldo < dim) return TWA_ERR_INVALID_ARG;
   const size_t ts = twa_dtype_size(t_dtype), os = twa_dtype_size(out_dtype);
@@ -595,7 +595,7 @@ int twa_embedding(twa_ctx* ctx, const void* table, int64_t ldt, twa_dtype t_dtyp
 }
 
 size_t twa_embedding_workspace_bytes(int64_t tokens, int vocab, int dim) {
-  if (tokens < 0 || tokens > TWA_EMBEDDING_MAX_TOKENS || vocab < 1 || dim < 1 || dim > TWA_EMBEDDING_MAX_DIM) return 0;
+  if (tokens < 0 || tokens > TWA_EMBEDDING_MAX_TOKENS || vocab < 1 || vocab > TWA_EMBEDDING_MAX_VOCAB || dim < 1 || dim > TWA_EMBEDDING_MAX_DIM) return 0;
   return emb_space(nullptr, tokens, vocab, dim).bytes;
 }
 
@@ -604,7 +604,7 @@ int twa_embedding_backward(twa_ctx* ctx, const void* dout, int64_t ldd, twa_dtyp
                            twa_dtype g_dtype, int accumulate, void* ws, size_t ws_bytes) {
   if (!ctx || !twa_dtype_ok(d_dtype) || !twa_dtype_ok(g_dtype) || !twa_itype_ok(id_type)) return TWA_ERR_INVALID_ARG;
   if (vocab < 1 || dim < 1 || tokens < 0 || accumulate < 0 || accumulate > 1) return TWA_ERR_INVALID_ARG;
-  if (tokens > TWA_EMBEDDING_MAX_TOKENS || dim > TWA_EMBEDDING_MAX_DIM) return TWA_ERR_UNSUPPORTED;
+  if (tokens > TWA_EMBEDDING_MAX_TOKENS || dim > TWA_EMBEDDING_MAX_DIM || vocab > TWA_EMBEDDING_MAX_VOCAB) return TWA_ERR_UNSUPPORTED;
   if (!dtable || ldg < dim || (tokens && (!dout || !ids || ldd < dim))) return TWA_ERR_INVALID_ARG;
   const size_t ds = twa_dtype_size(d_dtype), gs = twa_dtype_size(g_dtype);
   if (twa_misaligned_to(dout, ds) || twa_misaligned_to(dtable, gs) || twa_misaligned_to(ids, twa_itype_size(id_type)))

@@ -10,6 +10,7 @@ constexpr int LN_WARP_THREADS = 128;   // a warp or less per row: threads of a b
 constexpr int LN_BLOCK_THREADS = 512;  // a block per row: at most
 constexpr int LN_WIDE_THREADS = 1024, LN_WIDE_HELD = 16;
 constexpr int LN_LOOP_THREADS = 512;   // rows wider than the registers of a block
+constexpr int LN_LOOP_PARTS = 64;      // and the rows of partial sums for those
 constexpr int LN_MAX_SMEM = 220 * 1024;
 
 struct LnArgs {

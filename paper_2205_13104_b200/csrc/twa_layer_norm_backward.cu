@@ -440,7 +440,8 @@ extern "C" {
 
 size_t twa_layer_norm_workspace_bytes(int64_t rows, int cols) {
   if (rows < 0 || cols < 1) return 0;
-  const long long blocks = rows < LN_MAX_BLOCKS ? (rows + 8) / 8 * 8 : LN_MAX_BLOCKS;      // a plan rounds up by classes
+  const long long most = cols > LN_WIDE_THREADS * LN_WIDE_HELD ? LN_LOOP_PARTS : LN_MAX_BLOCKS;
+  const long long blocks = rows < most ? (rows + 8) / 8 * 8 : most;      // a plan rounds up by classes
   return twa_round256(sizeof(float) * 2 * static_cast<size_t>(cols) * blocks);
 }
 
@@ -472,14 +473,14 @@ int twa_layer_norm_backward(twa_ctx* ctx, const void* dy, int64_t lddy, const vo
     rc = dtype == TWA_BF16 ? ln_plan<bf16, true>(ctx, classes, rows, cols, &p) : ln_plan<float, true>(ctx, classes, rows, cols, &p);
     if (rc) return rc;
     a.log_lanes = p.log_lanes;
-  a.log_classes = p.log_classes;
+    a.log_classes = p.log_classes;
     if (p.kernel) {
       parts = p.blocks;
       twa_launch(ctx->stream, p.kernel, p.blocks, p.threads, p.smem, a);
     } else {
       const int blocks = static_cast<int>(rows < 8LL * ctx->sm_count ? rows : 8LL * ctx->sm_count);
       if (weights) {
-        parts = static_cast<int>(rows < 64 ? rows : 64);
+        parts = static_cast<int>(rows < LN_LOOP_PARTS ? rows : LN_LOOP_PARTS);
         const dim3 grid(static_cast<unsigned>(twa_ceil_div(cols, 256)), parts);
         if (dtype == TWA_BF16) twa_launch(ctx->stream, ln_weights_loop_kernel<bf16>, grid, 256, 0, a);
         else twa_launch(ctx->stream, ln_weights_loop_kernel<float>, grid, 256, 0, a);

@@ -33,6 +33,12 @@ TWA_F32 = 0
 TWA_BF16 = 1
 TWA_I32 = 0
 TWA_I64 = 1
+TWA_LAYER_NORM_MAX_COLS = 1 << 24
+TWA_EMBEDDING_MAX_TOKENS = 1 << 24
+TWA_EMBEDDING_MAX_DIM = 1 << 15
+TWA_EMBEDDING_MAX_VOCAB = 1 << 30
+TWA_LOGPROBS_MAX_ROWS = 1 << 24
+TWA_LOGPROBS_MAX_VOCAB = 1 << 24
 TWA_LOGPROBS_MAX_TOP = 32
 TWA_MAX_TENSORS = 65536
 TWA_TUNE_PROJECT_WARPS = 1

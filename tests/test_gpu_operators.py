@@ -632,6 +632,10 @@ def test_refusals(ctx):
     refused(twa.TWA_ERR_WORKSPACE, twa.twa_layer_norm_backward, ctx, x, x, w, v, v, x, w, w, None)
     refused(twa.TWA_ERR_MISALIGNED, twa.twa_layer_norm_backward, ctx, x, x, w, v, v, x, w, w, ws[1:])
     refused(twa.TWA_ERR_WORKSPACE, twa.twa_embedding_backward, ctx, x, ids, 1.0, x, small)
+    many = torch.empty(twa.TWA_EMBEDDING_MAX_VOCAB + 1, 1, dtype=BF16, device=DEV)
+    refused(twa.TWA_ERR_UNSUPPORTED, twa.twa_embedding, ctx, many, ids, 1.0, x[:, :1])
+    refused(twa.TWA_ERR_UNSUPPORTED, twa.twa_embedding_backward, ctx, x[:, :1], ids, 1.0, many, ws)
+    del many
     refused(twa.TWA_ERR_INVALID_ARG, twa.twa_token_logprobs, ctx, x, ids, v, v, top_ids=torch.zeros(4, 9, dtype=torch.int32, device=DEV),
             top_logp=torch.zeros(4, 9, device=DEV))
     wide = torch.zeros(4, 64, device=DEV)

@@ -18,6 +18,14 @@ def test_workspace_sizes():
     assert twa.twa_grad_norm_workspace_bytes(twa.TWA_MAX_TENSORS + 1) == 0
 
 
+def test_workspaces_of_the_widest_rows_and_the_largest_vocabularies():
+    twa.build_library()
+    cols = twa.TWA_LAYER_NORM_MAX_COLS
+    assert 64 * 2 * 4 * cols <= twa.twa_layer_norm_workspace_bytes(1 << 20, cols) <= 65 * 2 * 4 * cols
+    assert twa.twa_embedding_workspace_bytes(4, twa.TWA_EMBEDDING_MAX_VOCAB, 4) > twa.TWA_EMBEDDING_MAX_VOCAB // 8
+    assert twa.twa_embedding_workspace_bytes(4, twa.TWA_EMBEDDING_MAX_VOCAB + 1, 4) == 0
+
+
 def test_calls_without_a_context_are_refused():
     twa.build_library()
     lib = twa.load()
