@@ -158,22 +158,22 @@ __global__ void __launch_bounds__(LN_THREADS<PER>, 512 / LN_THREADS<PER>) ln_for
 template <typename T>
 __global__ void ln_forward_loop_kernel(LnArgs a) {
   twa_begin(a.x, a.w, a.b);
-  __shared__ float red[2][32][1];
+  __shared__ float red[2][32][2];
   int turn = 0;
   const T* x = static_cast<const T*>(a.x);
   T* y = static_cast<T*>(a.y);
   for (long long r = blockIdx.x; r < a.rows; r += gridDim.x) {
     const T* xr = x + r * a.ldx;
-    float s[1] = {0.0f};
+    float s[2] = {0.0f, 0.0f};
     for (int c = threadIdx.x; c < a.cols; c += blockDim.x) s[0] += twa_to_float(xr[c]);
-    block_sum<1>(s, red, turn);
+    ln_block_sums<0>(s, red, turn);
     const float mean = s[0] / static_cast<float>(a.cols);
-    float q[1] = {0.0f};
+    float q[2] = {0.0f, 0.0f};
     for (int c = threadIdx.x; c < a.cols; c += blockDim.x) {
       const float d = twa_to_float(xr[c]) - mean;
       q[0] += d * d;
     }
-    block_sum<1>(q, red, turn);
+    ln_block_sums<0>(q, red, turn);
     const float rstd = 1.0f / sqrtf(q[0] / static_cast<float>(a.cols) + a.eps);
     if (threadIdx.x == 0) {
       if (a.mean) a.mean[r] = mean;

@@ -42,24 +42,43 @@ __device__ __forceinline__ float ln_sum_lanes(float v, int log_lanes) {
   }
 }
 
-// Sum of N values over the block (one barrier; `red` is used in turn by successive calls, two sets, so that a set is
-// written again only after the next barrier).
-template <int N>
-__device__ __forceinline__ void block_sum(float (&v)[N], float (*red)[32][N], int& turn) {
+// Sums of a (lanes 0 .. 15) and b (lanes 16 .. 31) over a warp: after the first step each half goes on with one of them.
+__device__ __forceinline__ float ln_two_sums(float a, float b) {
+  const bool upper = threadIdx.x & 16;
+  float v = upper ? b : a;
+  v += __shfl_xor_sync(0xffffffffu, upper ? a : b, 16);
 #pragma unroll
-  for (int i = 0; i < N; ++i) v[i] = twa_warp_sum(v[i]);
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-  float(*set)[N] = red[turn];
+  for (int o = 8; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+
+// Sums of v[0] and v[1] over the block of WARPS warps (0: as it was launched), one barrier.  What follows the barrier is the
+// longest chain of a row: with the warps known it is two loads (gradient of 16384 x 2048 bfloat16: 39.4 us, with a loop and ten
+// shuffles instead of five 48.3), for 32 warps a loop is better (2048 x 12000: 67.7 us, unrolled 76.2). `red` is used in turn by
+// successive calls, two sets, so that a set is written again only after the next barrier.
+template <int WARPS>
+__device__ __forceinline__ void ln_block_sums(float (&v)[2], float (*red)[32][2], int& turn) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const float mine = ln_two_sums(v[0], v[1]);
+  float(*set)[2] = red[turn];
   turn ^= 1;
-  if (lane == 0)
-#pragma unroll
-    for (int i = 0; i < N; ++i) set[warp][i] = v[i];
+  if ((lane & 15) == 0) set[warp][lane >> 4] = mine;
   __syncthreads();
+  v[0] = v[1] = 0.0f;
+  if constexpr (WARPS != 0) {
 #pragma unroll
-  for (int i = 0; i < N; ++i) v[i] = 0.0f;
-  for (int w = 0; w < warps; ++w)
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] += set[w][i];
+    for (int w = 0; w < WARPS; w += 2) {
+      const float4 q = *reinterpret_cast<const float4*>(set[w]);
+      v[0] = v[0] + q.x + q.z;
+      v[1] = v[1] + q.y + q.w;
+    }
+  } else {
+    const int warps = blockDim.x >> 5;
+    for (int w = 0; w < warps; ++w) {
+      v[0] += set[w][0];
+      v[1] += set[w][1];
+    }
+  }
 }
 
 // PER: threads of a row.  32: a warp; more: a block of so many; 0: a part of a warp, 2^log_lanes threads.  With PER known all

@@ -12,7 +12,7 @@ __global__ void __launch_bounds__(LN_THREADS<PER>, 512 / LN_THREADS<PER>) ln_bac
   constexpr bool WARP = PER <= 32, ALONE = PER != 0;   // ALONE: a warp's threads are all of one row
   constexpr int LN_RING = LN_RING_ROWS<NV>;
   constexpr int TEAMS = PER == 32 ? LN_WARP_THREADS / 32 : 1, ROW = PER * NV;      // rings of a block, units of a row in one
-  __shared__ float red[2][32][2];
+  __shared__ __align__(16) float red[2][32][2];
   __shared__ unsigned long long full[RING ? TEAMS * LN_RING : 1];
   __shared__ int gave_up;
   typedef LnPairs<E, NV> Q;
@@ -113,11 +113,15 @@ __global__ void __launch_bounds__(LN_THREADS<PER>, 512 / LN_THREADS<PER>) ln_bac
     }
     fetch(r + at.step);
     float s[2] = {twa_pair_sum(s0), twa_pair_sum(s1)};
-    if (WARP) {
+    if constexpr (PER == 32) {
+      const float mine = ln_two_sums(s[0], s[1]), other = __shfl_xor_sync(0xffffffffu, mine, 16);
+      s[0] = threadIdx.x & 16 ? other : mine;
+      s[1] = threadIdx.x & 16 ? mine : other;
+    } else if constexpr (WARP) {
       s[0] = ln_sum_lanes<PER>(s[0], a.log_lanes);
       s[1] = ln_sum_lanes<PER>(s[1], a.log_lanes);
     } else {
-      block_sum<2>(s, red, turn);                      // and with its barrier the row has been read
+      ln_block_sums<PER / 32>(s, red, turn);           // and with its barrier the row has been read
     }
     if (WARP) __syncwarp();
     if (issuer) issue(it + LN_RING);
@@ -175,6 +179,14 @@ __global__ void __launch_bounds__(LN_THREADS<PER>, 512 / LN_THREADS<PER>) ln_bac
     }
     __syncthreads();
     for (int c = threadIdx.x; c < 2 * a.cols; c += blockDim.x) out[c] = ln_planes[c];
+  } else if constexpr (FULL) {
+#pragma unroll
+    for (int k = 0; k < NV; ++k)
+#pragma unroll
+      for (int e = 0; e < E; e += 4) {
+        twa_pack<float, 4>::store(out + at.column(k, e), fw + k * E + e);
+        twa_pack<float, 4>::store(out + a.cols + at.column(k, e), fb + k * E + e);
+      }
   } else {
 #pragma unroll
     for (int k = 0; k < NV; ++k)
@@ -192,7 +204,7 @@ __global__ void __launch_bounds__(LN_THREADS<PER>, 512 / LN_THREADS<PER>) ln_bac
 template <typename T, int E>
 __global__ void __launch_bounds__(LN_WIDE_THREADS) ln_backward_wide_kernel(LnArgs a) {
   twa_begin(a.x, a.dy, a.w, a.mean, a.rstd);
-  __shared__ float red[2][32][2];
+  __shared__ __align__(16) float red[2][32][2];
   int turn = 0;
   constexpr int NV = LN_WIDE_HELD / E;
   const int units = (a.cols + E - 1) / E, t = threadIdx.x;
@@ -239,7 +251,7 @@ __global__ void __launch_bounds__(LN_WIDE_THREADS) ln_backward_wide_kernel(LnArg
         s[1] += v * h[e];
       }
     }
-    block_sum<2>(s, red, turn);
+    ln_block_sums<0>(s, red, turn);
     const float c1 = s[0] * inv, c2 = s[1] * inv;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
@@ -266,7 +278,7 @@ __global__ void __launch_bounds__(LN_WIDE_THREADS) ln_backward_wide_kernel(LnArg
 template <typename T>
 __global__ void ln_backward_loop_kernel(LnArgs a) {
   twa_begin(a.x, a.dy, a.w, a.b, a.mean, a.rstd);
-  __shared__ float red[2][32][2];
+  __shared__ __align__(16) float red[2][32][2];
   int turn = 0;
   const T* x = static_cast<const T*>(a.x);
   const T* dy = static_cast<const T*>(a.dy);
@@ -280,7 +292,7 @@ __global__ void ln_backward_loop_kernel(LnArgs a) {
       s[0] += v;
       s[1] += v * ((twa_to_float(xr[c]) - mean) * rstd);
     }
-    block_sum<2>(s, red, turn);
+    ln_block_sums<0>(s, red, turn);
     const float c1 = s[0] / static_cast<float>(a.cols), c2 = s[1] / static_cast<float>(a.cols);
     for (int c = threadIdx.x; c < a.cols; c += blockDim.x) {
       const float v = twa_to_float(dr[c]) * (a.w ? twa_load_any(a.w, a.w_dtype, c) : 1.0f);
