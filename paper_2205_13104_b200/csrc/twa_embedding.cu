@@ -28,10 +28,12 @@ constexpr int SMALL_THREADS = 512, SMALL_WARPS = SMALL_THREADS / 32, SMALL_TILE 
 constexpr int SMALL_BLOCKS = 8, SMALL_TOKENS = SMALL_BLOCKS * SMALL_TILE;      // of a cluster
 constexpr int SMALL_BITS = 8, SMALL_BINS = 1 << SMALL_BITS;
 constexpr int SMALL_VOCAB = 1 << 20;                       // ids whose bitmap a block clears
-constexpr int FILL_BYTES = 1 << 15;                        // zeros of a block
-// Zeros written beside a sorting kernel: what its few us have room for, and those of the cluster's sort (16384 x 2048 into 50272
-// rows: 107.5 us with 32 MB beside that, 103.7 with 64, 99.6 with 96).
-constexpr long long FILL_BESIDE_SORT = 32LL << 20, FILL_BESIDE_CLUSTER = 96LL << 20;
+// Zeros of a block: with 16384 x 2048 into 50272 rows and 96 MB beside the sort 88.6 us with 8 KB, 85.2 with 16, 88.1 with 32.
+constexpr int FILL_BYTES = 1 << 14;
+constexpr int FILL_TEAM = 7;                               // log2 of the threads a row, those of the smallest block that writes zeros
+// Zeros written beside a sorting kernel: what its few us have room for, and those of the cluster's sort (the same case 85.2 us with
+// 96 MB, 83.8 with 128, 81.6 with 160; 16384 x 777 into 128000 rows 92.1, 93.1 and 94.8).
+constexpr long long FILL_BESIDE_SORT = 32LL << 20, FILL_BESIDE_CLUSTER = 160LL << 20;
 
 // E elements of any pairing of the two types; E = 8 wants both addresses on 16 bytes, E = 1 nothing.
 template <typename T, int E>
@@ -152,28 +154,27 @@ struct EmbFill {
   const uint32_t* used;         // null: all rows
   int row0, row1, each;         // rows row0 .. row1 - 1
   int size;                     // of an element
+  int log_team;                 // log2 of the threads that write a row together, at most FILL_TEAM
 };
-// Zeros into the unused ones of the block's rows (or all): 16 bytes a store between the ragged ends.
+// Zeros into the unused ones of the block's rows (or all): 16 bytes a store between the ragged ends.  A team takes a row at a time,
+// so that a store costs no division and no look at the bitmap.
 __device__ __forceinline__ void emb_fill(const EmbFill& f, int block) {
   const int r0 = f.row0 + block * f.each, rows = min(f.each, f.row1 - r0);      // none for a cluster's spare blocks
-  const int slots = static_cast<int>(f.bytes / 16) + 1;           // 0: the ends
-  for (int i = threadIdx.x; i < rows * slots; i += blockDim.x) {
-    const int r = i / slots, slot = i - r * slots, v = r0 + r;
+  const int step = 1 << f.log_team, team = threadIdx.x >> f.log_team, t = threadIdx.x & (step - 1);
+  for (int v = r0 + team; v < r0 + rows; v += blockDim.x >> f.log_team) {
     if (f.used && (__ldg(f.used + (v >> 5)) >> (v & 31) & 1)) continue;
     char* row = f.table + v * f.stride;
     const int head = static_cast<int>(min(f.bytes, static_cast<long long>(-reinterpret_cast<uintptr_t>(row) & 15)));
     const int whole = static_cast<int>((f.bytes - head) / 16);
-    if (slot) {
-      if (slot <= whole) *reinterpret_cast<uint4*>(row + head + (slot - 1) * 16LL) = make_uint4(0, 0, 0, 0);
-    } else {
-      for (int b = 0; b < head; b += f.size) {
-        if (f.size == 2) *reinterpret_cast<unsigned short*>(row + b) = 0;
-        else *reinterpret_cast<unsigned*>(row + b) = 0;
-      }
-      for (long long b = head + whole * 16LL; b < f.bytes; b += f.size) {
-        if (f.size == 2) *reinterpret_cast<unsigned short*>(row + b) = 0;
-        else *reinterpret_cast<unsigned*>(row + b) = 0;
-      }
+    uint4* to = reinterpret_cast<uint4*>(row + head) + t;
+#pragma unroll 4
+    for (int u = t; u < whole; u += step, to += step) *to = make_uint4(0, 0, 0, 0);
+    if (t) continue;
+    for (int b = 0; b < f.bytes; b += f.size) {
+      if (b == head) b += whole * 16;
+      if (b >= f.bytes) break;
+      if (f.size == 2) *reinterpret_cast<unsigned short*>(row + b) = 0;
+      else *reinterpret_cast<unsigned*>(row + b) = 0;
     }
   }
 }
@@ -618,7 +619,8 @@ int twa_embedding_backward(twa_ctx* ctx, const void* dout, int64_t ldd, twa_dtyp
   int total_bits = 1;
   while (total_bits < 32 && (static_cast<long long>(vocab) >> total_bits)) ++total_bits;      // keys 0 .. vocab
   EmbFill fill = {static_cast<char*>(dtable), static_cast<long long>(ldg * gs), static_cast<long long>(dim * gs), s.used, 0,
-                  accumulate ? 0 : vocab, 1, static_cast<int>(gs)};
+                  accumulate ? 0 : vocab, 1, static_cast<int>(gs), 0};
+  while (fill.log_team < FILL_TEAM && 16LL << fill.log_team < fill.bytes) ++fill.log_team;
   if (fill.bytes < FILL_BYTES) fill.each = static_cast<int>(FILL_BYTES / fill.bytes);
   int at = 0;
   if (n <= SMALL_TOKENS && vocab <= SMALL_VOCAB) {
