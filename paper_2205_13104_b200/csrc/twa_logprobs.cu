@@ -397,13 +397,18 @@ __global__ void __launch_bounds__(LP_BLOCK, LP_BLOCKS_PER_SM<TOP>) logprobs_kern
       if (TOP)
 #pragma unroll
         for (int i = 0; i < LP_WARPS; ++i) key[i] = sh.key[turn][i * 32 + lane];
-      __syncwarp();
-      if (lane == 0) twa_mbar_arrive(twa_smem_u32(&sh.row_empty[turn]));
+      // the summing warps may write the next row but one to where this one's stat, key and slot have been read
+      auto release = [&] {
+        __syncwarp();
+        if (lane == 0) twa_mbar_arrive(twa_smem_u32(&sh.row_empty[turn]));
+      };
+      if (!TOP) release();
       if (fabsf(st.m) >= LP_FAR && st.m != -INFINITY) st = lp_sum_far<T, ENT>(x.base + x.skew, from, to, st.m);
 
       u64 found = 0;                 // sorted
       if (TOP) {
         if (st.m == -INFINITY) {     // nothing above -inf: the first indices
+          release();
           if (lane < to - from) found = lp_key(-INFINITY, from + lane);
         } else {
           // a group: the eight threads of one lane number
@@ -449,7 +454,7 @@ __global__ void __launch_bounds__(LP_BLOCK, LP_BLOCKS_PER_SM<TOP>) logprobs_kern
               }
             }
           }
-          __syncwarp();
+          release();
           // their units that hold a value as large as the bound's
           constexpr int AHEAD = 4;
           const int log_each = 2 + log_slot, tasks = pairs <= LP_BUFFER ? pairs << log_each : 0;

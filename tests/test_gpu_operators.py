@@ -550,6 +550,24 @@ def test_norm_of_nothing_and_of_what_is_no_number(ctx):
     ok(ctx)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("vocab", [75, 505, 2840, 9001])
+@pytest.mark.parametrize("top", [1, 20])
+def test_best_tokens_of_many_short_rows(ctx, dtype, vocab, top):
+    # several rows for each of the warps that finish them, while the next rows are being added up
+    rows = 4001
+    z = (2.5 * torch.randn(rows, vocab, generator=gen(vocab + top), device=DEV)).to(dtype)
+    want = torch.sort(z.float(), dim=1, descending=True, stable=True).indices[:, :top]
+    t = torch.zeros(rows, dtype=torch.int64, device=DEV)
+    for again in range(3):
+        lp, lse = torch.empty(rows, device=DEV), torch.empty(rows, device=DEV)
+        ids = torch.empty(rows, top, dtype=torch.int32, device=DEV)
+        tlp = torch.empty(rows, top, device=DEV)
+        twa.twa_token_logprobs(ctx, z, t, lp, lse, top_ids=ids, top_logp=tlp)
+        assert torch.equal(ids.long(), want)
+    ok(ctx)
+
+
 # ------------------------------------------------------------------------------------------- streams, graphs, refusals
 def test_operators_replay_from_a_graph_on_a_stream_of_their_own(ctx):
     g = gen(21)
