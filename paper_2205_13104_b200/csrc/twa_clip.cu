@@ -9,6 +9,9 @@
 //
 // The tensors' addresses travel as kernel arguments (CLIP_TENSORS of them a launch), so a call uploads nothing.  They are
 // cut into chunks of at most CLIP_CHUNK elements; a block takes a run of chunks of equal length in either kernel.
+// 86.6 M float32 in 152 tensors: 195 us, 1.04 GB at 5.3 TB/s (59 us the norm); 1.32 G bfloat16 in 388: 1270 us, 7.9 GB at 6.2 TB/s.
+// With chunks dealt out to the blocks in turn 700 small tensors take 72 us instead of 38; streaming stores change nothing.
+//
 // Squares are added in float32 over a few elements and in float64 beyond, in a fixed order.
 #include <math.h>
 
@@ -20,7 +23,7 @@ constexpr int CLIP_TENSORS = 512;       // tensors of one launch
 constexpr int CLIP_FEW = 32;            // a smaller table, which costs less to hand over
 constexpr int CLIP_CHUNK = 8192;        // elements
 constexpr int CLIP_THREADS = 256;
-constexpr int CLIP_SM_BLOCKS = 5;       // blocks an SM
+constexpr int CLIP_SM_BLOCKS = 5;       // blocks an SM (86.6 M float32: 196 us, 4 blocks 201)
 constexpr int CLIP_MAX_BLOCKS = 148 * 8;
 constexpr int CLIP_HEAD = 256;          // bytes of the workspace before the partial sums: the factor
 
