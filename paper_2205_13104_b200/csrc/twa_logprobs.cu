@@ -35,8 +35,8 @@ constexpr int LP_FINISHERS = 2;
 constexpr int LP_BLOCK = LP_THREADS + 32 * (1 + LP_FINISHERS);
 constexpr int LP_PER_THREAD = 4;                            // 16-byte units of a thread in a chunk
 constexpr int LP_CHUNK = LP_THREADS * LP_PER_THREAD;        // units
-// Without the search three blocks fit an SM's registers, with it two (8192 x 50272 bfloat16 with entropy: without tokens 146 us
-// and 154 with two; with 5 tokens 162 us, with three 165 to 199).
+// Without the search three blocks fit an SM's registers, with it two (8192 x 50272 bfloat16 with entropy: without tokens 140 us
+// and 148 with two; with 5 tokens 162 us, with three 165 to 199).
 template <bool TOP>
 constexpr int LP_BLOCKS_PER_SM = TOP ? 2 : 3;
 template <bool TOP>
