@@ -568,6 +568,31 @@ def test_best_tokens_of_many_short_rows(ctx, dtype, vocab, top):
     ok(ctx)
 
 
+def test_logprobs_report_a_wait_that_ran_out(ctx):
+    """Rows of equal logits keep the warps that finish rows busy for milliseconds, and the summing warps wait for them: with a
+    limit of one millisecond that wait runs out, which has to be reported; with the usual one nothing is wrong."""
+    vocab, top = 1 << 21, 4
+    rows = 5 * 2 * torch.cuda.get_device_properties(0).multi_processor_count       # five for each resident block
+    z = torch.zeros(rows, vocab, dtype=BF16, device=DEV)
+    t = torch.zeros(rows, dtype=torch.int64, device=DEV)
+    logp, lse = torch.empty(rows, device=DEV), torch.empty(rows, device=DEV)
+    ids, tlp = torch.empty(rows, top, dtype=torch.int32, device=DEV), torch.empty(rows, top, device=DEV)
+    twa.twa_set_tuning(ctx, twa.TWA_TUNE_WAIT_LIMIT_MS, 1)
+    try:
+        twa.twa_token_logprobs(ctx, z, t, logp, lse, top_ids=ids, top_logp=tlp)
+        assert twa.twa_get_status(ctx)[0] == twa.TWA_ERR_TIMEOUT
+    finally:
+        twa.twa_set_tuning(ctx, twa.TWA_TUNE_WAIT_LIMIT_MS, 0)
+        twa.twa_clear_status(ctx)
+    twa.twa_token_logprobs(ctx, z, t, logp, lse, top_ids=ids, top_logp=tlp)
+    assert bool((ids == torch.arange(top, device=DEV)).all())
+    want = torch.full((rows,), math.log(vocab), dtype=torch.float64, device=DEV)
+    tol, _ = logprob_tolerances(z[:1], vocab)
+    close(lse, want, tol + 2 * U * want)
+    assert torch.equal(logp, -lse) and torch.equal(tlp, -lse[:, None].expand(rows, top))
+    ok(ctx)
+
+
 # ------------------------------------------------------------------------------------------- streams, graphs, refusals
 def test_operators_replay_from_a_graph_on_a_stream_of_their_own(ctx):
     g = gen(21)
