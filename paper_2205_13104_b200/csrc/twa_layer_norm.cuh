@@ -131,7 +131,7 @@ struct LnPlace {
     return FULL || (E == 1 ? in(k) : unit(k) * E >= skew && (unit(k) + 1) * E <= skew + cols);
   }
   // The unit of the row that begins at `row`.  Of a unit that the row has in part, elements outside are what is beside the row in
-  // memory (`inner`: there are rows before and after it), or 0.
+  // memory (`inner`: there are rows before and after it, E - 1 elements apart at least, see ln_classes), or 0.
   template <typename T>
   __device__ __forceinline__ void load(twa_pack<T, E>& p, const T* row, int k, bool inner) const {
     if (E == 1 || inner || whole(k)) {
@@ -236,12 +236,16 @@ struct LnPlan {
 template <int E, bool BACK, int PER>
 constexpr int LN_HELD = BACK ? 16 : (PER == 32 && E == 8 ? 64 : 32);
 
-// Ways in which the rows of all matrices lie on 16-byte boundaries, if they do alike.
+// Ways in which the rows of all matrices lie on 16-byte boundaries, if they do alike; else 0, and the rows are read element by
+// element.  So are rows that begin less than a unit of 16 bytes apart but for one element: a row's first and last unit reach up to
+// that far beside it, which then is more than a neighbouring row (3 x 2 bfloat16: row 1's unit is 8 of the matrix's 6 elements).
 int ln_classes(const void* p, long long ld, const void* q, long long ldq, const void* s, long long lds, long long rows, int cols,
                size_t size) {
   const uintptr_t a = reinterpret_cast<uintptr_t>(p) & 15;
   const long long d = (ld * static_cast<long long>(size)) & 15;
   if ((reinterpret_cast<uintptr_t>(q) & 15) != a || (reinterpret_cast<uintptr_t>(s) & 15) != a) return 0;
+  const long long unit = 16 / static_cast<long long>(size);
+  if (rows > 1 && (ld < unit - 1 || ldq < unit - 1 || lds < unit - 1)) return 0;
   if (rows > 1 && (((ldq * static_cast<long long>(size)) & 15) != d || ((lds * static_cast<long long>(size)) & 15) != d)) return 0;
   if (a == 0 && (d == 0 || rows <= 1) && cols * size % 16 == 0) return 1;
   return static_cast<int>(16 / size);

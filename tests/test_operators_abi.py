@@ -1,6 +1,7 @@
 """What of the model's operators runs without a GPU: workspace sizes, refusals before anything is enqueued."""
 
 import ctypes
+import subprocess
 
 from paper_2205_13104_b200 import twa
 
@@ -41,3 +42,41 @@ def test_calls_without_a_context_are_refused():
     assert lib.twa_grad_norm(None, ctypes.byref(t), d, d, 1 << 20) == bad
     assert lib.twa_clip_gather(None, ctypes.byref(t), 1.0, 1e-6, d, 0, d, d, 1 << 20) == bad
     assert lib.twa_clip_grads(None, ctypes.byref(t), 1.0, 1e-6, d, d, 1 << 20) == bad
+
+
+READS = """
+#include <stdio.h>
+#include "twa_layer_norm.cuh"
+// Units of E elements as LnPlace lays them out over a row; a unit that the row has in part is read whole where there are rows before
+// and after it.  Prints every read beside the matrix.
+int main() {
+  for (int size : {2, 4})
+    for (int rows = 1; rows <= 5; ++rows)
+      for (int cols = 1; cols <= 19; ++cols)
+        for (int ld = cols; ld <= cols + 9; ++ld)
+          for (int other = ld; other <= ld + 8; other += 8)
+            for (int start = 0; start < 8; ++start) {
+              const int E = 16 / size;
+              const char* at = reinterpret_cast<const char*>(4096) + start * size;
+              if (!ln_classes(at, ld, at, other, at, other, rows, cols, size)) continue;
+              for (int stride : {ld, other})
+                for (int r = 1; r + 1 < rows; ++r) {
+                  const int first = r * stride, skew = (start + first) % E, end = (rows - 1) * stride + cols;
+                  for (int k = 0; k * E < skew + cols; ++k) {
+                    const int from = first - skew + k * E;
+                    if (from < 0 || from + E > end)
+                      printf("%d bytes, %d x %d, stride %d, start %d: row %d reads %d .. %d of %d\\n", size, rows, cols, stride, start, r,
+                             from, from + E - 1, end);
+                  }
+                }
+            }
+}
+"""
+
+
+def test_layer_norm_reads_nothing_beside_the_matrix(tmp_path):
+    """The rule by which rows are read in units of 16 bytes, compiled for the host."""
+    source, program = tmp_path / "reads.cu", tmp_path / "reads"
+    source.write_text(READS)
+    subprocess.run([twa._nvcc(), *twa.NVCC_FLAGS, "-I", twa.CSRC, "-o", str(program), str(source)], check=True)
+    assert subprocess.run([str(program)], check=True, capture_output=True, text=True).stdout == ""
