@@ -78,8 +78,17 @@ __global__ void __launch_bounds__(LN_THREADS<PER>, 512 / LN_THREADS<PER>) ln_bac
     const float rs = rstd;
     if constexpr (RING) {
       const int q = it % LN_RING;
-      // after a wait that ran out the results are not defined, and every later wait ends at once
-      landed &= twa_wait(&full[team * LN_RING + q], it / LN_RING & 1, &gave_up, a.wait_limit_ns);
+      if (!twa_wait(&full[team * LN_RING + q], it / LN_RING & 1, &gave_up, a.wait_limit_ns)) {
+        // The results are not defined, and every later wait ends at once.  Nothing is copied any more: the last copy into the
+        // place of a row may not have landed; and none may still be on its way into this block's shared memory when it ends.
+        if (issuer && landed)
+          for (int i = it; i < it + LN_RING && at.first + i * at.step < a.rows; ++i) {
+            const unsigned long long begun = twa_globaltimer();
+            while (!twa_mbar_try_wait(twa_smem_u32(&full[team * LN_RING + i % LN_RING]), i / LN_RING & 1))
+              if (twa_globaltimer() - begun > a.wait_limit_ns) break;
+          }
+        landed = false;
+      }
 #pragma unroll
       for (int k = 0; k < NV; ++k)
         if (at.in(k)) {
@@ -124,7 +133,7 @@ __global__ void __launch_bounds__(LN_THREADS<PER>, 512 / LN_THREADS<PER>) ln_bac
       ln_block_sums<PER / 32>(s, red, turn);           // and with its barrier the row has been read
     }
     if (WARP) __syncwarp();
-    if (issuer) issue(it + LN_RING);
+    if (issuer && landed) issue(it + LN_RING);
     if (ALONE || r < a.rows) {
       // rstd (v - c1 - h c2)
       const twa_f2 c1 = twa_pair(-s[0] * inv), c2 = twa_pair(-s[1] * inv), r2 = twa_pair(rs);
@@ -136,16 +145,7 @@ __global__ void __launch_bounds__(LN_THREADS<PER>, 512 / LN_THREADS<PER>) ln_bac
         if (at.in(k)) at.store(dx + r * a.ldy, k, f + k * E);
     }
   }
-  if (RING && !landed) {
-    twa_set_status(a.status, TWA_ERR_TIMEOUT, -1);
-    // no copy may still be on its way into this block's shared memory when it ends
-    if (issuer)
-      for (int i = max(0, it - LN_RING); i < it; ++i) {
-        const unsigned long long begun = twa_globaltimer();
-        while (!twa_mbar_try_wait(twa_smem_u32(&full[team * LN_RING + i % LN_RING]), i / LN_RING & 1))
-          if (twa_globaltimer() - begun > a.wait_limit_ns) break;
-      }
-  }
+  if (RING && !landed) twa_set_status(a.status, TWA_ERR_TIMEOUT, -1);
   if (!a.part) return;
   float* out = a.part + static_cast<long long>(blockIdx.x) * 2 * a.cols;
   if constexpr (WARP) {
