@@ -578,7 +578,7 @@ typedef struct {
 } twa_tensors;
 /* norm = square root of the sum of all squares.  norm: one float on the device.
  *  ws  twa_grad_norm_workspace_bytes(count).
- * The squares are float32 and are added in float64 beyond 16 bytes of elements: elements above 1.8e19 give an infinite norm.
+ * Squares that leave float32 at either end are taken in float64: the norm is right as long as it is a float32 itself.
  * Device-side error: TWA_ERR_NONFINITE where the norm is not finite. */
 int twa_grad_norm(twa_ctx* ctx, const twa_tensors* tensors, float* norm, void* ws, size_t ws_bytes);
 /* The norm, and g = min(1, max_norm / (norm + eps)) times the tensors one after another, the flat gradient

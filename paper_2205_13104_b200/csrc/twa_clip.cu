@@ -12,7 +12,9 @@
 // 86.6 M float32 in 152 tensors: 195 us, 1.04 GB at 5.3 TB/s (59 us the norm); 1.32 G bfloat16 in 388: 1270 us, 7.9 GB at 6.2 TB/s.
 // With chunks dealt out to the blocks in turn 700 small tensors take 72 us instead of 38; streaming stores change nothing.
 //
-// Squares are added in float32 over a few elements and in float64 beyond, in a fixed order.
+// Squares are added in float32 over the elements of one load and in float64 beyond, in a fixed order.  Where that left float32, or a
+// load's squares are so small that they have lost digits, the thread takes its part of the chunk once more in float64 (a
+// branch at each load instead: 86.6 M float32 199 -> 224 us, 1.32 G bfloat16 1293 -> 2030).
 #include <math.h>
 
 #include "twa_ops.cuh"
@@ -48,19 +50,60 @@ __device__ __forceinline__ int clip_find(const ClipTable<N>& t, int q) {
   return lo;
 }
 
+// Below this a load's squares may have lost digits: each errs by 2^-150 at most, which is 2^-27 of such a sum of eight.
+constexpr float CLIP_SMALL = 0x1p-120f;
+
+// Bits that are set in any element, signs aside.
+__device__ __forceinline__ uint32_t clip_bits(const twa_pack<float, 4>& q) {
+  return (__float_as_uint(q.r.x) | __float_as_uint(q.r.y) | __float_as_uint(q.r.z) | __float_as_uint(q.r.w)) & 0x7fffffffu;
+}
+__device__ __forceinline__ uint32_t clip_bits(const twa_pack<bf16, 8>& q) { return (q.r.x | q.r.y | q.r.z | q.r.w) & 0x7fff7fffu; }
+
+// A chunk as elements before the first 16-byte boundary (`head` of them), units of 16 bytes, and the rest from `tail` on.
+template <typename T>
+struct ClipParts {
+  static constexpr int E = twa_vec<T>;
+  int head, units, tail;
+  __device__ __forceinline__ ClipParts(const T* p, int n) {
+    const int skew = static_cast<int>((reinterpret_cast<uintptr_t>(p) & 15) / sizeof(T));
+    head = min(n, skew ? E - skew : 0);
+    units = (n - head) / E;
+    tail = head + units * E;
+  }
+};
+
+// What clip_square_sum gives, every square in float64.
+template <typename T>
+__device__ __noinline__ double clip_square_sum_wide(const T* p, int n) {
+  const ClipParts<T> parts(p, n);
+  const int t = threadIdx.x;
+  double sum = 0.0;
+  auto square = [&](int i) {
+    const double v = twa_to_float(p[i]);
+    sum += v * v;
+  };
+  if (t < parts.head) square(t);
+  if (parts.tail + t < n) square(parts.tail + t);
+  for (int u = t; u < parts.units; u += CLIP_THREADS)
+    for (int e = 0; e < parts.E; ++e) square(parts.head + u * parts.E + e);
+  return sum;
+}
+
+// The squares of a thread's elements of a chunk.
 template <typename T>
 __device__ __forceinline__ double clip_square_sum(const T* p, int n) {
   constexpr int E = twa_vec<T>;
   double sum = 0.0;
-  const int skew = static_cast<int>((reinterpret_cast<uintptr_t>(p) & 15) / sizeof(T));
-  const int head = min(n, skew ? E - skew : 0), units = (n - head) / E, tail = head + units * E;
+  uint32_t small = 0;                   // bits of elements whose squares have lost digits
+  const ClipParts<T> parts(p, n);
+  const int head = parts.head, units = parts.units, tail = parts.tail;
   if (static_cast<int>(threadIdx.x) < head) {
-    const float v = twa_to_float(p[threadIdx.x]);
-    sum += static_cast<double>(v * v);
+    const double v = twa_to_float(p[threadIdx.x]);
+    sum += v * v;
   }
   if (tail + static_cast<int>(threadIdx.x) < n) {
-    const float v = twa_to_float(p[tail + threadIdx.x]);
-    sum += static_cast<double>(v * v);
+    const double v = twa_to_float(p[tail + threadIdx.x]);
+    sum += v * v;
   }
   constexpr int AHEAD = 4;
   const T* from = p + head + threadIdx.x * E;
@@ -71,6 +114,7 @@ __device__ __forceinline__ double clip_square_sum(const T* p, int n) {
 #pragma unroll
     for (int e = 0; e < E; ++e) s += v[e] * v[e];
     sum += static_cast<double>(s);
+    if (s < CLIP_SMALL) small |= clip_bits(q);
   };
   for (; left > (AHEAD - 1) * CLIP_THREADS; left -= AHEAD * CLIP_THREADS) {
     twa_pack<T, E> q[AHEAD];
@@ -87,7 +131,7 @@ __device__ __forceinline__ double clip_square_sum(const T* p, int n) {
     squares(q);
     from += CLIP_THREADS * E;
   }
-  return sum;
+  return small || !isfinite(sum) ? clip_square_sum_wide(p, n) : sum;
 }
 
 __device__ __forceinline__ double clip_block_sum(double v, double* red) {
@@ -136,10 +180,11 @@ __global__ void __launch_bounds__(CLIP_THREADS, CLIP_SM_BLOCKS) clip_norm_kernel
   if (threadIdx.x == 0) {
     *ticket = 0;
     const double norm = sqrt(all);
-    *norm_out = static_cast<float>(norm);
+    const float rounded = static_cast<float>(norm);
+    *norm_out = rounded;
     const double f = static_cast<double>(max_norm) / (norm + static_cast<double>(eps));
     if (factor) *factor = static_cast<float>(f >= 1.0 ? 1.0 : f);      // a norm that is no number gives none
-    if (!isfinite(norm)) twa_set_status(status, TWA_ERR_NONFINITE, -1);
+    if (!isfinite(rounded)) twa_set_status(status, TWA_ERR_NONFINITE, -1);
   }
 }
 

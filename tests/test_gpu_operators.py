@@ -551,6 +551,28 @@ def test_norm_of_nothing_and_of_what_is_no_number(ctx):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("size,spread", [(7e18, 1.0), (1.5e19, 1.0), (1e36, 1.0), (1e-22, 1.0), (3e-30, 1.0), (1e-38, 1.0), (1e-16, 1e-4), (1e16, 1e4)])
+def test_norm_and_clipping_at_the_ends_of_float32(ctx, dtype, size, spread):
+    """Elements whose squares are no float32, alone and beside others that are `spread` times as large."""
+    g = gen(9)
+    values = size * (1.0 + torch.rand(5003, generator=g, device=DEV, dtype=torch.float64))
+    values[::3] = 0.0
+    values[1::16] *= spread
+    grads = [values[:4001].to(dtype), values[4001:].to(dtype)]
+    ts = twa.Tensors(grads)
+    ws, norm = torch.empty(twa.twa_grad_norm_workspace_bytes(ts), dtype=torch.uint8, device=DEV), torch.empty(1, device=DEV)
+    want = math.sqrt(sum(float((t.double() ** 2).sum()) for t in grads))
+    # sixteen roundings of a relative U, and half a unit in the last place of a result below 2^-126
+    twa.twa_grad_norm(ctx, ts, norm, ws)
+    assert abs(float(norm) - want) <= 16 * U * want + 2.0 ** -149
+    out = torch.empty(5003, dtype=dtype, device=DEV)
+    twa.twa_clip_gather(ctx, ts, 0.5 * want, out, norm, ws, eps=0.0)
+    ref = 0.5 * torch.cat([t.double() for t in grads])
+    close(out, ref, (20 * U + ROUND[dtype]) * ref.abs() + (2.0 ** -149 if dtype is F32 else 2.0 ** -133))
+    ok(ctx)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("vocab", [75, 505, 2840, 9001])
 @pytest.mark.parametrize("top", [1, 20])
 def test_best_tokens_of_many_short_rows(ctx, dtype, vocab, top):
