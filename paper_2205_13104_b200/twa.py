@@ -304,12 +304,17 @@ def twa_last_error(ctx):
     return load().twa_last_error(ctx).decode()
 
 
+class Context(ctypes.c_void_p):
+    """The handle that twa_create returns, with the number of its device (`device`)."""
+
+
 def twa_create(device=0, stream=None):
     """Context on `device` bound to `stream` (a torch.cuda.Stream; None = the current one)."""
     lib = load()
     if stream is None:
         stream = torch.cuda.current_stream(device)
-    handle = ctypes.c_void_p()
+    handle = Context()
+    handle.device = int(device)
     rc = lib.twa_create(ctypes.byref(handle), int(device), ctypes.c_void_p(stream.cuda_stream))
     _check(rc, "twa_create")
     return handle
@@ -765,19 +770,19 @@ def _floats(t, what):
     return code
 
 
-def _numbers(t, count, what):
+def _numbers(t, count, what, dev):
     code = _ITYPES.get(t.dtype)
     if code is None:
         raise TypeError(f"{what}: dtype {t.dtype} not supported (int32 or int64)")
-    if t.numel() != count or not t.is_contiguous() or not t.is_cuda:
-        raise ValueError(f"{what}: {count} contiguous token numbers on the device are needed, got shape {tuple(t.shape)} on {t.device}")
+    if t.numel() != count or not t.is_contiguous() or t.get_device() != dev:
+        raise ValueError(f"{what}: {count} contiguous token numbers on the context's device are needed, got shape {tuple(t.shape)} on {t.device}")
     return code
 
 
-def _rows(t, shape, what, dtype=None):
+def _rows(t, shape, what, dev, dtype=None):
     """Row stride of a matrix of that shape whose rows are contiguous."""
-    if t.shape != shape or dtype is not None and t.dtype is not dtype or not t.is_cuda:
-        raise ValueError(f"{what}: shape {tuple(shape)}{'' if dtype is None else f' of {dtype}'} on the device is needed, "
+    if t.shape != shape or dtype is not None and t.dtype is not dtype or t.get_device() != dev:
+        raise ValueError(f"{what}: shape {tuple(shape)}{'' if dtype is None else f' of {dtype}'} on the context's device is needed, "
                          f"got {tuple(t.shape)} of {t.dtype} on {t.device}")
     ld, one = t.stride()
     if one != 1 and shape[1] > 1:
@@ -785,22 +790,22 @@ def _rows(t, shape, what, dtype=None):
     return ld if ld >= shape[1] or shape[0] > 1 else shape[1]
 
 
-def _vector(t, count, dtype, what):
+def _vector(t, count, dtype, what, dev):
     """Address of a contiguous tensor of `count` elements (0 for None)."""
     if t is None:
         return None
-    if t.dtype is not dtype or t.numel() != count or not t.is_contiguous() or not t.is_cuda:
-        raise ValueError(f"{what}: {count} contiguous elements of {dtype} on the device are needed, got {tuple(t.shape)} of {t.dtype} "
-                         f"on {t.device}")
+    if t.dtype is not dtype or t.numel() != count or not t.is_contiguous() or t.get_device() != dev:
+        raise ValueError(f"{what}: {count} contiguous elements of {dtype} on the context's device are needed, got {tuple(t.shape)} of "
+                         f"{t.dtype} on {t.device}")
     return t.data_ptr()
 
 
-def _space(ws):
+def _space(ws, dev):
     """Address and size of a workspace."""
     if ws is None:
         return None, 0
-    if not ws.is_cuda or not ws.is_contiguous():
-        raise ValueError("ws: a contiguous tensor on the device is needed")
+    if ws.get_device() != dev or not ws.is_contiguous():
+        raise ValueError(f"ws: a contiguous tensor on the context's device is needed, got one on {ws.device}")
     return ws.data_ptr(), ws.nbytes
 
 
@@ -811,13 +816,14 @@ def twa_layer_norm_workspace_bytes(rows, cols):
 def twa_layer_norm(ctx, x, weight, bias, eps, y, mean=None, rstd=None):
     """x, y: (rows, cols); weight, bias: (cols,) of one type, or None; mean, rstd: (rows,) float32, or None."""
     dt, shape = _floats(x, "x"), x.shape
+    dev = ctx.device
     rows, cols = shape
     p = weight if weight is not None else bias
     pt, wt = (p.dtype, _floats(p, "weight")) if p is not None else (None, TWA_F32)
-    rc = load().twa_layer_norm(ctx, x.data_ptr(), _rows(x, shape, "x"), dt,
-                               _vector(weight, cols, pt, "weight"), _vector(bias, cols, pt, "bias"), wt, rows, cols, eps,
-                               y.data_ptr(), _rows(y, shape, "y", x.dtype), _vector(mean, rows, torch.float32, "mean"),
-                               _vector(rstd, rows, torch.float32, "rstd"))
+    rc = load().twa_layer_norm(ctx, x.data_ptr(), _rows(x, shape, "x", dev), dt,
+                               _vector(weight, cols, pt, "weight", dev), _vector(bias, cols, pt, "bias", dev), wt, rows, cols, eps,
+                               y.data_ptr(), _rows(y, shape, "y", dev, x.dtype), _vector(mean, rows, torch.float32, "mean", dev),
+                               _vector(rstd, rows, torch.float32, "rstd", dev))
     if rc:
         _check(rc, "twa_layer_norm", ctx)
     return y
@@ -826,15 +832,16 @@ def twa_layer_norm(ctx, x, weight, bias, eps, y, mean=None, rstd=None):
 def twa_layer_norm_backward(ctx, dy, x, weight, mean, rstd, dx, dw, db, ws, accumulate=False):
     """dw, db: (cols,) of one type, or None (then ws may be None too when both are)."""
     dt, shape = _floats(x, "x"), x.shape
+    dev = ctx.device
     rows, cols = shape
     p = dw if dw is not None else db
     pt, gt = (p.dtype, _floats(p, "dw")) if p is not None else (None, TWA_F32)
     rc = load().twa_layer_norm_backward(
-        ctx, dy.data_ptr(), _rows(dy, shape, "dy", x.dtype), x.data_ptr(), _rows(x, shape, "x"), dt,
-        _vector(weight, cols, weight.dtype if weight is not None else None, "weight"),
-        _floats(weight, "weight") if weight is not None else TWA_F32, _vector(mean, rows, torch.float32, "mean"),
-        _vector(rstd, rows, torch.float32, "rstd"), rows, cols, dx.data_ptr(), _rows(dx, shape, "dx", x.dtype),
-        _vector(dw, cols, pt, "dw"), _vector(db, cols, pt, "db"), gt, 1 if accumulate else 0, *_space(ws))
+        ctx, dy.data_ptr(), _rows(dy, shape, "dy", dev, x.dtype), x.data_ptr(), _rows(x, shape, "x", dev), dt,
+        _vector(weight, cols, weight.dtype if weight is not None else None, "weight", dev),
+        _floats(weight, "weight") if weight is not None else TWA_F32, _vector(mean, rows, torch.float32, "mean", dev),
+        _vector(rstd, rows, torch.float32, "rstd", dev), rows, cols, dx.data_ptr(), _rows(dx, shape, "dx", dev, x.dtype),
+        _vector(dw, cols, pt, "dw", dev), _vector(db, cols, pt, "db", dev), gt, 1 if accumulate else 0, *_space(ws, dev))
     if rc:
         _check(rc, "twa_layer_norm_backward", ctx)
     return dx
@@ -847,10 +854,11 @@ def twa_embedding_workspace_bytes(tokens, vocab, dim):
 def twa_embedding(ctx, table, ids, scale, out):
     """table: (vocab, dim); ids: (tokens,) int32 or int64; out: (tokens, dim)."""
     vocab, dim = table.shape
+    dev = ctx.device
     tokens = ids.shape[0]
-    rc = load().twa_embedding(ctx, table.data_ptr(), _rows(table, table.shape, "table"), _floats(table, "table"), vocab, dim,
-                              ids.data_ptr(), _numbers(ids, tokens, "ids"), tokens, scale, out.data_ptr(),
-                              _rows(out, (tokens, dim), "out"), _floats(out, "out"))
+    rc = load().twa_embedding(ctx, table.data_ptr(), _rows(table, table.shape, "table", dev), _floats(table, "table"), vocab, dim,
+                              ids.data_ptr(), _numbers(ids, tokens, "ids", dev), tokens, scale, out.data_ptr(),
+                              _rows(out, (tokens, dim), "out", dev), _floats(out, "out"))
     if rc:
         _check(rc, "twa_embedding", ctx)
     return out
@@ -859,11 +867,12 @@ def twa_embedding(ctx, table, ids, scale, out):
 def twa_embedding_backward(ctx, dout, ids, scale, dtable, ws, padding_id=-1, accumulate=False):
     """dout: (tokens, dim); dtable: (vocab, dim)."""
     vocab, dim = dtable.shape
+    dev = ctx.device
     tokens = ids.shape[0]
-    rc = load().twa_embedding_backward(ctx, dout.data_ptr(), _rows(dout, (tokens, dim), "dout"), _floats(dout, "dout"),
-                                       ids.data_ptr(), _numbers(ids, tokens, "ids"), tokens, vocab, dim, scale, padding_id,
-                                       dtable.data_ptr(), _rows(dtable, dtable.shape, "dtable"), _floats(dtable, "dtable"),
-                                       1 if accumulate else 0, *_space(ws))
+    rc = load().twa_embedding_backward(ctx, dout.data_ptr(), _rows(dout, (tokens, dim), "dout", dev), _floats(dout, "dout"),
+                                       ids.data_ptr(), _numbers(ids, tokens, "ids", dev), tokens, vocab, dim, scale, padding_id,
+                                       dtable.data_ptr(), _rows(dtable, dtable.shape, "dtable", dev), _floats(dtable, "dtable"),
+                                       1 if accumulate else 0, *_space(ws, dev))
     if rc:
         _check(rc, "twa_embedding_backward", ctx)
     return dtable
@@ -873,17 +882,20 @@ def twa_token_logprobs(ctx, logits, targets, logp, lse, entropy=None, top_ids=No
     """logits: (rows, vocab); targets: (rows,); logp, lse, entropy: (rows,) float32; top_ids: (rows, k) int32 and
     top_logp: (rows, k) float32, contiguous, or both None."""
     rows, vocab = logits.shape
+    dev = ctx.device
     top = 0
     if top_ids is not None or top_logp is not None:
-        if top_ids is None or top_logp is None or not top_ids.is_cuda or not top_logp.is_cuda or top_ids.dtype is not torch.int32 or top_logp.dtype is not torch.float32 or \
+        if top_ids is None or top_logp is None or top_ids.get_device() != dev or top_logp.get_device() != dev or \
+                top_ids.dtype is not torch.int32 or top_logp.dtype is not torch.float32 or \
                 top_ids.shape != top_logp.shape or top_ids.dim() != 2 or len(top_ids) != rows or \
                 not top_ids.is_contiguous() or not top_logp.is_contiguous():
-            raise ValueError(f"top_ids and top_logp: contiguous ({rows}, k) matrices of int32 and float32 are needed, both or neither")
+            raise ValueError(f"top_ids and top_logp: contiguous ({rows}, k) matrices of int32 and float32 on the context's device are "
+                             "needed, both or neither")
         top = top_ids.shape[1]
-    rc = load().twa_token_logprobs(ctx, logits.data_ptr(), _rows(logits, logits.shape, "logits"), _floats(logits, "logits"), rows,
-                                   vocab, targets.data_ptr(), _numbers(targets, rows, "targets"), ignore_id,
-                                   _vector(logp, rows, torch.float32, "logp"), _vector(lse, rows, torch.float32, "lse"),
-                                   _vector(entropy, rows, torch.float32, "entropy"), top, _ptr(top_ids), _ptr(top_logp))
+    rc = load().twa_token_logprobs(ctx, logits.data_ptr(), _rows(logits, logits.shape, "logits", dev), _floats(logits, "logits"), rows,
+                                   vocab, targets.data_ptr(), _numbers(targets, rows, "targets", dev), ignore_id,
+                                   _vector(logp, rows, torch.float32, "logp", dev), _vector(lse, rows, torch.float32, "lse", dev),
+                                   _vector(entropy, rows, torch.float32, "entropy", dev), top, _ptr(top_ids), _ptr(top_logp))
     if rc:
         _check(rc, "twa_token_logprobs", ctx)
     return logp
@@ -893,12 +905,13 @@ def twa_token_logprobs_backward(ctx, logits, targets, lse, d_logp, dlogits, entr
     """lse, entropy: from the forward call; d_logp, d_entropy: (rows,) float32; dlogits: (rows, vocab) of logits' type, or
     logits itself."""
     rows, vocab = shape = logits.shape
+    dev = ctx.device
     rc = load().twa_token_logprobs_backward(
-        ctx, logits.data_ptr(), _rows(logits, shape, "logits"), _floats(logits, "logits"), rows, vocab, targets.data_ptr(),
-        _numbers(targets, rows, "targets"), ignore_id, _vector(lse, rows, torch.float32, "lse"),
-        _vector(entropy, rows, torch.float32, "entropy"), _vector(d_logp, rows, torch.float32, "d_logp"),
-        _vector(d_entropy, rows, torch.float32, "d_entropy"), dlogits.data_ptr(),
-        _rows(dlogits, shape, "dlogits", logits.dtype))
+        ctx, logits.data_ptr(), _rows(logits, shape, "logits", dev), _floats(logits, "logits"), rows, vocab, targets.data_ptr(),
+        _numbers(targets, rows, "targets", dev), ignore_id, _vector(lse, rows, torch.float32, "lse", dev),
+        _vector(entropy, rows, torch.float32, "entropy", dev), _vector(d_logp, rows, torch.float32, "d_logp", dev),
+        _vector(d_entropy, rows, torch.float32, "d_entropy", dev), dlogits.data_ptr(),
+        _rows(dlogits, shape, "dlogits", dev, logits.dtype))
     if rc:
         _check(rc, "twa_token_logprobs_backward", ctx)
     return dlogits
@@ -913,6 +926,10 @@ class Tensors:
         for t in self.tensors:
             if not t.is_contiguous() or not t.is_cuda:
                 raise ValueError("gradients have to be contiguous and on the device")
+        devices = {t.get_device() for t in self.tensors}
+        if len(devices) > 1:
+            raise ValueError(f"gradients have to be on one device, got {sorted(devices)}")
+        self.device = devices.pop() if devices else None
         n = len(self.tensors)
         self._data = (ctypes.c_void_p * n)(*[t.data_ptr() for t in self.tensors])
         self._sizes = (ctypes.c_int64 * n)(*[t.numel() for t in self.tensors])
@@ -927,9 +944,17 @@ def twa_grad_norm_workspace_bytes(tensors):
     return int(load().twa_grad_norm_workspace_bytes(int(count)))
 
 
+def _gradients(tensors, dev):
+    """The descriptor of a Tensors."""
+    if tensors.device != dev and tensors.device is not None:
+        raise ValueError(f"gradients on the context's device {dev} are needed, got them on {tensors.device}")
+    return ctypes.byref(tensors.desc)
+
+
 def twa_grad_norm(ctx, tensors, norm, ws):
     """tensors: a Tensors; norm: (1,) float32."""
-    rc = load().twa_grad_norm(ctx, ctypes.byref(tensors.desc), _vector(norm, 1, torch.float32, "norm"), *_space(ws))
+    dev = ctx.device
+    rc = load().twa_grad_norm(ctx, _gradients(tensors, dev), _vector(norm, 1, torch.float32, "norm", dev), *_space(ws, dev))
     if rc:
         _check(rc, "twa_grad_norm", ctx)
     return norm
@@ -937,18 +962,21 @@ def twa_grad_norm(ctx, tensors, norm, ws):
 
 def twa_clip_gather(ctx, tensors, max_norm, g, norm, ws, eps=1e-6):
     """g: contiguous, of at least as many elements as the tensors together (a padded flat gradient keeps its tail)."""
-    if g.dim() != 1 or g.numel() < tensors.total or not g.is_contiguous() or not g.is_cuda:
-        raise ValueError(f"g: a contiguous vector of at least {tensors.total} elements on the device is needed, got {tuple(g.shape)} on {g.device}")
-    rc = load().twa_clip_gather(ctx, ctypes.byref(tensors.desc), max_norm, eps, g.data_ptr(), _floats(g, "g"),
-                                _vector(norm, 1, torch.float32, "norm"), *_space(ws))
+    dev = ctx.device
+    if g.dim() != 1 or g.numel() < tensors.total or not g.is_contiguous() or g.get_device() != dev:
+        raise ValueError(f"g: a contiguous vector of at least {tensors.total} elements on the context's device is needed, got "
+                         f"{tuple(g.shape)} on {g.device}")
+    rc = load().twa_clip_gather(ctx, _gradients(tensors, dev), max_norm, eps, g.data_ptr(), _floats(g, "g"),
+                                _vector(norm, 1, torch.float32, "norm", dev), *_space(ws, dev))
     if rc:
         _check(rc, "twa_clip_gather", ctx)
     return g
 
 
 def twa_clip_grads(ctx, tensors, max_norm, norm, ws, eps=1e-6):
-    rc = load().twa_clip_grads(ctx, ctypes.byref(tensors.desc), max_norm, eps, _vector(norm, 1, torch.float32, "norm"),
-                               *_space(ws))
+    dev = ctx.device
+    rc = load().twa_clip_grads(ctx, _gradients(tensors, dev), max_norm, eps, _vector(norm, 1, torch.float32, "norm", dev),
+                               *_space(ws, dev))
     if rc:
         _check(rc, "twa_clip_grads", ctx)
     return norm

@@ -3,6 +3,9 @@
 import ctypes
 import subprocess
 
+import pytest
+import torch
+
 from paper_2205_13104_b200 import twa
 
 
@@ -80,3 +83,51 @@ def test_layer_norm_reads_nothing_beside_the_matrix(tmp_path):
     source.write_text(READS)
     subprocess.run([twa._nvcc(), *twa.NVCC_FLAGS, "-I", twa.CSRC, "-o", str(program), str(source)], check=True)
     assert subprocess.run([str(program)], check=True, capture_output=True, text=True).stdout == ""
+
+
+def on_device(number):
+    """A tensor type whose tensors say that they are on that device."""
+    class Elsewhere(torch.Tensor):
+        is_cuda = True
+
+        def get_device(self):
+            return number
+
+    return lambda *shape, dtype=torch.float32: torch.zeros(shape, dtype=dtype).as_subclass(Elsewhere)
+
+
+def test_tensors_of_another_device_than_the_contexts_are_refused():
+    twa.build_library()
+    ctx = twa.Context()                        # no handle: a call that gets through the checks is refused as without a context
+    ctx.device = 0
+    here, there = on_device(0), on_device(1)
+
+    def calls(n):
+        """Every call with its n-th tensor on the other device; None from the number on that a call does not have."""
+        def t(i, *shape, dtype=torch.float32):
+            return (there if i == n else here)(*shape, dtype=dtype)
+
+        ids, space = (dict(dtype=d) for d in (torch.int64, torch.uint8))
+        yield 6, lambda: twa.twa_layer_norm(ctx, t(0, 4, 8), t(1, 8), t(2, 8), 1e-5, t(3, 4, 8), t(4, 4), t(5, 4))
+        yield 9, lambda: twa.twa_layer_norm_backward(ctx, t(0, 4, 8), t(1, 4, 8), t(2, 8), t(3, 4), t(4, 4), t(5, 4, 8), t(6, 8), t(7, 8),
+                                                     t(8, 64, **space))
+        yield 3, lambda: twa.twa_embedding(ctx, t(0, 5, 8), t(1, 4, **ids), 1.0, t(2, 4, 8))
+        yield 4, lambda: twa.twa_embedding_backward(ctx, t(0, 4, 8), t(1, 4, **ids), 1.0, t(2, 5, 8), t(3, 64, **space))
+        yield 7, lambda: twa.twa_token_logprobs(ctx, t(0, 4, 8), t(1, 4, **ids), t(2, 4), t(3, 4), t(4, 4), t(5, 4, 2, dtype=torch.int32),
+                                                t(6, 4, 2))
+        yield 7, lambda: twa.twa_token_logprobs_backward(ctx, t(0, 4, 8), t(1, 4, **ids), t(2, 4), t(3, 4), t(4, 4, 8), t(5, 4), t(6, 4))
+        yield 4, lambda: twa.twa_grad_norm(ctx, twa.Tensors([t(0, 8), t(1, 8)]), t(2, 1), t(3, 64, **space))
+        yield 5, lambda: twa.twa_clip_gather(ctx, twa.Tensors([t(0, 8), t(1, 8)]), 1.0, t(2, 16), t(3, 1), t(4, 64, **space))
+        yield 4, lambda: twa.twa_clip_grads(ctx, twa.Tensors([t(0, 8), t(1, 8)]), 1.0, t(2, 1), t(3, 64, **space))
+
+    for n in range(9):
+        for count, call in calls(n):
+            if n < count:
+                with pytest.raises(ValueError, match="device"):
+                    call()
+    for count, call in calls(-1):              # and with all on the context's device the checks let them through
+        with pytest.raises(twa.TwaError):
+            call()
+    twice = twa.Tensors([there(8), there(8)])
+    with pytest.raises(ValueError, match="context's device"):
+        twa.twa_grad_norm(ctx, twice, here(1), here(64, dtype=torch.uint8))
