@@ -294,7 +294,7 @@ int clip_check(const twa_ctx* ctx, const twa_tensors* t) {
   for (int i = 0; i < t->count; ++i) {
     if (t->sizes[i] < 0 || !twa_dtype_ok(t->dtypes[i]) || (t->sizes[i] && !t->data[i])) return TWA_ERR_INVALID_ARG;
     if (t->sizes[i] > TWA_MAX_ROWS || (total += t->sizes[i]) > TWA_MAX_ROWS) return TWA_ERR_UNSUPPORTED;
-    if (twa_misaligned_to(t->data[i], twa_dtype_size(t->dtypes[i]))) return TWA_ERR_MISALIGNED;
+    if (t->sizes[i] && twa_misaligned_to(t->data[i], twa_dtype_size(t->dtypes[i]))) return TWA_ERR_MISALIGNED;
   }
   return TWA_OK;
 }

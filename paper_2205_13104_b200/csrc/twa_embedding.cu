@@ -611,7 +611,7 @@ int twa_embedding_backward(twa_ctx* ctx, const void* dout, int64_t ldd, twa_dtyp
   if (tokens > TWA_EMBEDDING_MAX_TOKENS || dim > TWA_EMBEDDING_MAX_DIM || vocab > TWA_EMBEDDING_MAX_VOCAB) return TWA_ERR_UNSUPPORTED;
   if (!dtable || ldg < dim || (tokens && (!dout || !ids || ldd < dim))) return TWA_ERR_INVALID_ARG;
   const size_t ds = twa_dtype_size(d_dtype), gs = twa_dtype_size(g_dtype);
-  if (twa_misaligned_to(dout, ds) || twa_misaligned_to(dtable, gs) || twa_misaligned_to(ids, twa_itype_size(id_type)))
+  if (twa_misaligned_to(dtable, gs) || (tokens && (twa_misaligned_to(dout, ds) || twa_misaligned_to(ids, twa_itype_size(id_type)))))
     return TWA_ERR_MISALIGNED;
   if (!ws || ws_bytes < twa_embedding_workspace_bytes(tokens, vocab, dim)) return TWA_ERR_WORKSPACE;
   if (twa_misaligned_to(ws, 16)) return TWA_ERR_MISALIGNED;

@@ -466,9 +466,11 @@ int twa_layer_norm_backward(twa_ctx* ctx, const void* dy, int64_t lddy, const vo
   if (!twa_dtype_ok(g_dtype) || accumulate < 0 || accumulate > 1) return TWA_ERR_INVALID_ARG;
   const size_t size = twa_dtype_size(dtype);
   if (rows && (!dy || !x || !mean || !rstd || !dx || lddy < cols || ldx < cols || lddx < cols)) return TWA_ERR_INVALID_ARG;
-  if (twa_misaligned_to(dy, size) || twa_misaligned_to(x, size) || twa_misaligned_to(dx, size) ||
-      twa_misaligned_to(w, twa_dtype_size(w_dtype)) || twa_misaligned_to(mean, 4) || twa_misaligned_to(rstd, 4) ||
-      twa_misaligned_to(dw, twa_dtype_size(g_dtype)) || twa_misaligned_to(db, twa_dtype_size(g_dtype)))
+  if (rows && (twa_misaligned_to(dy, size) || twa_misaligned_to(x, size) || twa_misaligned_to(dx, size) ||
+               twa_misaligned_to(mean, 4) || twa_misaligned_to(rstd, 4)))
+    return TWA_ERR_MISALIGNED;
+  if (twa_misaligned_to(w, twa_dtype_size(w_dtype)) || twa_misaligned_to(dw, twa_dtype_size(g_dtype)) ||
+      twa_misaligned_to(db, twa_dtype_size(g_dtype)))
     return TWA_ERR_MISALIGNED;
   const bool weights = dw || db;
   if (weights) {

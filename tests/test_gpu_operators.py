@@ -6,6 +6,7 @@ float32, a sum of float32 terms whose longest chain of additions is k errs by at
 magnitudes, and an output is rounded once to its type (relative 2^-8 for bfloat16, U for float32).
 """
 
+import ctypes
 import math
 
 import pytest
@@ -677,6 +678,24 @@ def test_empty_inputs(ctx):
     assert bool((grad == 0).all())
     twa.twa_token_logprobs(ctx, x, ids, none, none.clone())
     twa.twa_token_logprobs_backward(ctx, x, ids, none, none, x.clone())
+    ok(ctx)
+
+
+def test_pointers_of_empty_arrays_are_not_looked_at(ctx):
+    lib, odd = twa.load(), 7                      # on no element's boundary
+    ws, out = torch.empty(1 << 16, dtype=torch.uint8, device=DEV), torch.full((4, 16), 3.0, device=DEV)
+    dw, norm = torch.full((16,), 3.0, device=DEV), torch.full((1,), 3.0, device=DEV)
+    assert lib.twa_layer_norm(ctx, odd, 16, 0, None, None, 0, 0, 16, 1e-5, odd, 16, odd, odd) == 0
+    assert lib.twa_layer_norm_backward(ctx, odd, 16, odd, 16, 0, None, 0, odd, odd, 0, 16, odd, 16, dw.data_ptr(), None, 0, 0,
+                                       ws.data_ptr(), ws.nbytes) == 0
+    assert lib.twa_embedding(ctx, out.data_ptr(), 16, 0, 4, 16, odd, 1, 0, 1.0, odd, 16, 0) == 0
+    assert lib.twa_embedding_backward(ctx, odd, 16, 0, odd, 1, 0, 4, 16, 1.0, -1, out.data_ptr(), 16, 0, 0, ws.data_ptr(), ws.nbytes) == 0
+    assert lib.twa_token_logprobs(ctx, odd, 8, 0, 0, 8, odd, 1, -100, odd, odd, odd, 4, odd, odd) == 0
+    assert lib.twa_token_logprobs_backward(ctx, odd, 8, 0, 0, 8, odd, 1, -100, odd, odd, odd, odd, odd, 8) == 0
+    two = (ctypes.c_void_p * 2)(odd, dw.data_ptr()), (ctypes.c_int64 * 2)(0, 16), (ctypes.c_int32 * 2)(0, 0)
+    t = twa.twa_tensors(*(ctypes.addressof(a) for a in two), 2)
+    assert lib.twa_grad_norm(ctx, ctypes.byref(t), norm.data_ptr(), ws.data_ptr(), ws.nbytes) == 0
+    assert bool((dw == 0).all()) and bool((out == 0).all()) and float(norm) == 0.0
     ok(ctx)
 
 
