@@ -326,7 +326,7 @@ __global__ void ln_weights_loop_kernel(LnArgs a) {
 constexpr int LN_SUM_WARPS = 32, LN_SUM_EACH = (LN_MAX_BLOCKS + LN_SUM_WARPS - 1) / LN_SUM_WARPS;
 __global__ void __launch_bounds__(32 * LN_SUM_WARPS) ln_sum_kernel(const float* part, int blocks, int cols, void* dw, void* db,
                                                                   int g_dtype, int accumulate) {
-  twa_begin(part);
+  twa_begin(part, dw, db);
   __shared__ double run[LN_SUM_WARPS][33];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   int c = blockIdx.x * 32 + lane;                     // 0 .. 2 cols - 1: dw, then db

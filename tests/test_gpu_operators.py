@@ -173,6 +173,21 @@ def test_layer_norm_without_weights_and_with_bfloat16_gradients(ctx):
     ok(ctx)
 
 
+def test_layer_norm_sums_are_added_to_what_the_kernel_before_left(ctx):
+    """Launches may begin while the kernel before them ends: what that one writes last is not to be read too early."""
+    big, cols = torch.empty(1 << 26, device=DEV), 512
+    dw, db = big[-cols:], big[-2 * cols: -cols]
+    none, ws = torch.empty(0, device=DEV), torch.empty(twa.twa_layer_norm_workspace_bytes(0, cols), dtype=torch.uint8, device=DEV)
+    x = torch.empty(0, cols, device=DEV)
+    wrong = torch.zeros((), device=DEV)
+    for i in range(50):
+        big.fill_(float(i))
+        twa.twa_layer_norm_backward(ctx, x, x, None, none, none, x, dw, db, ws, accumulate=True)
+        wrong += (big[-2 * cols:] != float(i)).sum()
+    assert float(wrong) == 0
+    ok(ctx)
+
+
 def test_layer_norm_gradient_against_differences(ctx):
     g = gen(11)
     x, w, b, dy = randn(g, 6, 20), randn(g, 20), randn(g, 20), randn(g, 6, 20)
