@@ -149,6 +149,51 @@ def test_layer_norm_forward_and_backward(ctx, rows, cols, dtype, wtype, pad, shi
     ok(ctx)
 
 
+@pytest.mark.parametrize("rows,cols,dtype,wtype,pad,shift", [
+    (16384, 2048, BF16, F32, 0, 0), (3000, 2048, F32, F32, 0, 0), (9000, 768, BF16, BF16, 0, 0), (20000, 256, F32, F32, 0, 0),
+    (3001, 512, BF16, F32, 8, 8), (40000, 12, F32, F32, 0, 0), (30011, 96, BF16, F32, 0, 0), (6007, 1023, BF16, F32, 5, 3),
+    (20011, 37, F32, BF16, 3, 1), (60013, 3, F32, F32, 0, 0),
+    (1201, 8192, BF16, F32, 0, 0), (1500, 4099, F32, F32, 3, 2), (600, 12000, BF16, F32, 0, 0), (500, 16384, F32, F32, 0, 0),
+    (1300, 16400, BF16, F32, 0, 0), (700, 9001, F32, F32, 0, 1)])
+def test_layer_norm_of_many_rows(ctx, rows, cols, dtype, wtype, pad, shift):
+    """Several rows for every team of threads: the ring's second round, the row that is fetched ahead, sums over rows."""
+    test_layer_norm_forward_and_backward(ctx, rows, cols, dtype, wtype, pad, shift)
+
+
+ALIKE, APART = ((0, 1),) * 4, ((1, 1), (2, 0), (0, 2), (3, 1))
+
+
+@pytest.mark.parametrize("rows,cols,dtype,places", [(4099, 1023, F32, ALIKE), (50021, 7, BF16, ALIKE), (2000, 300, F32, APART),
+                                                    (6000, 64, F32, APART), (1000, 2047, F32, APART), (700, 9000, F32, APART),
+                                                    (9001, 5, F32, APART)])
+def test_layer_norm_of_rows_between_16_byte_boundaries(ctx, rows, cols, dtype, places):
+    """x, dy, y and dx with their rows at the same place between boundaries, or each at another (padding, start)."""
+    g = gen(rows + cols)
+    xv, dv, w = randn(g, rows, cols) + 0.5, randn(g, rows, cols), randn(g, cols)
+    _, x = strided(xv, dtype, *places[0])
+    _, dy = strided(dv, dtype, *places[1])
+    ybuf, y = strided(torch.zeros_like(xv), dtype, *places[2])
+    mean, rstd, dw, db = (torch.empty(n, device=DEV) for n in (rows, rows, cols, cols))
+    ws = torch.empty(twa.twa_layer_norm_workspace_bytes(rows, cols), dtype=torch.uint8, device=DEV)
+    twa.twa_layer_norm(ctx, x, w, None, 1e-5, y, mean, rstd)
+    y64, _, rstd64, _ = layer_norm_64(x, w, None, 1e-5)
+    chain = 64 + cols / 512
+    close(y, y64, norm_tolerances(x, w, None, y64, rstd64, chain))
+    assert untouched(ybuf, y)
+    dxbuf, dx = strided(torch.zeros_like(xv), dtype, *places[3])
+    twa.twa_layer_norm_backward(ctx, dy, x, w, mean, rstd, dx, dw, db, ws)
+    r, m, d = rstd.double()[:, None], mean.double()[:, None], dy.double()
+    h, v = (x.double() - m) * r, d * w.double()
+    dx64 = r * (v - v.mean(1, keepdim=True) - h * (v * h).mean(1, keepdim=True))
+    vb, hb = v.abs().max(1, keepdim=True).values, (r * (x.double().abs() + m.abs())).max(1, keepdim=True).values
+    close(dx, dx64, ROUND[dtype] * dx64.abs() + 3 * chain * U * r * vb * (1 + hb) ** 2 + 1e-30)
+    herr = 4 * U * r * (x.double().abs() + m.abs())
+    close(dw, (d * h).sum(0), (rows + 64) * U * (d * h).abs().sum(0) + (d.abs() * herr).sum(0) + 1e-30)
+    close(db, d.sum(0), (rows + 64) * U * d.abs().sum(0) + 1e-30)
+    assert untouched(dxbuf, dx)
+    ok(ctx)
+
+
 def test_layer_norm_without_weights_and_with_bfloat16_gradients(ctx):
     g = gen(5)
     x = randn(g, 40, 96)
@@ -258,6 +303,47 @@ def test_embedding_and_its_gradient(ctx, tokens, vocab, dim, ttype, atype, itype
         rest[ids.long()[keep]] = False
         assert torch.equal(grad[rest], held[rest])
     ok(ctx)
+
+
+@pytest.mark.parametrize("tokens,vocab,dim", [(20000, 300000, 8), (40000, 1000, 24), (130001, 50272, 8), (16385, 513, 7), (6, (1 << 20) + 5, 4)])
+@pytest.mark.parametrize("ttype,atype,itype,pad,shift", [(F32, BF16, torch.int64, 0, 0), (BF16, F32, torch.int32, 3, 1)])
+def test_embedding_gradient_of_many_tokens(ctx, tokens, vocab, dim, ttype, atype, itype, pad, shift):
+    """More ids than a cluster of blocks sorts, in one to three passes, and a vocabulary beyond its bitmap."""
+    test_embedding_and_its_gradient(ctx, tokens, vocab, dim, ttype, atype, itype, pad, shift)
+
+
+def test_embedding_gradient_of_many_tokens_replays_from_a_graph(ctx):
+    g = gen(77)
+    tokens, vocab, dim = 40000, 70000, 32
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        own = twa.twa_create(0)
+        ids = torch.randint(0, vocab, (tokens,), generator=g, device=DEV)
+        dout = torch.randint(-4, 5, (tokens, dim), generator=g, device=DEV).float()       # sums of whole numbers are exact
+        grad, added = torch.empty(vocab, dim, device=DEV), torch.zeros(vocab, dim, device=DEV)
+        ws = torch.empty(twa.twa_embedding_workspace_bytes(tokens, vocab, dim), dtype=torch.uint8, device=DEV)
+
+        def step():
+            twa.twa_embedding_backward(own, dout, ids, 1.0, grad, ws)
+            twa.twa_embedding_backward(own, dout, ids, 1.0, added, ws, accumulate=True)
+
+        step()
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            step()
+        added.zero_()
+        want = torch.zeros(vocab, dim, device=DEV)
+        for again in range(3):
+            ids.copy_(torch.randint(0, vocab >> again, (tokens,), generator=g, device=DEV))
+            graph.replay()
+            now = torch.zeros(vocab, dim, dtype=torch.float64, device=DEV).index_add_(0, ids, dout.double())
+            want += now.float()
+            assert torch.equal(grad.double(), now) and torch.equal(added, want)
+        assert twa.twa_get_status(own)[0] == 0
+        del graph
+        twa.twa_destroy(own)
 
 
 @pytest.mark.parametrize("tokens,vocab", [(20000, 5), (65536, 1), (6000, 70000)])
@@ -391,6 +477,92 @@ def test_token_logprobs_and_gradient(ctx, rows, vocab, top, dtype, itype, pad, s
         same = z.clone() if pad == 0 else strided(z, dtype, pad, shift)[1]
         twa.twa_token_logprobs_backward(ctx, same, t.to(itype), lse, d_logp, same, **extra)
         assert torch.equal(same, dz)
+    ok(ctx)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("vocab", [75, 2840, 20011])
+@pytest.mark.parametrize("top", [0, 5])
+@pytest.mark.parametrize("with_entropy", [False, True])
+def test_logprobs_of_many_rows(ctx, dtype, vocab, top, with_entropy):
+    """Several rows for every block, with and without the search and the entropy: every output of every row."""
+    rows = 4001
+    g = gen(vocab + top)
+    z = (2.5 * randn(g, rows, vocab) + 4.0 * randn(g, rows, 1)).to(dtype)
+    t = torch.randint(0, vocab, (rows,), generator=g, device=DEV)
+    t[::7] = -100
+    logp, lse = torch.empty(rows, device=DEV), torch.empty(rows, device=DEV)
+    ent = torch.empty(rows, device=DEV) if with_entropy else None
+    ids = torch.empty(rows, top, dtype=torch.int32, device=DEV) if top else None
+    tlp = torch.empty(rows, top, device=DEV) if top else None
+    twa.twa_token_logprobs(ctx, z, t, logp, lse, entropy=ent, top_ids=ids, top_logp=tlp)
+    want = logprobs_64(z, t, max(top, 1))
+    tol, big = logprob_tolerances(z, vocab)
+    lse_tol = tol + 2 * U * want[1].abs()
+    close(lse, want[1], lse_tol)
+    close(logp, want[0], lse_tol + 4 * U * (big + want[0].abs()))
+    if with_entropy:
+        close(ent, want[2], 4 * tol * (1.0 + want[2] + math.log(vocab)))
+    if top:
+        assert torch.equal(ids.long(), want[3])
+        close(tlp, want[4], (lse_tol + 4 * U * big)[:, None] + 4 * U * want[4].abs())
+    ok(ctx)
+
+
+FAR = [8191.5, 8192.0, 8193.0, 20000.0, 1e5, 1e30, 3e38]
+
+
+@pytest.mark.parametrize("vocab", [333, 20011, 200001])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows", [2 * len(FAR) + 2, 700])
+@pytest.mark.parametrize("mixed", [False, True])
+def test_logprobs_of_logits_far_from_zero(ctx, vocab, dtype, rows, mixed):
+    """Rows whose largest logit is far above or below zero, whole rows at the type's lowest value, and (mixed) with half of a row's
+    logits near zero; few rows, which clusters share, and many."""
+    if vocab > 100000 and rows > 100:
+        rows = 320
+    g = gen(vocab + rows)
+    base = torch.tensor([s * v for v in FAR for s in (1.0, -1.0)] + [0.0, 0.0], device=DEV).repeat(rows // (2 * len(FAR) + 2) + 1)[:rows]
+    z = randn(g, rows, vocab)
+    near = z[:, vocab // 2:].clone()
+    z += base[:, None]
+    if mixed:
+        z[:, vocab // 2:] = near
+    z[-1] = torch.finfo(dtype).min
+    z = z.to(dtype)
+    t = torch.randint(0, vocab, (rows,), generator=g, device=DEV)
+    logp, lse, ent = (torch.empty(rows, device=DEV) for _ in range(3))
+    ids, tlp = torch.empty(rows, 4, dtype=torch.int32, device=DEV), torch.empty(rows, 4, device=DEV)
+    twa.twa_token_logprobs(ctx, z, t, logp, lse, entropy=ent, top_ids=ids, top_logp=tlp)
+    want = logprobs_64(z, t, 4)
+    # Differences to the maximum come first, so its size does not count: a sum's longest chain is a warp's lane over the whole
+    # row, ex2 (2^-22), the exponent rounded twice at a magnitude below 2 x 40 where it counts; lse itself is rounded
+    tol = (vocab / 32 + 48 + 4 * 40.0) * U
+    close(lse, want[1], tol + 2 * U * want[1].abs())
+    # the result in 64 bits from the target's difference to the maximum, which 64 bits hold exactly
+    m = z.double().max(1, keepdim=True).values
+    d = z.double() - m
+    logs = torch.log(torch.exp(d).sum(1))
+    at = d.gather(1, t[:, None])[:, 0] - logs
+    close(logp, at, tol + 4 * U * at.abs())
+    p = torch.exp(d - logs[:, None])
+    h = -torch.where(p > 0, p * (d - logs[:, None]), 0.0).sum(1)
+    close(ent, h, 4 * tol * (1.0 + h + math.log(vocab)))
+    assert torch.equal(ids.long(), want[3])
+    best = d.gather(1, want[3]) - logs[:, None]
+    close(tlp, best, tol + 4 * U * best.abs())
+    only = [torch.empty_like(logp), torch.empty_like(lse)]
+    twa.twa_token_logprobs(ctx, z, t, *only)
+    assert torch.equal(only[0], logp) and torch.equal(only[1], lse)
+    # the gradient, from lse as it is in float32
+    d_logp, dz = randn(g, rows), torch.empty_like(z)
+    twa.twa_token_logprobs_backward(ctx, z, t, lse, d_logp, dz)
+    p = torch.exp(z.double() - lse.double()[:, None])
+    one = torch.zeros_like(p).scatter_(1, t[:, None], 1.0)
+    dz64 = d_logp.double()[:, None] * (one - p)
+    scale = d_logp.double().abs()[:, None]
+    # z - lse is one rounding of at most 40 where p counts (88 where lse, rounded, lies so far below the logits that p is that large)
+    close(dz, dz64, (2.0 ** -21 + 4 * 128 * U) * scale * p + 2 * U * scale * one + ROUND[dtype] * dz64.abs() + 1e-36)
     ok(ctx)
 
 
@@ -545,6 +717,18 @@ def test_norm_and_clipping(ctx, sizes, kinds, flat, shift):
     for a, b in zip(before, grads):
         close(b, a.double() * factor, (20 * U + ROUND[a.dtype]) * a.double().abs() * factor + 1e-38)
     ok(ctx)
+
+
+LARGE_SETS = [[20_000_001], [20_000_003, 5, 7_000_001], [1 + (i * 7919) % 85703 for i in range(700)],
+              [40_000 + 8 * i for i in range(450)] + [1] * 70]
+
+
+@pytest.mark.parametrize("sizes", LARGE_SETS, ids=lambda s: f"{len(s)}x{max(s)}")
+@pytest.mark.parametrize("kinds,flat", [((F32,), F32), ((BF16,), BF16), ((BF16, F32), F32), ((F32, BF16, BF16), BF16)])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_norm_and_clipping_of_many_chunks(ctx, sizes, kinds, flat, shift):
+    """Several chunks, and several tensors, for every block of either kernel."""
+    test_norm_and_clipping(ctx, sizes, kinds, flat, shift)
 
 
 def test_norm_of_nothing_and_of_what_is_no_number(ctx):
