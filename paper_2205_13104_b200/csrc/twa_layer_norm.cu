@@ -10,8 +10,9 @@
 // digits that a mean far from zero costs.  Instructions come next: what a row costs beside its elements (the reductions, the
 // root, addresses) is paid by every warp that shares it, so few threads share a row and hold many elements each, and sums
 // and products go in pairs (16384 x 2048 bfloat16 with 8 elements a thread: 35 instructions an element, 45 us).
-// Forward up to 2048 columns (backward 512) a warp or a part of one has a row and there is no barrier; above, a block has,
-// with one barrier a row: forward each warp takes its own mean and the squares about it, and those combine exactly.
+// Forward up to 2048 columns bfloat16 or 1024 float32 (backward 512) a warp or a part of one has a row and there is no
+// barrier; above, a block has, with one barrier a row: forward each warp takes its own mean and the squares about it, and
+// those combine exactly.
 // The weights lie in shared memory as float32, whatever their type and alignment.  Backward a thread keeps the same
 // columns for all its rows, and with them the columns' partial sums of dw and db in registers (from 8193 columns on in
 // shared memory).  The partial sums of the blocks are added in float64 by a second kernel in block order, so results
@@ -190,88 +191,20 @@ __global__ void ln_forward_loop_kernel(LnArgs a) {
   }
 }
 
-// The kernel that holds at least nv units a thread, and how many that is.
-template <typename T, int E, bool BACK, int PER>
-LnKernel ln_pick(int* nv, int units, bool aligned) {
-  const int wanted = *nv;
-  constexpr int held = LN_HELD<E, BACK, PER>;
-#define LN_TRY(n, if_more)                                                              \
-  if constexpr (E * n <= held && (PER <= 32 || 2 * E * n >= held) && (if_more)) {       \
-    if (wanted <= n) {                                                                  \
-      *nv = n;                                                                          \
-      if constexpr (E > 1 && PER > 0)                                                   \
-        if (aligned && units == PER * n) return ln_forward_kernel<T, E, n, PER, true>;          \
-      return ln_forward_kernel<T, E, n, PER, false>;                                            \
-    }                                                                                   \
+struct LnForward {
+  template <int E, int PER>
+  static constexpr int HELD = PER == 32 && E == 8 ? 64 : 32;
+  static constexpr long long MAX_BLOCKS = 1LL << 30;
+  static size_t ring_bytes(int, int, bool) { return 0; }
+  template <typename T, int E, int NV, int PER>
+  static LnKernel kernel(bool aligned, bool full) {
+    if constexpr (E > 1 && PER > 0)
+      if (aligned && full) return ln_forward_kernel<T, E, NV, PER, true>;
+    return ln_forward_kernel<T, E, NV, PER, false>;
   }
-  LN_TRY(1, true)
-  LN_TRY(2, true)
-  LN_TRY(3, E > 1 && PER > 0)
-  LN_TRY(4, true)
-  LN_TRY(6, E > 1 && PER > 0)
-  LN_TRY(8, true)
-  LN_TRY(16, true)
-  LN_TRY(32, true)
-#undef LN_TRY
-  return nullptr;
-}
-
-template <typename T, int E, bool BACK>
-int ln_plan_units(twa_ctx* ctx, int classes, long long rows, int cols, LnPlan* plan) {
-  // with several classes a row can begin anywhere in its first unit
-  const int units = (cols + E - 1) / E + (classes > 1 ? 1 : 0);
-  constexpr int warp_held = LN_HELD<E, BACK, 32> / E, held = LN_HELD<E, BACK, 64> / E;
-  const bool aligned = classes == 1;
-  LnPlan p = {nullptr, 0, 0, 5, 0, 0};
-  while (1 << p.log_classes < classes) ++p.log_classes;
-  int nv = 0, per = 32;
-  long long blocks = rows;
-  p.threads = LN_WARP_THREADS;
-  if (units <= 32 * warp_held) {
-    // as few threads a row as hold it, while there are rows enough to keep the SMs busy
-    while (p.log_lanes > 0 && units <= held << (p.log_lanes - 1) && (rows << (p.log_lanes - 1)) >= 32LL * 16 * ctx->sm_count) --p.log_lanes;
-    while (p.log_lanes > 0 && units <= 1 << (p.log_lanes - 1)) --p.log_lanes;
-    per = 1 << p.log_lanes;
-    nv = (units + per - 1) / per;
-    p.kernel = per == 32 ? ln_pick<T, E, BACK, 32>(&nv, units, aligned) : ln_pick<T, E, BACK, 0>(&nv, units, aligned);
-    blocks = twa_ceil_div(rows, p.threads / per);
-  } else if (units <= LN_BLOCK_THREADS * held) {
-    for (per = 64; units > per * held;) per *= 2;
-    nv = (units + per - 1) / per;
-    p.threads = per;
-    p.kernel = per == 64 ? ln_pick<T, E, BACK, 64>(&nv, units, aligned)
-               : per == 128 ? ln_pick<T, E, BACK, 128>(&nv, units, aligned)
-               : per == 256 ? ln_pick<T, E, BACK, 256>(&nv, units, aligned) : ln_pick<T, E, BACK, 512>(&nv, units, aligned);
-  }
-  p.smem = sizeof(float) * 2 * per * nv * E;
-  if (p.kernel && p.smem > 44 * 1024) {      // 48 KB with what the kernel declares
-    // which of the kernels that can need as much: by threads and what they hold
-    static int smem_set[5][40][2][64] = {};
-    int log = 0;
-    while (64 << log < p.threads) ++log;
-    int rc = twa_ensure_smem(ctx, reinterpret_cast<const void*>(p.kernel),
-                             &smem_set[log][nv][aligned && units == per * nv][ctx->device & 63], static_cast<int>(p.smem));
-    if (rc) return rc;
-  }
-  const long long per_sm = p.threads < 512 ? 512 / p.threads : 1;
-  long long most = ctx->sm_count * per_sm;
-  if (BACK && most > LN_MAX_BLOCKS) most = LN_MAX_BLOCKS;
-  if (blocks > most) blocks = most;
-  if (classes > 1) blocks = twa_ceil_div(blocks, classes) * classes;
-  p.blocks = static_cast<int>(blocks);
-  *plan = p;
-  return TWA_OK;
-}
-
-// classes: ways in which the rows lie on 16-byte boundaries (1: all begin on one), 0: the matrices differ in that.
-template <typename T, bool BACK>
-int ln_plan(twa_ctx* ctx, int classes, long long rows, int cols, LnPlan* plan) {
-  if (classes) {
-    int rc = ln_plan_units<T, twa_vec<T>, BACK>(ctx, classes, rows, cols, plan);
-    if (rc || plan->kernel) return rc;
-  }
-  return ln_plan_units<T, 1, BACK>(ctx, 1, rows, cols, plan);
-}
+  template <typename T, int E>
+  static void wide(int, LnPlan*) {}
+};
 
 }  // namespace
 
@@ -291,7 +224,7 @@ int twa_layer_norm(twa_ctx* ctx, const void* x, int64_t ldx, twa_dtype dtype, co
   LnArgs a = {x, nullptr, y, w, b, mean, rstd, nullptr, ldx, 0, ldy, rows, cols, w_dtype, 5, 0, eps, ctx->wait_limit_ns, ctx->d_status};
   const int classes = ln_classes(x, ldx, y, ldy, y, ldy, rows, cols, size);
   LnPlan p;
-  rc = dtype == TWA_BF16 ? ln_plan<bf16, false>(ctx, classes, rows, cols, &p) : ln_plan<float, false>(ctx, classes, rows, cols, &p);
+  rc = dtype == TWA_BF16 ? ln_plan<LnForward, bf16>(ctx, classes, rows, cols, &p) : ln_plan<LnForward, float>(ctx, classes, rows, cols, &p);
   if (rc) return rc;
   a.log_lanes = p.log_lanes;
   a.log_classes = p.log_classes;

@@ -11,7 +11,6 @@ constexpr int LN_BLOCK_THREADS = 512;  // a block per row: at most
 constexpr int LN_WIDE_THREADS = 1024, LN_WIDE_HELD = 16;
 constexpr int LN_LOOP_THREADS = 512;   // rows wider than the registers of a block
 constexpr int LN_LOOP_PARTS = 64;      // and the rows of partial sums for those
-constexpr int LN_MAX_SMEM = 220 * 1024;
 
 struct LnArgs {
   const void* x;
@@ -232,10 +231,6 @@ struct LnPlan {
   size_t smem;
 };
 
-// What a thread holds of a row at most.  The backward pass holds x, dy and two sums per column.
-template <int E, bool BACK, int PER>
-constexpr int LN_HELD = BACK ? 16 : (PER == 32 && E == 8 ? 64 : 32);
-
 // Ways in which the rows of all matrices lie on 16-byte boundaries, if they do alike; else 0, and the rows are read element by
 // element.  So are rows that begin less than a unit of 16 bytes apart but for one element: a row's first and last unit reach up to
 // that far beside it, which then is more than a neighbouring row (3 x 2 bfloat16: row 1's unit is 8 of the matrix's 6 elements).
@@ -255,6 +250,95 @@ int ln_check(const twa_ctx* ctx, twa_dtype dt, twa_dtype wt, int64_t rows, int c
   if (!ctx || !twa_dtype_ok(dt) || !twa_dtype_ok(wt) || rows < 0 || cols < 1) return TWA_ERR_INVALID_ARG;
   if (rows > (1LL << 40) || cols > TWA_LAYER_NORM_MAX_COLS) return TWA_ERR_UNSUPPORTED;
   return TWA_OK;
+}
+
+// ---- plans.  The directions (LnForward, LnBackward) differ in
+//   HELD<E, PER>    elements that a thread holds of a row at most
+//   MAX_BLOCKS      blocks at most
+//   kernel<..>()    the kernel of NV units a thread; full: the row is exactly the units of its threads
+//   ring_bytes()    shared memory of the rows under way
+//   wide<..>()      the plan of rows on 16-byte boundaries that are too wide for those kernels, where there is one
+
+// The kernel that holds at least nv units a thread, and how many that is.
+template <typename Dir, typename T, int E, int PER>
+LnKernel ln_pick(int* nv, int units, bool aligned) {
+  const int wanted = *nv;
+  constexpr int held = Dir::template HELD<E, PER>;
+#define LN_TRY(n, if_more)                                                              \
+  if constexpr (E * n <= held && (PER <= 32 || 2 * E * n >= held) && (if_more)) {       \
+    if (wanted <= n) {                                                                  \
+      *nv = n;                                                                          \
+      return Dir::template kernel<T, E, n, PER>(aligned, units == PER * n);             \
+    }                                                                                   \
+  }
+  LN_TRY(1, true)
+  LN_TRY(2, true)
+  LN_TRY(3, E > 1 && PER > 0)
+  LN_TRY(4, true)
+  LN_TRY(6, E > 1 && PER > 0)
+  LN_TRY(8, true)
+  LN_TRY(16, true)
+  LN_TRY(32, true)
+#undef LN_TRY
+  return nullptr;
+}
+
+template <typename Dir, typename T, int E>
+int ln_plan_units(twa_ctx* ctx, int classes, long long rows, int cols, LnPlan* plan) {
+  // with several classes a row can begin anywhere in its first unit
+  const int units = (cols + E - 1) / E + (classes > 1 ? 1 : 0);
+  constexpr int warp_held = Dir::template HELD<E, 32> / E, held = Dir::template HELD<E, 64> / E;
+  const bool aligned = classes == 1;
+  LnPlan p = {nullptr, 0, 0, 5, 0, 0};
+  while (1 << p.log_classes < classes) ++p.log_classes;
+  int nv = 0, per = 32;
+  long long blocks = rows;
+  p.threads = LN_WARP_THREADS;
+  if (units <= 32 * warp_held) {
+    // as few threads a row as hold it, while there are rows enough to keep the SMs busy
+    while (p.log_lanes > 0 && units <= held << (p.log_lanes - 1) && (rows << (p.log_lanes - 1)) >= 32LL * 16 * ctx->sm_count) --p.log_lanes;
+    while (p.log_lanes > 0 && units <= 1 << (p.log_lanes - 1)) --p.log_lanes;
+    per = 1 << p.log_lanes;
+    nv = (units + per - 1) / per;
+    p.kernel = per == 32 ? ln_pick<Dir, T, E, 32>(&nv, units, aligned) : ln_pick<Dir, T, E, 0>(&nv, units, aligned);
+    blocks = twa_ceil_div(rows, p.threads / per);
+  } else if (units <= LN_BLOCK_THREADS * held) {
+    for (per = 64; units > per * held;) per *= 2;
+    nv = (units + per - 1) / per;
+    p.threads = per;
+    p.kernel = per == 64 ? ln_pick<Dir, T, E, 64>(&nv, units, aligned)
+               : per == 128 ? ln_pick<Dir, T, E, 128>(&nv, units, aligned)
+               : per == 256 ? ln_pick<Dir, T, E, 256>(&nv, units, aligned) : ln_pick<Dir, T, E, 512>(&nv, units, aligned);
+  }
+  p.smem = sizeof(float) * 2 * per * nv * E + (E > 1 ? Dir::ring_bytes(per, nv, aligned) : 0);
+  if (!p.kernel && aligned) Dir::template wide<T, E>(units, &p);
+  if (p.kernel && p.smem > 44 * 1024) {      // 48 KB with what the kernel declares
+    // which of the kernels that can need as much: by threads of a row (0: the one of rows too wide for the others) and units of a thread
+    static int smem_set[6][40][3][64] = {};
+    int log = nv ? 1 : 0;
+    while (nv && 16 << log < per) ++log;
+    int rc = twa_ensure_smem(ctx, reinterpret_cast<const void*>(p.kernel),
+                             &smem_set[log][nv][aligned ? (units == per * nv ? 2 : 1) : 0][ctx->device & 63], static_cast<int>(p.smem));
+    if (rc) return rc;
+  }
+  const long long per_sm = p.threads < 512 ? 512 / p.threads : 1;
+  long long most = ctx->sm_count * per_sm;
+  if (most > Dir::MAX_BLOCKS) most = Dir::MAX_BLOCKS;
+  if (blocks > most) blocks = most;
+  if (classes > 1) blocks = twa_ceil_div(blocks, classes) * classes;
+  p.blocks = static_cast<int>(blocks);
+  *plan = p;
+  return TWA_OK;
+}
+
+// classes: ways in which the rows lie on 16-byte boundaries (1: all begin on one), 0: they are read element by element.
+template <typename Dir, typename T>
+int ln_plan(twa_ctx* ctx, int classes, long long rows, int cols, LnPlan* plan) {
+  if (classes) {
+    int rc = ln_plan_units<Dir, T, twa_vec<T>>(ctx, classes, rows, cols, plan);
+    if (rc || plan->kernel) return rc;
+  }
+  return ln_plan_units<Dir, T, 1>(ctx, 1, rows, cols, plan);
 }
 
 }  // namespace

@@ -353,98 +353,31 @@ __global__ void __launch_bounds__(32 * LN_SUM_WARPS) ln_sum_kernel(const float* 
   twa_store_any(out, g_dtype, i, static_cast<float>(s));
 }
 
-// The kernel that holds at least nv units a thread, and how many that is.
-template <typename T, int E, bool BACK, int PER>
-LnKernel ln_pick(int* nv, int units, bool aligned) {
-  const int wanted = *nv;
-  constexpr int held = LN_HELD<E, BACK, PER>;
-#define LN_TRY(n, if_more)                                                              \
-  if constexpr (E * n <= held && (PER <= 32 || 2 * E * n >= held) && (if_more)) {       \
-    if (wanted <= n) {                                                                  \
-      *nv = n;                                                                          \
-      if constexpr (E > 1 && PER > 0) {                                                 \
-        if (aligned && units == PER * n) return ln_backward_kernel<T, E, n, PER, true, true>; \
-        if (aligned) return ln_backward_kernel<T, E, n, PER, false, true>;              \
-      }                                                                                 \
-      return ln_backward_kernel<T, E, n, PER, false, false>;                            \
-    }                                                                                   \
+// x, dy and two sums a column take the registers.
+struct LnBackward {
+  template <int E, int PER>
+  static constexpr int HELD = 16;
+  static constexpr long long MAX_BLOCKS = LN_MAX_BLOCKS;
+  static size_t ring_bytes(int per, int nv, bool aligned) {
+    if (!aligned || per < 32) return 0;
+    return 16LL * 2 * per * nv * (nv >= 3 ? LN_RING_ROWS<3> : LN_RING_ROWS<1>) * (per == 32 ? LN_WARP_THREADS / 32 : 1);
   }
-  LN_TRY(1, true)
-  LN_TRY(2, true)
-  LN_TRY(3, E > 1 && PER > 0)
-  LN_TRY(4, true)
-  LN_TRY(6, E > 1 && PER > 0)
-  LN_TRY(8, true)
-  LN_TRY(16, true)
-  LN_TRY(32, true)
-#undef LN_TRY
-  return nullptr;
-}
-
-template <typename T, int E, bool BACK>
-int ln_plan_units(twa_ctx* ctx, int classes, long long rows, int cols, LnPlan* plan) {
-  // with several classes a row can begin anywhere in its first unit
-  const int units = (cols + E - 1) / E + (classes > 1 ? 1 : 0);
-  constexpr int warp_held = LN_HELD<E, BACK, 32> / E, held = LN_HELD<E, BACK, 64> / E;
-  const bool aligned = classes == 1;
-  LnPlan p = {nullptr, 0, 0, 5, 0, 0};
-  while (1 << p.log_classes < classes) ++p.log_classes;
-  int nv = 0, per = 32;
-  long long blocks = rows;
-  p.threads = LN_WARP_THREADS;
-  if (units <= 32 * warp_held) {
-    // as few threads a row as hold it, while there are rows enough to keep the SMs busy
-    while (p.log_lanes > 0 && units <= held << (p.log_lanes - 1) && (rows << (p.log_lanes - 1)) >= 32LL * 16 * ctx->sm_count) --p.log_lanes;
-    while (p.log_lanes > 0 && units <= 1 << (p.log_lanes - 1)) --p.log_lanes;
-    per = 1 << p.log_lanes;
-    nv = (units + per - 1) / per;
-    p.kernel = per == 32 ? ln_pick<T, E, BACK, 32>(&nv, units, aligned) : ln_pick<T, E, BACK, 0>(&nv, units, aligned);
-    blocks = twa_ceil_div(rows, p.threads / per);
-  } else if (units <= LN_BLOCK_THREADS * held) {
-    for (per = 64; units > per * held;) per *= 2;
-    nv = (units + per - 1) / per;
-    p.threads = per;
-    p.kernel = per == 64 ? ln_pick<T, E, BACK, 64>(&nv, units, aligned)
-               : per == 128 ? ln_pick<T, E, BACK, 128>(&nv, units, aligned)
-               : per == 256 ? ln_pick<T, E, BACK, 256>(&nv, units, aligned) : ln_pick<T, E, BACK, 512>(&nv, units, aligned);
-  }
-  p.smem = sizeof(float) * 2 * per * nv * E;
-  if (E > 1 && per >= 32 && aligned) p.smem += 16LL * 2 * per * nv * (nv >= 3 ? LN_RING_ROWS<3> : LN_RING_ROWS<1>) * (per == 32 ? LN_WARP_THREADS / 32 : 1);
-  if constexpr (BACK) {
-    if (!p.kernel && aligned && units <= LN_WIDE_THREADS * (LN_WIDE_HELD / E)) {
-      p.threads = LN_WIDE_THREADS;
-      p.smem = sizeof(float) * 3 * units * E;
-      p.kernel = ln_backward_wide_kernel<T, E>;
+  template <typename T, int E, int NV, int PER>
+  static LnKernel kernel(bool aligned, bool full) {
+    if constexpr (E > 1 && PER > 0) {
+      if (aligned && full) return ln_backward_kernel<T, E, NV, PER, true, true>;
+      if (aligned) return ln_backward_kernel<T, E, NV, PER, false, true>;
     }
+    return ln_backward_kernel<T, E, NV, PER, false, false>;
   }
-  if (p.kernel && p.smem > 44 * 1024) {      // 48 KB with what the kernel declares
-    // which of the kernels that can need as much: by threads and what they hold
-    static int smem_set[6][40][3][64] = {};
-    int log = per == 32 ? 5 : 0;
-    while (per > 32 && 64 << log < p.threads) ++log;
-    int rc = twa_ensure_smem(ctx, reinterpret_cast<const void*>(p.kernel),
-                             &smem_set[log][nv][aligned ? (units == per * nv ? 2 : 1) : 0][ctx->device & 63], static_cast<int>(p.smem));
-    if (rc) return rc;
+  template <typename T, int E>
+  static void wide(int units, LnPlan* p) {
+    if (units > LN_WIDE_THREADS * (LN_WIDE_HELD / E)) return;
+    p->threads = LN_WIDE_THREADS;
+    p->smem = sizeof(float) * 3 * units * E;
+    p->kernel = ln_backward_wide_kernel<T, E>;
   }
-  const long long per_sm = p.threads < 512 ? 512 / p.threads : 1;
-  long long most = ctx->sm_count * per_sm;
-  if (BACK && most > LN_MAX_BLOCKS) most = LN_MAX_BLOCKS;
-  if (blocks > most) blocks = most;
-  if (classes > 1) blocks = twa_ceil_div(blocks, classes) * classes;
-  p.blocks = static_cast<int>(blocks);
-  *plan = p;
-  return TWA_OK;
-}
-
-// classes: ways in which the rows lie on 16-byte boundaries (1: all begin on one), 0: the matrices differ in that.
-template <typename T, bool BACK>
-int ln_plan(twa_ctx* ctx, int classes, long long rows, int cols, LnPlan* plan) {
-  if (classes) {
-    int rc = ln_plan_units<T, twa_vec<T>, BACK>(ctx, classes, rows, cols, plan);
-    if (rc || plan->kernel) return rc;
-  }
-  return ln_plan_units<T, 1, BACK>(ctx, 1, rows, cols, plan);
-}
+};
 
 }  // namespace
 
@@ -484,7 +417,7 @@ int twa_layer_norm_backward(twa_ctx* ctx, const void* dy, int64_t lddy, const vo
   if (rows) {
     const int classes = ln_classes(x, ldx, dy, lddy, dx, lddx, rows, cols, size);
     LnPlan p;
-    rc = dtype == TWA_BF16 ? ln_plan<bf16, true>(ctx, classes, rows, cols, &p) : ln_plan<float, true>(ctx, classes, rows, cols, &p);
+    rc = dtype == TWA_BF16 ? ln_plan<LnBackward, bf16>(ctx, classes, rows, cols, &p) : ln_plan<LnBackward, float>(ctx, classes, rows, cols, &p);
     if (rc) return rc;
     a.log_lanes = p.log_lanes;
     a.log_classes = p.log_classes;
