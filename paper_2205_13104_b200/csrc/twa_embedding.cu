@@ -34,9 +34,8 @@ constexpr int SMALL_VOCAB = 1 << 20;                       // ids whose bitmap a
 // Zeros of a block: with 16384 x 2048 into 50272 rows and 96 MB beside the sort 88.6 us with 8 KB, 85.2 with 16, 88.1 with 32.
 constexpr int FILL_BYTES = 1 << 14;
 constexpr int FILL_TEAM = 7;                               // log2 of the threads a row, those of the smallest block that writes zeros
-// Zeros written beside a sorting kernel: what its few us have room for, and those of the cluster's sort (the same case 85.2 us with
-// 96 MB, 83.8 with 128, 81.6 with 160; 16384 x 777 into 128000 rows 92.1, 93.1 and 94.8).
-constexpr long long FILL_BESIDE_SORT = 32LL << 20, FILL_BESIDE_CLUSTER = 160LL << 20;
+// Zeros written beside a sorting kernel: what its few us have room for.
+constexpr long long FILL_BESIDE_SORT = 32LL << 20;
 
 // E elements of any pairing of the two types; E = 8 wants both addresses on 16 bytes, E = 1 nothing.
 template <typename T, int E>
@@ -539,6 +538,24 @@ void launch_embedding(twa_ctx* ctx, bool packs, const void* table, int64_t ldt, 
                                                                           ctx->d_status);
 }
 
+// Zeros written beside the one launch that sorts in shared memory: 160 MB, or 128 where rows do not begin and end on 16 bytes, which are
+// written more slowly.  A single block (up to 2048 ids) sorts in half the time of a cluster: at most half of the table then (but
+// 48 MB), because the sums that follow hide the rest if they take a run of ids and more.  In us, bfloat16 rows into
+// float32 or bfloat16 (b) tables, by MB beside the sort:
+//                         64    96   128   160                              32    64    96   128   160
+//   16384, 50272 x 2048   86.9  84.8  83.3  81.6      2048, 50272 x 2048     73.2  70.5  66.6  66.8  67.7
+//   16384, 128000 x 777   95.4  92.2  92.8  94.4      2048, 128000 x 777     76.6  71.8  72.4  73.9  75.1
+//   16384, 128000 x 1024b 69.9  66.0  63.1  62.9      2048, 128000 x 1024b   62.0  56.8  54.9  54.3  53.6
+//    4096, 128000 x 777   78.2  75.1  74.4  75.5      2048, 120000 x 256     37.0  34.8  37.4  39.8  39.8
+//    4096, 32000 x 4096   94.6  93.2  92.3  91.7        64, 120000 x 256     28.5  27.2  30.9  34.0  34.0
+// and half / all of the table: 1, 50272 x 768b 20.9 / 19.5; 64, 32003 x 129b 21.1 / 18.8; 2048, 24000 x 1024b 29.0 / 27.7.
+long long emb_beside(const EmbFill& fill, int tokens, int blocks) {
+  const bool whole = ((reinterpret_cast<uintptr_t>(fill.table) | fill.stride | fill.bytes) & 15) == 0;
+  const long long half = fill.bytes * fill.row1 / 2, least = 48LL << 20, most = (whole ? 160LL : 128LL) << 20;
+  if (blocks > 1 || tokens < EMB_RUN || half > most) return most;
+  return half > least ? half : least;
+}
+
 // The number of blocks that write the zeros of rows row0 .. of `fill` within `budget` bytes (0: all that are left); the
 // rows are taken off `left`.
 unsigned emb_fill_blocks(const EmbFill& left, long long budget, EmbFill* part) {
@@ -629,7 +646,7 @@ int twa_embedding_backward(twa_ctx* ctx, const void* dout, int64_t ldd, twa_dtyp
   if (n <= SMALL_TOKENS && vocab <= SMALL_VOCAB) {
     const int blocks = n <= SMALL_TILE ? 1 : (n <= 2 * SMALL_TILE ? 2 : (n <= 4 * SMALL_TILE ? 4 : 8));
     EmbFill part;
-    const unsigned zeros = emb_fill_blocks(fill, FILL_BESIDE_CLUSTER, &part);
+    const unsigned zeros = emb_fill_blocks(fill, emb_beside(fill, n, blocks), &part);
     part.used = nullptr;
     const unsigned grid = blocks + static_cast<unsigned>(twa_ceil_div(zeros, blocks)) * blocks;
     const cudaError_t launched =
