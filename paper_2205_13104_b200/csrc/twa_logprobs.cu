@@ -302,10 +302,11 @@ __device__ __noinline__ u64 lp_best_of_all(const T* row, int from, int to) {
   return list;
 }
 
-// Every wait that runs out sets gave_up, and whoever waits later does not wait long.  From then on nothing is passed on: the warp
-// that copies looks at the flag before it fills a stage again (the last copy into it may not have landed), a warp that
-// adds up before it hands over a row.  So a row whose barrier completes is right, and one whose does not is reported by the
-// warp that would finish it.  (A look and a vote after every wait: 2 % of the time, one of each a row: 1.5 %, this: below 1 %.)
+// Every wait that runs out sets gave_up, and whoever waits later does not wait long.  A thread sets it before its warp arrives anywhere
+// again, so two looks at it are enough: the warp that copies looks before it fills a stage again (the last copy into it
+// may not have landed), and a warp that finishes rows after its wait for one, whose results are right if the flag is not set, and
+// not stored but reported if it is.  The summing warps do not look (with a look of theirs at each row's end 1 % slower, in
+// every chunk 2 %).
 __device__ __forceinline__ bool lp_gave_up(const int* gave_up) { return *static_cast<const volatile int*>(gave_up) != 0; }
 
 // Chunks of a slot, as a power of two.
@@ -403,7 +404,8 @@ __global__ void __launch_bounds__(LP_BLOCK, LP_BLOCKS_PER_SM<TOP>) logprobs_kern
         target = twa_load_id(a.targets, a.itype, row);
         if (target >= 0 && target < a.vocab) zt = twa_to_float(x.base[x.skew + target]);
       }
-      if (!__all_sync(0xffffffffu, twa_wait(&sh.row_full[turn], r & 1, &sh.gave_up, a.wait_limit_ns))) {
+      const bool good = twa_wait(&sh.row_full[turn], r & 1, &sh.gave_up, a.wait_limit_ns) && !lp_gave_up(&sh.gave_up);
+      if (!__all_sync(0xffffffffu, good)) {
         if (lane == 0) twa_set_status(a.status, TWA_ERR_TIMEOUT, -1);
         if (parts > 1) {
           twa_cluster_sync();
@@ -722,7 +724,7 @@ __global__ void __launch_bounds__(LP_BLOCK, LP_BLOCKS_PER_SM<TOP>) logprobs_kern
     if (lane == 0) sh.stat[turn][warp] = st;
     if (TOP) sh.key[turn][threadIdx.x] = some ? lp_rank(m) : 0;
     __syncwarp();
-    if (lane == 0 && !lp_gave_up(&sh.gave_up)) twa_mbar_arrive(twa_smem_u32(&sh.row_full[turn]));
+    if (lane == 0) twa_mbar_arrive(twa_smem_u32(&sh.row_full[turn]));
   }
   if (parts > 1) {
     twa_cluster_sync();
