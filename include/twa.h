@@ -562,7 +562,8 @@ int twa_token_logprobs(twa_ctx* ctx, const void* logits, int64_t ld, twa_dtype d
 /* dlogits[j] = d_logp ([j == target] - p[j]) - d_entropy p[j] (log p[j] + entropy), with lse and entropy as the
  * forward call gave them; rows whose target is ignored have the second part only, rows of -inf only are 0.
  *  entropy, d_entropy  rows floats, or both NULL.   dlogits  rows x vocab of dtype; may be logits
- *  (with ldd == ld).  A mean cross entropy over m rows: d_logp = -1/m. */
+ *  (with ldd == ld).  A mean cross entropy over m rows: d_logp = -1/m.
+ * Device-side error: TWA_ERR_INVALID_ARG as above; such a row has no j == target. */
 int twa_token_logprobs_backward(twa_ctx* ctx, const void* logits, int64_t ld, twa_dtype dtype, int64_t rows,
                                 int vocab, const void* targets, twa_itype t_type, int64_t ignore_id, const float* lse,
                                 const float* entropy, const float* d_logp, const float* d_entropy, void* dlogits,

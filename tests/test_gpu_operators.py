@@ -669,6 +669,35 @@ def test_rows_beyond_2_31_elements(ctx):
     ok(ctx)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,cols", [(5, 7), (300, 1023), (40, 5000)])
+def test_what_lies_between_rows_does_not_count(ctx, dtype, rows, cols):
+    """NaN between the rows of every input gives what zeros there give, bit for bit."""
+    g = gen(rows)
+    xv, dv, t, w = randn(g, rows, cols), randn(g, rows, cols), torch.randint(0, cols, (rows,), generator=g, device=DEV), randn(g, cols)
+    ws = torch.empty(max(twa.twa_layer_norm_workspace_bytes(rows, cols), twa.twa_embedding_workspace_bytes(rows, rows, cols)),
+                     dtype=torch.uint8, device=DEV)
+    got = []
+    for fill in (0.0, math.nan):
+        x, dy = (strided(v, dtype, 3, 1, fill)[1] for v in (xv, dv))
+        y, dx, dz = (strided(torch.zeros_like(xv), dtype, 3, 1, fill)[1] for _ in range(3))
+        out = torch.empty(rows, cols, device=DEV)
+        mean, rstd, logp, lse, ent = (torch.empty(rows, device=DEV) for _ in range(5))
+        dw, db, grad = torch.empty(cols, device=DEV), torch.empty(cols, device=DEV), torch.empty(rows, cols, device=DEV)
+        ids, tlp = torch.empty(rows, 5, dtype=torch.int32, device=DEV), torch.empty(rows, 5, device=DEV)
+        twa.twa_layer_norm(ctx, x, w, None, 1e-5, y, mean, rstd)
+        twa.twa_layer_norm_backward(ctx, dy, x, w, mean, rstd, dx, dw, db, ws)
+        twa.twa_token_logprobs(ctx, x, t, logp, lse, entropy=ent, top_ids=ids, top_logp=tlp)
+        twa.twa_token_logprobs_backward(ctx, x, t, lse, lse, dz, entropy=ent, d_entropy=lse)
+        where = torch.arange(rows, device=DEV) // 2
+        twa.twa_embedding(ctx, x, where, 1.5, out)
+        twa.twa_embedding_backward(ctx, dy, where, 1.5, grad, ws)
+        got.append([a.clone() for a in (y, mean, rstd, dx, dw, db, logp, lse, ent, ids, tlp, dz, out, grad)])
+    for a, b in zip(*got):
+        assert torch.equal(a, b) and bool(torch.isfinite(a).all())
+    ok(ctx)
+
+
 # ------------------------------------------------------------------------------------------- gradient norm and clipping
 def gradients(g, sizes, kinds, shift):
     out = []
