@@ -9,7 +9,9 @@
 //
 // The tensors' addresses travel as kernel arguments (CLIP_TENSORS of them a launch), so a call uploads nothing.  They are
 // cut into chunks of at most CLIP_CHUNK elements; a block takes a run of chunks of equal length in either kernel.
-// 86.6 M float32 in 152 tensors: 195 us, 1.04 GB at 5.3 TB/s (59 us the norm); 1.32 G bfloat16 in 388: 1270 us, 7.9 GB at 6.2 TB/s.
+// 86.6 M float32 in 152 tensors: 195 us, 1.04 GB at 5.3 TB/s (60 us the norm); 1.32 G bfloat16 in 388: 1280 to 1306 us, 7.9 GB at
+// 6.1 TB/s; 400 M bfloat16 in 388 tensors of odd sizes, of which most lie on other boundaries than their place in the flat vector and
+// are scaled element by element: 527 us, 2.4 GB at 4.6 TB/s.
 // With chunks dealt out to the blocks in turn 700 small tensors take 72 us instead of 38; streaming stores change nothing.
 //
 // Squares are added in float32 over the elements of one load and in float64 beyond, in a fixed order.  Where that left float32, or a

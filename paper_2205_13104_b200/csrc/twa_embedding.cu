@@ -16,8 +16,10 @@
 // write zeros on the others, and the rest of them go beside the sums.  Up to 16384 ids a cluster of blocks sorts them in
 // its shared memory, in one launch; the zeros beside it go to rows whether used or not (the sums come later).
 //
-// Forward 2048 x 2048 out of a float32 table: 5.9 us, most of it the call.  Backward 16384 x 2048 bfloat16 into 50272 float32
-// rows: 81.6 us for 479 MB, 5.9 TB/s; 26 us the sort with its zeros, 47 the sums with the rest.
+// Forward 2048 x 2048 out of a float32 table: 6 us, most of it the call.  Backward 16384 x 2048 bfloat16 into 50272 float32
+// rows: 81.7 us for 479 MB, 5.9 TB/s; 26 us the sort with its zeros, 48 the sums with the rest.  Beyond 16384 ids a pass of the
+// sort adds the counts of all tiles in each tile, which grows with the square of the ids: 32768 ids 108 us (floor 83), 131072
+// 201 (145), 2^20 1266 (720).
 #include "twa_ops.cuh"
 
 namespace {

@@ -18,9 +18,10 @@
 // shared memory).  The partial sums of the blocks are added in float64 by a second kernel in block order, so results
 // repeat bit for bit.
 //
-// 16384 x 2048 bfloat16: 25.5 us forward (134 MB, 5.3 TB/s), 39.4 us backward (201 MB, 5.1 TB/s), of which the sum of the
+// 16384 x 2048 bfloat16: 25.7 us forward (134 MB, 5.2 TB/s), 40.5 us backward (201 MB, 5.0 TB/s), of which the sum of the
 // blocks' parts takes 5; 4099 x 1023 float32 on no 16-byte boundary 17.8 us backward (50 MB): 7 rows a block, bound by the latency
-// of a row and of the second launch.
+// of a row and of the second launch.  16384 x 1023 bfloat16 on none 49 us backward (floor 15: every unit carries the tests of a
+// row's ends, and only the next row is under way); 2048 x 12000 bfloat16 68 us (floor 22: one block an SM, no row under way).
 #include "twa_layer_norm.cuh"
 
 namespace {

@@ -22,9 +22,11 @@
 // maxima of its parts of the row (SLOTS of them): only the parts of those threads that reach T (some 1.5 k) are
 // looked at again, in L2, and the few elements of T or more are sorted by (value, smaller index first).
 //
-// 8192 x 50272 bfloat16 with entropy and 5 tokens: 162 us, 5.1 TB/s, bound by the sums' chains (issue slots 63 % in use, the unit
-// for exponentials 56 %, with 19 warps an SM); 333 x 32003 float32 with 20 tokens 18.8 us (43 MB): a little more than a row a
-// block, whose end nothing hides.  Backward 8192 x 50272: 265 us, 6.2 TB/s.
+// 8192 x 50272 bfloat16 with entropy and 5 tokens: 162 to 178 us (by the SM clock), 4.6 to 5.1 TB/s, bound by the sums' chains (issue
+// slots 63 % in use, the unit for exponentials 56 %, with 19 warps an SM); 333 x 32003 float32 with 20 tokens 19 us (43 MB): a
+// little more than a row a block, whose end nothing hides.  Where fewer groups than `top` have a token above -inf every
+// thread's parts are candidates, and a warp looks at the whole row again: 8192 rows with 20 tokens 174 us with 300 of 50272 tokens
+// allowed, 2980 us with 30.  Backward 8192 x 50272: 264 to 278 us, 5.9 to 6.2 TB/s.
 #include "twa_ops.cuh"
 
 namespace {
