@@ -509,6 +509,15 @@ typedef enum { TWA_I32 = 0, TWA_I64 = 1 } twa_itype; /* type of token numbers */
 #define TWA_LOGPROBS_MAX_VOCAB (1 << 24)
 #define TWA_LOGPROBS_MAX_TOP 32
 #define TWA_MAX_TENSORS 65536
+#define TWA_DROPOUT_MAX_ROWS (1 << 30)
+#define TWA_DROPOUT_MAX_COLS (1 << 24)
+#define TWA_SCAN_MAX_TOKENS (1LL << 36)
+#define TWA_SCAN_MAX_CHANNELS (1 << 20)
+#define TWA_SCAN_MAX_SEQUENCES (1 << 24)
+#define TWA_EXPERTS_MAX 1024
+#define TWA_EXPERTS_MAX_TOP 32
+#define TWA_EXPERTS_MAX_ASSIGNMENTS (1 << 28)
+#define TWA_EXPERTS_MAX_DIM (1 << 16)
 
 /* y = (x - mean) rstd w + b for every row, mean = sum x / cols, rstd = 1 / sqrt(sum (x - mean)^2 / cols + eps).
  *  x, y   rows x cols of dtype, row strides ldx, ldy; y may be x (with ldy == ldx).
@@ -590,6 +599,78 @@ int twa_clip_gather(twa_ctx* ctx, const twa_tensors* tensors, float max_norm, fl
 int twa_clip_grads(twa_ctx* ctx, const twa_tensors* tensors, float max_norm, float eps, float* norm, void* ws,
                    size_t ws_bytes);
 size_t twa_grad_norm_workspace_bytes(int count);
+
+/* Dropout whose mask is never stored: y = residual + m x with m = 65536 / (65536 - t) where u >= t and 0 where not,
+ * t = min(65535, p * 65536 rounded to even), so that the mean of m is 1 whatever p is rounded to.
+ *  x, y      rows x cols of dtype; residual the same, or NULL (0).  y may be x or residual (same row stride).
+ *  p         0 <= p < 1.
+ *  rng       two numbers on the DEVICE: a seed of 64 bits, and a step whose low 32 bits count.  A captured call
+ *            draws anew when the program changes the step before it replays.
+ *  site      0 .. 2^32 - 1: which of a model's dropouts this is.
+ * u, 16 bits for every element: counter (column / 8, row, site, step) and key (low, high half of the seed) give the four
+ * words of Philox4x32-10, and element `column` takes the half column % 2 (0 low) of word (column % 8) / 2: the same
+ * whatever type, strides and shape around the element are.
+ * What is dropped does not count, NaN and infinities included. */
+int twa_dropout(twa_ctx* ctx, const void* x, int64_t ldx, twa_dtype dtype, int64_t rows, int cols, float p,
+                const int64_t* rng, int64_t site, const void* residual, int64_t ldr, void* y, int64_t ldy);
+/* dx = m dy with the m of the call that had the same rng and site.  (The residual's gradient is dy itself.)
+ * dx may be dy. */
+int twa_dropout_backward(twa_ctx* ctx, const void* dy, int64_t lddy, twa_dtype dtype, int64_t rows, int cols, float p,
+                         const int64_t* rng, int64_t site, void* dx, int64_t lddx);
+
+/* Gated linear recurrence along every sequence, every channel alone:
+ *   a_t = sigmoid(f_t),   h_t = a_t h_{t-1} + (1 - a_t) x_t
+ *  x, f, h   tokens x channels of dtype; h may be x or f (same row stride).
+ *  starts    sequences + 1 numbers of s_type on the device: sequence s has the rows starts[s] .. starts[s+1]-1 (an
+ *            empty one: none; rows in no sequence are left as they were).  NULL: all of tokens / sequences rows.
+ *  h0        sequences x channels floats, the states before the first tokens, or NULL (0).
+ *  h_last    out: sequences x channels floats, the states after the last tokens, or NULL; may be h0.  One call a
+ *            token with both carries a sequence that is being generated.
+ *  states    out: what the backward call needs, twa_gated_scan_states_bytes(tokens, sequences, channels), 16-byte
+ *            aligned, or NULL.
+ * States are float32 throughout.  A value that is not finite spoils its own channel from its token to the sequence's end.
+ * Device-side error: TWA_ERR_INVALID_ARG, detail = a sequence whose starts go down or leave 0 .. tokens; it is left alone,
+ * and rows that starts give to two sequences are undefined. */
+int twa_gated_scan(twa_ctx* ctx, const void* x, int64_t ldx, const void* f, int64_t ldf, twa_dtype dtype, int64_t tokens,
+                   int channels, const void* starts, twa_itype s_type, int sequences, const float* h0, void* h, int64_t ldh,
+                   float* h_last, void* states, size_t states_bytes);
+/* With G_t = dh_t + a_{t+1} G_{t+1} (the last one dh_t + d_last):
+ *   dx_t = (1 - a_t) G_t,   df_t = a_t (1 - a_t) (h_{t-1} - x_t) G_t,   dh0 = a_1 G_1.
+ *  states    as the forward call with the same x, f, starts and h0 left them.
+ *  d_last    sequences x channels floats, the gradient of h_last, or NULL (0).
+ *  dx, df    tokens x channels of dtype; each may be one of dh, x, f (same row stride), not the same.
+ *  dh0       out: sequences x channels floats, or NULL; may be d_last. */
+int twa_gated_scan_backward(twa_ctx* ctx, const void* dh, int64_t lddh, const void* x, int64_t ldx, const void* f, int64_t ldf,
+                            twa_dtype dtype, int64_t tokens, int channels, const void* starts, twa_itype s_type, int sequences,
+                            const void* states, size_t states_bytes, const float* d_last, void* dx, int64_t lddx, void* df,
+                            int64_t lddf, float* dh0);
+size_t twa_gated_scan_states_bytes(int64_t tokens, int sequences, int channels);
+
+/* The assignments (t, j), j < top, of tokens to experts sorted by expert, equal ones by t and then j, and every
+ * token's row copied to its places:  out[place[t, j]] = x[t].
+ *  ids       tokens x top numbers of id_type; -1: no expert.
+ *  place     out: tokens x top, -1 where there is no expert.
+ *  starts    out: experts + 1 numbers; expert e has the rows starts[e] .. starts[e+1]-1.
+ *  order     out: the assignment t * top + j of every row, or NULL.
+ *  x, out    tokens x dim and tokens * top x dim of dtype, or both NULL (dim then still >= 1).
+ * Elements of order and rows of out from starts[experts] on are left as they were.
+ * Device-side error: TWA_ERR_INVALID_ARG, detail = a token with an id outside -1 .. experts-1, which counts as -1.
+ * The gradient of x is twa_expert_combine of out's gradient without weights. */
+int twa_expert_dispatch(twa_ctx* ctx, const void* x, int64_t ldx, twa_dtype dtype, int64_t tokens, int dim, const void* ids,
+                        twa_itype id_type, int top, int experts, int32_t* place, int32_t* starts, int32_t* order, void* out,
+                        int64_t ldo);
+/* out[t] = sum over j of weights[t, j] y[place[t, j]], added in the order of j in float32; a negative place adds nothing.
+ *  y, out    rows x dim and tokens x dim of dtype.    weights  tokens x top floats, or NULL (1).
+ * Device-side error: TWA_ERR_INVALID_ARG, detail = a token with a place that is not below rows; it adds nothing. */
+int twa_expert_combine(twa_ctx* ctx, const void* y, int64_t ldy, twa_dtype dtype, int64_t rows, const int32_t* place,
+                       const float* weights, int64_t tokens, int top, int dim, void* out, int64_t ldo);
+/* dy[place[t, j]] = weights[t, j] dout[t],   dw[t, j] = sum of dout[t] y[place[t, j]] (0 where the place is negative).
+ *  dy        rows x dim of dtype, no place twice; rows that no place names are left as they were.  May be y.
+ *  dw        tokens x top floats, or NULL.
+ * Device-side error as above. */
+int twa_expert_combine_backward(twa_ctx* ctx, const void* dout, int64_t lddout, const void* y, int64_t ldy, twa_dtype dtype,
+                                int64_t rows, const int32_t* place, const float* weights, int64_t tokens, int top, int dim,
+                                void* dy, int64_t lddy, float* dw);
 
 /* ---- projection without any allocation ----------------------------------------------- */
 

@@ -1,0 +1,207 @@
+// Dropout whose mask is never stored, and its gradient.
+//
+//   y = residual + [u >= t] x 65536 / (65536 - t),   t = round(65536 p)
+//
+// u are 16 bits of a counter-based generator, Philox4x32 with 10 rounds (Salmon, Moraes, Dror and Shaw, "Parallel random
+// numbers: as easy as 1, 2, 3", 2011): a round multiplies two words of the counter by constants and adds the key's halves, which
+// go up by constants from round to round.  The counter is (column / 8, row, site, step), the key the seed: a call's 128 bits
+// are the numbers of 8 neighbouring columns, and the backward pass draws them again from the same place.
+#include "twa_ops.cuh"
+
+namespace {
+
+constexpr int DROP_THREADS = 256;
+
+// n / d for n < 2^31: (n m) >> shift with m = ceil(2^shift / d), shift = 31 + ceil(log2 d).  m exceeds 2^shift / d by less than
+// one, the product by less than n / 2^31 2^-ceil(log2 d) <= 1 / d of the result, which does not reach the next integer.
+struct Divisor {
+  uint32_t d, m;
+  int shift;
+  explicit Divisor(uint32_t by) : d(by) {
+    int log = 0;
+    while ((1ULL << log) < d) ++log;
+    shift = 31 + log;
+    m = static_cast<uint32_t>(((1ULL << shift) + d - 1) / d);
+  }
+  __device__ __forceinline__ uint32_t divide(uint32_t n) const {
+    return static_cast<uint32_t>((static_cast<unsigned long long>(n) * m) >> shift);
+  }
+};
+
+struct DropArgs {
+  const void* x;
+  const void* residual;
+  void* y;
+  const unsigned long long* rng;     // seed, step
+  long long ldx, ldr, ldy;
+  unsigned rows, row0;               // of this launch, and the first one's number
+  int cols;
+  uint32_t site, threshold;          // threshold: t << 16
+  float scale;
+  Divisor parts;                     // of a row
+};
+
+struct Words {
+  uint32_t w[4];
+};
+__device__ __forceinline__ Words philox(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3, uint32_t k0, uint32_t k1) {
+#pragma unroll
+  for (int r = 0; r < 10; ++r) {
+    const unsigned long long p0 = static_cast<unsigned long long>(c0) * 0xD2511F53u, p1 = static_cast<unsigned long long>(c2) * 0xCD9E8D57u;
+    c0 = static_cast<uint32_t>(p1 >> 32) ^ c1 ^ k0;
+    c2 = static_cast<uint32_t>(p0 >> 32) ^ c3 ^ k1;
+    c1 = static_cast<uint32_t>(p1);
+    c3 = static_cast<uint32_t>(p0);
+    k0 += 0x9E3779B9u;
+    k1 += 0xBB67AE85u;
+  }
+  return {{c0, c1, c2, c3}};
+}
+// Whether element e of the eight is kept.
+__device__ __forceinline__ bool drop_keeps(const Words& u, int e, uint32_t threshold) {
+  return (e & 1 ? u.w[e >> 1] : u.w[e >> 1] << 16) >= threshold;
+}
+
+// Eight columns a unit, on 16-byte boundaries; DROP_UNITS units a thread.  The generator needs nothing from memory but the
+// seed, so it runs while the loads are under way.
+constexpr int DROP_UNITS = 2;
+template <typename T, bool RESIDUAL>
+__global__ void __launch_bounds__(DROP_THREADS) dropout_kernel(DropArgs a) {
+  twa_begin(a.x, a.residual, a.rng);
+  constexpr int V = twa_vec<T>, N = 8 / V;
+  const T* x = static_cast<const T*>(a.x);
+  const T* res = static_cast<const T*>(a.residual);
+  T* y = static_cast<T*>(a.y);
+  const unsigned long long seed = __ldg(a.rng), step = __ldg(a.rng + 1);
+  const unsigned total = a.rows * a.parts.d;
+  const unsigned first = blockIdx.x * (DROP_THREADS * DROP_UNITS) + threadIdx.x;
+  twa_pack<T, V> raw[DROP_UNITS][N], add[DROP_UNITS][N];
+  unsigned row[DROP_UNITS], unit[DROP_UNITS];
+#pragma unroll
+  for (int k = 0; k < DROP_UNITS; ++k) {
+    const unsigned n = first + k * DROP_THREADS;
+    row[k] = a.parts.divide(n);
+    unit[k] = n - row[k] * a.parts.d;
+    if (n >= total) continue;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      raw[k][i].load(x + row[k] * a.ldx + unit[k] * 8 + i * V);
+      if (RESIDUAL) add[k][i].load(res + row[k] * a.ldr + unit[k] * 8 + i * V);
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < DROP_UNITS; ++k) {
+    if (first + k * DROP_THREADS >= total) return;
+    const Words u = philox(unit[k], a.row0 + row[k], a.site, static_cast<uint32_t>(step), static_cast<uint32_t>(seed),
+                           static_cast<uint32_t>(seed >> 32));
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      float v[V], r[V];
+      raw[k][i].widen(v);
+      if (RESIDUAL) add[k][i].widen(r);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const float kept = RESIDUAL ? fmaf(v[e], a.scale, r[e]) : v[e] * a.scale;
+        v[e] = drop_keeps(u, i * V + e, a.threshold) ? kept : (RESIDUAL ? r[e] : 0.0f);
+      }
+      twa_pack<T, V>::store(y + row[k] * a.ldy + unit[k] * 8 + i * V, v);
+    }
+  }
+}
+
+// Rows on any boundary: a warp takes 256 columns.  Each lane draws the numbers of eight neighbouring columns and keeps one bit
+// of each; elements go by lane, so that accesses are contiguous, and find their bit in another lane.
+template <typename T, bool RESIDUAL>
+__global__ void __launch_bounds__(DROP_THREADS) dropout_any_kernel(DropArgs a) {
+  twa_begin(a.x, a.residual, a.rng);
+  const T* x = static_cast<const T*>(a.x);
+  const T* res = static_cast<const T*>(a.residual);
+  T* y = static_cast<T*>(a.y);
+  const unsigned task = blockIdx.x * (DROP_THREADS / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (task >= a.rows * a.parts.d) return;
+  const unsigned row = a.parts.divide(task), part = task - row * a.parts.d;
+  const int c0 = part * 256 + lane;
+  twa_pack<T, 1> raw[8], add[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k)
+    if (c0 + k * 32 < a.cols) {
+      raw[k].load(x + row * a.ldx + c0 + k * 32);
+      if (RESIDUAL) add[k].load(res + row * a.ldr + c0 + k * 32);
+    }
+  const unsigned long long seed = __ldg(a.rng), step = __ldg(a.rng + 1);
+  const Words u = philox(part * 32 + lane, a.row0 + row, a.site, static_cast<uint32_t>(step), static_cast<uint32_t>(seed),
+                         static_cast<uint32_t>(seed >> 32));
+  unsigned bits = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) bits |= (drop_keeps(u, e, a.threshold) ? 1u : 0u) << e;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const bool keep = __shfl_sync(0xffffffffu, bits, 4 * k + (lane >> 3)) >> (lane & 7) & 1;
+    if (c0 + k * 32 >= a.cols) continue;
+    float v, r = 0.0f;
+    raw[k].widen(&v);
+    if (RESIDUAL) add[k].widen(&r);
+    y[row * a.ldy + c0 + k * 32] = twa_from_float<T>(keep ? fmaf(v, a.scale, r) : r);
+  }
+}
+
+bool drop_packs(const void* p, long long ld, size_t size) { return !twa_misaligned_to(p, 16) && ld * size % 16 == 0; }
+
+template <typename T>
+void drop_launch(twa_ctx* ctx, DropArgs a, int64_t rows) {
+  const size_t size = sizeof(T);
+  const bool packs = a.cols % 8 == 0 && drop_packs(a.x, a.ldx, size) && drop_packs(a.y, a.ldy, size) &&
+                     (!a.residual || drop_packs(a.residual, a.ldr, size));
+  a.parts = Divisor(static_cast<uint32_t>(packs ? a.cols / 8 : twa_ceil_div(a.cols, 256)));
+  // tasks of a launch are counted in 31 bits
+  const long long most = ((1LL << 31) - DROP_THREADS * DROP_UNITS) / a.parts.d;
+  for (long long r = 0; r < rows; r += most) {
+    a.row0 = static_cast<unsigned>(r);
+    a.rows = static_cast<unsigned>(rows - r < most ? rows - r : most);
+    const long long tasks = static_cast<long long>(a.rows) * a.parts.d;
+    if (packs) {
+      const unsigned blocks = static_cast<unsigned>(twa_ceil_div(tasks, DROP_THREADS * DROP_UNITS));
+      if (a.residual) twa_launch(ctx->stream, dropout_kernel<T, true>, blocks, DROP_THREADS, 0, a);
+      else twa_launch(ctx->stream, dropout_kernel<T, false>, blocks, DROP_THREADS, 0, a);
+    } else {
+      const unsigned blocks = static_cast<unsigned>(twa_ceil_div(tasks, DROP_THREADS / 32));
+      if (a.residual) twa_launch(ctx->stream, dropout_any_kernel<T, true>, blocks, DROP_THREADS, 0, a);
+      else twa_launch(ctx->stream, dropout_any_kernel<T, false>, blocks, DROP_THREADS, 0, a);
+    }
+    a.x = static_cast<const T*>(a.x) + most * a.ldx;
+    a.y = static_cast<T*>(a.y) + most * a.ldy;
+    if (a.residual) a.residual = static_cast<const T*>(a.residual) + most * a.ldr;
+  }
+}
+
+}  // namespace
+
+extern "C" {
+
+int twa_dropout(twa_ctx* ctx, const void* x, int64_t ldx, twa_dtype dtype, int64_t rows, int cols, float p, const int64_t* rng,
+                int64_t site, const void* residual, int64_t ldr, void* y, int64_t ldy) {
+  if (!ctx || !twa_dtype_ok(dtype) || rows < 0 || cols < 1 || !(p >= 0.0f && p < 1.0f)) return TWA_ERR_INVALID_ARG;
+  if (site < 0 || site > 0xFFFFFFFFLL) return TWA_ERR_INVALID_ARG;
+  if (rows > TWA_DROPOUT_MAX_ROWS || cols > TWA_DROPOUT_MAX_COLS) return TWA_ERR_UNSUPPORTED;
+  if (rows == 0) return TWA_OK;
+  if (!x || !y || !rng || ldx < cols || ldy < cols || (residual && ldr < cols)) return TWA_ERR_INVALID_ARG;
+  const size_t size = twa_dtype_size(dtype);
+  if (twa_misaligned_to(x, size) || twa_misaligned_to(y, size) || twa_misaligned_to(residual, size) || twa_misaligned_to(rng, 8))
+    return TWA_ERR_MISALIGNED;
+  TWA_CUDA_OK(ctx, cudaSetDevice(ctx->device));
+  int t = static_cast<int>(rint(static_cast<double>(p) * 65536.0));
+  if (t > 65535) t = 65535;
+  DropArgs a = {x, residual, y, reinterpret_cast<const unsigned long long*>(rng), ldx, ldr, ldy, 0, 0, cols, static_cast<uint32_t>(site),
+                static_cast<uint32_t>(t) << 16, static_cast<float>(65536.0 / (65536 - t)), Divisor(1)};
+  if (dtype == TWA_BF16) drop_launch<bf16>(ctx, a, rows);
+  else drop_launch<float>(ctx, a, rows);
+  TWA_CUDA_OK(ctx, cudaGetLastError());
+  return TWA_OK;
+}
+
+int twa_dropout_backward(twa_ctx* ctx, const void* dy, int64_t lddy, twa_dtype dtype, int64_t rows, int cols, float p, const int64_t* rng,
+                         int64_t site, void* dx, int64_t lddx) {
+  return twa_dropout(ctx, dy, lddy, dtype, rows, cols, p, rng, site, nullptr, 0, dx, lddx);
+}
+
+}  // extern "C"

@@ -17,7 +17,8 @@ _ROOT = os.path.dirname(_HERE)
 LIB_PATH = os.path.join(_HERE, "libtwa.so")
 CSRC = os.path.join(_HERE, "csrc")
 SOURCES = ["twa_api.cu", "twa_basis.cu", "twa_chunked.cu", "twa_layered_build.cu", "twa_layered_step.cu", "twa_project_batch.cu", "twa_panel.cu", "twa_stream.cu",
-           "twa_stream_mma.cu", "twa_noalloc.cu", "twa_layer_norm.cu", "twa_layer_norm_backward.cu", "twa_embedding.cu", "twa_logprobs.cu", "twa_clip.cu"]
+           "twa_stream_mma.cu", "twa_noalloc.cu", "twa_layer_norm.cu", "twa_layer_norm_backward.cu", "twa_embedding.cu", "twa_logprobs.cu", "twa_clip.cu", "twa_dropout.cu",
+           "twa_scan.cu", "twa_experts.cu"]
 
 TWA_MAX_N = 128
 TWA_OK = 0
@@ -41,6 +42,15 @@ TWA_LOGPROBS_MAX_ROWS = 1 << 24
 TWA_LOGPROBS_MAX_VOCAB = 1 << 24
 TWA_LOGPROBS_MAX_TOP = 32
 TWA_MAX_TENSORS = 65536
+TWA_DROPOUT_MAX_ROWS = 1 << 30
+TWA_DROPOUT_MAX_COLS = 1 << 24
+TWA_SCAN_MAX_TOKENS = 1 << 36
+TWA_SCAN_MAX_CHANNELS = 1 << 20
+TWA_SCAN_MAX_SEQUENCES = 1 << 24
+TWA_EXPERTS_MAX = 1024
+TWA_EXPERTS_MAX_TOP = 32
+TWA_EXPERTS_MAX_ASSIGNMENTS = 1 << 28
+TWA_EXPERTS_MAX_DIM = 1 << 16
 TWA_TUNE_PROJECT_WARPS = 1
 TWA_TUNE_LIFT_WARPS = 2
 TWA_TUNE_STAGES = 3
@@ -66,6 +76,8 @@ EXPORTS = [
     "twa_layer_norm", "twa_layer_norm_backward", "twa_layer_norm_workspace_bytes", "twa_embedding", "twa_embedding_backward",
     "twa_embedding_workspace_bytes", "twa_token_logprobs", "twa_token_logprobs_backward", "twa_grad_norm", "twa_clip_gather",
     "twa_clip_grads", "twa_grad_norm_workspace_bytes",
+    "twa_dropout", "twa_dropout_backward", "twa_gated_scan", "twa_gated_scan_backward", "twa_gated_scan_states_bytes",
+    "twa_expert_dispatch", "twa_expert_combine", "twa_expert_combine_backward",
 ]
 
 
@@ -243,6 +255,14 @@ def load():
         "twa_clip_gather": (i32, [vp, ctypes.POINTER(twa_tensors), f32, f32, vp, i32, vp, vp, szt]),
         "twa_clip_grads": (i32, [vp, ctypes.POINTER(twa_tensors), f32, f32, vp, vp, szt]),
         "twa_grad_norm_workspace_bytes": (szt, [i32]),
+        "twa_dropout": (i32, [vp, vp, i64, i32, i64, i32, f32, vp, i64, vp, i64, vp, i64]),
+        "twa_dropout_backward": (i32, [vp, vp, i64, i32, i64, i32, f32, vp, i64, vp, i64]),
+        "twa_gated_scan": (i32, [vp, vp, i64, vp, i64, i32, i64, i32, vp, i32, i32, vp, vp, i64, vp, vp, szt]),
+        "twa_gated_scan_backward": (i32, [vp, vp, i64, vp, i64, vp, i64, i32, i64, i32, vp, i32, i32, vp, szt, vp, vp, i64, vp, i64, vp]),
+        "twa_gated_scan_states_bytes": (szt, [i64, i32, i32]),
+        "twa_expert_dispatch": (i32, [vp, vp, i64, i32, i64, i32, vp, i32, i32, i32, vp, vp, vp, vp, i64]),
+        "twa_expert_combine": (i32, [vp, vp, i64, i32, i64, vp, vp, i64, i32, i32, vp, i64]),
+        "twa_expert_combine_backward": (i32, [vp, vp, i64, vp, i64, i32, i64, vp, vp, i64, i32, i32, vp, i64, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -980,3 +1000,142 @@ def twa_clip_grads(ctx, tensors, max_norm, norm, ws, eps=1e-6):
     if rc:
         _check(rc, "twa_clip_grads", ctx)
     return norm
+
+
+def _rng(rng, dev):
+    """Address of a generator's seed and step."""
+    if rng.dtype is not torch.int64 or rng.shape != (2,) or not rng.is_contiguous() or rng.get_device() != dev:
+        raise ValueError(f"rng: two contiguous int64 (seed, step) on the context's device are needed, got {tuple(rng.shape)} of {rng.dtype} "
+                         f"on {rng.device}")
+    return rng.data_ptr()
+
+
+def twa_dropout(ctx, x, p, rng, site, y, residual=None):
+    """x, y, residual: (rows, cols); rng: (2,) int64 on the device, seed and step; site: which of a model's dropouts this is."""
+    dt, shape = _floats(x, "x"), x.shape
+    dev = ctx.device
+    res, ldr = (None, 0) if residual is None else (residual.data_ptr(), _rows(residual, shape, "residual", dev, x.dtype))
+    rc = load().twa_dropout(ctx, x.data_ptr(), _rows(x, shape, "x", dev), dt, shape[0], shape[1], p, _rng(rng, dev), site, res, ldr,
+                            y.data_ptr(), _rows(y, shape, "y", dev, x.dtype))
+    if rc:
+        _check(rc, "twa_dropout", ctx)
+    return y
+
+
+def twa_dropout_backward(ctx, dy, p, rng, site, dx):
+    """dx of the call with the same rng and site; the residual's gradient is dy."""
+    dt, shape = _floats(dy, "dy"), dy.shape
+    dev = ctx.device
+    rc = load().twa_dropout_backward(ctx, dy.data_ptr(), _rows(dy, shape, "dy", dev), dt, shape[0], shape[1], p, _rng(rng, dev), site,
+                                     dx.data_ptr(), _rows(dx, shape, "dx", dev, dy.dtype))
+    if rc:
+        _check(rc, "twa_dropout_backward", ctx)
+    return dx
+
+
+def twa_gated_scan_states_bytes(tokens, sequences, channels):
+    return int(load().twa_gated_scan_states_bytes(int(tokens), int(sequences), int(channels)))
+
+
+def _starts(starts, sequences, dev):
+    """Address and type of the sequences' offsets."""
+    if starts is None:
+        return None, TWA_I32
+    code = _numbers(starts, sequences + 1, "starts", dev)
+    return starts.data_ptr(), code
+
+
+def twa_gated_scan(ctx, x, f, h, starts=None, sequences=1, h0=None, h_last=None, states=None):
+    """x, f, h: (tokens, channels); starts: (sequences + 1,) int32 or int64 on the device, or None (equal lengths); h0, h_last:
+    (sequences, channels) float32 or None; states: for the backward call, a tensor of twa_gated_scan_states_bytes bytes, or None."""
+    dt, shape = _floats(x, "x"), x.shape
+    dev = ctx.device
+    tokens, channels = shape
+    count = sequences * channels
+    rc = load().twa_gated_scan(ctx, x.data_ptr(), _rows(x, shape, "x", dev), f.data_ptr(), _rows(f, shape, "f", dev, x.dtype), dt, tokens,
+                               channels, *_starts(starts, sequences, dev), sequences, _vector(h0, count, torch.float32, "h0", dev),
+                               h.data_ptr(), _rows(h, shape, "h", dev, x.dtype), _vector(h_last, count, torch.float32, "h_last", dev),
+                               *_space(states, dev))
+    if rc:
+        _check(rc, "twa_gated_scan", ctx)
+    return h
+
+
+def twa_gated_scan_backward(ctx, dh, x, f, states, dx, df, starts=None, sequences=1, d_last=None, dh0=None):
+    """states: as the forward call left them; d_last, dh0: (sequences, channels) float32 or None."""
+    dt, shape = _floats(x, "x"), x.shape
+    dev = ctx.device
+    tokens, channels = shape
+    count = sequences * channels
+
+    def at(t, what):
+        return t.data_ptr(), _rows(t, shape, what, dev, x.dtype)
+
+    rc = load().twa_gated_scan_backward(
+        ctx, *at(dh, "dh"), *at(x, "x"), *at(f, "f"), dt, tokens, channels, *_starts(starts, sequences, dev), sequences, *_space(states, dev),
+        _vector(d_last, count, torch.float32, "d_last", dev), *at(dx, "dx"), *at(df, "df"), _vector(dh0, count, torch.float32, "dh0", dev))
+    if rc:
+        _check(rc, "twa_gated_scan_backward", ctx)
+    return dx
+
+
+def _places(place, dev):
+    """Tokens and top of a matrix of places."""
+    if place.dim() != 2 or place.dtype is not torch.int32 or not place.is_contiguous() or place.get_device() != dev:
+        raise ValueError(f"place: a contiguous (tokens, top) matrix of int32 on the context's device is needed, got {tuple(place.shape)} of "
+                         f"{place.dtype} on {place.device}")
+    return place.shape
+
+
+def twa_expert_dispatch(ctx, x, ids, experts, place, starts, out, order=None):
+    """x: (tokens, dim); ids: (tokens, top) int32 or int64, -1 for none; place: (tokens, top) int32; starts: (experts + 1,) int32;
+    out: (tokens * top or more, dim); order: (tokens * top,) int32, or None.  x and out may both be None: places only."""
+    dev = ctx.device
+    tokens, top = _places(place, dev)
+    if ids.shape != place.shape:
+        raise ValueError(f"ids: a (tokens, top) matrix as place is needed, got {tuple(ids.shape)} and {tuple(place.shape)}")
+    code = _numbers(ids, tokens * top, "ids", dev)
+    if (x is None) != (out is None):
+        raise ValueError("x and out: both or neither")
+    rows, dim, dt = (None, 0), 1, TWA_F32
+    to = (None, 0)
+    if x is not None:
+        dt, dim = _floats(x, "x"), x.shape[1]
+        rows = x.data_ptr(), _rows(x, (tokens, dim), "x", dev)
+        if len(out) < tokens * top:
+            raise ValueError(f"out: at least {tokens * top} rows are needed, got {len(out)}")
+        to = out.data_ptr(), _rows(out, (len(out), dim), "out", dev, x.dtype)
+    rc = load().twa_expert_dispatch(ctx, *rows, dt, tokens, dim, ids.data_ptr(), code, top, experts, place.data_ptr(),
+                                    _vector(starts, experts + 1, torch.int32, "starts", dev),
+                                    _vector(order, tokens * top, torch.int32, "order", dev), *to)
+    if rc:
+        _check(rc, "twa_expert_dispatch", ctx)
+    return out
+
+
+def twa_expert_combine(ctx, y, place, weights, out):
+    """y: (rows, dim); place: (tokens, top) int32; weights: (tokens, top) float32, or None; out: (tokens, dim)."""
+    dt, shape = _floats(y, "y"), y.shape
+    dev = ctx.device
+    tokens, top = _places(place, dev)
+    rc = load().twa_expert_combine(ctx, y.data_ptr(), _rows(y, shape, "y", dev), dt, shape[0], place.data_ptr(),
+                                   _vector(weights, tokens * top, torch.float32, "weights", dev), tokens, top, shape[1], out.data_ptr(),
+                                   _rows(out, (tokens, shape[1]), "out", dev, y.dtype))
+    if rc:
+        _check(rc, "twa_expert_combine", ctx)
+    return out
+
+
+def twa_expert_combine_backward(ctx, dout, y, place, weights, dy, dw=None):
+    """dout: (tokens, dim); y, dy: (rows, dim); weights, dw: (tokens, top) float32; dw may be None."""
+    dt, shape = _floats(y, "y"), y.shape
+    dev = ctx.device
+    tokens, top = _places(place, dev)
+    rc = load().twa_expert_combine_backward(ctx, dout.data_ptr(), _rows(dout, (tokens, shape[1]), "dout", dev, y.dtype), y.data_ptr(),
+                                            _rows(y, shape, "y", dev), dt, shape[0], place.data_ptr(),
+                                            _vector(weights, tokens * top, torch.float32, "weights", dev), tokens, top, shape[1],
+                                            dy.data_ptr(), _rows(dy, shape, "dy", dev, y.dtype),
+                                            _vector(dw, tokens * top, torch.float32, "dw", dev))
+    if rc:
+        _check(rc, "twa_expert_combine_backward", ctx)
+    return dy
