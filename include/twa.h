@@ -511,7 +511,7 @@ typedef enum { TWA_I32 = 0, TWA_I64 = 1 } twa_itype; /* type of token numbers */
 #define TWA_MAX_TENSORS 65536
 #define TWA_DROPOUT_MAX_ROWS (1 << 30)
 #define TWA_DROPOUT_MAX_COLS (1 << 24)
-#define TWA_SCAN_MAX_TOKENS (1LL << 36)
+#define TWA_SCAN_MAX_TOKENS (1 << 30)
 #define TWA_SCAN_MAX_CHANNELS (1 << 20)
 #define TWA_SCAN_MAX_SEQUENCES (1 << 24)
 #define TWA_EXPERTS_MAX 1024

@@ -3,81 +3,84 @@
 //   forward    h_t = a_t h_{t-1} + (1 - a_t) x_t,   a_t = sigmoid(f_t)
 //   backward   G_t = dh_t + a_{t+1} G_{t+1},   dx_t = (1 - a_t) G_t,   df_t = a_t (1 - a_t) (h_{t-1} - x_t) G_t
 //
-// Backward the states before every row are taken again from those that the forward pass kept in float32, one every 64 rows, and
-// what goes from row to row is k_t = a_t G_t, affine in the one that enters: k = A k_in + M with the same A as forward.
+// Backward the states before every row are taken again from those that the forward pass kept in float32, one a segment.  What goes
+// from row to row is k_t = a_t G_t, affine in the one that enters a segment from behind: k = A k_in + M with the same A as forward
+// and M = sum over its rows of A_t dh_t, A_t the product of the gates up to t: both directions of a segment are taken in one pass.
 #include "twa_scan.cuh"
 
 namespace {
 
-// Maps of the segments of a tile, and of the tiles of a cluster's blocks: twice, so that the next ones go beside those being read.
-template <int MAPS>
+// Affine maps v -> A v + B of two channels.
+struct __align__(16) Map {
+  twa_f2 A, B;
+  __device__ __forceinline__ twa_f2 of(twa_f2 v) const { return twa_fma2(A, v, B); }
+};
+
+// What the segments of a tile make of what enters them (the state, or backward k), and what enters the next tile: twice, so that the
+// next ones go beside those being read.
 struct Joins {
-  twa_f2 seg[2][SCAN_WARPS][MAPS][32], tile[2][MAX_CLUSTER][MAPS][32];
+  Map seg[2][SCAN_WARPS][32];
+  twa_f2 carry[2][32];
+};
+// The same of the tiles of a cluster's blocks.
+struct Tiles {
+  Map tile[2][MAX_CLUSTER][32];
 };
 
-// Where a thread stands: its lane's channels c and c + 1, of which n exist, and its block's rank along the sequence.
-struct Place {
-  int lane, warp, c, n, rank, ranks;
-  __device__ __forceinline__ Place(const ScanArgs& a, int slice) {
-    lane = threadIdx.x & 31;
-    warp = threadIdx.x >> 5;
-    c = slice * SCAN_CHANNELS + 2 * lane;
-    const int left = a.channels - c;
-    n = left < 0 ? 0 : (left < 2 ? left : 2);
-    ranks = a.cluster;
-    rank = ranks > 1 ? static_cast<int>(twa_cluster_rank()) : 0;
-  }
-};
-
-// The blocks of a cluster tell each other what their tiles make of a state: every block's warp 0 joins its segments' maps and
-// stores the tile's into every block.  FORWARD: segments in their order, otherwise from the last.  A map is (A, B): v -> A v + B; the
-// B is the last of the MAPS that a segment leaves.
-template <bool FORWARD, int MAPS>
-__device__ __forceinline__ void share_tile(Joins<MAPS>& joins, const Place& at, int turn) {
-  if (at.warp == 0) {
-    twa_f2 A = twa_pair(1.0f), B = 0;
+// The blocks of a cluster tell each other what their tiles make of a state: every warp joins its block's segments' maps, from the
+// first on (FORWARD) or from the last, and the warp of each rank stores the tile's into that block.
+template <bool FORWARD, int FEED>
+__device__ __forceinline__ void share_tile(const Joins& joins, Tiles& tiles, const Place<FEED>& at, int turn) {
+  if (at.warp < at.ranks) {
+    Map all = joins.seg[turn][FORWARD ? 0 : SCAN_WARPS - 1][at.lane];
 #pragma unroll
-    for (int i = 0; i < SCAN_WARPS; ++i) {
-      const int w = FORWARD ? i : SCAN_WARPS - 1 - i;
-      const twa_f2 m = joins.seg[turn][w][0][at.lane];
-      A = twa_mul2(m, A);
-      B = twa_fma2(m, B, joins.seg[turn][w][MAPS - 1][at.lane]);
+    for (int i = 1; i < SCAN_WARPS; ++i) {
+      const Map m = joins.seg[turn][FORWARD ? i : SCAN_WARPS - 1 - i][at.lane];
+      all.A = twa_mul2(m.A, all.A);
+      all.B = m.of(all.B);
     }
-    for (int r = 0; r < at.ranks; ++r) {
-      twa_store_remote(&joins.tile[turn][at.rank][0][at.lane], r, A);
-      twa_store_remote(&joins.tile[turn][at.rank][1][at.lane], r, B);
-    }
+    twa_store_remote(&tiles.tile[turn][at.rank][at.lane].A, at.warp, all.A);
+    twa_store_remote(&tiles.tile[turn][at.rank][at.lane].B, at.warp, all.B);
   }
   twa_cluster_sync();
 }
+static_assert(MAX_CLUSTER <= SCAN_WARPS, "a warp for every rank");
 
 template <typename T, int FEED>
 struct ScanForward {
-  static constexpr int MAPS = 2, STAGES = FEED == BY_ELEMENTS ? 1 : (sizeof(T) == 2 ? 4 : 3);
-  static constexpr bool PACKED = FEED != BY_ELEMENTS;
+  static constexpr int STAGES = 3;
+  static constexpr bool TOGETHER = FEED != BY_ELEMENTS;
+  static constexpr int N = SEG<T>;
   typedef Ring<T, FEED, 2, STAGES> Rows;
   const ScanArgs& a;
-  const Place at;
-  twa_f2 A[SEG], L[SEG];                           // of the rows up to each
+  const Place<FEED> at;
+  twa_f2 A[N], L[N];                               // of the rows up to each
 
   __device__ __forceinline__ ScanForward(const ScanArgs& args, int slice) : a(args), at(args, slice) {}
 
-  __device__ __forceinline__ void row(int i, const Pair<T>& x, const Pair<T>& f, twa_f2& s, twa_f2& l) {
+  __device__ __forceinline__ void row(int i, const Pair<T>& x, const Pair<T>& f) {
     const twa_f2 n = scan_gate<T>(f);
-    s = scan_decay(n, s);
-    l = scan_step(n, l, x.both());
-    A[i] = s;
-    L[i] = l;
+    A[i] = i ? scan_decay(n, A[i - 1]) : scan_decay(n, twa_pair(1.0f));
+    L[i] = i ? scan_step(n, L[i - 1], x.both()) : scan_step(n, 0, x.both());
   }
   __device__ __forceinline__ void store(long long first, int rows, twa_f2 in) {
     T* h = static_cast<T*>(a.h) + first * a.ldh + at.c;
 #pragma unroll
-    for (int i = 0; i < SEG; ++i)
+    for (int i = 0; i < N; ++i) {
       if (i < rows && at.n > 0) {
         float lo, hi;
         twa_unpair(twa_fma2(A[i], in, L[i]), lo, hi);
-        Pair<T>::template store<PACKED>(h + i * a.ldh, lo, hi, at.n);
+        Pair<T>::template store<TOGETHER>(h, lo, hi, at.n);
       }
+      h += a.ldh;
+    }
+  }
+  __device__ __forceinline__ Map last(int rows) const {
+    Map m = {twa_pair(1.0f), 0};
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (i < rows) m = {A[i], L[i]};
+    return m;
   }
 
   // A sequence of at most SEG rows, by one warp.
@@ -85,108 +88,155 @@ struct ScanForward {
     const int rows = static_cast<int>(s.len);
     const T* x = static_cast<const T*>(a.x) + s.begin * a.ldx + at.c;
     const T* f = static_cast<const T*>(a.f) + s.begin * a.ldf + at.c;
-    Pair<T> rx[SEG], rf[SEG];
+    Pair<T> rx[N], rf[N];
 #pragma unroll
-    for (int i = 0; i < SEG; ++i)
+    for (int i = 0; i < N; ++i)
       if (i < rows && at.n > 0) {
-        rx[i].template load<PACKED>(x + i * a.ldx, at.n);
-        rf[i].template load<PACKED>(f + i * a.ldf, at.n);
+        rx[i].template load<TOGETHER>(x + i * a.ldx, at.n);
+        rf[i].template load<TOGETHER>(f + i * a.ldf, at.n);
       }
-    const twa_f2 in = scan_state(a.h0, seq, a.channels, at.c, at.n);
-    if (rows) scan_keep(a.states, scan_slot(s, seq), a.channels, at.c, at.n, in);
-    twa_f2 A1 = twa_pair(1.0f), L1 = 0;
+    const twa_f2 in = at.state(a.h0, seq, a.channels);
+    if (rows) keep_state(at, a.states, scan_slot<T>(s, seq), a.channels, in);
 #pragma unroll
-    for (int i = 0; i < SEG; ++i)
-      if (i < rows) row(i, rx[i], rf[i], A1, L1);
+    for (int i = 0; i < N; ++i)
+      if (i < rows) row(i, rx[i], rf[i]);
     store(s.begin, rows, in);
-    scan_keep(a.h_last, seq, a.channels, at.c, at.n, twa_fma2(A1, in, L1));
+    at.keep(a.h_last, seq, a.channels, last(rows).of(in));
   }
 
+  __device__ __forceinline__ void copy(Rows& ring, int array, const T* from, const void* all, long long ld, int rows, int left) {
+    const T* first = static_cast<const T*>(all);
+    ring.copy(array, from, ld, rows, left, first, first + (a.tokens - 1) * ld + a.channels - 1);
+  }
   // A sequence by the whole cluster.
-  __device__ __forceinline__ void whole(const Span& s, int seq, char* shared, Joins<MAPS>& joins, int& turn) {
-    Rows ring(shared, at.warp);
-    const long long stride = static_cast<long long>(SCAN_ROWS) * at.ranks;
-    const int left = a.channels - (at.c - 2 * at.lane);                   // channels from this slice's first on
-    long long ahead = at.rank * SCAN_ROWS + at.warp * SEG;                // row of the next segment to be fetched
-    auto rows_at = [&](long long r) { return static_cast<int>(s.len - r < SEG ? (s.len - r < 0 ? 0 : s.len - r) : SEG); };
+  __device__ __forceinline__ void whole(const Span& s, int seq, char* shared, Joins& joins, Tiles& tiles, int& turn) {
+    Rows ring(shared, at.warp, at.lane);
+    const int stride = SCAN_ROWS<T> * at.ranks, left = a.channels - at.slice;
+    const bool wide = __all_sync(0xffffffffu, at.n == 2);
+    int ahead = at.rank * SCAN_ROWS<T> + at.warp * N;                     // row of the next segment to be fetched
+    ring.lies(0, static_cast<const T*>(a.x) + (s.begin + ahead) * a.ldx + at.slice, a.ldx);
+    ring.lies(1, static_cast<const T*>(a.f) + (s.begin + ahead) * a.ldf + at.slice, a.ldf);
+    const T* x = Rows::own(static_cast<const T*>(a.x) + (s.begin + ahead) * a.ldx + at.slice, a.ldx);
+    const T* f = Rows::own(static_cast<const T*>(a.f) + (s.begin + ahead) * a.ldf + at.slice, a.ldf);
+    T* h = Rows::own(static_cast<T*>(a.h) + (s.begin + ahead) * a.ldh + at.slice, a.ldh);
     auto fetch = [&]() {
-      const int rows = rows_at(ahead);
+      const int rows = scan_rows<T>(s, ahead);
       if (rows) {
-        ring.copy(0, static_cast<const T*>(a.x) + (s.begin + ahead) * a.ldx + (at.c - 2 * at.lane), a.ldx, rows, left);
-        ring.copy(1, static_cast<const T*>(a.f) + (s.begin + ahead) * a.ldf + (at.c - 2 * at.lane), a.ldf, rows, left);
+        copy(ring, 0, x, a.x, a.ldx, rows, left);
+        copy(ring, 1, f, a.f, a.ldf, rows, left);
       }
       ring.filled();
       ahead += stride;
+      x += stride * a.ldx;
+      f += stride * a.ldf;
     };
 #pragma unroll
     for (int i = 0; i < Rows::AHEAD; ++i) fetch();
-    twa_f2 state = scan_state(a.h0, seq, a.channels, at.c, at.n);
-    long long slot = scan_slot(s, seq) + at.rank;
-    for (long long t = at.rank * SCAN_ROWS; t - at.rank * SCAN_ROWS < s.len; t += stride, slot += at.ranks) {
-      const long long mine = t + at.warp * SEG;
-      const int rows = rows_at(mine);
+    twa_f2 state = at.state(a.h0, seq, a.channels);
+    if (at.warp == SCAN_WARPS - 1) joins.carry[turn ^ 1][at.lane] = state;
+    int slot = scan_slot<T>(s, seq) + at.rank * SCAN_WARPS + at.warp;
+    for (int t = 0; t < s.len; t += stride, slot += at.ranks * SCAN_WARPS, h += stride * a.ldh) {
+      const int mine = t + at.rank * SCAN_ROWS<T> + at.warp * N, rows = scan_rows<T>(s, mine);
       ring.wait();
       fetch();
-      twa_f2 A1 = twa_pair(1.0f), L1 = 0;
-      if (rows == SEG) {
+      Map end;
+      if (rows == N) {
 #pragma unroll
-        for (int i = 0; i < SEG; ++i) row(i, ring.get(0, i), ring.get(1, i), A1, L1);
+        for (int i = 0; i < N; ++i) row(i, ring.get(0, i), ring.get(1, i));
+        end = {A[N - 1], L[N - 1]};
       } else {
 #pragma unroll
-        for (int i = 0; i < SEG; ++i)
-          if (i < rows) row(i, ring.get(0, i), ring.get(1, i), A1, L1);
+        for (int i = 0; i < N; ++i)
+          if (i < rows) row(i, ring.get(0, i), ring.get(1, i));
+        end = last(rows);
       }
-      ring.done();
-      joins.seg[turn][at.warp][0][at.lane] = A1;
-      joins.seg[turn][at.warp][1][at.lane] = L1;
+      joins.seg[turn][at.warp][at.lane] = end;
       __syncthreads();
-      twa_f2 in = state;
+      twa_f2 in;
       if (at.ranks > 1) {
-        share_tile<true>(joins, at, turn);
+        share_tile<true>(joins, tiles, at, turn);
+        in = state;
         for (int r = 0; r < at.ranks; ++r) {
           if (r == at.rank) in = state;
-          state = twa_fma2(joins.tile[turn][r][0][at.lane], state, joins.tile[turn][r][1][at.lane]);
+          state = tiles.tile[turn][r][at.lane].of(state);
         }
-        if (at.warp == 0 && t < s.len) scan_keep(a.states, slot, a.channels, at.c, at.n, in);
-        for (int w = 0; w < at.warp; ++w) in = twa_fma2(joins.seg[turn][w][0][at.lane], in, joins.seg[turn][w][1][at.lane]);
       } else {
-        if (at.warp == 0) scan_keep(a.states, slot, a.channels, at.c, at.n, state);
-#pragma unroll
-        for (int w = 0; w < SCAN_WARPS; ++w) {
-          if (w == at.warp) in = state;
-          state = twa_fma2(joins.seg[turn][w][0][at.lane], state, joins.seg[turn][w][1][at.lane]);
-        }
+        in = joins.carry[turn ^ 1][at.lane];
       }
+#pragma unroll
+      for (int w = 0; w < SCAN_WARPS - 1; ++w)
+        if (w < at.warp) in = joins.seg[turn][w][at.lane].of(in);
+      if (rows) keep_state(at, a.states, slot, a.channels, in);
+      if (at.ranks == 1 && at.warp == SCAN_WARPS - 1) joins.carry[turn][at.lane] = state = end.of(in);
       turn ^= 1;
-      store(s.begin + mine, rows, in);
+      if (FEED == BY_UNITS && rows == N && wide) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          float lo, hi;
+          twa_unpair(twa_fma2(A[i], in, L[i]), lo, hi);
+          ring.put(0, i, lo, hi);
+        }
+        __syncwarp();
+        ring.flush(0, h, a.ldh);
+      } else {
+        store(s.begin + mine, rows, in);
+      }
+      ring.done();
     }
-    if (at.warp == 0 && at.rank == 0) scan_keep(a.h_last, seq, a.channels, at.c, at.n, state);
+    if (at.warp == SCAN_WARPS - 1 && at.rank == 0) at.keep(a.h_last, seq, a.channels, state);
   }
 };
 
 template <typename T, int FEED>
 struct ScanBackward {
-  static constexpr int MAPS = 3, STAGES = FEED == BY_ELEMENTS ? 1 : (sizeof(T) == 2 ? 3 : 2);      // maps: A, L, M
-  static constexpr bool PACKED = FEED != BY_ELEMENTS;
+  static constexpr int STAGES = 2;
+  static constexpr bool TOGETHER = FEED != BY_ELEMENTS;
+  static constexpr int N = SEG<T>;
   typedef Ring<T, FEED, 3, STAGES> Rows;
   const ScanArgs& a;
-  const Place at;
-  twa_f2 n[SEG], d[SEG];                           // gates; h_{t-1} - x_t
+  const Place<FEED> at;
+  twa_f2 n[N], e[N];                               // gates; a (1 - a) (h_{t-1} - x_t)
 
   __device__ __forceinline__ ScanBackward(const ScanArgs& args, int slice) : a(args), at(args, slice) {}
 
-  // Gradients of a row from g = dh + k, where k is what comes from the rows behind it; k becomes this row's.
-  __device__ __forceinline__ void back(int i, T* dx, T* df, twa_f2 dh, twa_f2& k) {
-    const twa_f2 g = twa_add2(dh, k);
-    float g0, g1, n0, n1, d0, d1;
-    twa_unpair(g, g0, g1);
+  // A row on the way from the state before the segment's first row to the one behind its last; off: the segment's A and M so far.
+  __device__ __forceinline__ void row(int i, const Pair<T>& x, const Pair<T>& f, const Pair<T>& dh, twa_f2& h, Map& off) {
+    n[i] = scan_gate<T>(f);
+    const twa_f2 d = scan_minus(h, x.both());
+    h = twa_fma2(n[i], d, scan_pick(n[i], h, x.both()));
+    off.A = scan_decay(n[i], off.A);
+    off.B = twa_fma2(off.A, dh.both(), off.B);
+    float n0, n1;
     twa_unpair(n[i], n0, n1);
-    twa_unpair(d[i], d0, d1);
-    k = scan_decay(n[i], g);
-    if (at.n > 0) {
-      Pair<T>::template store<PACKED>(dx + i * a.lddx, fmaf(-n0, g0, scan_open(n0) ? 0.0f : g0), fmaf(-n1, g1, scan_open(n1) ? 0.0f : g1), at.n);
-      const float s0 = fabsf(n0), s1 = fabsf(n1);
-      Pair<T>::template store<PACKED>(df + i * a.lddf, fmaf(-s0, s0, s0) * d0 * g0, fmaf(-s1, s1, s1) * d1 * g1, at.n);
+    e[i] = twa_mul2(twa_pair(fmaf(-n0, n0, fabsf(n0)), fmaf(-n1, n1, fabsf(n1))), d);
+  }
+  // Gradients of a row from g = dh + k, where k is what comes from the rows behind it; k becomes this row's.  With p = n g, k is
+  // g + p where the gate is open and p where not, and dx = (1 - a) g is -p or g - p.
+  template <typename Out>
+  __device__ __forceinline__ void back(int i, twa_f2 dh, twa_f2& k, Out out) {
+    const twa_f2 g = twa_add2(dh, k), p = twa_mul2(n[i], g), open = scan_pick(n[i], g, twa_pair(0.0f));
+    k = twa_add2(open, p);
+    float x0, x1, f0, f1;
+    twa_unpair(scan_minus(scan_minus(g, open), p), x0, x1);
+    twa_unpair(twa_mul2(e[i], g), f0, f1);
+    out(x0, x1, f0, f1);
+  }
+  // Of the first `rows` rows from `first` on, straight to memory.
+  template <typename Dh>
+  __device__ __forceinline__ void store(long long first, int rows, twa_f2& k, Dh dh) {
+    T* dx = static_cast<T*>(a.dx) + (first + N - 1) * a.lddx + at.c;
+    T* df = static_cast<T*>(a.df) + (first + N - 1) * a.lddf + at.c;
+#pragma unroll
+    for (int i = N - 1; i >= 0; --i) {
+      if (i < rows)
+        back(i, dh(i), k, [&](float x0, float x1, float f0, float f1) {
+          if (at.n > 0) {
+            Pair<T>::template store<TOGETHER>(dx, x0, x1, at.n);
+            Pair<T>::template store<TOGETHER>(df, f0, f1, at.n);
+          }
+        });
+      dx -= a.lddx;
+      df -= a.lddf;
     }
   }
 
@@ -195,112 +245,120 @@ struct ScanBackward {
     const T* x = static_cast<const T*>(a.x) + s.begin * a.ldx + at.c;
     const T* f = static_cast<const T*>(a.f) + s.begin * a.ldf + at.c;
     const T* g = static_cast<const T*>(a.dh) + s.begin * a.lddh + at.c;
-    Pair<T> rx[SEG], rf[SEG], rd[SEG];
+    Pair<T> rx[N], rf[N], rd[N];
 #pragma unroll
-    for (int i = 0; i < SEG; ++i)
+    for (int i = 0; i < N; ++i)
       if (i < rows && at.n > 0) {
-        rx[i].template load<PACKED>(x + i * a.ldx, at.n);
-        rf[i].template load<PACKED>(f + i * a.ldf, at.n);
-        rd[i].template load<PACKED>(g + i * a.lddh, at.n);
+        rx[i].template load<TOGETHER>(x + i * a.ldx, at.n);
+        rf[i].template load<TOGETHER>(f + i * a.ldf, at.n);
+        rd[i].template load<TOGETHER>(g + i * a.lddh, at.n);
       }
-    twa_f2 h = rows ? scan_state(a.states, scan_slot(s, seq), a.channels, at.c, at.n) : 0;
-    twa_f2 k = scan_state(a.d_last, seq, a.channels, at.c, at.n);
+    twa_f2 h = rows ? kept_state(at, a.states, scan_slot<T>(s, seq), a.channels) : 0;
+    twa_f2 k = at.state(a.d_last, seq, a.channels);
+    Map off = {twa_pair(1.0f), 0};
 #pragma unroll
-    for (int i = 0; i < SEG; ++i)
-      if (i < rows) {
-        n[i] = scan_gate<T>(rf[i]);
-        d[i] = scan_minus(h, rx[i].both());
-        h = scan_step(n[i], h, rx[i].both());
-      }
-    T* dx = static_cast<T*>(a.dx) + s.begin * a.lddx + at.c;
-    T* df = static_cast<T*>(a.df) + s.begin * a.lddf + at.c;
-#pragma unroll
-    for (int i = SEG - 1; i >= 0; --i)
-      if (i < rows) back(i, dx, df, rd[i].both(), k);
-    scan_keep(a.dh0, seq, a.channels, at.c, at.n, k);
+    for (int i = 0; i < N; ++i)
+      if (i < rows) row(i, rx[i], rf[i], rd[i], h, off);
+    store(s.begin, rows, k, [&](int i) { return rd[i].both(); });
+    at.keep(a.dh0, seq, a.channels, k);
   }
 
-  __device__ __forceinline__ void whole(const Span& s, int seq, char* shared, Joins<MAPS>& joins, int& turn) {
-    Rows ring(shared, at.warp);
-    const long long stride = static_cast<long long>(SCAN_ROWS) * at.ranks;
-    const long long rounds = (s.len + stride - 1) / stride;
-    const int left = a.channels - (at.c - 2 * at.lane);
-    long long ahead = (rounds - 1) * stride + at.rank * SCAN_ROWS + at.warp * SEG;
-    auto rows_at = [&](long long r) { return static_cast<int>(s.len - r < SEG ? (s.len - r < 0 ? 0 : s.len - r) : SEG); };
+  __device__ __forceinline__ void copy(Rows& ring, int array, const T* from, const void* all, long long ld, int rows, int left) {
+    const T* first = static_cast<const T*>(all);
+    ring.copy(array, from, ld, rows, left, first, first + (a.tokens - 1) * ld + a.channels - 1);
+  }
+  __device__ __forceinline__ void whole(const Span& s, int seq, char* shared, Joins& joins, Tiles& tiles, int& turn) {
+    Rows ring(shared, at.warp, at.lane);
+    const int stride = SCAN_ROWS<T> * at.ranks, rounds = (s.len + stride - 1) / stride, left = a.channels - at.slice;
+    const bool wide = __all_sync(0xffffffffu, at.n == 2);
+    int ahead = (rounds - 1) * stride + at.rank * SCAN_ROWS<T> + at.warp * N;
+    ring.lies(0, static_cast<const T*>(a.x) + (s.begin + ahead) * a.ldx + at.slice, a.ldx);
+    ring.lies(1, static_cast<const T*>(a.f) + (s.begin + ahead) * a.ldf + at.slice, a.ldf);
+    ring.lies(2, static_cast<const T*>(a.dh) + (s.begin + ahead) * a.lddh + at.slice, a.lddh);
+    const T* x = Rows::own(static_cast<const T*>(a.x) + (s.begin + ahead) * a.ldx + at.slice, a.ldx);
+    const T* f = Rows::own(static_cast<const T*>(a.f) + (s.begin + ahead) * a.ldf + at.slice, a.ldf);
+    const T* g = Rows::own(static_cast<const T*>(a.dh) + (s.begin + ahead) * a.lddh + at.slice, a.lddh);
+    T* dx = Rows::own(static_cast<T*>(a.dx) + (s.begin + ahead) * a.lddx + at.slice, a.lddx);
+    T* df = Rows::own(static_cast<T*>(a.df) + (s.begin + ahead) * a.lddf + at.slice, a.lddf);
     auto fetch = [&]() {
-      const int rows = ahead < 0 ? 0 : rows_at(ahead);
+      const int rows = ahead < 0 ? 0 : scan_rows<T>(s, ahead);
       if (rows) {
-        ring.copy(0, static_cast<const T*>(a.x) + (s.begin + ahead) * a.ldx + (at.c - 2 * at.lane), a.ldx, rows, left);
-        ring.copy(1, static_cast<const T*>(a.f) + (s.begin + ahead) * a.ldf + (at.c - 2 * at.lane), a.ldf, rows, left);
-        ring.copy(2, static_cast<const T*>(a.dh) + (s.begin + ahead) * a.lddh + (at.c - 2 * at.lane), a.lddh, rows, left);
+        copy(ring, 0, x, a.x, a.ldx, rows, left);
+        copy(ring, 1, f, a.f, a.ldf, rows, left);
+        copy(ring, 2, g, a.dh, a.lddh, rows, left);
       }
       ring.filled();
       ahead -= stride;
+      x -= stride * a.ldx;
+      f -= stride * a.ldf;
+      g -= stride * a.lddh;
     };
 #pragma unroll
     for (int i = 0; i < Rows::AHEAD; ++i) fetch();
-    twa_f2 k = scan_state(a.d_last, seq, a.channels, at.c, at.n);
-    for (long long round = rounds - 1; round >= 0; --round) {
-      const long long t = round * stride + at.rank * SCAN_ROWS, mine = t + at.warp * SEG;
-      const int rows = rows_at(mine);
-      twa_f2 h = t < s.len ? scan_state(a.states, scan_slot(s, seq) + round * at.ranks + at.rank, a.channels, at.c, at.n) : 0;
+    twa_f2 k = at.state(a.d_last, seq, a.channels);
+    if (at.warp == 0) joins.carry[turn ^ 1][at.lane] = k;
+    // the state before the next segment, fetched one tile ahead
+    int slot = scan_slot<T>(s, seq) + ((rounds - 1) * at.ranks + at.rank) * SCAN_WARPS + at.warp;
+    twa_f2 next = rounds && scan_rows<T>(s, (rounds - 1) * stride + at.rank * SCAN_ROWS<T> + at.warp * N) ? kept_state(at, a.states, slot, a.channels) : 0;
+    for (int round = rounds - 1; round >= 0; --round, dx -= stride * a.lddx, df -= stride * a.lddf) {
+      const int mine = round * stride + at.rank * SCAN_ROWS<T> + at.warp * N, rows = scan_rows<T>(s, mine);
+      twa_f2 h = next;
       ring.wait();
       fetch();
-      twa_f2 A1 = twa_pair(1.0f), L1 = 0, M1 = 0;
+      Map off = {twa_pair(1.0f), 0};
+      const bool full = rows == N && wide;
+      if (rows == N) {
 #pragma unroll
-      for (int i = 0; i < SEG; ++i)
-        if (i < rows) {
-          n[i] = scan_gate<T>(ring.get(1, i));
-          A1 = scan_decay(n[i], A1);
-          L1 = scan_step(n[i], L1, ring.get(0, i).both());
-        }
-#pragma unroll
-      for (int i = SEG - 1; i >= 0; --i)
-        if (i < rows) M1 = scan_decay(n[i], twa_add2(ring.get(2, i).both(), M1));
-      joins.seg[turn][at.warp][0][at.lane] = A1;
-      joins.seg[turn][at.warp][1][at.lane] = L1;
-      joins.seg[turn][at.warp][2][at.lane] = M1;
-      __syncthreads();
-      twa_f2 in = k;
-      if (at.ranks > 1) {
-        share_tile<false>(joins, at, turn);
-        for (int r = at.ranks - 1; r >= 0; --r) {
-          if (r == at.rank) in = k;
-          k = twa_fma2(joins.tile[turn][r][0][at.lane], k, joins.tile[turn][r][1][at.lane]);
-        }
-        for (int w = SCAN_WARPS - 1; w > at.warp; --w) in = twa_fma2(joins.seg[turn][w][0][at.lane], in, joins.seg[turn][w][2][at.lane]);
+        for (int i = 0; i < N; ++i) row(i, ring.get(0, i), ring.get(1, i), ring.get(2, i), h, off);
       } else {
 #pragma unroll
-        for (int w = SCAN_WARPS - 1; w >= 0; --w) {
-          if (w == at.warp) in = k;
-          k = twa_fma2(joins.seg[turn][w][0][at.lane], k, joins.seg[turn][w][2][at.lane]);
-        }
+        for (int i = 0; i < N; ++i)
+          if (i < rows) row(i, ring.get(0, i), ring.get(1, i), ring.get(2, i), h, off);
       }
-      for (int w = 0; w < at.warp; ++w) h = twa_fma2(joins.seg[turn][w][0][at.lane], h, joins.seg[turn][w][1][at.lane]);
-      turn ^= 1;
-      T* dx = static_cast<T*>(a.dx) + (s.begin + mine) * a.lddx + at.c;
-      T* df = static_cast<T*>(a.df) + (s.begin + mine) * a.lddf + at.c;
-#pragma unroll
-      for (int i = 0; i < SEG; ++i)
-        if (i < rows) {
-          const twa_f2 x = ring.get(0, i).both();
-          d[i] = scan_minus(h, x);
-          h = scan_step(n[i], h, x);
+      joins.seg[turn][at.warp][at.lane] = off;
+      slot -= at.ranks * SCAN_WARPS;
+      next = round ? kept_state(at, a.states, slot, a.channels) : 0;
+      __syncthreads();
+      twa_f2 in;
+      if (at.ranks > 1) {
+        share_tile<false>(joins, tiles, at, turn);
+        in = k;
+        for (int r = at.ranks - 1; r >= 0; --r) {
+          if (r == at.rank) in = k;
+          k = tiles.tile[turn][r][at.lane].of(k);
         }
+      } else {
+        in = joins.carry[turn ^ 1][at.lane];
+      }
 #pragma unroll
-      for (int i = SEG - 1; i >= 0; --i)
-        if (i < rows) back(i, dx, df, ring.get(2, i).both(), in);
+      for (int w = SCAN_WARPS - 1; w > 0; --w)
+        if (w > at.warp) in = joins.seg[turn][w][at.lane].of(in);
+      if (at.ranks == 1 && at.warp == 0) joins.carry[turn][at.lane] = k = off.of(in);
+      turn ^= 1;
+      if (FEED == BY_UNITS && full) {
+#pragma unroll
+        for (int i = N - 1; i >= 0; --i)
+          back(i, ring.get(2, i).both(), in, [&](float x0, float x1, float f0, float f1) {
+            ring.put(0, i, x0, x1);
+            ring.put(1, i, f0, f1);
+          });
+        __syncwarp();
+        ring.flush(0, dx, a.lddx);
+        ring.flush(1, df, a.lddf);
+      } else {
+        store(s.begin + mine, rows, in, [&](int i) { return ring.get(2, i).both(); });
+      }
       ring.done();
     }
-    if (at.warp == 0 && at.rank == 0) scan_keep(a.dh0, seq, a.channels, at.c, at.n, k);
+    if (at.warp == 0 && at.rank == 0) at.keep(a.dh0, seq, a.channels, k);
   }
 };
 
 // GROUP sequences of a slice of channels a block.  The ones of at most SEG rows go to one warp each, the others to the block.
-template <typename Direction, int GROUP>
-__device__ __forceinline__ void scan_block(const ScanArgs& a) {
+template <typename Direction, int GROUP, typename J>
+__device__ __forceinline__ void scan_block(const ScanArgs& a, J& joins) {
   extern __shared__ __align__(16) char shared[];
-  __shared__ Joins<Direction::MAPS> joins;
+  Tiles& tiles = *reinterpret_cast<Tiles*>(shared + Direction::Rows::BLOCK_BYTES);         // of clusters only
   const unsigned task = blockIdx.x / a.cluster;
   const int slice = task % a.slices, first = task / a.slices * GROUP;
   Direction d(a, slice);
@@ -309,7 +367,7 @@ __device__ __forceinline__ void scan_block(const ScanArgs& a) {
     const int seq = first + d.at.warp;
     if (seq < a.sequences) {
       const Span s = scan_span(a, seq, slice == 0 && d.at.lane == 0);
-      if (s.len >= 0 && s.len <= SEG) d.brief(s, seq);
+      if (s.len >= 0 && s.len <= Direction::N) d.brief(s, seq);
     }
   }
   int turn = 0;
@@ -317,19 +375,21 @@ __device__ __forceinline__ void scan_block(const ScanArgs& a) {
     const int seq = first + g;
     if (seq >= a.sequences) break;
     const Span s = scan_span(a, seq, GROUP == 1 && slice == 0 && threadIdx.x == 0);
-    if (s.len > SEG || (GROUP == 1 && s.len >= 0)) d.whole(s, seq, shared, joins, turn);
+    if (s.len > Direction::N || (GROUP == 1 && s.len >= 0)) d.whole(s, seq, shared, joins, tiles, turn);
   }
 }
 
 template <typename T, int FEED, int GROUP>
 __global__ void __launch_bounds__(SCAN_THREADS, 2) scan_forward_kernel(ScanArgs a) {
   twa_begin(a.x, a.f, a.starts, a.h0);
-  scan_block<ScanForward<T, FEED>, GROUP>(a);
+  __shared__ Joins joins;
+  scan_block<ScanForward<T, FEED>, GROUP>(a, joins);
 }
 template <typename T, int FEED, int GROUP>
 __global__ void __launch_bounds__(SCAN_THREADS, 2) scan_backward_kernel(ScanArgs a) {
   twa_begin(a.x, a.f, a.dh, a.starts, a.states, a.d_last);
-  scan_block<ScanBackward<T, FEED>, GROUP>(a);
+  __shared__ Joins joins;
+  scan_block<ScanBackward<T, FEED>, GROUP>(a, joins);
 }
 
 // How rows of two pointers and strides can be fetched together.
@@ -338,26 +398,22 @@ int scan_feed(const void* p, long long ld, size_t size, int channels, int so_far
   if (so_far == BY_PAIRS && (channels % 2 || twa_misaligned_to(p, 2 * size) || ld % 2)) so_far = BY_ELEMENTS;
   return so_far;
 }
-// Stores go by pairs at most.
-int scan_feed_out(const void* p, long long ld, size_t size, int so_far) {
-  return so_far != BY_ELEMENTS && (twa_misaligned_to(p, 2 * size) || ld % 2) ? BY_ELEMENTS : so_far;
-}
-
 template <typename T, int FEED, int GROUP>
 cudaError_t scan_launch(twa_ctx* ctx, const ScanArgs& a, bool back) {
   auto kernel = back ? scan_backward_kernel<T, FEED, GROUP> : scan_forward_kernel<T, FEED, GROUP>;
-  const size_t smem = back ? ScanBackward<T, FEED>::Rows::BLOCK_BYTES : ScanForward<T, FEED>::Rows::BLOCK_BYTES;
+  const size_t smem = (back ? ScanBackward<T, FEED>::Rows::BLOCK_BYTES : ScanForward<T, FEED>::Rows::BLOCK_BYTES) + (a.cluster > 1 ? sizeof(Tiles) : 0);
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
   if (e != cudaSuccess) return e;
   const unsigned blocks = static_cast<unsigned>(twa_ceil_div(a.sequences, GROUP) * a.slices * a.cluster);
   return twa_launch_clusters(ctx->stream, kernel, blocks, a.cluster, SCAN_THREADS, smem, a);
 }
+constexpr int SCAN_RESIDENT = 2;                   // blocks of an SM
 template <typename T>
 cudaError_t scan_launch(twa_ctx* ctx, ScanArgs& a, bool back, int feed) {
-  const bool brief = a.tokens <= 2LL * SEG * a.sequences;
+  const bool brief = a.tokens <= 2LL * SEG<T> * a.sequences;
   a.cluster = 1;
-  while (!brief && a.cluster < MAX_CLUSTER && a.tokens > 2LL * a.cluster * SCAN_ROWS * a.sequences &&
-         static_cast<long long>(a.sequences) * a.slices * a.cluster < ctx->sm_count)
+  while (!brief && a.cluster < MAX_CLUSTER && a.tokens > 2LL * a.cluster * SCAN_ROWS<T> * a.sequences &&
+         2LL * a.sequences * a.slices * a.cluster <= SCAN_RESIDENT * ctx->sm_count)
     a.cluster *= 2;
   if (brief)
     return feed == BY_UNITS ? scan_launch<T, BY_UNITS, SHORT_GROUP>(ctx, a, back)
@@ -385,7 +441,7 @@ size_t twa_gated_scan_states_bytes(int64_t tokens, int sequences, int channels) 
   if (tokens < 0 || tokens > TWA_SCAN_MAX_TOKENS || sequences < 0 || sequences > TWA_SCAN_MAX_SEQUENCES || channels < 1 ||
       channels > TWA_SCAN_MAX_CHANNELS)
     return 0;
-  return static_cast<size_t>(tokens / SCAN_ROWS + sequences) * channels * sizeof(float);
+  return static_cast<size_t>(tokens / STATE_ROWS + sequences) * channels * sizeof(float);
 }
 
 int twa_gated_scan(twa_ctx* ctx, const void* x, int64_t ldx, const void* f, int64_t ldf, twa_dtype dtype, int64_t tokens, int channels,
@@ -407,7 +463,7 @@ int twa_gated_scan(twa_ctx* ctx, const void* x, int64_t ldx, const void* f, int6
   a.tokens = tokens, a.channels = channels, a.starts = starts, a.s_type = s_type, a.sequences = sequences;
   a.slices = static_cast<int>(twa_ceil_div(channels, SCAN_CHANNELS));
   a.h0 = h0, a.h_last = h_last, a.states = static_cast<float*>(states), a.status = ctx->d_status;
-  const int feed = scan_feed_out(h, ldh, size, scan_feed(f, ldf, size, channels, scan_feed(x, ldx, size, channels, BY_UNITS)));
+  const int feed = scan_feed(h, ldh, size, channels, scan_feed(f, ldf, size, channels, scan_feed(x, ldx, size, channels, BY_UNITS)));
   TWA_CUDA_OK(ctx, dtype == TWA_BF16 ? scan_launch<bf16>(ctx, a, false, feed) : scan_launch<float>(ctx, a, false, feed));
   return TWA_OK;
 }
@@ -434,7 +490,7 @@ int twa_gated_scan_backward(twa_ctx* ctx, const void* dh, int64_t lddh, const vo
   a.slices = static_cast<int>(twa_ceil_div(channels, SCAN_CHANNELS));
   a.states = const_cast<float*>(static_cast<const float*>(states)), a.d_last = d_last, a.dh0 = dh0, a.status = ctx->d_status;
   int feed = scan_feed(dh, lddh, size, channels, scan_feed(f, ldf, size, channels, scan_feed(x, ldx, size, channels, BY_UNITS)));
-  feed = scan_feed_out(df, lddf, size, scan_feed_out(dx, lddx, size, feed));
+  feed = scan_feed(df, lddf, size, channels, scan_feed(dx, lddx, size, channels, feed));
   TWA_CUDA_OK(ctx, dtype == TWA_BF16 ? scan_launch<bf16>(ctx, a, true, feed) : scan_launch<float>(ctx, a, true, feed));
   return TWA_OK;
 }

@@ -8,9 +8,9 @@
 // is half a unit of the result; a gate rounded to 1 - 2^-24 k would err the same way step after step.  Steps in a row are
 // affine in the state that enters, h = A h_in + L; A comes from the same steps with x = 0 from 1, L with h_in = 0.
 //
-// A lane has two neighbouring channels, a warp a segment of SEG rows of 64 channels, the warps of a block consecutive segments:
-// a tile of 64 rows.  Every warp takes its own segment from 0, the segments' (A, L) go through shared memory, and
-// every thread joins those before its own with the state that enters the tile.  States are float32.
+// A lane has two channels, a warp a segment of SEG rows of 64 channels, the warps of a block consecutive segments: a tile.  Every warp
+// takes its own segment from 0, the segments' (A, L) go through shared memory, and every thread joins those before its own with
+// the state that enters the tile.  States are float32.
 #pragma once
 
 #include "twa_ops.cuh"
@@ -18,8 +18,11 @@
 namespace {
 
 constexpr int SCAN_WARPS = 8, SCAN_THREADS = SCAN_WARPS * 32;
-constexpr int SEG = 8;                             // rows of a segment
-constexpr int SCAN_ROWS = SCAN_WARPS * SEG;        // of a tile, and from one kept state to the next
+template <typename T>
+constexpr int SEG = 32 / sizeof(T);                // rows of a segment
+template <typename T>
+constexpr int SCAN_ROWS = SCAN_WARPS * SEG<T>;     // of a tile
+constexpr int STATE_ROWS = SEG<float>;             // from one kept state to the next, at least
 constexpr int SCAN_CHANNELS = 64;                  // of a block
 constexpr int SHORT_GROUP = SCAN_WARPS;            // sequences of a block where most are short
 constexpr int MAX_CLUSTER = 8;                     // blocks along a sequence
@@ -41,80 +44,93 @@ struct ScanArgs {
 
 // Rows of a sequence; len -1: its offsets are wrong and it is left alone.
 struct Span {
-  long long begin, len;
+  long long begin;
+  int len;
 };
 __device__ __forceinline__ Span scan_span(const ScanArgs& a, int seq, bool report) {
   if (!a.starts) {
-    const long long each = a.tokens / a.sequences;
-    return {seq * each, each};
+    const int each = static_cast<int>(a.tokens / a.sequences);
+    return {static_cast<long long>(seq) * each, each};
   }
   const long long b = twa_load_id(a.starts, a.s_type, seq), e = twa_load_id(a.starts, a.s_type, seq + 1);
   if (b < 0 || e < b || e > a.tokens) {
     if (report) twa_set_status(a.status, TWA_ERR_INVALID_ARG, seq);
     return {0, -1};
   }
-  return {b, e - b};
+  return {b, static_cast<int>(e - b)};
 }
 // The first of a sequence's kept states: those of sequences before it end before this place, for
 // (b + len) / R + 1 >= b / R + ceil(len / R).
-__device__ __forceinline__ long long scan_slot(const Span& s, int seq) { return s.begin / SCAN_ROWS + seq; }
+template <typename T>
+__device__ __forceinline__ int scan_slot(const Span& s, int seq) { return static_cast<int>(s.begin / SEG<T>) + seq; }
+// Rows that a sequence has from row r on, of a segment.
+template <typename T>
+__device__ __forceinline__ int scan_rows(const Span& s, int r) { return min(max(s.len - r, 0), SEG<T>); }
 
-// Two neighbouring elements as they lie in memory.  PACKED: one access, on the pair's boundary; otherwise one each, `n` of them.
+// How rows are fetched, and which two channels a lane has.  In units of 16 bytes, any lane's, or in pairs: neighbouring channels,
+// loaded and stored together.  Element by element, where rows lie on no such boundary: channels 32 apart, so that a warp's accesses
+// are contiguous.
+enum { BY_UNITS, BY_PAIRS, BY_ELEMENTS };
+
+// Two elements in one or two registers.
 template <typename T>
 struct Pair;
 template <>
 struct Pair<float> {
   float2 r;
-  template <bool PACKED>
+  template <bool TOGETHER>
   __device__ __forceinline__ void load(const float* p, int n) {
-    if constexpr (PACKED) r = __ldg(reinterpret_cast<const float2*>(p));
+    if constexpr (TOGETHER) r = __ldg(reinterpret_cast<const float2*>(p));
     else {
       r.x = __ldg(p);
-      r.y = n > 1 ? __ldg(p + 1) : 0.0f;
+      r.y = n > 1 ? __ldg(p + 32) : 0.0f;
     }
   }
   __device__ __forceinline__ float lo() const { return r.x; }
   __device__ __forceinline__ float hi() const { return r.y; }
   __device__ __forceinline__ twa_f2 both() const { return twa_pair(r.x, r.y); }
-  template <bool PACKED>
+  template <bool TOGETHER>
   static __device__ __forceinline__ void store(float* p, float a, float b, int n) {
-    if constexpr (PACKED) *reinterpret_cast<float2*>(p) = make_float2(a, b);
+    if constexpr (TOGETHER) *reinterpret_cast<float2*>(p) = make_float2(a, b);
     else {
       p[0] = a;
-      if (n > 1) p[1] = b;
+      if (n > 1) p[32] = b;
     }
   }
 };
 template <>
 struct Pair<bf16> {
   uint32_t r;
-  template <bool PACKED>
+  template <bool TOGETHER>
   __device__ __forceinline__ void load(const bf16* p, int n) {
-    if constexpr (PACKED) r = __ldg(reinterpret_cast<const uint32_t*>(p));
+    if constexpr (TOGETHER) r = __ldg(reinterpret_cast<const uint32_t*>(p));
     else {
       const unsigned short* q = reinterpret_cast<const unsigned short*>(p);
       r = __ldg(q);
-      if (n > 1) r |= static_cast<uint32_t>(__ldg(q + 1)) << 16;
+      if (n > 1) r |= static_cast<uint32_t>(__ldg(q + 32)) << 16;
     }
   }
   __device__ __forceinline__ float lo() const { return twa_bf16_lo(r); }
   __device__ __forceinline__ float hi() const { return twa_bf16_hi(r); }
   __device__ __forceinline__ twa_f2 both() const { return twa_pair(lo(), hi()); }
-  template <bool PACKED>
+  template <bool TOGETHER>
   static __device__ __forceinline__ void store(bf16* p, float a, float b, int n) {
-    if constexpr (PACKED) *reinterpret_cast<uint32_t*>(p) = twa_bf16_pair(a, b);
+    if constexpr (TOGETHER) *reinterpret_cast<uint32_t*>(p) = twa_bf16_pair(a, b);
     else {
       p[0] = twa_from_float<bf16>(a);
-      if (n > 1) p[1] = twa_from_float<bf16>(b);
+      if (n > 1) p[32] = twa_from_float<bf16>(b);
     }
   }
 };
 
-// -q of two gates; their signs say which form a step takes.  The exponential of a bfloat16 gate may err by some units of float32,
-// that of a float32 gate may not.
+// -q of two gates; their signs say which form a step takes.  1 + e^|f|: the exponential of a bfloat16 gate may err by some units of
+// float32 and is taken as a power of two at once, that of a float32 gate may not.
 template <typename T>
 __device__ __forceinline__ float scan_exp(float f) {
-  return sizeof(T) == 2 ? __expf(f) : expf(f);
+  if (sizeof(T) == 4) return expf(fabsf(f));
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(fabsf(f) * 1.44269504f));
+  return r;
 }
 __device__ __forceinline__ float scan_reciprocal(float v) {
   float r;
@@ -127,7 +143,7 @@ __device__ __forceinline__ float scan_turn(float s, float f) {
 template <typename T>
 __device__ __forceinline__ twa_f2 scan_gate(const Pair<T>& f) {
   float a, b;
-  twa_unpair(twa_add2(twa_pair(1.0f), twa_pair(scan_exp<T>(fabsf(f.lo())), scan_exp<T>(fabsf(f.hi())))), a, b);
+  twa_unpair(twa_add2(twa_pair(1.0f), twa_pair(scan_exp<T>(f.lo()), scan_exp<T>(f.hi()))), a, b);
   return twa_pair(scan_turn(scan_reciprocal(a), f.lo()), scan_turn(scan_reciprocal(b), f.hi()));
 }
 __device__ __forceinline__ bool scan_open(float n) { return __float_as_int(n) < 0; }
@@ -144,87 +160,178 @@ __device__ __forceinline__ twa_f2 scan_step(twa_f2 n, twa_f2 h, twa_f2 x) { retu
 // a times v: what a step makes of a state where x is 0.
 __device__ __forceinline__ twa_f2 scan_decay(twa_f2 n, twa_f2 v) { return twa_fma2(n, v, scan_pick(n, v, twa_pair(0.0f))); }
 
-// ---- rows on their way --------------------------------------------------------------------------------
-// How a warp fetches its segments' rows: in units of 16 bytes, any lane's; in pairs, each lane its own; or element by element.
-enum { BY_UNITS, BY_PAIRS, BY_ELEMENTS };
+// Where a thread stands: its two channels, c and c + 1 or c and c + 32, of which n exist; its block's rank along the sequence.
+template <int FEED>
+struct Place {
+  static constexpr int NEXT = FEED == BY_ELEMENTS ? 32 : 1;
+  int lane, warp, slice, c, n, rank, ranks;
+  __device__ __forceinline__ Place(const ScanArgs& a, int part) {
+    lane = threadIdx.x & 31;
+    warp = threadIdx.x >> 5;
+    slice = part * SCAN_CHANNELS;
+    c = slice + (FEED == BY_ELEMENTS ? lane : 2 * lane);
+    n = (c < a.channels ? 1 : 0) + (c + NEXT < a.channels ? 1 : 0);
+    ranks = a.cluster;
+    rank = ranks > 1 ? static_cast<int>(twa_cluster_rank()) : 0;
+  }
+  // Its channels of a row of float32 states.
+  __device__ __forceinline__ twa_f2 state(const float* p, long long row, int channels) const {
+    if (!p) return 0;
+    return twa_pair(n > 0 ? p[row * channels + c] : 0.0f, n > 1 ? p[row * channels + c + NEXT] : 0.0f);
+  }
+  __device__ __forceinline__ void keep(float* p, long long row, int channels, twa_f2 v) const {
+    if (!p) return;
+    float lo, hi;
+    twa_unpair(v, lo, hi);
+    if (n > 0) p[row * channels + c] = lo;
+    if (n > 1) p[row * channels + c + NEXT] = hi;
+  }
+};
 
-// A ring of a warp's segments in shared memory, STAGES deep, of ARRAYS matrices.  The copies are asynchronous but for those by
-// elements, which go through registers one segment ahead.
+// The states that the forward pass keeps: the same, but the buffer is the library's and begins on 16 bytes.
+template <int FEED>
+__device__ __forceinline__ twa_f2 kept_state(const Place<FEED>& at, const float* p, long long row, int channels) {
+  if (FEED == BY_ELEMENTS) return at.state(p, row, channels);
+  twa_f2 v = 0;
+  if (at.n > 0) v = *reinterpret_cast<const twa_f2*>(p + row * channels + at.c);
+  return v;
+}
+template <int FEED>
+__device__ __forceinline__ void keep_state(const Place<FEED>& at, float* p, long long row, int channels, twa_f2 v) {
+  if (FEED == BY_ELEMENTS) at.keep(p, row, channels, v);
+  else if (p && at.n > 0) *reinterpret_cast<twa_f2*>(p + row * channels + at.c) = v;
+}
+
+// A ring of a warp's segments in shared memory, STAGES deep, of ARRAYS matrices, filled by asynchronous copies.  By units, results go
+// out the same way: pairs into the stage that has been read, and from there 16 bytes a lane.
+// By elements, bfloat16 rows may begin between the 4-byte words that are the least an asynchronous copy takes.  Then a row's words
+// come as they lie, one more than a row has, and elements are found one place further; which rows those are changes with the
+// row's number where the stride is odd, and is the same for a segment's every tile.  A word that reaches out of the matrix,
+// before its first element or behind its last, is filled by the element.
 template <typename T, int FEED, int ARRAYS, int STAGES>
 struct Ring {
-  static constexpr int ROW = SCAN_CHANNELS * sizeof(T), BYTES = ARRAYS * SEG * ROW;     // of a row, of a segment
+  static constexpr int N = SEG<T>;
+  static constexpr bool WORDS = FEED == BY_ELEMENTS && sizeof(T) == 2;
+  static constexpr int ROW = SCAN_CHANNELS * sizeof(T) + (WORDS ? 16 : 0), AREA = N * ROW, BYTES = ARRAYS * AREA;       // of a row, a matrix, a stage
   static constexpr size_t BLOCK_BYTES = static_cast<size_t>(SCAN_WARPS) * STAGES * BYTES;
+  static constexpr int AHEAD = STAGES - 1;        // segments under way before the first is waited for
+  static constexpr int V = 16 / static_cast<int>(sizeof(T)), UNITS = SCAN_CHANNELS / V, EACH = 32 / UNITS;       // units of a row, rows a warp copies at once
   char* base;
-  Pair<T> held[FEED == BY_ELEMENTS ? ARRAYS * SEG : 1];
-  int fill, read;
+  int fill, read;                                 // bytes from the base: the stage to be filled, to be read
+  int mine[WORDS ? ARRAYS : 1][WORDS ? 2 : 1];    // this lane's elements of a row, by the row's parity
 
-  __device__ __forceinline__ Ring(char* shared, int warp) : base(shared + static_cast<size_t>(warp) * STAGES * BYTES), fill(0), read(0) {}
+  __device__ __forceinline__ Ring(char* shared, int warp, int lane) : base(shared + static_cast<size_t>(warp) * STAGES * BYTES), fill(0), read(0) {
+    if constexpr (!WORDS) mine[0][0] = lane * static_cast<int>(sizeof(T)) * (FEED == BY_ELEMENTS ? 1 : 2);
+  }
+  // Says where a matrix's segments lie: p is the first element of one of them.
+  __device__ __forceinline__ void lies(int array, const T* p, long long ld) {
+    if constexpr (WORDS) {
+      const int lane = threadIdx.x & 31;
+      mine[array][0] = lane * 2 + static_cast<int>(reinterpret_cast<uintptr_t>(p) & 2);
+      mine[array][1] = lane * 2 + static_cast<int>(reinterpret_cast<uintptr_t>(p + ld) & 2);
+    }
+  }
+  __device__ __forceinline__ int at(int array, int row) const { return WORDS ? mine[array][row & 1] : mine[0][0]; }
 
-  __device__ __forceinline__ void copy(int array, const T* p, long long ld, int rows, int channels) {
+  // This lane's first element of a segment that begins at p.
+  template <typename P>
+  static __device__ __forceinline__ P* own(P* p, long long ld) {
     const int lane = threadIdx.x & 31;
+    if constexpr (FEED == BY_UNITS) return p + lane / UNITS * ld + lane % UNITS * V;
+    else return p + (FEED == BY_PAIRS || WORDS ? 2 * lane : lane);
+  }
+  template <int SIZE>
+  static __device__ __forceinline__ void copy_async(uint32_t to, const void* from) {
+    if constexpr (SIZE == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(from), "n"(SIZE) : "memory");
+  }
+  // Rows from own(); `channels` remain from the slice's first.  first, last: the matrix's.
+  __device__ __forceinline__ void copy(int array, const T* from, long long ld, int rows, int channels, const T* first, const T* last) {
+    const int lane = threadIdx.x & 31;
+    const uint32_t area = twa_smem_u32(base + fill + array * AREA);
     if constexpr (FEED == BY_UNITS) {
-      constexpr int UNITS = ROW / 16, EACH = 32 / UNITS;
-      const int u = lane % UNITS, r0 = lane / UNITS;
-      const uint32_t to = twa_smem_u32(base + fill * BYTES + array * SEG * ROW + r0 * ROW + u * 16);
-      const T* from = p + r0 * ld + u * (16 / static_cast<int>(sizeof(T)));
-      const bool in = u * (16 / static_cast<int>(sizeof(T))) < channels;
+      const int upto = lane % UNITS * V < channels ? rows - lane / UNITS : 0;
 #pragma unroll
-      for (int i = 0; i < SEG / EACH; ++i)
-        if (in && r0 + i * EACH < rows)
-          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + i * EACH * ROW), "l"(from + i * EACH * ld) : "memory");
+      for (int i = 0; i < N; i += EACH) {
+        if (i < upto) copy_async<16>(area + lane * 16 + i * ROW, from);
+        from += EACH * ld;
+      }
     } else if constexpr (FEED == BY_PAIRS) {
-      const uint32_t to = twa_smem_u32(base + fill * BYTES + array * SEG * ROW + lane * 2 * sizeof(T));
-      const T* from = p + 2 * lane;
+      const int upto = 2 * lane < channels ? rows : 0;
 #pragma unroll
-      for (int i = 0; i < SEG; ++i)
-        if (2 * lane < channels && i < rows)
-          asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to + i * ROW), "l"(from + i * ld), "n"(2 * sizeof(T)) : "memory");
+      for (int i = 0; i < N; ++i) {
+        if (i < upto) copy_async<2 * sizeof(T)>(area + lane * 2 * sizeof(T) + i * ROW, from);
+        from += ld;
+      }
+    } else if constexpr (!WORDS) {
+      const int upto = lane < channels ? rows : 0, upto32 = lane + 32 < channels ? rows : 0;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        if (i < upto) copy_async<4>(area + lane * 4 + i * ROW, from);
+        if (i < upto32) copy_async<4>(area + lane * 4 + 128 + i * ROW, from + 32);
+        from += ld;
+      }
     } else {
-      const T* from = p + 2 * lane;
+      const T* row = from - 2 * lane;
+      const bool edge = row <= first || row + (rows - 1) * ld + channels > last;         // of the matrix; true of the whole warp
 #pragma unroll
-      for (int i = 0; i < SEG; ++i)
-        if (2 * lane < channels && i < rows) held[array * SEG + i].template load<false>(from + i * ld, channels - 2 * lane);
+      for (int i = 0; i < N; ++i) {
+        const int odd = (mine[array][i & 1] >> 1) - lane;                                // the row begins inside a word
+        const char* word = reinterpret_cast<const char*>(from) - 2 * odd;
+        if (i < rows && 2 * lane < channels + odd) {
+          if (!edge || (reinterpret_cast<const T*>(word) >= first && reinterpret_cast<const T*>(word) + 1 <= last)) {
+            copy_async<4>(area + i * ROW + lane * 4, word);
+          } else {
+            for (int e = 0; e < 2; ++e) {
+              const T* p = reinterpret_cast<const T*>(word) + e;
+              if (p >= first && p <= last) *reinterpret_cast<T*>(base + fill + array * AREA + i * ROW + lane * 4 + e * 2) = *p;
+            }
+          }
+        }
+        from += ld;
+      }
+      // the last element of a row that begins inside a word, alone in one more
+      if (lane < rows && channels >= SCAN_CHANNELS && (lane & 1 ? mine[array][1] : mine[array][0]) != lane * 2) {
+        const T* p = row + lane * ld + SCAN_CHANNELS - 1;
+        if (!edge || p < last) copy_async<4>(area + lane * ROW + SCAN_CHANNELS * 2, p);
+        else *reinterpret_cast<T*>(base + fill + array * AREA + lane * ROW + SCAN_CHANNELS * 2) = *p;
+      }
     }
   }
   // Ends the copies of one segment.
   __device__ __forceinline__ void filled() {
-    if constexpr (FEED != BY_ELEMENTS) asm volatile("cp.async.commit_group;" ::: "memory");
-    fill = fill + 1 == STAGES ? 0 : fill + 1;
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    fill = fill == (STAGES - 1) * BYTES ? 0 : fill + BYTES;
   }
   // Waits for the oldest segment.
   __device__ __forceinline__ void wait() {
-    if constexpr (FEED == BY_ELEMENTS) {
-      const int lane = threadIdx.x & 31;
-#pragma unroll
-      for (int i = 0; i < ARRAYS * SEG; ++i) *reinterpret_cast<Pair<T>*>(base + i * ROW + lane * 2 * sizeof(T)) = held[i];
-    } else {
-      asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
-      if (FEED == BY_UNITS) __syncwarp();
-    }
+    asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
+    if (FEED == BY_UNITS || WORDS) __syncwarp();
   }
   __device__ __forceinline__ Pair<T> get(int array, int row) const {
-    const int stage = FEED == BY_ELEMENTS ? 0 : read;
-    return *reinterpret_cast<const Pair<T>*>(base + stage * BYTES + (array * SEG + row) * ROW + (threadIdx.x & 31) * 2 * sizeof(T));
+    const char* p = base + read + array * AREA + row * ROW + at(array, row);
+    Pair<T> v;
+    if constexpr (WORDS) v.r = *reinterpret_cast<const unsigned short*>(p) | static_cast<uint32_t>(*reinterpret_cast<const unsigned short*>(p + 64)) << 16;
+    else if constexpr (FEED == BY_ELEMENTS) v.r = make_float2(*reinterpret_cast<const float*>(p), *reinterpret_cast<const float*>(p + 128));
+    else v = *reinterpret_cast<const Pair<T>*>(p);
+    return v;
+  }
+  // By units: a result in the place of what get() gave, and the whole segment of them to memory, from own().
+  __device__ __forceinline__ void put(int array, int row, float lo, float hi) const {
+    Pair<T>::template store<true>(reinterpret_cast<T*>(base + read + array * AREA + row * ROW + mine[0][0]), lo, hi, 2);
+  }
+  __device__ __forceinline__ void flush(int array, T* to, long long ld) const {
+    const char* from = base + read + array * AREA + (threadIdx.x & 31) * 16;
+#pragma unroll
+    for (int i = 0; i < N; i += EACH) {
+      *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(from + i * ROW);
+      to += EACH * ld;
+    }
   }
   __device__ __forceinline__ void done() {
-    read = read + 1 == STAGES ? 0 : read + 1;
-    if (FEED == BY_UNITS) __syncwarp();           // other lanes fill this stage again
+    read = read == (STAGES - 1) * BYTES ? 0 : read + BYTES;
+    if (FEED == BY_UNITS || WORDS) __syncwarp();  // other lanes fill this stage again
   }
-  // Segments that are under way before the first one is waited for.
-  static constexpr int AHEAD = FEED == BY_ELEMENTS ? 1 : STAGES - 1;
 };
-
-// Two neighbouring channels of a row of float32 states.
-__device__ __forceinline__ twa_f2 scan_state(const float* p, long long row, int channels, int c, int n) {
-  if (!p) return 0;
-  return twa_pair(n > 0 ? p[row * channels + c] : 0.0f, n > 1 ? p[row * channels + c + 1] : 0.0f);
-}
-__device__ __forceinline__ void scan_keep(float* p, long long row, int channels, int c, int n, twa_f2 v) {
-  if (!p) return;
-  float lo, hi;
-  twa_unpair(v, lo, hi);
-  if (n > 0) p[row * channels + c] = lo;
-  if (n > 1) p[row * channels + c + 1] = hi;
-}
 
 }  // namespace

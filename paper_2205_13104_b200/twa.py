@@ -44,7 +44,7 @@ TWA_LOGPROBS_MAX_TOP = 32
 TWA_MAX_TENSORS = 65536
 TWA_DROPOUT_MAX_ROWS = 1 << 30
 TWA_DROPOUT_MAX_COLS = 1 << 24
-TWA_SCAN_MAX_TOKENS = 1 << 36
+TWA_SCAN_MAX_TOKENS = 1 << 30
 TWA_SCAN_MAX_CHANNELS = 1 << 20
 TWA_SCAN_MAX_SEQUENCES = 1 << 24
 TWA_EXPERTS_MAX = 1024
