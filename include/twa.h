@@ -149,10 +149,14 @@ const char* twa_last_error(const twa_ctx* ctx);
  *      of more rows is walked in slabs of that many rows (at most 16 of them, else the call
  *      returns TWA_ERR_INVALID_ARG), exactly as bases above TWA_MAX_LAUNCH_ROWS always are: shorter
  *      kernels where the GPU is shared and a long launch holds others up.  0 = one launch up to
- *      TWA_MAX_LAUNCH_ROWS, slabs of 2^30 rows above. */
+ *      TWA_MAX_LAUNCH_ROWS, slabs of 2^30 rows above.
+ *  TWA_TUNE_SCAN_CLUSTER, TWA_TUNE_SCAN_CHANNELS: twa_gated_scan and its backward call, where sequences are not mostly
+ *      short: blocks that share a sequence (1, 2, 4 or 8) and channels of a block (16, 32 or 64; rows on 16-byte
+ *      boundaries only).  0 = as many as fill the device. */
 enum { TWA_TUNE_PROJECT_WARPS = 1, TWA_TUNE_LIFT_WARPS = 2, TWA_TUNE_STAGES = 3,
        TWA_TUNE_WAIT_LIMIT_MS = 4, TWA_TUNE_DEQUANT_PATH = 5, TWA_TUNE_TILE_SEGMENTS = 6,
-       TWA_TUNE_BUILD_PANEL = 7, TWA_TUNE_LIFT_VECTORS = 8, TWA_TUNE_SLAB_ROWS = 9 };
+       TWA_TUNE_BUILD_PANEL = 7, TWA_TUNE_LIFT_VECTORS = 8, TWA_TUNE_SLAB_ROWS = 9,
+       TWA_TUNE_SCAN_CLUSTER = 10, TWA_TUNE_SCAN_CHANNELS = 11 };
 int twa_set_tuning(twa_ctx* ctx, int key, int value);
 
 /* Exercises the bounded wait every streaming kernel uses, without any fault: enqueues one block

@@ -241,6 +241,14 @@ int twa_set_tuning(twa_ctx* ctx, int key, int value) {
       if ((value & 65535) || static_cast<long long>(value) > TWA_SLAB_ROWS) return TWA_ERR_INVALID_ARG;
       ctx->tune_slab_rows = value;
       return TWA_OK;
+    case TWA_TUNE_SCAN_CLUSTER:
+      if (value != 0 && value != 1 && value != 2 && value != 4 && value != 8) return TWA_ERR_INVALID_ARG;
+      ctx->tune_scan_cluster = value;
+      return TWA_OK;
+    case TWA_TUNE_SCAN_CHANNELS:
+      if (value != 0 && value != 16 && value != 32 && value != 64) return TWA_ERR_INVALID_ARG;
+      ctx->tune_scan_channels = value;
+      return TWA_OK;
     case TWA_TUNE_WAIT_LIMIT_MS:
       ctx->wait_limit_ns = (value ? static_cast<unsigned long long>(value) : 2000ull) * 1000000ull;
       return TWA_OK;

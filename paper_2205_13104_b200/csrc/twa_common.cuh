@@ -32,6 +32,7 @@ struct twa_ctx {
   int tune_build_panel;       // resident basis build: 0 = panels of 8 columns, Gram form inside; 1 = column by column; 2 = panels, column sweeps inside
   int tune_lift_base_path;    // tensor-pipe lift, base / output vectors: 0 = choose, 1 = lanes, 2 = base through the ring, 3 = both
   int tune_slab_rows;         // stepping calls: rows per launch (0 = one launch up to TWA_MAX_LAUNCH_ROWS, slabs of 2^30 above)
+  int tune_scan_cluster, tune_scan_channels;      // gated scan: blocks along a sequence, channels of a block (0 = choose)
   cudaEvent_t* prof_events;   // 3 per recorded step, or null
   int prof_cap, prof_count;   // steps
   // state of a row-chunked basis build (twa_build_begin .. twa_build_end_pass)

@@ -14,46 +14,72 @@ namespace {
 struct __align__(16) Map {
   twa_f2 A, B;
   __device__ __forceinline__ twa_f2 of(twa_f2 v) const { return twa_fma2(A, v, B); }
+  __device__ __forceinline__ Map after(const Map& m) const { return {twa_mul2(A, m.A), of(m.B)}; }
 };
+// Of a warp's segments, joined in the order in which they are met (FORWARD: from the first): every lane's with those before its own,
+// and, as `before`, those before alone.
+template <bool FORWARD, int SEGS>
+__device__ __forceinline__ Map join_segments(Map m, int seg, Map& before) {
+  before = {twa_pair(1.0f), 0};
+  if constexpr (SEGS > 1) {
+    constexpr int LANES = 32 / SEGS;
+    const int met = FORWARD ? seg : SEGS - 1 - seg;
+    auto from = [&](const Map& v, int lanes) {
+      Map r;
+      r.A = FORWARD ? __shfl_up_sync(0xffffffffu, v.A, lanes) : __shfl_down_sync(0xffffffffu, v.A, lanes);
+      r.B = FORWARD ? __shfl_up_sync(0xffffffffu, v.B, lanes) : __shfl_down_sync(0xffffffffu, v.B, lanes);
+      return r;
+    };
+#pragma unroll
+    for (int o = 1; o < SEGS; o *= 2) {
+      const Map prev = from(m, o * LANES);
+      if (met >= o) m = m.after(prev);
+    }
+    const Map prev = from(m, LANES);
+    if (met) before = prev;
+  }
+  return m;
+}
 
 // What the segments of a tile make of what enters them (the state, or backward k), and what enters the next tile: twice, so that the
 // next ones go beside those being read.
+template <int PAIRS>
 struct Joins {
-  Map seg[2][SCAN_WARPS][32];
-  twa_f2 carry[2][32];
+  Map seg[2][SCAN_WARPS][PAIRS];
+  twa_f2 carry[2][PAIRS];
 };
 // The same of the tiles of a cluster's blocks.
+template <int PAIRS>
 struct Tiles {
-  Map tile[2][MAX_CLUSTER][32];
+  Map tile[2][MAX_CLUSTER][PAIRS];
 };
 
 // The blocks of a cluster tell each other what their tiles make of a state: every warp joins its block's segments' maps, from the
 // first on (FORWARD) or from the last, and the warp of each rank stores the tile's into that block.
-template <bool FORWARD, int FEED>
-__device__ __forceinline__ void share_tile(const Joins& joins, Tiles& tiles, const Place<FEED>& at, int turn) {
+template <bool FORWARD, int FEED, int CH>
+__device__ __forceinline__ void share_tile(const Joins<CH / 2>& joins, Tiles<CH / 2>& tiles, const Place<FEED, CH>& at, int turn) {
   if (at.warp < at.ranks) {
-    Map all = joins.seg[turn][FORWARD ? 0 : SCAN_WARPS - 1][at.lane];
+    Map all = joins.seg[turn][FORWARD ? 0 : SCAN_WARPS - 1][at.pair];
 #pragma unroll
-    for (int i = 1; i < SCAN_WARPS; ++i) {
-      const Map m = joins.seg[turn][FORWARD ? i : SCAN_WARPS - 1 - i][at.lane];
-      all.A = twa_mul2(m.A, all.A);
-      all.B = m.of(all.B);
+    for (int i = 1; i < SCAN_WARPS; ++i) all = joins.seg[turn][FORWARD ? i : SCAN_WARPS - 1 - i][at.pair].after(all);
+    if (at.seg == 0) {
+      twa_store_remote(&tiles.tile[turn][at.rank][at.pair].A, at.warp, all.A);
+      twa_store_remote(&tiles.tile[turn][at.rank][at.pair].B, at.warp, all.B);
     }
-    twa_store_remote(&tiles.tile[turn][at.rank][at.lane].A, at.warp, all.A);
-    twa_store_remote(&tiles.tile[turn][at.rank][at.lane].B, at.warp, all.B);
   }
   twa_cluster_sync();
 }
 static_assert(MAX_CLUSTER <= SCAN_WARPS, "a warp for every rank");
 
-template <typename T, int FEED>
+template <typename T, int FEED, int CH>
 struct ScanForward {
   static constexpr int STAGES = 3;
   static constexpr bool TOGETHER = FEED != BY_ELEMENTS;
   static constexpr int N = SEG<T>;
-  typedef Ring<T, FEED, 2, STAGES> Rows;
+  static constexpr int SEGS = SCAN_CHANNELS / CH, WARP_ROWS = SEGS * N, TILE = SCAN_WARPS * WARP_ROWS;       // rows
+  typedef Ring<T, FEED, CH, 2, STAGES> Rows;
   const ScanArgs& a;
-  const Place<FEED> at;
+  const Place<FEED, CH> at;
   twa_f2 A[N], L[N];                               // of the rows up to each
 
   __device__ __forceinline__ ScanForward(const ScanArgs& args, int slice) : a(args), at(args, slice) {}
@@ -109,18 +135,18 @@ struct ScanForward {
     ring.copy(array, from, ld, rows, left, first, first + (a.tokens - 1) * ld + a.channels - 1);
   }
   // A sequence by the whole cluster.
-  __device__ __forceinline__ void whole(const Span& s, int seq, char* shared, Joins& joins, Tiles& tiles, int& turn) {
+  __device__ __forceinline__ void whole(const Span& s, int seq, char* shared, Joins<CH / 2>& joins, Tiles<CH / 2>& tiles, int& turn) {
     Rows ring(shared, at.warp, at.lane);
-    const int stride = SCAN_ROWS<T> * at.ranks, left = a.channels - at.slice;
-    const bool wide = __all_sync(0xffffffffu, at.n == 2);
-    int ahead = at.rank * SCAN_ROWS<T> + at.warp * N;                     // row of the next segment to be fetched
+    const int stride = TILE * at.ranks, left = a.channels - at.slice;
+    const bool wide = __all_sync(0xffffffffu, at.n == 2), last_seg = at.warp == SCAN_WARPS - 1 && at.seg == SEGS - 1;
+    int ahead = at.rank * TILE + at.warp * WARP_ROWS;                     // row of the warp's next segments to be fetched
     ring.lies(0, static_cast<const T*>(a.x) + (s.begin + ahead) * a.ldx + at.slice, a.ldx);
     ring.lies(1, static_cast<const T*>(a.f) + (s.begin + ahead) * a.ldf + at.slice, a.ldf);
     const T* x = Rows::own(static_cast<const T*>(a.x) + (s.begin + ahead) * a.ldx + at.slice, a.ldx);
     const T* f = Rows::own(static_cast<const T*>(a.f) + (s.begin + ahead) * a.ldf + at.slice, a.ldf);
     T* h = Rows::own(static_cast<T*>(a.h) + (s.begin + ahead) * a.ldh + at.slice, a.ldh);
     auto fetch = [&]() {
-      const int rows = scan_rows<T>(s, ahead);
+      const int rows = scan_rows(s, ahead, WARP_ROWS);
       if (rows) {
         copy(ring, 0, x, a.x, a.ldx, rows, left);
         copy(ring, 1, f, a.f, a.ldf, rows, left);
@@ -133,14 +159,16 @@ struct ScanForward {
 #pragma unroll
     for (int i = 0; i < Rows::AHEAD; ++i) fetch();
     twa_f2 state = at.state(a.h0, seq, a.channels);
-    if (at.warp == SCAN_WARPS - 1) joins.carry[turn ^ 1][at.lane] = state;
-    int slot = scan_slot<T>(s, seq) + at.rank * SCAN_WARPS + at.warp;
-    for (int t = 0; t < s.len; t += stride, slot += at.ranks * SCAN_WARPS, h += stride * a.ldh) {
-      const int mine = t + at.rank * SCAN_ROWS<T> + at.warp * N, rows = scan_rows<T>(s, mine);
+    if (last_seg) joins.carry[turn ^ 1][at.pair] = state;
+    int slot = scan_slot<T>(s, seq) + (at.rank * SCAN_WARPS + at.warp) * SEGS + at.seg;
+    for (int t = 0; t < s.len; t += stride, slot += at.ranks * SCAN_WARPS * SEGS, h += stride * a.ldh) {
+      const int first = t + at.rank * TILE + at.warp * WARP_ROWS, mine = first + at.seg * N;
+      const bool full = first + WARP_ROWS <= s.len;                       // the whole warp's rows exist
+      const int rows = scan_rows(s, mine, N);
       ring.wait();
       fetch();
       Map end;
-      if (rows == N) {
+      if (full) {
 #pragma unroll
         for (int i = 0; i < N; ++i) row(i, ring.get(0, i), ring.get(1, i));
         end = {A[N - 1], L[N - 1]};
@@ -150,7 +178,9 @@ struct ScanForward {
           if (i < rows) row(i, ring.get(0, i), ring.get(1, i));
         end = last(rows);
       }
-      joins.seg[turn][at.warp][at.lane] = end;
+      Map before;
+      const Map upto = join_segments<true, SEGS>(end, at.seg, before);
+      if (at.seg == SEGS - 1) joins.seg[turn][at.warp][at.pair] = upto;
       __syncthreads();
       twa_f2 in;
       if (at.ranks > 1) {
@@ -158,18 +188,19 @@ struct ScanForward {
         in = state;
         for (int r = 0; r < at.ranks; ++r) {
           if (r == at.rank) in = state;
-          state = tiles.tile[turn][r][at.lane].of(state);
+          state = tiles.tile[turn][r][at.pair].of(state);
         }
       } else {
-        in = joins.carry[turn ^ 1][at.lane];
+        in = joins.carry[turn ^ 1][at.pair];
       }
 #pragma unroll
       for (int w = 0; w < SCAN_WARPS - 1; ++w)
-        if (w < at.warp) in = joins.seg[turn][w][at.lane].of(in);
+        if (w < at.warp) in = joins.seg[turn][w][at.pair].of(in);
+      if (SEGS > 1) in = before.of(in);
       if (rows) keep_state(at, a.states, slot, a.channels, in);
-      if (at.ranks == 1 && at.warp == SCAN_WARPS - 1) joins.carry[turn][at.lane] = state = end.of(in);
+      if (at.ranks == 1 && last_seg) joins.carry[turn][at.pair] = state = end.of(in);
       turn ^= 1;
-      if (FEED == BY_UNITS && rows == N && wide) {
+      if (FEED == BY_UNITS && full && wide) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
           float lo, hi;
@@ -183,18 +214,19 @@ struct ScanForward {
       }
       ring.done();
     }
-    if (at.warp == SCAN_WARPS - 1 && at.rank == 0) at.keep(a.h_last, seq, a.channels, state);
+    if (last_seg && at.rank == 0) at.keep(a.h_last, seq, a.channels, state);
   }
 };
 
-template <typename T, int FEED>
+template <typename T, int FEED, int CH>
 struct ScanBackward {
   static constexpr int STAGES = 2;
   static constexpr bool TOGETHER = FEED != BY_ELEMENTS;
   static constexpr int N = SEG<T>;
-  typedef Ring<T, FEED, 3, STAGES> Rows;
+  static constexpr int SEGS = SCAN_CHANNELS / CH, WARP_ROWS = SEGS * N, TILE = SCAN_WARPS * WARP_ROWS;
+  typedef Ring<T, FEED, CH, 3, STAGES> Rows;
   const ScanArgs& a;
-  const Place<FEED> at;
+  const Place<FEED, CH> at;
   twa_f2 n[N], e[N];                               // gates; a (1 - a) (h_{t-1} - x_t)
 
   __device__ __forceinline__ ScanBackward(const ScanArgs& args, int slice) : a(args), at(args, slice) {}
@@ -267,11 +299,11 @@ struct ScanBackward {
     const T* first = static_cast<const T*>(all);
     ring.copy(array, from, ld, rows, left, first, first + (a.tokens - 1) * ld + a.channels - 1);
   }
-  __device__ __forceinline__ void whole(const Span& s, int seq, char* shared, Joins& joins, Tiles& tiles, int& turn) {
+  __device__ __forceinline__ void whole(const Span& s, int seq, char* shared, Joins<CH / 2>& joins, Tiles<CH / 2>& tiles, int& turn) {
     Rows ring(shared, at.warp, at.lane);
-    const int stride = SCAN_ROWS<T> * at.ranks, rounds = (s.len + stride - 1) / stride, left = a.channels - at.slice;
-    const bool wide = __all_sync(0xffffffffu, at.n == 2);
-    int ahead = (rounds - 1) * stride + at.rank * SCAN_ROWS<T> + at.warp * N;
+    const int stride = TILE * at.ranks, rounds = (s.len + stride - 1) / stride, left = a.channels - at.slice;
+    const bool wide = __all_sync(0xffffffffu, at.n == 2), first_seg = at.warp == 0 && at.seg == 0;
+    int ahead = (rounds - 1) * stride + at.rank * TILE + at.warp * WARP_ROWS;
     ring.lies(0, static_cast<const T*>(a.x) + (s.begin + ahead) * a.ldx + at.slice, a.ldx);
     ring.lies(1, static_cast<const T*>(a.f) + (s.begin + ahead) * a.ldf + at.slice, a.ldf);
     ring.lies(2, static_cast<const T*>(a.dh) + (s.begin + ahead) * a.lddh + at.slice, a.lddh);
@@ -280,8 +312,11 @@ struct ScanBackward {
     const T* g = Rows::own(static_cast<const T*>(a.dh) + (s.begin + ahead) * a.lddh + at.slice, a.lddh);
     T* dx = Rows::own(static_cast<T*>(a.dx) + (s.begin + ahead) * a.lddx + at.slice, a.lddx);
     T* df = Rows::own(static_cast<T*>(a.df) + (s.begin + ahead) * a.lddf + at.slice, a.lddf);
+    // the state before the next segment, fetched one tile ahead
+    int slot = scan_slot<T>(s, seq) + ((rounds - 1) * at.ranks + at.rank) * SCAN_WARPS * SEGS + at.warp * SEGS + at.seg;
+    twa_f2 next = rounds && ahead + at.seg * N < s.len ? kept_state(at, a.states, slot, a.channels) : 0;
     auto fetch = [&]() {
-      const int rows = ahead < 0 ? 0 : scan_rows<T>(s, ahead);
+      const int rows = ahead < 0 ? 0 : scan_rows(s, ahead, WARP_ROWS);
       if (rows) {
         copy(ring, 0, x, a.x, a.ldx, rows, left);
         copy(ring, 1, f, a.f, a.ldf, rows, left);
@@ -296,18 +331,16 @@ struct ScanBackward {
 #pragma unroll
     for (int i = 0; i < Rows::AHEAD; ++i) fetch();
     twa_f2 k = at.state(a.d_last, seq, a.channels);
-    if (at.warp == 0) joins.carry[turn ^ 1][at.lane] = k;
-    // the state before the next segment, fetched one tile ahead
-    int slot = scan_slot<T>(s, seq) + ((rounds - 1) * at.ranks + at.rank) * SCAN_WARPS + at.warp;
-    twa_f2 next = rounds && scan_rows<T>(s, (rounds - 1) * stride + at.rank * SCAN_ROWS<T> + at.warp * N) ? kept_state(at, a.states, slot, a.channels) : 0;
+    if (first_seg) joins.carry[turn ^ 1][at.pair] = k;
     for (int round = rounds - 1; round >= 0; --round, dx -= stride * a.lddx, df -= stride * a.lddf) {
-      const int mine = round * stride + at.rank * SCAN_ROWS<T> + at.warp * N, rows = scan_rows<T>(s, mine);
+      const int first = round * stride + at.rank * TILE + at.warp * WARP_ROWS, mine = first + at.seg * N;
+      const bool full = first + WARP_ROWS <= s.len;
+      const int rows = scan_rows(s, mine, N);
       twa_f2 h = next;
       ring.wait();
       fetch();
       Map off = {twa_pair(1.0f), 0};
-      const bool full = rows == N && wide;
-      if (rows == N) {
+      if (full) {
 #pragma unroll
         for (int i = 0; i < N; ++i) row(i, ring.get(0, i), ring.get(1, i), ring.get(2, i), h, off);
       } else {
@@ -315,8 +348,10 @@ struct ScanBackward {
         for (int i = 0; i < N; ++i)
           if (i < rows) row(i, ring.get(0, i), ring.get(1, i), ring.get(2, i), h, off);
       }
-      joins.seg[turn][at.warp][at.lane] = off;
-      slot -= at.ranks * SCAN_WARPS;
+      Map behind;
+      const Map upto = join_segments<false, SEGS>(off, at.seg, behind);
+      if (at.seg == 0) joins.seg[turn][at.warp][at.pair] = upto;
+      slot -= at.ranks * SCAN_WARPS * SEGS;
       next = round ? kept_state(at, a.states, slot, a.channels) : 0;
       __syncthreads();
       twa_f2 in;
@@ -325,17 +360,18 @@ struct ScanBackward {
         in = k;
         for (int r = at.ranks - 1; r >= 0; --r) {
           if (r == at.rank) in = k;
-          k = tiles.tile[turn][r][at.lane].of(k);
+          k = tiles.tile[turn][r][at.pair].of(k);
         }
       } else {
-        in = joins.carry[turn ^ 1][at.lane];
+        in = joins.carry[turn ^ 1][at.pair];
       }
 #pragma unroll
       for (int w = SCAN_WARPS - 1; w > 0; --w)
-        if (w > at.warp) in = joins.seg[turn][w][at.lane].of(in);
-      if (at.ranks == 1 && at.warp == 0) joins.carry[turn][at.lane] = k = off.of(in);
+        if (w > at.warp) in = joins.seg[turn][w][at.pair].of(in);
+      if (SEGS > 1) in = behind.of(in);
+      if (at.ranks == 1 && first_seg) joins.carry[turn][at.pair] = k = off.of(in);
       turn ^= 1;
-      if (FEED == BY_UNITS && full) {
+      if (FEED == BY_UNITS && full && wide) {
 #pragma unroll
         for (int i = N - 1; i >= 0; --i)
           back(i, ring.get(2, i).both(), in, [&](float x0, float x1, float f0, float f1) {
@@ -350,15 +386,16 @@ struct ScanBackward {
       }
       ring.done();
     }
-    if (at.warp == 0 && at.rank == 0) at.keep(a.dh0, seq, a.channels, k);
+    if (first_seg && at.rank == 0) at.keep(a.dh0, seq, a.channels, k);
   }
 };
 
 // GROUP sequences of a slice of channels a block.  The ones of at most SEG rows go to one warp each, the others to the block.
-template <typename Direction, int GROUP, typename J>
-__device__ __forceinline__ void scan_block(const ScanArgs& a, J& joins) {
+template <typename Direction, int CH, int GROUP>
+__device__ __forceinline__ void scan_block(const ScanArgs& a) {
   extern __shared__ __align__(16) char shared[];
-  Tiles& tiles = *reinterpret_cast<Tiles*>(shared + Direction::Rows::BLOCK_BYTES);         // of clusters only
+  __shared__ Joins<CH / 2> joins;
+  Tiles<CH / 2>& tiles = *reinterpret_cast<Tiles<CH / 2>*>(shared + Direction::Rows::BLOCK_BYTES);         // of clusters only
   const unsigned task = blockIdx.x / a.cluster;
   const int slice = task % a.slices, first = task / a.slices * GROUP;
   Direction d(a, slice);
@@ -379,17 +416,15 @@ __device__ __forceinline__ void scan_block(const ScanArgs& a, J& joins) {
   }
 }
 
-template <typename T, int FEED, int GROUP>
+template <typename T, int FEED, int CH, int GROUP>
 __global__ void __launch_bounds__(SCAN_THREADS, 2) scan_forward_kernel(ScanArgs a) {
   twa_begin(a.x, a.f, a.starts, a.h0);
-  __shared__ Joins joins;
-  scan_block<ScanForward<T, FEED>, GROUP>(a, joins);
+  scan_block<ScanForward<T, FEED, CH>, CH, GROUP>(a);
 }
-template <typename T, int FEED, int GROUP>
+template <typename T, int FEED, int CH, int GROUP>
 __global__ void __launch_bounds__(SCAN_THREADS, 2) scan_backward_kernel(ScanArgs a) {
   twa_begin(a.x, a.f, a.dh, a.starts, a.states, a.d_last);
-  __shared__ Joins joins;
-  scan_block<ScanBackward<T, FEED>, GROUP>(a, joins);
+  scan_block<ScanBackward<T, FEED, CH>, CH, GROUP>(a);
 }
 
 // How rows of two pointers and strides can be fetched together.
@@ -398,10 +433,10 @@ int scan_feed(const void* p, long long ld, size_t size, int channels, int so_far
   if (so_far == BY_PAIRS && (channels % 2 || twa_misaligned_to(p, 2 * size) || ld % 2)) so_far = BY_ELEMENTS;
   return so_far;
 }
-template <typename T, int FEED, int GROUP>
+template <typename T, int FEED, int CH, int GROUP>
 cudaError_t scan_launch(twa_ctx* ctx, const ScanArgs& a, bool back) {
-  auto kernel = back ? scan_backward_kernel<T, FEED, GROUP> : scan_forward_kernel<T, FEED, GROUP>;
-  const size_t smem = (back ? ScanBackward<T, FEED>::Rows::BLOCK_BYTES : ScanForward<T, FEED>::Rows::BLOCK_BYTES) + (a.cluster > 1 ? sizeof(Tiles) : 0);
+  auto kernel = back ? scan_backward_kernel<T, FEED, CH, GROUP> : scan_forward_kernel<T, FEED, CH, GROUP>;
+  const size_t smem = (back ? ScanBackward<T, FEED, CH>::Rows::BLOCK_BYTES : ScanForward<T, FEED, CH>::Rows::BLOCK_BYTES) + (a.cluster > 1 ? sizeof(Tiles<CH / 2>) : 0);
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
   if (e != cudaSuccess) return e;
   const unsigned blocks = static_cast<unsigned>(twa_ceil_div(a.sequences, GROUP) * a.slices * a.cluster);
@@ -410,16 +445,27 @@ cudaError_t scan_launch(twa_ctx* ctx, const ScanArgs& a, bool back) {
 constexpr int SCAN_RESIDENT = 2;                   // blocks of an SM
 template <typename T>
 cudaError_t scan_launch(twa_ctx* ctx, ScanArgs& a, bool back, int feed) {
-  const bool brief = a.tokens <= 2LL * SEG<T> * a.sequences;
   a.cluster = 1;
-  while (!brief && a.cluster < MAX_CLUSTER && a.tokens > 2LL * a.cluster * SCAN_ROWS<T> * a.sequences &&
-         2LL * a.sequences * a.slices * a.cluster <= SCAN_RESIDENT * ctx->sm_count)
-    a.cluster *= 2;
-  if (brief)
-    return feed == BY_UNITS ? scan_launch<T, BY_UNITS, SHORT_GROUP>(ctx, a, back)
-                            : (feed == BY_PAIRS ? scan_launch<T, BY_PAIRS, SHORT_GROUP>(ctx, a, back) : scan_launch<T, BY_ELEMENTS, SHORT_GROUP>(ctx, a, back));
-  return feed == BY_UNITS ? scan_launch<T, BY_UNITS, 1>(ctx, a, back)
-                          : (feed == BY_PAIRS ? scan_launch<T, BY_PAIRS, 1>(ctx, a, back) : scan_launch<T, BY_ELEMENTS, 1>(ctx, a, back));
+  if (a.tokens <= 2LL * SEG<T> * a.sequences) {
+    a.slices = static_cast<int>(twa_ceil_div(a.channels, SCAN_CHANNELS));
+    return feed == BY_UNITS ? scan_launch<T, BY_UNITS, SCAN_CHANNELS, SHORT_GROUP>(ctx, a, back)
+                            : (feed == BY_PAIRS ? scan_launch<T, BY_PAIRS, SCAN_CHANNELS, SHORT_GROUP>(ctx, a, back)
+                                                : scan_launch<T, BY_ELEMENTS, SCAN_CHANNELS, SHORT_GROUP>(ctx, a, back));
+  }
+  int channels = SCAN_CHANNELS;
+  auto blocks = [&]() { return twa_ceil_div(a.channels, channels) * a.sequences * a.cluster; };
+  auto rows = [&]() { return a.cluster * SCAN_WARPS * SEG<T> * (SCAN_CHANNELS / channels); };       // of a round
+  auto more = [&]() { return 2 * blocks() <= SCAN_RESIDENT * ctx->sm_count && a.tokens > 2LL * rows() * a.sequences; };
+  if (ctx->tune_scan_channels && feed == BY_UNITS) channels = ctx->tune_scan_channels;
+  else if (feed == BY_UNITS && more()) channels = 32;
+  while (a.cluster < MAX_CLUSTER && more()) a.cluster *= 2;
+  if (!ctx->tune_scan_channels && channels == 32 && more()) channels = 16;
+  if (ctx->tune_scan_cluster) a.cluster = ctx->tune_scan_cluster;
+  a.slices = static_cast<int>(twa_ceil_div(a.channels, channels));
+  if (feed == BY_PAIRS) return scan_launch<T, BY_PAIRS, SCAN_CHANNELS, 1>(ctx, a, back);
+  if (feed == BY_ELEMENTS) return scan_launch<T, BY_ELEMENTS, SCAN_CHANNELS, 1>(ctx, a, back);
+  return channels == 64 ? scan_launch<T, BY_UNITS, 64, 1>(ctx, a, back)
+                        : (channels == 32 ? scan_launch<T, BY_UNITS, 32, 1>(ctx, a, back) : scan_launch<T, BY_UNITS, 16, 1>(ctx, a, back));
 }
 
 // Arguments that both directions have.
@@ -429,7 +475,7 @@ int scan_check(twa_ctx* ctx, int dtype, int64_t tokens, int channels, const void
   if (!starts && (sequences ? tokens % sequences : tokens)) return TWA_ERR_INVALID_ARG;
   if (starts && twa_misaligned_to(starts, twa_itype_size(s_type))) return TWA_ERR_MISALIGNED;
   // blocks of a launch
-  if (static_cast<long long>(sequences) * twa_ceil_div(channels, SCAN_CHANNELS) * MAX_CLUSTER > 0x7FFFFFFFLL) return TWA_ERR_UNSUPPORTED;
+  if (static_cast<long long>(sequences) * twa_ceil_div(channels, SCAN_LEAST_CHANNELS) * MAX_CLUSTER > 0x7FFFFFFFLL) return TWA_ERR_UNSUPPORTED;
   return TWA_OK;
 }
 
@@ -461,7 +507,6 @@ int twa_gated_scan(twa_ctx* ctx, const void* x, int64_t ldx, const void* f, int6
   ScanArgs a = {};
   a.x = x, a.ldx = ldx, a.f = f, a.ldf = ldf, a.h = h, a.ldh = ldh;
   a.tokens = tokens, a.channels = channels, a.starts = starts, a.s_type = s_type, a.sequences = sequences;
-  a.slices = static_cast<int>(twa_ceil_div(channels, SCAN_CHANNELS));
   a.h0 = h0, a.h_last = h_last, a.states = static_cast<float*>(states), a.status = ctx->d_status;
   const int feed = scan_feed(h, ldh, size, channels, scan_feed(f, ldf, size, channels, scan_feed(x, ldx, size, channels, BY_UNITS)));
   TWA_CUDA_OK(ctx, dtype == TWA_BF16 ? scan_launch<bf16>(ctx, a, false, feed) : scan_launch<float>(ctx, a, false, feed));
@@ -487,7 +532,6 @@ int twa_gated_scan_backward(twa_ctx* ctx, const void* dh, int64_t lddh, const vo
   ScanArgs a = {};
   a.dh = dh, a.lddh = lddh, a.x = x, a.ldx = ldx, a.f = f, a.ldf = ldf, a.dx = dx, a.lddx = lddx, a.df = df, a.lddf = lddf;
   a.tokens = tokens, a.channels = channels, a.starts = starts, a.s_type = s_type, a.sequences = sequences;
-  a.slices = static_cast<int>(twa_ceil_div(channels, SCAN_CHANNELS));
   a.states = const_cast<float*>(static_cast<const float*>(states)), a.d_last = d_last, a.dh0 = dh0, a.status = ctx->d_status;
   int feed = scan_feed(dh, lddh, size, channels, scan_feed(f, ldf, size, channels, scan_feed(x, ldx, size, channels, BY_UNITS)));
   feed = scan_feed(df, lddf, size, channels, scan_feed(dx, lddx, size, channels, feed));

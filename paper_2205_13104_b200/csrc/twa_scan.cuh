@@ -8,9 +8,10 @@
 // is half a unit of the result; a gate rounded to 1 - 2^-24 k would err the same way step after step.  Steps in a row are
 // affine in the state that enters, h = A h_in + L; A comes from the same steps with x = 0 from 1, L with h_in = 0.
 //
-// A lane has two channels, a warp a segment of SEG rows of 64 channels, the warps of a block consecutive segments: a tile.  Every warp
-// takes its own segment from 0, the segments' (A, L) go through shared memory, and every thread joins those before its own with
-// the state that enters the tile.  States are float32.
+// A lane has two channels and SEG rows of them, a segment, which it takes from 0.  A slice of 64 channels gives every warp one
+// segment, one of 32 or 16 two or four, a lane's neighbours in other segments; the segments of a block follow each other and are its
+// tile.  A warp joins its segments' (A, L) by shuffles, the warps' go through shared memory, and every thread joins those before its
+// own with the state that enters the tile.  States are float32.
 #pragma once
 
 #include "twa_ops.cuh"
@@ -20,10 +21,8 @@ namespace {
 constexpr int SCAN_WARPS = 8, SCAN_THREADS = SCAN_WARPS * 32;
 template <typename T>
 constexpr int SEG = 32 / sizeof(T);                // rows of a segment
-template <typename T>
-constexpr int SCAN_ROWS = SCAN_WARPS * SEG<T>;     // of a tile
 constexpr int STATE_ROWS = SEG<float>;             // from one kept state to the next, at least
-constexpr int SCAN_CHANNELS = 64;                  // of a block
+constexpr int SCAN_CHANNELS = 64, SCAN_LEAST_CHANNELS = 16;               // of a block, at most and at least
 constexpr int SHORT_GROUP = SCAN_WARPS;            // sequences of a block where most are short
 constexpr int MAX_CLUSTER = 8;                     // blocks along a sequence
 
@@ -63,9 +62,8 @@ __device__ __forceinline__ Span scan_span(const ScanArgs& a, int seq, bool repor
 // (b + len) / R + 1 >= b / R + ceil(len / R).
 template <typename T>
 __device__ __forceinline__ int scan_slot(const Span& s, int seq) { return static_cast<int>(s.begin / SEG<T>) + seq; }
-// Rows that a sequence has from row r on, of a segment.
-template <typename T>
-__device__ __forceinline__ int scan_rows(const Span& s, int r) { return min(max(s.len - r, 0), SEG<T>); }
+// Rows that a sequence has from row r on, of `most`.
+__device__ __forceinline__ int scan_rows(const Span& s, int r, int most) { return min(max(s.len - r, 0), most); }
 
 // How rows are fetched, and which two channels a lane has.  In units of 16 bytes, any lane's, or in pairs: neighbouring channels,
 // loaded and stored together.  Element by element, where rows lie on no such boundary: channels 32 apart, so that a warp's accesses
@@ -160,16 +158,19 @@ __device__ __forceinline__ twa_f2 scan_step(twa_f2 n, twa_f2 h, twa_f2 x) { retu
 // a times v: what a step makes of a state where x is 0.
 __device__ __forceinline__ twa_f2 scan_decay(twa_f2 n, twa_f2 v) { return twa_fma2(n, v, scan_pick(n, v, twa_pair(0.0f))); }
 
-// Where a thread stands: its two channels, c and c + 1 or c and c + 32, of which n exist; its block's rank along the sequence.
-template <int FEED>
+// Where a thread stands: its two channels, c and c + 1 or c and c + 32, of which n exist; which of its warp's segments it has, and which
+// pair of the segment's channels; its block's rank along the sequence.
+template <int FEED, int CH>
 struct Place {
-  static constexpr int NEXT = FEED == BY_ELEMENTS ? 32 : 1;
-  int lane, warp, slice, c, n, rank, ranks;
+  static constexpr int NEXT = FEED == BY_ELEMENTS ? 32 : 1, SEGS = SCAN_CHANNELS / CH, PAIRS = CH / 2;
+  int lane, warp, slice, seg, pair, c, n, rank, ranks;
   __device__ __forceinline__ Place(const ScanArgs& a, int part) {
     lane = threadIdx.x & 31;
     warp = threadIdx.x >> 5;
-    slice = part * SCAN_CHANNELS;
-    c = slice + (FEED == BY_ELEMENTS ? lane : 2 * lane);
+    slice = part * CH;
+    seg = SEGS > 1 ? lane / PAIRS : 0;
+    pair = SEGS > 1 ? lane % PAIRS : lane;
+    c = slice + (FEED == BY_ELEMENTS ? lane : 2 * pair);
     n = (c < a.channels ? 1 : 0) + (c + NEXT < a.channels ? 1 : 0);
     ranks = a.cluster;
     rank = ranks > 1 ? static_cast<int>(twa_cluster_rank()) : 0;
@@ -189,39 +190,43 @@ struct Place {
 };
 
 // The states that the forward pass keeps: the same, but the buffer is the library's and begins on 16 bytes.
-template <int FEED>
-__device__ __forceinline__ twa_f2 kept_state(const Place<FEED>& at, const float* p, long long row, int channels) {
+template <int FEED, int CH>
+__device__ __forceinline__ twa_f2 kept_state(const Place<FEED, CH>& at, const float* p, long long row, int channels) {
   if (FEED == BY_ELEMENTS) return at.state(p, row, channels);
   twa_f2 v = 0;
   if (at.n > 0) v = *reinterpret_cast<const twa_f2*>(p + row * channels + at.c);
   return v;
 }
-template <int FEED>
-__device__ __forceinline__ void keep_state(const Place<FEED>& at, float* p, long long row, int channels, twa_f2 v) {
+template <int FEED, int CH>
+__device__ __forceinline__ void keep_state(const Place<FEED, CH>& at, float* p, long long row, int channels, twa_f2 v) {
   if (FEED == BY_ELEMENTS) at.keep(p, row, channels, v);
   else if (p && at.n > 0) *reinterpret_cast<twa_f2*>(p + row * channels + at.c) = v;
 }
 
-// A ring of a warp's segments in shared memory, STAGES deep, of ARRAYS matrices, filled by asynchronous copies.  By units, results go
+// A ring of a warp's segments in shared memory, STAGES deep, of ARRAYS matrices, filled by asynchronous copies.  A segment begins a
+// row's length behind the one before it, so that lanes of different segments read different banks.  By units, results go
 // out the same way: pairs into the stage that has been read, and from there 16 bytes a lane.
 // By elements, bfloat16 rows may begin between the 4-byte words that are the least an asynchronous copy takes.  Then a row's words
 // come as they lie, one more than a row has, and elements are found one place further; which rows those are changes with the
 // row's number where the stride is odd, and is the same for a segment's every tile.  A word that reaches out of the matrix,
 // before its first element or behind its last, is filled by the element.
-template <typename T, int FEED, int ARRAYS, int STAGES>
+template <typename T, int FEED, int CH, int ARRAYS, int STAGES>
 struct Ring {
-  static constexpr int N = SEG<T>;
+  static constexpr int N = SEG<T>, SEGS = SCAN_CHANNELS / CH;
+  static_assert(SEGS == 1 || FEED == BY_UNITS, "narrow slices by units only");
   static constexpr bool WORDS = FEED == BY_ELEMENTS && sizeof(T) == 2;
-  static constexpr int ROW = SCAN_CHANNELS * sizeof(T) + (WORDS ? 16 : 0), AREA = N * ROW, BYTES = ARRAYS * AREA;       // of a row, a matrix, a stage
+  static constexpr int ROW = CH * sizeof(T) + (WORDS ? 16 : 0), NEXT_SEG = (N + (SEGS > 1 ? 1 : 0)) * ROW;       // bytes
+  static constexpr int AREA = SEGS * NEXT_SEG, BYTES = ARRAYS * AREA;                                            // of a matrix, a stage
   static constexpr size_t BLOCK_BYTES = static_cast<size_t>(SCAN_WARPS) * STAGES * BYTES;
   static constexpr int AHEAD = STAGES - 1;        // segments under way before the first is waited for
-  static constexpr int V = 16 / static_cast<int>(sizeof(T)), UNITS = SCAN_CHANNELS / V, EACH = 32 / UNITS;       // units of a row, rows a warp copies at once
+  static constexpr int V = 16 / static_cast<int>(sizeof(T)), UNITS = CH / V, EACH = 32 / UNITS;       // units of a row, rows a warp copies at once
+  static_assert(FEED != BY_UNITS || N % EACH == 0, "a copy stays in its segment");
   char* base;
   int fill, read;                                 // bytes from the base: the stage to be filled, to be read
   int mine[WORDS ? ARRAYS : 1][WORDS ? 2 : 1];    // this lane's elements of a row, by the row's parity
 
   __device__ __forceinline__ Ring(char* shared, int warp, int lane) : base(shared + static_cast<size_t>(warp) * STAGES * BYTES), fill(0), read(0) {
-    if constexpr (!WORDS) mine[0][0] = lane * static_cast<int>(sizeof(T)) * (FEED == BY_ELEMENTS ? 1 : 2);
+    if constexpr (!WORDS) mine[0][0] = lane / (CH / 2) * NEXT_SEG + lane % (CH / 2) * static_cast<int>(sizeof(T)) * (FEED == BY_ELEMENTS ? 1 : 2);
   }
   // Says where a matrix's segments lie: p is the first element of one of them.
   __device__ __forceinline__ void lies(int array, const T* p, long long ld) {
@@ -252,8 +257,8 @@ struct Ring {
     if constexpr (FEED == BY_UNITS) {
       const int upto = lane % UNITS * V < channels ? rows - lane / UNITS : 0;
 #pragma unroll
-      for (int i = 0; i < N; i += EACH) {
-        if (i < upto) copy_async<16>(area + lane * 16 + i * ROW, from);
+      for (int i = 0; i < SEGS * N; i += EACH) {
+        if (i < upto) copy_async<16>(area + lane * 16 + i / N * NEXT_SEG + i % N * ROW, from);
         from += EACH * ld;
       }
     } else if constexpr (FEED == BY_PAIRS) {
@@ -323,8 +328,8 @@ struct Ring {
   __device__ __forceinline__ void flush(int array, T* to, long long ld) const {
     const char* from = base + read + array * AREA + (threadIdx.x & 31) * 16;
 #pragma unroll
-    for (int i = 0; i < N; i += EACH) {
-      *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(from + i * ROW);
+    for (int i = 0; i < SEGS * N; i += EACH) {
+      *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(from + i / N * NEXT_SEG + i % N * ROW);
       to += EACH * ld;
     }
   }

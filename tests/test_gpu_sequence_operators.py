@@ -270,6 +270,23 @@ def test_gated_scan_over_long_axes(ctx, sequences, length, channels, dtype, ragg
     ok(ctx)
 
 
+@pytest.mark.parametrize("cluster", [1, 2, 8])
+@pytest.mark.parametrize("channels", [16, 32, 64])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_gated_scan_however_it_is_shared(ctx, cluster, channels, dtype):
+    """Every number of blocks along a sequence and of channels a block, with ragged sequences, tails of channels and empty sequences."""
+    twa.twa_set_tuning(ctx, twa.TWA_TUNE_SCAN_CLUSTER, cluster)
+    twa.twa_set_tuning(ctx, twa.TWA_TUNE_SCAN_CHANNELS, channels)
+    try:
+        for state in (False, True):
+            test_gated_scan_and_its_gradient(ctx, [700, 1, 0, 1025, 130], 72, dtype, 0, 0, state)
+            test_gated_scan_and_its_gradient(ctx, [2100], 24, dtype, 8, 8, state)
+            test_gated_scan_and_its_gradient(ctx, [129, 400, 64], 71, dtype, 0, 1, state)
+    finally:
+        twa.twa_set_tuning(ctx, twa.TWA_TUNE_SCAN_CLUSTER, 0)
+        twa.twa_set_tuning(ctx, twa.TWA_TUNE_SCAN_CHANNELS, 0)
+
+
 def test_gated_scan_of_constant_gates_keeps_its_digits(ctx):
     """A gate next to one over many tokens: h_t = 1 - a^t for x = 1.  A gate held as a float32 would be off by 2^-25 each step."""
     n, q = 40000, torch.tensor([8.0, 9.0, 10.0, 11.0], device=DEV)
