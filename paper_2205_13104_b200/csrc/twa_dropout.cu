@@ -44,18 +44,23 @@ struct DropArgs {
 struct Words {
   uint32_t w[4];
 };
-__device__ __forceinline__ Words philox(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3, uint32_t k0, uint32_t k1) {
+// For N counters at once: the key's halves are the same for all.
+template <int N>
+__device__ __forceinline__ void philox(Words (&u)[N], uint32_t k0, uint32_t k1) {
 #pragma unroll
   for (int r = 0; r < 10; ++r) {
-    const unsigned long long p0 = static_cast<unsigned long long>(c0) * 0xD2511F53u, p1 = static_cast<unsigned long long>(c2) * 0xCD9E8D57u;
-    c0 = static_cast<uint32_t>(p1 >> 32) ^ c1 ^ k0;
-    c2 = static_cast<uint32_t>(p0 >> 32) ^ c3 ^ k1;
-    c1 = static_cast<uint32_t>(p1);
-    c3 = static_cast<uint32_t>(p0);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      uint32_t* c = u[i].w;
+      const unsigned long long p0 = static_cast<unsigned long long>(c[0]) * 0xD2511F53u, p1 = static_cast<unsigned long long>(c[2]) * 0xCD9E8D57u;
+      c[0] = static_cast<uint32_t>(p1 >> 32) ^ c[1] ^ k0;
+      c[2] = static_cast<uint32_t>(p0 >> 32) ^ c[3] ^ k1;
+      c[1] = static_cast<uint32_t>(p1);
+      c[3] = static_cast<uint32_t>(p0);
+    }
     k0 += 0x9E3779B9u;
     k1 += 0xBB67AE85u;
   }
-  return {{c0, c1, c2, c3}};
 }
 // Whether element e of the eight is kept.
 __device__ __forceinline__ bool drop_keeps(const Words& u, int e, uint32_t threshold) {
@@ -89,11 +94,13 @@ __global__ void __launch_bounds__(DROP_THREADS) dropout_kernel(DropArgs a) {
       if (RESIDUAL) add[k][i].load(res + row[k] * a.ldr + unit[k] * 8 + i * V);
     }
   }
+  Words u[DROP_UNITS];
+#pragma unroll
+  for (int k = 0; k < DROP_UNITS; ++k) u[k] = {{unit[k], a.row0 + row[k], a.site, static_cast<uint32_t>(step)}};
+  philox(u, static_cast<uint32_t>(seed), static_cast<uint32_t>(seed >> 32));
 #pragma unroll
   for (int k = 0; k < DROP_UNITS; ++k) {
     if (first + k * DROP_THREADS >= total) return;
-    const Words u = philox(unit[k], a.row0 + row[k], a.site, static_cast<uint32_t>(step), static_cast<uint32_t>(seed),
-                           static_cast<uint32_t>(seed >> 32));
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       float v[V], r[V];
@@ -102,7 +109,7 @@ __global__ void __launch_bounds__(DROP_THREADS) dropout_kernel(DropArgs a) {
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         const float kept = RESIDUAL ? fmaf(v[e], a.scale, r[e]) : v[e] * a.scale;
-        v[e] = drop_keeps(u, i * V + e, a.threshold) ? kept : (RESIDUAL ? r[e] : 0.0f);
+        v[e] = drop_keeps(u[k], i * V + e, a.threshold) ? kept : (RESIDUAL ? r[e] : 0.0f);
       }
       twa_pack<T, V>::store(y + row[k] * a.ldy + unit[k] * 8 + i * V, v);
     }
@@ -129,11 +136,11 @@ __global__ void __launch_bounds__(DROP_THREADS) dropout_any_kernel(DropArgs a) {
       if (RESIDUAL) add[k].load(res + row * a.ldr + c0 + k * 32);
     }
   const unsigned long long seed = __ldg(a.rng), step = __ldg(a.rng + 1);
-  const Words u = philox(part * 32 + lane, a.row0 + row, a.site, static_cast<uint32_t>(step), static_cast<uint32_t>(seed),
-                         static_cast<uint32_t>(seed >> 32));
+  Words u[1] = {{{part * 32 + lane, a.row0 + row, a.site, static_cast<uint32_t>(step)}}};
+  philox(u, static_cast<uint32_t>(seed), static_cast<uint32_t>(seed >> 32));
   unsigned bits = 0;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) bits |= (drop_keeps(u, e, a.threshold) ? 1u : 0u) << e;
+  for (int e = 0; e < 8; ++e) bits |= (drop_keeps(u[0], e, a.threshold) ? 1u : 0u) << e;
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
     const bool keep = __shfl_sync(0xffffffffu, bits, 4 * k + (lane >> 3)) >> (lane & 7) & 1;

@@ -6,24 +6,24 @@
 //   combine backward   dy[place[t, j]] = w[t, j] dout[t],   dw[t, j] = sum dout[t] y[place[t, j]]
 //
 // The sort is a counting sort by one cluster of blocks in its shared memory, one launch whatever the number: every warp has a
-// run of assignments and counts them by expert, 32 at a time (lanes of the same expert find each other by a match, the first of
-// them adds their number), a prefix over warps, blocks and experts gives every warp its first place for every expert, and a
-// second walk gives places out.  No count depends on which block came first.  What moves rows is bound by memory and
-// goes token by token, so that a token's row is read, or written, once for all its experts.
+// run of assignments and counts them by expert, 32 at a time: lanes of the same expert find each other by one ballot for every bit of
+// its number, the first of them adds how many they are.  An assignment's place among its warp's goes to where its place will be; a
+// prefix over warps, blocks and experts gives what is to be added to it.  No count depends on which block came first.
+// Where there are few assignments every block sorts them all and moves its own tokens' rows at once.
+// What moves rows is bound by memory and goes token by token, so that a token's row is read, or written, once for all its experts.
 #include "twa_ops.cuh"
 
 namespace {
 
 // ---- the sort -----------------------------------------------------------------------------------
-constexpr int SORT_THREADS = 512, SORT_WARPS = SORT_THREADS / 32;
-constexpr int SORT_LOADS = 4;                     // ids of a lane under way together
+constexpr int SORT_THREADS = 1024, SORT_WARPS = SORT_THREADS / 32;
+constexpr int SORT_LOADS = 8;                     // ids of a lane under way together
 
 struct SortArgs {
   const void* ids;
   int itype;
-  long long tokens;
-  int count, top, experts;                        // count: assignments
-  int warps;                                      // of a block that take part (shared memory holds a count of each expert for each)
+  int count, top, experts, bits;                  // count: assignments; bits: of an expert's number, or `experts` for none
+  int warps;                                      // of a block (shared memory holds a count of each expert for each of them)
   int run;                                        // assignments of a warp
   int* place;
   int* order;
@@ -31,42 +31,58 @@ struct SortArgs {
   int* status;
 };
 
-// Expert of an assignment, -1 for none.
-__device__ __forceinline__ int expert_of(const SortArgs& a, long long i, bool report) {
+// Expert of an assignment, `experts` for none.
+__device__ __forceinline__ int expert_of(const SortArgs& a, int i, bool report) {
   const long long id = twa_load_id(a.ids, a.itype, i);
   if (id >= 0 && id < a.experts) return static_cast<int>(id);
-  if (report && id != -1) twa_set_status(a.status, TWA_ERR_INVALID_ARG, static_cast<int>(i / a.top));
-  return -1;
+  if (report && id != -1) twa_set_status(a.status, TWA_ERR_INVALID_ARG, i / a.top);
+  return a.experts;
 }
 
-__global__ void __launch_bounds__(SORT_THREADS) expert_sort_kernel(SortArgs a, int blocks) {
-  twa_begin(a.ids);
-  extern __shared__ int shared[];
+// Between the walks place holds an assignment's expert and its number among its warp's of that expert.
+constexpr int RANK_BITS = 21;
+static_assert(TWA_EXPERTS_MAX < 1 << (32 - RANK_BITS) && TWA_EXPERTS_MAX_ASSIGNMENTS / (8 * SORT_WARPS) + 32 < 1 << RANK_BITS, "both fit");
+
+// Sorts with `blocks` blocks, this one the rank-th.  place: where every assignment's place goes; `write`: whether this block writes
+// starts and, where it is wanted here, order.  shared: (warps + 3) x experts integers.
+__device__ __forceinline__ void sort_block(const SortArgs& a, int blocks, int rank, int* shared, int* place, bool write) {
   int* total = shared;                            // of this block, by expert
   int* base = total + a.experts;                  // place of this block's first assignment of an expert
-  int* count = base + a.experts;                  // [warps][experts]
-  const int rank = blocks > 1 ? static_cast<int>(twa_cluster_rank()) : 0;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  for (int i = threadIdx.x; i < a.warps * a.experts; i += SORT_THREADS) count[i] = 0;
+  int* all = base + a.experts;                    // of all blocks
+  int* count = all + a.experts;                   // [warps][experts]
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, threads = a.warps * 32;
+  for (int i = threadIdx.x; i < a.warps * a.experts; i += threads) count[i] = 0;
   __syncthreads();
   const long long from = static_cast<long long>(rank * a.warps + warp) * a.run;
-  const int first = warp < a.warps && from < a.count ? static_cast<int>(from) : a.count;
-  const int last = a.count - first < a.run ? a.count : first + a.run;
-  int* mine = count + (warp < a.warps ? warp * a.experts : 0);
+  const int first = from < a.count ? static_cast<int>(from) : a.count, last = a.count - first < a.run ? a.count : first + a.run;
+  int* mine = count + warp * a.experts;
   for (int i = first; i < last; i += 32 * SORT_LOADS) {
     int e[SORT_LOADS];
 #pragma unroll
-    for (int k = 0; k < SORT_LOADS; ++k) e[k] = i + k * 32 + lane < last ? expert_of(a, i + k * 32 + lane, true) : -1;
+    for (int k = 0; k < SORT_LOADS; ++k) e[k] = i + k * 32 + lane < last ? expert_of(a, i + k * 32 + lane, write) : a.experts;
 #pragma unroll
     for (int k = 0; k < SORT_LOADS; ++k) {
-      const unsigned same = __match_any_sync(0xffffffffu, e[k]);
-      if (e[k] >= 0 && (same & ((1u << lane) - 1)) == 0) mine[e[k]] += __popc(same);
+      if (i + k * 32 >= last) break;
+      unsigned same = 0xffffffffu;
+      for (int b = 0; b < a.bits; ++b) {
+        const bool set = e[k] >> b & 1;
+        const unsigned votes = __ballot_sync(0xffffffffu, set);
+        same &= set ? votes : ~votes;
+      }
+      const unsigned before = same & ((1u << lane) - 1);
+      int held = 0;
+      if (e[k] < a.experts) held = mine[e[k]];
       __syncwarp();
+      if (e[k] < a.experts && before == 0) mine[e[k]] = held + __popc(same);
+      __syncwarp();
+      if (i + k * 32 + lane < last)
+        place[i + k * 32 + lane] = static_cast<int>(static_cast<unsigned>(e[k]) << RANK_BITS | static_cast<unsigned>(held + __popc(before)));
     }
   }
   __syncthreads();
-  for (int e = threadIdx.x; e < a.experts; e += SORT_THREADS) {
+  for (int e = threadIdx.x; e < a.experts; e += threads) {
     int sum = 0;
+#pragma unroll 4
     for (int w = 0; w < a.warps; ++w) {
       const int c = count[w * a.experts + e];
       count[w * a.experts + e] = sum;
@@ -77,8 +93,7 @@ __global__ void __launch_bounds__(SORT_THREADS) expert_sort_kernel(SortArgs a, i
   if (blocks > 1) twa_cluster_sync();
   else __syncthreads();
   // assignments of every expert in all blocks, and of them those in blocks before this one
-  int* all = count + a.warps * a.experts;
-  for (int e = threadIdx.x; e < a.experts; e += SORT_THREADS) {
+  for (int e = threadIdx.x; e < a.experts; e += threads) {
     int before = 0, sum = 0;
     for (int r = 0; r < blocks; ++r) {
       const int c = r == rank ? total[e] : twa_remote(total + e, r);
@@ -102,58 +117,91 @@ __global__ void __launch_bounds__(SORT_THREADS) expert_sort_kernel(SortArgs a, i
       }
       if (e < a.experts) {
         base[e] += sum + upto - c;
-        if (rank == 0) a.starts[e] = sum + upto - c;
+        if (write && rank == 0) a.starts[e] = sum + upto - c;
       }
       sum += __shfl_sync(0xffffffffu, upto, 31);
     }
-    if (rank == 0 && lane == 0) a.starts[a.experts] = sum;
+    if (write && rank == 0 && lane == 0) a.starts[a.experts] = sum;
   }
   __syncthreads();
-  for (int i = first; i < last; i += 32 * SORT_LOADS) {
-    int e[SORT_LOADS];
+  for (int i = first + lane; i < last; i += 32 * SORT_LOADS) {
+    unsigned held[SORT_LOADS];
 #pragma unroll
-    for (int k = 0; k < SORT_LOADS; ++k) e[k] = i + k * 32 + lane < last ? expert_of(a, i + k * 32 + lane, false) : -1;
+    for (int k = 0; k < SORT_LOADS; ++k)
+      if (i + k * 32 < last) held[k] = static_cast<unsigned>(place[i + k * 32]);
 #pragma unroll
-    for (int k = 0; k < SORT_LOADS; ++k) {
-      const int n = i + k * 32 + lane;
-      const unsigned same = __match_any_sync(0xffffffffu, e[k]), before = same & ((1u << lane) - 1);
-      const int at = e[k] >= 0 ? base[e[k]] + mine[e[k]] + __popc(before) : -1;
-      __syncwarp();
-      if (e[k] >= 0 && before == 0) mine[e[k]] += __popc(same);
-      __syncwarp();
-      if (n < last) {
-        a.place[n] = at;
-        if (a.order && at >= 0) a.order[at] = n;
+    for (int k = 0; k < SORT_LOADS; ++k)
+      if (i + k * 32 < last) {
+        const int e = static_cast<int>(held[k] >> RANK_BITS);
+        const int at = e < a.experts ? base[e] + mine[e] + static_cast<int>(held[k] & ((1u << RANK_BITS) - 1)) : -1;
+        place[i + k * 32] = at;
+        if (write && a.order && at >= 0) a.order[at] = i + k * 32;
       }
-    }
   }
+}
+
+__global__ void __launch_bounds__(SORT_THREADS) expert_sort_kernel(SortArgs a, int blocks) {
+  twa_begin(a.ids);
+  extern __shared__ int shared[];
+  sort_block(a, blocks, blocks > 1 ? static_cast<int>(twa_cluster_rank()) : 0, shared, a.place, true);
 }
 
 // ---- rows to their experts ------------------------------------------------------------------------
 constexpr int MOVE_WARPS = 8;
 
-// A warp takes UNITS x 32 units of a token's row, as bytes.
+// Rows as units of type W.
+struct Rows {
+  const char* x;
+  char* out;
+  long long ldx, ldo, tokens;                     // strides in bytes
+  int units, parts, top;                          // parts: of a row, for one warp each
+};
+// A warp takes UNITS x 32 units of a token's row and stores them wherever `place` says.
 template <typename W, int UNITS>
-__global__ void __launch_bounds__(MOVE_WARPS * 32) expert_gather_kernel(const char* x, long long ldx, long long tokens, int units, int parts,
-                                                                         const int* place, int top, char* out, long long ldo) {
-  twa_begin(x, place);
-  const long long task = static_cast<long long>(blockIdx.x) * MOVE_WARPS + (threadIdx.x >> 5);
-  const long long t = task / parts;
-  if (t >= tokens) return;
-  const int lane = threadIdx.x & 31, u0 = static_cast<int>(task - t * parts) * (UNITS * 32) + lane;
-  const int mine = lane < top ? __ldg(place + t * top + lane) : -1;
-  const W* from = reinterpret_cast<const W*>(x + t * ldx);
+__device__ __forceinline__ void move_row(const Rows& r, long long t, int part, int place) {
+  const int u0 = part * (UNITS * 32) + (threadIdx.x & 31);
+  const W* from = reinterpret_cast<const W*>(r.x + t * r.ldx);
   W v[UNITS];
 #pragma unroll
   for (int k = 0; k < UNITS; ++k)
-    if (u0 + k * 32 < units) v[k] = __ldg(from + u0 + k * 32);
-  for (int j = 0; j < top; ++j) {
-    const int p = __shfl_sync(0xffffffffu, mine, j);
+    if (u0 + k * 32 < r.units) v[k] = __ldg(from + u0 + k * 32);
+  for (int j = 0; j < r.top; ++j) {
+    const int p = __shfl_sync(0xffffffffu, place, j);
     if (p < 0) continue;
-    W* to = reinterpret_cast<W*>(out + p * ldo);
+    W* to = reinterpret_cast<W*>(r.out + p * r.ldo);
 #pragma unroll
     for (int k = 0; k < UNITS; ++k)
-      if (u0 + k * 32 < units) to[u0 + k * 32] = v[k];
+      if (u0 + k * 32 < r.units) to[u0 + k * 32] = v[k];
+  }
+}
+
+template <typename W, int UNITS>
+__global__ void __launch_bounds__(MOVE_WARPS * 32) expert_gather_kernel(Rows r, const int* place, int* order) {
+  twa_begin(r.x, place);
+  const long long task = static_cast<long long>(blockIdx.x) * MOVE_WARPS + (threadIdx.x >> 5);
+  const long long t = task / r.parts;
+  if (t >= r.tokens) return;
+  const int lane = threadIdx.x & 31, part = static_cast<int>(task - t * r.parts), at = lane < r.top ? __ldg(place + t * r.top + lane) : -1;
+  if (order && part == 0 && at >= 0) order[at] = static_cast<int>(t) * r.top + lane;      // scattered: not for the sort's few SMs
+  move_row<W, UNITS>(r, t, part, at);
+}
+
+// Few assignments: every block sorts them, block 0 says so, and each moves its share of the rows.  A launch after a launch would cost
+// as much again (16 tokens of 512 bfloat16, two of eight experts).
+constexpr int SMALL_COUNT = 1024;                 // assignments
+template <typename W, int UNITS>
+__global__ void __launch_bounds__(MOVE_WARPS * 32) expert_small_kernel(SortArgs a, Rows r) {
+  twa_begin(a.ids, r.x);
+  extern __shared__ int shared[];
+  __shared__ int place[SMALL_COUNT];
+  sort_block(a, 1, 0, shared, place, blockIdx.x == 0);
+  __syncthreads();
+  if (blockIdx.x == 0)
+    for (int i = threadIdx.x; i < a.count; i += MOVE_WARPS * 32) a.place[i] = place[i];
+  const int lane = threadIdx.x & 31;
+  for (int task = blockIdx.x * MOVE_WARPS + (threadIdx.x >> 5); task < static_cast<int>(r.tokens) * r.parts; task += gridDim.x * MOVE_WARPS) {
+    const int t = task / r.parts;
+    move_row<W, UNITS>(r, t, task - t * r.parts, lane < r.top ? place[t * r.top + lane] : -1);
   }
 }
 
@@ -180,43 +228,54 @@ __device__ __forceinline__ int place_of(const CombineArgs& a, long long t, int j
   return p;
 }
 
-constexpr int COMBINE_LOADS = 4;                  // rows of a token under way together
-template <typename T, int E>
+// A warp takes UNITS x 32 packs of E elements of a token's row, JOIN of its experts' rows under way together.
+template <typename T, int E, int UNITS, int JOIN>
 __global__ void __launch_bounds__(MOVE_WARPS * 32) expert_combine_kernel(CombineArgs a) {
   twa_begin(a.y, a.place, a.weights);
   const long long task = static_cast<long long>(blockIdx.x) * MOVE_WARPS + (threadIdx.x >> 5);
   const long long t = task / a.parts;
   if (t >= a.tokens) return;
-  const int lane = threadIdx.x & 31, part = static_cast<int>(task - t * a.parts), c = (part * 32 + lane) * E;
+  const int lane = threadIdx.x & 31, part = static_cast<int>(task - t * a.parts), c0 = (part * UNITS * 32 + lane) * E;
   const int place = lane < a.top ? place_of(a, t, lane, part == 0) : -1;
   const float weight = lane < a.top ? (a.weights ? __ldg(a.weights + t * a.top + lane) : 1.0f) : 0.0f;
-  const T* y = static_cast<const T*>(a.y) + c;
-  float sum[E] = {};
-  for (int j0 = 0; j0 < a.top; j0 += COMBINE_LOADS) {
-    twa_pack<T, E> raw[COMBINE_LOADS];
-    int p[COMBINE_LOADS];
+  const T* y = static_cast<const T*>(a.y) + c0;
+  float sum[UNITS][E] = {};
+  for (int j0 = 0; j0 < a.top; j0 += JOIN) {
+    twa_pack<T, E> raw[JOIN][UNITS];
+    int p[JOIN];
 #pragma unroll
-    for (int k = 0; k < COMBINE_LOADS; ++k) {
+    for (int k = 0; k < JOIN; ++k) {
       p[k] = __shfl_sync(0xffffffffu, place, (j0 + k) & 31);
-      if (j0 + k >= a.top || c >= a.dim) p[k] = -1;
-      if (p[k] >= 0) raw[k].load(y + p[k] * a.ldy);
+      if (j0 + k >= a.top) p[k] = -1;
+      if (p[k] < 0) continue;
+      const T* row = y + p[k] * a.ldy;
+#pragma unroll
+      for (int u = 0; u < UNITS; ++u)
+        if (c0 + u * 32 * E < a.dim) raw[k][u].load(row + u * 32 * E);
     }
 #pragma unroll
-    for (int k = 0; k < COMBINE_LOADS; ++k) {
+    for (int k = 0; k < JOIN; ++k) {
       const float w = __shfl_sync(0xffffffffu, weight, (j0 + k) & 31);
       if (p[k] < 0) continue;
-      float v[E];
-      raw[k].widen(v);
 #pragma unroll
-      for (int e = 0; e < E; ++e) sum[e] = fmaf(w, v[e], sum[e]);
+      for (int u = 0; u < UNITS; ++u)
+        if (c0 + u * 32 * E < a.dim) {
+          float v[E];
+          raw[k][u].widen(v);
+#pragma unroll
+          for (int e = 0; e < E; ++e) sum[u][e] = fmaf(w, v[e], sum[u][e]);
+        }
     }
   }
-  if (c < a.dim) twa_pack<T, E>::store(static_cast<T*>(a.out) + t * a.ldo + c, sum);
+  T* out = static_cast<T*>(a.out) + t * a.ldo + c0;
+#pragma unroll
+  for (int u = 0; u < UNITS; ++u)
+    if (c0 + u * 32 * E < a.dim) twa_pack<T, E>::store(out + u * 32 * E, sum[u]);
 }
 
-// A token's row for a group of LANES threads (a warp, or the block): the dot products need the whole row.  BATCH experts at a time.
-constexpr int BACK_BATCH = 4;
-template <typename T, int E, int LANES>
+// A token's row for a group of LANES threads (a warp, or the block), UNITS packs of each at a time: the dot products need the whole row.
+// JOIN of its experts at a time.
+template <typename T, int E, int UNITS, int JOIN, int LANES>
 __global__ void __launch_bounds__(MOVE_WARPS * 32) expert_combine_backward_kernel(CombineArgs a) {
   twa_begin(a.y, a.dout, a.place, a.weights);
   __shared__ float part[LANES > 32 ? MOVE_WARPS : 1][32];
@@ -226,39 +285,50 @@ __global__ void __launch_bounds__(MOVE_WARPS * 32) expert_combine_backward_kerne
   const int place = lane < a.top ? place_of(a, t, lane, warp == 0 || LANES == 32) : -1;
   const float weight = lane < a.top ? __ldg(a.weights + t * a.top + lane) : 0.0f;
   const T* dout = static_cast<const T*>(a.dout) + t * a.ldd;
-  for (int j0 = 0; j0 < a.top; j0 += BACK_BATCH) {
-    int p[BACK_BATCH];
-    float w[BACK_BATCH], dot[BACK_BATCH];
+  for (int j0 = 0; j0 < a.top; j0 += JOIN) {
+    int p[JOIN];
+    float w[JOIN], dot[JOIN];
 #pragma unroll
-    for (int k = 0; k < BACK_BATCH; ++k) {
+    for (int k = 0; k < JOIN; ++k) {
       p[k] = __shfl_sync(0xffffffffu, place, (j0 + k) & 31);
       w[k] = __shfl_sync(0xffffffffu, weight, (j0 + k) & 31);
       if (j0 + k >= a.top) p[k] = -1;
       dot[k] = 0.0f;
     }
-    for (int c = at * E; c < a.dim; c += LANES * E) {
-      twa_pack<T, E> rd, ry[BACK_BATCH];
-      rd.load(dout + c);
+    for (int c = at * E; c < a.dim; c += UNITS * LANES * E) {
+      twa_pack<T, E> rd[UNITS], ry[JOIN][UNITS];
 #pragma unroll
-      for (int k = 0; k < BACK_BATCH; ++k)
-        if (p[k] >= 0) ry[k].load(static_cast<const T*>(a.y) + p[k] * a.ldy + c);
-      float d[E];
-      rd.widen(d);
+      for (int u = 0; u < UNITS; ++u)
+        if (c + u * LANES * E < a.dim) rd[u].load(dout + c + u * LANES * E);
 #pragma unroll
-      for (int k = 0; k < BACK_BATCH; ++k) {
-        if (p[k] < 0) continue;
-        float v[E];
-        ry[k].widen(v);
+      for (int k = 0; k < JOIN; ++k)
+        if (p[k] >= 0) {
+          const T* row = static_cast<const T*>(a.y) + p[k] * a.ldy + c;
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-          dot[k] = fmaf(d[e], v[e], dot[k]);
-          v[e] = w[k] * d[e];
+          for (int u = 0; u < UNITS; ++u)
+            if (c + u * LANES * E < a.dim) ry[k][u].load(row + u * LANES * E);
         }
-        twa_pack<T, E>::store(static_cast<T*>(a.out) + p[k] * a.ldo + c, v);
+#pragma unroll
+      for (int u = 0; u < UNITS; ++u) {
+        if (c + u * LANES * E >= a.dim) break;
+        float d[E];
+        rd[u].widen(d);
+#pragma unroll
+        for (int k = 0; k < JOIN; ++k) {
+          if (p[k] < 0) continue;
+          float v[E];
+          ry[k][u].widen(v);
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            dot[k] = fmaf(d[e], v[e], dot[k]);
+            v[e] = w[k] * d[e];
+          }
+          twa_pack<T, E>::store(static_cast<T*>(a.out) + p[k] * a.ldo + c + u * LANES * E, v);
+        }
       }
     }
 #pragma unroll
-    for (int k = 0; k < BACK_BATCH; ++k) {
+    for (int k = 0; k < JOIN; ++k) {
       const float sum = twa_warp_sum(dot[k]);
       if (LANES > 32) {
         if (lane == 0 && j0 + k < a.top) part[warp][j0 + k] = sum;
@@ -280,12 +350,44 @@ __global__ void __launch_bounds__(MOVE_WARPS * 32) expert_combine_backward_kerne
 
 bool on_unit(const void* p, long long ld_bytes, size_t unit) { return !twa_misaligned_to(p, unit) && ld_bytes % unit == 0; }
 
+// Moves rows as units of W, after the sort or (small) with it.
 template <typename W, int UNITS>
-void launch_gather(twa_ctx* ctx, const void* x, long long ldx, long long tokens, long long bytes, const int* place, int top, void* out,
-                   long long ldo) {
-  const int units = static_cast<int>(bytes / sizeof(W)), parts = static_cast<int>(twa_ceil_div(units, UNITS * 32));
-  twa_launch(ctx->stream, expert_gather_kernel<W, UNITS>, static_cast<unsigned>(twa_ceil_div(tokens * parts, MOVE_WARPS)), MOVE_WARPS * 32, 0,
-             static_cast<const char*>(x), ldx, tokens, units, parts, place, top, static_cast<char*>(out), ldo);
+cudaError_t launch_gather(twa_ctx* ctx, const SortArgs& s, Rows r, long long bytes, bool small) {
+  r.units = static_cast<int>(bytes / sizeof(W));
+  r.parts = static_cast<int>(twa_ceil_div(r.units, UNITS * 32));
+  const unsigned blocks = static_cast<unsigned>(twa_ceil_div(r.tokens * r.parts, MOVE_WARPS));
+  if (!small) return twa_launch(ctx->stream, expert_gather_kernel<W, UNITS>, blocks, MOVE_WARPS * 32, 0, r, s.place, s.order);
+  SortArgs one = s;
+  one.warps = MOVE_WARPS;
+  one.run = static_cast<int>(twa_ceil_div(twa_ceil_div(s.count, MOVE_WARPS), 32) * 32);
+  return twa_launch(ctx->stream, expert_small_kernel<W, UNITS>, blocks < 2 * ctx->sm_count ? blocks : 2 * ctx->sm_count, MOVE_WARPS * 32,
+                    sizeof(int) * (MOVE_WARPS + 3) * s.experts, one, r);
+}
+
+// Blocks of a sorting cluster at most: 16 where the device has room for such a cluster, which not every one need have, otherwise 8.
+cudaError_t sort_cluster(twa_ctx* ctx, int* most) {
+  if (!ctx->expert_cluster) {
+    cudaError_t e = cudaFuncSetAttribute(expert_sort_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e != cudaSuccess) return e;
+    e = cudaFuncSetAttribute(expert_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(int) * (SORT_WARPS + 3) * TWA_EXPERTS_MAX);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(16);
+    cfg.blockDim = dim3(SORT_THREADS);
+    cfg.dynamicSmemBytes = sizeof(int) * (SORT_WARPS + 3) * TWA_EXPERTS_MAX;
+    cudaLaunchAttribute attr = {};
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = 16;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    int clusters = 0;
+    e = cudaOccupancyMaxActiveClusters(&clusters, expert_sort_kernel, &cfg);
+    if (e != cudaSuccess) return e;
+    ctx->expert_cluster = clusters > 0 ? 16 : 8;
+  }
+  *most = ctx->expert_cluster;
+  return cudaSuccess;
 }
 
 int expert_sizes(twa_ctx* ctx, int64_t tokens, int top) {
@@ -294,22 +396,66 @@ int expert_sizes(twa_ctx* ctx, int64_t tokens, int top) {
   return TWA_OK;
 }
 
-template <typename T>
-void launch_combine(twa_ctx* ctx, CombineArgs a, bool packs) {
-  constexpr int V = twa_vec<T>;
-  a.parts = static_cast<int>(twa_ceil_div(a.dim, 32 * (packs ? V : 1)));
-  const unsigned blocks = static_cast<unsigned>(twa_ceil_div(a.tokens * a.parts, MOVE_WARPS));
-  if (packs) twa_launch(ctx->stream, expert_combine_kernel<T, V>, blocks, MOVE_WARPS * 32, 0, a);
-  else twa_launch(ctx->stream, expert_combine_kernel<T, 1>, blocks, MOVE_WARPS * 32, 0, a);
+template <typename T, int E, int UNITS, int JOIN>
+void launch_combine(twa_ctx* ctx, CombineArgs& a) {
+  a.parts = static_cast<int>(twa_ceil_div(a.dim, UNITS * 32 * E));
+  twa_launch(ctx->stream, expert_combine_kernel<T, E, UNITS, JOIN>, static_cast<unsigned>(twa_ceil_div(a.tokens * a.parts, MOVE_WARPS)),
+             MOVE_WARPS * 32, 0, a);
+}
+// As much of a row a warp as keeps some eight loads of a lane under way, but where there are few rows more warps a row.
+template <typename T, int E>
+void launch_combine(twa_ctx* ctx, CombineArgs& a) {
+  const bool few = a.tokens * twa_ceil_div(a.dim, 32 * E) < 32LL * ctx->sm_count;
+  if constexpr (E == twa_vec<T>) {
+    if (few) launch_combine<T, E, 1, 4>(ctx, a);
+    else if (a.top <= 2) launch_combine<T, E, 4, 2>(ctx, a);
+    else launch_combine<T, E, 2, 4>(ctx, a);
+  } else {
+    if (few) launch_combine<T, E, 2, 4>(ctx, a);
+    else launch_combine<T, E, 8, 2>(ctx, a);
+  }
 }
 
-template <typename T, int E>
+template <typename T, int E, int UNITS, int JOIN>
 void launch_combine_backward(twa_ctx* ctx, const CombineArgs& a) {
   if (a.tokens >= 16LL * ctx->sm_count)
-    twa_launch(ctx->stream, expert_combine_backward_kernel<T, E, 32>, static_cast<unsigned>(twa_ceil_div(a.tokens, MOVE_WARPS)), MOVE_WARPS * 32,
-               0, a);
+    twa_launch(ctx->stream, expert_combine_backward_kernel<T, E, UNITS, JOIN, 32>, static_cast<unsigned>(twa_ceil_div(a.tokens, MOVE_WARPS)),
+               MOVE_WARPS * 32, 0, a);
   else
-    twa_launch(ctx->stream, expert_combine_backward_kernel<T, E, MOVE_WARPS * 32>, static_cast<unsigned>(a.tokens), MOVE_WARPS * 32, 0, a);
+    twa_launch(ctx->stream, expert_combine_backward_kernel<T, E, UNITS, JOIN, MOVE_WARPS * 32>, static_cast<unsigned>(a.tokens), MOVE_WARPS * 32, 0, a);
+}
+template <typename T, int E>
+void launch_combine_backward(twa_ctx* ctx, CombineArgs& a) {
+  if constexpr (E == twa_vec<T>) {
+    if (a.top <= 2) launch_combine_backward<T, E, 4, 2>(ctx, a);
+    else launch_combine_backward<T, E, 1, 4>(ctx, a);
+  } else {
+    launch_combine_backward<T, E, 4, 2>(ctx, a);
+  }
+}
+struct Forward {
+  template <typename T, int E>
+  static void launch(twa_ctx* ctx, CombineArgs& a) { launch_combine<T, E>(ctx, a); }
+};
+struct Backward {
+  template <typename T, int E>
+  static void launch(twa_ctx* ctx, CombineArgs& a) { launch_combine_backward<T, E>(ctx, a); }
+};
+// Packs of 16 bytes where all rows lie on them, of 4, or by the element.
+template <typename D>
+void launch_packed(twa_ctx* ctx, CombineArgs& a, int dtype) {
+  const size_t size = twa_dtype_size(dtype);
+  auto fits = [&](size_t unit) {
+    return a.dim * size % unit == 0 && on_unit(a.y, a.ldy * size, unit) && on_unit(a.out, a.ldo * size, unit) && on_unit(a.dout, a.ldd * size, unit);
+  };
+  if (dtype == TWA_BF16) {
+    if (fits(16)) D::template launch<bf16, 8>(ctx, a);
+    else if (fits(4)) D::template launch<bf16, 2>(ctx, a);
+    else D::template launch<bf16, 1>(ctx, a);
+  } else {
+    if (fits(16)) D::template launch<float, 4>(ctx, a);
+    else D::template launch<float, 1>(ctx, a);
+  }
 }
 
 }  // namespace
@@ -329,21 +475,30 @@ int twa_expert_dispatch(twa_ctx* ctx, const void* x, int64_t ldx, twa_dtype dtyp
                                                   twa_misaligned_to(order, 4) || twa_misaligned_to(x, size) || twa_misaligned_to(out, size))))
     return TWA_ERR_MISALIGNED;
   TWA_CUDA_OK(ctx, cudaSetDevice(ctx->device));
-  SortArgs s = {ids, id_type, tokens, static_cast<int>(tokens * top), top, experts, SORT_WARPS, 0, place, order, starts, ctx->d_status};
-  while (s.warps > 1 && sizeof(int) * (s.warps + 3) * experts > 48 * 1024) s.warps /= 2;
-  int blocks = 1;
-  while (blocks < 8 && s.count > blocks * s.warps * 32 * SORT_LOADS) blocks *= 2;
-  s.run = static_cast<int>(twa_ceil_div(twa_ceil_div(s.count, blocks * s.warps), 32) * 32);
-  TWA_CUDA_OK(ctx, twa_launch_clusters(ctx->stream, expert_sort_kernel, blocks, blocks, SORT_THREADS, sizeof(int) * (s.warps + 3) * experts, s,
-                                       blocks));
-  if (x && tokens) {
-    const long long bytes = static_cast<long long>(dim) * size, lx = ldx * size, lo = ldo * size;
-    const bool wide = bytes % 16 == 0 && on_unit(x, lx, 16) && on_unit(out, lo, 16);
-    if (wide) launch_gather<uint4, 4>(ctx, x, lx, tokens, bytes, place, top, out, lo);
-    else if (bytes % 4 == 0 && on_unit(x, lx, 4) && on_unit(out, lo, 4)) launch_gather<uint32_t, 8>(ctx, x, lx, tokens, bytes, place, top, out, lo);
-    else launch_gather<unsigned short, 8>(ctx, x, lx, tokens, bytes, place, top, out, lo);
+  SortArgs s = {ids, id_type, static_cast<int>(tokens * top), top, experts, 1, SORT_WARPS, 0, place, order, starts, ctx->d_status};
+  while (experts >> s.bits) ++s.bits;
+  const bool moves = x && tokens;
+  const bool small = moves && s.count <= SMALL_COUNT && sizeof(int) * ((MOVE_WARPS + 3) * experts + SMALL_COUNT) <= 48 * 1024;
+  if (!small) {
+    const size_t smem = sizeof(int) * (s.warps + 3) * experts;
+    int blocks = 1, most;
+    TWA_CUDA_OK(ctx, sort_cluster(ctx, &most));
+    while (blocks < most && s.count > blocks * s.warps * 32) blocks *= 2;
+    s.run = static_cast<int>(twa_ceil_div(twa_ceil_div(s.count, blocks * s.warps), 32) * 32);
+    SortArgs first = s;
+    if (moves) first.order = nullptr;              // the blocks that move rows write it
+    TWA_CUDA_OK(ctx, twa_launch_clusters(ctx->stream, expert_sort_kernel, blocks, blocks, s.warps * 32, smem, first, blocks));
   }
-  TWA_CUDA_OK(ctx, cudaGetLastError());
+  if (moves) {
+    const long long bytes = static_cast<long long>(dim) * size;
+    const Rows r = {static_cast<const char*>(x), static_cast<char*>(out), static_cast<long long>(ldx * size), static_cast<long long>(ldo * size),
+                    tokens, 0, 0, top};
+    auto fits = [&](size_t unit) { return bytes % unit == 0 && on_unit(x, r.ldx, unit) && on_unit(out, r.ldo, unit); };
+    const cudaError_t launched = fits(16)  ? launch_gather<uint4, 4>(ctx, s, r, bytes, small)
+                                 : fits(4) ? launch_gather<uint32_t, 8>(ctx, s, r, bytes, small)
+                                           : launch_gather<unsigned short, 8>(ctx, s, r, bytes, small);
+    TWA_CUDA_OK(ctx, launched);
+  }
   return TWA_OK;
 }
 
@@ -359,10 +514,8 @@ int twa_expert_combine(twa_ctx* ctx, const void* y, int64_t ldy, twa_dtype dtype
   if (twa_misaligned_to(place, 4) || twa_misaligned_to(weights, 4) || twa_misaligned_to(out, size) || (rows && twa_misaligned_to(y, size)))
     return TWA_ERR_MISALIGNED;
   TWA_CUDA_OK(ctx, cudaSetDevice(ctx->device));
-  const bool packs = dim * size % 16 == 0 && on_unit(y, ldy * size, 16) && on_unit(out, ldo * size, 16);
   CombineArgs a = {y, nullptr, place, weights, out, nullptr, ldy, 0, ldo, rows, tokens, top, dim, 0, ctx->d_status};
-  if (dtype == TWA_BF16) launch_combine<bf16>(ctx, a, packs);
-  else launch_combine<float>(ctx, a, packs);
+  launch_packed<Forward>(ctx, a, dtype);
   TWA_CUDA_OK(ctx, cudaGetLastError());
   return TWA_OK;
 }
@@ -381,15 +534,8 @@ int twa_expert_combine_backward(twa_ctx* ctx, const void* dout, int64_t lddout, 
       (rows && (twa_misaligned_to(y, size) || twa_misaligned_to(dy, size))))
     return TWA_ERR_MISALIGNED;
   TWA_CUDA_OK(ctx, cudaSetDevice(ctx->device));
-  const bool packs = dim * size % 16 == 0 && on_unit(dout, lddout * size, 16) && on_unit(y, ldy * size, 16) && on_unit(dy, lddy * size, 16);
-  const CombineArgs a = {y, dout, place, weights, dy, dw, ldy, lddout, lddy, rows, tokens, top, dim, 0, ctx->d_status};
-  if (dtype == TWA_BF16) {
-    if (packs) launch_combine_backward<bf16, 8>(ctx, a);
-    else launch_combine_backward<bf16, 1>(ctx, a);
-  } else {
-    if (packs) launch_combine_backward<float, 4>(ctx, a);
-    else launch_combine_backward<float, 1>(ctx, a);
-  }
+  CombineArgs a = {y, dout, place, weights, dy, dw, ldy, lddout, lddy, rows, tokens, top, dim, 0, ctx->d_status};
+  launch_packed<Backward>(ctx, a, dtype);
   TWA_CUDA_OK(ctx, cudaGetLastError());
   return TWA_OK;
 }

@@ -78,6 +78,14 @@ __device__ __forceinline__ uint32_t twa_bf16_pair(float lo, float hi) {
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
 }
+// The two elements of a 4-byte word.
+template <>
+struct twa_pack<bf16, 2> {
+  uint32_t r;
+  __device__ __forceinline__ void load(const bf16* p) { r = __ldg(reinterpret_cast<const uint32_t*>(p)); }
+  __device__ __forceinline__ void widen(float* v) const { v[0] = twa_bf16_lo(r); v[1] = twa_bf16_hi(r); }
+  static __device__ __forceinline__ void store(bf16* p, const float* v) { *reinterpret_cast<uint32_t*>(p) = twa_bf16_pair(v[0], v[1]); }
+};
 template <>
 struct twa_pack<bf16, 8> {
   uint4 r;
