@@ -73,7 +73,7 @@ static_assert(MAX_CLUSTER <= SCAN_WARPS, "a warp for every rank");
 
 template <typename T, int FEED, int CH>
 struct ScanForward {
-  static constexpr int STAGES = 3;
+  static constexpr int STAGES = FEED == BY_ELEMENTS ? 2 : 3;     // of which two blocks an SM have room
   static constexpr bool TOGETHER = FEED != BY_ELEMENTS;
   static constexpr int N = SEG<T>;
   static constexpr int SEGS = SCAN_CHANNELS / CH, WARP_ROWS = SEGS * N, TILE = SCAN_WARPS * WARP_ROWS;       // rows
