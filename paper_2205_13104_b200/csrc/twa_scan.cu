@@ -73,7 +73,7 @@ static_assert(MAX_CLUSTER <= SCAN_WARPS, "a warp for every rank");
 
 template <typename T, int FEED, int CH>
 struct ScanForward {
-  static constexpr int STAGES = FEED == BY_ELEMENTS ? 2 : 3;     // of which two blocks an SM have room
+  static constexpr int STAGES = 3;                 // of which two blocks an SM have room
   static constexpr bool TOGETHER = FEED != BY_ELEMENTS;
   static constexpr int N = SEG<T>;
   static constexpr int SEGS = SCAN_CHANNELS / CH, WARP_ROWS = SEGS * N, TILE = SCAN_WARPS * WARP_ROWS;       // rows
@@ -82,7 +82,7 @@ struct ScanForward {
   const Place<FEED, CH> at;
   twa_f2 A[N], L[N];                               // of the rows up to each
 
-  __device__ __forceinline__ ScanForward(const ScanArgs& args, int slice) : a(args), at(args, slice) {}
+  __device__ __forceinline__ ScanForward(const ScanArgs& args, const Place<FEED, CH>& place) : a(args), at(place) {}
 
   __device__ __forceinline__ void row(int i, const Pair<T>& x, const Pair<T>& f) {
     const twa_f2 n = scan_gate<T>(f);
@@ -107,27 +107,6 @@ struct ScanForward {
     for (int i = 0; i < N; ++i)
       if (i < rows) m = {A[i], L[i]};
     return m;
-  }
-
-  // A sequence of at most SEG rows, by one warp.
-  __device__ __forceinline__ void brief(const Span& s, int seq) {
-    const int rows = static_cast<int>(s.len);
-    const T* x = static_cast<const T*>(a.x) + s.begin * a.ldx + at.c;
-    const T* f = static_cast<const T*>(a.f) + s.begin * a.ldf + at.c;
-    Pair<T> rx[N], rf[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (i < rows && at.n > 0) {
-        rx[i].template load<TOGETHER>(x + i * a.ldx, at.n);
-        rf[i].template load<TOGETHER>(f + i * a.ldf, at.n);
-      }
-    const twa_f2 in = at.state(a.h0, seq, a.channels);
-    if (rows) keep_state(at, a.states, scan_slot<T>(s, seq), a.channels, in);
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (i < rows) row(i, rx[i], rf[i]);
-    store(s.begin, rows, in);
-    at.keep(a.h_last, seq, a.channels, last(rows).of(in));
   }
 
   __device__ __forceinline__ void copy(Rows& ring, int array, const T* from, const void* all, long long ld, int rows, int left) {
@@ -220,7 +199,7 @@ struct ScanForward {
 
 template <typename T, int FEED, int CH>
 struct ScanBackward {
-  static constexpr int STAGES = 2;
+  static constexpr int STAGES = 2;                 // as above
   static constexpr bool TOGETHER = FEED != BY_ELEMENTS;
   static constexpr int N = SEG<T>;
   static constexpr int SEGS = SCAN_CHANNELS / CH, WARP_ROWS = SEGS * N, TILE = SCAN_WARPS * WARP_ROWS;
@@ -229,7 +208,7 @@ struct ScanBackward {
   const Place<FEED, CH> at;
   twa_f2 n[N], e[N];                               // gates; a (1 - a) (h_{t-1} - x_t)
 
-  __device__ __forceinline__ ScanBackward(const ScanArgs& args, int slice) : a(args), at(args, slice) {}
+  __device__ __forceinline__ ScanBackward(const ScanArgs& args, const Place<FEED, CH>& place) : a(args), at(place) {}
 
   // A row on the way from the state before the segment's first row to the one behind its last; off: the segment's A and M so far.
   __device__ __forceinline__ void row(int i, const Pair<T>& x, const Pair<T>& f, const Pair<T>& dh, twa_f2& h, Map& off) {
@@ -270,29 +249,6 @@ struct ScanBackward {
       dx -= a.lddx;
       df -= a.lddf;
     }
-  }
-
-  __device__ __forceinline__ void brief(const Span& s, int seq) {
-    const int rows = static_cast<int>(s.len);
-    const T* x = static_cast<const T*>(a.x) + s.begin * a.ldx + at.c;
-    const T* f = static_cast<const T*>(a.f) + s.begin * a.ldf + at.c;
-    const T* g = static_cast<const T*>(a.dh) + s.begin * a.lddh + at.c;
-    Pair<T> rx[N], rf[N], rd[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (i < rows && at.n > 0) {
-        rx[i].template load<TOGETHER>(x + i * a.ldx, at.n);
-        rf[i].template load<TOGETHER>(f + i * a.ldf, at.n);
-        rd[i].template load<TOGETHER>(g + i * a.lddh, at.n);
-      }
-    twa_f2 h = rows ? kept_state(at, a.states, scan_slot<T>(s, seq), a.channels) : 0;
-    twa_f2 k = at.state(a.d_last, seq, a.channels);
-    Map off = {twa_pair(1.0f), 0};
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (i < rows) row(i, rx[i], rf[i], rd[i], h, off);
-    store(s.begin, rows, k, [&](int i) { return rd[i].both(); });
-    at.keep(a.dh0, seq, a.channels, k);
   }
 
   __device__ __forceinline__ void copy(Rows& ring, int array, const T* from, const void* all, long long ld, int rows, int left) {
@@ -390,21 +346,98 @@ struct ScanBackward {
   }
 };
 
+// A sequence of at most SEG rows, by one warp: the state before each row is at hand, and rows go by, BRIEF_LOADS under way together.
+constexpr int BRIEF_LOADS = 4;
+template <typename T, int FEED>
+__device__ __forceinline__ void brief_forward(const ScanArgs& a, const Place<FEED, SCAN_CHANNELS>& at, const Span& s, int seq) {
+  constexpr bool TOGETHER = FEED != BY_ELEMENTS;
+  const T* x = static_cast<const T*>(a.x) + s.begin * a.ldx + at.c;
+  const T* f = static_cast<const T*>(a.f) + s.begin * a.ldf + at.c;
+  T* h = static_cast<T*>(a.h) + s.begin * a.ldh + at.c;
+  twa_f2 state = 0;
+  for (int r = 0; r < s.len; r += BRIEF_LOADS) {
+    Pair<T> rx[BRIEF_LOADS], rf[BRIEF_LOADS];
+#pragma unroll
+    for (int i = 0; i < BRIEF_LOADS; ++i)
+      if (r + i < s.len && at.n > 0) {
+        rx[i].template load<TOGETHER>(x + (r + i) * a.ldx, at.n);
+        rf[i].template load<TOGETHER>(f + (r + i) * a.ldf, at.n);
+      }
+    if (r == 0) {
+      state = at.state(a.h0, seq, a.channels);
+      keep_state(at, a.states, scan_slot<T>(s, seq), a.channels, state);
+    }
+#pragma unroll
+    for (int i = 0; i < BRIEF_LOADS; ++i)
+      if (r + i < s.len && at.n > 0) {
+        state = scan_step(scan_gate<T>(rf[i]), state, rx[i].both());
+        float lo, hi;
+        twa_unpair(state, lo, hi);
+        Pair<T>::template store<TOGETHER>(h + (r + i) * a.ldh, lo, hi, at.n);
+      }
+  }
+  if (s.len == 0) state = at.state(a.h0, seq, a.channels);
+  at.keep(a.h_last, seq, a.channels, state);
+}
+template <typename T, int FEED>
+__device__ __forceinline__ void brief_backward(const ScanArgs& a, const Place<FEED, SCAN_CHANNELS>& at, const Span& s, int seq) {
+  constexpr bool TOGETHER = FEED != BY_ELEMENTS;
+  const T* x = static_cast<const T*>(a.x) + s.begin * a.ldx + at.c;
+  const T* f = static_cast<const T*>(a.f) + s.begin * a.ldf + at.c;
+  const T* g = static_cast<const T*>(a.dh) + s.begin * a.lddh + at.c;
+  ScanBackward<T, FEED, SCAN_CHANNELS> back(a, at);
+  constexpr int N = SEG<T>;
+  Pair<T> rd[N];
+  twa_f2 h = s.len ? kept_state(at, a.states, scan_slot<T>(s, seq), a.channels) : 0;
+  twa_f2 k = at.state(a.d_last, seq, a.channels);
+  Map off = {twa_pair(1.0f), 0};
+#pragma unroll
+  for (int r = 0; r < N; r += BRIEF_LOADS)
+    if (r < s.len) {
+      Pair<T> rx[BRIEF_LOADS], rf[BRIEF_LOADS];
+#pragma unroll
+      for (int i = 0; i < BRIEF_LOADS; ++i)
+        if (r + i < s.len && at.n > 0) {
+          rx[i].template load<TOGETHER>(x + (r + i) * a.ldx, at.n);
+          rf[i].template load<TOGETHER>(f + (r + i) * a.ldf, at.n);
+          rd[r + i].template load<TOGETHER>(g + (r + i) * a.lddh, at.n);
+        }
+#pragma unroll
+      for (int i = 0; i < BRIEF_LOADS; ++i)
+        if (r + i < s.len) back.row(r + i, rx[i], rf[i], rd[r + i], h, off);
+    }
+  back.store(s.begin, s.len, k, [&](int i) { return rd[i].both(); });
+  at.keep(a.dh0, seq, a.channels, k);
+}
+template <typename T, int FEED, bool BACK>
+__device__ __forceinline__ void scan_brief(const ScanArgs& a, const Place<FEED, SCAN_CHANNELS>& at, const Span& s, int seq) {
+  if constexpr (BACK) brief_backward<T, FEED>(a, at, s, seq);
+  else brief_forward<T, FEED>(a, at, s, seq);
+}
+// Where no sequence is longer: a warp for each, of each slice.
+template <typename T, int FEED, bool BACK>
+__global__ void __launch_bounds__(SCAN_THREADS) scan_brief_kernel(ScanArgs a) {
+  twa_begin(a.x, a.f, a.dh, a.h0, a.states, a.d_last);
+  const int slice = blockIdx.x % a.slices, seq = blockIdx.x / a.slices * SHORT_GROUP + (threadIdx.x >> 5);
+  const Place<FEED, SCAN_CHANNELS> at(a, slice);
+  if (seq < a.sequences) scan_brief<T, FEED, BACK>(a, at, scan_span(a, seq, false), seq);
+}
+
 // GROUP sequences of a slice of channels a block.  The ones of at most SEG rows go to one warp each, the others to the block.
-template <typename Direction, int CH, int GROUP>
+template <typename Direction, typename T, int FEED, bool BACK, int CH, int GROUP>
 __device__ __forceinline__ void scan_block(const ScanArgs& a) {
   extern __shared__ __align__(16) char shared[];
   __shared__ Joins<CH / 2> joins;
   Tiles<CH / 2>& tiles = *reinterpret_cast<Tiles<CH / 2>*>(shared + Direction::Rows::BLOCK_BYTES);         // of clusters only
   const unsigned task = blockIdx.x / a.cluster;
   const int slice = task % a.slices, first = task / a.slices * GROUP;
-  Direction d(a, slice);
+  Direction d(a, Place<FEED, CH>(a, slice));
   if (a.cluster > 1) twa_cluster_sync();           // no block stores into one that has not begun
-  if (GROUP > 1) {
+  if constexpr (GROUP > 1) {
     const int seq = first + d.at.warp;
     if (seq < a.sequences) {
       const Span s = scan_span(a, seq, slice == 0 && d.at.lane == 0);
-      if (s.len >= 0 && s.len <= Direction::N) d.brief(s, seq);
+      if (s.len >= 0 && s.len <= Direction::N) scan_brief<T, FEED, BACK>(a, d.at, s, seq);
     }
   }
   int turn = 0;
@@ -419,12 +452,12 @@ __device__ __forceinline__ void scan_block(const ScanArgs& a) {
 template <typename T, int FEED, int CH, int GROUP>
 __global__ void __launch_bounds__(SCAN_THREADS, 2) scan_forward_kernel(ScanArgs a) {
   twa_begin(a.x, a.f, a.starts, a.h0);
-  scan_block<ScanForward<T, FEED, CH>, CH, GROUP>(a);
+  scan_block<ScanForward<T, FEED, CH>, T, FEED, false, CH, GROUP>(a);
 }
 template <typename T, int FEED, int CH, int GROUP>
 __global__ void __launch_bounds__(SCAN_THREADS, 2) scan_backward_kernel(ScanArgs a) {
   twa_begin(a.x, a.f, a.dh, a.starts, a.states, a.d_last);
-  scan_block<ScanBackward<T, FEED, CH>, CH, GROUP>(a);
+  scan_block<ScanBackward<T, FEED, CH>, T, FEED, true, CH, GROUP>(a);
 }
 
 // How rows of two pointers and strides can be fetched together.
@@ -448,6 +481,12 @@ cudaError_t scan_launch(twa_ctx* ctx, ScanArgs& a, bool back, int feed) {
   a.cluster = 1;
   if (a.tokens <= 2LL * SEG<T> * a.sequences) {
     a.slices = static_cast<int>(twa_ceil_div(a.channels, SCAN_CHANNELS));
+    if (!a.starts && a.tokens <= static_cast<long long>(SEG<T>) * a.sequences) {
+      const unsigned blocks = static_cast<unsigned>(twa_ceil_div(a.sequences, SHORT_GROUP) * a.slices);
+      auto launch = [&](auto kernel) { return twa_launch(ctx->stream, kernel, blocks, SCAN_THREADS, 0, a); };
+      if (back) return feed == BY_ELEMENTS ? launch(scan_brief_kernel<T, BY_ELEMENTS, true>) : launch(scan_brief_kernel<T, BY_PAIRS, true>);
+      return feed == BY_ELEMENTS ? launch(scan_brief_kernel<T, BY_ELEMENTS, false>) : launch(scan_brief_kernel<T, BY_PAIRS, false>);
+    }
     return feed == BY_UNITS ? scan_launch<T, BY_UNITS, SCAN_CHANNELS, SHORT_GROUP>(ctx, a, back)
                             : (feed == BY_PAIRS ? scan_launch<T, BY_PAIRS, SCAN_CHANNELS, SHORT_GROUP>(ctx, a, back)
                                                 : scan_launch<T, BY_ELEMENTS, SCAN_CHANNELS, SHORT_GROUP>(ctx, a, back));

@@ -215,7 +215,7 @@ struct Ring {
   static constexpr int N = SEG<T>, SEGS = SCAN_CHANNELS / CH;
   static_assert(SEGS == 1 || FEED == BY_UNITS, "narrow slices by units only");
   static constexpr bool WORDS = FEED == BY_ELEMENTS && sizeof(T) == 2;
-  static constexpr int ROW = CH * sizeof(T) + (WORDS ? 16 : 0), NEXT_SEG = (N + (SEGS > 1 ? 1 : 0)) * ROW;       // bytes
+  static constexpr int ROW = CH * sizeof(T) + (WORDS ? 4 : 0), NEXT_SEG = (N + (SEGS > 1 ? 1 : 0)) * ROW;       // bytes
   static constexpr int AREA = SEGS * NEXT_SEG, BYTES = ARRAYS * AREA;                                            // of a matrix, a stage
   static constexpr size_t BLOCK_BYTES = static_cast<size_t>(SCAN_WARPS) * STAGES * BYTES;
   static constexpr int AHEAD = STAGES - 1;        // segments under way before the first is waited for
