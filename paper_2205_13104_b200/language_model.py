@@ -129,6 +129,12 @@ def train(vocab=2000, dim=128, hidden=512, tokens=4096, checkpoints=10, between=
     """Stage one and stage two; returns the losses on fresh text of the last checkpoint, of the checkpoints' mean and of the
     weights that the subspace training found."""
     model, text = LanguageModel(vocab, dim, hidden, tokens, device), Text(vocab, seed + 1, device)
+    return stages(model, text, checkpoints, between, steps, lr, subspace_lr, max_norm, seed, say)
+
+
+def stages(model, text, checkpoints, between, steps, lr, subspace_lr, max_norm, seed, say):
+    """Both stages for a model and its text; closes the model."""
+    device, tokens = model.device, model.tokens
     w = model.initial(seed)
     W = torch.zeros((checkpoints, padded_ld(model.D)), device=device)
     for step in range((checkpoints + 2) * between):
@@ -155,7 +161,7 @@ def train(vocab=2000, dim=128, hidden=512, tokens=4096, checkpoints=10, between=
     found = measure(lifted)
     code, detail = twa.twa_get_status(model.ctx)
     if code:
-        raise twa.TwaError(code, "language_model.train", f"detail {detail}")
+        raise twa.TwaError(code, "stages", f"detail {detail}")
     say(f"loss on fresh text: last checkpoint {last:.4f}, mean of {checkpoints} checkpoints {mean:.4f}, "
         f"after {steps} steps in their subspace {found:.4f}")
     model.close()
