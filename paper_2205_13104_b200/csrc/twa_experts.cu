@@ -148,6 +148,7 @@ __global__ void __launch_bounds__(SORT_THREADS) expert_sort_kernel(SortArgs a, i
 
 // ---- rows to their experts ------------------------------------------------------------------------
 constexpr int MOVE_WARPS = 8;
+constexpr int NARROW = 8;                         // threads of a row that is no wider than they hold
 
 // Rows as units of type W.
 struct Rows {
@@ -156,34 +157,38 @@ struct Rows {
   long long ldx, ldo, tokens;                     // strides in bytes
   int units, parts, top;                          // parts: of a row, for one warp each
 };
-// A warp takes UNITS x 32 units of a token's row and stores them wherever `place` says.
-template <typename W, int UNITS>
-__device__ __forceinline__ void move_row(const Rows& r, long long t, int part, int place) {
-  const int u0 = part * (UNITS * 32) + (threadIdx.x & 31);
+// LANES threads take UNITS units each of a token's row and store them wherever its places say; `where(j)` gives the j-th.
+template <typename W, int UNITS, int LANES, typename Where>
+__device__ __forceinline__ void move_row(const Rows& r, long long t, int part, Where where) {
+  const int u0 = part * (UNITS * LANES) + (threadIdx.x & (LANES - 1));
   const W* from = reinterpret_cast<const W*>(r.x + t * r.ldx);
   W v[UNITS];
 #pragma unroll
   for (int k = 0; k < UNITS; ++k)
-    if (u0 + k * 32 < r.units) v[k] = __ldg(from + u0 + k * 32);
+    if (u0 + k * LANES < r.units) v[k] = __ldg(from + u0 + k * LANES);
   for (int j = 0; j < r.top; ++j) {
-    const int p = __shfl_sync(0xffffffffu, place, j);
+    const int p = where(j);
     if (p < 0) continue;
     W* to = reinterpret_cast<W*>(r.out + p * r.ldo);
 #pragma unroll
     for (int k = 0; k < UNITS; ++k)
-      if (u0 + k * 32 < r.units) to[u0 + k * 32] = v[k];
+      if (u0 + k * LANES < r.units) to[u0 + k * LANES] = v[k];
   }
 }
 
-template <typename W, int UNITS>
+template <typename W, int UNITS, int LANES>
 __global__ void __launch_bounds__(MOVE_WARPS * 32) expert_gather_kernel(Rows r, const int* place, int* order) {
   twa_begin(r.x, place);
-  const long long task = static_cast<long long>(blockIdx.x) * MOVE_WARPS + (threadIdx.x >> 5);
+  constexpr int TEAMS = MOVE_WARPS * 32 / LANES;
+  const long long task = static_cast<long long>(blockIdx.x) * TEAMS + threadIdx.x / LANES;
   const long long t = task / r.parts;
   if (t >= r.tokens) return;
-  const int lane = threadIdx.x & 31, part = static_cast<int>(task - t * r.parts), at = lane < r.top ? __ldg(place + t * r.top + lane) : -1;
-  if (order && part == 0 && at >= 0) order[at] = static_cast<int>(t) * r.top + lane;      // scattered: not for the sort's few SMs
-  move_row<W, UNITS>(r, t, part, at);
+  const int part = static_cast<int>(task - t * r.parts);
+  const int* places = place + t * r.top;
+  if (order && part == 0)                          // scattered: not for the sort's few SMs
+    for (int j = threadIdx.x & (LANES - 1); j < r.top; j += LANES)
+      if (__ldg(places + j) >= 0) order[__ldg(places + j)] = static_cast<int>(t) * r.top + j;
+  move_row<W, UNITS, LANES>(r, t, part, [&](int j) { return __ldg(places + j); });
 }
 
 // Few assignments: every block sorts them, block 0 says so, and each moves its share of the rows.  A launch after a launch would cost
@@ -198,10 +203,9 @@ __global__ void __launch_bounds__(MOVE_WARPS * 32) expert_small_kernel(SortArgs 
   __syncthreads();
   if (blockIdx.x == 0)
     for (int i = threadIdx.x; i < a.count; i += MOVE_WARPS * 32) a.place[i] = place[i];
-  const int lane = threadIdx.x & 31;
   for (int task = blockIdx.x * MOVE_WARPS + (threadIdx.x >> 5); task < static_cast<int>(r.tokens) * r.parts; task += gridDim.x * MOVE_WARPS) {
     const int t = task / r.parts;
-    move_row<W, UNITS>(r, t, task - t * r.parts, lane < r.top ? place[t * r.top + lane] : -1);
+    move_row<W, UNITS, 32>(r, t, task - t * r.parts, [&](int j) { return place[t * r.top + j]; });
   }
 }
 
@@ -228,71 +232,74 @@ __device__ __forceinline__ int place_of(const CombineArgs& a, long long t, int j
   return p;
 }
 
-// A warp takes UNITS x 32 packs of E elements of a token's row, JOIN of its experts' rows under way together.
-template <typename T, int E, int UNITS, int JOIN>
+// LANES threads take UNITS packs of E elements each of a token's row, JOIN of its experts' rows under way together.
+template <typename T, int E, int UNITS, int JOIN, int LANES>
 __global__ void __launch_bounds__(MOVE_WARPS * 32) expert_combine_kernel(CombineArgs a) {
   twa_begin(a.y, a.place, a.weights);
-  const long long task = static_cast<long long>(blockIdx.x) * MOVE_WARPS + (threadIdx.x >> 5);
+  constexpr int TEAMS = MOVE_WARPS * 32 / LANES;
+  const long long task = static_cast<long long>(blockIdx.x) * TEAMS + threadIdx.x / LANES;
   const long long t = task / a.parts;
   if (t >= a.tokens) return;
-  const int lane = threadIdx.x & 31, part = static_cast<int>(task - t * a.parts), c0 = (part * UNITS * 32 + lane) * E;
-  const int place = lane < a.top ? place_of(a, t, lane, part == 0) : -1;
-  const float weight = lane < a.top ? (a.weights ? __ldg(a.weights + t * a.top + lane) : 1.0f) : 0.0f;
+  const int lane = threadIdx.x & (LANES - 1), part = static_cast<int>(task - t * a.parts), c0 = (part * UNITS * LANES + lane) * E;
   const T* y = static_cast<const T*>(a.y) + c0;
   float sum[UNITS][E] = {};
   for (int j0 = 0; j0 < a.top; j0 += JOIN) {
     twa_pack<T, E> raw[JOIN][UNITS];
     int p[JOIN];
+    float w[JOIN];
 #pragma unroll
     for (int k = 0; k < JOIN; ++k) {
-      p[k] = __shfl_sync(0xffffffffu, place, (j0 + k) & 31);
-      if (j0 + k >= a.top) p[k] = -1;
+      p[k] = j0 + k < a.top ? place_of(a, t, j0 + k, part == 0 && lane == 0) : -1;
+      w[k] = j0 + k < a.top && a.weights ? __ldg(a.weights + t * a.top + j0 + k) : 1.0f;
+    }
+#pragma unroll
+    for (int k = 0; k < JOIN; ++k) {
       if (p[k] < 0) continue;
       const T* row = y + p[k] * a.ldy;
 #pragma unroll
       for (int u = 0; u < UNITS; ++u)
-        if (c0 + u * 32 * E < a.dim) raw[k][u].load(row + u * 32 * E);
+        if (c0 + u * LANES * E < a.dim) raw[k][u].load(row + u * LANES * E);
     }
 #pragma unroll
     for (int k = 0; k < JOIN; ++k) {
-      const float w = __shfl_sync(0xffffffffu, weight, (j0 + k) & 31);
       if (p[k] < 0) continue;
 #pragma unroll
       for (int u = 0; u < UNITS; ++u)
-        if (c0 + u * 32 * E < a.dim) {
+        if (c0 + u * LANES * E < a.dim) {
           float v[E];
           raw[k][u].widen(v);
 #pragma unroll
-          for (int e = 0; e < E; ++e) sum[u][e] = fmaf(w, v[e], sum[u][e]);
+          for (int e = 0; e < E; ++e) sum[u][e] = fmaf(w[k], v[e], sum[u][e]);
         }
     }
   }
   T* out = static_cast<T*>(a.out) + t * a.ldo + c0;
 #pragma unroll
   for (int u = 0; u < UNITS; ++u)
-    if (c0 + u * 32 * E < a.dim) twa_pack<T, E>::store(out + u * 32 * E, sum[u]);
+    if (c0 + u * LANES * E < a.dim) twa_pack<T, E>::store(out + u * LANES * E, sum[u]);
 }
 
-// A token's row for a group of LANES threads (a warp, or the block), UNITS packs of each at a time: the dot products need the whole row.
-// JOIN of its experts at a time.
+// A token's row for LANES threads (a part of a warp, a warp, or the block), UNITS packs of each at a time: the dot products need the
+// whole row.  JOIN of its experts at a time.
 template <typename T, int E, int UNITS, int JOIN, int LANES>
 __global__ void __launch_bounds__(MOVE_WARPS * 32) expert_combine_backward_kernel(CombineArgs a) {
   twa_begin(a.y, a.dout, a.place, a.weights);
-  __shared__ float part[LANES > 32 ? MOVE_WARPS : 1][32];
-  const long long t = LANES > 32 ? blockIdx.x : static_cast<long long>(blockIdx.x) * MOVE_WARPS + (threadIdx.x >> 5);
-  if (t >= a.tokens) return;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, at = LANES > 32 ? threadIdx.x : lane;
-  const int place = lane < a.top ? place_of(a, t, lane, warp == 0 || LANES == 32) : -1;
-  const float weight = lane < a.top ? __ldg(a.weights + t * a.top + lane) : 0.0f;
+  constexpr bool BLOCK = LANES > 32;
+  constexpr int TEAMS = MOVE_WARPS * 32 / LANES;
+  __shared__ float part[BLOCK ? MOVE_WARPS : 1][32];
+  const long long own = static_cast<long long>(blockIdx.x) * TEAMS + threadIdx.x / LANES;
+  const bool live = own < a.tokens;
+  if (LANES >= 32 && !live) return;
+  const long long t = live ? own : a.tokens - 1;             // threads beside the tokens take part in their warp's shuffles
+  const int at = threadIdx.x & (LANES - 1), warp = threadIdx.x >> 5;
   const T* dout = static_cast<const T*>(a.dout) + t * a.ldd;
   for (int j0 = 0; j0 < a.top; j0 += JOIN) {
     int p[JOIN];
     float w[JOIN], dot[JOIN];
 #pragma unroll
     for (int k = 0; k < JOIN; ++k) {
-      p[k] = __shfl_sync(0xffffffffu, place, (j0 + k) & 31);
-      w[k] = __shfl_sync(0xffffffffu, weight, (j0 + k) & 31);
-      if (j0 + k >= a.top) p[k] = -1;
+      p[k] = live && j0 + k < a.top ? place_of(a, t, j0 + k, at == 0) : -1;
+      w[k] = j0 + k < a.top ? __ldg(a.weights + t * a.top + j0 + k) : 0.0f;
       dot[k] = 0.0f;
     }
     for (int c = at * E; c < a.dim; c += UNITS * LANES * E) {
@@ -329,15 +336,17 @@ __global__ void __launch_bounds__(MOVE_WARPS * 32) expert_combine_backward_kerne
     }
 #pragma unroll
     for (int k = 0; k < JOIN; ++k) {
-      const float sum = twa_warp_sum(dot[k]);
-      if (LANES > 32) {
-        if (lane == 0 && j0 + k < a.top) part[warp][j0 + k] = sum;
-      } else if (a.dw && lane == 0 && j0 + k < a.top) {
+      float sum = dot[k];
+#pragma unroll
+      for (int o = (LANES < 32 ? LANES : 32) / 2; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      if (BLOCK) {
+        if ((at & 31) == 0 && j0 + k < a.top) part[warp][j0 + k] = sum;
+      } else if (a.dw && at == 0 && live && j0 + k < a.top) {
         a.dw[t * a.top + j0 + k] = sum;
       }
     }
   }
-  if (LANES > 32 && a.dw) {
+  if (BLOCK && a.dw) {
     __syncthreads();
     if (threadIdx.x < a.top) {
       float sum = 0.0f;
@@ -354,9 +363,14 @@ bool on_unit(const void* p, long long ld_bytes, size_t unit) { return !twa_misal
 template <typename W, int UNITS>
 cudaError_t launch_gather(twa_ctx* ctx, const SortArgs& s, Rows r, long long bytes, bool small) {
   r.units = static_cast<int>(bytes / sizeof(W));
+  if (!small && r.units <= UNITS * NARROW) {
+    r.parts = 1;
+    return twa_launch(ctx->stream, expert_gather_kernel<W, UNITS, NARROW>, static_cast<unsigned>(twa_ceil_div(r.tokens, MOVE_WARPS * 32 / NARROW)),
+                      MOVE_WARPS * 32, 0, r, s.place, s.order);
+  }
   r.parts = static_cast<int>(twa_ceil_div(r.units, UNITS * 32));
   const unsigned blocks = static_cast<unsigned>(twa_ceil_div(r.tokens * r.parts, MOVE_WARPS));
-  if (!small) return twa_launch(ctx->stream, expert_gather_kernel<W, UNITS>, blocks, MOVE_WARPS * 32, 0, r, s.place, s.order);
+  if (!small) return twa_launch(ctx->stream, expert_gather_kernel<W, UNITS, 32>, blocks, MOVE_WARPS * 32, 0, r, s.place, s.order);
   SortArgs one = s;
   one.warps = MOVE_WARPS;
   one.run = static_cast<int>(twa_ceil_div(twa_ceil_div(s.count, MOVE_WARPS), 32) * 32);
@@ -396,42 +410,42 @@ int expert_sizes(twa_ctx* ctx, int64_t tokens, int top) {
   return TWA_OK;
 }
 
-template <typename T, int E, int UNITS, int JOIN>
+template <typename T, int E, int UNITS, int JOIN, int LANES = 32>
 void launch_combine(twa_ctx* ctx, CombineArgs& a) {
-  a.parts = static_cast<int>(twa_ceil_div(a.dim, UNITS * 32 * E));
-  twa_launch(ctx->stream, expert_combine_kernel<T, E, UNITS, JOIN>, static_cast<unsigned>(twa_ceil_div(a.tokens * a.parts, MOVE_WARPS)),
-             MOVE_WARPS * 32, 0, a);
+  a.parts = static_cast<int>(twa_ceil_div(a.dim, UNITS * LANES * E));
+  twa_launch(ctx->stream, expert_combine_kernel<T, E, UNITS, JOIN, LANES>,
+             static_cast<unsigned>(twa_ceil_div(a.tokens * a.parts, MOVE_WARPS * 32 / LANES)), MOVE_WARPS * 32, 0, a);
 }
-// As much of a row a warp as keeps some eight loads of a lane under way, but where there are few rows more warps a row.
+// As much of a row a thread as keeps some eight loads of it under way, but where there are few rows more threads a row.
 template <typename T, int E>
 void launch_combine(twa_ctx* ctx, CombineArgs& a) {
   const bool few = a.tokens * twa_ceil_div(a.dim, 32 * E) < 32LL * ctx->sm_count;
-  if constexpr (E == twa_vec<T>) {
+  if (a.dim <= 2 * NARROW * E) {
+    launch_combine<T, E, 2, 4, NARROW>(ctx, a);
+  } else if constexpr (E == twa_vec<T>) {
     if (few) launch_combine<T, E, 1, 4>(ctx, a);
     else if (a.top <= 2) launch_combine<T, E, 4, 2>(ctx, a);
     else launch_combine<T, E, 2, 4>(ctx, a);
   } else {
     if (few) launch_combine<T, E, 2, 4>(ctx, a);
-    else launch_combine<T, E, 8, 2>(ctx, a);
+    else if (a.top <= 2) launch_combine<T, E, 8, 2>(ctx, a);
+    else launch_combine<T, E, 4, 4>(ctx, a);
   }
 }
 
-template <typename T, int E, int UNITS, int JOIN>
+template <typename T, int E, int UNITS, int JOIN, int LANES>
 void launch_combine_backward(twa_ctx* ctx, const CombineArgs& a) {
-  if (a.tokens >= 16LL * ctx->sm_count)
-    twa_launch(ctx->stream, expert_combine_backward_kernel<T, E, UNITS, JOIN, 32>, static_cast<unsigned>(twa_ceil_div(a.tokens, MOVE_WARPS)),
-               MOVE_WARPS * 32, 0, a);
-  else
-    twa_launch(ctx->stream, expert_combine_backward_kernel<T, E, UNITS, JOIN, MOVE_WARPS * 32>, static_cast<unsigned>(a.tokens), MOVE_WARPS * 32, 0, a);
+  twa_launch(ctx->stream, expert_combine_backward_kernel<T, E, UNITS, JOIN, LANES>,
+             static_cast<unsigned>(twa_ceil_div(a.tokens, MOVE_WARPS * 32 / LANES)), MOVE_WARPS * 32, 0, a);
 }
 template <typename T, int E>
 void launch_combine_backward(twa_ctx* ctx, CombineArgs& a) {
-  if constexpr (E == twa_vec<T>) {
-    if (a.top <= 2) launch_combine_backward<T, E, 4, 2>(ctx, a);
-    else launch_combine_backward<T, E, 1, 4>(ctx, a);
-  } else {
-    launch_combine_backward<T, E, 4, 2>(ctx, a);
-  }
+  constexpr bool WIDE = E == twa_vec<T>;
+  constexpr int BLOCK = MOVE_WARPS * 32;
+  if (a.dim <= 4 * NARROW * E) launch_combine_backward<T, E, 2, 4, NARROW>(ctx, a);
+  else if (a.tokens < 16LL * ctx->sm_count) launch_combine_backward<T, E, WIDE ? 1 : 4, 4, BLOCK>(ctx, a);
+  else if (a.top <= 2) launch_combine_backward<T, E, 4, 2, 32>(ctx, a);
+  else launch_combine_backward<T, E, WIDE ? 1 : 4, 4, 32>(ctx, a);
 }
 struct Forward {
   template <typename T, int E>

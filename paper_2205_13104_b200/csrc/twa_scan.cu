@@ -479,9 +479,11 @@ constexpr int SCAN_RESIDENT = 2;                   // blocks of an SM
 template <typename T>
 cudaError_t scan_launch(twa_ctx* ctx, ScanArgs& a, bool back, int feed) {
   a.cluster = 1;
-  if (a.tokens <= 2LL * SEG<T> * a.sequences) {
+  // A warp a sequence: all of them where they are short enough, or, of ragged ones, those that are, where most must be.
+  const bool short_all = !a.starts && a.tokens <= static_cast<long long>(SEG<T>) * a.sequences;
+  if (short_all || (a.starts && 2 * a.tokens <= static_cast<long long>(SEG<T>) * a.sequences)) {
     a.slices = static_cast<int>(twa_ceil_div(a.channels, SCAN_CHANNELS));
-    if (!a.starts && a.tokens <= static_cast<long long>(SEG<T>) * a.sequences) {
+    if (short_all) {
       const unsigned blocks = static_cast<unsigned>(twa_ceil_div(a.sequences, SHORT_GROUP) * a.slices);
       auto launch = [&](auto kernel) { return twa_launch(ctx->stream, kernel, blocks, SCAN_THREADS, 0, a); };
       if (back) return feed == BY_ELEMENTS ? launch(scan_brief_kernel<T, BY_ELEMENTS, true>) : launch(scan_brief_kernel<T, BY_PAIRS, true>);
@@ -494,7 +496,10 @@ cudaError_t scan_launch(twa_ctx* ctx, ScanArgs& a, bool back, int feed) {
   int channels = SCAN_CHANNELS;
   auto blocks = [&]() { return twa_ceil_div(a.channels, channels) * a.sequences * a.cluster; };
   auto rows = [&]() { return a.cluster * SCAN_WARPS * SEG<T> * (SCAN_CHANNELS / channels); };       // of a round
-  auto more = [&]() { return 2 * blocks() <= SCAN_RESIDENT * ctx->sm_count && a.tokens > 2LL * rows() * a.sequences; };
+  // Twice as many where there is room for them and rows enough; ragged sequences wait for the longest, which takes the more blocks
+  // (15 ragged sequences of 13138 x 1016 bfloat16, both directions 133 us with one block each, RAGGED_US with two).
+  const int places = (a.starts ? 2 : 1) * SCAN_RESIDENT * ctx->sm_count;
+  auto more = [&]() { return 2 * blocks() <= places && a.tokens > 2LL * rows() * a.sequences; };
   if (ctx->tune_scan_channels && feed == BY_UNITS) channels = ctx->tune_scan_channels;
   else if (feed == BY_UNITS && more()) channels = 32;
   while (a.cluster < MAX_CLUSTER && more()) a.cluster *= 2;

@@ -283,23 +283,26 @@ struct Ring {
       for (int i = 0; i < N; ++i) {
         const int odd = (mine[array][i & 1] >> 1) - lane;                                // the row begins inside a word
         const char* word = reinterpret_cast<const char*>(from) - 2 * odd;
-        if (i < rows && 2 * lane < channels + odd) {
-          if (!edge || (reinterpret_cast<const T*>(word) >= first && reinterpret_cast<const T*>(word) + 1 <= last)) {
-            copy_async<4>(area + i * ROW + lane * 4, word);
-          } else {
-            for (int e = 0; e < 2; ++e) {
-              const T* p = reinterpret_cast<const T*>(word) + e;
-              if (p >= first && p <= last) *reinterpret_cast<T*>(base + fill + array * AREA + i * ROW + lane * 4 + e * 2) = *p;
-            }
-          }
-        }
+        if (i < rows && 2 * lane < channels + odd &&
+            (!edge || (reinterpret_cast<const T*>(word) >= first && reinterpret_cast<const T*>(word) < last)))
+          copy_async<4>(area + i * ROW + lane * 4, word);
         from += ld;
       }
       // the last element of a row that begins inside a word, alone in one more
       if (lane < rows && channels >= SCAN_CHANNELS && (lane & 1 ? mine[array][1] : mine[array][0]) != lane * 2) {
         const T* p = row + lane * ld + SCAN_CHANNELS - 1;
         if (!edge || p < last) copy_async<4>(area + lane * ROW + SCAN_CHANNELS * 2, p);
-        else *reinterpret_cast<T*>(base + fill + array * AREA + lane * ROW + SCAN_CHANNELS * 2) = *p;
+      }
+      // the matrix's first and last element where they lie in a word with something else
+      if (edge && lane < 2) {
+        const T* p = lane ? last : first;
+        const long long off = p - row;
+        const int i = off < 0 ? -1 : static_cast<int>(off / ld), e = static_cast<int>(off - i * ld);
+        const bool apart = lane ? (reinterpret_cast<uintptr_t>(p) & 2) == 0 : (reinterpret_cast<uintptr_t>(p) & 2) != 0;
+        if (apart && i >= 0 && i < rows && e < channels && e < SCAN_CHANNELS) {
+          const int odd = (i & 1 ? mine[array][1] : mine[array][0]) / 2 - lane;
+          *reinterpret_cast<T*>(base + fill + array * AREA + i * ROW + (e + odd) * 2) = *p;
+        }
       }
     }
   }

@@ -87,7 +87,8 @@ def scan_64(x, f, lengths, first, h0, dh=None, d_last=None):
     a, b = torch.sigmoid(f), torch.sigmoid(-f)
     s = torch.minimum(a, b)
     # relative error of s: of the exponential (expf one unit; the fast one 2 + 1.2 |f| units), then of the sum and the quotient
-    es = 2 * U * ((3.0 if x_dtype(x, f) == F32 else 0) + 3 + 1.2 * f.abs())
+    # (a gate beyond 128, an infinite one too: s is below 2^-184, zero in float32, so that its error counts for nothing)
+    es = 2 * U * ((3.0 if x_dtype(x, f) == F32 else 0) + 3 + 1.2 * f.abs().clamp(max=128.0))
     n, c = x.shape
     q = len(lengths)
     zero = torch.zeros((q, c), dtype=torch.float64, device=DEV)
@@ -677,6 +678,94 @@ def test_operators_replay_from_a_graph_on_another_stream(ctx):
         del graph
         twa.twa_destroy(own)
     torch.cuda.current_stream().wait_stream(stream)
+
+
+def test_gated_scan_with_shut_gates_begins_anew(ctx):
+    """Gates of -inf part sequences that share a row range: whatever the state was, the next one begins from the token."""
+    g = gen(21)
+    for dtype, c in ((F32, 64), (BF16, 37)):
+        n = 1000
+        x, f = randn(g, n, c).to(dtype), randn(g, n, c).to(dtype)
+        h0 = 1e8 * torch.ones(1, c, device=DEV)                     # as far from the tokens as float32 has digits
+        f[0], f[300], f[301], f[900] = -float("inf"), -float("inf"), float("inf"), -float("inf")
+        h, parts = torch.empty_like(x), torch.empty_like(x)
+        twa.twa_gated_scan(ctx, x, f, h, None, 1, h0)
+        assert torch.equal(h[0], x[0]) and torch.equal(h[300], x[300]) and torch.equal(h[301], h[300]) and torch.equal(h[900], x[900])
+        starts = torch.tensor([0, 300, 900, n], device=DEV)
+        twa.twa_gated_scan(ctx, x, f, parts, starts, 3)
+        scan_64.dtype = dtype
+        want, e = scan_64(x, f, [300, 600, 100], [0, 300, 900], None)["h"]
+        for got in (h, parts):
+            close(got, want, e + ROUND[dtype] * (want.abs() + e) + 1e-37)
+    ok(ctx)
+
+
+def test_two_graphs_of_one_context_and_two_contexts_at_once(ctx):
+    """Calls that a cluster of blocks shares, captured twice from one context and replayed together with a second context's."""
+    g = gen(31)
+    side = [torch.cuda.Stream() for _ in range(3)]
+    cases = []
+    for i, s in enumerate(side):
+        n, c, tokens, experts = 6000 + 64 * i, 48, 9000 + i, 40 + i
+        x, f, dh = (randn(g, n, c).to(BF16) for _ in range(3))
+        cases.append(dict(x=x, f=f, dh=dh, h=torch.empty_like(x), dx=torch.empty_like(x), df=torch.empty_like(x),
+                          states=torch.empty(twa.twa_gated_scan_states_bytes(n, 1, c), dtype=torch.uint8, device=DEV),
+                          ids=torch.randint(-1, experts, (tokens, 4), generator=g, device=DEV), experts=experts,
+                          place=torch.empty((tokens, 4), dtype=torch.int32, device=DEV), starts=torch.empty(experts + 1, dtype=torch.int32, device=DEV),
+                          rows=randn(g, tokens, 24), out=torch.zeros(tokens * 4, 24, device=DEV)))
+    torch.cuda.synchronize()
+
+    def step(own, v):
+        twa.twa_gated_scan(own, v["x"], v["f"], v["h"], states=v["states"])
+        twa.twa_expert_dispatch(own, v["rows"], v["ids"], v["experts"], v["place"], v["starts"], v["out"])
+        twa.twa_gated_scan_backward(own, v["dh"], v["x"], v["f"], v["states"], v["dx"], v["df"])
+
+    names = ("h", "dx", "df", "place", "starts", "out")
+    want, contexts, graphs = [], {}, []
+    for s, v in zip(side, cases):
+        with torch.cuda.stream(s):
+            one = twa.twa_create(0)
+            step(one, v)
+            s.synchronize()
+            assert twa.twa_get_status(one)[0] == 0
+            twa.twa_destroy(one)
+        want.append([v[k].clone() for k in names])
+    with torch.cuda.stream(side[0]):
+        contexts[0] = contexts[1] = twa.twa_create(0)               # the first two graphs are this context's
+    with torch.cuda.stream(side[2]):
+        contexts[2] = twa.twa_create(0)
+    for i, v in enumerate(cases):
+        s = side[0] if i < 2 else side[2]
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            step(contexts[i], v)
+        graphs.append(graph)
+    for _ in range(5):
+        for v in cases:
+            for k in names:
+                v[k].zero_()
+        torch.cuda.synchronize()
+        for s, graph in zip(side, graphs):                          # all three at once
+            with torch.cuda.stream(s):
+                graph.replay()
+        torch.cuda.synchronize()
+        for v, w in zip(cases, want):
+            assert all(torch.equal(v[k], t) for k, t in zip(names, w))
+    for c in (contexts[0], contexts[2]):
+        assert twa.twa_get_status(c)[0] == 0
+    del graphs
+    twa.twa_destroy(contexts[0])
+    twa.twa_destroy(contexts[2])
+
+
+def test_scan_knobs_take_what_they_mean(ctx):
+    for key, good in ((twa.TWA_TUNE_SCAN_CLUSTER, (1, 2, 4, 8)), (twa.TWA_TUNE_SCAN_CHANNELS, (16, 32, 64))):
+        for value in good + (0,):
+            twa.twa_set_tuning(ctx, key, value)
+        for value in (3, 12, 128):
+            with pytest.raises(twa.TwaError):
+                twa.twa_set_tuning(ctx, key, value)
+        twa.twa_set_tuning(ctx, key, 0)
 
 
 def test_offsets_beyond_32_bits(ctx):

@@ -22,15 +22,16 @@ def test_state_sizes():
     size = twa.twa_gated_scan_states_bytes
     assert size(0, 0, 8) == 0
     assert size(1, 1, 8) >= 4 * 8
-    assert size(65536, 3, 100) >= 4 * 100 * (65536 // 64)
+    assert size(65536, 3, 100) >= 4 * 100 * (65536 // 8)
     # every sequence's states have a place of their own, wherever sequences begin
-    for lengths in ([1] * 9, [63, 65, 64, 1], [0, 0, 200, 0], [64] * 5, [5, 500]):
-        at, end = 0, 0
-        for s, n in enumerate(lengths):
-            first = at // 64 + s
-            assert first >= end
-            end, at = first + -(-n // 64), at + n
-        assert end * 4 * 8 <= size(at, len(lengths), 8)
+    for rows in (8, 16):                        # from one kept state to the next, of float32 and bfloat16
+        for lengths in ([1] * 9, [63, 65, 64, 1], [0, 0, 200, 0], [64] * 5, [5, 500], [7, 9, 8, 15, 17], [16] * 4):
+            at, end = 0, 0
+            for s, n in enumerate(lengths):
+                first = at // rows + s
+                assert first >= end
+                end, at = first + -(-n // rows), at + n
+            assert end * 4 * 8 <= size(at, len(lengths), 8)
     assert size(-1, 1, 8) == 0 and size(8, -1, 8) == 0 and size(8, 1, 0) == 0 and size(8, 1, twa.TWA_SCAN_MAX_CHANNELS + 1) == 0
 
 
