@@ -497,7 +497,7 @@ cudaError_t scan_launch(twa_ctx* ctx, ScanArgs& a, bool back, int feed) {
   auto blocks = [&]() { return twa_ceil_div(a.channels, channels) * a.sequences * a.cluster; };
   auto rows = [&]() { return a.cluster * SCAN_WARPS * SEG<T> * (SCAN_CHANNELS / channels); };       // of a round
   // Twice as many where there is room for them and rows enough; ragged sequences wait for the longest, which takes the more blocks
-  // (15 ragged sequences of 13138 x 1016 bfloat16, both directions 133 us with one block each, RAGGED_US with two).
+  // (15 ragged sequences of 13138 x 1016 bfloat16, both directions 133 us with one block each, 110 with two).
   const int places = (a.starts ? 2 : 1) * SCAN_RESIDENT * ctx->sm_count;
   auto more = [&]() { return 2 * blocks() <= places && a.tokens > 2LL * rows() * a.sequences; };
   if (ctx->tune_scan_channels && feed == BY_UNITS) channels = ctx->tune_scan_channels;
