@@ -116,39 +116,47 @@ __global__ void __launch_bounds__(DROP_THREADS) dropout_kernel(DropArgs a) {
   }
 }
 
-// Rows on any boundary: a warp takes 256 columns.  Each lane draws the numbers of eight neighbouring columns and keeps one bit
-// of each; elements go by lane, so that accesses are contiguous, and find their bit in another lane.
+// Rows on any boundary: a warp takes DROP_UNITS x 256 columns.  Each lane draws the numbers of eight neighbouring columns and keeps one
+// bit of each; elements go by lane, so that accesses are contiguous, and find their bit in another lane.
+constexpr int DROP_PART = DROP_UNITS * 256;
 template <typename T, bool RESIDUAL>
 __global__ void __launch_bounds__(DROP_THREADS) dropout_any_kernel(DropArgs a) {
   twa_begin(a.x, a.residual, a.rng);
-  const T* x = static_cast<const T*>(a.x);
-  const T* res = static_cast<const T*>(a.residual);
-  T* y = static_cast<T*>(a.y);
   const unsigned task = blockIdx.x * (DROP_THREADS / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   if (task >= a.rows * a.parts.d) return;
   const unsigned row = a.parts.divide(task), part = task - row * a.parts.d;
-  const int c0 = part * 256 + lane;
-  twa_pack<T, 1> raw[8], add[8];
+  const int left = a.cols - static_cast<int>(part) * DROP_PART - static_cast<int>(lane);
+  const T* x = static_cast<const T*>(a.x) + row * a.ldx + part * DROP_PART + lane;
+  const T* res = static_cast<const T*>(a.residual) + (RESIDUAL ? row * a.ldr + part * DROP_PART + lane : 0);
+  T* y = static_cast<T*>(a.y) + row * a.ldy + part * DROP_PART + lane;
+  twa_pack<T, 1> raw[DROP_UNITS * 8], add[DROP_UNITS * 8];
 #pragma unroll
-  for (int k = 0; k < 8; ++k)
-    if (c0 + k * 32 < a.cols) {
-      raw[k].load(x + row * a.ldx + c0 + k * 32);
-      if (RESIDUAL) add[k].load(res + row * a.ldr + c0 + k * 32);
+  for (int k = 0; k < DROP_UNITS * 8; ++k)
+    if (k * 32 < left) {
+      raw[k].load(x + k * 32);
+      if (RESIDUAL) add[k].load(res + k * 32);
     }
   const unsigned long long seed = __ldg(a.rng), step = __ldg(a.rng + 1);
-  Words u[1] = {{{part * 32 + lane, a.row0 + row, a.site, static_cast<uint32_t>(step)}}};
+  Words u[DROP_UNITS];
+#pragma unroll
+  for (int i = 0; i < DROP_UNITS; ++i) u[i] = {{(part * DROP_UNITS + i) * 32 + lane, a.row0 + row, a.site, static_cast<uint32_t>(step)}};
   philox(u, static_cast<uint32_t>(seed), static_cast<uint32_t>(seed >> 32));
-  unsigned bits = 0;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) bits |= (drop_keeps(u[0], e, a.threshold) ? 1u : 0u) << e;
+  for (int i = 0; i < DROP_UNITS; ++i) {
+    unsigned bits = 0;
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    const bool keep = __shfl_sync(0xffffffffu, bits, 4 * k + (lane >> 3)) >> (lane & 7) & 1;
-    if (c0 + k * 32 >= a.cols) continue;
-    float v, r = 0.0f;
-    raw[k].widen(&v);
-    if (RESIDUAL) add[k].widen(&r);
-    y[row * a.ldy + c0 + k * 32] = twa_from_float<T>(keep ? fmaf(v, a.scale, r) : r);
+    for (int e = 0; e < 8; ++e)
+      if (drop_keeps(u[i], e, a.threshold)) bits |= 1u << e;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const bool keep = __shfl_sync(0xffffffffu, bits, 4 * k + (lane >> 3)) >> (lane & 7) & 1;
+      const int n = i * 8 + k;
+      if (n * 32 >= left) continue;
+      float v, r = 0.0f;
+      raw[n].widen(&v);
+      if (RESIDUAL) add[n].widen(&r);
+      y[n * 32] = twa_from_float<T>(keep ? fmaf(v, a.scale, r) : r);
+    }
   }
 }
 
@@ -159,22 +167,19 @@ void drop_launch(twa_ctx* ctx, DropArgs a, int64_t rows) {
   const size_t size = sizeof(T);
   const bool packs = a.cols % 8 == 0 && drop_packs(a.x, a.ldx, size) && drop_packs(a.y, a.ldy, size) &&
                      (!a.residual || drop_packs(a.residual, a.ldr, size));
-  a.parts = Divisor(static_cast<uint32_t>(packs ? a.cols / 8 : twa_ceil_div(a.cols, 256)));
+  a.parts = Divisor(static_cast<uint32_t>(packs ? a.cols / 8 : twa_ceil_div(a.cols, DROP_PART)));
   // tasks of a launch are counted in 31 bits
   const long long most = ((1LL << 31) - DROP_THREADS * DROP_UNITS) / a.parts.d;
   for (long long r = 0; r < rows; r += most) {
     a.row0 = static_cast<unsigned>(r);
     a.rows = static_cast<unsigned>(rows - r < most ? rows - r : most);
     const long long tasks = static_cast<long long>(a.rows) * a.parts.d;
-    if (packs) {
-      const unsigned blocks = static_cast<unsigned>(twa_ceil_div(tasks, DROP_THREADS * DROP_UNITS));
-      if (a.residual) twa_launch(ctx->stream, dropout_kernel<T, true>, blocks, DROP_THREADS, 0, a);
-      else twa_launch(ctx->stream, dropout_kernel<T, false>, blocks, DROP_THREADS, 0, a);
-    } else {
-      const unsigned blocks = static_cast<unsigned>(twa_ceil_div(tasks, DROP_THREADS / 32));
-      if (a.residual) twa_launch(ctx->stream, dropout_any_kernel<T, true>, blocks, DROP_THREADS, 0, a);
-      else twa_launch(ctx->stream, dropout_any_kernel<T, false>, blocks, DROP_THREADS, 0, a);
-    }
+    auto launch = [&](auto kernel, int tasks_a_block) {
+      twa_launch(ctx->stream, kernel, static_cast<unsigned>(twa_ceil_div(tasks, tasks_a_block)), DROP_THREADS, 0, a);
+    };
+    constexpr int WARPS = DROP_THREADS / 32;
+    if (packs) a.residual ? launch(dropout_kernel<T, true>, DROP_THREADS * DROP_UNITS) : launch(dropout_kernel<T, false>, DROP_THREADS * DROP_UNITS);
+    else a.residual ? launch(dropout_any_kernel<T, true>, WARPS) : launch(dropout_any_kernel<T, false>, WARPS);
     a.x = static_cast<const T*>(a.x) + most * a.ldx;
     a.y = static_cast<T*>(a.y) + most * a.ldy;
     if (a.residual) a.residual = static_cast<const T*>(a.residual) + most * a.ldr;

@@ -109,15 +109,15 @@ struct ScanForward {
     return m;
   }
 
-  __device__ __forceinline__ void copy(Rows& ring, int array, const T* from, const void* all, long long ld, int rows, int left) {
+  __device__ __forceinline__ void copy(Rows& ring, int array, const T* from, const void* all, long long ld, int rows) {
     const T* first = static_cast<const T*>(all);
-    ring.copy(array, from, ld, rows, left, first, first + (a.tokens - 1) * ld + a.channels - 1);
+    ring.copy(array, from, ld, rows, at.left, first, first + (a.tokens - 1) * ld + a.channels - 1);
   }
   // A sequence by the whole cluster.
   __device__ __forceinline__ void whole(const Span& s, int seq, char* shared, Joins<CH / 2>& joins, Tiles<CH / 2>& tiles, int& turn) {
     Rows ring(shared, at.warp, at.lane);
-    const int stride = TILE * at.ranks, left = a.channels - at.slice;
-    const bool wide = __all_sync(0xffffffffu, at.n == 2), last_seg = at.warp == SCAN_WARPS - 1 && at.seg == SEGS - 1;
+    const int stride = TILE * at.ranks;
+    const bool last_seg = at.warp == SCAN_WARPS - 1 && at.seg == SEGS - 1;
     int ahead = at.rank * TILE + at.warp * WARP_ROWS;                     // row of the warp's next segments to be fetched
     ring.lies(0, static_cast<const T*>(a.x) + (s.begin + ahead) * a.ldx + at.slice, a.ldx);
     ring.lies(1, static_cast<const T*>(a.f) + (s.begin + ahead) * a.ldf + at.slice, a.ldf);
@@ -127,8 +127,8 @@ struct ScanForward {
     auto fetch = [&]() {
       const int rows = scan_rows(s, ahead, WARP_ROWS);
       if (rows) {
-        copy(ring, 0, x, a.x, a.ldx, rows, left);
-        copy(ring, 1, f, a.f, a.ldf, rows, left);
+        copy(ring, 0, x, a.x, a.ldx, rows);
+        copy(ring, 1, f, a.f, a.ldf, rows);
       }
       ring.filled();
       ahead += stride;
@@ -165,9 +165,11 @@ struct ScanForward {
       if (at.ranks > 1) {
         share_tile<true>(joins, tiles, at, turn);
         in = state;
-        for (int r = 0; r < at.ranks; ++r) {
+#pragma unroll
+        for (int r = 0; r < MAX_CLUSTER; ++r) {
+          const Map m = tiles.tile[turn][r][at.pair];        // at hand early; what lies behind the last rank is not used
           if (r == at.rank) in = state;
-          state = tiles.tile[turn][r][at.pair].of(state);
+          if (r < at.ranks) state = m.of(state);
         }
       } else {
         in = joins.carry[turn ^ 1][at.pair];
@@ -179,7 +181,7 @@ struct ScanForward {
       if (rows) keep_state(at, a.states, slot, a.channels, in);
       if (at.ranks == 1 && last_seg) joins.carry[turn][at.pair] = state = end.of(in);
       turn ^= 1;
-      if (FEED == BY_UNITS && full && wide) {
+      if (FEED == BY_UNITS && full) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
           float lo, hi;
@@ -187,7 +189,7 @@ struct ScanForward {
           ring.put(0, i, lo, hi);
         }
         __syncwarp();
-        ring.flush(0, h, a.ldh);
+        ring.flush(0, h, a.ldh, at.left);
       } else {
         store(s.begin + mine, rows, in);
       }
@@ -251,14 +253,14 @@ struct ScanBackward {
     }
   }
 
-  __device__ __forceinline__ void copy(Rows& ring, int array, const T* from, const void* all, long long ld, int rows, int left) {
+  __device__ __forceinline__ void copy(Rows& ring, int array, const T* from, const void* all, long long ld, int rows) {
     const T* first = static_cast<const T*>(all);
-    ring.copy(array, from, ld, rows, left, first, first + (a.tokens - 1) * ld + a.channels - 1);
+    ring.copy(array, from, ld, rows, at.left, first, first + (a.tokens - 1) * ld + a.channels - 1);
   }
   __device__ __forceinline__ void whole(const Span& s, int seq, char* shared, Joins<CH / 2>& joins, Tiles<CH / 2>& tiles, int& turn) {
     Rows ring(shared, at.warp, at.lane);
-    const int stride = TILE * at.ranks, rounds = (s.len + stride - 1) / stride, left = a.channels - at.slice;
-    const bool wide = __all_sync(0xffffffffu, at.n == 2), first_seg = at.warp == 0 && at.seg == 0;
+    const int stride = TILE * at.ranks, rounds = (s.len + stride - 1) / stride;
+    const bool first_seg = at.warp == 0 && at.seg == 0;
     int ahead = (rounds - 1) * stride + at.rank * TILE + at.warp * WARP_ROWS;
     ring.lies(0, static_cast<const T*>(a.x) + (s.begin + ahead) * a.ldx + at.slice, a.ldx);
     ring.lies(1, static_cast<const T*>(a.f) + (s.begin + ahead) * a.ldf + at.slice, a.ldf);
@@ -274,9 +276,9 @@ struct ScanBackward {
     auto fetch = [&]() {
       const int rows = ahead < 0 ? 0 : scan_rows(s, ahead, WARP_ROWS);
       if (rows) {
-        copy(ring, 0, x, a.x, a.ldx, rows, left);
-        copy(ring, 1, f, a.f, a.ldf, rows, left);
-        copy(ring, 2, g, a.dh, a.lddh, rows, left);
+        copy(ring, 0, x, a.x, a.ldx, rows);
+        copy(ring, 1, f, a.f, a.ldf, rows);
+        copy(ring, 2, g, a.dh, a.lddh, rows);
       }
       ring.filled();
       ahead -= stride;
@@ -314,9 +316,11 @@ struct ScanBackward {
       if (at.ranks > 1) {
         share_tile<false>(joins, tiles, at, turn);
         in = k;
-        for (int r = at.ranks - 1; r >= 0; --r) {
+#pragma unroll
+        for (int r = MAX_CLUSTER - 1; r >= 0; --r) {
+          const Map m = tiles.tile[turn][r][at.pair];
           if (r == at.rank) in = k;
-          k = tiles.tile[turn][r][at.pair].of(k);
+          if (r < at.ranks) k = m.of(k);
         }
       } else {
         in = joins.carry[turn ^ 1][at.pair];
@@ -327,7 +331,7 @@ struct ScanBackward {
       if (SEGS > 1) in = behind.of(in);
       if (at.ranks == 1 && first_seg) joins.carry[turn][at.pair] = k = off.of(in);
       turn ^= 1;
-      if (FEED == BY_UNITS && full && wide) {
+      if (FEED == BY_UNITS && full) {
 #pragma unroll
         for (int i = N - 1; i >= 0; --i)
           back(i, ring.get(2, i).both(), in, [&](float x0, float x1, float f0, float f1) {
@@ -335,8 +339,8 @@ struct ScanBackward {
             ring.put(1, i, f0, f1);
           });
         __syncwarp();
-        ring.flush(0, dx, a.lddx);
-        ring.flush(1, df, a.lddf);
+        ring.flush(0, dx, a.lddx, at.left);
+        ring.flush(1, df, a.lddf, at.left);
       } else {
         store(s.begin + mine, rows, in, [&](int i) { return ring.get(2, i).both(); });
       }

@@ -163,11 +163,12 @@ __device__ __forceinline__ twa_f2 scan_decay(twa_f2 n, twa_f2 v) { return twa_fm
 template <int FEED, int CH>
 struct Place {
   static constexpr int NEXT = FEED == BY_ELEMENTS ? 32 : 1, SEGS = SCAN_CHANNELS / CH, PAIRS = CH / 2;
-  int lane, warp, slice, seg, pair, c, n, rank, ranks;
+  int lane, warp, slice, left, seg, pair, c, n, rank, ranks;      // left: channels of the slice
   __device__ __forceinline__ Place(const ScanArgs& a, int part) {
     lane = threadIdx.x & 31;
     warp = threadIdx.x >> 5;
     slice = part * CH;
+    left = min(CH, a.channels - slice);
     seg = SEGS > 1 ? lane / PAIRS : 0;
     pair = SEGS > 1 ? lane % PAIRS : lane;
     c = slice + (FEED == BY_ELEMENTS ? lane : 2 * pair);
@@ -328,8 +329,10 @@ struct Ring {
   __device__ __forceinline__ void put(int array, int row, float lo, float hi) const {
     Pair<T>::template store<true>(reinterpret_cast<T*>(base + read + array * AREA + row * ROW + mine[0][0]), lo, hi, 2);
   }
-  __device__ __forceinline__ void flush(int array, T* to, long long ld) const {
-    const char* from = base + read + array * AREA + (threadIdx.x & 31) * 16;
+  __device__ __forceinline__ void flush(int array, T* to, long long ld, int channels) const {
+    const int lane = threadIdx.x & 31;
+    const char* from = base + read + array * AREA + lane * 16;
+    if (lane % UNITS * V >= channels) return;
 #pragma unroll
     for (int i = 0; i < SEGS * N; i += EACH) {
       *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(from + i / N * NEXT_SEG + i % N * ROW);

@@ -441,6 +441,24 @@ def test_dropout_and_its_gradient(ctx, rows, cols, dtype, pad, shift):
     ok(ctx)
 
 
+@pytest.mark.parametrize("rows,cols", [(7, 1), (5, 2), (300, 255), (31, 256), (9, 257), (64, 515), (3, 4099)])
+def test_dropout_of_rows_at_other_places_between_words(ctx, rows, cols):
+    """bfloat16 matrices whose rows begin on 4-byte words and between them, alike in all matrices or not."""
+    g = gen(rows * cols)
+    rng = torch.tensor([9, 8], device=DEV)
+    kept = torch.from_numpy(dropout_numbers(9, 8, 7, rows, cols) >= 32768).to(DEV)
+    xv, rv = randn(g, rows, cols), randn(g, rows, cols)
+    for places in (((0, 0),) * 3, ((0, 1),) * 3, ((1, 1),) * 3, ((2, 1), (4, 3), (0, 1)), ((1, 1), (3, 3), (1, 1)), ((0, 0), (0, 1), (0, 0)), ((1, 0), (0, 0), (1, 0))):
+        (_, x), (_, res) = strided(xv, BF16, *places[0]), strided(rv, BF16, *places[1])
+        for residual in (None, res):
+            ybuf, y = blank(rows, cols, BF16, *places[2])
+            twa.twa_dropout(ctx, x, 0.5, rng, 7, y, residual)
+            want = torch.where(kept, 2 * x.float(), 0.0) + (0.0 if residual is None else residual.float())
+            assert torch.equal(y, want.to(BF16))                      # twice a value and one sum: rounded as float32 does
+            assert untouched(ybuf, y)
+    ok(ctx)
+
+
 def test_dropout_at_the_ends_of_its_probability(ctx):
     x = torch.ones(64, 1024, device=DEV)
     rng, y = torch.tensor([1, 2], device=DEV), torch.empty(64, 1024, device=DEV)
