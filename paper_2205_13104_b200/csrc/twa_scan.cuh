@@ -24,6 +24,7 @@ constexpr int SEG = 32 / sizeof(T);                // rows of a segment
 constexpr int STATE_ROWS = SEG<float>;             // from one kept state to the next, at least
 constexpr int SCAN_CHANNELS = 64, SCAN_LEAST_CHANNELS = 16;               // of a block, at most and at least
 constexpr int SHORT_GROUP = SCAN_WARPS;            // sequences of a block where most are short
+constexpr int BRIEF_LOADS = 4;
 constexpr int MAX_CLUSTER = 8;                     // blocks along a sequence
 
 struct ScanArgs {
@@ -33,6 +34,7 @@ struct ScanArgs {
   long long tokens;
   const void* starts;
   int s_type, sequences, channels, slices, cluster;
+  bool by_length;                                  // ragged sequences, the longest first
   const float* h0;
   float* h_last;
   float* states;
@@ -46,8 +48,9 @@ struct Span {
   long long begin;
   int len;
 };
+template <bool RAGGED>
 __device__ __forceinline__ Span scan_span(const ScanArgs& a, int seq, bool report) {
-  if (!a.starts) {
+  if (!RAGGED) {
     const int each = static_cast<int>(a.tokens / a.sequences);
     return {static_cast<long long>(seq) * each, each};
   }
@@ -344,5 +347,223 @@ struct Ring {
     if (FEED == BY_UNITS || WORDS) __syncwarp();  // other lanes fill this stage again
   }
 };
+
+// Affine maps v -> A v + B of two channels.
+struct __align__(16) Map {
+  twa_f2 A, B;
+  __device__ __forceinline__ twa_f2 of(twa_f2 v) const { return twa_fma2(A, v, B); }
+  __device__ __forceinline__ Map after(const Map& m) const { return {twa_mul2(A, m.A), of(m.B)}; }
+};
+// Of a warp's segments, joined in the order in which they are met (FORWARD: from the first): every lane's with those before its own,
+// and, as `before`, those before alone.
+template <bool FORWARD, int SEGS>
+__device__ __forceinline__ Map join_segments(Map m, int seg, Map& before) {
+  before = {twa_pair(1.0f), 0};
+  if constexpr (SEGS > 1) {
+    constexpr int LANES = 32 / SEGS;
+    const int met = FORWARD ? seg : SEGS - 1 - seg;
+    auto from = [&](const Map& v, int lanes) {
+      Map r;
+      r.A = FORWARD ? __shfl_up_sync(0xffffffffu, v.A, lanes) : __shfl_down_sync(0xffffffffu, v.A, lanes);
+      r.B = FORWARD ? __shfl_up_sync(0xffffffffu, v.B, lanes) : __shfl_down_sync(0xffffffffu, v.B, lanes);
+      return r;
+    };
+#pragma unroll
+    for (int o = 1; o < SEGS; o *= 2) {
+      const Map prev = from(m, o * LANES);
+      if (met >= o) m = m.after(prev);
+    }
+    const Map prev = from(m, LANES);
+    if (met) before = prev;
+  }
+  return m;
+}
+
+// What the segments of a tile make of what enters them (the state, or backward k), and what enters the next tile: twice, so that the
+// next ones go beside those being read.
+template <int PAIRS>
+struct Joins {
+  Map seg[2][SCAN_WARPS][PAIRS];
+  twa_f2 carry[2][PAIRS];
+};
+// The same of the tiles of a cluster's blocks.
+template <int PAIRS>
+struct Tiles {
+  Map tile[2][MAX_CLUSTER][PAIRS];
+};
+
+// The blocks of a cluster tell each other what their tiles make of a state: every warp joins its block's segments' maps, from the
+// first on (FORWARD) or from the last, and the warp of each rank stores the tile's into that block.
+template <bool FORWARD, int FEED, int CH>
+__device__ __forceinline__ void share_tile(const Joins<CH / 2>& joins, Tiles<CH / 2>& tiles, const Place<FEED, CH>& at, int turn) {
+  if (at.warp < at.ranks) {
+    Map all = joins.seg[turn][FORWARD ? 0 : SCAN_WARPS - 1][at.pair];
+#pragma unroll
+    for (int i = 1; i < SCAN_WARPS; ++i) all = joins.seg[turn][FORWARD ? i : SCAN_WARPS - 1 - i][at.pair].after(all);
+    if (at.seg == 0) {
+      twa_store_remote(&tiles.tile[turn][at.rank][at.pair].A, at.warp, all.A);
+      twa_store_remote(&tiles.tile[turn][at.rank][at.pair].B, at.warp, all.B);
+    }
+  }
+  twa_cluster_sync();
+}
+static_assert(MAX_CLUSTER <= SCAN_WARPS, "a warp for every rank");
+
+// The sequence that has `place` longer ones before it, of at most SCAN_THREADS; by the whole block, which has `shared` for it.
+__device__ __forceinline__ int by_length(const ScanArgs& a, int place, int* shared) {
+  const int own = threadIdx.x;
+  const int len = own < a.sequences ? scan_span<true>(a, own, false).len : -1;
+  shared[own] = len;
+  __syncthreads();
+  int before = 0;
+  for (int i = 0; i < a.sequences; ++i) before += shared[i] > len || (shared[i] == len && i < own) ? 1 : 0;
+  __syncthreads();
+  if (own < a.sequences && before == place) shared[0] = own;
+  __syncthreads();
+  const int seq = shared[0];
+  __syncthreads();
+  return seq;
+}
+
+// GROUP sequences of a slice of channels a block.  The ones of at most SEG rows go to one warp each, the others to the block, or
+// the cluster.  Offsets on the device are read once and handed on: a block, and a cluster, has one opinion of where its sequences lie.
+// (Equal lengths are a matter of their own: what follows from them alone stays in uniform registers; 8 x 2048 x 2048 bfloat16 forward
+// 47 us, 53 when they come the same way.)
+template <typename Direction, int GROUP, bool RAGGED>
+__device__ __forceinline__ void scan_block(const ScanArgs& a) {
+  typedef Tiles<Direction::CHANNELS / 2> T;
+  extern __shared__ __align__(16) char shared[];
+  __shared__ Joins<Direction::CHANNELS / 2> joins;
+  T& tiles = *reinterpret_cast<T*>(shared + Direction::Rows::BLOCK_BYTES);       // of clusters only
+  const unsigned task = blockIdx.x / a.cluster;
+  const int slice = task % a.slices, first = task / a.slices * GROUP;
+  Direction d(a, slice);
+  if (a.cluster > 1) twa_cluster_sync();           // no block stores into one that has not begun
+  int turn = 0;
+  if constexpr (!RAGGED) {
+    const Span s = scan_span<false>(a, first, false);
+    d.whole(s, first, shared, joins, tiles, turn);
+  } else {
+    __shared__ unsigned long long begins[GROUP], lengths[GROUP];    // lengths: and the sequence's number above them
+    if (d.at.rank == 0) {
+      const int from = GROUP == 1 && a.by_length ? by_length(a, first, reinterpret_cast<int*>(shared)) : first;
+      if (threadIdx.x < GROUP) {
+        const int seq = from + threadIdx.x;
+        Span s = {0, -1};
+        if (seq < a.sequences) s = scan_span<true>(a, seq, slice == 0);
+        const unsigned long long length = static_cast<unsigned long long>(seq) << 32 | static_cast<unsigned>(s.len);
+        begins[threadIdx.x] = static_cast<unsigned long long>(s.begin);
+        lengths[threadIdx.x] = length;
+        for (int r = 1; r < a.cluster; ++r) {
+          twa_store_remote(begins + threadIdx.x, r, static_cast<unsigned long long>(s.begin));
+          twa_store_remote(lengths + threadIdx.x, r, length);
+        }
+      }
+    }
+    if (a.cluster > 1) twa_cluster_sync();
+    else __syncthreads();
+    auto span = [&](int g) { return Span{static_cast<long long>(begins[g]), static_cast<int>(static_cast<unsigned>(lengths[g]))}; };
+    auto number = [&](int g) { return static_cast<int>(lengths[g] >> 32); };
+    if constexpr (GROUP > 1) {
+      const Span s = span(d.at.warp);
+      if (s.len >= 0 && s.len <= Direction::N) Direction::brief(a, d.at, s, number(d.at.warp));
+    }
+    for (int g = 0; g < GROUP; ++g) {
+      const Span s = span(g);
+      if (s.len > Direction::N || (GROUP == 1 && s.len >= 0)) d.whole(s, number(g), shared, joins, tiles, turn);
+    }
+  }
+}
+
+template <typename Direction, int GROUP, bool RAGGED>
+__global__ void __launch_bounds__(SCAN_THREADS, 2) scan_kernel(ScanArgs a) {
+  twa_begin(a.x, a.f, a.dh, a.starts, a.h0, a.states, a.d_last);
+  scan_block<Direction, GROUP, RAGGED>(a);
+}
+// Where no sequence is longer than SEG rows: a warp for each, of each slice.
+template <typename Direction>
+__global__ void __launch_bounds__(SCAN_THREADS) scan_brief_kernel(ScanArgs a) {
+  twa_begin(a.x, a.f, a.dh, a.h0, a.states, a.d_last);
+  const int slice = blockIdx.x % a.slices, seq = blockIdx.x / a.slices * SHORT_GROUP + (threadIdx.x >> 5);
+  if (seq < a.sequences) Direction::brief(a, typename Direction::At(a, slice), scan_span<false>(a, seq, false), seq);
+}
+
+constexpr int SCAN_RESIDENT = 2;                   // blocks of an SM
+
+// ---- the host's side ------------------------------------------------------------------------------------
+// How rows of two pointers and strides can be fetched together.
+inline int scan_feed(const void* p, long long ld, size_t size, int channels, int so_far) {
+  if (so_far == BY_UNITS && (channels * size % 16 || twa_misaligned_to(p, 16) || ld * size % 16)) so_far = BY_PAIRS;
+  if (so_far == BY_PAIRS && (channels % 2 || twa_misaligned_to(p, 2 * size) || ld % 2)) so_far = BY_ELEMENTS;
+  return so_far;
+}
+template <typename Direction, int GROUP, bool RAGGED>
+cudaError_t scan_launch(twa_ctx* ctx, const ScanArgs& a) {
+  auto kernel = scan_kernel<Direction, GROUP, RAGGED>;
+  const size_t smem = Direction::Rows::BLOCK_BYTES + (a.cluster > 1 ? sizeof(Tiles<Direction::CHANNELS / 2>) : 0);
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+  if (e != cudaSuccess) return e;
+  const unsigned blocks = static_cast<unsigned>(twa_ceil_div(a.sequences, GROUP) * a.slices * a.cluster);
+  return twa_launch_clusters(ctx->stream, kernel, blocks, a.cluster, SCAN_THREADS, smem, a);
+}
+template <typename Direction>
+cudaError_t scan_launch(twa_ctx* ctx, const ScanArgs& a) {
+  return a.starts ? scan_launch<Direction, 1, true>(ctx, a) : scan_launch<Direction, 1, false>(ctx, a);
+}
+template <template <typename, int, int> class Direction, typename T>
+cudaError_t scan_launch(twa_ctx* ctx, ScanArgs& a, int feed) {
+  a.cluster = 1;
+  // A warp a sequence: all of them where they are short enough, or, of ragged ones, those that are, where most must be.
+  const bool short_all = !a.starts && a.tokens <= static_cast<long long>(SEG<T>) * a.sequences;
+  if (short_all || (a.starts && 2 * a.tokens <= static_cast<long long>(SEG<T>) * a.sequences)) {
+    a.slices = static_cast<int>(twa_ceil_div(a.channels, SCAN_CHANNELS));
+    if (short_all) {
+      const unsigned blocks = static_cast<unsigned>(twa_ceil_div(a.sequences, SHORT_GROUP) * a.slices);
+      auto launch = [&](auto kernel) { return twa_launch(ctx->stream, kernel, blocks, SCAN_THREADS, 0, a); };
+      return feed == BY_ELEMENTS ? launch(scan_brief_kernel<Direction<T, BY_ELEMENTS, SCAN_CHANNELS>>)
+                                 : launch(scan_brief_kernel<Direction<T, BY_PAIRS, SCAN_CHANNELS>>);
+    }
+    return feed == BY_UNITS   ? scan_launch<Direction<T, BY_UNITS, SCAN_CHANNELS>, SHORT_GROUP, true>(ctx, a)
+           : feed == BY_PAIRS ? scan_launch<Direction<T, BY_PAIRS, SCAN_CHANNELS>, SHORT_GROUP, true>(ctx, a)
+                              : scan_launch<Direction<T, BY_ELEMENTS, SCAN_CHANNELS>, SHORT_GROUP, true>(ctx, a);
+  }
+  int channels = SCAN_CHANNELS;
+  auto blocks = [&]() { return twa_ceil_div(a.channels, channels) * a.sequences * a.cluster; };
+  auto rows = [&]() { return a.cluster * SCAN_WARPS * SEG<T> * (SCAN_CHANNELS / channels); };       // of a round
+  // Twice as many where there is room for them and rows enough; ragged sequences wait for the longest, which takes the more blocks
+  // (15 ragged sequences of 13138 x 1016 bfloat16, both directions 133 us with one block each, 110 with two).
+  const int slots = SCAN_RESIDENT * ctx->sm_count, places = (a.starts ? 2 : 1) * slots;
+  auto more = [&]() { return 2 * blocks() <= places && a.tokens > 2LL * rows() * a.sequences; };
+  if (ctx->tune_scan_channels && feed == BY_UNITS) channels = ctx->tune_scan_channels;
+  else if (feed == BY_UNITS && more()) channels = 32;
+  while (a.cluster < MAX_CLUSTER && more()) a.cluster *= 2;
+  if (!ctx->tune_scan_channels && channels == 32 && more()) channels = 16;
+  if (ctx->tune_scan_cluster) a.cluster = ctx->tune_scan_cluster;
+  // Ragged sequences that do not all begin at once go by their length, the longest first (12 ragged sequences of 16384 x 2048 bfloat16
+  // 88 us forward in their own order, 72 so); where there are many more than begin at once, a late long one is rare, and finding
+  // a block's sequence costs each of them (200 of 32768 x 1024: 70 and 104 us).
+  a.by_length = a.starts && a.sequences <= SCAN_THREADS && blocks() > slots && blocks() <= 2 * slots;
+  a.slices = static_cast<int>(twa_ceil_div(a.channels, channels));
+  if (feed == BY_PAIRS) return scan_launch<Direction<T, BY_PAIRS, SCAN_CHANNELS>>(ctx, a);
+  if (feed == BY_ELEMENTS) return scan_launch<Direction<T, BY_ELEMENTS, SCAN_CHANNELS>>(ctx, a);
+  return channels == 64   ? scan_launch<Direction<T, BY_UNITS, 64>>(ctx, a)
+         : channels == 32 ? scan_launch<Direction<T, BY_UNITS, 32>>(ctx, a)
+                          : scan_launch<Direction<T, BY_UNITS, 16>>(ctx, a);
+}
+template <template <typename, int, int> class Direction>
+cudaError_t scan_launch(twa_ctx* ctx, ScanArgs& a, int dtype, int feed) {
+  return dtype == TWA_BF16 ? scan_launch<Direction, bf16>(ctx, a, feed) : scan_launch<Direction, float>(ctx, a, feed);
+}
+
+// Arguments that both directions have.
+inline int scan_check(twa_ctx* ctx, int dtype, int64_t tokens, int channels, const void* starts, int s_type, int sequences) {
+  if (!ctx || !twa_dtype_ok(dtype) || tokens < 0 || channels < 1 || sequences < 0 || (starts && !twa_itype_ok(s_type))) return TWA_ERR_INVALID_ARG;
+  if (tokens > TWA_SCAN_MAX_TOKENS || channels > TWA_SCAN_MAX_CHANNELS || sequences > TWA_SCAN_MAX_SEQUENCES) return TWA_ERR_UNSUPPORTED;
+  if (!starts && (sequences ? tokens % sequences : tokens)) return TWA_ERR_INVALID_ARG;
+  if (starts && twa_misaligned_to(starts, twa_itype_size(s_type))) return TWA_ERR_MISALIGNED;
+  // blocks of a launch
+  if (static_cast<long long>(sequences) * twa_ceil_div(channels, SCAN_LEAST_CHANNELS) * MAX_CLUSTER > 0x7FFFFFFFLL) return TWA_ERR_UNSUPPORTED;
+  return TWA_OK;
+}
 
 }  // namespace
