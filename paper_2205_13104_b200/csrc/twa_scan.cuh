@@ -161,6 +161,9 @@ __device__ __forceinline__ twa_f2 scan_step(twa_f2 n, twa_f2 h, twa_f2 x) { retu
 // a times v: what a step makes of a state where x is 0.
 __device__ __forceinline__ twa_f2 scan_decay(twa_f2 n, twa_f2 v) { return twa_fma2(n, v, scan_pick(n, v, twa_pair(0.0f))); }
 
+// A value that is the same for the whole warp, in a register of the warp's: addresses and counts that follow from it cost a lane nothing.
+__device__ __forceinline__ int uniform(int v) { return static_cast<int>(__reduce_max_sync(0xffffffffu, static_cast<unsigned>(v))); }
+
 // Where a thread stands: its two channels, c and c + 1 or c and c + 32, of which n exist; which of its warp's segments it has, and which
 // pair of the segment's channels; its block's rank along the sequence.
 template <int FEED, int CH>
@@ -169,7 +172,7 @@ struct Place {
   int lane, warp, slice, left, seg, pair, c, n, rank, ranks;      // left: channels of the slice
   __device__ __forceinline__ Place(const ScanArgs& a, int part) {
     lane = threadIdx.x & 31;
-    warp = threadIdx.x >> 5;
+    warp = uniform(threadIdx.x >> 5);
     slice = part * CH;
     left = min(CH, a.channels - slice);
     seg = SEGS > 1 ? lane / PAIRS : 0;
@@ -462,8 +465,11 @@ __device__ __forceinline__ void scan_block(const ScanArgs& a) {
     }
     if (a.cluster > 1) twa_cluster_sync();
     else __syncthreads();
-    auto span = [&](int g) { return Span{static_cast<long long>(begins[g]), static_cast<int>(static_cast<unsigned>(lengths[g]))}; };
-    auto number = [&](int g) { return static_cast<int>(lengths[g] >> 32); };
+    auto span = [&](int g) {
+      const unsigned lo = uniform(static_cast<int>(begins[g])), hi = uniform(static_cast<int>(begins[g] >> 32));
+      return Span{static_cast<long long>(static_cast<unsigned long long>(hi) << 32 | lo), uniform(static_cast<int>(lengths[g]))};
+    };
+    auto number = [&](int g) { return uniform(static_cast<int>(lengths[g] >> 32)); };
     if constexpr (GROUP > 1) {
       const Span s = span(d.at.warp);
       if (s.len >= 0 && s.len <= Direction::N) Direction::brief(a, d.at, s, number(d.at.warp));
