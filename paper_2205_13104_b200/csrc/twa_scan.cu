@@ -50,9 +50,10 @@ struct ScanForward {
     ring.copy(array, from, ld, rows, at.left, first, first + (a.tokens - 1) * ld + a.channels - 1);
   }
   // A sequence by the whole cluster.
-  __device__ __forceinline__ void whole(const Span& s, int seq, char* shared, Joins<CH / 2>& joins, Tiles<CH / 2>& tiles, int& turn) {
+  __device__ __forceinline__ void whole(Span s, int seq, char* shared, Joins<CH / 2>& joins, Tiles<CH / 2>& tiles, int& turn) {
     Rows ring(shared, at.warp, at.lane);
     const int stride = TILE * at.ranks;
+    unsigned phases = 0;
     const bool last_seg = at.warp == SCAN_WARPS - 1 && at.seg == SEGS - 1;
     int ahead = at.rank * TILE + at.warp * WARP_ROWS;                     // row of the warp's next segments to be fetched
     ring.lies(0, static_cast<const T*>(a.x) + (s.begin + ahead) * a.ldx + at.slice, a.ldx);
@@ -76,10 +77,11 @@ struct ScanForward {
     twa_f2 state = at.state(a.h0, seq, a.channels);
     if (last_seg) joins.carry[turn ^ 1][at.pair] = state;
     int slot = scan_slot<T>(s, seq) + (at.rank * SCAN_WARPS + at.warp) * SEGS + at.seg;
-    for (int t = 0; t < s.len; t += stride, slot += at.ranks * SCAN_WARPS * SEGS, h += stride * a.ldh) {
+    const int end_row = s.len;
+    for (int t = 0; t < end_row; t += stride, slot += at.ranks * SCAN_WARPS * SEGS, h += stride * a.ldh) {
       const int first = t + at.rank * TILE + at.warp * WARP_ROWS, mine = first + at.seg * N;
-      const bool full = first + WARP_ROWS <= s.len;                       // the whole warp's rows exist
-      const int rows = scan_rows(s, mine, N);
+      bool full = first + WARP_ROWS <= s.len;                       // the whole warp's rows exist
+      int rows = scan_rows(s, mine, N);
       ring.wait();
       fetch();
       Map end;
@@ -99,7 +101,12 @@ struct ScanForward {
       __syncthreads();
       twa_f2 in;
       if (at.ranks > 1) {
-        share_tile<true>(joins, tiles, at, turn);
+        if (!share_tile<true>(a, joins, tiles, at, turn, phases, s.len < 0)) {
+          if (s.len >= 0 && threadIdx.x == 0) twa_set_status(a.status, TWA_ERR_TIMEOUT, seq);
+          s.len = -1;                              // nothing more is stored
+          rows = 0;
+          full = false;
+        }
         in = state;
 #pragma unroll
         for (int r = 0; r < MAX_CLUSTER; ++r) {
@@ -131,7 +138,7 @@ struct ScanForward {
       }
       ring.done();
     }
-    if (last_seg && at.rank == 0) at.keep(a.h_last, seq, a.channels, state);
+    if (last_seg && at.rank == 0 && s.len >= 0) at.keep(a.h_last, seq, a.channels, state);
   }
 
   // A sequence of at most SEG rows, by one warp: the state before each row is at hand, and rows go by, BRIEF_LOADS under way together.
@@ -194,7 +201,7 @@ int twa_gated_scan(twa_ctx* ctx, const void* x, int64_t ldx, const void* f, int6
   ScanArgs a = {};
   a.x = x, a.ldx = ldx, a.f = f, a.ldf = ldf, a.h = h, a.ldh = ldh;
   a.tokens = tokens, a.channels = channels, a.starts = starts, a.s_type = s_type, a.sequences = sequences;
-  a.h0 = h0, a.h_last = h_last, a.states = static_cast<float*>(states), a.status = ctx->d_status;
+  a.h0 = h0, a.h_last = h_last, a.states = static_cast<float*>(states), a.status = ctx->d_status, a.wait_limit_ns = ctx->wait_limit_ns;
   const int feed = scan_feed(h, ldh, size, channels, scan_feed(f, ldf, size, channels, scan_feed(x, ldx, size, channels, BY_UNITS)));
   TWA_CUDA_OK(ctx, scan_launch<ScanForward>(ctx, a, dtype, feed));
   return TWA_OK;

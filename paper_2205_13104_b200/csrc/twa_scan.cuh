@@ -41,6 +41,7 @@ struct ScanArgs {
   const float* d_last;
   float* dh0;
   int* status;
+  unsigned long long wait_limit_ns;
 };
 
 // Rows of a sequence; len -1: its offsets are wrong and it is left alone.
@@ -389,26 +390,38 @@ struct Joins {
   Map seg[2][SCAN_WARPS][PAIRS];
   twa_f2 carry[2][PAIRS];
 };
-// The same of the tiles of a cluster's blocks.
+// The same of the tiles of a cluster's blocks, and how they arrive.
 template <int PAIRS>
 struct Tiles {
   Map tile[2][MAX_CLUSTER][PAIRS];
+  unsigned long long arrived[2];
+  int abort_flag;
 };
 
 // The blocks of a cluster tell each other what their tiles make of a state: every warp joins its block's segments' maps, from the
-// first on (FORWARD) or from the last, and the warp of each rank stores the tile's into that block.
+// first on (FORWARD) or from the last, and the warp of each rank sends the tile's to that block, whose barrier counts the bytes.
+// (A barrier of the whole cluster instead would also wait until every thread's results are in memory: 1 x 65536 x 512 float32
+// both directions 277 us, so 237.)  Two sets take turns: a block sends into one again only after it has the maps of the
+// round between, which the receiver sends when all its warps have read the first.  False: the maps did not come in time, now or (lost) before.
 template <bool FORWARD, int FEED, int CH>
-__device__ __forceinline__ void share_tile(const Joins<CH / 2>& joins, Tiles<CH / 2>& tiles, const Place<FEED, CH>& at, int turn) {
+__device__ __forceinline__ bool share_tile(const ScanArgs& a, const Joins<CH / 2>& joins, Tiles<CH / 2>& tiles, const Place<FEED, CH>& at, int turn,
+                                           unsigned& phases, bool lost) {
+  if (threadIdx.x == 0 && !lost) twa_mbar_expect_tx(twa_smem_u32(&tiles.arrived[turn]), at.ranks * (CH / 2) * sizeof(Map));
   if (at.warp < at.ranks) {
     Map all = joins.seg[turn][FORWARD ? 0 : SCAN_WARPS - 1][at.pair];
 #pragma unroll
     for (int i = 1; i < SCAN_WARPS; ++i) all = joins.seg[turn][FORWARD ? i : SCAN_WARPS - 1 - i][at.pair].after(all);
     if (at.seg == 0) {
-      twa_store_remote(&tiles.tile[turn][at.rank][at.pair].A, at.warp, all.A);
-      twa_store_remote(&tiles.tile[turn][at.rank][at.pair].B, at.warp, all.B);
+      uint32_t to, bar;
+      asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(twa_smem_u32(&tiles.tile[turn][at.rank][at.pair])), "r"(at.warp));
+      asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(bar) : "r"(twa_smem_u32(&tiles.arrived[turn])), "r"(at.warp));
+      asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.b64 [%0], {%1, %2}, [%3];" ::"r"(to), "l"(all.A), "l"(all.B), "r"(bar)
+                   : "memory");
     }
   }
-  twa_cluster_sync();
+  const bool good = twa_wait(&tiles.arrived[turn], phases >> turn & 1, &tiles.abort_flag, a.wait_limit_ns);
+  phases ^= 1u << turn;
+  return good;
 }
 static_assert(MAX_CLUSTER <= SCAN_WARPS, "a warp for every rank");
 
@@ -441,7 +454,14 @@ __device__ __forceinline__ void scan_block(const ScanArgs& a) {
   const unsigned task = blockIdx.x / a.cluster;
   const int slice = task % a.slices, first = task / a.slices * GROUP;
   Direction d(a, slice);
-  if (a.cluster > 1) twa_cluster_sync();           // no block stores into one that has not begun
+  if (a.cluster > 1) {
+    if (threadIdx.x == 0) {
+      for (int i = 0; i < 2; ++i) twa_mbar_init(twa_smem_u32(&tiles.arrived[i]), 1);
+      tiles.abort_flag = 0;
+      twa_fence_barrier_init();
+    }
+    twa_cluster_sync();                            // no block stores into one that has not begun
+  }
   int turn = 0;
   if constexpr (!RAGGED) {
     const Span s = scan_span<false>(a, first, false);
@@ -479,6 +499,7 @@ __device__ __forceinline__ void scan_block(const ScanArgs& a) {
       if (s.len > Direction::N || (GROUP == 1 && s.len >= 0)) d.whole(s, number(g), shared, joins, tiles, turn);
     }
   }
+  if (a.cluster > 1) twa_cluster_sync();           // none ends while another may still send to it, one whose wait ran out included
 }
 
 template <typename Direction, int GROUP, bool RAGGED>
