@@ -23,6 +23,7 @@ namespace {
 
 // ---- the sort -----------------------------------------------------------------------------------
 constexpr int SORT_THREADS = 1024, SORT_WARPS = SORT_THREADS / 32;
+constexpr int SORT_BLOCKS = 16;                   // of a cluster at most
 constexpr int SORT_LOADS = 8;                     // ids of a lane under way together
 
 struct SortArgs {
@@ -47,6 +48,7 @@ __device__ __forceinline__ int expert_of(const SortArgs& a, int i, bool report) 
 
 // Between the walks place holds an assignment's expert and its number among its warp's of that expert.
 constexpr int RANK_BITS = 21;
+static_assert(TWA_EXPERTS_MAX <= 32 * 32, "a lane for every 32 experts");
 static_assert(TWA_EXPERTS_MAX < 1 << (32 - RANK_BITS) && TWA_EXPERTS_MAX_ASSIGNMENTS / (8 * SORT_WARPS) + 32 < 1 << RANK_BITS, "both fit");
 
 // Sorts with `blocks` blocks, this one the rank-th.  place: where every assignment's place goes; `write`: whether this block writes
@@ -56,6 +58,7 @@ __device__ __forceinline__ void sort_block(const SortArgs& a, int blocks, int ra
   int* base = total + a.experts;                  // place of this block's first assignment of an expert
   int* all = base + a.experts;                    // of all blocks
   int* count = all + a.experts;                   // [warps][experts]
+  __shared__ int group[TWA_EXPERTS_MAX / 32];     // assignments of 32 experts
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, threads = a.warps * 32;
   for (int i = threadIdx.x; i < a.warps * a.experts; i += threads) count[i] = 0;
   __syncthreads();
@@ -88,46 +91,57 @@ __device__ __forceinline__ void sort_block(const SortArgs& a, int blocks, int ra
   __syncthreads();
   for (int e = threadIdx.x; e < a.experts; e += threads) {
     int sum = 0;
-#pragma unroll 4
-    for (int w = 0; w < a.warps; ++w) {
-      const int c = count[w * a.experts + e];
-      count[w * a.experts + e] = sum;
-      sum += c;
+    for (int w0 = 0; w0 < a.warps; w0 += 8) {
+      int c[8];
+#pragma unroll
+      for (int w = 0; w < 8; ++w) c[w] = w0 + w < a.warps ? count[(w0 + w) * a.experts + e] : 0;
+#pragma unroll
+      for (int w = 0; w < 8; ++w) {
+        if (w0 + w < a.warps) count[(w0 + w) * a.experts + e] = sum;
+        sum += c[w];
+      }
     }
     total[e] = sum;
   }
   if (blocks > 1) twa_cluster_sync();
   else __syncthreads();
-  // assignments of every expert in all blocks, and of them those in blocks before this one
-  for (int e = threadIdx.x; e < a.experts; e += threads) {
+  // Assignments of every expert in all blocks, those of them in blocks before this one, and those of the experts before it among
+  // its 32; then those of the 32s before.
+  for (int e0 = warp * 32; e0 < a.experts; e0 += threads) {
+    const int e = e0 + lane;
     int before = 0, sum = 0;
-    for (int r = 0; r < blocks; ++r) {
-      const int c = r == rank ? total[e] : twa_remote(total + e, r);
-      before += r < rank ? c : 0;
-      sum += c;
+    if (e < a.experts) {
+      int c[SORT_BLOCKS];
+#pragma unroll
+      for (int r = 0; r < SORT_BLOCKS; ++r) c[r] = r < blocks ? (r == rank ? total[e] : twa_remote(total + e, r)) : 0;
+#pragma unroll
+      for (int r = 0; r < SORT_BLOCKS; ++r) {
+        before += r < rank ? c[r] : 0;
+        sum += c[r];
+      }
     }
-    base[e] = before;
-    all[e] = sum;
+    int upto = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += v;
+    }
+    if (e < a.experts) {
+      base[e] = before;
+      all[e] = upto - sum;
+    }
+    if (lane == 31) group[e0 >> 5] = upto;
   }
   if (blocks > 1) twa_cluster_sync();             // no block ends while another reads its totals
   else __syncthreads();
-  if (warp == 0) {
-    int sum = 0;
-    for (int e0 = 0; e0 < a.experts; e0 += 32) {
-      const int e = e0 + lane, c = e < a.experts ? all[e] : 0;
-      int upto = c;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int v = __shfl_up_sync(0xffffffffu, upto, o);
-        if (lane >= o) upto += v;
-      }
-      if (e < a.experts) {
-        base[e] += sum + upto - c;
-        if (write && rank == 0) a.starts[e] = sum + upto - c;
-      }
-      sum += __shfl_sync(0xffffffffu, upto, 31);
+  for (int e0 = warp * 32; e0 < a.experts; e0 += threads) {
+    const int e = e0 + lane;
+    const int ahead = __reduce_add_sync(0xffffffffu, lane < e0 >> 5 ? group[lane] : 0);
+    if (e < a.experts) {
+      base[e] += ahead + all[e];
+      if (write && rank == 0) a.starts[e] = ahead + all[e];
     }
-    if (write && rank == 0 && lane == 0) a.starts[a.experts] = sum;
+    if (write && rank == 0 && lane == 0 && e0 + 32 >= a.experts) a.starts[a.experts] = ahead + group[e0 >> 5];
   }
   __syncthreads();
   for (int i = first + lane; i < last; i += 32 * SORT_LOADS) {
@@ -402,19 +416,19 @@ cudaError_t sort_cluster(twa_ctx* ctx, int* most) {
     e = cudaFuncSetAttribute(expert_sort_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(int) * (SORT_WARPS + 3) * TWA_EXPERTS_MAX);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(16);
+    cfg.gridDim = dim3(SORT_BLOCKS);
     cfg.blockDim = dim3(SORT_THREADS);
     cfg.dynamicSmemBytes = sizeof(int) * (SORT_WARPS + 3) * TWA_EXPERTS_MAX;
     cudaLaunchAttribute attr = {};
     attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = 16;
+    attr.val.clusterDim.x = SORT_BLOCKS;
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
     int clusters = 0;
     e = cudaOccupancyMaxActiveClusters(&clusters, expert_sort_kernel, &cfg);
     if (e != cudaSuccess) return e;
-    ctx->expert_cluster = clusters > 0 ? 16 : 8;
+    ctx->expert_cluster = clusters > 0 ? SORT_BLOCKS : 8;
   }
   *most = ctx->expert_cluster;
   return cudaSuccess;
@@ -507,7 +521,7 @@ int twa_expert_dispatch(twa_ctx* ctx, const void* x, int64_t ldx, twa_dtype dtyp
   SortArgs s = {ids, id_type, static_cast<int>(tokens * top), top, experts, 1, SORT_WARPS, 0, place, order, starts, ctx->d_status};
   while (experts >> s.bits) ++s.bits;
   const bool moves = x && tokens;
-  const bool small = moves && s.count <= SMALL_COUNT && sizeof(int) * ((MOVE_WARPS + 3) * experts + SMALL_COUNT) <= 48 * 1024;
+  const bool small = moves && s.count <= SMALL_COUNT && sizeof(int) * ((MOVE_WARPS + 3) * experts + SMALL_COUNT + TWA_EXPERTS_MAX / 32) <= 48 * 1024;
   if (!small) {
     const size_t smem = sizeof(int) * (s.warps + 3) * experts;
     int blocks = 1, most;
