@@ -633,8 +633,9 @@ int twa_dropout_backward(twa_ctx* ctx, const void* dy, int64_t lddy, twa_dtype d
  *  states    out: what the backward call needs, twa_gated_scan_states_bytes(tokens, sequences, channels), 16-byte
  *            aligned, or NULL.
  * States are float32 throughout.  A value that is not finite spoils its own channel from its token to the sequence's end.
- * Device-side error: TWA_ERR_INVALID_ARG, detail = a sequence whose starts go down or leave 0 .. tokens; it is left alone,
- * and rows that starts give to two sequences are undefined. */
+ * Device-side errors: TWA_ERR_INVALID_ARG, detail = a sequence whose starts go down or leave 0 .. tokens; it is left alone,
+ * and rows that starts give to two sequences are undefined.  TWA_ERR_TIMEOUT, detail = a sequence that several blocks share, one of
+ * which did not hear from another in time; some of its outputs are then not written. */
 int twa_gated_scan(twa_ctx* ctx, const void* x, int64_t ldx, const void* f, int64_t ldf, twa_dtype dtype, int64_t tokens,
                    int channels, const void* starts, twa_itype s_type, int sequences, const float* h0, void* h, int64_t ldh,
                    float* h_last, void* states, size_t states_bytes);
@@ -643,7 +644,8 @@ int twa_gated_scan(twa_ctx* ctx, const void* x, int64_t ldx, const void* f, int6
  *  states    as the forward call with the same x, f, starts and h0 left them.
  *  d_last    sequences x channels floats, the gradient of h_last, or NULL (0).
  *  dx, df    tokens x channels of dtype; each may be one of dh, x, f (same row stride), not the same.
- *  dh0       out: sequences x channels floats, or NULL; may be d_last. */
+ *  dh0       out: sequences x channels floats, or NULL; may be d_last.
+ * Device-side errors as above. */
 int twa_gated_scan_backward(twa_ctx* ctx, const void* dh, int64_t lddh, const void* x, int64_t ldx, const void* f, int64_t ldf,
                             twa_dtype dtype, int64_t tokens, int channels, const void* starts, twa_itype s_type, int sequences,
                             const void* states, size_t states_bytes, const float* d_last, void* dx, int64_t lddx, void* df,

@@ -432,7 +432,7 @@ __device__ __forceinline__ bool share_tile(const ScanArgs& a, const Joins<CH / 2
   }
   const bool good = twa_wait(&tiles.arrived[turn], phases >> turn & 1, &tiles.abort_flag, a.wait_limit_ns);
   phases ^= 1u << turn;
-  return good;
+  return __all_sync(0xffffffffu, good);            // a warp goes on as one
 }
 static_assert(MAX_CLUSTER <= SCAN_WARPS, "a warp for every rank");
 
