@@ -1083,33 +1083,35 @@ def twa_gated_scan_backward(ctx, dh, x, f, states, dx, df, starts=None, sequence
 
 def _places(place, dev):
     """Tokens and top of a matrix of places."""
-    if place.dim() != 2 or place.dtype is not torch.int32 or not place.is_contiguous() or place.get_device() != dev:
-        raise ValueError(f"place: a contiguous (tokens, top) matrix of int32 on the context's device is needed, got {tuple(place.shape)} of "
+    shape = place.shape
+    if len(shape) != 2 or place.dtype is not torch.int32 or not place.is_contiguous() or place.get_device() != dev:
+        raise ValueError(f"place: a contiguous (tokens, top) matrix of int32 on the context's device is needed, got {tuple(shape)} of "
                          f"{place.dtype} on {place.device}")
-    return place.shape
+    return shape
 
 
 def twa_expert_dispatch(ctx, x, ids, experts, place, starts, out, order=None):
     """x: (tokens, dim); ids: (tokens, top) int32 or int64, -1 for none; place: (tokens, top) int32; starts: (experts + 1,) int32;
     out: (tokens * top or more, dim); order: (tokens * top,) int32, or None.  x and out may both be None: places only."""
     dev = ctx.device
-    tokens, top = _places(place, dev)
-    if ids.shape != place.shape:
-        raise ValueError(f"ids: a (tokens, top) matrix as place is needed, got {tuple(ids.shape)} and {tuple(place.shape)}")
-    code = _numbers(ids, tokens * top, "ids", dev)
-    if (x is None) != (out is None):
+    shape = tokens, top = _places(place, dev)
+    code = _ITYPES.get(ids.dtype)
+    if code is None or ids.shape != shape or not ids.is_contiguous() or ids.get_device() != dev:
+        raise ValueError(f"ids: a contiguous matrix as place, {tuple(shape)}, of int32 or int64 on the context's device is needed, got "
+                         f"{tuple(ids.shape)} of {ids.dtype} on {ids.device}")
+    count = tokens * top
+    if x is None and out is None:
+        source, ld, dt, dim, to, ldo = None, 0, TWA_F32, 1, None, 0
+    elif x is None or out is None:
         raise ValueError("x and out: both or neither")
-    rows, dim, dt = (None, 0), 1, TWA_F32
-    to = (None, 0)
-    if x is not None:
-        dt, dim = _floats(x, "x"), x.shape[1]
-        rows = x.data_ptr(), _rows(x, (tokens, dim), "x", dev)
-        if len(out) < tokens * top:
-            raise ValueError(f"out: at least {tokens * top} rows are needed, got {len(out)}")
-        to = out.data_ptr(), _rows(out, (len(out), dim), "out", dev, x.dtype)
-    rc = load().twa_expert_dispatch(ctx, *rows, dt, tokens, dim, ids.data_ptr(), code, top, experts, place.data_ptr(),
+    else:
+        dt, (rows, dim) = _floats(x, "x"), out.shape
+        if rows < count:
+            raise ValueError(f"out: at least {count} rows are needed, got {rows}")
+        source, ld, to, ldo = x.data_ptr(), _rows(x, (tokens, dim), "x", dev), out.data_ptr(), _rows(out, (rows, dim), "out", dev, x.dtype)
+    rc = load().twa_expert_dispatch(ctx, source, ld, dt, tokens, dim, ids.data_ptr(), code, top, experts, place.data_ptr(),
                                     _vector(starts, experts + 1, torch.int32, "starts", dev),
-                                    _vector(order, tokens * top, torch.int32, "order", dev), *to)
+                                    _vector(order, count, torch.int32, "order", dev), to, ldo)
     if rc:
         _check(rc, "twa_expert_dispatch", ctx)
     return out
