@@ -25,11 +25,12 @@ struct ScanForward {
     A[i] = i ? scan_decay(n, A[i - 1]) : scan_decay(n, twa_pair(1.0f));
     L[i] = i ? scan_step(n, L[i - 1], x.both()) : scan_step(n, 0, x.both());
   }
+  template <bool FULL>
   __device__ __forceinline__ void store(long long first, int rows, twa_f2 in) {
     T* h = static_cast<T*>(a.h) + first * a.ldh + at.c;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      if (i < rows && at.n > 0) {
+      if ((FULL || i < rows) && (!TOGETHER || at.n > 0)) {
         float lo, hi;
         twa_unpair(twa_fma2(A[i], in, L[i]), lo, hi);
         Pair<T>::template store<TOGETHER>(h, lo, hi, at.n);
@@ -133,8 +134,10 @@ struct ScanForward {
         }
         __syncwarp();
         ring.flush(0, h, a.ldh, at.left);
+      } else if (full) {
+        store<true>(s.begin + mine, rows, in);
       } else {
-        store(s.begin + mine, rows, in);
+        store<false>(s.begin + mine, rows, in);
       }
       ring.done();
     }

@@ -85,6 +85,18 @@ __device__ __forceinline__ int scan_rows(const Span& s, int r, int most) { retur
 // are contiguous.
 enum { BY_UNITS, BY_PAIRS, BY_ELEMENTS };
 
+// Stores an element where `exists`: a predicate, no branch.
+template <int OFFSET>
+__device__ __forceinline__ void scan_store(float* p, uint32_t v, bool exists) {
+  asm volatile("{\n.reg .pred q;\nsetp.ne.b32 q, %2, 0;\n@q st.global.b32 [%0 + %3], %1;\n}" ::"l"(p), "r"(v), "r"(static_cast<int>(exists)), "n"(OFFSET)
+               : "memory");
+}
+template <int OFFSET>
+__device__ __forceinline__ void scan_store(bf16* p, unsigned short v, bool exists) {
+  asm volatile("{\n.reg .pred q;\nsetp.ne.b32 q, %2, 0;\n@q st.global.b16 [%0 + %3], %1;\n}" ::"l"(p), "h"(v), "r"(static_cast<int>(exists)), "n"(OFFSET)
+               : "memory");
+}
+
 // Two elements in one or two registers.
 template <typename T>
 struct Pair;
@@ -106,8 +118,8 @@ struct Pair<float> {
   static __device__ __forceinline__ void store(float* p, float a, float b, int n) {
     if constexpr (TOGETHER) *reinterpret_cast<float2*>(p) = make_float2(a, b);
     else {
-      p[0] = a;
-      if (n > 1) p[32] = b;
+      scan_store<0>(p, __float_as_uint(a), n > 0);
+      scan_store<128>(p, __float_as_uint(b), n > 1);
     }
   }
 };
@@ -130,8 +142,8 @@ struct Pair<bf16> {
   static __device__ __forceinline__ void store(bf16* p, float a, float b, int n) {
     if constexpr (TOGETHER) *reinterpret_cast<uint32_t*>(p) = twa_bf16_pair(a, b);
     else {
-      p[0] = twa_from_float<bf16>(a);
-      if (n > 1) p[32] = twa_from_float<bf16>(b);
+      scan_store<0>(p, __bfloat16_as_ushort(twa_from_float<bf16>(a)), n > 0);
+      scan_store<64>(p, __bfloat16_as_ushort(twa_from_float<bf16>(b)), n > 1);
     }
   }
 };
@@ -298,14 +310,23 @@ struct Ring {
     } else {
       const T* row = from - 2 * lane;
       const bool edge = row <= first || row + (rows - 1) * ld + channels > last;         // of the matrix; true of the whole warp
+      // of the even and the odd rows: one begins inside a word, its word of this lane, and whether it has one
+      const int odd[2] = {(mine[array][0] >> 1) - lane, (mine[array][1] >> 1) - lane};
+      const T* word[2] = {from - odd[0], from + ld - odd[1]};
+      const bool has[2] = {2 * lane < channels + odd[0], 2 * lane < channels + odd[1]};
+      if (rows == N && !edge) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const int odd = (mine[array][i & 1] >> 1) - lane;                                // the row begins inside a word
-        const char* word = reinterpret_cast<const char*>(from) - 2 * odd;
-        if (i < rows && 2 * lane < channels + odd &&
-            (!edge || (reinterpret_cast<const T*>(word) >= first && reinterpret_cast<const T*>(word) < last)))
-          copy_async<4>(area + i * ROW + lane * 4, word);
-        from += ld;
+        for (int i = 0; i < N; ++i) {
+          if (has[i & 1]) copy_async<4>(area + i * ROW + lane * 4, word[i & 1]);
+          word[i & 1] += 2 * ld;
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          if (i < rows && has[i & 1] && (!edge || (word[i & 1] >= first && word[i & 1] < last)))
+            copy_async<4>(area + i * ROW + lane * 4, word[i & 1]);
+          word[i & 1] += 2 * ld;
+        }
       }
       // the last element of a row that begins inside a word, alone in one more
       if (lane < rows && channels >= SCAN_CHANNELS && (lane & 1 ? mine[array][1] : mine[array][0]) != lane * 2) {

@@ -48,15 +48,15 @@ struct ScanBackward {
     out(x0, x1, f0, f1);
   }
   // Of the first `rows` rows from `first` on, straight to memory.
-  template <typename Dh>
+  template <bool FULL, typename Dh>
   __device__ __forceinline__ void store(long long first, int rows, twa_f2& k, Dh dh) {
     T* dx = static_cast<T*>(a.dx) + (first + N - 1) * a.lddx + at.c;
     T* df = static_cast<T*>(a.df) + (first + N - 1) * a.lddf + at.c;
 #pragma unroll
     for (int i = N - 1; i >= 0; --i) {
-      if (i < rows)
+      if (FULL || i < rows)
         back(i, dh(i), k, [&](float x0, float x1, float f0, float f1) {
-          if (at.n > 0) {
+          if (!TOGETHER || at.n > 0) {
             Pair<T>::template store<TOGETHER>(dx, x0, x1, at.n);
             Pair<T>::template store<TOGETHER>(df, f0, f1, at.n);
           }
@@ -160,8 +160,10 @@ struct ScanBackward {
         __syncwarp();
         ring.flush(0, dx, a.lddx, at.left);
         ring.flush(1, df, a.lddf, at.left);
+      } else if (full) {
+        store<true>(s.begin + mine, rows, in, [&](int i) { return ring.get(2, i).both(); });
       } else {
-        store(s.begin + mine, rows, in, [&](int i) { return ring.get(2, i).both(); });
+        store<false>(s.begin + mine, rows, in, [&](int i) { return ring.get(2, i).both(); });
       }
       ring.done();
     }
@@ -193,7 +195,7 @@ struct ScanBackward {
         for (int i = 0; i < BRIEF_LOADS; ++i)
           if (r + i < s.len) back.row(r + i, rx[i], rf[i], rd[r + i], h, off);
       }
-    back.store(s.begin, s.len, k, [&](int i) { return rd[i].both(); });
+    back.template store<false>(s.begin, s.len, k, [&](int i) { return rd[i].both(); });
     at.keep(a.dh0, seq, a.channels, k);
   }
 };
