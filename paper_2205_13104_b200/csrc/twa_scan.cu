@@ -9,11 +9,12 @@ template <typename T, int FEED, int CH>
 struct ScanForward {
   typedef Place<FEED, CH> At;
   static constexpr int CHANNELS = CH;
-  static constexpr int STAGES = 3;                 // of which two blocks an SM have room
+  static constexpr bool PIECES = FEED != BY_UNITS;
+  static constexpr int STAGES = PIECES ? 2 : 3;    // of which two blocks an SM have room
   static constexpr bool TOGETHER = FEED != BY_ELEMENTS;
   static constexpr int N = SEG<T>;
   static constexpr int SEGS = SCAN_CHANNELS / CH, WARP_ROWS = SEGS * N, TILE = SCAN_WARPS * WARP_ROWS;       // rows
-  typedef Ring<T, FEED, CH, 2, STAGES> Rows;
+  typedef Ring<T, FEED, CH, 2, STAGES, PIECES> Rows;
   const ScanArgs& a;
   const At at;
   twa_f2 A[N], L[N];                               // of the rows up to each

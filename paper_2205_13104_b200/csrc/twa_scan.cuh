@@ -241,12 +241,15 @@ __device__ __forceinline__ void keep_state(const Place<FEED, CH>& at, float* p, 
 // come as they lie, one more than a row has, and elements are found one place further; which rows those are changes with the
 // row's number where the stride is odd, and is the same for a segment's every tile.  A word that reaches out of the matrix,
 // before its first element or behind its last, is filled by the element.
-template <typename T, int FEED, int CH, int ARRAYS, int STAGES>
+// PIECES, a way for rows that are not in units: the 16-byte pieces in which a row lies, one more than a row has, as they lie; elements
+// are found from where the row begins in its first piece.  A quarter of the copies for 16 bytes of shared memory a row.
+template <typename T, int FEED, int CH, int ARRAYS, int STAGES, bool PIECES = false>
 struct Ring {
   static constexpr int N = SEG<T>, SEGS = SCAN_CHANNELS / CH;
   static_assert(SEGS == 1 || FEED == BY_UNITS, "narrow slices by units only");
-  static constexpr bool WORDS = FEED == BY_ELEMENTS && sizeof(T) == 2;
-  static constexpr int ROW = CH * sizeof(T) + (WORDS ? 4 : 0), NEXT_SEG = (N + (SEGS > 1 ? 1 : 0)) * ROW;       // bytes
+  static_assert(!PIECES || FEED != BY_UNITS, "pieces of rows that are not in units");
+  static constexpr bool WORDS = FEED == BY_ELEMENTS && sizeof(T) == 2 && !PIECES;
+  static constexpr int ROW = CH * sizeof(T) + (PIECES ? 16 : WORDS ? 4 : 0), NEXT_SEG = (N + (SEGS > 1 ? 1 : 0)) * ROW;       // bytes
   static constexpr int AREA = SEGS * NEXT_SEG, BYTES = ARRAYS * AREA;                                            // of a matrix, a stage
   static constexpr size_t BLOCK_BYTES = static_cast<size_t>(SCAN_WARPS) * STAGES * BYTES;
   static constexpr int AHEAD = STAGES - 1;        // segments under way before the first is waited for
@@ -255,6 +258,7 @@ struct Ring {
   char* base;
   int fill, read;                                 // bytes from the base: the stage to be filled, to be read
   int mine[WORDS ? ARRAYS : 1][WORDS ? 2 : 1];    // this lane's elements of a row, by the row's parity
+  int begin[PIECES ? ARRAYS : 1], step[PIECES ? ARRAYS : 1];      // bytes: where a segment's first row begins in a piece, from row to row
 
   __device__ __forceinline__ Ring(char* shared, int warp, int lane) : base(shared + static_cast<size_t>(warp) * STAGES * BYTES), fill(0), read(0) {
     if constexpr (!WORDS) mine[0][0] = lane / (CH / 2) * NEXT_SEG + lane % (CH / 2) * static_cast<int>(sizeof(T)) * (FEED == BY_ELEMENTS ? 1 : 2);
@@ -266,14 +270,22 @@ struct Ring {
       mine[array][0] = lane * 2 + static_cast<int>(reinterpret_cast<uintptr_t>(p) & 2);
       mine[array][1] = lane * 2 + static_cast<int>(reinterpret_cast<uintptr_t>(p + ld) & 2);
     }
+    if constexpr (PIECES) {
+      begin[array] = uniform(static_cast<int>(reinterpret_cast<uintptr_t>(p) & 15));
+      step[array] = static_cast<int>(ld * static_cast<long long>(sizeof(T)) & 15);
+    }
   }
-  __device__ __forceinline__ int at(int array, int row) const { return WORDS ? mine[array][row & 1] : mine[0][0]; }
+  __device__ __forceinline__ int at(int array, int row) const {
+    if constexpr (PIECES) return mine[0][0] + ((begin[array] + row % V * step[array]) & 15);
+    return WORDS ? mine[array][row & 1] : mine[0][0];
+  }
 
   // This lane's first element of a segment that begins at p.
   template <typename P>
   static __device__ __forceinline__ P* own(P* p, long long ld) {
     const int lane = threadIdx.x & 31;
     if constexpr (FEED == BY_UNITS) return p + lane / UNITS * ld + lane % UNITS * V;
+    else if constexpr (PIECES) return p;
     else return p + (FEED == BY_PAIRS || WORDS ? 2 * lane : lane);
   }
   template <int SIZE>
@@ -291,6 +303,28 @@ struct Ring {
       for (int i = 0; i < SEGS * N; i += EACH) {
         if (i < upto) copy_async<16>(area + lane * 16 + i / N * NEXT_SEG + i % N * ROW, from);
         from += EACH * ld;
+      }
+    } else if constexpr (PIECES) {
+      constexpr int OF_ROW = ROW / 16, ROWS = 32 / OF_ROW;                                // pieces of a row, rows a warp copies at once
+      const int piece = lane % OF_ROW * 16, upto = lane < ROWS * OF_ROW ? rows - lane / OF_ROW : 0;
+      const int bytes = min(channels, CH) * static_cast<int>(sizeof(T));
+      const uintptr_t lo = reinterpret_cast<uintptr_t>(first), hi = reinterpret_cast<uintptr_t>(last + 1);
+      uintptr_t row = reinterpret_cast<uintptr_t>(from);
+      const bool edge = row < lo + 16 || row + (rows - 1) * ld * sizeof(T) + CH * sizeof(T) + 16 > hi;       // of the matrix; true of the whole warp
+      row += lane / OF_ROW * ld * sizeof(T);
+#pragma unroll
+      for (int i = 0; i < N; i += ROWS) {
+        const uintptr_t p = (row & ~static_cast<uintptr_t>(15)) + piece;
+        if (i < upto && piece < bytes + static_cast<int>(row & 15)) {
+          if (!edge || (p >= lo && p + 16 <= hi)) {
+            copy_async<16>(area + i * ROW + lane * 16, reinterpret_cast<const void*>(p));
+          } else {                                 // reaches out of the matrix: what lies in it, by the element
+            for (int e = 0; e < 16; e += sizeof(T))
+              if (p + e >= lo && p + e < hi)
+                *reinterpret_cast<T*>(base + fill + array * AREA + i * ROW + lane * 16 + e) = *reinterpret_cast<const T*>(p + e);
+          }
+        }
+        row += ROWS * ld * sizeof(T);
       }
     } else if constexpr (FEED == BY_PAIRS) {
       const int upto = 2 * lane < channels ? rows : 0;
@@ -354,12 +388,16 @@ struct Ring {
   // Waits for the oldest segment.
   __device__ __forceinline__ void wait() {
     asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
-    if (FEED == BY_UNITS || WORDS) __syncwarp();
+    if (FEED == BY_UNITS || WORDS || PIECES) __syncwarp();
+    if constexpr (PIECES) {                        // rows' places are found anew for every segment: they would fill the registers
+#pragma unroll
+      for (int i = 0; i < ARRAYS; ++i) asm volatile("" : "+r"(begin[i]));
+    }
   }
   __device__ __forceinline__ Pair<T> get(int array, int row) const {
     const char* p = base + read + array * AREA + row * ROW + at(array, row);
     Pair<T> v;
-    if constexpr (WORDS) v.r = *reinterpret_cast<const unsigned short*>(p) | static_cast<uint32_t>(*reinterpret_cast<const unsigned short*>(p + 64)) << 16;
+    if constexpr (FEED == BY_ELEMENTS && sizeof(T) == 2) v.r = *reinterpret_cast<const unsigned short*>(p) | static_cast<uint32_t>(*reinterpret_cast<const unsigned short*>(p + 64)) << 16;
     else if constexpr (FEED == BY_ELEMENTS) v.r = make_float2(*reinterpret_cast<const float*>(p), *reinterpret_cast<const float*>(p + 128));
     else v = *reinterpret_cast<const Pair<T>*>(p);
     return v;
@@ -380,7 +418,7 @@ struct Ring {
   }
   __device__ __forceinline__ void done() {
     read = read == (STAGES - 1) * BYTES ? 0 : read + BYTES;
-    if (FEED == BY_UNITS || WORDS) __syncwarp();  // other lanes fill this stage again
+    if (FEED == BY_UNITS || WORDS || PIECES) __syncwarp();       // other lanes fill this stage again
   }
 };
 
