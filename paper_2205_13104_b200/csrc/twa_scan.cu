@@ -9,12 +9,11 @@ template <typename T, int FEED, int CH>
 struct ScanForward {
   typedef Place<FEED, CH> At;
   static constexpr int CHANNELS = CH;
-  static constexpr bool PIECES = FEED != BY_UNITS;
-  static constexpr int STAGES = PIECES ? 2 : 3;    // of which two blocks an SM have room
+  static constexpr int STAGES = FEED == BY_UNITS ? 3 : 2, SETS = 2;           // for which two blocks an SM have room
   static constexpr bool TOGETHER = FEED != BY_ELEMENTS;
   static constexpr int N = SEG<T>;
   static constexpr int SEGS = SCAN_CHANNELS / CH, WARP_ROWS = SEGS * N, TILE = SCAN_WARPS * WARP_ROWS;       // rows
-  typedef Ring<T, FEED, CH, 2, STAGES, PIECES> Rows;
+  typedef Ring<T, FEED, CH, 2, STAGES> Rows;
   const ScanArgs& a;
   const At at;
   twa_f2 A[N], L[N];                               // of the rows up to each
@@ -52,7 +51,7 @@ struct ScanForward {
     ring.copy(array, from, ld, rows, at.left, first, first + (a.tokens - 1) * ld + a.channels - 1);
   }
   // A sequence by the whole cluster.
-  __device__ __forceinline__ void whole(Span s, int seq, char* shared, Joins<CH / 2>& joins, Tiles<CH / 2>& tiles, int& turn) {
+  __device__ __forceinline__ void whole(Span s, int seq, char* shared, Joins<CH / 2, SETS>& joins, Tiles<CH / 2>& tiles, int& turn) {
     Rows ring(shared, at.warp, at.lane);
     const int stride = TILE * at.ranks;
     unsigned phases = 0;

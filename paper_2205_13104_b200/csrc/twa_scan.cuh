@@ -237,19 +237,15 @@ __device__ __forceinline__ void keep_state(const Place<FEED, CH>& at, float* p, 
 // A ring of a warp's segments in shared memory, STAGES deep, of ARRAYS matrices, filled by asynchronous copies.  A segment begins a
 // row's length behind the one before it, so that lanes of different segments read different banks.  By units, results go
 // out the same way: pairs into the stage that has been read, and from there 16 bytes a lane.
-// By elements, bfloat16 rows may begin between the 4-byte words that are the least an asynchronous copy takes.  Then a row's words
-// come as they lie, one more than a row has, and elements are found one place further; which rows those are changes with the
-// row's number where the stride is odd, and is the same for a segment's every tile.  A word that reaches out of the matrix,
-// before its first element or behind its last, is filled by the element.
-// PIECES, a way for rows that are not in units: the 16-byte pieces in which a row lies, one more than a row has, as they lie; elements
-// are found from where the row begins in its first piece.  A quarter of the copies for 16 bytes of shared memory a row.
-template <typename T, int FEED, int CH, int ARRAYS, int STAGES, bool PIECES = false>
+// Rows that are not in units come in the 16-byte pieces in which they lie, one more than a row has, and elements are found from where
+// the row begins in its first piece; a piece that reaches out of the matrix is filled by the element.  (Copies of the 4-byte words,
+// or of the pairs, were four times as many: 37 ragged sequences of 20011 x 771 bfloat16 67 and 101 us, so 53 and 82.)
+template <typename T, int FEED, int CH, int ARRAYS, int STAGES>
 struct Ring {
   static constexpr int N = SEG<T>, SEGS = SCAN_CHANNELS / CH;
   static_assert(SEGS == 1 || FEED == BY_UNITS, "narrow slices by units only");
-  static_assert(!PIECES || FEED != BY_UNITS, "pieces of rows that are not in units");
-  static constexpr bool WORDS = FEED == BY_ELEMENTS && sizeof(T) == 2 && !PIECES;
-  static constexpr int ROW = CH * sizeof(T) + (PIECES ? 16 : WORDS ? 4 : 0), NEXT_SEG = (N + (SEGS > 1 ? 1 : 0)) * ROW;       // bytes
+  static constexpr bool PIECES = FEED != BY_UNITS;
+  static constexpr int ROW = CH * sizeof(T) + (PIECES ? 16 : 0), NEXT_SEG = (N + (SEGS > 1 ? 1 : 0)) * ROW;       // bytes
   static constexpr int AREA = SEGS * NEXT_SEG, BYTES = ARRAYS * AREA;                                            // of a matrix, a stage
   static constexpr size_t BLOCK_BYTES = static_cast<size_t>(SCAN_WARPS) * STAGES * BYTES;
   static constexpr int AHEAD = STAGES - 1;        // segments under way before the first is waited for
@@ -257,41 +253,33 @@ struct Ring {
   static_assert(FEED != BY_UNITS || N % EACH == 0, "a copy stays in its segment");
   char* base;
   int fill, read;                                 // bytes from the base: the stage to be filled, to be read
-  int mine[WORDS ? ARRAYS : 1][WORDS ? 2 : 1];    // this lane's elements of a row, by the row's parity
+  int mine;                                       // this lane's elements of a row
   int begin[PIECES ? ARRAYS : 1], step[PIECES ? ARRAYS : 1];      // bytes: where a segment's first row begins in a piece, from row to row
 
   __device__ __forceinline__ Ring(char* shared, int warp, int lane) : base(shared + static_cast<size_t>(warp) * STAGES * BYTES), fill(0), read(0) {
-    if constexpr (!WORDS) mine[0][0] = lane / (CH / 2) * NEXT_SEG + lane % (CH / 2) * static_cast<int>(sizeof(T)) * (FEED == BY_ELEMENTS ? 1 : 2);
+    mine = lane / (CH / 2) * NEXT_SEG + lane % (CH / 2) * static_cast<int>(sizeof(T)) * (FEED == BY_ELEMENTS ? 1 : 2);
   }
-  // Says where a matrix's segments lie: p is the first element of one of them.
+  // Says where a matrix's segments lie: p is the first element of one of them; it is the same for every tile's.
   __device__ __forceinline__ void lies(int array, const T* p, long long ld) {
-    if constexpr (WORDS) {
-      const int lane = threadIdx.x & 31;
-      mine[array][0] = lane * 2 + static_cast<int>(reinterpret_cast<uintptr_t>(p) & 2);
-      mine[array][1] = lane * 2 + static_cast<int>(reinterpret_cast<uintptr_t>(p + ld) & 2);
-    }
     if constexpr (PIECES) {
       begin[array] = uniform(static_cast<int>(reinterpret_cast<uintptr_t>(p) & 15));
       step[array] = static_cast<int>(ld * static_cast<long long>(sizeof(T)) & 15);
     }
   }
   __device__ __forceinline__ int at(int array, int row) const {
-    if constexpr (PIECES) return mine[0][0] + ((begin[array] + row % V * step[array]) & 15);
-    return WORDS ? mine[array][row & 1] : mine[0][0];
+    if constexpr (PIECES) return mine + ((begin[array] + row % V * step[array]) & 15);
+    return mine;
   }
 
-  // This lane's first element of a segment that begins at p.
+  // This lane's first element of a segment that begins at p; in pieces, the segment's.
   template <typename P>
   static __device__ __forceinline__ P* own(P* p, long long ld) {
     const int lane = threadIdx.x & 31;
     if constexpr (FEED == BY_UNITS) return p + lane / UNITS * ld + lane % UNITS * V;
-    else if constexpr (PIECES) return p;
-    else return p + (FEED == BY_PAIRS || WORDS ? 2 * lane : lane);
+    else return p;
   }
-  template <int SIZE>
   static __device__ __forceinline__ void copy_async(uint32_t to, const void* from) {
-    if constexpr (SIZE == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(to), "l"(from), "n"(SIZE) : "memory");
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
   }
   // Rows from own(); `channels` remain from the slice's first.  first, last: the matrix's.
   __device__ __forceinline__ void copy(int array, const T* from, long long ld, int rows, int channels, const T* first, const T* last) {
@@ -301,10 +289,10 @@ struct Ring {
       const int upto = lane % UNITS * V < channels ? rows - lane / UNITS : 0;
 #pragma unroll
       for (int i = 0; i < SEGS * N; i += EACH) {
-        if (i < upto) copy_async<16>(area + lane * 16 + i / N * NEXT_SEG + i % N * ROW, from);
+        if (i < upto) copy_async(area + lane * 16 + i / N * NEXT_SEG + i % N * ROW, from);
         from += EACH * ld;
       }
-    } else if constexpr (PIECES) {
+    } else {
       constexpr int OF_ROW = ROW / 16, ROWS = 32 / OF_ROW;                                // pieces of a row, rows a warp copies at once
       const int piece = lane % OF_ROW * 16, upto = lane < ROWS * OF_ROW ? rows - lane / OF_ROW : 0;
       const int bytes = min(channels, CH) * static_cast<int>(sizeof(T));
@@ -317,7 +305,7 @@ struct Ring {
         const uintptr_t p = (row & ~static_cast<uintptr_t>(15)) + piece;
         if (i < upto && piece < bytes + static_cast<int>(row & 15)) {
           if (!edge || (p >= lo && p + 16 <= hi)) {
-            copy_async<16>(area + i * ROW + lane * 16, reinterpret_cast<const void*>(p));
+            copy_async(area + i * ROW + lane * 16, reinterpret_cast<const void*>(p));
           } else {                                 // reaches out of the matrix: what lies in it, by the element
             for (int e = 0; e < 16; e += sizeof(T))
               if (p + e >= lo && p + e < hi)
@@ -325,58 +313,6 @@ struct Ring {
           }
         }
         row += ROWS * ld * sizeof(T);
-      }
-    } else if constexpr (FEED == BY_PAIRS) {
-      const int upto = 2 * lane < channels ? rows : 0;
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        if (i < upto) copy_async<2 * sizeof(T)>(area + lane * 2 * sizeof(T) + i * ROW, from);
-        from += ld;
-      }
-    } else if constexpr (!WORDS) {
-      const int upto = lane < channels ? rows : 0, upto32 = lane + 32 < channels ? rows : 0;
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        if (i < upto) copy_async<4>(area + lane * 4 + i * ROW, from);
-        if (i < upto32) copy_async<4>(area + lane * 4 + 128 + i * ROW, from + 32);
-        from += ld;
-      }
-    } else {
-      const T* row = from - 2 * lane;
-      const bool edge = row <= first || row + (rows - 1) * ld + channels > last;         // of the matrix; true of the whole warp
-      // of the even and the odd rows: one begins inside a word, its word of this lane, and whether it has one
-      const int odd[2] = {(mine[array][0] >> 1) - lane, (mine[array][1] >> 1) - lane};
-      const T* word[2] = {from - odd[0], from + ld - odd[1]};
-      const bool has[2] = {2 * lane < channels + odd[0], 2 * lane < channels + odd[1]};
-      if (rows == N && !edge) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-          if (has[i & 1]) copy_async<4>(area + i * ROW + lane * 4, word[i & 1]);
-          word[i & 1] += 2 * ld;
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-          if (i < rows && has[i & 1] && (!edge || (word[i & 1] >= first && word[i & 1] < last)))
-            copy_async<4>(area + i * ROW + lane * 4, word[i & 1]);
-          word[i & 1] += 2 * ld;
-        }
-      }
-      // the last element of a row that begins inside a word, alone in one more
-      if (lane < rows && channels >= SCAN_CHANNELS && (lane & 1 ? mine[array][1] : mine[array][0]) != lane * 2) {
-        const T* p = row + lane * ld + SCAN_CHANNELS - 1;
-        if (!edge || p < last) copy_async<4>(area + lane * ROW + SCAN_CHANNELS * 2, p);
-      }
-      // the matrix's first and last element where they lie in a word with something else
-      if (edge && lane < 2) {
-        const T* p = lane ? last : first;
-        const long long off = p - row;
-        const int i = off < 0 ? -1 : static_cast<int>(off / ld), e = static_cast<int>(off - i * ld);
-        const bool apart = lane ? (reinterpret_cast<uintptr_t>(p) & 2) == 0 : (reinterpret_cast<uintptr_t>(p) & 2) != 0;
-        if (apart && i >= 0 && i < rows && e < channels && e < SCAN_CHANNELS) {
-          const int odd = (i & 1 ? mine[array][1] : mine[array][0]) / 2 - lane;
-          *reinterpret_cast<T*>(base + fill + array * AREA + i * ROW + (e + odd) * 2) = *p;
-        }
       }
     }
   }
@@ -388,7 +324,7 @@ struct Ring {
   // Waits for the oldest segment.
   __device__ __forceinline__ void wait() {
     asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
-    if (FEED == BY_UNITS || WORDS || PIECES) __syncwarp();
+    __syncwarp();
     if constexpr (PIECES) {                        // rows' places are found anew for every segment: they would fill the registers
 #pragma unroll
       for (int i = 0; i < ARRAYS; ++i) asm volatile("" : "+r"(begin[i]));
@@ -404,7 +340,7 @@ struct Ring {
   }
   // By units: a result in the place of what get() gave, and the whole segment of them to memory, from own().
   __device__ __forceinline__ void put(int array, int row, float lo, float hi) const {
-    Pair<T>::template store<true>(reinterpret_cast<T*>(base + read + array * AREA + row * ROW + mine[0][0]), lo, hi, 2);
+    Pair<T>::template store<true>(reinterpret_cast<T*>(base + read + array * AREA + row * ROW + mine), lo, hi, 2);
   }
   __device__ __forceinline__ void flush(int array, T* to, long long ld, int channels) const {
     const int lane = threadIdx.x & 31;
@@ -418,7 +354,7 @@ struct Ring {
   }
   __device__ __forceinline__ void done() {
     read = read == (STAGES - 1) * BYTES ? 0 : read + BYTES;
-    if (FEED == BY_UNITS || WORDS || PIECES) __syncwarp();       // other lanes fill this stage again
+    __syncwarp();                                 // other lanes fill this stage again
   }
 };
 
@@ -455,9 +391,9 @@ __device__ __forceinline__ Map join_segments(Map m, int seg, Map& before) {
 
 // What the segments of a tile make of what enters them (the state, or backward k), and what enters the next tile: twice, so that the
 // next ones go beside those being read.
-template <int PAIRS>
+template <int PAIRS, int SETS>
 struct Joins {
-  Map seg[2][SCAN_WARPS][PAIRS];
+  Map seg[SETS][SCAN_WARPS][PAIRS];                // one set: a barrier more
   twa_f2 carry[2][PAIRS];
 };
 // The same of the tiles of a cluster's blocks, and how they arrive.
@@ -473,14 +409,14 @@ struct Tiles {
 // (A barrier of the whole cluster instead would also wait until every thread's results are in memory: 1 x 65536 x 512 float32
 // both directions 277 us, so 237.)  Two sets take turns: a block sends into one again only after it has the maps of the
 // round between, which the receiver sends when all its warps have read the first.  False: the maps did not come in time, now or (lost) before.
-template <bool FORWARD, int FEED, int CH>
-__device__ __forceinline__ bool share_tile(const ScanArgs& a, const Joins<CH / 2>& joins, Tiles<CH / 2>& tiles, const Place<FEED, CH>& at, int turn,
+template <bool FORWARD, int FEED, int CH, int SETS>
+__device__ __forceinline__ bool share_tile(const ScanArgs& a, const Joins<CH / 2, SETS>& joins, Tiles<CH / 2>& tiles, const Place<FEED, CH>& at, int turn,
                                            unsigned& phases, bool lost) {
   if (threadIdx.x == 0 && !lost) twa_mbar_expect_tx(twa_smem_u32(&tiles.arrived[turn]), at.ranks * (CH / 2) * sizeof(Map));
   if (at.warp < at.ranks) {
-    Map all = joins.seg[turn][FORWARD ? 0 : SCAN_WARPS - 1][at.pair];
+    Map all = joins.seg[turn % SETS][FORWARD ? 0 : SCAN_WARPS - 1][at.pair];
 #pragma unroll
-    for (int i = 1; i < SCAN_WARPS; ++i) all = joins.seg[turn][FORWARD ? i : SCAN_WARPS - 1 - i][at.pair].after(all);
+    for (int i = 1; i < SCAN_WARPS; ++i) all = joins.seg[turn % SETS][FORWARD ? i : SCAN_WARPS - 1 - i][at.pair].after(all);
     if (at.seg == 0) {
       uint32_t to, bar;
       asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(twa_smem_u32(&tiles.tile[turn][at.rank][at.pair])), "r"(at.warp));
@@ -519,7 +455,7 @@ template <typename Direction, int GROUP, bool RAGGED>
 __device__ __forceinline__ void scan_block(const ScanArgs& a) {
   typedef Tiles<Direction::CHANNELS / 2> T;
   extern __shared__ __align__(16) char shared[];
-  __shared__ Joins<Direction::CHANNELS / 2> joins;
+  __shared__ Joins<Direction::CHANNELS / 2, Direction::SETS> joins;
   T& tiles = *reinterpret_cast<T*>(shared + Direction::Rows::BLOCK_BYTES);       // of clusters only
   const unsigned task = blockIdx.x / a.cluster;
   const int slice = task % a.slices, first = task / a.slices * GROUP;

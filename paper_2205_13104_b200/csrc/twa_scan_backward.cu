@@ -13,7 +13,7 @@ template <typename T, int FEED, int CH>
 struct ScanBackward {
   typedef Place<FEED, CH> At;
   static constexpr int CHANNELS = CH;
-  static constexpr int STAGES = 2;                 // as above
+  static constexpr int STAGES = 2, SETS = FEED == BY_UNITS ? 2 : 1;           // for which two blocks an SM have room
   static constexpr bool TOGETHER = FEED != BY_ELEMENTS;
   static constexpr int N = SEG<T>;
   static constexpr int SEGS = SCAN_CHANNELS / CH, WARP_ROWS = SEGS * N, TILE = SCAN_WARPS * WARP_ROWS;
@@ -70,7 +70,7 @@ struct ScanBackward {
     const T* first = static_cast<const T*>(all);
     ring.copy(array, from, ld, rows, at.left, first, first + (a.tokens - 1) * ld + a.channels - 1);
   }
-  __device__ __forceinline__ void whole(Span s, int seq, char* shared, Joins<CH / 2>& joins, Tiles<CH / 2>& tiles, int& turn) {
+  __device__ __forceinline__ void whole(Span s, int seq, char* shared, Joins<CH / 2, SETS>& joins, Tiles<CH / 2>& tiles, int& turn) {
     Rows ring(shared, at.warp, at.lane);
     const int stride = TILE * at.ranks, rounds = (s.len + stride - 1) / stride;
     unsigned phases = 0;
@@ -122,7 +122,7 @@ struct ScanBackward {
       }
       Map behind;
       const Map upto = join_segments<false, SEGS>(off, at.seg, behind);
-      if (at.seg == 0) joins.seg[turn][at.warp][at.pair] = upto;
+      if (at.seg == 0) joins.seg[turn % SETS][at.warp][at.pair] = upto;
       slot -= at.ranks * SCAN_WARPS * SEGS;
       next = round ? kept_state(at, a.states, slot, a.channels) : 0;
       __syncthreads();
@@ -146,7 +146,8 @@ struct ScanBackward {
       }
 #pragma unroll
       for (int w = SCAN_WARPS - 1; w > 0; --w)
-        if (w > at.warp) in = joins.seg[turn][w][at.pair].of(in);
+        if (w > at.warp) in = joins.seg[turn % SETS][w][at.pair].of(in);
+      if (SETS == 1) __syncthreads();
       if (SEGS > 1) in = behind.of(in);
       if (at.ranks == 1 && first_seg) joins.carry[turn][at.pair] = k = off.of(in);
       turn ^= 1;
