@@ -80,9 +80,9 @@ __device__ __forceinline__ int scan_slot(const Span& s, int seq) { return static
 // Rows that a sequence has from row r on, of `most`.
 __device__ __forceinline__ int scan_rows(const Span& s, int r, int most) { return min(max(s.len - r, 0), most); }
 
-// How rows are fetched, and which two channels a lane has.  In units of 16 bytes, any lane's, or in pairs: neighbouring channels,
-// loaded and stored together.  Element by element, where rows lie on no such boundary: channels 32 apart, so that a warp's accesses
-// are contiguous.
+// How rows lie, and which two channels a lane has.  In units of 16 bytes: neighbours; rows are copied and stored by the unit, any
+// lane's.  In pairs: neighbours, stored together.  Element by element, where rows lie on no such boundary: channels 32 apart, so
+// that a warp's accesses are contiguous.
 enum { BY_UNITS, BY_PAIRS, BY_ELEMENTS };
 
 // Stores an element where `exists`: a predicate, no branch.
@@ -390,10 +390,10 @@ __device__ __forceinline__ Map join_segments(Map m, int seg, Map& before) {
 }
 
 // What the segments of a tile make of what enters them (the state, or backward k), and what enters the next tile: twice, so that the
-// next ones go beside those being read.
+// next ones go beside those being read, or, where the ring leaves no room, the segments' once and a barrier behind the reading.
 template <int PAIRS, int SETS>
 struct Joins {
-  Map seg[SETS][SCAN_WARPS][PAIRS];                // one set: a barrier more
+  Map seg[SETS][SCAN_WARPS][PAIRS];
   twa_f2 carry[2][PAIRS];
 };
 // The same of the tiles of a cluster's blocks, and how they arrive.

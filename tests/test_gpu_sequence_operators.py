@@ -877,3 +877,38 @@ def test_refusals(ctx):
         assert grad(**kw) == want, kw
     torch.cuda.synchronize()
     ok(ctx)
+
+
+@pytest.mark.parametrize("channels,pads,step", [(71, (0, 3, 2), 1), (5, (2, 0, 7), 1), (129, (1, 1, 0), 1), (70, (2, 4, 0), 2), (130, (0, 6, 2), 2)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_gated_scan_takes_rows_from_any_place(ctx, channels, pads, step, dtype):
+    # every place of a row in the 16 bytes around it, another one for each matrix, between values that must not reach a result:
+    # the same numbers at the head of an allocation give the same bits
+    lengths = [129, 5, 0, 128, 17, 40]
+    n, q = sum(lengths), len(lengths)
+    starts = torch.tensor([sum(lengths[:i]) for i in range(q + 1)], device=DEV, dtype=torch.int32)
+    g = gen(channels)
+    src = [randn(g, n, channels).to(dtype), (2.0 * randn(g, n, channels) + 2.0).to(dtype), randn(g, n, channels).to(dtype)]
+    size = twa.twa_gated_scan_states_bytes(n, q, channels)
+
+    def run(x, f, dh):
+        states = torch.empty(size, dtype=torch.uint8, device=DEV)
+        h, dx, df = (torch.empty((n, channels), dtype=dtype, device=DEV) for _ in range(3))
+        twa.twa_gated_scan(ctx, x, f, h, starts, q, states=states)
+        twa.twa_gated_scan_backward(ctx, dh, x, f, states, dx, df, starts, q)
+        return h, dx, df
+
+    def lain(v, pad, shift):
+        ld = channels + pad
+        buf = torch.full((shift + (n - 1) * ld + channels + 9,), float("nan"), dtype=dtype, device=DEV)
+        view = buf[shift:].as_strided((n, channels), (ld, 1), buf.storage_offset() + shift)
+        view.copy_(v)
+        return view
+
+    # rows `step` elements longer than the matrix is wide: not in units of 16 bytes there either
+    want = run(*(lain(v, step, 0) for v in src))
+    for shift in range(0, 9, step):
+        got = run(*(lain(v, pad, (shift * k) % 9 // step * step) for k, (v, pad) in enumerate(zip(src, pads), 1)))
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
+    ok(ctx)
