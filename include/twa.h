@@ -152,11 +152,13 @@ const char* twa_last_error(const twa_ctx* ctx);
  *      TWA_MAX_LAUNCH_ROWS, slabs of 2^30 rows above.
  *  TWA_TUNE_SCAN_CLUSTER, TWA_TUNE_SCAN_CHANNELS: twa_gated_scan and its backward call, where sequences are not mostly
  *      short: blocks that share a sequence (1, 2, 4 or 8) and channels of a block (16, 32 or 64; rows on 16-byte
- *      boundaries only).  0 = as many as fill the device. */
+ *      boundaries only).  0 = as many as fill the device.
+ *  TWA_TUNE_SCAN_GIVE_UP: exercises what these calls do when a wait runs out: 1 + 8 r + w lets warp w of the r-th
+ *      of the blocks that share a sequence take its first wait for one that did (r, w: 0 .. 7).  0 = none. */
 enum { TWA_TUNE_PROJECT_WARPS = 1, TWA_TUNE_LIFT_WARPS = 2, TWA_TUNE_STAGES = 3,
        TWA_TUNE_WAIT_LIMIT_MS = 4, TWA_TUNE_DEQUANT_PATH = 5, TWA_TUNE_TILE_SEGMENTS = 6,
        TWA_TUNE_BUILD_PANEL = 7, TWA_TUNE_LIFT_VECTORS = 8, TWA_TUNE_SLAB_ROWS = 9,
-       TWA_TUNE_SCAN_CLUSTER = 10, TWA_TUNE_SCAN_CHANNELS = 11 };
+       TWA_TUNE_SCAN_CLUSTER = 10, TWA_TUNE_SCAN_CHANNELS = 11, TWA_TUNE_SCAN_GIVE_UP = 12 };
 int twa_set_tuning(twa_ctx* ctx, int key, int value);
 
 /* Exercises the bounded wait every streaming kernel uses, without any fault: enqueues one block
@@ -635,7 +637,7 @@ int twa_dropout_backward(twa_ctx* ctx, const void* dy, int64_t lddy, twa_dtype d
  * States are float32 throughout.  A value that is not finite spoils its own channel from its token to the sequence's end.
  * Device-side errors: TWA_ERR_INVALID_ARG, detail = a sequence whose starts go down or leave 0 .. tokens; it is left alone,
  * and rows that starts give to two sequences are undefined.  TWA_ERR_TIMEOUT, detail = a sequence that several blocks share, one of
- * which did not hear from another in time; some of its outputs are then not written. */
+ * which did not hear from another in time: outputs of it are then missing, those that are written are right, and states is not to be used. */
 int twa_gated_scan(twa_ctx* ctx, const void* x, int64_t ldx, const void* f, int64_t ldf, twa_dtype dtype, int64_t tokens,
                    int channels, const void* starts, twa_itype s_type, int sequences, const float* h0, void* h, int64_t ldh,
                    float* h_last, void* states, size_t states_bytes);

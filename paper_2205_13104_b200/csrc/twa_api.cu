@@ -249,6 +249,10 @@ int twa_set_tuning(twa_ctx* ctx, int key, int value) {
       if (value != 0 && value != 16 && value != 32 && value != 64) return TWA_ERR_INVALID_ARG;
       ctx->tune_scan_channels = value;
       return TWA_OK;
+    case TWA_TUNE_SCAN_GIVE_UP:
+      if (value > 64) return TWA_ERR_INVALID_ARG;
+      ctx->tune_scan_give_up = value;
+      return TWA_OK;
     case TWA_TUNE_WAIT_LIMIT_MS:
       ctx->wait_limit_ns = (value ? static_cast<unsigned long long>(value) : 2000ull) * 1000000ull;
       return TWA_OK;

@@ -33,6 +33,7 @@ struct twa_ctx {
   int tune_lift_base_path;    // tensor-pipe lift, base / output vectors: 0 = choose, 1 = lanes, 2 = base through the ring, 3 = both
   int tune_slab_rows;         // stepping calls: rows per launch (0 = one launch up to TWA_MAX_LAUNCH_ROWS, slabs of 2^30 above)
   int tune_scan_cluster, tune_scan_channels;      // gated scan: blocks along a sequence, channels of a block (0 = choose)
+  int tune_scan_give_up;      // gated scan: 1 + 8 x block + warp whose wait is taken for one that ran out (0 = none)
   int expert_cluster;         // expert dispatch: blocks of a sorting cluster at most (0 = not yet asked)
   cudaEvent_t* prof_events;   // 3 per recorded step, or null
   int prof_cap, prof_count;   // steps

@@ -51,10 +51,11 @@ struct ScanForward {
     ring.copy(array, from, ld, rows, at.left, first, first + (a.tokens - 1) * ld + a.channels - 1);
   }
   // A sequence by the whole cluster.
-  __device__ __forceinline__ void whole(Span s, int seq, char* shared, Joins<CH / 2, SETS>& joins, Tiles<CH / 2>& tiles, int& turn) {
+  __device__ __forceinline__ void whole(const Span& s, int seq, char* shared, Joins<CH / 2, SETS>& joins, Tiles<CH / 2>& tiles, int& turn) {
     Rows ring(shared, at.warp, at.lane);
     const int stride = TILE * at.ranks;
     unsigned phases = 0;
+    bool lost = false;                             // the maps of a round did not come to this warp, or block
     const bool last_seg = at.warp == SCAN_WARPS - 1 && at.seg == SEGS - 1;
     int ahead = at.rank * TILE + at.warp * WARP_ROWS;                     // row of the warp's next segments to be fetched
     ring.lies(0, static_cast<const T*>(a.x) + (s.begin + ahead) * a.ldx + at.slice, a.ldx);
@@ -78,8 +79,7 @@ struct ScanForward {
     twa_f2 state = at.state(a.h0, seq, a.channels);
     if (last_seg) joins.carry[turn ^ 1][at.pair] = state;
     int slot = scan_slot<T>(s, seq) + (at.rank * SCAN_WARPS + at.warp) * SEGS + at.seg;
-    const int end_row = s.len;
-    for (int t = 0; t < end_row; t += stride, slot += at.ranks * SCAN_WARPS * SEGS, h += stride * a.ldh) {
+    for (int t = 0; t < s.len; t += stride, slot += at.ranks * SCAN_WARPS * SEGS, h += stride * a.ldh) {
       const int first = t + at.rank * TILE + at.warp * WARP_ROWS, mine = first + at.seg * N;
       bool full = first + WARP_ROWS <= s.len;                       // the whole warp's rows exist
       int rows = scan_rows(s, mine, N);
@@ -99,12 +99,15 @@ struct ScanForward {
       Map before;
       const Map upto = join_segments<true, SEGS>(end, at.seg, before);
       if (at.seg == SEGS - 1) joins.seg[turn][at.warp][at.pair] = upto;
-      __syncthreads();
+      if (scan_round(at.ranks > 1, lost)) {
+        lost = true;
+        Rows::drain();
+        break;
+      }
       twa_f2 in;
       if (at.ranks > 1) {
-        if (!share_tile<true>(a, joins, tiles, at, turn, phases, s.len < 0)) {
-          if (s.len >= 0 && threadIdx.x == 0) twa_set_status(a.status, TWA_ERR_TIMEOUT, seq);
-          s.len = -1;                              // nothing more is stored
+        if (!share_tile<true>(a, joins, tiles, at, turn, phases, seq)) {
+          lost = true;                             // nothing more is stored
           rows = 0;
           full = false;
         }
@@ -141,7 +144,7 @@ struct ScanForward {
       }
       ring.done();
     }
-    if (last_seg && at.rank == 0 && s.len >= 0) at.keep(a.h_last, seq, a.channels, state);
+    if (last_seg && at.rank == 0 && !lost) at.keep(a.h_last, seq, a.channels, state);
   }
 
   // A sequence of at most SEG rows, by one warp: the state before each row is at hand, and rows go by, BRIEF_LOADS under way together.
@@ -204,7 +207,7 @@ int twa_gated_scan(twa_ctx* ctx, const void* x, int64_t ldx, const void* f, int6
   ScanArgs a = {};
   a.x = x, a.ldx = ldx, a.f = f, a.ldf = ldf, a.h = h, a.ldh = ldh;
   a.tokens = tokens, a.channels = channels, a.starts = starts, a.s_type = s_type, a.sequences = sequences;
-  a.h0 = h0, a.h_last = h_last, a.states = static_cast<float*>(states), a.status = ctx->d_status, a.wait_limit_ns = ctx->wait_limit_ns;
+  a.h0 = h0, a.h_last = h_last, a.states = static_cast<float*>(states), a.status = ctx->d_status, a.wait_limit_ns = ctx->wait_limit_ns, a.give_up = ctx->tune_scan_give_up;
   const int feed = scan_feed(h, ldh, size, channels, scan_feed(f, ldf, size, channels, scan_feed(x, ldx, size, channels, BY_UNITS)));
   TWA_CUDA_OK(ctx, scan_launch<ScanForward>(ctx, a, dtype, feed));
   return TWA_OK;

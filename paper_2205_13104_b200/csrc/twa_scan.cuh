@@ -53,6 +53,7 @@ struct ScanArgs {
   float* dh0;
   int* status;
   unsigned long long wait_limit_ns;
+  int give_up;                                     // 1 + 8 x rank + warp: which takes its wait for one that ran out (0: none)
 };
 
 // Rows of a sequence; len -1: its offsets are wrong and it is left alone.
@@ -356,6 +357,8 @@ struct Ring {
     read = read == (STAGES - 1) * BYTES ? 0 : read + BYTES;
     __syncwarp();                                 // other lanes fill this stage again
   }
+  // Waits for every copy under way: none reaches shared memory after a block that goes no further.
+  static __device__ __forceinline__ void drain() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 };
 
 // Affine maps v -> A v + B of two channels.
@@ -408,11 +411,12 @@ struct Tiles {
 // first on (FORWARD) or from the last, and the warp of each rank sends the tile's to that block, whose barrier counts the bytes.
 // (A barrier of the whole cluster instead would also wait until every thread's results are in memory: 1 x 65536 x 512 float32
 // both directions 277 us, so 237.)  Two sets take turns: a block sends into one again only after it has the maps of the
-// round between, which the receiver sends when all its warps have read the first.  False: the maps did not come in time, now or (lost) before.
+// round between, which the receiver sends when all its warps have read the first.  False: the maps did not come to this warp in
+// time, which it reports: warps wait each for themselves, and another of the block may have had them just before the limit.
 template <bool FORWARD, int FEED, int CH, int SETS>
 __device__ __forceinline__ bool share_tile(const ScanArgs& a, const Joins<CH / 2, SETS>& joins, Tiles<CH / 2>& tiles, const Place<FEED, CH>& at, int turn,
-                                           unsigned& phases, bool lost) {
-  if (threadIdx.x == 0 && !lost) twa_mbar_expect_tx(twa_smem_u32(&tiles.arrived[turn]), at.ranks * (CH / 2) * sizeof(Map));
+                                           unsigned& phases, int seq) {
+  if (threadIdx.x == 0) twa_mbar_expect_tx(twa_smem_u32(&tiles.arrived[turn]), at.ranks * (CH / 2) * sizeof(Map));
   if (at.warp < at.ranks) {
     Map all = joins.seg[turn % SETS][FORWARD ? 0 : SCAN_WARPS - 1][at.pair];
 #pragma unroll
@@ -425,11 +429,22 @@ __device__ __forceinline__ bool share_tile(const ScanArgs& a, const Joins<CH / 2
                    : "memory");
     }
   }
-  const bool good = twa_wait(&tiles.arrived[turn], phases >> turn & 1, &tiles.abort_flag, a.wait_limit_ns);
+  const bool good = a.give_up != 1 + at.rank * SCAN_WARPS + at.warp &&
+                    twa_wait(&tiles.arrived[turn], phases >> turn & 1, &tiles.abort_flag, a.wait_limit_ns);
   phases ^= 1u << turn;
-  return __all_sync(0xffffffffu, good);            // a warp goes on as one
+  if (__all_sync(0xffffffffu, good)) return true;  // a warp goes on as one
+  if (at.lane == 0) twa_set_status(a.status, TWA_ERR_TIMEOUT, seq);
+  return false;
 }
 static_assert(MAX_CLUSTER <= SCAN_WARPS, "a warp for every rank");
+// A round's barrier.  Of a cluster's block it says whether a warp of the block's has lost the maps of the round before: then the block
+// goes no further, as one.  It tells the others nothing more, so that they do not take what it has left for its tiles' maps, nor
+// send into a set that another has not read: every map that a block receives is right, and so is every row that it stores.
+__device__ __forceinline__ bool scan_round(bool cluster, bool lost) {
+  if (cluster) return __syncthreads_or(lost);
+  __syncthreads();
+  return false;
+}
 
 // The sequence that has `place` longer ones before it, of at most SCAN_THREADS; by the whole block, which has `shared` for it.
 __device__ __forceinline__ int by_length(const ScanArgs& a, int place, int* shared) {

@@ -70,10 +70,11 @@ struct ScanBackward {
     const T* first = static_cast<const T*>(all);
     ring.copy(array, from, ld, rows, at.left, first, first + (a.tokens - 1) * ld + a.channels - 1);
   }
-  __device__ __forceinline__ void whole(Span s, int seq, char* shared, Joins<CH / 2, SETS>& joins, Tiles<CH / 2>& tiles, int& turn) {
+  __device__ __forceinline__ void whole(const Span& s, int seq, char* shared, Joins<CH / 2, SETS>& joins, Tiles<CH / 2>& tiles, int& turn) {
     Rows ring(shared, at.warp, at.lane);
     const int stride = TILE * at.ranks, rounds = (s.len + stride - 1) / stride;
     unsigned phases = 0;
+    bool lost = false;                             // the maps of a round did not come to this warp, or block
     const bool first_seg = at.warp == 0 && at.seg == 0;
     int ahead = (rounds - 1) * stride + at.rank * TILE + at.warp * WARP_ROWS;
     ring.lies(0, static_cast<const T*>(a.x) + (s.begin + ahead) * a.ldx + at.slice, a.ldx);
@@ -125,12 +126,15 @@ struct ScanBackward {
       if (at.seg == 0) joins.seg[turn % SETS][at.warp][at.pair] = upto;
       slot -= at.ranks * SCAN_WARPS * SEGS;
       next = round ? kept_state(at, a.states, slot, a.channels) : 0;
-      __syncthreads();
+      if (scan_round(at.ranks > 1, lost)) {
+        lost = true;
+        Rows::drain();
+        break;
+      }
       twa_f2 in;
       if (at.ranks > 1) {
-        if (!share_tile<false>(a, joins, tiles, at, turn, phases, s.len < 0)) {
-          if (s.len >= 0 && threadIdx.x == 0) twa_set_status(a.status, TWA_ERR_TIMEOUT, seq);
-          s.len = -1;                              // nothing more is stored
+        if (!share_tile<false>(a, joins, tiles, at, turn, phases, seq)) {
+          lost = true;                             // nothing more is stored
           rows = 0;
           full = false;
         }
@@ -168,7 +172,7 @@ struct ScanBackward {
       }
       ring.done();
     }
-    if (first_seg && at.rank == 0 && s.len >= 0) at.keep(a.dh0, seq, a.channels, k);
+    if (first_seg && at.rank == 0 && !lost) at.keep(a.dh0, seq, a.channels, k);
   }
 
   // A sequence of at most SEG rows, by one warp: the state before each row is at hand, and rows go by, BRIEF_LOADS under way together.
@@ -224,7 +228,7 @@ int twa_gated_scan_backward(twa_ctx* ctx, const void* dh, int64_t lddh, const vo
   ScanArgs a = {};
   a.dh = dh, a.lddh = lddh, a.x = x, a.ldx = ldx, a.f = f, a.ldf = ldf, a.dx = dx, a.lddx = lddx, a.df = df, a.lddf = lddf;
   a.tokens = tokens, a.channels = channels, a.starts = starts, a.s_type = s_type, a.sequences = sequences;
-  a.states = const_cast<float*>(static_cast<const float*>(states)), a.d_last = d_last, a.dh0 = dh0, a.status = ctx->d_status, a.wait_limit_ns = ctx->wait_limit_ns;
+  a.states = const_cast<float*>(static_cast<const float*>(states)), a.d_last = d_last, a.dh0 = dh0, a.status = ctx->d_status, a.wait_limit_ns = ctx->wait_limit_ns, a.give_up = ctx->tune_scan_give_up;
   int feed = scan_feed(dh, lddh, size, channels, scan_feed(f, ldf, size, channels, scan_feed(x, ldx, size, channels, BY_UNITS)));
   feed = scan_feed(df, lddf, size, channels, scan_feed(dx, lddx, size, channels, feed));
   TWA_CUDA_OK(ctx, scan_launch<ScanBackward>(ctx, a, dtype, feed));

@@ -62,6 +62,7 @@ TWA_TUNE_LIFT_VECTORS = 8
 TWA_TUNE_SLAB_ROWS = 9
 TWA_TUNE_SCAN_CLUSTER = 10
 TWA_TUNE_SCAN_CHANNELS = 11
+TWA_TUNE_SCAN_GIVE_UP = 12
 
 EXPORTS = [
     "twa_create", "twa_destroy", "twa_get_status", "twa_clear_status", "twa_strerror",

@@ -1,0 +1,69 @@
+"""What calls of the sequence model's operators do at their edges: waits that run out, states in place where several blocks share a
+sequence, values at the ends of float32's range, calls without tokens, launches in parts."""
+
+import pytest
+import torch
+
+from paper_2205_13104_b200 import twa
+from test_gpu_sequence_operators import BF16, DEV, F32, FILL, clean, ctx, gen, ok, randn  # noqa: F401 (two fixtures among them)
+
+pytestmark = pytest.mark.gpu
+
+
+def scan_case(g, lengths, channels, dtype, equal=False):
+    """Inputs and a function that runs both directions into outputs of FILL."""
+    q, n = len(lengths), sum(lengths)
+    starts = None if equal else torch.tensor([sum(lengths[:i]) for i in range(q + 1)], device=DEV)
+    x, f, dh = randn(g, n, channels).to(dtype), (2 * randn(g, n, channels) + 2).to(dtype), randn(g, n, channels).to(dtype)
+    h0, d_last = randn(g, q, channels), randn(g, q, channels)
+    states = torch.empty(twa.twa_gated_scan_states_bytes(n, q, channels), dtype=torch.uint8, device=DEV)
+
+    def forward(ctx):
+        h, last = torch.full_like(x, FILL), torch.full_like(h0, FILL)
+        twa.twa_gated_scan(ctx, x, f, h, starts, q, h0, last, states)
+        return h, last
+
+    def backward(ctx):
+        dx, df, dh0 = torch.full_like(x, FILL), torch.full_like(x, FILL), torch.full_like(h0, FILL)
+        twa.twa_gated_scan_backward(ctx, dh, x, f, states, dx, df, starts, q, d_last, dh0)
+        return dx, df, dh0
+
+    return forward, backward
+
+
+@pytest.mark.parametrize("cluster,rank,warp", [(2, 0, 0), (2, 1, 3), (2, 0, 7), (8, 0, 2), (8, 0, 7), (8, 7, 0), (8, 3, 5)])
+@pytest.mark.parametrize("lengths,channels,dtype", [([4200], 64, F32), ([4200, 4200], 40, BF16), ([900, 0, 5000, 1, 2100], 24, F32), ([3000, 17, 4100], 71, BF16)])
+def test_gated_scan_reports_a_wait_that_ran_out_in_any_warp(ctx, lengths, channels, dtype, cluster, rank, warp):
+    """One warp of one block takes its first wait for one that ran out; the others of its block have had the maps.  It has to be
+    reported, and nothing wrong may be stored: an output is right, or was not written."""
+    forward, backward = scan_case(gen(sum(lengths) + channels), lengths, channels, dtype, len(set(lengths)) == 1)
+    twa.twa_set_tuning(ctx, twa.TWA_TUNE_SCAN_CLUSTER, cluster)
+    twa.twa_set_tuning(ctx, twa.TWA_TUNE_SCAN_CHANNELS, 64)
+    try:
+        for call in (forward, backward):
+            want = call(ctx)
+            ok(ctx)
+            twa.twa_set_tuning(ctx, twa.TWA_TUNE_WAIT_LIMIT_MS, 5)
+            twa.twa_set_tuning(ctx, twa.TWA_TUNE_SCAN_GIVE_UP, 1 + 8 * rank + warp)
+            got = call(ctx)
+            code, detail = twa.twa_get_status(ctx)
+            assert code == twa.TWA_ERR_TIMEOUT and lengths[detail] > 0
+            for a, b in zip(got, want):
+                assert bool(((a == b) | (a == FILL)).all())
+            assert not torch.equal(got[0], want[0])                # the warp's own rows at least
+            twa.twa_clear_status(ctx)
+            twa.twa_set_tuning(ctx, twa.TWA_TUNE_SCAN_GIVE_UP, 0)
+            twa.twa_set_tuning(ctx, twa.TWA_TUNE_WAIT_LIMIT_MS, 0)
+            assert all(torch.equal(a, b) for a, b in zip(call(ctx), want))
+            ok(ctx)
+    finally:
+        for key in (twa.TWA_TUNE_SCAN_GIVE_UP, twa.TWA_TUNE_WAIT_LIMIT_MS, twa.TWA_TUNE_SCAN_CLUSTER, twa.TWA_TUNE_SCAN_CHANNELS):
+            twa.twa_set_tuning(ctx, key, 0)
+
+
+def test_the_scan_knob_for_waits_takes_what_it_means(ctx):
+    for value in (1, 64, 0):
+        twa.twa_set_tuning(ctx, twa.TWA_TUNE_SCAN_GIVE_UP, value)
+    for value in (65, -1):
+        with pytest.raises(twa.TwaError):
+            twa.twa_set_tuning(ctx, twa.TWA_TUNE_SCAN_GIVE_UP, value)
