@@ -50,8 +50,8 @@ struct ScanForward {
     const T* first = static_cast<const T*>(all);
     ring.copy(array, from, ld, rows, at.left, first, first + (a.tokens - 1) * ld + a.channels - 1);
   }
-  // A sequence by the whole cluster.
-  __device__ __forceinline__ void whole(const Span& s, int seq, char* shared, Joins<CH / 2, SETS>& joins, Tiles<CH / 2>& tiles, int& turn) {
+  // A sequence by the whole cluster.  True: `state` is the one behind it, which carry() writes.
+  __device__ __forceinline__ bool whole(const Span& s, int seq, char* shared, Joins<CH / 2, SETS>& joins, Tiles<CH / 2>& tiles, int& turn, twa_f2& state) {
     Rows ring(shared, at.warp, at.lane);
     const int stride = TILE * at.ranks;
     unsigned phases = 0;
@@ -76,7 +76,7 @@ struct ScanForward {
     };
 #pragma unroll
     for (int i = 0; i < Rows::AHEAD; ++i) fetch();
-    twa_f2 state = at.state(a.h0, seq, a.channels);
+    state = at.state(a.h0, seq, a.channels);
     if (last_seg) joins.carry[turn ^ 1][at.pair] = state;
     int slot = scan_slot<T>(s, seq) + (at.rank * SCAN_WARPS + at.warp) * SEGS + at.seg;
     for (int t = 0; t < s.len; t += stride, slot += at.ranks * SCAN_WARPS * SEGS, h += stride * a.ldh) {
@@ -144,8 +144,9 @@ struct ScanForward {
       }
       ring.done();
     }
-    if (last_seg && at.rank == 0 && !lost) at.keep(a.h_last, seq, a.channels, state);
+    return last_seg && at.rank == 0 && !lost;
   }
+  __device__ __forceinline__ void carry(int seq, twa_f2 state) const { at.keep(a.h_last, seq, a.channels, state); }
 
   // A sequence of at most SEG rows, by one warp: the state before each row is at hand, and rows go by, BRIEF_LOADS under way together.
   static __device__ __forceinline__ void brief(const ScanArgs& a, const At& at, const Span& s, int seq) {

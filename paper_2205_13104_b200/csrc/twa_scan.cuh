@@ -463,7 +463,8 @@ __device__ __forceinline__ int by_length(const ScanArgs& a, int place, int* shar
 }
 
 // GROUP sequences of a slice of channels a block.  The ones of at most SEG rows go to one warp each, the others to the block, or
-// the cluster.  Offsets on the device are read once and handed on: a block, and a cluster, has one opinion of where its sequences lie.
+// the cluster.  The state that leaves a sequence may lie where the one that enters it does, which every block of a cluster reads: it is
+// written behind the barrier at the end.  Offsets on the device are read once and handed on: a block, and a cluster, has one opinion of where its sequences lie.
 // (Equal lengths are a matter of their own: what follows from them alone stays in uniform registers; 8 x 2048 x 2048 bfloat16 forward
 // 47 us, 53 when they come the same way.)
 template <typename Direction, int GROUP, bool RAGGED>
@@ -483,10 +484,12 @@ __device__ __forceinline__ void scan_block(const ScanArgs& a) {
     }
     twa_cluster_sync();                            // no block stores into one that has not begun
   }
-  int turn = 0;
+  int turn = 0, seq = first;
+  bool leaves = false;
+  twa_f2 state = 0;
   if constexpr (!RAGGED) {
     const Span s = scan_span<false>(a, first, false);
-    d.whole(s, first, shared, joins, tiles, turn);
+    leaves = d.whole(s, first, shared, joins, tiles, turn, state);
   } else {
     __shared__ unsigned long long begins[GROUP], lengths[GROUP];    // lengths: and the sequence's number above them
     if (d.at.rank == 0) {
@@ -517,10 +520,15 @@ __device__ __forceinline__ void scan_block(const ScanArgs& a) {
     }
     for (int g = 0; g < GROUP; ++g) {
       const Span s = span(g);
-      if (s.len > Direction::N || (GROUP == 1 && s.len >= 0)) d.whole(s, number(g), shared, joins, tiles, turn);
+      if (s.len > Direction::N || (GROUP == 1 && s.len >= 0)) {
+        seq = number(g);
+        leaves = d.whole(s, seq, shared, joins, tiles, turn, state);
+        if (GROUP > 1 && leaves) d.carry(seq, state);              // never in a cluster
+      }
     }
   }
   if (a.cluster > 1) twa_cluster_sync();           // none ends while another may still send to it, one whose wait ran out included
+  if (GROUP == 1 && leaves) d.carry(seq, state);
 }
 
 template <typename Direction, int GROUP, bool RAGGED>

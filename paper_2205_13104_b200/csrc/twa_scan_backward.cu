@@ -70,7 +70,8 @@ struct ScanBackward {
     const T* first = static_cast<const T*>(all);
     ring.copy(array, from, ld, rows, at.left, first, first + (a.tokens - 1) * ld + a.channels - 1);
   }
-  __device__ __forceinline__ void whole(const Span& s, int seq, char* shared, Joins<CH / 2, SETS>& joins, Tiles<CH / 2>& tiles, int& turn) {
+  // True: `k` is the one before the sequence, which carry() writes.
+  __device__ __forceinline__ bool whole(const Span& s, int seq, char* shared, Joins<CH / 2, SETS>& joins, Tiles<CH / 2>& tiles, int& turn, twa_f2& k) {
     Rows ring(shared, at.warp, at.lane);
     const int stride = TILE * at.ranks, rounds = (s.len + stride - 1) / stride;
     unsigned phases = 0;
@@ -103,7 +104,7 @@ struct ScanBackward {
     };
 #pragma unroll
     for (int i = 0; i < Rows::AHEAD; ++i) fetch();
-    twa_f2 k = at.state(a.d_last, seq, a.channels);
+    k = at.state(a.d_last, seq, a.channels);
     if (first_seg) joins.carry[turn ^ 1][at.pair] = k;
     for (int round = rounds - 1; round >= 0; --round, dx -= stride * a.lddx, df -= stride * a.lddf) {
       const int first = round * stride + at.rank * TILE + at.warp * WARP_ROWS, mine = first + at.seg * N;
@@ -172,8 +173,9 @@ struct ScanBackward {
       }
       ring.done();
     }
-    if (first_seg && at.rank == 0 && !lost) at.keep(a.dh0, seq, a.channels, k);
+    return first_seg && at.rank == 0 && !lost;
   }
+  __device__ __forceinline__ void carry(int seq, twa_f2 k) const { at.keep(a.dh0, seq, a.channels, k); }
 
   // A sequence of at most SEG rows, by one warp: the state before each row is at hand, and rows go by, BRIEF_LOADS under way together.
   static __device__ __forceinline__ void brief(const ScanArgs& a, const At& at, const Span& s, int seq) {

@@ -67,3 +67,32 @@ def test_the_scan_knob_for_waits_takes_what_it_means(ctx):
     for value in (65, -1):
         with pytest.raises(twa.TwaError):
             twa.twa_set_tuning(ctx, twa.TWA_TUNE_SCAN_GIVE_UP, value)
+
+
+@pytest.mark.parametrize("cluster", [2, 4, 8])
+@pytest.mark.parametrize("lengths", [[300], [90, 0, 255, 1], [70] * 6, [2500, 40], [64, 128]])
+@pytest.mark.parametrize("channels,dtype", [(64, F32), (48, BF16), (33, F32)])
+def test_gated_scan_states_in_place_where_blocks_share_a_sequence(ctx, lengths, channels, dtype, cluster):
+    """Every block of a cluster reads the state that enters, one writes the state that leaves: behind a barrier of all of them, in
+    sequences of a single round too."""
+    g = gen(sum(lengths) * cluster)
+    q, n = len(lengths), sum(lengths)
+    starts = None if len(set(lengths)) == 1 else torch.tensor([sum(lengths[:i]) for i in range(q + 1)], device=DEV)
+    x, f, dh = randn(g, n, channels).to(dtype), (2 * randn(g, n, channels) + 2).to(dtype), randn(g, n, channels).to(dtype)
+    h, dx, df = (torch.empty_like(x) for _ in range(3))
+    states = torch.empty(twa.twa_gated_scan_states_bytes(n, q, channels), dtype=torch.uint8, device=DEV)
+    twa.twa_set_tuning(ctx, twa.TWA_TUNE_SCAN_CLUSTER, cluster)
+    try:
+        for _ in range(20):
+            h0, d_last = randn(g, q, channels), randn(g, q, channels)
+            last, dh0 = torch.empty_like(h0), torch.empty_like(h0)
+            twa.twa_gated_scan(ctx, x, f, h, starts, q, h0, last, states)
+            twa.twa_gated_scan_backward(ctx, dh, x, f, states, dx, df, starts, q, d_last, dh0)
+            want = [t.clone() for t in (h, dx, df)]
+            twa.twa_gated_scan(ctx, x, f, h, starts, q, h0, h0, states)
+            twa.twa_gated_scan_backward(ctx, dh, x, f, states, dx, df, starts, q, d_last, d_last)
+            assert torch.equal(h0, last) and torch.equal(d_last, dh0)
+            assert all(torch.equal(a, b) for a, b in zip((h, dx, df), want))
+    finally:
+        twa.twa_set_tuning(ctx, twa.TWA_TUNE_SCAN_CLUSTER, 0)
+    ok(ctx)
