@@ -55,7 +55,6 @@ struct ScanForward {
     Rows ring(shared, at.warp, at.lane);
     const int stride = TILE * at.ranks;
     unsigned phases = 0;
-    bool lost = false;                             // the maps of a round did not come to this warp, or block
     const bool last_seg = at.warp == SCAN_WARPS - 1 && at.seg == SEGS - 1;
     int ahead = at.rank * TILE + at.warp * WARP_ROWS;                     // row of the warp's next segments to be fetched
     ring.lies(0, static_cast<const T*>(a.x) + (s.begin + ahead) * a.ldx + at.slice, a.ldx);
@@ -99,15 +98,10 @@ struct ScanForward {
       Map before;
       const Map upto = join_segments<true, SEGS>(end, at.seg, before);
       if (at.seg == SEGS - 1) joins.seg[turn][at.warp][at.pair] = upto;
-      if (scan_round(at.ranks > 1, lost)) {
-        lost = true;
-        Rows::drain();
-        break;
-      }
+      __syncthreads();
       twa_f2 in;
       if (at.ranks > 1) {
         if (!share_tile<true>(a, joins, tiles, at, turn, phases, seq)) {
-          lost = true;                             // nothing more is stored
           rows = 0;
           full = false;
         }
@@ -144,7 +138,7 @@ struct ScanForward {
       }
       ring.done();
     }
-    return last_seg && at.rank == 0 && !lost;
+    return !scan_stopped(tiles, at.ranks) && at.rank == 0 && last_seg;
   }
   __device__ __forceinline__ void carry(int seq, twa_f2 state) const { at.keep(a.h_last, seq, a.channels, state); }
 

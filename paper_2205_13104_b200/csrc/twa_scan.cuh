@@ -357,8 +357,6 @@ struct Ring {
     read = read == (STAGES - 1) * BYTES ? 0 : read + BYTES;
     __syncwarp();                                 // other lanes fill this stage again
   }
-  // Waits for every copy under way: none reaches shared memory after a block that goes no further.
-  static __device__ __forceinline__ void drain() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 };
 
 // Affine maps v -> A v + B of two channels.
@@ -399,29 +397,37 @@ struct Joins {
   Map seg[SETS][SCAN_WARPS][PAIRS];
   twa_f2 carry[2][PAIRS];
 };
-// The same of the tiles of a cluster's blocks, and how they arrive.
+// The same of the tiles of a cluster's blocks, and how they arrive.  stop: what a block does in the round after: GO_ON, STOP, or, 1 + w,
+// let its warp w take its wait for one that ran out.
+enum { STOP = -1, GO_ON = 0 };
 template <int PAIRS>
 struct Tiles {
   Map tile[2][MAX_CLUSTER][PAIRS];
   unsigned long long arrived[2];
   int abort_flag;
+  int stop[2];
+  static constexpr unsigned BYTES = PAIRS * sizeof(Map);         // of one block's
 };
 
 // The blocks of a cluster tell each other what their tiles make of a state: every warp joins its block's segments' maps, from the
 // first on (FORWARD) or from the last, and the warp of each rank sends the tile's to that block, whose barrier counts the bytes.
 // (A barrier of the whole cluster instead would also wait until every thread's results are in memory: 1 x 65536 x 512 float32
 // both directions 277 us, so 237.)  Two sets take turns: a block sends into one again only after it has the maps of the
-// round between, which the receiver sends when all its warps have read the first.  False: the maps did not come to this warp in
-// time, which it reports: warps wait each for themselves, and another of the block may have had them just before the limit.
+// round between, which the receiver sends when all its warps have read the first.
+// A barrier is told what to wait for next as soon as it has been waited for, not when that round's maps are due.
+// Warps wait each for themselves.  One to which the maps do not come in time reports it, even where another of its block has had them
+// just before the limit, and tells its block to stop, which from the next round on sends nothing, waits for nothing and stores nothing:
+// its maps would be wrong, and others would take those of later rounds for missing ones.  So every map that arrives is right, and every
+// row that is stored.  False: the maps are not here.
 template <bool FORWARD, int FEED, int CH, int SETS>
 __device__ __forceinline__ bool share_tile(const ScanArgs& a, const Joins<CH / 2, SETS>& joins, Tiles<CH / 2>& tiles, const Place<FEED, CH>& at, int turn,
                                            unsigned& phases, int seq) {
-  if (threadIdx.x == 0) twa_mbar_expect_tx(twa_smem_u32(&tiles.arrived[turn]), at.ranks * (CH / 2) * sizeof(Map));
+  const int stop = tiles.stop[turn ^ 1];           // written before the barrier that the block has passed
   if (at.warp < at.ranks) {
     Map all = joins.seg[turn % SETS][FORWARD ? 0 : SCAN_WARPS - 1][at.pair];
 #pragma unroll
     for (int i = 1; i < SCAN_WARPS; ++i) all = joins.seg[turn % SETS][FORWARD ? i : SCAN_WARPS - 1 - i][at.pair].after(all);
-    if (at.seg == 0) {
+    if (at.seg == 0 && stop != STOP) {
       uint32_t to, bar;
       asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(twa_smem_u32(&tiles.tile[turn][at.rank][at.pair])), "r"(at.warp));
       asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(bar) : "r"(twa_smem_u32(&tiles.arrived[turn])), "r"(at.warp));
@@ -429,21 +435,24 @@ __device__ __forceinline__ bool share_tile(const ScanArgs& a, const Joins<CH / 2
                    : "memory");
     }
   }
-  const bool good = a.give_up != 1 + at.rank * SCAN_WARPS + at.warp &&
-                    twa_wait(&tiles.arrived[turn], phases >> turn & 1, &tiles.abort_flag, a.wait_limit_ns);
+  const bool good = stop != STOP && stop != 1 + at.warp && twa_wait(&tiles.arrived[turn], phases >> turn & 1, &tiles.abort_flag, a.wait_limit_ns);
   phases ^= 1u << turn;
-  if (__all_sync(0xffffffffu, good)) return true;  // a warp goes on as one
-  if (at.lane == 0) twa_set_status(a.status, TWA_ERR_TIMEOUT, seq);
+  if (__all_sync(0xffffffffu, good)) {             // a warp goes on as one
+    if (threadIdx.x == 0) twa_mbar_expect_tx(twa_smem_u32(&tiles.arrived[turn]), at.ranks * Tiles<CH / 2>::BYTES);
+    return true;
+  }
+  if (at.lane == 0) {
+    tiles.stop[turn] = STOP;
+    twa_set_status(a.status, TWA_ERR_TIMEOUT, seq);
+  }
+  __syncwarp();
   return false;
 }
 static_assert(MAX_CLUSTER <= SCAN_WARPS, "a warp for every rank");
-// A round's barrier.  Of a cluster's block it says whether a warp of the block's has lost the maps of the round before: then the block
-// goes no further, as one.  It tells the others nothing more, so that they do not take what it has left for its tiles' maps, nor
-// send into a set that another has not read: every map that a block receives is right, and so is every row that it stores.
-__device__ __forceinline__ bool scan_round(bool cluster, bool lost) {
-  if (cluster) return __syncthreads_or(lost);
-  __syncthreads();
-  return false;
+// Whether a warp's block was told to stop, by the warp itself or, a round ago, by another: what it has of a state is not the sequence's.
+template <int PAIRS>
+__device__ __forceinline__ bool scan_stopped(const Tiles<PAIRS>& tiles, int ranks) {
+  return ranks > 1 && (tiles.stop[0] == STOP || tiles.stop[1] == STOP);
 }
 
 // The sequence that has `place` longer ones before it, of at most SCAN_THREADS; by the whole block, which has `shared` for it.
@@ -480,7 +489,10 @@ __device__ __forceinline__ void scan_block(const ScanArgs& a) {
     if (threadIdx.x == 0) {
       for (int i = 0; i < 2; ++i) twa_mbar_init(twa_smem_u32(&tiles.arrived[i]), 1);
       tiles.abort_flag = 0;
+      tiles.stop[0] = GO_ON;
+      tiles.stop[1] = a.give_up && (a.give_up - 1) / SCAN_WARPS == d.at.rank ? 1 + (a.give_up - 1) % SCAN_WARPS : GO_ON;
       twa_fence_barrier_init();
+      for (int i = 0; i < 2; ++i) twa_mbar_expect_tx(twa_smem_u32(&tiles.arrived[i]), a.cluster * T::BYTES);
     }
     twa_cluster_sync();                            // no block stores into one that has not begun
   }

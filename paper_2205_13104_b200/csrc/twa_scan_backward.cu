@@ -75,7 +75,6 @@ struct ScanBackward {
     Rows ring(shared, at.warp, at.lane);
     const int stride = TILE * at.ranks, rounds = (s.len + stride - 1) / stride;
     unsigned phases = 0;
-    bool lost = false;                             // the maps of a round did not come to this warp, or block
     const bool first_seg = at.warp == 0 && at.seg == 0;
     int ahead = (rounds - 1) * stride + at.rank * TILE + at.warp * WARP_ROWS;
     ring.lies(0, static_cast<const T*>(a.x) + (s.begin + ahead) * a.ldx + at.slice, a.ldx);
@@ -127,15 +126,10 @@ struct ScanBackward {
       if (at.seg == 0) joins.seg[turn % SETS][at.warp][at.pair] = upto;
       slot -= at.ranks * SCAN_WARPS * SEGS;
       next = round ? kept_state(at, a.states, slot, a.channels) : 0;
-      if (scan_round(at.ranks > 1, lost)) {
-        lost = true;
-        Rows::drain();
-        break;
-      }
+      __syncthreads();
       twa_f2 in;
       if (at.ranks > 1) {
         if (!share_tile<false>(a, joins, tiles, at, turn, phases, seq)) {
-          lost = true;                             // nothing more is stored
           rows = 0;
           full = false;
         }
@@ -173,7 +167,7 @@ struct ScanBackward {
       }
       ring.done();
     }
-    return first_seg && at.rank == 0 && !lost;
+    return !scan_stopped(tiles, at.ranks) && at.rank == 0 && first_seg;
   }
   __device__ __forceinline__ void carry(int seq, twa_f2 k) const { at.keep(a.dh0, seq, a.channels, k); }
 
