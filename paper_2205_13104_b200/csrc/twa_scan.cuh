@@ -150,13 +150,17 @@ struct Pair<bf16> {
 };
 
 // -q of two gates; their signs say which form a step takes.  1 + e^|f|: the exponential of a bfloat16 gate may err by some units of
-// float32 and is taken as a power of two at once, that of a float32 gate may not.
-template <typename T>
-__device__ __forceinline__ float scan_exp(float f) {
-  if (sizeof(T) == 4) return expf(fabsf(f));
+// float32 and is taken as a power of two at once, both exponents by one product; that of a float32 gate may not.
+__device__ __forceinline__ float scan_exp2(float v) {
   float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(fabsf(f) * 1.44269504f));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(fabsf(v)));
   return r;
+}
+__device__ __forceinline__ twa_f2 scan_exp(const Pair<float>& f) { return twa_pair(expf(fabsf(f.lo())), expf(fabsf(f.hi()))); }
+__device__ __forceinline__ twa_f2 scan_exp(const Pair<bf16>& f) {
+  float a, b;
+  twa_unpair(twa_mul2(f.both(), twa_pair(1.44269504f)), a, b);
+  return twa_pair(scan_exp2(a), scan_exp2(b));
 }
 __device__ __forceinline__ float scan_reciprocal(float v) {
   float r;
@@ -169,7 +173,7 @@ __device__ __forceinline__ float scan_turn(float s, float f) {
 template <typename T>
 __device__ __forceinline__ twa_f2 scan_gate(const Pair<T>& f) {
   float a, b;
-  twa_unpair(twa_add2(twa_pair(1.0f), twa_pair(scan_exp<T>(f.lo()), scan_exp<T>(f.hi()))), a, b);
+  twa_unpair(twa_add2(twa_pair(1.0f), scan_exp(f)), a, b);
   return twa_pair(scan_turn(scan_reciprocal(a), f.lo()), scan_turn(scan_reciprocal(b), f.hi()));
 }
 __device__ __forceinline__ bool scan_open(float n) { return __float_as_int(n) < 0; }
@@ -182,7 +186,10 @@ __device__ __forceinline__ twa_f2 scan_pick(twa_f2 n, twa_f2 a, twa_f2 b) {
   return twa_pair(scan_open(n0) ? a0 : b0, scan_open(n1) ? a1 : b1);
 }
 __device__ __forceinline__ twa_f2 scan_minus(twa_f2 a, twa_f2 b) { return twa_fma2(b, twa_pair(-1.0f), a); }
-__device__ __forceinline__ twa_f2 scan_step(twa_f2 n, twa_f2 h, twa_f2 x) { return twa_fma2(n, scan_minus(h, x), scan_pick(n, h, x)); }
+// Half of h - x, which twice a gate is multiplied with: two finite values may be further apart than the largest float32.  Halves and
+// doubles have the digits of the whole (but for the last ones of numbers next to the smallest).
+__device__ __forceinline__ twa_f2 scan_half(twa_f2 h, twa_f2 x) { return twa_fma2(h, twa_pair(0.5f), twa_mul2(x, twa_pair(-0.5f))); }
+__device__ __forceinline__ twa_f2 scan_step(twa_f2 n, twa_f2 h, twa_f2 x) { return twa_fma2(twa_add2(n, n), scan_half(h, x), scan_pick(n, h, x)); }
 // a times v: what a step makes of a state where x is 0.
 __device__ __forceinline__ twa_f2 scan_decay(twa_f2 n, twa_f2 v) { return twa_fma2(n, v, scan_pick(n, v, twa_pair(0.0f))); }
 

@@ -28,13 +28,14 @@ struct ScanBackward {
   // A row on the way from the state before the segment's first row to the one behind its last; off: the segment's A and M so far.
   __device__ __forceinline__ void row(int i, const Pair<T>& x, const Pair<T>& f, const Pair<T>& dh, twa_f2& h, Map& off) {
     n[i] = scan_gate<T>(f);
-    const twa_f2 d = scan_minus(h, x.both());
-    h = twa_fma2(n[i], d, scan_pick(n[i], h, x.both()));
+    const twa_f2 d = scan_half(h, x.both()), m = twa_add2(n[i], n[i]);
+    h = twa_fma2(m, d, scan_pick(n[i], h, x.both()));
     off.A = scan_decay(n[i], off.A);
     off.B = twa_fma2(off.A, dh.both(), off.B);
-    float n0, n1;
+    float n0, n1, m0, m1;
     twa_unpair(n[i], n0, n1);
-    e[i] = twa_mul2(twa_pair(fmaf(-n0, n0, fabsf(n0)), fmaf(-n1, n1, fabsf(n1))), d);
+    twa_unpair(m, m0, m1);
+    e[i] = twa_mul2(twa_pair(fmaf(-m0, n0, fabsf(m0)), fmaf(-m1, n1, fabsf(m1))), d);
   }
   // Gradients of a row from g = dh + k, where k is what comes from the rows behind it; k becomes this row's.  With p = n g, k is
   // g + p where the gate is open and p where not, and dx = (1 - a) g is -p or g - p.

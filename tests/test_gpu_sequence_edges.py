@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2205_13104_b200 import twa
-from test_gpu_sequence_operators import BF16, DEV, F32, FILL, clean, ctx, gen, ok, randn  # noqa: F401 (two fixtures among them)
+from test_gpu_sequence_operators import BF16, DEV, F32, FILL, ROUND, clean, close, ctx, gen, ok, randn, scan_64  # noqa: F401 (two fixtures among them)
 
 pytestmark = pytest.mark.gpu
 
@@ -95,4 +95,36 @@ def test_gated_scan_states_in_place_where_blocks_share_a_sequence(ctx, lengths, 
             assert all(torch.equal(a, b) for a, b in zip((h, dx, df), want))
     finally:
         twa.twa_set_tuning(ctx, twa.TWA_TUNE_SCAN_CLUSTER, 0)
+    ok(ctx)
+
+
+@pytest.mark.parametrize("cluster", [0, 2, 8])
+@pytest.mark.parametrize("lengths", [[1], [3, 1, 20, 0, 2], [2] * 9, [700], [129, 400], [1, 2, 1, 1, 3, 1, 1, 1, 1, 40, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1]])
+@pytest.mark.parametrize("channels,dtype", [(64, F32), (71, F32), (64, BF16), (37, BF16), (70, BF16)])
+def test_gated_scan_of_values_further_apart_than_the_largest_float(ctx, lengths, channels, dtype, cluster):
+    """A state lies between its tokens, whatever their difference: 3e38 and -3e38 included."""
+    g = gen(sum(lengths) + channels)
+    q, n = len(lengths), sum(lengths)
+    first = [sum(lengths[:i]) for i in range(q)]
+    starts = None if len(set(lengths)) == 1 else torch.tensor(first + [n], device=DEV)
+    x = ((0.5 + 0.5 * torch.rand((n, channels), generator=g, device=DEV)) * 3e38 * torch.sign(randn(g, n, channels))).to(dtype)
+    f, dh = (3 * randn(g, n, channels)).to(dtype), (0.01 * randn(g, n, channels)).to(dtype)
+    h0, d_last = 3e38 * torch.sign(randn(g, q, channels)), 0.01 * randn(g, q, channels)
+    h, dx, df = (torch.empty_like(x) for _ in range(3))
+    last, dh0 = torch.empty_like(h0), torch.empty_like(h0)
+    states = torch.empty(twa.twa_gated_scan_states_bytes(n, q, channels), dtype=torch.uint8, device=DEV)
+    twa.twa_set_tuning(ctx, twa.TWA_TUNE_SCAN_CLUSTER, cluster)
+    try:
+        twa.twa_gated_scan(ctx, x, f, h, starts, q, h0, last, states)
+        twa.twa_gated_scan_backward(ctx, dh, x, f, states, dx, df, starts, q, d_last, dh0)
+    finally:
+        twa.twa_set_tuning(ctx, twa.TWA_TUNE_SCAN_CLUSTER, 0)
+    scan_64.dtype = dtype
+    want = scan_64(x, f, lengths, first, h0, dh, d_last)
+    for name, got in (("h", h), ("dx", dx), ("df", df)):
+        v, e = want[name]
+        close(got, v, e + ROUND[dtype] * (v.abs() + e) + 1e-37)
+    for name, got in (("h_last", last), ("dh0", dh0)):
+        v, e = want[name]
+        close(got, v, e + 1e-37)
     ok(ctx)
