@@ -511,7 +511,7 @@ int twa_expert_dispatch(twa_ctx* ctx, const void* x, int64_t ldx, twa_dtype dtyp
   if (rc) return rc;
   if (!twa_dtype_ok(dtype) || !twa_itype_ok(id_type) || experts < 1 || dim < 1) return TWA_ERR_INVALID_ARG;
   if (experts > TWA_EXPERTS_MAX || dim > TWA_EXPERTS_MAX_DIM) return TWA_ERR_UNSUPPORTED;
-  if (!starts || (tokens && (!ids || !place)) || !x != !out) return TWA_ERR_INVALID_ARG;
+  if (!starts || (tokens && (!ids || !place || !x != !out))) return TWA_ERR_INVALID_ARG;
   if (x && tokens && (ldx < dim || ldo < dim)) return TWA_ERR_INVALID_ARG;
   const size_t size = twa_dtype_size(dtype);
   if (twa_misaligned_to(starts, 4) || (tokens && (twa_misaligned_to(ids, twa_itype_size(id_type)) || twa_misaligned_to(place, 4) ||

@@ -128,3 +128,27 @@ def test_gated_scan_of_values_further_apart_than_the_largest_float(ctx, lengths,
         v, e = want[name]
         close(got, v, e + 1e-37)
     ok(ctx)
+
+
+@pytest.mark.parametrize("experts", [1, 4, 1000])
+def test_dispatch_of_no_tokens_with_room_for_some(ctx, experts):
+    """A program's buffers stay as large as they are where a batch has no token: an empty tensor has no address, its buffers have one."""
+    none, x = torch.empty((0, 2), dtype=torch.int64, device=DEV), torch.empty((0, 8), device=DEV)
+    place, starts = torch.empty((0, 2), dtype=torch.int32, device=DEV), torch.full((experts + 1,), 9, dtype=torch.int32, device=DEV)
+    out = torch.full((6, 8), FILL, device=DEV)
+    twa.twa_expert_dispatch(ctx, x, none, experts, place, starts, out)
+    assert bool((starts == 0).all()) and bool((out == FILL).all())
+    back, h = torch.empty_like(x), torch.empty_like(x)
+    twa.twa_expert_combine(ctx, out, place, None, back)
+    twa.twa_expert_combine_backward(ctx, x, out, place, torch.empty((0, 2), device=DEV), out)
+    twa.twa_dropout(ctx, x, 0.5, torch.tensor([1, 2], device=DEV), 0, h)
+    h0, last = torch.ones(3, 8, device=DEV), torch.zeros(3, 8, device=DEV)
+    states = torch.empty(1024, dtype=torch.uint8, device=DEV)
+    for starts in (None, torch.zeros(4, dtype=torch.int64, device=DEV)):
+        twa.twa_gated_scan(ctx, x, x, h, starts, 3, h0, last, states)
+        assert torch.equal(last, h0)
+        twa.twa_gated_scan_backward(ctx, x, x, x, states, h, back, starts, 3, h0, last.zero_())
+        assert torch.equal(last, h0)
+        last.zero_()
+    assert bool((out == FILL).all())
+    ok(ctx)
