@@ -5,6 +5,7 @@ import pytest
 import torch
 
 from paper_2205_13104_b200 import twa
+from philox import dropout_numbers
 from test_gpu_sequence_operators import BF16, DEV, F32, FILL, ROUND, clean, close, ctx, gen, ok, randn, scan_64  # noqa: F401 (two fixtures among them)
 
 pytestmark = pytest.mark.gpu
@@ -151,4 +152,67 @@ def test_dispatch_of_no_tokens_with_room_for_some(ctx, experts):
         assert torch.equal(last, h0)
         last.zero_()
     assert bool((out == FILL).all())
+    ok(ctx)
+
+
+@pytest.mark.parametrize("shared", [("one block", 1, 64), ("clusters", 2, 64), ("clusters", 8, 16), ("by length", 0, 2560)], ids=lambda v: f"{v[0]}-{v[1]}")
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("wrong", [(0, -1), (3, 2000), (10, 1 << 40), (9, 1001)])
+def test_gated_scan_leaves_wrong_sequences_alone_however_they_are_shared(ctx, shared, dtype, wrong):
+    """Offsets outside the tokens where one block's opinion of them goes to others, or they are ranked by their length: sequences on
+    both sides of a wrong offset are reported and left alone, the others give the bits that they give among right ones."""
+    way, cluster, channels = shared
+    n, edges = 1000, [0, 37, 300, 301, 301, 450, 600, 700, 790, 800, 1000]
+    if way == "by length":                                        # more blocks than begin at once, fewer than twice as many
+        blocks = (len(edges) - 1) * channels // 64
+        sms = torch.cuda.get_device_properties(0).multi_processor_count
+        assert 2 * sms < blocks <= 4 * sms
+    at, value = wrong
+    bad = [s for s in (at - 1, at) if 0 <= s < len(edges) - 1]
+    q, g = len(edges) - 1, gen(channels + at)
+    x, f, dh = randn(g, n, channels).to(dtype), (2 * randn(g, n, channels) + 2).to(dtype), randn(g, n, channels).to(dtype)
+    h0, d_last = randn(g, q, channels), randn(g, q, channels)
+    twa.twa_set_tuning(ctx, twa.TWA_TUNE_SCAN_CLUSTER, cluster)
+    twa.twa_set_tuning(ctx, twa.TWA_TUNE_SCAN_CHANNELS, channels if cluster else 0)
+    states = torch.empty(twa.twa_gated_scan_states_bytes(n, q, channels), dtype=torch.uint8, device=DEV)
+
+    def run(edges, back):
+        starts = torch.tensor(edges, device=DEV)
+        out = [torch.full_like(x, FILL) for _ in range(2)] + [torch.full_like(h0, FILL)]
+        if back:
+            twa.twa_gated_scan_backward(ctx, dh, x, f, states, out[0], out[1], starts, q, d_last, out[2])
+        else:
+            twa.twa_gated_scan(ctx, x, f, out[0], starts, q, h0, out[2], states)
+        return out
+
+    try:
+        for back in (False, True):
+            want = run(edges, back)
+            ok(ctx)
+            got = run(edges[:at] + [value] + edges[at + 1:], back)
+            code, detail = twa.twa_get_status(ctx)
+            assert code == twa.TWA_ERR_INVALID_ARG and detail in bad
+            twa.twa_clear_status(ctx)
+            for s in bad:
+                for t in want[:2]:
+                    t[edges[s]: edges[s + 1]] = FILL
+                want[2][s] = FILL
+            assert all(torch.equal(a, b) for a, b in zip(got, want))
+            if not back:
+                run(edges, back)                                   # the states of all sequences, for the way back
+    finally:
+        twa.twa_set_tuning(ctx, twa.TWA_TUNE_SCAN_CLUSTER, 0)
+        twa.twa_set_tuning(ctx, twa.TWA_TUNE_SCAN_CHANNELS, 0)
+
+
+def test_dropout_in_more_than_one_launch(ctx):
+    """A launch counts its work in 31 bits; rows beyond that go in another, with the numbers of their own places."""
+    rows, cols = twa.TWA_DROPOUT_MAX_ROWS, 16
+    if torch.cuda.mem_get_info()[0] < 48 << 30:
+        pytest.skip("needs 48 GB of device memory")
+    x = torch.ones((rows, cols), dtype=BF16, device=DEV)
+    twa.twa_dropout(ctx, x, 0.5, torch.tensor([5, 6], device=DEV), 7, x)
+    for first, count in ((0, 8), (rows // 2 - 4, 8), (rows - 1000, 1000)):        # the second launch begins some hundred rows before the end
+        kept = torch.from_numpy(dropout_numbers(5, 6, 7, count, cols, first) >= 32768).to(DEV)
+        assert torch.equal(x[first: first + count], torch.where(kept, 2.0, 0.0).to(BF16))
     ok(ctx)
