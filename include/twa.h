@@ -626,6 +626,7 @@ int twa_dropout_backward(twa_ctx* ctx, const void* dy, int64_t lddy, twa_dtype d
 
 /* Gated linear recurrence along every sequence, every channel alone:
  *   a_t = sigmoid(f_t),   h_t = a_t h_{t-1} + (1 - a_t) x_t
+ * sequences * ceil(channels / 16) is at most 2^28 - 1 (TWA_ERR_UNSUPPORTED).
  *  x, f, h   tokens x channels of dtype; h may be x or f (same row stride).
  *  starts    sequences + 1 numbers of s_type on the device: sequence s has the rows starts[s] .. starts[s+1]-1 (an
  *            empty one: none; rows in no sequence are left as they were).  NULL: all of tokens / sequences rows.

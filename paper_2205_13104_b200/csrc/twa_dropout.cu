@@ -7,11 +7,13 @@
 // go up by constants from round to round.  The counter is (column / 8, row, site, step), the key the seed: a call's 128 bits
 // are the numbers of 8 neighbouring columns, and the backward pass draws them again from the same place.
 //
-// Bound by memory with a residual: 32768 x 2048 bfloat16 59 us (403 MB, 6.8 TB/s); without one 47 us (268 MB, 5.7 TB/s), where the
-// generator's products count: some 60 instructions a call of it, the key's additions shared by a thread's two calls (53 us apart).
+// Bound by memory with a residual: 32768 x 2048 bfloat16 59 us in a row of calls (403 MB, 6.9 TB/s: two thirds are loads, which are
+// faster than the halves of a copy; a single call leaves some 50 MB of its stores in L2 and moves 357 MB at 6.5 TB/s, 80 % of DRAM's
+// peak); without one 43 us (268 MB, 6.3 TB/s), where the generator's products count: some 60 instructions a call of it, the key's
+// additions shared by a thread's two calls (47 us for a single call, 53 when they are apart).
 // 16 bits an element halve it against 32; a probability is then a multiple of 2^-16, and the scale is that of the multiple.
-// Rows between 16-byte boundaries go by the element and find their bit in another lane: 32768 x 2047 bfloat16 93 us with a residual,
-// 73 without, bound by instructions (two elements an access, where rows lie alike between words: 88 and 88).
+// Rows between 16-byte boundaries go by the element and find their bit in another lane: 32768 x 2047 bfloat16 84 us with a residual,
+// 67 without (a single call 93 and 73), bound by instructions (two elements an access, where rows lie alike between words: 88 and 88).
 #include "twa_ops.cuh"
 
 namespace {

@@ -15,8 +15,10 @@
 // 32768 x 2048 bfloat16, 8 of 128 experts: 215 us (1.21 GB, floor 187), of which the sort of 262144 assignments takes 28 on 16 SMs
 // (128 warps of 8 blocks, finding each other by a match, which serves one expert after another: 104).  More SMs would need counts in
 // memory, and a workspace for them.  Combine 16384 x 1024, two experts: 19 us (100 MB, some of it in L2).  Combine backward
-// 16384 x 2048, 8 experts of 64: 191 us (1.14 GB, 6.0 TB/s); rows between 16-byte boundaries, 17489 x 1032, 172 us (floor 95):
-// two bytes an access.
+// 16384 x 2048, 8 experts of 64: 191 us (1.14 GB, 6.0 TB/s).  Rows between 16-byte boundaries go by the word or the element: 17489 x 1032,
+// 8 experts, forward 56 us in units, 61 by words, 82 by elements (floor 51), backward 112, 131 and 170 (floor 95); 16384 x 1024, two
+// experts, 17.7, 17.9 and 26.7 (15.6), backward 28.9, 31.3 and 42.2 (26.0).
+// Figures beside the rules below are of calls in a row, whose data L2 holds where it fits, bfloat16 unless they say otherwise.
 #include "twa_ops.cuh"
 
 namespace {
@@ -211,8 +213,9 @@ __global__ void __launch_bounds__(MOVE_WARPS * 32) expert_gather_kernel(Rows r, 
   move_row<W, UNITS, LANES>(r, t, part, [&](int j) { return __ldg(places + j); });
 }
 
-// Few assignments: every block sorts them, block 0 says so, and each moves its share of the rows.  A launch after a launch would cost
-// as much again (16 tokens of 512 bfloat16, two of eight experts).
+// Few assignments: every block sorts them, block 0 says so, and each moves its share of the rows, in one launch.  It and two launches:
+// 8 x 512, two of 8 experts, 3.4 and 5.2 us; 512 x 1024, two of 16, 5.4 and 6.3; 1024 x 1024 7.7 and 7.0, 2048 x 1024 13.5 and 7.6;
+// 128 x 2048, 8 of 128, 7.2 and 8.1; 256 x 2048 9.5 and 8.8.
 constexpr int SMALL_COUNT = 1024;                 // assignments
 template <typename W, int UNITS>
 __global__ void __launch_bounds__(MOVE_WARPS * 32) expert_small_kernel(SortArgs a, Rows r) {
@@ -389,7 +392,8 @@ __global__ void __launch_bounds__(MOVE_WARPS * 32) expert_combine_backward_kerne
 
 bool on_unit(const void* p, long long ld_bytes, size_t unit) { return !twa_misaligned_to(p, unit) && ld_bytes % unit == 0; }
 
-// Moves rows as units of W, after the sort or (small) with it.
+// Moves rows as units of W, after the sort or (small) with it.  Rows that few threads hold go to as many, not to a warp: 16384 tokens to
+// two experts, 64 columns 8.5 us (10.8 by warps), 128 9.2 (10.8), 256 10.4 (11.0); by words and elements 10.0 to 10.5 either way.
 template <typename W, int UNITS>
 cudaError_t launch_gather(twa_ctx* ctx, const SortArgs& s, Rows r, long long bytes, bool small) {
   r.units = static_cast<int>(bytes / sizeof(W));
@@ -446,7 +450,11 @@ void launch_combine(twa_ctx* ctx, CombineArgs& a) {
   twa_launch(ctx->stream, expert_combine_kernel<T, E, UNITS, JOIN, LANES>,
              static_cast<unsigned>(twa_ceil_div(a.tokens * a.parts, MOVE_WARPS * 32 / LANES)), MOVE_WARPS * 32, 0, a);
 }
-// As much of a row a thread as keeps some eight loads of it under way, but where there are few rows more threads a row.
+// As much of a row a thread as keeps some eight loads of it under way, but where there are few rows more threads a row: 512 x 1024, two
+// experts, 2.2 us (2.8 otherwise), 1024 x 1024 2.6 (2.9), 2048 x 1024 3.9 (3.4); 8 experts 3.2 (3.4), 4.0 (3.9) and 6.5 (5.5); by elements
+// 140 x 1023, 8 experts, 2.9 (3.4), 512 x 1023, two, 3.0 (2.4).  Narrow rows for a few threads each: 16384 tokens of 64 columns 3.5 us
+// (9.7 by warps), of 128 4.0 (9.8); wider ones up to 256 columns would gain too (5.6 and 9.8).  Loads of two experts at a time, or of four and half the columns:
+// 16384 x 1024, one expert 10.8 and 11.6, two 17.5 and 18.9, three 25.7 and 23.4, 8 50.7 and 46.8.
 template <typename T, int E>
 void launch_combine(twa_ctx* ctx, CombineArgs& a) {
   const bool few = a.tokens * twa_ceil_div(a.dim, 32 * E) < 32LL * ctx->sm_count;
@@ -467,6 +475,12 @@ void launch_combine_backward(twa_ctx* ctx, const CombineArgs& a) {
   twa_launch(ctx->stream, expert_combine_backward_kernel<T, E, UNITS, JOIN, LANES>,
              static_cast<unsigned>(twa_ceil_div(a.tokens, MOVE_WARPS * 32 / LANES)), MOVE_WARPS * 32, 0, a);
 }
+// Narrow rows for a few threads each: 16384 tokens to two experts, 64 columns 4.2 us (9.5 by warps), 256 6.9 (9.8), and
+// wider ones would too (512: 12.9 and 14.1).  A block a token
+// where there are few, a warp otherwise: 256 x 1024, two experts, 2.4 us a block and 2.8 a warp, 512 x 4096 4.1 and 6.0; 8 experts,
+// 1024 x 2048 10.0 and 12.6, 2048 x 4096 48 and 57; where tokens are some ten an SM and rows short a warp would do better (two experts,
+// 1024 x 1024 4.3 and 3.0, 2048 x 1024 7.0 and 3.9; 8 experts, 2048 x 1024 14.0 and 10.4).  Experts at a time by warps, two with four
+// packs a thread or four with one: 16384 x 1024, one expert 17.5 and 21.2, two 28.9 and 30.9, three 39.7 and 39.7, 8 of 2048 columns 188 and 192.
 template <typename T, int E>
 void launch_combine_backward(twa_ctx* ctx, CombineArgs& a) {
   constexpr bool WIDE = E == twa_vec<T>;
@@ -526,6 +540,7 @@ int twa_expert_dispatch(twa_ctx* ctx, const void* x, int64_t ldx, twa_dtype dtyp
     const size_t smem = sizeof(int) * (s.warps + 3) * experts;
     int blocks = 1, most;
     TWA_CUDA_OK(ctx, sort_cluster(ctx, &most));
+    // as soon as warps have more than 32 assignments each (4096 x 2 of 16 experts 5.1 us, 5.8 where they have 64 first, 7.5 where 128)
     while (blocks < most && s.count > blocks * s.warps * 32) blocks *= 2;
     s.run = static_cast<int>(twa_ceil_div(twa_ceil_div(s.count, blocks * s.warps), 32) * 32);
     SortArgs first = s;

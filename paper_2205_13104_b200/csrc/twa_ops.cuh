@@ -42,8 +42,8 @@ __device__ __forceinline__ long long twa_load_id(const void* p, int itype, long 
   return itype == TWA_I64 ? __ldg(static_cast<const long long*>(p) + i) : static_cast<long long>(__ldg(static_cast<const int*>(p) + i));
 }
 
-// E consecutive elements as they lie in memory: E = 1, or 16 bytes (E = 4 float, 8 bfloat16; the address on 16
-// bytes).  from() packs values of the type, as widen() gave them.  Loading and widening are apart so that the loads of the next row can be under way while this one is worked on.
+// E consecutive elements as they lie in memory: E = 1, a 4-byte word (2 bfloat16; the address on 4 bytes) or 16 bytes (4 float, 8
+// bfloat16; the address on 16 bytes).  from() packs values of the type, as widen() gave them.  Loading and widening are apart so that the loads of the next row can be under way while this one is worked on.
 template <typename T, int E>
 struct twa_pack;
 template <>

@@ -16,12 +16,14 @@
 // One pass over x and f (and dh), which come through a ring of asynchronous copies, and one store.  Blocks differ in sequence and
 // slice; where those are few a cluster of blocks takes a sequence together, a tile each a round, and tells each other what the tiles
 // make of a state.  Everything is joined in a fixed order: results repeat bit for bit.
-// With blocks enough the bound is memory: 2 x 8192 x 9472 bfloat16 forward, 296 equal blocks, 170 us for 931 MB (5.5 TB/s).
-// 8 x 2048 x 2048 gives 256 blocks for the 296 places: 47 us forward (201 MB) and 69 backward (335 MB), some SMs with one block.
-// Where a round's latency counts: 1 x 65536 x 512 float32 98 and 138 us (floors 62 and 104).
+// With equal blocks in every place the bound is memory: 2 x 8192 x 9472 bfloat16 forward, 296 of them, 153 us for 931 MB (6.1 TB/s).
+// 8 x 2048 x 2048 bfloat16: 42 us forward (201 MB, floor 31) and 61 backward (335 MB, 52).  256 blocks for 296 places are a factor of
+// 1.16; the rest is latency: DRAM at 45 and 57 % of its peak and issue slots at 55 and 59 %, while two blocks of 8 warps an SM, 128
+// registers each, are all there is to hide the copies' wait, the steps that follow one another, the barrier and the joins.
+// Where a round's latency counts: 1 x 65536 x 512 float32 99 and 139 us (floors 62 and 104).  (Calls in a row, inputs from DRAM.)
 // A lane's rows are as many as its registers hold between the two passes over them (their A and L): 8 rows of bfloat16 a lane and three
-// blocks an SM instead of 16 and two took 55 and 86 us for 47 and 68, as the joins are paid once a tile; slices of 56 channels, which
-// give 296 blocks, 55 and 82, as rows of 112 bytes share sectors.  Plain instead of packed arithmetic costs 24 instead of 21
+// blocks an SM instead of 16 and two took 55 and 86 us for 47 and 68 (single calls), as the joins are paid once a tile; slices of 56 channels, which
+// give 296 blocks, 55 and 82, as rows of 112 bytes share sectors.  Plain instead of packed arithmetic cost 24 instead of 21
 // instructions an element forward and the same time.
 #pragma once
 
