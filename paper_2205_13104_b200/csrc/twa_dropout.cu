@@ -8,7 +8,7 @@
 // are the numbers of 8 neighbouring columns, and the backward pass draws them again from the same place.
 //
 // Bound by memory with a residual: 32768 x 2048 bfloat16 59 us in a row of calls (403 MB, 6.9 TB/s: two thirds are loads, which are
-// faster than the halves of a copy; a single call leaves some 50 MB of its stores in L2 and moves 357 MB at 6.5 TB/s, 80 % of DRAM's
+// faster than the halves of a copy; a single call leaves some 50 MB of its stores in L2 and moves 351 MB at 6.4 TB/s, 80 % of DRAM's
 // peak); without one 43 us (268 MB, 6.3 TB/s), where the generator's products count: some 60 instructions a call of it, the key's
 // additions shared by a thread's two calls (47 us for a single call, 53 when they are apart).
 // 16 bits an element halve it against 32; a probability is then a multiple of 2^-16, and the scale is that of the multiple.
